@@ -262,6 +262,169 @@ acid_status acid_layernorm_mod(int32_t x_dtype, const void* x, int32_t y_dtype, 
                                float eps, acid_stream_t stream);
 
 /* ------------------------------------------------------------------------ */
+/* Norm sites: the gate, residual, norms and modulation between two branches */
+/* ------------------------------------------------------------------------ */
+
+typedef enum {
+  ACID_NORM_NONE = 0,        /* N(v) = v */
+  ACID_NORM_RMS = 1,         /* N(v) = v / sqrt(mean v^2 + eps) */
+  ACID_NORM_LAYER = 2        /* N(v) = (v - mean v) / sqrt(var v + eps) */
+} acid_norm_kind;
+
+/* A site lies between a branch (attention or MLP) and the next one.  It norms
+ * the branch's output y (sandwich norm), gates it, adds it to the scaled
+ * residual stream x, and norms and modulates the sum for the next branch.  With
+ * b the modulation group of a row:
+ *     r = res_scale x + branch_scale g_b * (N_post(y) * post_w)
+ *     u = N_pre(r) * pre_w * (1 + scale_b) + shift_b,    g_b = gate_b or tanh(gate_b)
+ * in fp32; r and u are each rounded once, u from the unrounded r.  The paper
+ * has no counterpart: its models are named, their blocks are not given, and
+ * models of the same kind norm a branch on both sides or modulate each latent
+ * frame by its own timestep.
+ * Modulation groups: rows [0, first_rows) are group 0 (the text rows of a
+ * joint sequence; none if first_rows is 0); each group_rows rows after them
+ * are a group (one latent frame, one sample; 1: every row its own), the last
+ * may be shorter; group_rows 0: all rows after them are one group. */
+typedef struct {
+  int64_t rows;              /* >= 0 */
+  int32_t d;                 /* row width, a multiple of 8, 8 .. 4096 */
+  int32_t stream_dtype;      /* acid_dtype of x, r and their gradients */
+  int32_t branch_dtype;      /* acid_dtype of y, u and their gradients */
+  int32_t post_norm;         /* acid_norm_kind of the branch's output */
+  int32_t pre_norm;          /* acid_norm_kind of the next branch's input */
+  int32_t gate_tanh;         /* 1: the gate is tanh(gate) */
+  float eps, res_scale, branch_scale;
+  int64_t first_rows, group_rows;
+  const float* gate;         /* device fp32 [groups, d], row stride ld_mod; NULL: 1 */
+  const float* scale;        /* the same; NULL: 0 */
+  const float* shift;        /* the same; NULL: 0 */
+  int64_t ld_mod;            /* elements, a multiple of 4, >= d (ignored for one group) */
+  const float* post_w;       /* device fp32 [d] or NULL (1) */
+  const float* pre_w;        /* device fp32 [d] or NULL (1) */
+} acid_norm_site;
+
+/* Number of modulation groups of a site. */
+acid_status acid_norm_site_groups(const acid_norm_site* site, int64_t* groups);
+
+/* r and u of a site, in one pass over its rows.
+ *   x, y   device [rows, d], row strides ldx, ldy (elements).  y may be NULL:
+ *          no branch, r = res_scale x (the norm in front of the first one);
+ *          the gate and post_w are then not read.
+ *   r, u   device [rows, d], row strides ldr, ldu; either may be NULL (not
+ *          written), not both.  r may be x and u may be y (same strides and
+ *          type); no other overlap.
+ * Matrices and vectors are 16-byte aligned, row strides multiples of 8.
+ * rows = 0 returns ACID_OK without a launch. */
+acid_status acid_norm_site_forward(const acid_norm_site* site, const void* x, int64_t ldx, const void* y,
+                                   int64_t ldy, void* r, int64_t ldr, void* u, int64_t ldu,
+                                   acid_stream_t stream);
+
+/* Gradients that acid_norm_site_backward writes; NULL ones are left out. */
+typedef struct {
+  void* dx; int64_t lddx;    /* device [rows, d], stream dtype */
+  void* dy; int64_t lddy;    /* device [rows, d], branch dtype */
+  float* dgate;              /* device fp32 [groups, d], row stride ld_dmod */
+  float* dscale;             /* the same */
+  float* dshift;             /* the same */
+  int64_t ld_dmod;           /* elements, a multiple of 4, >= d (ignored for one group) */
+  float* dpost_w;            /* device fp32 [d] */
+  float* dpre_w;             /* device fp32 [d] */
+} acid_norm_site_grads;
+
+/* Bytes of device workspace acid_norm_site_backward needs. */
+acid_status acid_norm_site_workspace_size(const acid_norm_site* site, size_t* bytes);
+
+/* Gradients of a site from those of its outputs.  Both norms' statistics are
+ * formed again from r (the forward call's output) and y (its input), so that
+ * nothing else is kept from the forward call.
+ *   du     device [rows, d], branch dtype: the gradient of u, or NULL (u was
+ *          not formed: dscale, dshift and dpre_w must be NULL).
+ *   r      device [rows, d], stream dtype; may be NULL if du is.
+ *   y      device [rows, d], branch dtype, or NULL as in the forward call (dy,
+ *          dgate and dpost_w must be NULL).
+ *   dr     device [rows, d], stream dtype: the gradient that reaches r by the
+ *          residual stream, or NULL (0).  du and dr may not both be NULL.
+ * dx may be dr; dy may be du or y (same strides).  Sums over rows are formed
+ * in fp32 in an order that depends on the sizes and the device alone, so that
+ * the same call gives the same bits.  workspace: device, 16-byte aligned. */
+acid_status acid_norm_site_backward(const acid_norm_site* site, const void* du, int64_t lddu, const void* r,
+                                    int64_t ldr, const void* y, int64_t ldy, const void* dr, int64_t lddr,
+                                    const acid_norm_site_grads* grads, void* workspace, size_t workspace_bytes,
+                                    acid_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Modulation projections with 4-bit weights                                 */
+/* ------------------------------------------------------------------------ */
+
+/* A weight W[N, K] held in 4 bits: W[n, k] = s (q - z), with a 4-bit code q for
+ * each element and a scale s and zero point z for each `group` columns of a
+ * row (the last group of a row may be shorter).
+ *   packed  device [N, acid_q4_row_bytes(K)], 16-byte aligned.  Each 128
+ *           columns of a row are 64 bytes, 16 little-endian 32-bit words; word
+ *           4 t + i (t, i = 0 .. 3) holds columns 32 i + 8 t .. 32 i + 8 t + 7
+ *           of the 128, column j of the eight in bits 4 j .. 4 j + 3.  Codes
+ *           past the last column are not used.
+ *   scales  device [N, ceil(K / group)] of scale_dtype (finite).
+ *   zeros   device uint8 [N, ceil(K / group)], each 0 .. 15, or NULL: z = 8. */
+typedef struct {
+  const void* packed;
+  const void* scales;
+  const uint8_t* zeros;
+  int64_t n;                 /* N, 1 .. 2^31 - 1 */
+  int32_t k;                 /* K, 1 .. 65536 */
+  int32_t group;             /* 32, 64 or 128 */
+  int32_t scale_dtype;       /* acid_dtype */
+} acid_q4_weight;
+
+/* Bytes of one row of packed codes: 64 ceil(K / 128). */
+acid_status acid_q4_row_bytes(int32_t k, size_t* bytes);
+
+/* Quantises W [N, K] (row stride ldw, w_dtype) into a weight's packed codes,
+ * scales and, if zeros is not NULL, zero points.  Over each group, in fp32:
+ *   without zero points  s = max|w| / 7,                      q = clamp(rint(w / s), -8, 7) + 8
+ *   with zero points     s = (max(w, 0) - min(w, 0)) / 15,
+ *                        z = clamp(rint(-min(w, 0) / s), 0, 15), q = clamp(rint(w / s) + z, 0, 15)
+ * where s is rounded to scale_dtype before it divides and rint takes ties to
+ * the even code.  A group whose s is 0 has the codes of 0 (q = z).  W is
+ * expected to be finite: a group with an infinity or a NaN gets a scale that
+ * is not finite.  The weight's pointers are written through here. */
+acid_status acid_q4_quantize(int32_t w_dtype, const void* W, int64_t ldw, const acid_q4_weight* weight,
+                             acid_stream_t stream);
+
+/* out[N, K] (row stride ldo, out_dtype) = the values s (q - z), formed in fp32. */
+acid_status acid_q4_dequantize(const acid_q4_weight* weight, int32_t out_dtype, void* out, int64_t ldo,
+                               acid_stream_t stream);
+
+/* out[M, N] = a(x[M, K]) W^T + bias for a few rows (timestep embeddings of the
+ * branches, frames or steps), a = identity, or SiLU if silu_input.  Sums in fp32;
+ * an fp32 a(x) enters the products to within 2^-22 of its row's largest value.
+ *   x      device [M, K], row stride ldx, x_dtype.
+ *   bias   device fp32 [N] or NULL.
+ *   out    device [M, N], row stride ldo, out_dtype.
+ * 0 <= M <= 32768 (0 returns ACID_OK without a launch); past 64 rows the weight
+ * is read once for each 64. */
+acid_status acid_q4_linear_forward(int32_t x_dtype, const void* x, int64_t ldx, int64_t M,
+                                   const acid_q4_weight* weight, const float* bias, int32_t silu_input,
+                                   int32_t out_dtype, void* out, int64_t ldo, acid_stream_t stream);
+
+/* Bytes of device workspace acid_q4_linear_backward needs for M rows. */
+acid_status acid_q4_linear_workspace_size(const acid_q4_weight* weight, int64_t M, size_t* bytes);
+
+/* Gradients of acid_q4_linear_forward for a frozen weight:
+ *   dx[M, K] = a'(x) * (g W),  dbias[N] = sum over the M rows of g.
+ *   g      device [M, N], row stride ldg, g_dtype: the gradient of out.
+ *   x      device [M, K], row stride ldx, x_dtype: the forward call's input;
+ *          may be NULL without silu_input.
+ *   dx     device [M, K], row stride lddx, x_dtype, or NULL.
+ *   dbias  device fp32 [N], or NULL.  Not both NULL.
+ * Deterministic, as acid_norm_site_backward.  workspace: device, 16-byte
+ * aligned.  M = 0 writes zeros to dbias. */
+acid_status acid_q4_linear_backward(int32_t g_dtype, const void* g, int64_t ldg, int64_t M,
+                                    const acid_q4_weight* weight, int32_t x_dtype, const void* x, int64_t ldx,
+                                    int32_t silu_input, void* dx, int64_t lddx, float* dbias, void* workspace,
+                                    size_t workspace_bytes, acid_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
 /* DiT block forward: the denoiser f_theta the method skips (Sec. 3.1, Eq. 2;  */
 /* Algorithm 1 runs it on computed steps).  The paper names the models         */
 /* (Sec. 4.1) but not their blocks; the block definitions follow the          */

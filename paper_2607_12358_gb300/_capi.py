@@ -20,6 +20,8 @@ ACID_BLOCK_WAN, ACID_BLOCK_COG, ACID_BLOCK_HV_DUAL, ACID_BLOCK_HV_SINGLE = range
 ACID_METHOD_TEACACHE, ACID_METHOD_EASYCACHE, ACID_METHOD_DICACHE = 0, 1, 2
 ACID_EPI_BIAS, ACID_EPI_GELU, ACID_EPI_GATED_RES, ACID_EPI_RES = 0, 1, 3, 4
 
+ACID_NORM_NONE, ACID_NORM_RMS, ACID_NORM_LAYER = 0, 1, 2
+
 STATUS_NAMES = {0: "ACID_OK", 1: "ACID_ERR_INVALID_ARG", 2: "ACID_ERR_UNSUPPORTED", 3: "ACID_ERR_WORKSPACE",
                 4: "ACID_ERR_CUDA", 5: "ACID_ERR_TIMEOUT"}
 
@@ -75,6 +77,27 @@ class acid_loop_state(C.Structure):
 
 
 _P = C.c_void_p
+
+
+class acid_norm_site(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("d", C.c_int32), ("stream_dtype", C.c_int32), ("branch_dtype", C.c_int32),
+                ("post_norm", C.c_int32), ("pre_norm", C.c_int32), ("gate_tanh", C.c_int32), ("eps", C.c_float),
+                ("res_scale", C.c_float), ("branch_scale", C.c_float), ("first_rows", C.c_int64),
+                ("group_rows", C.c_int64), ("gate", _P), ("scale", _P), ("shift", _P), ("ld_mod", C.c_int64),
+                ("post_w", _P), ("pre_w", _P)]
+
+
+class acid_norm_site_grads(C.Structure):
+    _fields_ = [("dx", _P), ("lddx", C.c_int64), ("dy", _P), ("lddy", C.c_int64), ("dgate", _P), ("dscale", _P),
+                ("dshift", _P), ("ld_dmod", C.c_int64), ("dpost_w", _P), ("dpre_w", _P)]
+
+
+class acid_q4_weight(C.Structure):
+    _fields_ = [("packed", _P), ("scales", _P), ("zeros", _P), ("n", C.c_int64), ("k", C.c_int32),
+                ("group", C.c_int32), ("scale_dtype", C.c_int32)]
+
+
+_SITE, _GRADS, _Q4 = C.POINTER(acid_norm_site), C.POINTER(acid_norm_site_grads), C.POINTER(acid_q4_weight)
 _PROTOS = {
     "acid_last_error": (C.c_char_p, []),
     "acid_version": (C.c_char_p, []),
@@ -99,6 +122,19 @@ _PROTOS = {
                                          C.c_int64, C.c_int64, C.c_int32, C.c_int32, _P, C.c_size_t, _P]),
     "acid_attention_workspace_size": (C.c_int, [C.c_int32, C.POINTER(C.c_size_t)]),
     "acid_layernorm_mod": (C.c_int, [C.c_int32, _P, C.c_int32, _P, C.c_int64, C.c_int32, _P, _P, C.c_float, _P]),
+    "acid_norm_site_groups": (C.c_int, [_SITE, C.POINTER(C.c_int64)]),
+    "acid_norm_site_forward": (C.c_int, [_SITE, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P]),
+    "acid_norm_site_workspace_size": (C.c_int, [_SITE, C.POINTER(C.c_size_t)]),
+    "acid_norm_site_backward": (C.c_int, [_SITE, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _GRADS,
+                                          _P, C.c_size_t, _P]),
+    "acid_q4_row_bytes": (C.c_int, [C.c_int32, C.POINTER(C.c_size_t)]),
+    "acid_q4_quantize": (C.c_int, [C.c_int32, _P, C.c_int64, _Q4, _P]),
+    "acid_q4_dequantize": (C.c_int, [_Q4, C.c_int32, _P, C.c_int64, _P]),
+    "acid_q4_linear_forward": (C.c_int, [C.c_int32, _P, C.c_int64, C.c_int64, _Q4, _P, C.c_int32, C.c_int32, _P,
+                                         C.c_int64, _P]),
+    "acid_q4_linear_workspace_size": (C.c_int, [_Q4, C.c_int64, C.POINTER(C.c_size_t)]),
+    "acid_q4_linear_backward": (C.c_int, [C.c_int32, _P, C.c_int64, C.c_int64, _Q4, C.c_int32, _P, C.c_int64,
+                                          C.c_int32, _P, C.c_int64, _P, _P, C.c_size_t, _P]),
     "acid_block_rows": (C.c_int, [C.POINTER(acid_block_desc), C.POINTER(C.c_int64)]),
     "acid_block_workspace_size": (C.c_int, [C.POINTER(acid_block_desc), C.POINTER(C.c_size_t)]),
     "acid_dit_block_forward": (C.c_int, [C.POINTER(acid_block_desc), _P, C.POINTER(acid_cond),

@@ -235,6 +235,247 @@ def acid_layernorm_mod(x: torch.Tensor, shift: torch.Tensor | None = None, scale
 
 
 # ---------------------------------------------------------------------------
+# norm sites
+# ---------------------------------------------------------------------------
+
+_NORM = {"none": A.ACID_NORM_NONE, "rms": A.ACID_NORM_RMS, "layer": A.ACID_NORM_LAYER}
+
+
+def norm_site_groups(rows: int, first_rows: int = 0, group_rows: int = 0) -> int:
+    """Modulation groups of a site: the first rows, then each group_rows rows (0: all the rest)."""
+    rest = rows - first_rows
+    return (first_rows > 0) + -(-rest // (group_rows or max(rest, 1)))
+
+
+def _rows_of(name: str, t: torch.Tensor, rows: int, d: int, dtype) -> int:
+    """Row stride of an operand [rows, d] (0 for none)."""
+    if t is None:
+        return 0
+    if not t.is_cuda or t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != d or t.stride(1) != 1:
+        raise ValueError(f"{name} must be a CUDA tensor [{rows}, {d}] of {dtype} with contiguous rows")
+    return t.stride(0) if rows > 1 else d
+
+
+def _site(rows, d, stream_dtype, branch_dtype, gate, scale, shift, post_w, pre_w, post_norm, pre_norm, eps, res_scale,
+          branch_scale, gate_tanh, first_rows, group_rows):
+    """(C descriptor of a site, its groups) after a check of the vectors' shapes."""
+    if not 0 <= first_rows <= rows or group_rows < 0:
+        raise ValueError("need 0 <= first_rows <= rows and group_rows >= 0")
+    groups = norm_site_groups(rows, first_rows, group_rows)
+    ld, ptrs = 0, []
+    for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
+        if t is None:
+            ptrs.append(None)
+            continue
+        shape = t.shape
+        if not t.is_cuda or t.dtype != torch.float32 or t.stride(-1) != 1 or shape[-1] != d or not (
+                (len(shape) == 2 and shape[0] == groups) or (len(shape) == 1 and groups == 1)):
+            raise ValueError(f"{name} must be a CUDA fp32 tensor [{groups}, {d}] with contiguous rows")
+        if groups > 1:
+            if ld and ld != t.stride(0):
+                raise ValueError("gate, scale and shift must have one row stride")
+            ld = t.stride(0)
+        ptrs.append(t.data_ptr())
+    for name, t in (("post_w", post_w), ("pre_w", pre_w)):
+        if t is not None and not (t.is_cuda and t.dtype == torch.float32 and t.shape == (d,) and t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous CUDA fp32 tensor [{d}]")
+    return A.acid_norm_site(rows, d, _DT[stream_dtype], _DT[branch_dtype], _NORM[post_norm], _NORM[pre_norm],
+                            bool(gate_tanh), eps, res_scale, branch_scale, first_rows, group_rows, *ptrs, ld,
+                            _ptr(post_w), _ptr(pre_w)), groups
+
+
+def acid_norm_site_forward(x: torch.Tensor, y: torch.Tensor | None = None, *, gate: torch.Tensor | None = None,
+                           scale: torch.Tensor | None = None, shift: torch.Tensor | None = None,
+                           post_w: torch.Tensor | None = None, pre_w: torch.Tensor | None = None,
+                           post_norm: str = "rms", pre_norm: str = "layer", eps: float = 1e-6, res_scale: float = 1.0,
+                           branch_scale: float = 1.0, gate_tanh: bool = False, first_rows: int = 0,
+                           group_rows: int = 0, r: torch.Tensor | None = None, u: torch.Tensor | None = None,
+                           want_r: bool = True, want_u: bool = True, branch_dtype=None, stream=None):
+    """(r, u) of a norm site: r = res_scale x + branch_scale g (N_post(y) post_w), u = N_pre(r) pre_w (1 + scale) + shift,
+    g = gate or tanh(gate).  x, r [rows, d] of the stream's dtype, y, u of the branch's (branch_dtype where y is None);
+    gate, scale, shift fp32 [groups, d] (norm_site_groups).  r and u are allocated unless given (r may be x, u may be
+    y); want_r / want_u False leave one out (None)."""
+    if x.dim() != 2 or x.dtype not in _DT:
+        raise ValueError("x must be a [rows, d] tensor of bf16 or fp32")
+    rows, d = x.shape
+    bdt = y.dtype if y is not None else branch_dtype or x.dtype
+    if bdt not in _DT:
+        raise TypeError(f"unsupported dtype {bdt}")
+    site, _ = _site(rows, d, x.dtype, bdt, gate, scale, shift, post_w, pre_w, post_norm, pre_norm, eps, res_scale,
+                    branch_scale, gate_tanh, first_rows, group_rows)
+    if r is None and want_r:
+        r = torch.empty((rows, d), dtype=x.dtype, device=x.device)
+    if u is None and want_u:
+        u = torch.empty((rows, d), dtype=bdt, device=x.device)
+    ldx, ldy = _rows_of("x", x, rows, d, x.dtype), _rows_of("y", y, rows, d, bdt)
+    ldr, ldu = _rows_of("r", r, rows, d, x.dtype), _rows_of("u", u, rows, d, bdt)
+    check(load().acid_norm_site_forward(C.byref(site), x.data_ptr(), ldx, _ptr(y), ldy, _ptr(r), ldr, _ptr(u), ldu,
+                                        _stream(stream)))
+    return r, u
+
+
+def norm_site_workspace_size(site: A.acid_norm_site) -> int:
+    b = C.c_size_t()
+    check(load().acid_norm_site_workspace_size(C.byref(site), C.byref(b)))
+    return b.value
+
+
+def acid_norm_site_backward(du: torch.Tensor | None, r: torch.Tensor | None, y: torch.Tensor | None = None, *,
+                            dr: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+                            scale: torch.Tensor | None = None, shift: torch.Tensor | None = None,
+                            post_w: torch.Tensor | None = None, pre_w: torch.Tensor | None = None,
+                            post_norm: str = "rms", pre_norm: str = "layer", eps: float = 1e-6, res_scale: float = 1.0,
+                            branch_scale: float = 1.0, gate_tanh: bool = False, first_rows: int = 0,
+                            group_rows: int = 0, dx: torch.Tensor | None = None, dy: torch.Tensor | None = None,
+                            vectors: bool = True, workspace: torch.Tensor | None = None, stream=None) -> dict:
+    """Gradients of acid_norm_site_forward from du (of u) and dr (of r), with the forward call's r and y and its other
+    arguments: a dict of dx, dy and, with ``vectors``, dgate, dscale, dshift [groups, d], dpost_w, dpre_w [d] (those
+    whose input is given; dshift where scale or shift is)."""
+    like = next((t for t in (r, dr) if t is not None), None)
+    if like is None or like.dim() != 2 or like.dtype not in _DT:
+        raise ValueError("need r or dr, [rows, d] of bf16 or fp32")
+    rows, d = like.shape
+    bdt = y.dtype if y is not None else du.dtype if du is not None else like.dtype
+    if bdt not in _DT:
+        raise TypeError(f"unsupported dtype {bdt}")
+    site, groups = _site(rows, d, like.dtype, bdt, gate, scale, shift, post_w, pre_w, post_norm, pre_norm, eps,
+                         res_scale, branch_scale, gate_tanh, first_rows, group_rows)
+    dev = like.device
+    out = {"dx": torch.empty((rows, d), dtype=like.dtype, device=dev) if dx is None else dx}
+    if y is not None:
+        out["dy"] = torch.empty((rows, d), dtype=bdt, device=dev) if dy is None else dy
+    if vectors:
+        want = [n for n, t in (("dgate", gate if y is not None else None), ("dscale", scale if du is not None else None),
+                               ("dshift", (scale if shift is None else shift) if du is not None else None))
+                if t is not None]
+        if want:
+            out.update(zip(want, torch.empty((len(want), groups, d), dtype=torch.float32, device=dev).unbind(0)))
+        if post_w is not None and y is not None:
+            out["dpost_w"] = torch.empty(d, dtype=torch.float32, device=dev)
+        if pre_w is not None and du is not None:
+            out["dpre_w"] = torch.empty(d, dtype=torch.float32, device=dev)
+    ws = torch.empty(norm_site_workspace_size(site), dtype=torch.uint8, device=dev) if workspace is None else workspace
+    get = out.get
+    grads = A.acid_norm_site_grads(out["dx"].data_ptr(), _rows_of("dx", out["dx"], rows, d, like.dtype),
+                                   _ptr(get("dy")), _rows_of("dy", get("dy"), rows, d, bdt), _ptr(get("dgate")),
+                                   _ptr(get("dscale")), _ptr(get("dshift")), d, _ptr(get("dpost_w")),
+                                   _ptr(get("dpre_w")))
+    check(load().acid_norm_site_backward(C.byref(site), _ptr(du), _rows_of("du", du, rows, d, bdt), _ptr(r),
+                                         _rows_of("r", r, rows, d, like.dtype), _ptr(y), _rows_of("y", y, rows, d, bdt),
+                                         _ptr(dr), _rows_of("dr", dr, rows, d, like.dtype), C.byref(grads),
+                                         ws.data_ptr(), ws.numel(), _stream(stream)))
+    return out
+
+
+# ---------------------------------------------------------------------------
+# modulation projections with 4-bit weights
+# ---------------------------------------------------------------------------
+
+class Q4Weight:
+    """A weight [n, k] in 4 bits: s (q - z) with a scale (and zero point; None: z = 8) for each ``group`` columns.
+    packed uint8 [n, 64 ceil(k / 128)] (layout: include/acid.h), scales [n, ceil(k / group)] bf16 or fp32, zeros
+    uint8 of the scales' shape or None, all contiguous and left as they are while the weight is in use."""
+
+    __slots__ = ("packed", "scales", "zeros", "n", "k", "group", "struct")
+
+    def __init__(self, packed: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor | None, n: int, k: int,
+                 group: int):
+        per_row = -(-k // group) if group > 0 else 0
+        if not (packed.is_cuda and packed.dtype == torch.uint8 and packed.is_contiguous()
+                and packed.numel() == n * 64 * -(-k // 128)):
+            raise ValueError("packed must be a contiguous CUDA uint8 tensor [n, 64 ceil(k / 128)]")
+        if not (scales.is_cuda and scales.dtype in _DT and scales.is_contiguous() and scales.numel() == n * per_row):
+            raise ValueError("scales must be a contiguous CUDA bf16 or fp32 tensor [n, ceil(k / group)]")
+        if zeros is not None and not (zeros.is_cuda and zeros.dtype == torch.uint8 and zeros.is_contiguous()
+                                      and zeros.numel() == n * per_row):
+            raise ValueError("zeros must be a contiguous CUDA uint8 tensor [n, ceil(k / group)]")
+        self.packed, self.scales, self.zeros, self.n, self.k, self.group = packed, scales, zeros, n, k, group
+        self.struct = A.acid_q4_weight(packed.data_ptr(), scales.data_ptr(), _ptr(zeros), n, k, group,
+                                       _DT[scales.dtype])
+
+
+def _matrix(name: str, t: torch.Tensor, rows: int, cols: int) -> int:
+    """Row stride of an operand [rows, cols]."""
+    if not t.is_cuda or t.dtype not in _DT or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (
+            t.stride(1) != 1 and cols > 1):
+        raise ValueError(f"{name} must be a CUDA tensor [{rows}, {cols}] of bf16 or fp32 with contiguous rows")
+    return max(t.stride(0), cols) if rows > 1 else cols
+
+
+def acid_q4_quantize(w: torch.Tensor, group: int = 128, zeros: bool = False, scale_dtype=torch.bfloat16,
+                     stream=None) -> Q4Weight:
+    """w [n, k] (bf16 or fp32) in 4 bits with a scale, and with ``zeros`` a zero point, for each ``group`` columns."""
+    if w.dim() != 2:
+        raise ValueError("w must be a matrix")
+    n, k = w.shape
+    ld = _matrix("w", w, n, k)
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128")
+    per_row = -(-k // group)
+    q = Q4Weight(torch.empty((n, 64 * -(-k // 128)), dtype=torch.uint8, device=w.device),
+                 torch.empty((n, per_row), dtype=scale_dtype, device=w.device),
+                 torch.empty((n, per_row), dtype=torch.uint8, device=w.device) if zeros else None, n, k, group)
+    check(load().acid_q4_quantize(_DT[w.dtype], w.data_ptr(), ld, C.byref(q.struct), _stream(stream)))
+    return q
+
+
+def acid_q4_dequantize(weight: Q4Weight, dtype=torch.float32, out: torch.Tensor | None = None,
+                       stream=None) -> torch.Tensor:
+    """The weight's values s (q - z) as a [n, k] tensor."""
+    out = torch.empty((weight.n, weight.k), dtype=dtype, device=weight.packed.device) if out is None else out
+    ld = _matrix("out", out, weight.n, weight.k)
+    check(load().acid_q4_dequantize(C.byref(weight.struct), _DT[out.dtype], out.data_ptr(), ld, _stream(stream)))
+    return out
+
+
+def acid_q4_linear_forward(x: torch.Tensor, weight: Q4Weight, bias: torch.Tensor | None = None, silu: bool = False,
+                           out: torch.Tensor | None = None, out_dtype=torch.float32, stream=None) -> torch.Tensor:
+    """out [m, n] = a(x [m, k]) W^T + bias, a = SiLU with ``silu``; bias fp32 [n]."""
+    m = x.shape[0]
+    ldx = _matrix("x", x, m, weight.k)
+    if bias is not None and not (bias.is_cuda and bias.dtype == torch.float32 and bias.shape == (weight.n,)
+                                 and bias.is_contiguous()):
+        raise ValueError("bias must be a contiguous CUDA fp32 tensor [n]")
+    out = torch.empty((m, weight.n), dtype=out_dtype, device=x.device) if out is None else out
+    ldo = _matrix("out", out, m, weight.n)
+    check(load().acid_q4_linear_forward(_DT[x.dtype], x.data_ptr(), ldx, m, C.byref(weight.struct), _ptr(bias),
+                                        bool(silu), _DT[out.dtype], out.data_ptr(), ldo, _stream(stream)))
+    return out
+
+
+def q4_linear_workspace_size(weight: Q4Weight, m: int) -> int:
+    b = C.c_size_t()
+    check(load().acid_q4_linear_workspace_size(C.byref(weight.struct), int(m), C.byref(b)))
+    return b.value
+
+
+def acid_q4_linear_backward(g: torch.Tensor, weight: Q4Weight, x: torch.Tensor | None = None, silu: bool = False,
+                            dx: torch.Tensor | None = None, want_dx: bool = True, want_dbias: bool = True,
+                            dx_dtype=torch.float32, workspace: torch.Tensor | None = None, stream=None):
+    """(dx [m, k], dbias [n]) of acid_q4_linear_forward from g [m, n], the gradient of its output, and x, its input
+    (needed with ``silu``; dx has its dtype, dx_dtype without it).  want_dx / want_dbias False leave one out (None)."""
+    m, dev = g.shape[0], g.device
+    ldg = _matrix("g", g, m, weight.n)
+    ldx = 0 if x is None else _matrix("x", x, m, weight.k)
+    if silu and x is None and want_dx:
+        raise ValueError("silu needs x")
+    dbias = torch.empty(weight.n, dtype=torch.float32, device=dev) if want_dbias else None
+    if want_dx and dx is None:
+        dx = torch.empty((m, weight.k), dtype=dx_dtype if x is None else x.dtype, device=dev)
+    lddx = 0 if dx is None else _matrix("dx", dx, m, weight.k)
+    if dx is not None and x is not None and dx.dtype != x.dtype:
+        raise ValueError("dx must have the dtype of x")
+    ws = workspace
+    if ws is None and dx is not None:
+        ws = torch.empty(q4_linear_workspace_size(weight, m), dtype=torch.uint8, device=dev)
+    xdt = x.dtype if x is not None else dx.dtype if dx is not None else torch.float32
+    check(load().acid_q4_linear_backward(_DT[g.dtype], g.data_ptr(), ldg, m, C.byref(weight.struct), _DT[xdt],
+                                         _ptr(x), ldx, bool(silu), _ptr(dx), lddx, _ptr(dbias), _ptr(ws),
+                                         0 if ws is None else ws.numel(), _stream(stream)))
+    return dx, dbias
+
+
+# ---------------------------------------------------------------------------
 # blocks
 # ---------------------------------------------------------------------------
 

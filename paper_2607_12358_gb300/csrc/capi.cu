@@ -19,6 +19,8 @@ unsigned int take_device_error_attention();
 BoundsRecord take_bounds_elementwise();
 BoundsRecord take_bounds_gemm();
 BoundsRecord take_bounds_attention();
+BoundsRecord take_bounds_site();
+BoundsRecord take_bounds_q4();
 
 namespace {
 thread_local std::string t_last_error;
@@ -222,8 +224,8 @@ extern "C" acid_status acid_bounds_report(int32_t* checked, int64_t* site, int64
   clear_error();
   ACID_REQUIRE(checked && site && index && extent, ACID_ERR_INVALID_ARG, "acid_bounds_report: null argument");
   ACID_CUDA(cudaDeviceSynchronize());
-  const BoundsRecord recs[4] = {take_bounds_elementwise(), take_bounds_gemm(), take_bounds_attention(),
-                                take_bounds_capi()};
+  const BoundsRecord recs[6] = {take_bounds_elementwise(), take_bounds_gemm(), take_bounds_attention(),
+                                take_bounds_site(),        take_bounds_q4(),   take_bounds_capi()};
   *checked = kBoundsChecked ? 1 : 0;
   *site = *index = *extent = 0;
   for (const BoundsRecord& r : recs) {

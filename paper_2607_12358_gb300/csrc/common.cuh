@@ -165,7 +165,7 @@ static __device__ unsigned int g_device_error = 0;
 enum BoundsSite : int {
   kSiteDrift = 1, kSiteAdd = 2, kSiteLayerNorm = 3, kSiteTemni = 4, kSitePatchify = 5, kSiteUnpatchify = 6,
   kSiteGemv = 7, kSiteGemmResidual = 8, kSiteGemmStore = 9, kSiteGemmRope = 10, kSiteGemmF32 = 11,
-  kSiteAttnMerge = 12, kSiteAttnF32 = 13, kSiteSelftest = 99
+  kSiteAttnMerge = 12, kSiteAttnF32 = 13, kSiteNormSite = 14, kSiteQ4 = 15, kSiteSelftest = 99
 };
 struct BoundsRecord {
   long long site, index, extent;
