@@ -14,8 +14,9 @@ ACID_BOUNDS_READER(take_bounds_site)
 
 namespace {
 
-constexpr int kMaxWidth = 4096;           // 16 warps of 8 columns a lane
-constexpr int kMaxWarps = kMaxWidth / 256;
+using bf16 = __nv_bfloat16;
+constexpr int kMaxWidth = 4096;           // 8 warps of 16 columns a lane
+constexpr int kMaxWarps = kMaxWidth / 512;
 
 // What both directions read, as the kernels see it.
 struct Site {
@@ -59,284 +60,496 @@ struct SiteBwd {
   int64_t per;   // rows of a CTA
 };
 
-// 8 columns of a vector, or 8 times the same value where there is none.
-__device__ __forceinline__ void vec8(const float* p, int c, int d, float none, float* v) {
-  if (p != nullptr && ACID_IN_BOUNDS(kSiteNormSite, c + 7, d)) {
-    load8(p + c, v);
-  } else {
+// A thread's 16 columns: two octets, 8 (tid + j blockDim) ..., as eight fp32
+// pairs, so that one instruction does the arithmetic of two columns.  Octets
+// past the row's end hold zeros all through.
+struct Cols {
+  uint64_t v[8];
+};
+#define FOR_PAIRS _Pragma("unroll") for (int i = 0; i < 8; ++i)
+__device__ __forceinline__ uint64_t f2_same(float x) { return f2_pack(x, x); }
+__device__ __forceinline__ float f2_total(uint64_t x) {
+  float a, b;
+  f2_unpack(x, a, b);
+  return a + b;
+}
+// Sum of the pairs.
+__device__ __forceinline__ float total(const uint64_t (&p)[8]) {
+  return f2_total(f2_add(f2_add(f2_add(p[0], p[1]), f2_add(p[2], p[3])), f2_add(f2_add(p[4], p[5]), f2_add(p[6], p[7]))));
+}
+__device__ __forceinline__ float total(const Cols& a) { return total(a.v); }
+// Sum of the products.
+__device__ __forceinline__ float dot(const Cols& a, const Cols& b) {
+  uint64_t s = f2_mul(a.v[0], b.v[0]), t = f2_mul(a.v[1], b.v[1]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = none;
+  for (int i = 2; i < 8; i += 2) {
+    s = f2_fma(a.v[i], b.v[i], s);
+    t = f2_fma(a.v[i + 1], b.v[i + 1], t);
   }
-}
-template <typename T>
-__device__ __forceinline__ void row8(const void* p, int64_t ld, int64_t row, int64_t rows, int c, float* v) {
-  if (ACID_IN_BOUNDS(kSiteNormSite, row, rows)) load8(static_cast<const T*>(p) + row * ld + c, v);
-}
-template <typename T>
-__device__ __forceinline__ void put8(void* p, int64_t ld, int64_t row, int64_t rows, int c, const float* v) {
-  if (ACID_IN_BOUNDS(kSiteNormSite, row, rows)) store8(static_cast<T*>(p) + row * ld + c, v);
+  return f2_total(f2_add(s, t));
 }
 
-// Sums of N values over the CTA; every thread gets them.  Rounds alternate
-// between two buffers, so that one barrier a round is enough: a thread writes a
-// buffer again behind the other one's barrier.
-template <int N>
-__device__ __forceinline__ void cta_sum(float (&v)[N], float (*red)[kMaxWarps][4], int& round) {
-  static_assert(N <= 4, "a warp's slot holds four sums");
-  const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
+struct Place {
+  int c[2], d;  // first column of each octet
+  bool on[2];
+};
+__device__ __forceinline__ Place place(int d) {
+  const int c0 = threadIdx.x * 8, c1 = c0 + blockDim.x * 8;
+  return {{c0, c1}, d, {c0 < d, c1 < d}};
+}
+__device__ __forceinline__ void fill(Cols& a, int j, float x) {
 #pragma unroll
-  for (int i = 0; i < N; ++i)
+  for (int i = 0; i < 4; ++i) a.v[4 * j + i] = f2_same(x);
+}
+// Columns of a vector; `none` in all of the row's where there is none.
+__device__ __forceinline__ Cols vec(const float* p, const Place& at, float none) {
+  Cols a;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-  if (warps == 1) return;
-  if ((threadIdx.x & 31) == 0)
+  for (int j = 0; j < 2; ++j) {
+    if (!at.on[j] || p == nullptr) {
+      fill(a, j, at.on[j] ? none : 0.f);
+    } else if (ACID_IN_BOUNDS(kSiteNormSite, at.c[j] + 7, at.d)) {
+      const float4 lo = *reinterpret_cast<const float4*>(p + at.c[j]);
+      const float4 hi = *reinterpret_cast<const float4*>(p + at.c[j] + 4);
+      a.v[4 * j] = f2_pack(lo.x, lo.y);
+      a.v[4 * j + 1] = f2_pack(lo.z, lo.w);
+      a.v[4 * j + 2] = f2_pack(hi.x, hi.y);
+      a.v[4 * j + 3] = f2_pack(hi.z, hi.w);
+    }
+  }
+  return a;
+}
+__device__ __forceinline__ void times(Cols& a, const Cols& b) { FOR_PAIRS a.v[i] = f2_mul(a.v[i], b.v[i]); }
+__device__ __forceinline__ void plus(Cols& a, float x, const Place& at) {
+  FOR_PAIRS a.v[i] = f2_add(a.v[i], f2_same(at.on[i >> 2] ? x : 0.f));
+}
+// branch_scale times the gate's columns of a group.
+__device__ __forceinline__ Cols gate_cols(const Site& s, int64_t m, const Place& at) {
+  Cols g = vec(s.gate ? s.gate + m : nullptr, at, 1.f);
+  FOR_PAIRS {
+    if (s.tanh && s.gate) {
+      float lo, hi;
+      f2_unpack(g.v[i], lo, hi);
+      g.v[i] = f2_pack(tanhf(lo), tanhf(hi));
+    }
+    g.v[i] = f2_mul(g.v[i], f2_same(s.branch));
+  }
+  return g;
+}
+// 1 + scale of a group.
+__device__ __forceinline__ Cols scale_cols(const Site& s, int64_t m, const Place& at) {
+  Cols a = vec(s.scale ? s.scale + m : nullptr, at, 0.f);
+  plus(a, 1.f, at);
+  return a;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_pairs(T* p, const uint64_t* v) {
+  float f[8];
 #pragma unroll
-    for (int i = 0; i < N; ++i) red[round][warp][i] = v[i];
+  for (int i = 0; i < 4; ++i) f2_unpack(v[i], f[2 * i], f[2 * i + 1]);
+  store8(p, f);
+}
+// To a row of the operand, whose first element is `row`.
+template <typename T>
+__device__ __forceinline__ void put(T* row, const Place& at, const Cols& a, int64_t r, int64_t rows) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+    if (at.on[j] && ACID_IN_BOUNDS(kSiteNormSite, r, rows)) store_pairs(row + at.c[j], a.v + 4 * j);
+}
+
+// Sums of N values over the CTA; every thread gets them.  The first shuffles
+// hand half of the values to half of the lanes, so that four sums take six
+// shuffles and not twenty.  Rounds alternate between two buffers, so that one
+// barrier a round is enough: a thread writes a buffer again behind the other
+// one's barrier.  Slots of warps that the CTA does not have are zero.
+struct Reducer {
+  float4 (*red)[kMaxWarps];
+  int round, warps, warp, lane;
+  template <int N>
+  __device__ __forceinline__ float4 sum(float a, float b = 0.f, float c = 0.f, float e = 0.f) {
+    float* out = reinterpret_cast<float*>(&red[round][warp]);
+    if constexpr (N > 2) {
+      const bool hi = lane & 16, mid = lane & 8;
+      float p = hi ? c : a, q = hi ? e : b;
+      p += __shfl_xor_sync(0xffffffffu, hi ? a : c, 16);
+      q += __shfl_xor_sync(0xffffffffu, hi ? b : e, 16);
+      a = mid ? q : p;
+      a += __shfl_xor_sync(0xffffffffu, mid ? p : q, 8);
+    } else if constexpr (N == 2) {
+      const bool hi = lane & 16;
+      const float p = hi ? b : a;
+      a = p + __shfl_xor_sync(0xffffffffu, hi ? a : b, 16);
+      a += __shfl_xor_sync(0xffffffffu, a, 8);
+    } else {
+      a += __shfl_xor_sync(0xffffffffu, a, 16);
+      a += __shfl_xor_sync(0xffffffffu, a, 8);
+    }
+    a += __shfl_xor_sync(0xffffffffu, a, 4);
+    a += __shfl_xor_sync(0xffffffffu, a, 2);
+    a += __shfl_xor_sync(0xffffffffu, a, 1);
+    constexpr int kOwn = N > 2 ? 8 : N == 2 ? 16 : 32;  // lanes that hold one of the sums
+    if ((lane & (kOwn - 1)) == 0) out[lane / kOwn] = a;
+    __syncthreads();
+    const float4* t = red[round];
+    round ^= 1;
+    auto add = [](float4 x, float4 y) { return make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w); };
+    float4 v = add(add(t[0], t[1]), add(t[2], t[3]));
+    if (warps > 4) v = add(v, add(add(t[4], t[5]), add(t[6], t[7])));
+    return v;
+  }
+};
+__device__ __forceinline__ Reducer reducer(float4 (*red)[kMaxWarps]) {
+  if (threadIdx.x < 2 * kMaxWarps) red[0][threadIdx.x] = make_float4(0.f, 0.f, 0.f, 0.f);
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = 0.f;
-  for (int w = 0; w < warps; ++w)
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += red[round][w][i];
-  round ^= 1;
+  return {red, 0, (int)(blockDim.x >> 5), (int)(threadIdx.x >> 5), (int)(threadIdx.x & 31)};
 }
 
-// v (0 in the columns past the row) becomes N(v); returns 1 / the root.
-__device__ __forceinline__ float norm_row(float (&v)[8], int kind, bool on, int d, float eps,
-                                          float (*red)[kMaxWarps][4], int& round) {
-  if (kind == ACID_NORM_NONE) return 1.f;
-  if (kind == ACID_NORM_LAYER) {
-    float s[1] = {0.f};
+// A thread's own ring of row pieces in shared memory: it copies the columns
+// that it will work on and nobody else reads them, so that waiting for its own
+// copies is all the synchronisation there is.  A stage is planes of 16 bytes a
+// thread.
+template <typename T>
+constexpr int kPlanes = sizeof(T);  // of 16 columns
+template <typename T>
+__device__ __forceinline__ void stage(uint8_t* mine, int plane, const T* row, const Place& at, int64_t r, int64_t rows) {
+  constexpr int kOctet = kPlanes<T> / 2;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s[0] += v[j];
-    cta_sum(s, red, round);
-    const float mean = s[0] / d;
+  for (int j = 0; j < 2; ++j)
+    if (at.on[j] && ACID_IN_BOUNDS(kSiteNormSite, r, rows))
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = on ? v[j] - mean : 0.f;
+      for (int i = 0; i < kOctet; ++i)
+        cp_async<16>(mine + (plane + j * kOctet + i) * blockDim.x * 16,
+                     reinterpret_cast<const uint8_t*>(row + at.c[j]) + 16 * i, true);
+}
+template <typename T>
+__device__ __forceinline__ Cols unstage(const uint8_t* mine, int plane, const Place& at) {
+  constexpr int kOctet = kPlanes<T> / 2;
+  Cols a;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    if (!at.on[j]) {
+      fill(a, j, 0.f);
+      continue;
+    }
+    const uint8_t* q = mine + (plane + j * kOctet) * blockDim.x * 16;
+    uint64_t* v = a.v + 4 * j;
+    if constexpr (sizeof(T) == 2) {
+      const uint4 u = *reinterpret_cast<const uint4*>(q);
+      v[0] = f2_pack(bf16_lo(u.x), bf16_hi(u.x));
+      v[1] = f2_pack(bf16_lo(u.y), bf16_hi(u.y));
+      v[2] = f2_pack(bf16_lo(u.z), bf16_hi(u.z));
+      v[3] = f2_pack(bf16_lo(u.w), bf16_hi(u.w));
+    } else {
+      const ulonglong2 lo = *reinterpret_cast<const ulonglong2*>(q);
+      const ulonglong2 hi = *reinterpret_cast<const ulonglong2*>(q + blockDim.x * 16);
+      v[0] = lo.x;
+      v[1] = lo.y;
+      v[2] = hi.x;
+      v[3] = hi.y;
+    }
   }
-  float q[1] = {0.f};
-#pragma unroll
-  for (int j = 0; j < 8; ++j) q[0] = fmaf(v[j], v[j], q[0]);
-  cta_sum(q, red, round);
-  const float inv = rsqrtf(q[0] / d + eps);
-#pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] *= inv;
-  return inv;
+  return a;
 }
 
-// One row at a time, 8 columns a thread.
-template <typename TS, typename TB>
-__global__ void __launch_bounds__(32 * kMaxWarps) site_forward_kernel(SiteFwd a) {
-  __shared__ float red[2][kMaxWarps][4];
+// A CTA takes a row at a time; row k of CTA b is b start + k step, k < count.
+constexpr int kFwdStages = 4;
+template <typename TS, typename TB, bool BRANCH>
+__global__ void __launch_bounds__(32 * kMaxWarps, 2) site_forward_kernel(SiteFwd a, int64_t start, int64_t step,
+                                                                        uint32_t count) {
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ float4 red[2][kMaxWarps];
   pdl_wait();
   const Site& s = a.s;
-  const int c = threadIdx.x * 8, d = s.d;
-  const bool on = c < d;
-  int round = 0;
-  for (int64_t row = blockIdx.x; row < s.rows; row += gridDim.x) {
-    const int64_t m = group_of(s, row) * s.ld_mod;
-    float r[8] = {}, t[8];
-    if (on) {
-      row8<TS>(a.x, a.ldx, row, s.rows, c, r);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) r[j] *= s.res;
+  const Place at = place(s.d);
+  Reducer sums = reducer(red);
+  const float d = (float)s.d, per_d = 1.f / d;
+  int64_t row = blockIdx.x * start;
+  const uint32_t n = row < s.rows ? (uint32_t)min((int64_t)count, (s.rows - 1 - row) / step + 1) : 0;
+  constexpr int kStage = kPlanes<TS> + (BRANCH ? kPlanes<TB> : 0);
+  uint8_t* mine = ring + threadIdx.x * 16;
+  const int stride = kStage * blockDim.x * 16;
+  int64_t ahead = row;  // the next row to be copied
+  uint32_t copied = 0;
+  int to = 0;
+  auto issue = [&] {
+    if (copied < n) {
+      stage(mine + to * stride, 0, static_cast<const TS*>(a.x) + ahead * a.ldx, at, ahead, s.rows);
+      if constexpr (BRANCH)
+        stage(mine + to * stride, kPlanes<TS>, static_cast<const TB*>(a.y) + ahead * a.ldy, at, ahead, s.rows);
+      ahead += step;
+      ++copied;
     }
-    if (a.y != nullptr) {
-      float y[8] = {};
-      if (on) row8<TB>(a.y, a.ldy, row, s.rows, c, y);
-      norm_row(y, s.post, on, d, s.eps, red, round);
-      if (on) {
-        vec8(s.post_w, c, d, 1.f, t);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] *= t[j];
-        vec8(s.gate ? s.gate + m : nullptr, c, d, 1.f, t);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float g = s.tanh && s.gate ? tanhf(t[j]) : t[j];
-          r[j] = fmaf(s.branch * g, y[j], r[j]);
+    to = to + 1 == kFwdStages ? 0 : to + 1;
+    cp_async_commit();
+  };
+  for (int k = 0; k < kFwdStages - 1; ++k) issue();
+  const bool wants_mean = s.pre == ACID_NORM_LAYER && a.u != nullptr;
+  int st = 0;
+  for (uint32_t k = 0; k < n;) {
+    // the rows of one group
+    const int64_t g = group_of(s, row), m = g * s.ld_mod;
+    const uint32_t stop = (uint32_t)min((int64_t)n, k + (group_end(s, g) - 1 - row) / step + 1);
+    Cols gw, sc = scale_cols(s, m, at);  // gate and post_w, (1 + scale) and pre_w, shift
+    const Cols sh = vec(s.shift ? s.shift + m : nullptr, at, 0.f);
+    times(sc, vec(s.pre_w, at, 1.f));
+    if constexpr (BRANCH) {
+      gw = gate_cols(s, m, at);
+      times(gw, vec(s.post_w, at, 1.f));
+    }
+    for (; k < stop; ++k, row += step) {
+      cp_async_wait<kFwdStages - 2>();
+      Cols r = unstage<TS>(mine + st * stride, 0, at);
+      FOR_PAIRS r.v[i] = f2_mul(r.v[i], f2_same(s.res));
+      float mean = 0.f;
+      if constexpr (BRANCH) {
+        Cols y = unstage<TB>(mine + st * stride, kPlanes<TS>, at);
+        issue();
+        if (s.post == ACID_NORM_LAYER) plus(y, -(sums.sum<1>(total(y)).x / d), at);
+        // the sum of r comes with the branch's sum of squares, from those of x and of g w y
+        const float sq = dot(y, y);
+        times(y, gw);
+        float inv = 1.f;
+        if (s.post != ACID_NORM_NONE || wants_mean) {
+          const float4 t = sums.sum<3>(sq, total(y), total(r));
+          if (s.post != ACID_NORM_NONE) inv = rsqrtf(fmaf(t.x, per_d, s.eps));
+          mean = fmaf(inv, t.y, t.z) / d;
         }
+        FOR_PAIRS r.v[i] = f2_fma(f2_same(inv), y.v[i], r.v[i]);
+      } else {
+        issue();
+        if (wants_mean) mean = sums.sum<1>(total(r)).x / d;
       }
+      st = st + 1 == kFwdStages ? 0 : st + 1;
+      if (a.r != nullptr) put(static_cast<TS*>(a.r) + row * a.ldr, at, r, row, s.rows);
+      if (a.u == nullptr) continue;
+      if (s.pre != ACID_NORM_NONE) {
+        if (s.pre == ACID_NORM_LAYER) plus(r, -mean, at);
+        const float inv = rsqrtf(fmaf(sums.sum<1>(dot(r, r)).x, per_d, s.eps));
+        FOR_PAIRS r.v[i] = f2_mul(r.v[i], f2_same(inv));
+      }
+      FOR_PAIRS r.v[i] = f2_fma(r.v[i], sc.v[i], sh.v[i]);
+      put(static_cast<TB*>(a.u) + row * a.ldu, at, r, row, s.rows);
     }
-    if (on && a.r != nullptr) put8<TS>(a.r, a.ldr, row, s.rows, c, r);
-    if (a.u == nullptr) continue;
-    norm_row(r, s.pre, on, d, s.eps, red, round);
-    if (!on) continue;
-    vec8(s.pre_w, c, d, 1.f, t);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) r[j] *= t[j];
-    vec8(s.scale ? s.scale + m : nullptr, c, d, 0.f, t);
-    float h[8];
-    vec8(s.shift ? s.shift + m : nullptr, c, d, 0.f, h);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) r[j] = fmaf(r[j], 1.f + t[j], h[j]);
-    put8<TB>(a.u, a.ldu, row, s.rows, c, r);
   }
-}
-
-// The gradient of a norm's input from dn, that of its output n.
-__device__ __forceinline__ void norm_back(float (&dn)[8], const float (&n)[8], float inv, int kind, bool on, int d,
-                                          float (*red)[kMaxWarps][4], int& round) {
-  if (kind == ACID_NORM_NONE) return;
-  float s[2] = {0.f, 0.f};
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    s[0] += dn[j];
-    s[1] = fmaf(dn[j], n[j], s[1]);
-  }
-  cta_sum(s, red, round);
-  const float mean = kind == ACID_NORM_LAYER ? s[0] / d : 0.f, along = s[1] / d;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) dn[j] = on ? (dn[j] - mean - n[j] * along) * inv : 0.f;
 }
 
 // Gradients of the site's vectors for one group from the raw sums
-// A = sum du, S = sum du n, T = sum dr p over its rows.
-__device__ __forceinline__ void put_group(const SiteBwd& a, int64_t g, int c, const float (&A)[8], const float (&S)[8],
-                                          const float (&T)[8]) {
+// sum du, sum du n and sum dr p over its rows (which = 0, 1, 2): one column.
+__device__ __forceinline__ void put_sum(const SiteBwd& a, int which, int64_t g, int c, float v) {
   const Site& s = a.s;
-  float w[8], o[8];
-  const int64_t at = g * a.ld_dmod + c, m = g * s.ld_mod;
-  if (a.dshift != nullptr) store8(a.dshift + at, A);
-  if (a.dscale != nullptr) {
-    vec8(s.pre_w, c, s.d, 1.f, w);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = w[j] * S[j];
-    store8(a.dscale + at, o);
+  float* out = which == 0 ? a.dshift : which == 1 ? a.dscale : a.dgate;
+  if (out == nullptr || !ACID_IN_BOUNDS(kSiteNormSite, c, s.d)) return;
+  if (which == 1 && s.pre_w != nullptr) v *= s.pre_w[c];
+  if (which == 2) {
+    const float th = s.tanh && s.gate ? tanhf(s.gate[g * s.ld_mod + c]) : 0.f;
+    v *= s.branch * (1.f - th * th) * (s.post_w != nullptr ? s.post_w[c] : 1.f);
   }
-  if (a.dgate != nullptr) {
-    vec8(s.post_w, c, s.d, 1.f, w);
-    float t[8];
-    vec8(s.gate ? s.gate + m : nullptr, c, s.d, 1.f, t);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float th = s.tanh && s.gate ? tanhf(t[j]) : 0.f;
-      o[j] = s.branch * w[j] * T[j] * (1.f - th * th);
+  out[g * a.ld_dmod + c] = v;
+}
+// The same for a thread's columns.
+__device__ __forceinline__ void put_sums(const SiteBwd& a, int which, int64_t g, int64_t m, const Place& at, Cols v) {
+  const Site& s = a.s;
+  float* out = which == 0 ? a.dshift : which == 1 ? a.dscale : a.dgate;
+  if (out == nullptr) return;
+  if (which == 1) times(v, vec(s.pre_w, at, 1.f));
+  if (which == 2) {
+    times(v, vec(s.post_w, at, 1.f));
+    const Cols t = vec(s.tanh && s.gate ? s.gate + m : nullptr, at, 0.f);
+    FOR_PAIRS {
+      float lo, hi;
+      f2_unpack(t.v[i], lo, hi);
+      lo = tanhf(lo);
+      hi = tanhf(hi);
+      v.v[i] = f2_mul(v.v[i], f2_pack(s.branch * (1.f - lo * lo), s.branch * (1.f - hi * hi)));
     }
-    store8(a.dgate + at, o);
   }
+  put(out + g * a.ld_dmod, at, v, g, s.groups);
 }
 
-// CTA b takes the rows [b per, (b + 1) per).  A group that lies in it is
-// finished here; of one that reaches over its edge the sums go to the CTA's
-// slot 2 b (the group began earlier) or 2 b + 1 (it begins here).
+// The gradients.  CTA b takes the rows [b per, (b + 1) per) and keeps the sums
+// over the rows of its group in registers.  A group that lies in the CTA's rows
+// is finished here; of one that reaches over their edge the sums go to the
+// CTA's slot 2 b (the group began earlier) or 2 b + 1 (it begins here), and
+// site_join_kernel adds the slots.
+// (two stages where four fp32 rows of 4096 columns have to fit)
 template <typename TS, typename TB>
-__global__ void __launch_bounds__(32 * kMaxWarps) site_backward_kernel(SiteBwd a) {
-  __shared__ float red[2][kMaxWarps][4];
+constexpr int kBwdStages = sizeof(TS) + sizeof(TB) == 8 ? 2 : 3;
+template <typename TS, typename TB>
+__global__ void __launch_bounds__(32 * kMaxWarps, 1) site_backward_kernel(SiteBwd a) {
+  constexpr int kStages = kBwdStages<TS, TB>;
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ float4 red[2][kMaxWarps];
   pdl_wait();
   const Site& s = a.s;
-  const int c = threadIdx.x * 8, d = s.d;
-  const bool on = c < d;
-  int round = 0;
+  const Place at = place(s.d);
+  Reducer sums = reducer(red);
+  const float d = (float)s.d, per_d = 1.f / d;
   const int64_t begin = blockIdx.x * a.per, end = min(s.rows, begin + a.per);
-  float W[2][8] = {};
-  for (int64_t row = begin; row < end;) {
-    const int64_t g = group_of(s, row), m = g * s.ld_mod, from = row, to = min(end, group_end(s, g));
-    float A[8] = {}, S[8] = {}, T[8] = {}, sc[8] = {}, gp[8] = {}, w[8];
-    if (on) {
-      vec8(s.scale ? s.scale + m : nullptr, c, d, 0.f, sc);
-      vec8(s.gate ? s.gate + m : nullptr, c, d, 1.f, gp);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        sc[j] += 1.f;
-        gp[j] = s.branch * (s.tanh && s.gate ? tanhf(gp[j]) : gp[j]);
-      }
-    }
-    for (; row < to; ++row) {
-      float dr[8] = {};
-      if (on && a.dr != nullptr) row8<TS>(a.dr, a.lddr, row, s.rows, c, dr);
+  constexpr int kR = 0, kDr = kPlanes<TS>, kY = 2 * kPlanes<TS>, kDu = kY + kPlanes<TB>, kStage = kDu + kPlanes<TB>;
+  uint8_t* mine = ring + threadIdx.x * 16;
+  const int stride = kStage * blockDim.x * 16;
+  ulonglong2* wsum = reinterpret_cast<ulonglong2*>(ring + kStages * stride) + threadIdx.x;  // 8 planes of 4 columns
+  int64_t ahead = begin;
+  int to = 0;
+  auto issue = [&] {
+    if (ahead < end) {
+      uint8_t* p = mine + to * stride;
       if (a.du != nullptr) {
-        float n[8] = {}, du[8] = {};
-        if (on) {
-          row8<TS>(a.r, a.ldr, row, s.rows, c, n);
-          row8<TB>(a.du, a.lddu, row, s.rows, c, du);
-        }
-        const float inv = norm_row(n, s.pre, on, d, s.eps, red, round);
-        if (on) vec8(s.pre_w, c, d, 1.f, w);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          A[j] += du[j];
-          S[j] = fmaf(du[j], n[j], S[j]);
-          du[j] = on ? du[j] * sc[j] * w[j] : 0.f;
-        }
-        norm_back(du, n, inv, s.pre, on, d, red, round);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) dr[j] += du[j];
+        stage(p, kR, static_cast<const TS*>(a.r) + ahead * a.ldr, at, ahead, s.rows);
+        stage(p, kDu, static_cast<const TB*>(a.du) + ahead * a.lddu, at, ahead, s.rows);
       }
-      if (on && a.dx != nullptr) {
-        float o[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = s.res * dr[j];
-        put8<TS>(a.dx, a.lddx, row, s.rows, c, o);
+      if (a.dr != nullptr) stage(p, kDr, static_cast<const TS*>(a.dr) + ahead * a.lddr, at, ahead, s.rows);
+      if (a.y != nullptr) stage(p, kY, static_cast<const TB*>(a.y) + ahead * a.ldy, at, ahead, s.rows);
+      ++ahead;
+    }
+    to = to + 1 == kStages ? 0 : to + 1;
+    cp_async_commit();
+  };
+  for (int k = 0; k < kStages - 1; ++k) issue();
+  const bool weights = a.dpre_w != nullptr || a.dpost_w != nullptr;
+  for (int i = 0; weights && i < 8; ++i) wsum[i * blockDim.x] = make_ulonglong2(0, 0);
+  const Cols zero = {};
+  int st = 0;
+  for (int64_t row = begin; row < end;) {
+    const int64_t g = group_of(s, row), m = g * s.ld_mod, from = row, last = min(end, group_end(s, g));
+    Cols A = {}, S = {}, T = {}, sc = scale_cols(s, m, at), gw = gate_cols(s, m, at);
+    times(sc, vec(s.pre_w, at, 1.f));
+    times(gw, vec(s.post_w, at, 1.f));
+    for (; row < last; ++row) {
+      cp_async_wait<kStages - 2>();
+      const uint8_t* p = mine + st * stride;
+      Cols n = a.du != nullptr ? unstage<TS>(p, kR, at) : zero, du = a.du != nullptr ? unstage<TB>(p, kDu, at) : zero;
+      Cols y = a.y != nullptr ? unstage<TB>(p, kY, at) : zero, dr = a.dr != nullptr ? unstage<TS>(p, kDr, at) : zero;
+      issue();
+      st = st + 1 == kStages ? 0 : st + 1;
+      if (s.pre == ACID_NORM_LAYER || s.post == ACID_NORM_LAYER) {
+        const float4 t = sums.sum<2>(total(n), total(y));
+        if (s.pre == ACID_NORM_LAYER) plus(n, -(t.x / d), at);
+        if (s.post == ACID_NORM_LAYER) plus(y, -(t.y / d), at);
       }
-      if (a.y == nullptr) continue;
-      float p[8] = {};
-      if (on) row8<TB>(a.y, a.ldy, row, s.rows, c, p);
-      const float inv = norm_row(p, s.post, on, d, s.eps, red, round);
-      if (on) vec8(s.post_w, c, d, 1.f, w);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        T[j] = fmaf(dr[j], p[j], T[j]);
-        dr[j] = on ? dr[j] * gp[j] * w[j] : 0.f;
+      FOR_PAIRS A.v[i] = f2_add(A.v[i], du.v[i]);
+      // S takes du n before du becomes dn = du (1 + scale) pre_w, so the root comes first
+      Cols dn = du;
+      times(dn, sc);
+      float in = 1.f, ip = 1.f, mean = 0.f, along = 0.f;
+      if (s.pre != ACID_NORM_NONE || s.post != ACID_NORM_NONE) {
+        const float4 t = sums.sum<4>(dot(n, n), dot(y, y), total(dn), dot(dn, n));
+        if (s.pre != ACID_NORM_NONE) {
+          in = rsqrtf(fmaf(t.x, per_d, s.eps));
+          mean = s.pre == ACID_NORM_LAYER ? t.z * per_d : 0.f;
+          along = t.w * in * in * per_d;
+        }
+        if (s.post != ACID_NORM_NONE) ip = rsqrtf(fmaf(t.y, per_d, s.eps));
+      }
+      FOR_PAIRS {
+        S.v[i] = f2_fma(f2_mul(du.v[i], f2_same(in)), n.v[i], S.v[i]);
+        dn.v[i] = f2_fma(n.v[i], f2_same(-along), dn.v[i]);
+      }
+      plus(dn, -mean, at);
+      FOR_PAIRS {
+        dr.v[i] = f2_fma(f2_same(in), dn.v[i], dr.v[i]);
+        y.v[i] = f2_mul(y.v[i], f2_same(ip));
+        T.v[i] = f2_fma(dr.v[i], y.v[i], T.v[i]);
+      }
+      if (a.dx != nullptr) {
+        Cols o;
+        FOR_PAIRS o.v[i] = f2_mul(dr.v[i], f2_same(s.res));
+        put(static_cast<TS*>(a.dx) + row * a.lddx, at, o, row, s.rows);
       }
       if (a.dy == nullptr) continue;
-      norm_back(dr, p, inv, s.post, on, d, red, round);
-      if (on) put8<TB>(a.dy, a.lddy, row, s.rows, c, dr);
+      times(dr, gw);
+      if (s.post != ACID_NORM_NONE) {
+        const float4 t = sums.sum<2>(total(dr), dot(dr, y));
+        FOR_PAIRS dr.v[i] = f2_fma(y.v[i], f2_same(-t.y * per_d), dr.v[i]);
+        if (s.post == ACID_NORM_LAYER) plus(dr, -t.x * per_d, at);
+        FOR_PAIRS dr.v[i] = f2_mul(dr.v[i], f2_same(ip));
+      }
+      put(static_cast<TB*>(a.dy) + row * a.lddy, at, dr, row, s.rows);
     }
-    if (!on) continue;
+    if (weights) {  // dpre_w gathers (1 + scale) S, dpost_w branch_scale gate T
+      const Cols f = scale_cols(s, m, at), h = gate_cols(s, m, at);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      W[0][j] = fmaf(sc[j], S[j], W[0][j]);
-      W[1][j] = fmaf(gp[j], T[j], W[1][j]);
+      for (int i = 0; i < 4; ++i) {
+        ulonglong2& p = wsum[i * blockDim.x];
+        ulonglong2& q = wsum[(4 + i) * blockDim.x];
+        p = make_ulonglong2(f2_fma(f.v[2 * i], S.v[2 * i], p.x), f2_fma(f.v[2 * i + 1], S.v[2 * i + 1], p.y));
+        q = make_ulonglong2(f2_fma(h.v[2 * i], T.v[2 * i], q.x), f2_fma(h.v[2 * i + 1], T.v[2 * i + 1], q.y));
+      }
     }
-    const bool starts = group_begin(s, g) == from, ends = group_end(s, g) == to;
+    const bool starts = group_begin(s, g) == from, ends = group_end(s, g) == last;
     if (starts && ends) {
-      put_group(a, g, c, A, S, T);
+      put_sums(a, 0, g, m, at, A);
+      put_sums(a, 1, g, m, at, S);
+      put_sums(a, 2, g, m, at, T);
     } else {
-      float* slot = a.part + (2 * (int64_t)blockIdx.x + starts) * 3 * d + c;
-      store8(slot, A);
-      store8(slot + d, S);
-      store8(slot + 2 * d, T);
+      const int64_t i = 2 * (int64_t)blockIdx.x + starts, slots = 2 * (int64_t)gridDim.x;
+      float* slot = a.part + i * 3 * s.d;
+      put(slot, at, A, i, slots);
+      put(slot + s.d, at, S, i, slots);
+      put(slot + 2 * s.d, at, T, i, slots);
     }
   }
-  if (!on) return;
-  float* wp = a.wpart + (int64_t)blockIdx.x * 2 * d + c;
-  store8(wp, W[0]);
-  store8(wp + d, W[1]);
+  if (!weights) return;
+  float* wp = a.wpart + (int64_t)blockIdx.x * 2 * s.d;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    Cols v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const ulonglong2 p = wsum[(4 * w + i) * blockDim.x];
+      v.v[2 * i] = p.x;
+      v.v[2 * i + 1] = p.y;
+    }
+    put(wp + w * s.d, at, v, blockIdx.x, gridDim.x);
+  }
 }
 
-// Joins the CTAs' sums in the CTAs' order: blockIdx.y < ctas: the group that
-// begins in that CTA and reaches past its end (if there is one); y = ctas: the
-// weights' gradients.
-__global__ void __launch_bounds__(128) site_join_kernel(SiteBwd a, int ctas) {
+// Adds the CTAs' slots in the CTAs' order.  A job is one vector of one group
+// that reaches over an edge (jobs counted by groups, or by CTAs where these are
+// fewer: the group that begins in the CTA and leaves it), or one of the two
+// weights' gradients.  `segs` warps share a job's slots, a lane takes a column.
+constexpr int kJoinWarps = 16;
+__global__ void __launch_bounds__(32 * kJoinWarps) site_join_kernel(SiteBwd a, int ctas, int jobs, int segs,
+                                                                   bool by_cta) {
+  __shared__ float part[kJoinWarps][32];
   pdl_wait();
   const Site& s = a.s;
-  const int c = (blockIdx.x * 128 + threadIdx.x) * 8, d = s.d;
-  if (c >= d) return;
-  float v[3][8] = {}, t[8];
-  if ((int)blockIdx.y == ctas) {
-    for (int b = 0; b < ctas; ++b)
-      for (int i = 0; i < 2; ++i) {
-        load8(a.wpart + ((int64_t)b * 2 + i) * d + c, t);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] += t[j];
-      }
-    if (a.dpre_w != nullptr) store8(a.dpre_w + c, v[0]);
-    if (a.dpost_w != nullptr) store8(a.dpost_w + c, v[1]);
-    return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, seg = warp % segs;
+  const int c = blockIdx.x * 32 + lane, d = s.d, job = blockIdx.y * (kJoinWarps / segs) + warp / segs;
+  const int which = job / jobs;  // 0 .. 2: dshift, dscale, dgate; 3, 4: dpre_w, dpost_w
+  int64_t g = 0, lo = 0, hi = -1;  // slots lo .. hi
+  if (which < 3) {
+    const int64_t i = job - which * jobs;
+    g = by_cta ? group_of(s, min(s.rows, (i + 1) * a.per) - 1) : i;
+    lo = group_begin(s, g) / a.per;
+    hi = (group_end(s, g) - 1) / a.per;
+    if (lo == hi || (by_cta && lo != i)) hi = lo - 1;  // finished by its CTA, or another job's
+  } else if (job - 3 * jobs < 2) {
+    hi = ctas - 1;
   }
-  const int64_t b = blockIdx.y, end = min(s.rows, (b + 1) * a.per), g = group_of(s, end - 1);
-  if (group_end(s, g) <= end || group_begin(s, g) < b * a.per) return;
-  const int64_t last = (group_end(s, g) - 1) / a.per;
-  for (int64_t k = b; k <= last; ++k)
-    for (int i = 0; i < 3; ++i) {
-      load8(a.part + ((2 * k + (k == b)) * 3 + i) * d + c, t);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] += t[j];
-    }
-  put_group(a, g, c, v[0], v[1], v[2]);
+  float v = 0.f;
+  if (c < d) {
+    const float* base = which < 3 ? a.part + which * d : a.wpart + (job - 3 * jobs) * d;
+    const int64_t width = which < 3 ? 6 * (int64_t)d : 2 * (int64_t)d;
+#pragma unroll 8
+    for (int64_t k = lo + seg; k <= hi; k += segs)
+      v += base[k * width + (which < 3 && k == lo ? 3 * d : 0) + c];
+  }
+  part[warp][lane] = v;
+  __syncthreads();
+  if (seg != 0 || c >= d || hi < lo) return;
+  float t = 0.f;
+  for (int i = 0; i < segs; ++i) t += part[warp + i][lane];
+  if (which < 3) {
+    put_sum(a, which, g, c, t);
+  } else {
+    float* out = job - 3 * jobs == 0 ? a.dpre_w : a.dpost_w;
+    if (out != nullptr) out[c] = t;
+  }
 }
 
-constexpr int kMaxCtas = 1024;
+constexpr int kMaxCtas = 2048;  // of the backward pass (workspace)
 
 int64_t num_groups(const acid_norm_site& s) {
   const int64_t rest = s.rows - s.first_rows;
@@ -353,7 +566,7 @@ acid_status check_site(const acid_norm_site* s) {
   ACID_REQUIRE(known_dtype(s->stream_dtype) && known_dtype(s->branch_dtype), ACID_ERR_INVALID_ARG,
                "norm_site: unknown dtype");
   ACID_REQUIRE(known_norm(s->post_norm) && known_norm(s->pre_norm), ACID_ERR_INVALID_ARG, "norm_site: unknown norm");
-  ACID_REQUIRE(s->rows >= 0 && s->d > 0 && s->rows <= (int64_t(1) << 40), ACID_ERR_INVALID_ARG, "norm_site: bad shape");
+  ACID_REQUIRE(s->rows >= 0 && s->d > 0 && s->rows <= (int64_t(1) << 39), ACID_ERR_INVALID_ARG, "norm_site: bad shape");
   ACID_REQUIRE(s->d % 8 == 0 && s->d <= kMaxWidth, ACID_ERR_UNSUPPORTED,
                "norm_site: d must be a multiple of 8, <= 4096");
   ACID_REQUIRE(s->first_rows >= 0 && s->first_rows <= s->rows && s->group_rows >= 0, ACID_ERR_INVALID_ARG,
@@ -400,17 +613,26 @@ Site site_args(const acid_norm_site& s) {
   return a;
 }
 
-int threads_for(int d) { return (d + 255) / 256 * 32; }
+int threads_for(int d) { return (d + 511) / 512 * 32; }
 
-// Rows of a CTA of the backward pass, and the CTAs.
-struct Split {
-  int64_t per;
-  int ctas;
-};
-Split split_rows(int64_t rows, int most) {
-  const int64_t per = std::max<int64_t>(1, (rows + most - 1) / most);
-  return {per, (int)((rows + per - 1) / per)};
+constexpr size_t kMaxSmem = 200 * 1024;
+// CTAs that an SM keeps of a kernel with so much shared memory; sets the kernel
+// up in the context.  (An occupancy query at each launch would take longer than
+// the smallest kernels.)
+template <typename K>
+acid_status ctas_per_sm(PerContext& known, K kernel, int threads, size_t smem, int* ctas) {
+  int regs = 0;
+  ACID_TRY(known.get(&regs, [&](int* v) {
+    ACID_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxSmem));
+    cudaFuncAttributes f = {};
+    ACID_CUDA(cudaFuncGetAttributes(&f, kernel));
+    *v = f.numRegs > 0 ? (f.numRegs + 7) / 8 * 8 : 256;
+    return ACID_OK;
+  }));
+  *ctas = (int)std::max<size_t>(1, std::min<size_t>({(size_t)65536 / (threads * regs), 224 * 1024 / (smem + 1536), 24}));
+  return ACID_OK;
 }
+size_t part_bytes(int d, int ctas) { return (size_t)ctas * 2 * 3 * d * sizeof(float); }
 
 template <template <typename, typename> class F, typename A>
 acid_status by_types(const acid_norm_site& s, const A& a) {
@@ -425,28 +647,62 @@ struct FwdLaunch {
 };
 template <typename TS, typename TB>
 struct RunFwd {
-  static acid_status run(const FwdLaunch& l) {
-    const unsigned grid = (unsigned)std::min<int64_t>(l.a.s.rows, (int64_t)num_sms() * 8);
-    launch_pdl(site_forward_kernel<TS, TB>, grid, threads_for(l.a.s.d), 0, l.s, l.a);
+  static acid_status run(const FwdLaunch& l) { return l.a.y != nullptr ? go<true>(l) : go<false>(l); }
+  template <bool BRANCH>
+  static acid_status go(const FwdLaunch& l) {
+    static PerContext known;
+    const Site& s = l.a.s;
+    const int threads = threads_for(s.d);
+    const size_t smem = (size_t)kFwdStages * threads * 16 * (kPlanes<TS> + (BRANCH ? kPlanes<TB> : 0));
+    int fit;
+    ACID_TRY(ctas_per_sm(known, site_forward_kernel<TS, TB, BRANCH>, threads, smem, &fit));
+    const int64_t most = (int64_t)num_sms() * fit;
+    const int64_t ctas = std::min(s.rows, most), per = (s.rows + ctas - 1) / ctas;
+    const bool strided = s.groups == 1;
+    launch_pdl(site_forward_kernel<TS, TB, BRANCH>, (unsigned)(strided ? ctas : (s.rows + per - 1) / per), threads,
+               smem, l.s, l.a, strided ? int64_t(1) : per, strided ? ctas : int64_t(1), (uint32_t)per);
     ACID_CHECK_LAUNCH();
     return ACID_OK;
   }
 };
 struct BwdLaunch {
   SiteBwd a;
-  int ctas;
   cudaStream_t s;
 };
 template <typename TS, typename TB>
 struct RunBwd {
   static acid_status run(const BwdLaunch& l) {
-    launch_pdl(site_backward_kernel<TS, TB>, l.ctas, threads_for(l.a.s.d), 0, l.s, l.a);
+    static PerContext known;
+    SiteBwd a = l.a;
+    const Site& s = a.s;
+    const int threads = threads_for(s.d);
+    const size_t smem = (size_t)threads * (kBwdStages<TS, TB> * 16 * 2 * (kPlanes<TS> + kPlanes<TB>) + 128);
+    int fit;
+    ACID_TRY(ctas_per_sm(known, site_backward_kernel<TS, TB>, threads, smem, &fit));
+    const int64_t most = std::min<int64_t>(kMaxCtas, (int64_t)num_sms() * fit);
+    a.per = std::max<int64_t>(1, (s.rows + most - 1) / most);
+    const int ctas = (int)((s.rows + a.per - 1) / a.per);
+    a.wpart = a.part + part_bytes(s.d, ctas) / sizeof(float);
+    launch_pdl(site_backward_kernel<TS, TB>, ctas, threads, smem, l.s, a);
+    ACID_CHECK_LAUNCH();
+    const bool weights = a.dpre_w != nullptr || a.dpost_w != nullptr;
+    const bool vectors = a.dgate != nullptr || a.dscale != nullptr || a.dshift != nullptr;
+    // does any group reach over an edge?
+    const int64_t head = s.first > 0 ? s.first : 0, longest = std::max(head, std::min(s.group, s.rows - head));
+    if (!weights && (!vectors || (longest == 1))) return ACID_OK;
+    const bool by_cta = s.groups > ctas;
+    const int jobs = by_cta ? ctas : (int)s.groups;
+    const int64_t span = std::max<int64_t>(longest / a.per + 2, weights ? ctas : 0);
+    int segs = 1;
+    while (segs < kJoinWarps && segs * 8 < span) segs *= 2;
+    const int per_cta = kJoinWarps / segs;
+    launch_pdl(site_join_kernel, dim3((s.d + 31) / 32, (3 * jobs + 2 + per_cta - 1) / per_cta), 32 * kJoinWarps, 0, l.s, a,
+               ctas, jobs, segs, by_cta);
     ACID_CHECK_LAUNCH();
     return ACID_OK;
   }
 };
 
-size_t part_bytes(int d, int ctas) { return (size_t)ctas * 2 * 3 * d * sizeof(float); }
 size_t workspace_bytes(const acid_norm_site& s) {
   const int ctas = (int)std::min<int64_t>(kMaxCtas, std::max<int64_t>(s.rows, 1));
   return part_bytes(s.d, ctas) + (size_t)ctas * 2 * s.d * sizeof(float);
@@ -527,13 +783,8 @@ extern "C" acid_status acid_norm_site_backward(const acid_norm_site* site, const
   const size_t need = workspace_bytes(*site);
   ACID_REQUIRE(ws_bytes >= need, ACID_ERR_WORKSPACE,
                "acid_norm_site_backward: workspace too small (need " + std::to_string(need) + ")");
-  const Split sp = split_rows(site->rows, std::min(kMaxCtas, num_sms() * 2));
-  BwdLaunch l{{site_args(*site), du, r, y, dr, lddu, ldr, ldy, lddr, o.dx, o.dy, o.lddx, o.lddy, o.dgate, o.dscale,
-               o.dshift, o.dpost_w, o.dpre_w, o.ld_dmod, static_cast<float*>(ws), nullptr, sp.per},
-              sp.ctas, s};
-  l.a.wpart = l.a.part + part_bytes(site->d, sp.ctas) / sizeof(float);
-  ACID_TRY(by_types<RunBwd>(*site, l));
-  launch_pdl(site_join_kernel, dim3((site->d / 8 + 127) / 128, sp.ctas + 1), 128, 0, s, l.a, sp.ctas);
-  ACID_CHECK_LAUNCH();
-  return ACID_OK;
+  const BwdLaunch l{{site_args(*site), du, r, y, dr, lddu, ldr, ldy, lddr, o.dx, o.dy, o.lddx, o.lddy, o.dgate, o.dscale,
+                     o.dshift, o.dpost_w, o.dpre_w, o.ld_dmod, static_cast<float*>(ws), nullptr, 1},
+                    s};
+  return by_types<RunBwd>(*site, l);
 }
