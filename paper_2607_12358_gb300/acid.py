@@ -429,8 +429,11 @@ def acid_q4_dequantize(weight: Q4Weight, dtype=torch.float32, out: torch.Tensor 
 
 
 def acid_q4_linear_forward(x: torch.Tensor, weight: Q4Weight, bias: torch.Tensor | None = None, silu: bool = False,
-                           out: torch.Tensor | None = None, out_dtype=torch.float32, stream=None) -> torch.Tensor:
-    """out [m, n] = a(x [m, k]) W^T + bias, a = SiLU with ``silu``; bias fp32 [n]."""
+                           out: torch.Tensor | None = None, out_dtype=torch.float32,
+                           workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """out [m, n] = a(x [m, k]) W^T + bias, a = SiLU with ``silu``; bias fp32 [n].  ``workspace``:
+    q4_linear_workspace_size bytes, not needed up to four rows with
+    m k <= 16384."""
     m = x.shape[0]
     ldx = _matrix("x", x, m, weight.k)
     if bias is not None and not (bias.is_cuda and bias.dtype == torch.float32 and bias.shape == (weight.n,)
@@ -438,8 +441,11 @@ def acid_q4_linear_forward(x: torch.Tensor, weight: Q4Weight, bias: torch.Tensor
         raise ValueError("bias must be a contiguous CUDA fp32 tensor [n]")
     out = torch.empty((m, weight.n), dtype=out_dtype, device=x.device) if out is None else out
     ldo = _matrix("out", out, m, weight.n)
+    if workspace is None and (m > 4 or m * weight.k > 16384):
+        workspace = torch.empty(q4_linear_workspace_size(weight, m), dtype=torch.uint8, device=x.device)
     check(load().acid_q4_linear_forward(_DT[x.dtype], x.data_ptr(), ldx, m, C.byref(weight.struct), _ptr(bias),
-                                        bool(silu), _DT[out.dtype], out.data_ptr(), ldo, _stream(stream)))
+                                        bool(silu), _DT[out.dtype], out.data_ptr(), ldo, _ptr(workspace),
+                                        0 if workspace is None else workspace.numel(), _stream(stream)))
     return out
 
 

@@ -376,7 +376,7 @@ __device__ __forceinline__ void put_sums(const SiteBwd& a, int which, int64_t g,
 template <typename TS, typename TB>
 constexpr int kBwdStages = sizeof(TS) + sizeof(TB) == 8 ? 2 : 3;
 template <typename TS, typename TB>
-__global__ void __launch_bounds__(32 * kMaxWarps, 1) site_backward_kernel(SiteBwd a) {
+__global__ void __launch_bounds__(384, 1) site_backward_kernel(SiteBwd a) {
   constexpr int kStages = kBwdStages<TS, TB>;
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float4 red[2][kMaxWarps];
@@ -629,7 +629,8 @@ acid_status ctas_per_sm(PerContext& known, K kernel, int threads, size_t smem, i
     *v = f.numRegs > 0 ? (f.numRegs + 7) / 8 * 8 : 256;
     return ACID_OK;
   }));
-  *ctas = (int)std::max<size_t>(1, std::min<size_t>({(size_t)65536 / (threads * regs), 224 * 1024 / (smem + 1536), 24}));
+  const size_t warps = 4 * (512 / (size_t)regs);  // each of the four schedulers holds 512 registers of 32 lanes
+  *ctas = (int)std::max<size_t>(1, std::min<size_t>({warps * 32 / threads, 224 * 1024 / (smem + 1536), 24}));
   return ACID_OK;
 }
 size_t part_bytes(int d, int ctas) { return (size_t)ctas * 2 * 3 * d * sizeof(float); }

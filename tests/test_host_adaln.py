@@ -115,19 +115,20 @@ def test_q4_refusals(lib):
         a.update(kw)
         return C.byref(A.acid_q4_weight(**a))
 
-    def fwd(xt=A.ACID_FP32, x=P, ldx=256, m=3, bias=None, ot=A.ACID_FP32, out=P, ldo=100, **kw):
-        return L.acid_q4_linear_forward(xt, x, ldx, m, weight(**kw), bias, 1, ot, out, ldo, None)
+    def fwd(xt=A.ACID_FP32, x=P, ldx=256, m=3, bias=None, ot=A.ACID_FP32, out=P, ldo=100, ws=None, nws=0, **kw):
+        return L.acid_q4_linear_forward(xt, x, ldx, m, weight(**kw), bias, 1, ot, out, ldo, ws, nws, None)
 
     for kw, want in ((dict(n=0), INV), (dict(n=1 << 31), INV), (dict(k=0), INV), (dict(k=65537), INV),
                      (dict(group=48), UNS), (dict(group=0), UNS), (dict(scale_dtype=3), INV), (dict(packed=None), INV),
                      (dict(scales=None), INV), (dict(packed=P + 4), UNS), (dict(scales=P + 1), UNS),
                      (dict(n=(1 << 31) - 1, k=65536, ldx=65536, ldo=1 << 31), UNS), (dict(xt=5), INV), (dict(x=None), INV),
                      (dict(x=P + 2), UNS), (dict(ldx=255), INV), (dict(m=-1), INV), (dict(m=32769), INV),
-                     (dict(ot=7), INV), (dict(out=None), INV), (dict(ldo=99), INV), (dict(bias=P + 2), UNS)):
+                     (dict(ot=7), INV), (dict(out=None), INV), (dict(ldo=99), INV), (dict(bias=P + 2), UNS),
+                     (dict(m=5), WS), (dict(m=5, ws=P + 8, nws=1 << 20), WS), (dict(m=5, ws=P, nws=100), WS)):
         assert fwd(**kw) == want, kw
         assert L.acid_last_error()
     assert fwd(m=0, x=None, out=None) == A.ACID_OK
-    assert L.acid_q4_linear_forward(A.ACID_FP32, P, 256, 3, None, None, 0, A.ACID_FP32, P, 100, None) == INV
+    assert L.acid_q4_linear_forward(A.ACID_FP32, P, 256, 3, None, None, 0, A.ACID_FP32, P, 100, None, 0, None) == INV
     b = C.c_size_t()
     assert L.acid_q4_linear_workspace_size(weight(), 5, C.byref(b)) == A.ACID_OK and b.value > 0
     assert L.acid_q4_linear_workspace_size(weight(), -1, C.byref(b)) == INV
