@@ -247,13 +247,45 @@ def norm_site_groups(rows: int, first_rows: int = 0, group_rows: int = 0) -> int
     return (first_rows > 0) + -(-rest // (group_rows or max(rest, 1)))
 
 
+# These calls are a few microseconds of GPU work on small sites, so their checks are written to cost little: plain
+# comparisons on the way through, the messages formed only where one fails.
+_F32 = torch.float32
+_empty = torch.empty
+
+
 def _rows_of(name: str, t: torch.Tensor, rows: int, d: int, dtype) -> int:
-    """Row stride of an operand [rows, d] (0 for none)."""
-    if t is None:
-        return 0
-    if not t.is_cuda or t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != d or t.stride(1) != 1:
+    """Row stride of an operand [rows, d]."""
+    ld = t.stride()
+    if t.dtype is not dtype or not t.is_cuda or t.shape != (rows, d) or ld[1] != 1:
         raise ValueError(f"{name} must be a CUDA tensor [{rows}, {d}] of {dtype} with contiguous rows")
-    return t.stride(0) if rows > 1 else d
+    return ld[0] if rows > 1 else d
+
+
+def _group_vectors(gate, scale, shift, groups, d):
+    """(pointers, row stride) of the vectors of a site's groups."""
+    ld, ptrs = 0, []
+    for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
+        if t is None:
+            ptrs.append(None)
+            continue
+        st, shape = t.stride(), t.shape
+        if t.dtype is not _F32 or not t.is_cuda or st[-1] != 1 or not (
+                shape == (groups, d) or (groups == 1 and shape == (d,))):
+            raise ValueError(f"{name} must be a CUDA fp32 tensor [{groups}, {d}] with contiguous rows")
+        if groups > 1:
+            if ld and ld != st[0]:
+                raise ValueError("gate, scale and shift must have one row stride")
+            ld = st[0]
+        ptrs.append(t.data_ptr())
+    return ptrs, ld
+
+
+def _column_vector(name: str, t: torch.Tensor, d: int):
+    if t is None:
+        return None
+    if t.dtype is not _F32 or not t.is_cuda or t.shape != (d,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous CUDA fp32 tensor [{d}]")
+    return t.data_ptr()
 
 
 def _site(rows, d, stream_dtype, branch_dtype, gate, scale, shift, post_w, pre_w, post_norm, pre_norm, eps, res_scale,
@@ -262,26 +294,10 @@ def _site(rows, d, stream_dtype, branch_dtype, gate, scale, shift, post_w, pre_w
     if not 0 <= first_rows <= rows or group_rows < 0:
         raise ValueError("need 0 <= first_rows <= rows and group_rows >= 0")
     groups = norm_site_groups(rows, first_rows, group_rows)
-    ld, ptrs = 0, []
-    for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
-        if t is None:
-            ptrs.append(None)
-            continue
-        shape = t.shape
-        if not t.is_cuda or t.dtype != torch.float32 or t.stride(-1) != 1 or shape[-1] != d or not (
-                (len(shape) == 2 and shape[0] == groups) or (len(shape) == 1 and groups == 1)):
-            raise ValueError(f"{name} must be a CUDA fp32 tensor [{groups}, {d}] with contiguous rows")
-        if groups > 1:
-            if ld and ld != t.stride(0):
-                raise ValueError("gate, scale and shift must have one row stride")
-            ld = t.stride(0)
-        ptrs.append(t.data_ptr())
-    for name, t in (("post_w", post_w), ("pre_w", pre_w)):
-        if t is not None and not (t.is_cuda and t.dtype == torch.float32 and t.shape == (d,) and t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous CUDA fp32 tensor [{d}]")
+    ptrs, ld = _group_vectors(gate, scale, shift, groups, d)
     return A.acid_norm_site(rows, d, _DT[stream_dtype], _DT[branch_dtype], _NORM[post_norm], _NORM[pre_norm],
-                            bool(gate_tanh), eps, res_scale, branch_scale, first_rows, group_rows, *ptrs, ld,
-                            _ptr(post_w), _ptr(pre_w)), groups
+                            gate_tanh, eps, res_scale, branch_scale, first_rows, group_rows, ptrs[0], ptrs[1], ptrs[2],
+                            ld, _column_vector("post_w", post_w, d), _column_vector("pre_w", pre_w, d)), groups
 
 
 def acid_norm_site_forward(x: torch.Tensor, y: torch.Tensor | None = None, *, gate: torch.Tensor | None = None,
@@ -295,22 +311,35 @@ def acid_norm_site_forward(x: torch.Tensor, y: torch.Tensor | None = None, *, ga
     g = gate or tanh(gate).  x, r [rows, d] of the stream's dtype, y, u of the branch's (branch_dtype where y is None);
     gate, scale, shift fp32 [groups, d] (norm_site_groups).  r and u are allocated unless given (r may be x, u may be
     y); want_r / want_u False leave one out (None)."""
-    if x.dim() != 2 or x.dtype not in _DT:
+    xdt = x.dtype
+    if x.dim() != 2 or xdt not in _DT:
         raise ValueError("x must be a [rows, d] tensor of bf16 or fp32")
     rows, d = x.shape
-    bdt = y.dtype if y is not None else branch_dtype or x.dtype
+    bdt = y.dtype if y is not None else branch_dtype or xdt
     if bdt not in _DT:
         raise TypeError(f"unsupported dtype {bdt}")
-    site, _ = _site(rows, d, x.dtype, bdt, gate, scale, shift, post_w, pre_w, post_norm, pre_norm, eps, res_scale,
+    ldx = _rows_of("x", x, rows, d, xdt)
+    site, _ = _site(rows, d, xdt, bdt, gate, scale, shift, post_w, pre_w, post_norm, pre_norm, eps, res_scale,
                     branch_scale, gate_tanh, first_rows, group_rows)
-    if r is None and want_r:
-        r = torch.empty((rows, d), dtype=x.dtype, device=x.device)
-    if u is None and want_u:
-        u = torch.empty((rows, d), dtype=bdt, device=x.device)
-    ldx, ldy = _rows_of("x", x, rows, d, x.dtype), _rows_of("y", y, rows, d, bdt)
-    ldr, ldu = _rows_of("r", r, rows, d, x.dtype), _rows_of("u", u, rows, d, bdt)
-    check(load().acid_norm_site_forward(C.byref(site), x.data_ptr(), ldx, _ptr(y), ldy, _ptr(r), ldr, _ptr(u), ldu,
-                                        _stream(stream)))
+    yp = rp = up = None
+    ldy = ldr = ldu = d
+    if y is not None:
+        ldy, yp = _rows_of("y", y, rows, d, bdt), y.data_ptr()
+    if r is not None:
+        ldr = _rows_of("r", r, rows, d, xdt)
+    elif want_r:
+        r = _empty((rows, d), dtype=xdt, device=x.device)
+    if u is not None:
+        ldu = _rows_of("u", u, rows, d, bdt)
+    elif want_u:
+        u = _empty((rows, d), dtype=bdt, device=x.device)
+    if r is not None:
+        rp = r.data_ptr()
+    if u is not None:
+        up = u.data_ptr()
+    status = load().acid_norm_site_forward(C.byref(site), x.data_ptr(), ldx, yp, ldy, rp, ldr, up, ldu, _stream(stream))
+    if status:
+        check(status)
     return r, u
 
 
@@ -331,39 +360,60 @@ def acid_norm_site_backward(du: torch.Tensor | None, r: torch.Tensor | None, y: 
     """Gradients of acid_norm_site_forward from du (of u) and dr (of r), with the forward call's r and y and its other
     arguments: a dict of dx, dy and, with ``vectors``, dgate, dscale, dshift [groups, d], dpost_w, dpre_w [d] (those
     whose input is given; dshift where scale or shift is)."""
-    like = next((t for t in (r, dr) if t is not None), None)
+    like = dr if r is None else r
     if like is None or like.dim() != 2 or like.dtype not in _DT:
         raise ValueError("need r or dr, [rows, d] of bf16 or fp32")
     rows, d = like.shape
-    bdt = y.dtype if y is not None else du.dtype if du is not None else like.dtype
+    sdt, dev = like.dtype, like.device
+    bdt = y.dtype if y is not None else du.dtype if du is not None else sdt
     if bdt not in _DT:
         raise TypeError(f"unsupported dtype {bdt}")
-    site, groups = _site(rows, d, like.dtype, bdt, gate, scale, shift, post_w, pre_w, post_norm, pre_norm, eps,
-                         res_scale, branch_scale, gate_tanh, first_rows, group_rows)
-    dev = like.device
-    out = {"dx": torch.empty((rows, d), dtype=like.dtype, device=dev) if dx is None else dx}
+    site, groups = _site(rows, d, sdt, bdt, gate, scale, shift, post_w, pre_w, post_norm, pre_norm, eps, res_scale,
+                         branch_scale, gate_tanh, first_rows, group_rows)
+    dup = rp = yp = drp = dyp = dgate = dscale = dshift = dpost = dpre = None
+    lddu = ldr = ldy = lddr = lddx = lddy = d
+    out = {}
+    if dx is None:
+        dx = _empty((rows, d), dtype=sdt, device=dev)
+    else:
+        lddx = _rows_of("dx", dx, rows, d, sdt)
+    out["dx"] = dx
+    if r is not None:
+        ldr, rp = _rows_of("r", r, rows, d, sdt), r.data_ptr()
+    if dr is not None:
+        lddr, drp = _rows_of("dr", dr, rows, d, sdt), dr.data_ptr()
     if y is not None:
-        out["dy"] = torch.empty((rows, d), dtype=bdt, device=dev) if dy is None else dy
-    if vectors:
-        want = [n for n, t in (("dgate", gate if y is not None else None), ("dscale", scale if du is not None else None),
-                               ("dshift", (scale if shift is None else shift) if du is not None else None))
-                if t is not None]
-        if want:
-            out.update(zip(want, torch.empty((len(want), groups, d), dtype=torch.float32, device=dev).unbind(0)))
-        if post_w is not None and y is not None:
-            out["dpost_w"] = torch.empty(d, dtype=torch.float32, device=dev)
-        if pre_w is not None and du is not None:
-            out["dpre_w"] = torch.empty(d, dtype=torch.float32, device=dev)
-    ws = torch.empty(norm_site_workspace_size(site), dtype=torch.uint8, device=dev) if workspace is None else workspace
-    get = out.get
-    grads = A.acid_norm_site_grads(out["dx"].data_ptr(), _rows_of("dx", out["dx"], rows, d, like.dtype),
-                                   _ptr(get("dy")), _rows_of("dy", get("dy"), rows, d, bdt), _ptr(get("dgate")),
-                                   _ptr(get("dscale")), _ptr(get("dshift")), d, _ptr(get("dpost_w")),
-                                   _ptr(get("dpre_w")))
-    check(load().acid_norm_site_backward(C.byref(site), _ptr(du), _rows_of("du", du, rows, d, bdt), _ptr(r),
-                                         _rows_of("r", r, rows, d, like.dtype), _ptr(y), _rows_of("y", y, rows, d, bdt),
-                                         _ptr(dr), _rows_of("dr", dr, rows, d, like.dtype), C.byref(grads),
-                                         ws.data_ptr(), ws.numel(), _stream(stream)))
+        ldy, yp = _rows_of("y", y, rows, d, bdt), y.data_ptr()
+        if dy is None:
+            dy = _empty((rows, d), dtype=bdt, device=dev)
+        else:
+            lddy = _rows_of("dy", dy, rows, d, bdt)
+        out["dy"] = dy
+        dyp = dy.data_ptr()
+        if vectors and gate is not None:
+            t = out["dgate"] = _empty((groups, d), dtype=_F32, device=dev)
+            dgate = t.data_ptr()
+        if vectors and post_w is not None:
+            t = out["dpost_w"] = _empty(d, dtype=_F32, device=dev)
+            dpost = t.data_ptr()
+    if du is not None:
+        lddu, dup = _rows_of("du", du, rows, d, bdt), du.data_ptr()
+        if vectors and scale is not None:
+            t = out["dscale"] = _empty((groups, d), dtype=_F32, device=dev)
+            dscale = t.data_ptr()
+        if vectors and (scale is not None or shift is not None):
+            t = out["dshift"] = _empty((groups, d), dtype=_F32, device=dev)
+            dshift = t.data_ptr()
+        if vectors and pre_w is not None:
+            t = out["dpre_w"] = _empty(d, dtype=_F32, device=dev)
+            dpre = t.data_ptr()
+    if workspace is None:
+        workspace = _empty(norm_site_workspace_size(site), dtype=torch.uint8, device=dev)
+    grads = A.acid_norm_site_grads(dx.data_ptr(), lddx, dyp, lddy, dgate, dscale, dshift, d, dpost, dpre)
+    status = load().acid_norm_site_backward(C.byref(site), dup, lddu, rp, ldr, yp, ldy, drp, lddr, C.byref(grads),
+                                            workspace.data_ptr(), workspace.numel(), _stream(stream))
+    if status:
+        check(status)
     return out
 
 
@@ -380,26 +430,28 @@ class Q4Weight:
 
     def __init__(self, packed: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor | None, n: int, k: int,
                  group: int):
-        per_row = -(-k // group) if group > 0 else 0
-        if not (packed.is_cuda and packed.dtype == torch.uint8 and packed.is_contiguous()
-                and packed.numel() == n * 64 * -(-k // 128)):
+        slabs = -(-k // 128)
+        number = n * -(-k // group) if group > 0 else 0
+        if packed.dtype is not torch.uint8 or not packed.is_cuda or not packed.is_contiguous() \
+                or packed.numel() != n * 64 * slabs:
             raise ValueError("packed must be a contiguous CUDA uint8 tensor [n, 64 ceil(k / 128)]")
-        if not (scales.is_cuda and scales.dtype in _DT and scales.is_contiguous() and scales.numel() == n * per_row):
+        sdt = scales.dtype
+        if sdt not in _DT or not scales.is_cuda or not scales.is_contiguous() or scales.numel() != number:
             raise ValueError("scales must be a contiguous CUDA bf16 or fp32 tensor [n, ceil(k / group)]")
-        if zeros is not None and not (zeros.is_cuda and zeros.dtype == torch.uint8 and zeros.is_contiguous()
-                                      and zeros.numel() == n * per_row):
+        if zeros is not None and (zeros.dtype is not torch.uint8 or not zeros.is_cuda or not zeros.is_contiguous()
+                                  or zeros.numel() != number):
             raise ValueError("zeros must be a contiguous CUDA uint8 tensor [n, ceil(k / group)]")
         self.packed, self.scales, self.zeros, self.n, self.k, self.group = packed, scales, zeros, n, k, group
-        self.struct = A.acid_q4_weight(packed.data_ptr(), scales.data_ptr(), _ptr(zeros), n, k, group,
-                                       _DT[scales.dtype])
+        self.struct = A.acid_q4_weight(packed.data_ptr(), scales.data_ptr(),
+                                       None if zeros is None else zeros.data_ptr(), n, k, group, _DT[sdt])
 
 
 def _matrix(name: str, t: torch.Tensor, rows: int, cols: int) -> int:
     """Row stride of an operand [rows, cols]."""
-    if not t.is_cuda or t.dtype not in _DT or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (
-            t.stride(1) != 1 and cols > 1):
+    ld = t.stride()
+    if t.dtype not in _DT or not t.is_cuda or t.shape != (rows, cols) or (ld[1] != 1 and cols > 1):
         raise ValueError(f"{name} must be a CUDA tensor [{rows}, {cols}] of bf16 or fp32 with contiguous rows")
-    return max(t.stride(0), cols) if rows > 1 else cols
+    return max(ld[0], cols) if rows > 1 else cols
 
 
 def acid_q4_quantize(w: torch.Tensor, group: int = 128, zeros: bool = False, scale_dtype=torch.bfloat16,
@@ -434,18 +486,22 @@ def acid_q4_linear_forward(x: torch.Tensor, weight: Q4Weight, bias: torch.Tensor
     """out [m, n] = a(x [m, k]) W^T + bias, a = SiLU with ``silu``; bias fp32 [n].  ``workspace``:
     q4_linear_workspace_size bytes, not needed up to four rows with
     m k <= 16384."""
-    m = x.shape[0]
-    ldx = _matrix("x", x, m, weight.k)
-    if bias is not None and not (bias.is_cuda and bias.dtype == torch.float32 and bias.shape == (weight.n,)
-                                 and bias.is_contiguous()):
-        raise ValueError("bias must be a contiguous CUDA fp32 tensor [n]")
-    out = torch.empty((m, weight.n), dtype=out_dtype, device=x.device) if out is None else out
-    ldo = _matrix("out", out, m, weight.n)
-    if workspace is None and (m > 4 or m * weight.k > 16384):
-        workspace = torch.empty(q4_linear_workspace_size(weight, m), dtype=torch.uint8, device=x.device)
-    check(load().acid_q4_linear_forward(_DT[x.dtype], x.data_ptr(), ldx, m, C.byref(weight.struct), _ptr(bias),
-                                        bool(silu), _DT[out.dtype], out.data_ptr(), ldo, _ptr(workspace),
-                                        0 if workspace is None else workspace.numel(), _stream(stream)))
+    m, n, k = x.shape[0], weight.n, weight.k
+    ldx, ldo = _matrix("x", x, m, k), n
+    bp, ws, nws = _column_vector("bias", bias, n), None, 0
+    if out is None:
+        out = _empty((m, n), dtype=out_dtype, device=x.device)
+    else:
+        out_dtype = out.dtype
+        ldo = _matrix("out", out, m, n)
+    if workspace is None and (m > 4 or m * k > 16384):
+        workspace = _empty(q4_linear_workspace_size(weight, m), dtype=torch.uint8, device=x.device)
+    if workspace is not None:
+        ws, nws = workspace.data_ptr(), workspace.numel()
+    status = load().acid_q4_linear_forward(_DT[x.dtype], x.data_ptr(), ldx, m, C.byref(weight.struct), bp, silu,
+                                           _DT[out_dtype], out.data_ptr(), ldo, ws, nws, _stream(stream))
+    if status:
+        check(status)
     return out
 
 
@@ -460,24 +516,33 @@ def acid_q4_linear_backward(g: torch.Tensor, weight: Q4Weight, x: torch.Tensor |
                             dx_dtype=torch.float32, workspace: torch.Tensor | None = None, stream=None):
     """(dx [m, k], dbias [n]) of acid_q4_linear_forward from g [m, n], the gradient of its output, and x, its input
     (needed with ``silu``; dx has its dtype, dx_dtype without it).  want_dx / want_dbias False leave one out (None)."""
-    m, dev = g.shape[0], g.device
-    ldg = _matrix("g", g, m, weight.n)
-    ldx = 0 if x is None else _matrix("x", x, m, weight.k)
-    if silu and x is None and want_dx:
+    m, n, k, dev = g.shape[0], weight.n, weight.k, g.device
+    ldg = _matrix("g", g, m, n)
+    xp = dxp = bp = ws = dbias = None
+    ldx, lddx, nws = k, k, 0
+    if x is not None:
+        ldx, xp, dx_dtype = _matrix("x", x, m, k), x.data_ptr(), x.dtype
+    elif silu and want_dx:
         raise ValueError("silu needs x")
-    dbias = torch.empty(weight.n, dtype=torch.float32, device=dev) if want_dbias else None
-    if want_dx and dx is None:
-        dx = torch.empty((m, weight.k), dtype=dx_dtype if x is None else x.dtype, device=dev)
-    lddx = 0 if dx is None else _matrix("dx", dx, m, weight.k)
-    if dx is not None and x is not None and dx.dtype != x.dtype:
-        raise ValueError("dx must have the dtype of x")
-    ws = workspace
-    if ws is None and dx is not None:
-        ws = torch.empty(q4_linear_workspace_size(weight, m), dtype=torch.uint8, device=dev)
-    xdt = x.dtype if x is not None else dx.dtype if dx is not None else torch.float32
-    check(load().acid_q4_linear_backward(_DT[g.dtype], g.data_ptr(), ldg, m, C.byref(weight.struct), _DT[xdt],
-                                         _ptr(x), ldx, bool(silu), _ptr(dx), lddx, _ptr(dbias), _ptr(ws),
-                                         0 if ws is None else ws.numel(), _stream(stream)))
+    if want_dbias:
+        dbias = _empty(n, dtype=_F32, device=dev)
+        bp = dbias.data_ptr()
+    if dx is not None:
+        lddx = _matrix("dx", dx, m, k)
+        if x is not None and dx.dtype is not dx_dtype:
+            raise ValueError("dx must have the dtype of x")
+        dx_dtype = dx.dtype
+    elif want_dx:
+        dx = _empty((m, k), dtype=dx_dtype, device=dev)
+    if dx is not None:
+        dxp = dx.data_ptr()
+        if workspace is None:
+            workspace = _empty(q4_linear_workspace_size(weight, m), dtype=torch.uint8, device=dev)
+        ws, nws = workspace.data_ptr(), workspace.numel()
+    status = load().acid_q4_linear_backward(_DT[g.dtype], g.data_ptr(), ldg, m, C.byref(weight.struct), _DT[dx_dtype], xp,
+                                            ldx, silu, dxp, lddx, bp, ws, nws, _stream(stream))
+    if status:
+        check(status)
     return dx, dbias
 
 
