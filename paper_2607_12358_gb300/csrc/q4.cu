@@ -68,6 +68,14 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// The same from zero: D = A B.
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                              uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
   asm volatile(
@@ -179,11 +187,188 @@ __device__ __forceinline__ void halves_of(uint32_t w, uint32_t z1, uint32_t z64,
   d[3] = bits(__hfma2(half2_of((v & 0x00f000f0u) | 0x64006400u), sixteenth, __hneg2(half2_of(z64))));
 }
 
-// A warp takes 32 rows of the weight (two tiles) and every kw-th slab of their
-// columns; the CTA's 8 / kw row tiles are neighbours.  A lane reads 16 bytes of four
-// rows: word i of them holds its columns of the slab's 32 columns i, so that
-// four lanes' words make a tile's step of 16 columns twice.
-template <int NT, bool PACKED, typename TS>
+// The four pairs of a word as halves q - 8: what halves_of gives without a zero
+// point, which the few-rows kernel takes into account by the sum of a(x) over
+// the group, sum x (q - z) = sum x (q - 8) + (8 - z) sum x.
+__device__ __forceinline__ void halves_of(uint32_t w, uint32_t (&d)[4]) { halves_of(w, 0x64086408u, 0x54805480u, d); }
+
+// Where a warp reads its row tile: 32 rows g, g + 8, g + 16, g + 24 of a lane, rows
+// past the end as the last one.
+struct TileRows {
+  const uint4* q[4];
+  int64_t s[4];
+};
+__device__ __forceinline__ TileRows tile_rows(const Q4& w, int64_t tile, int g, int t) {
+  TileRows r;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int64_t row = min(tile * 32 + g + 8 * q, w.n - 1);
+    r.q[q] = reinterpret_cast<const uint4*>(w.packed) + row * w.slabs * 4 + t;
+    r.s[q] = row * w.groups;
+  }
+  return r;
+}
+
+// A few rows: a CTA's warps split a row tile's slabs among kw of them, and 8 / kw
+// row tiles are neighbours.  A lane reads 16 bytes of four rows: word i of them
+// holds its columns of the slab's 32 columns i, so that four lanes' words make a
+// tile's step of 16 columns twice.
+template <typename TS, bool ZEROS>
+__global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  const Q4& w = a.w;
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, warp = warp_index();
+  const int kw = a.kw, rw = kThreads / 32 / kw, kwarp = warp % kw, rwarp = warp / kw;
+  const int rows = (int)a.m, cols = 2 * rows;
+  uint4* frag = reinterpret_cast<uint4*>(smem);                                   // [slab][word][column][t]
+  float* back = reinterpret_cast<float*>(smem + (size_t)w.slabs * 16 * cols * 16);  // [slab][row]
+  float* xsum = back + w.slabs * kPackedRows;                                     // [slab][32 columns][row]
+  float* red = xsum + (ZEROS ? 4 * w.slabs * kPackedRows : 0);                    // [8 warps][row][33]
+  const int64_t tiles = (w.n + 31) / 32, sets = (tiles + rw - 1) / rw;
+  const int mine = (w.slabs - kwarp + kw - 1) / kw;  // slabs of this warp
+  const int per_slab = 128 >> w.group_log, lane_group = t >> (w.group_log - 5);
+  struct Load {
+    uint4 q[4];
+    float s[4];
+    uint8_t z[4];
+  };
+  pdl_wait();
+  // this warp's steps (row set, slab), two fetched ahead
+  int64_t set = blockIdx.x, fset = set;
+  int k = 0, fslab = kwarp;
+  TileRows at = tile_rows(w, fset * rw + rwarp, g, t);
+  auto next = [&](Load& l) {
+    if (fset < sets) {
+      const int group = min(fslab * per_slab + lane_group, w.groups - 1);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint4* p = at.q[q] + fslab * 4;
+        if (ACID_IN_BOUNDS(kSiteQ4, (p - reinterpret_cast<const uint4*>(w.packed)) * 4 + 3, w.n * w.slabs * 16))
+          l.q[q] = load_stream(p);
+        if (ACID_IN_BOUNDS(kSiteQ4, at.s[q] + group, w.n * w.groups)) {
+          l.s[q] = io<TS>::ld(static_cast<const TS*>(w.scales) + at.s[q] + group);
+          if constexpr (ZEROS) l.z[q] = w.zeros[at.s[q] + group];
+        }
+      }
+    }
+    fslab += kw;
+    if (fslab >= w.slabs) {
+      fslab = kwarp;
+      fset += gridDim.x;
+      if (fset < sets) at = tile_rows(w, fset * rw + rwarp, g, t);
+    }
+  };
+  Load l[2];
+  next(l[0]);
+  next(l[1]);
+  // a(x) in parts, while the first weights are on their way
+  {
+    const int per_row = w.slabs * 16, all = per_row * rows;
+    for (int base = threadIdx.x & ~31; base < all; base += kThreads) {
+      const int i = base + lane, m = i / per_row, o = i - m * per_row;
+      float v[8];
+      const float by = octet_of(a, m, o * 8, v);
+      float sum = 0.f;
+      if constexpr (ZEROS) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += v[j];
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      }
+      if (m >= rows) continue;
+      uint4 hi, lo;
+      split_octet(v, by, hi, lo);
+      uint4* p = frag + ((o >> 2) * cols + 2 * m) * 4 + (o & 3);
+      p[0] = hi;
+      p[4] = lo;
+      if ((o & 15) == 0) back[(o >> 4) * kPackedRows + m] = 1.f / by;
+      if (ZEROS && (o & 3) == 0) xsum[(o >> 2) * kPackedRows + m] = sum;
+    }
+    __syncthreads();
+  }
+  float sum[2][2];  // row t of the input, rows g + 8 h + 16 r of the tile
+  auto clear = [&] { sum[0][0] = sum[0][1] = sum[1][0] = sum[1][1] = 0.f; };
+  const uint4* mine_b = frag + (g < cols ? g * 4 + t : 0);
+  auto compute = [&](const Load& l, int slab) {
+    const float bk = back[slab * kPackedRows + t];
+    float acc[2][4], xs = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint4 b = mine_b[(slab * 4 + i) * cols * 4];
+      if (g >= cols) b = make_uint4(0, 0, 0, 0);
+      const bool first = (i << 5 & ((1 << w.group_log) - 1)) == 0;
+      if (ZEROS) xs = (first ? 0.f : xs) + xsum[(slab * 4 + i) * kPackedRows + t];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        uint32_t d[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint4& v = l.q[2 * r + h];
+          halves_of(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w, d[h]);
+        }
+        if (first)
+          mma_f16_first(acc[r], d[0][0], d[1][0], d[0][1], d[1][1], b.x, b.y);
+        else
+          mma_f16(acc[r], d[0][0], d[1][0], d[0][1], d[1][1], b.x, b.y);
+        mma_f16(acc[r], d[0][2], d[1][2], d[0][3], d[1][3], b.z, b.w);
+      }
+      if (((i + 1) << 5 & ((1 << w.group_log) - 1)) == 0) {  // the group ends
+        const int from = (lane & ~3) | (i >> (w.group_log - 5) << (w.group_log - 5));  // a lane that has its scale
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int q = 2 * r + h;
+            const float s = __shfl_sync(0xffffffffu, l.s[q], from);
+            float v = (acc[r][2 * h] + acc[r][2 * h + 1]) * bk;  // both parts of row t are in this lane
+            if constexpr (ZEROS)
+              v = fmaf((float)(8 - (int)__shfl_sync(0xffffffffu, (uint32_t)l.z[q], from)), xs, v);
+            sum[r][h] = fmaf(s, v, sum[r][h]);
+          }
+      }
+    }
+  };
+  auto put = [&](int64_t row, int m, float v) {
+    if (row < w.n && m < rows)
+      put_value(a.out_dtype, a.out, m * a.ldo + row, v + (a.bias != nullptr ? a.bias[row] : 0.f));
+  };
+  auto finish = [&] {
+    if (kw == 1) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) put((set * rw + rwarp) * 32 + 8 * q + g, t, sum[q >> 1][q & 1]);
+      return;
+    }
+    __syncthreads();  // the buffer's last readers are done
+#pragma unroll
+    for (int q = 0; q < 4; ++q) red[(warp * kPackedRows + t) * 33 + 8 * q + g] = sum[q >> 1][q & 1];
+    __syncthreads();
+    for (int i = threadIdx.x; i < rw * rows * 32; i += kThreads) {
+      const int row = i & 31, m = (i >> 5) % rows, rt = (i >> 5) / rows;
+      float v = 0.f;
+      for (int j = 0; j < kw; ++j) v += red[((rt * kw + j) * kPackedRows + m) * 33 + row];
+      put((set * rw + rt) * 32 + row, m, v);
+    }
+  };
+  clear();
+  auto step = [&](Load& cur) {
+    if (set >= sets) return;
+    compute(cur, kwarp + k * kw);
+    next(cur);
+    if (++k == mine) {
+      finish();
+      clear();
+      k = 0;
+      set += gridDim.x;
+    }
+  };
+  while (set < sets) {
+    step(l[0]);
+    step(l[1]);
+  }
+}
+
+// More rows: the same tiles of the weight against 8 NT columns of parts.
+template <int NT, typename TS>
 __global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) q4_forward_kernel(Fwd a) {
   extern __shared__ __align__(16) uint8_t smem[];
   pdl_wait();
@@ -191,28 +376,8 @@ __global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) q4_forward_kernel(F
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, warp = warp_index();
   const int kw = a.kw, rw = kThreads / 32 / kw, kwarp = warp % kw, rwarp = warp / kw;
   const int64_t chunk = blockIdx.y, m0 = chunk * kChunk;
-  const int cols = (int)a.m * 2;  // (PACKED)
-  uint4* frag = reinterpret_cast<uint4*>(smem);
-  float* back = reinterpret_cast<float*>(smem + (PACKED ? (size_t)w.slabs * 16 * cols * 16 : 0));
-  if constexpr (PACKED) {
-    const int per_row = w.slabs * 16, all = per_row * (int)a.m;
-    for (int base = threadIdx.x & ~31; base < all; base += kThreads) {
-      const int i = base + lane, m = i / per_row, o = i - m * per_row;
-      float v[8];
-      const float by = octet_of(a, m, o * 8, v);
-      if (m >= a.m) continue;
-      uint4 hi, lo;
-      split_octet(v, by, hi, lo);
-      uint4* p = frag + ((o >> 2) * cols + 2 * m) * 4 + (o & 3);
-      p[0] = hi;
-      p[4] = lo;
-      if ((o & 15) == 0) back[(o >> 4) * kPackedRows + m] = 1.f / by;
-    }
-    __syncthreads();
-  }
-  // partial sums of the warps that share rows: [8 warps][32 rows][columns]
-  constexpr int kCols = PACKED ? kPackedRows : NT * 8;
-  float* red = back + (PACKED ? w.slabs * kPackedRows : 0);
+  constexpr int kCols = NT * 8;
+  float* red = reinterpret_cast<float*>(smem);  // [8 warps][column][33]: sums of the warps that share rows
 
   const int64_t tiles = (w.n + 31) / 32, sets = (tiles + rw - 1) / rw;
   const int mine = (w.slabs - kwarp + kw - 1) / kw;  // slabs of this warp
@@ -240,15 +405,10 @@ __global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) q4_forward_kernel(F
   auto compute = [&](const Load& l, int slab) {
     float bk[NT][2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      if constexpr (PACKED) {
-        bk[0][0] = back[slab * kPackedRows + t];
-      } else {
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-          bk[n][e] = m0 + 8 * n + 2 * t + e < a.m ? a.back[(m0 + 8 * n + 2 * t + e) * w.slabs + slab] : 0.f;
-      }
-    }
+      for (int e = 0; e < 2; ++e)
+        bk[n][e] = m0 + 8 * n + 2 * t + e < a.m ? a.back[(m0 + 8 * n + 2 * t + e) * w.slabs + slab] : 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int from = (lane & ~3) | (i >> (w.group_log - 5) << (w.group_log - 5));  // a lane that has the group's scale
@@ -261,23 +421,14 @@ __global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) q4_forward_kernel(F
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        if constexpr (PACKED) {
-          const uint4 b = g < cols ? frag[((slab * 4 + i) * cols + g) * 4 + t] : make_uint4(0, 0, 0, 0);
+        const uint4* p = a.parts + (((chunk * w.slabs + slab) * 4 + i) * 2 * NT * 8 + n * 8 + g) * 4 + t;
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+          const uint4 b = p[part * NT * 8 * 4];
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
             mma_f16(acc[r][n], d[2 * r][0], d[2 * r + 1][0], d[2 * r][1], d[2 * r + 1][1], b.x, b.y);
             mma_f16(acc[r][n], d[2 * r][2], d[2 * r + 1][2], d[2 * r][3], d[2 * r + 1][3], b.z, b.w);
-          }
-        } else {
-          const uint4* p = a.parts + (((chunk * w.slabs + slab) * 4 + i) * 2 * NT * 8 + n * 8 + g) * 4 + t;
-#pragma unroll
-          for (int part = 0; part < 2; ++part) {
-            const uint4 b = p[part * NT * 8 * 4];
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-              mma_f16(acc[r][n], d[2 * r][0], d[2 * r + 1][0], d[2 * r][1], d[2 * r + 1][1], b.x, b.y);
-              mma_f16(acc[r][n], d[2 * r][2], d[2 * r + 1][2], d[2 * r][3], d[2 * r + 1][3], b.z, b.w);
-            }
           }
         }
       }
@@ -288,21 +439,12 @@ __global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) q4_forward_kernel(F
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const float s = sc[2 * r + h];
-              if constexpr (PACKED) {  // both parts of row t are in this lane
-                sum[r][n][h] = fmaf(s, (acc[r][n][2 * h] + acc[r][n][2 * h + 1]) * bk[0][0], sum[r][n][h]);
-              } else {
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                  sum[r][n][2 * h + e] = fmaf(s, acc[r][n][2 * h + e] * bk[n][e], sum[r][n][2 * h + e]);
-              }
+            for (int e = 0; e < 4; ++e) {
+              sum[r][n][e] = fmaf(sc[2 * r + (e >> 1)], acc[r][n][e] * bk[n][e & 1], sum[r][n][e]);
+              acc[r][n][e] = 0.f;
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[r][n][e] = 0.f;
-          }
       }
     }
   };
@@ -310,22 +452,13 @@ __global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) q4_forward_kernel(F
     if (row < w.n && m0 + m < a.m)
       put_value(a.out_dtype, a.out, (m0 + m) * a.ldo + row, v + (a.bias != nullptr ? a.bias[row] : 0.f));
   };
-  // the sums of a row tile: v(r, n, e, row of the tile, column) in every lane that has them
-  auto each = [&](auto&& f) {
+  auto each = [&](auto&& f) {  // f(sum, row of the tile, column)
 #pragma unroll
     for (int r = 0; r < 2; ++r)
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int row = 16 * r + 8 * h + g;
-          if constexpr (PACKED) {
-            f(sum[r][n][h], row, t);
-          } else {
-            f(sum[r][n][2 * h], row, 8 * n + 2 * t);
-            f(sum[r][n][2 * h + 1], row, 8 * n + 2 * t + 1);
-          }
-        }
+        for (int e = 0; e < 4; ++e) f(sum[r][n][e], 16 * r + 8 * (e >> 1) + g, 8 * n + 2 * t + (e & 1));
   };
   auto finish = [&](int64_t set) {
     const int64_t row0 = (set * rw + rwarp) * 32;
@@ -613,74 +746,172 @@ __global__ void __launch_bounds__(kThreads) q4_backward_join_kernel(Bwd a) {
 }
 
 // ---------------------------------------------------------------- quantiser
-// max of two values; a NaN wins
-__device__ __forceinline__ float max_or_nan(float a, float b) { return a != a ? a : b != b ? b : fmaxf(a, b); }
+// A lane takes eight columns of a row (one word), a warp 32 such octets of one
+// row at a time: two slabs, whose groups are 4, 8 or 16 lanes.
+constexpr int kUnits = 4;  // octet runs of a warp, all loaded before the first is worked on
+struct Runs {
+  int64_t n;    // runs: n rows of per_row
+  int per_row;
+};
+__host__ __device__ inline Runs runs_of(int64_t rows, int k) {
+  const int per_row = (k + 255) / 256;
+  return {rows * per_row, per_row};
+}
 
-// A warp takes 128 columns of a row, four a lane; a group is 8, 16 or 32 lanes.
+// the larger of two values; a NaN wins
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+// Code of v in 0 .. 15: rint(v / s) + z.  The quotient comes from a product with
+// inv = 1 / s, off by less than 2^-22 of it, and is rounded to even by the sum with
+// 1.5 2^23; only within 1e-4 of the middle of two codes (and where inv is no use)
+// does the division decide.
+__device__ __forceinline__ uint32_t code_of(float v, float s, float inv, int z) {
+  constexpr float kRound = 12582912.f;
+  float q = v * inv, r = q + kRound;
+  if (!(fabsf(q - (r - kRound)) < 0.4999f)) {
+    q = fminf(fmaxf(rintf(v / s), -64.f), 64.f);  // (a NaN becomes -64)
+    r = q + kRound;
+  }
+  return (uint32_t)min(max((int)(__float_as_uint(r) - __float_as_uint(kRound)) + z, 0), 15);
+}
+
 template <typename TW, typename TS>
 __global__ void __launch_bounds__(kThreads) q4_quantize_kernel(const TW* W, int64_t ldw, Q4 w, uint32_t* packed,
-                                                               TS* scales, uint8_t* zeros) {
+                                                               TS* scales, uint8_t* zeros, bool wide) {
   pdl_wait();
   const int lane = threadIdx.x & 31;
-  const int64_t unit = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-  if (unit >= w.n * w.slabs) return;
-  const int64_t row = unit / w.slabs;
-  const int slab = (int)(unit - row * w.slabs), col = slab * 128 + lane * 4;
-  float v[4], hi = 0.f, lo = 0.f;  // lo: -min(w, 0)
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    v[j] = col + j < w.k ? io<TW>::ld(W + row * ldw + col + j) : 0.f;
-    hi = max_or_nan(hi, v[j]);
-    lo = max_or_nan(lo, -v[j]);
-  }
-  const int span = 1 << (w.group_log - 2);  // lanes of a group
-  for (int o = span >> 1; o > 0; o >>= 1) {
-    hi = max_or_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    lo = max_or_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-  }
+  const Runs runs = runs_of(w.n, w.k);
+  const int64_t first = ((int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * kUnits;
   const bool asym = zeros != nullptr;
-  TS st;
-  io<TS>::st(&st, asym ? (hi + lo) / 15.f : max_or_nan(hi, lo) / 7.f);
-  const float s = io<TS>::ld(&st), div = s == 0.f ? 1.f : s;
-  const float z = asym ? fminf(fmaxf(rintf(lo / div), 0.f), 15.f) : 8.f;
-  uint32_t q = 0;
+  const int span = 1 << (w.group_log - 3);  // lanes of a group
+  float v[kUnits][8];
+  int64_t row = first / runs.per_row;
+  int at = (int)(first - row * runs.per_row);
+  const int64_t row0 = row;
+  const int at0 = at;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) q |= (uint32_t)fminf(fmaxf(rintf(v[j] / div) + z, 0.f), 15.f) << (4 * j);
-  const uint32_t other = __shfl_down_sync(0xffffffffu, q, 1);
-  if ((lane & 1) == 0) {
-    const int64_t at = row * w.slabs * 16 + column_word(col >> 3);
-    if (ACID_IN_BOUNDS(kSiteQ4, at, w.n * w.slabs * 16)) packed[at] = q | other << 16;
+  for (int u = 0; u < kUnits; ++u) {
+    const int col = (at * 32 + lane) * 8;
+    const bool in = first + u < runs.n;
+    if (in && wide && col + 8 <= w.k && ACID_IN_BOUNDS(kSiteQ4, row, w.n)) {
+      load8(W + row * ldw + col, v[u]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[u][j] = in && col + j < w.k ? io<TW>::ld(W + row * ldw + col + j) : 0.f;
+    }
+    if (++at == runs.per_row) {
+      at = 0;
+      ++row;
+    }
   }
-  if ((lane & (span - 1)) == 0 && col < w.k) {
-    const int64_t at = row * w.groups + (col >> w.group_log);
-    if (ACID_IN_BOUNDS(kSiteQ4, at, w.n * w.groups)) {
-      scales[at] = st;
-      if (asym) zeros[at] = (uint8_t)z;
+  row = row0;
+  at = at0;
+#pragma unroll
+  for (int u = 0; u < kUnits; ++u) {
+    if (first + u >= runs.n) break;
+    const int octet = at * 32 + lane, col = octet * 8;
+    float hi = 0.f, lo = 0.f;  // max(w, 0) and -min(w, 0), or max |w|
+#pragma unroll
+    for (int j = 0; j < 8; ++j) hi = max_or_nan(hi, asym ? v[u][j] : fabsf(v[u][j]));
+    if (asym)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) lo = max_or_nan(lo, -v[u][j]);
+    for (int o = span >> 1; o > 0; o >>= 1) {
+      hi = max_or_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+      if (asym) lo = max_or_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    }
+    TS st;
+    io<TS>::st(&st, asym ? (hi + lo) / 15.f : hi / 7.f);
+    const float s = io<TS>::ld(&st), div = s == 0.f ? 1.f : s, inv = 1.f / div;
+    const int z = asym ? (int)fminf(fmaxf(rintf(lo / div), 0.f), 15.f) : 8;
+    uint32_t q = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q |= code_of(v[u][j], div, inv, z) << (4 * j);
+    if (octet < w.slabs * 16) {
+      const int64_t p = row * w.slabs * 16 + column_word(octet);
+      if (ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.slabs * 16)) packed[p] = q;
+    }
+    if ((lane & (span - 1)) == 0 && col < w.k) {
+      const int64_t p = row * w.groups + (col >> w.group_log);
+      if (ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.groups)) {
+        scales[p] = st;
+        if (asym) zeros[p] = (uint8_t)z;
+      }
+    }
+    if (++at == runs.per_row) {
+      at = 0;
+      ++row;
     }
   }
 }
 
-template <typename TS, typename TO>
-__global__ void __launch_bounds__(kThreads) q4_dequantize_kernel(Q4 w, TO* out, int64_t ldo, bool wide) {
-  pdl_wait();
-  const int octets = (w.k + 7) / 8;
-  const int64_t unit = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (unit >= w.n * octets) return;
-  const int64_t row = unit / octets;
-  const int o = (int)(unit - row * octets), col = o * 8;
-  const uint32_t word = word_at(w, row, column_word(o));
-  const float s = scale_at<TS>(w, row, col);
-  const int z = zero_at(w, row, col);
-  float v[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = s * (float)((int)(word >> (4 * j) & 15u) - z);
-  TO* p = out + row * ldo + col;
-  if (wide && col + 8 <= w.k) {
-    store8(p, v);
+// 32 bytes with one store where the address allows it: a lane's own sector.
+__device__ __forceinline__ void store_octet(float* p, const float* v, bool sector) {
+  if (sector) {
+    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+                 "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                 : "memory");
   } else {
+    store8(p, v);
+  }
+}
+__device__ __forceinline__ void store_octet(bf16* p, const float* v, bool) { store8(p, v); }
+
+template <typename TS, typename TO>
+__global__ void __launch_bounds__(kThreads) q4_dequantize_kernel(Q4 w, TO* out, int64_t ldo, bool wide, bool sector) {
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const Runs runs = runs_of(w.n, w.k);
+  const int64_t first = ((int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * kUnits;
+  int64_t row = first / runs.per_row;
+  int at = (int)(first - row * runs.per_row);
+  uint32_t word[kUnits];
+  float s[kUnits];
+  int z[kUnits];
+  const int64_t row0 = row;
+  const int at0 = at;
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (col + j < w.k) io<TO>::st(p + j, v[j]);
+  for (int u = 0; u < kUnits; ++u) {
+    const int octet = at * 32 + lane;
+    word[u] = 0;
+    s[u] = 0.f;
+    z[u] = 8;
+    if (first + u < runs.n && octet * 8 < w.k) {
+      word[u] = word_at(w, row, column_word(octet));
+      s[u] = scale_at<TS>(w, row, octet * 8);
+      z[u] = zero_at(w, row, octet * 8);
+    }
+    if (++at == runs.per_row) {
+      at = 0;
+      ++row;
+    }
+  }
+  row = row0;
+  at = at0;
+#pragma unroll
+  for (int u = 0; u < kUnits; ++u) {
+    const int col = (at * 32 + lane) * 8;
+    if (first + u < runs.n && col < w.k) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)  // 2^23 + q is the float with q in its last bits
+        v[j] = s[u] * (__uint_as_float((word[u] >> (4 * j) & 15u) | 0x4B000000u) - (8388608.f + (float)z[u]));
+      TO* p = out + row * ldo + col;
+      if (wide && col + 8 <= w.k) {
+        if (ACID_IN_BOUNDS(kSiteQ4, row, w.n)) store_octet(p, v, sector);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (col + j < w.k) io<TO>::st(p + j, v[j]);
+      }
+    }
+    if (++at == runs.per_row) {
+      at = 0;
+      ++row;
+    }
   }
 }
 
@@ -755,22 +986,36 @@ size_t workspace_bytes(const acid_q4_weight& w, int64_t m) {
   return std::max<size_t>({16, fwd_bytes(w, m), bwd_bytes(w, m)});
 }
 
-template <int NT, bool PACKED, typename TS>
+// Warps of a CTA that share a row's columns: as many as give every SM eight warps
+// where the rows alone would not.
+int sharing_warps(const Q4& w) {
+  int kw = 1;
+  while (kw < 8 && 2 * kw <= w.slabs && (w.n + 31) / 32 * kw < 8 * num_sms()) kw *= 2;
+  return kw;
+}
+template <typename TS, bool ZEROS>
+acid_status launch_few(Fwd a, cudaStream_t s) {
+  static PerContext allowed;
+  a.kw = sharing_warps(a.w);
+  const int rw = kThreads / 32 / a.kw;
+  const size_t smem = (size_t)a.w.slabs * (512 * a.m + 4 * kPackedRows * (ZEROS ? 5 : 1)) +
+                      (a.kw == 1 ? 0 : 8 * kPackedRows * 33 * sizeof(float));
+  ACID_TRY(allow_smem(allowed, q4_few_kernel<TS, ZEROS>, 110 * 1024));
+  const int64_t sets = ((a.w.n + 31) / 32 + rw - 1) / rw;
+  launch_pdl(q4_few_kernel<TS, ZEROS>, (unsigned)std::min<int64_t>(sets, (int64_t)num_sms() * 2), kThreads, smem, s, a);
+  ACID_CHECK_LAUNCH();
+  return ACID_OK;
+}
+template <int NT, typename TS>
 acid_status launch_forward(Fwd a, cudaStream_t s) {
   static PerContext allowed;
-  const auto kernel = q4_forward_kernel<NT, PACKED, TS>;
-  const int64_t tiles = (a.w.n + 31) / 32;
-  // Warps share a row's columns where the rows alone would not give every SM eight warps.
-  a.kw = 1;
-  while (a.kw < 8 && 2 * a.kw <= a.w.slabs && tiles * a.kw < 8 * num_sms()) a.kw *= 2;
+  a.kw = sharing_warps(a.w);
   const int rw = kThreads / 32 / a.kw;
-  const size_t red = a.kw == 1 ? 0 : (size_t)8 * (PACKED ? kPackedRows : NT * 8) * 33 * sizeof(float);
-  const size_t frag = PACKED ? (size_t)a.w.slabs * (512 * a.m + 4 * kPackedRows) : 0;
-  ACID_TRY(allow_smem(allowed, kernel, 220 * 1024));
-  const int64_t sets = (tiles + rw - 1) / rw;
-  const int per_sm = NT <= 2 && 2 * (red + frag + 1024) <= 220 * 1024 ? 2 : 1;
-  const dim3 grid((unsigned)std::min<int64_t>(sets, (int64_t)num_sms() * per_sm), (unsigned)chunks_of(a.m));
-  launch_pdl(kernel, grid, kThreads, red + frag, s, a);
+  const size_t smem = a.kw == 1 ? 0 : (size_t)8 * NT * 8 * 33 * sizeof(float);
+  ACID_TRY(allow_smem(allowed, q4_forward_kernel<NT, TS>, 8 * NT * 8 * 33 * sizeof(float)));
+  const int64_t sets = ((a.w.n + 31) / 32 + rw - 1) / rw;
+  const dim3 grid((unsigned)std::min<int64_t>(sets, (int64_t)num_sms() * (NT <= 2 ? 2 : 1)), (unsigned)chunks_of(a.m));
+  launch_pdl(q4_forward_kernel<NT, TS>, grid, kThreads, smem, s, a);
   ACID_CHECK_LAUNCH();
   return ACID_OK;
 }
@@ -779,7 +1024,7 @@ acid_status launch_parts_forward(const Fwd& a, bool half_scales, cudaStream_t s)
   const int64_t octets = a.m * a.w.slabs * 16;
   launch_pdl(q4_parts_kernel<NT>, (unsigned)((octets + kThreads - 1) / kThreads), kThreads, 0, s, a);
   ACID_CHECK_LAUNCH();
-  return half_scales ? launch_forward<NT, false, bf16>(a, s) : launch_forward<NT, false, float>(a, s);
+  return half_scales ? launch_forward<NT, bf16>(a, s) : launch_forward<NT, float>(a, s);
 }
 
 template <int NT, int IW, bool PACKED>
@@ -813,14 +1058,16 @@ extern "C" acid_status acid_q4_quantize(int32_t w_dtype, const void* W, int64_t 
   ACID_TRY(check_matrix(w_dtype, W, ldw, weight->k, "W"));
   cudaStream_t s = (cudaStream_t)stream;
   const Q4 w = q4_args(*weight);
-  const unsigned grid = (unsigned)((w.n * w.slabs + kThreads / 32 - 1) / (kThreads / 32));
+  const bool wide = aligned(W, 16) && ldw % 8 == 0;
+  const int64_t per_cta = kThreads / 32 * kUnits;
+  const unsigned grid = (unsigned)((runs_of(w.n, w.k).n + per_cta - 1) / per_cta);
   auto packed = static_cast<uint32_t*>(const_cast<void*>(weight->packed));
   auto scales = const_cast<void*>(weight->scales);
   auto zeros = const_cast<uint8_t*>(weight->zeros);
   auto launch = [&](auto* src, auto* sc) {
     launch_pdl(q4_quantize_kernel<std::remove_const_t<std::remove_pointer_t<decltype(src)>>,
                                   std::remove_pointer_t<decltype(sc)>>,
-               grid, kThreads, 0, s, src, ldw, w, packed, sc, zeros);
+               grid, kThreads, 0, s, src, ldw, w, packed, sc, zeros, wide);
   };
   auto by_scale = [&](auto* src) {
     if (weight->scale_dtype == ACID_BF16)
@@ -844,15 +1091,16 @@ extern "C" acid_status acid_q4_dequantize(const acid_q4_weight* weight, int32_t 
   ACID_TRY(check_matrix(out_dtype, out, ldo, weight->k, "out"));
   cudaStream_t s = (cudaStream_t)stream;
   const Q4 w = q4_args(*weight);
-  const unsigned grid = (unsigned)((w.n * ((w.k + 7) / 8) + kThreads - 1) / kThreads);
-  const bool wide = aligned(out, 16) && ldo % 8 == 0;
+  const int64_t per_cta = kThreads / 32 * kUnits;
+  const unsigned grid = (unsigned)((runs_of(w.n, w.k).n + per_cta - 1) / per_cta);
+  const bool wide = aligned(out, 16) && ldo % 8 == 0, sector = wide && aligned(out, 32);
   const bool h = weight->scale_dtype == ACID_BF16;
   if (out_dtype == ACID_BF16)
     launch_pdl(h ? q4_dequantize_kernel<bf16, bf16> : q4_dequantize_kernel<float, bf16>, grid, kThreads, 0, s, w,
-               static_cast<bf16*>(out), ldo, wide);
+               static_cast<bf16*>(out), ldo, wide, sector);
   else
     launch_pdl(h ? q4_dequantize_kernel<bf16, float> : q4_dequantize_kernel<float, float>, grid, kThreads, 0, s, w,
-               static_cast<float*>(out), ldo, wide);
+               static_cast<float*>(out), ldo, wide, sector);
   ACID_CHECK_LAUNCH();
   return ACID_OK;
 }
@@ -878,7 +1126,10 @@ extern "C" acid_status acid_q4_linear_forward(int32_t x_dtype, const void* x, in
   a.back = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + parts_bytes(*weight, M));
   const bool h = weight->scale_dtype == ACID_BF16;
   cudaStream_t s = (cudaStream_t)stream;
-  if (need == 0) return h ? launch_forward<1, true, bf16>(a, s) : launch_forward<1, true, float>(a, s);
+  if (need == 0) {
+    if (weight->zeros != nullptr) return h ? launch_few<bf16, true>(a, s) : launch_few<float, true>(a, s);
+    return h ? launch_few<bf16, false>(a, s) : launch_few<float, false>(a, s);
+  }
   switch (tiles_for(M)) {
     case 1: return launch_parts_forward<1>(a, h, s);
     case 2: return launch_parts_forward<2>(a, h, s);
