@@ -26,7 +26,7 @@ LIB = os.path.join(PKG, "libacid_gb300.so")
 BUILD_DEBUG = os.path.join(PKG, "_build_debug")
 LIB_DEBUG = os.path.join(PKG, "libacid_gb300_debug.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
-SOURCES = ["capi.cu", "elementwise.cu", "gemm.cu", "attention.cu", "block.cu", "loop.cu", "site.cu", "q4.cu",
+SOURCES = ["capi.cu", "elementwise.cu", "gemm.cu", "attention.cu", "block.cu", "loop.cu", "site.cu", "q4.cu", "q4_rows.cu",
            "noalloc.cu"]
 
 

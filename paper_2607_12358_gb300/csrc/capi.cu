@@ -21,6 +21,8 @@ BoundsRecord take_bounds_gemm();
 BoundsRecord take_bounds_attention();
 BoundsRecord take_bounds_site();
 BoundsRecord take_bounds_q4();
+unsigned int take_device_error_q4_rows();
+BoundsRecord take_bounds_q4_rows();
 
 namespace {
 thread_local std::string t_last_error;
@@ -224,8 +226,8 @@ extern "C" acid_status acid_bounds_report(int32_t* checked, int64_t* site, int64
   clear_error();
   ACID_REQUIRE(checked && site && index && extent, ACID_ERR_INVALID_ARG, "acid_bounds_report: null argument");
   ACID_CUDA(cudaDeviceSynchronize());
-  const BoundsRecord recs[6] = {take_bounds_elementwise(), take_bounds_gemm(), take_bounds_attention(),
-                                take_bounds_site(),        take_bounds_q4(),   take_bounds_capi()};
+  const BoundsRecord recs[7] = {take_bounds_elementwise(), take_bounds_gemm(), take_bounds_attention(), take_bounds_site(),
+                                take_bounds_q4(),          take_bounds_q4_rows(), take_bounds_capi()};
   *checked = kBoundsChecked ? 1 : 0;
   *site = *index = *extent = 0;
   for (const BoundsRecord& r : recs) {
@@ -267,7 +269,7 @@ extern "C" acid_status acid_check_device_error(void) {
   clear_error();
   ACID_CUDA(cudaDeviceSynchronize());
   const unsigned int flag = take_device_error_elementwise() | take_device_error_gemm() |
-                            take_device_error_attention() | take_device_error_capi();
+                            take_device_error_attention() | take_device_error_q4_rows() | take_device_error_capi();
   if (flag) {
     set_error("a bounded device-side wait timed out");
     return ACID_ERR_TIMEOUT;

@@ -4,10 +4,7 @@
 #include <string>
 
 #define ACID_UNIT_WITHOUT_WAITS
-#include <cuda_fp16.h>
-
-#include "common.cuh"
-#include "internal.h"
+#include "q4.cuh"
 
 namespace acid {
 
@@ -19,14 +16,6 @@ namespace {
 constexpr int kThreads = 256;
 using bf16 = __nv_bfloat16;
 
-// A weight as the kernels see it.
-struct Q4 {
-  const uint32_t* packed;  // [n][16 slabs] words
-  const void* scales;
-  const uint8_t* zeros;
-  int64_t n;
-  int k, slabs, group_log, groups;  // group = 1 << group_log columns; groups = ceil(k / group)
-};
 // First of the eight columns that word `w` of a row holds.
 __device__ __forceinline__ int word_column(int w) { return (w >> 4) * 128 + (w & 3) * 32 + ((w >> 2) & 3) * 8; }
 // The word that holds the columns 8 o .. 8 o + 7.
@@ -44,16 +33,6 @@ __device__ __forceinline__ int zero_at(const Q4& w, int64_t row, int col) {
 __device__ __forceinline__ uint32_t word_at(const Q4& w, int64_t row, int i) {
   const int64_t at = row * w.slabs * 16 + i;
   return ACID_IN_BOUNDS(kSiteQ4, at, w.n * w.slabs * 16) ? w.packed[at] : 0u;
-}
-
-__device__ __forceinline__ float value_at(int dtype, const void* p, int64_t i) {
-  return dtype == ACID_BF16 ? __bfloat162float(static_cast<const bf16*>(p)[i]) : static_cast<const float*>(p)[i];
-}
-__device__ __forceinline__ void put_value(int dtype, void* p, int64_t i, float v) {
-  if (dtype == ACID_BF16)
-    static_cast<bf16*>(p)[i] = __float2bfloat16_rn(v);
-  else
-    static_cast<float*>(p)[i] = v;
 }
 
 // D += A B of one 16 x 8 x 16 tile of the warp-wide tensor instruction.  Lane
@@ -83,13 +62,6 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-template <typename H2>
-__device__ __forceinline__ uint32_t bits(H2 h) {
-  return *reinterpret_cast<uint32_t*>(&h);
-}
-__device__ __forceinline__ __half2 half2_of(uint32_t u) { return *reinterpret_cast<__half2*>(&u); }
-__device__ __forceinline__ __nv_bfloat162 bf162_of(uint32_t u) { return *reinterpret_cast<__nv_bfloat162*>(&u); }
-
 __device__ __forceinline__ uint4 load_stream(const uint4* p) {
   uint4 v;
   asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
@@ -98,99 +70,14 @@ __device__ __forceinline__ uint4 load_stream(const uint4* p) {
   return v;
 }
 
-// ------------------------------------------------------------------ product
-// out^T = W a(x)^T on the tensor cores, the codes as the exact halves q - z
-// (16 rows of the weight to a tile) against the rows of a(x), 8 to a tile.  a(x)
-// enters as two halves, high and low part, after a power of two that brings
-// the largest value of each 128 columns of a row to 2^13 .. 2^14: together 22 bits
-// of it.  Products are exact, a group's sum is formed by the tensor cores in
-// fp32 and multiplied by the group's scale in fp32.
-// Up to kPackedRows rows: the parts of row m are columns 2 m and 2 m + 1 of one
-// tile, prepared by each CTA in its shared memory.  More rows: q4_parts_kernel
-// prepares them once, in the order in which the lanes read them.
-struct Fwd {
-  Q4 w;
-  const void* x;
-  int64_t ldx, m;
-  int x_dtype, silu, out_dtype;
-  const float* bias;
-  void* out;
-  int64_t ldo;
-  uint4* parts;  // [chunks of 64 rows][slab][4 words][2 parts][8 NT columns][4 lanes]
-  float* back;   // [m][slabs]: the powers of two taken back
-  int kw;        // warps of a CTA that share a row's columns
-};
-constexpr int kPackedRows = 4, kChunk = 64;
-
-// The activated octet's eight values and the factor of their slab; 16 lanes in a
-// row hold a slab's octets.
-__device__ __forceinline__ float octet_of(const Fwd& a, int64_t m, int col, float (&v)[8]) {
-  float top = 0.f;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    v[j] = 0.f;
-    if (m < a.m && col + j < a.w.k) {
-      v[j] = value_at(a.x_dtype, a.x, m * a.ldx + col + j);
-      if (a.silu) v[j] = silu(v[j]);
-    }
-    if (isfinite(v[j])) top = fmaxf(top, fabsf(v[j]));
-  }
-#pragma unroll
-  for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  return __uint_as_float(min(267u - (__float_as_uint(top) >> 23), 254u) << 23);
-}
-// High and low parts of an octet, columns j and j + 4 to a register.
-__device__ __forceinline__ void split_octet(const float (&v)[8], float by, uint4& hi, uint4& lo) {
-  uint32_t h[4], l[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float x = v[j] * by, y = v[j + 4] * by;
-    const __half2 p = __floats2half2_rn(x, y);
-    const float2 f = __half22float2(p);
-    h[j] = bits(p);
-    // nothing is left of an infinity or a NaN
-    l[j] = bits(__floats2half2_rn(isfinite(f.x) ? x - f.x : 0.f, isfinite(f.y) ? y - f.y : 0.f));
-  }
-  hi = make_uint4(h[0], h[1], h[2], h[3]);
-  lo = make_uint4(l[0], l[1], l[2], l[3]);
-}
-
-template <int NT>
-__global__ void __launch_bounds__(kThreads) q4_parts_kernel(Fwd a) {
-  pdl_wait();
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int per_row = a.w.slabs * 16;
-  const int64_t m = i / per_row;
-  const int o = (int)(i - m * per_row), slab = o >> 4;
-  float v[8];
-  const float by = octet_of(a, m, o * 8, v);
-  if (m >= a.m) return;
-  uint4 hi, lo;
-  split_octet(v, by, hi, lo);
-  const int64_t chunk = m / kChunk;
-  const int n = (int)(m - chunk * kChunk), word = (o >> 2) & 3, t = o & 3;
-  uint4* p = a.parts + (((chunk * a.w.slabs + slab) * 4 + word) * 2 * NT * 8 + n) * 4 + t;
-  p[0] = hi;
-  p[NT * 8 * 4] = lo;
-  if ((o & 15) == 0) a.back[m * a.w.slabs + slab] = 1.f / by;
-}
-
-// The four pairs (columns j and j + 4) of a word as halves q - z; z1 = 1024 + z and
-// z64 = 64 + z in both halves.  A code in the low bits of the half 1024 (or in
-// the next four bits, worth 16) is read without a conversion.
-__device__ __forceinline__ void halves_of(uint32_t w, uint32_t z1, uint32_t z64, uint32_t (&d)[4]) {
-  const __half2 sixteenth = __float2half2_rn(0.0625f);
-  const uint32_t v = w >> 8;
-  d[0] = bits(__hsub2(half2_of((w & 0x000f000fu) | 0x64006400u), half2_of(z1)));
-  d[1] = bits(__hfma2(half2_of((w & 0x00f000f0u) | 0x64006400u), sixteenth, __hneg2(half2_of(z64))));
-  d[2] = bits(__hsub2(half2_of((v & 0x000f000fu) | 0x64006400u), half2_of(z1)));
-  d[3] = bits(__hfma2(half2_of((v & 0x00f000f0u) | 0x64006400u), sixteenth, __hneg2(half2_of(z64))));
-}
-
-// The four pairs of a word as halves q - 8: what halves_of gives without a zero
-// point, which the few-rows kernel takes into account by the sum of a(x) over
-// the group, sum x (q - z) = sum x (q - 8) + (8 - z) sum x.
-__device__ __forceinline__ void halves_of(uint32_t w, uint32_t (&d)[4]) { halves_of(w, 0x64086408u, 0x54805480u, d); }
+// ------------------------------------------------- product with a few rows
+// out^T = W a(x)^T on the tensor cores, the codes as the exact halves q - z (16
+// rows of the weight to a tile) against the two parts of a(x).  Products are
+// exact, a group's sum is formed by the tensor cores in fp32 and multiplied by
+// the group's scale in fp32.  The parts of row m are columns 2 m and 2 m + 1 of one
+// tile of eight, prepared by each CTA in its shared memory.
+using Fwd = Q4Fwd;
+constexpr int kPackedRows = 4;
 
 // Where a warp reads its row tile: 32 rows g, g + 8, g + 16, g + 24 of a lane, rows
 // past the end as the last one.
@@ -209,12 +96,14 @@ __device__ __forceinline__ TileRows tile_rows(const Q4& w, int64_t tile, int g, 
   return r;
 }
 
-// A few rows: a CTA's warps split a row tile's slabs among kw of them, and 8 / kw
+// A few rows: the codes enter as q - 8 and a zero point by the sum of a(x) over
+// the group, sum x (q - z) = sum x (q - 8) + (8 - z) sum x.  A CTA's warps split a row tile's slabs among kw of them, and 8 / kw
 // row tiles are neighbours.  A lane reads 16 bytes of four rows: word i of them
 // holds its columns of the slab's 32 columns i, so that four lanes' words make a
 // tile's step of 16 columns twice.
-template <typename TS, bool ZEROS>
+template <typename TS, bool ZEROS, int LOG>
 __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
+  constexpr int kWords = 1 << (LOG - 5);  // of 32 columns, to a group
   extern __shared__ __align__(16) uint8_t smem[];
   const Q4& w = a.w;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, warp = warp_index();
@@ -223,10 +112,12 @@ __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
   uint4* frag = reinterpret_cast<uint4*>(smem);                                   // [slab][word][column][t]
   float* back = reinterpret_cast<float*>(smem + (size_t)w.slabs * 16 * cols * 16);  // [slab][row]
   float* xsum = back + w.slabs * kPackedRows;                                     // [slab][32 columns][row]
-  float* red = xsum + (ZEROS ? 4 * w.slabs * kPackedRows : 0);                    // [8 warps][row][33]
+  uint4* none = reinterpret_cast<uint4*>(xsum + (ZEROS ? 4 * w.slabs * kPackedRows : 0));  // zeros
+  float* red = reinterpret_cast<float*>(none + 1);                                // [8 warps][row][33]
   const int64_t tiles = (w.n + 31) / 32, sets = (tiles + rw - 1) / rw;
   const int mine = (w.slabs - kwarp + kw - 1) / kw;  // slabs of this warp
-  const int per_slab = 128 >> w.group_log, lane_group = t >> (w.group_log - 5);
+  constexpr int per_slab = 4 / kWords;
+  const int lane_group = t / kWords;
   struct Load {
     uint4 q[4];
     float s[4];
@@ -284,45 +175,48 @@ __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
       if ((o & 15) == 0) back[(o >> 4) * kPackedRows + m] = 1.f / by;
       if (ZEROS && (o & 3) == 0) xsum[(o >> 2) * kPackedRows + m] = sum;
     }
+    if (threadIdx.x == 0) *none = make_uint4(0, 0, 0, 0);
     __syncthreads();
   }
   float sum[2][2];  // row t of the input, rows g + 8 h + 16 r of the tile
   auto clear = [&] { sum[0][0] = sum[0][1] = sum[1][0] = sum[1][1] = 0.f; };
-  const uint4* mine_b = frag + (g < cols ? g * 4 + t : 0);
+  const uint4* mine_b = g < cols ? frag + g * 4 + t : none;  // columns past the parts are zeros
+  const int word_b = g < cols ? cols * 4 : 0;
   auto compute = [&](const Load& l, int slab) {
     const float bk = back[slab * kPackedRows + t];
-    float acc[2][4], xs = 0.f;
+    const uint4* pb = mine_b + slab * 4 * word_b;
+    float acc[2][4], xs = 0.f, z[4];
+    if constexpr (ZEROS)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) z[q] = 8.f - (float)l.z[q];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      uint4 b = mine_b[(slab * 4 + i) * cols * 4];
-      if (g >= cols) b = make_uint4(0, 0, 0, 0);
-      const bool first = (i << 5 & ((1 << w.group_log) - 1)) == 0;
-      if (ZEROS) xs = (first ? 0.f : xs) + xsum[(slab * 4 + i) * kPackedRows + t];
+      const uint4 b = pb[i * word_b];
+      if (ZEROS) xs = (i % kWords == 0 ? 0.f : xs) + xsum[(slab * 4 + i) * kPackedRows + t];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         uint32_t d[2][4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const uint4& v = l.q[2 * r + h];
-          halves_of(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w, d[h]);
+          halves_of(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w, 8u, d[h]);
         }
-        if (first)
+        if (i % kWords == 0)
           mma_f16_first(acc[r], d[0][0], d[1][0], d[0][1], d[1][1], b.x, b.y);
         else
           mma_f16(acc[r], d[0][0], d[1][0], d[0][1], d[1][1], b.x, b.y);
         mma_f16(acc[r], d[0][2], d[1][2], d[0][3], d[1][3], b.z, b.w);
       }
-      if (((i + 1) << 5 & ((1 << w.group_log) - 1)) == 0) {  // the group ends
-        const int from = (lane & ~3) | (i >> (w.group_log - 5) << (w.group_log - 5));  // a lane that has its scale
+      if ((i + 1) % kWords == 0) {  // the group ends
+        const int from = (lane & ~3) | i / kWords * kWords;  // a lane that has its scale
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const int q = 2 * r + h;
-            const float s = __shfl_sync(0xffffffffu, l.s[q], from);
+            const float s = kWords == 4 ? l.s[q] : __shfl_sync(0xffffffffu, l.s[q], from);
             float v = (acc[r][2 * h] + acc[r][2 * h + 1]) * bk;  // both parts of row t are in this lane
-            if constexpr (ZEROS)
-              v = fmaf((float)(8 - (int)__shfl_sync(0xffffffffu, (uint32_t)l.z[q], from)), xs, v);
+            if constexpr (ZEROS) v = fmaf(kWords == 4 ? z[q] : __shfl_sync(0xffffffffu, z[q], from), xs, v);
             sum[r][h] = fmaf(s, v, sum[r][h]);
           }
       }
@@ -367,332 +261,140 @@ __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
   }
 }
 
-// More rows: the same tiles of the weight against 8 NT columns of parts.
-template <int NT, typename TS>
-__global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) q4_forward_kernel(Fwd a) {
-  extern __shared__ __align__(16) uint8_t smem[];
-  pdl_wait();
-  const Q4& w = a.w;
-  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, warp = warp_index();
-  const int kw = a.kw, rw = kThreads / 32 / kw, kwarp = warp % kw, rwarp = warp / kw;
-  const int64_t chunk = blockIdx.y, m0 = chunk * kChunk;
-  constexpr int kCols = NT * 8;
-  float* red = reinterpret_cast<float*>(smem);  // [8 warps][column][33]: sums of the warps that share rows
-
-  const int64_t tiles = (w.n + 31) / 32, sets = (tiles + rw - 1) / rw;
-  const int mine = (w.slabs - kwarp + kw - 1) / kw;  // slabs of this warp
-  struct Load {
-    uint4 q[4];
-    float s[4];
-    uint32_t z[4];
-  };
-  const int per_slab = 128 >> w.group_log, lane_group = t >> (w.group_log - 5);
-  auto fetch = [&](Load& l, int64_t set, int slab) {
-    const int64_t row0 = (set * rw + rwarp) * 32 + g;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int64_t row = min(row0 + 8 * q, w.n - 1);
-      const int64_t at = row * w.slabs + slab;
-      if (ACID_IN_BOUNDS(kSiteQ4, at, w.n * w.slabs)) l.q[q] = load_stream(reinterpret_cast<const uint4*>(w.packed) + at * 4 + t);
-      const int64_t i = row * w.groups + min(slab * per_slab + lane_group, w.groups - 1);
-      if (ACID_IN_BOUNDS(kSiteQ4, i, w.n * w.groups)) {
-        l.s[q] = io<TS>::ld(static_cast<const TS*>(w.scales) + i);
-        l.z[q] = w.zeros != nullptr ? w.zeros[i] : 8u;
-      }
-    }
-  };
-  float acc[2][NT][4], sum[2][NT][4];
-  auto compute = [&](const Load& l, int slab) {
-    float bk[NT][2];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        bk[n][e] = m0 + 8 * n + 2 * t + e < a.m ? a.back[(m0 + 8 * n + 2 * t + e) * w.slabs + slab] : 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int from = (lane & ~3) | (i >> (w.group_log - 5) << (w.group_log - 5));  // a lane that has the group's scale
-      uint32_t d[4][4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const uint32_t z = w.zeros != nullptr ? __shfl_sync(0xffffffffu, l.z[q], from) * 0x00010001u : 0x00080008u;
-        const uint32_t word = i == 0 ? l.q[q].x : i == 1 ? l.q[q].y : i == 2 ? l.q[q].z : l.q[q].w;
-        halves_of(word, 0x64006400u | z, 0x54005400u | z << 4, d[q]);
-      }
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const uint4* p = a.parts + (((chunk * w.slabs + slab) * 4 + i) * 2 * NT * 8 + n * 8 + g) * 4 + t;
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-          const uint4 b = p[part * NT * 8 * 4];
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            mma_f16(acc[r][n], d[2 * r][0], d[2 * r + 1][0], d[2 * r][1], d[2 * r + 1][1], b.x, b.y);
-            mma_f16(acc[r][n], d[2 * r][2], d[2 * r + 1][2], d[2 * r][3], d[2 * r + 1][3], b.z, b.w);
-          }
-        }
-      }
-      if (((i + 1) << 5 & ((1 << w.group_log) - 1)) == 0) {  // the group ends
-        float sc[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) sc[q] = __shfl_sync(0xffffffffu, l.s[q], from);
-#pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              sum[r][n][e] = fmaf(sc[2 * r + (e >> 1)], acc[r][n][e] * bk[n][e & 1], sum[r][n][e]);
-              acc[r][n][e] = 0.f;
-            }
-      }
-    }
-  };
-  auto put = [&](int64_t row, int m, float v) {
-    if (row < w.n && m0 + m < a.m)
-      put_value(a.out_dtype, a.out, (m0 + m) * a.ldo + row, v + (a.bias != nullptr ? a.bias[row] : 0.f));
-  };
-  auto each = [&](auto&& f) {  // f(sum, row of the tile, column)
-#pragma unroll
-    for (int r = 0; r < 2; ++r)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f(sum[r][n][e], 16 * r + 8 * (e >> 1) + g, 8 * n + 2 * t + (e & 1));
-  };
-  auto finish = [&](int64_t set) {
-    const int64_t row0 = (set * rw + rwarp) * 32;
-    if (kw == 1) {
-      each([&](float v, int row, int m) { put(row0 + row, m, v); });
-      return;
-    }
-    __syncthreads();  // the buffer's last readers are done
-    each([&](float v, int row, int m) { red[(warp * kCols + m) * 33 + row] = v; });
-    __syncthreads();
-    for (int i = threadIdx.x; i < rw * kCols * 32; i += kThreads) {
-      const int row = i & 31, m = (i >> 5) % kCols, rt = (i >> 5) / kCols;
-      float v = 0.f;
-      for (int k = 0; k < kw; ++k) v += red[((rt * kw + k) * kCols + m) * 33 + row];
-      put((set * rw + rt) * 32 + row, m, v);
-    }
-  };
-  auto clear = [&] {
-#pragma unroll
-    for (int r = 0; r < 2; ++r)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[r][n][e] = sum[r][n][e] = 0.f;
-  };
-  // this warp's steps (row set, slab), two fetched ahead
-  int64_t set = blockIdx.x, fset = set;
-  int k = 0, fk = 0;
-  auto advance = [&](int64_t& st, int& i) {
-    if (++i == mine) {
-      i = 0;
-      st += gridDim.x;
-    }
-  };
-  Load l[2];
-  auto next = [&](Load& into) {
-    if (fset < sets) fetch(into, fset, kwarp + fk * kw);
-    advance(fset, fk);
-  };
-  next(l[0]);
-  next(l[1]);
-  clear();
-  auto step = [&](Load& cur) {
-    if (set >= sets) return;
-    compute(cur, kwarp + k * kw);
-    next(cur);
-    if (k == mine - 1) {
-      finish(set);
-      clear();
-    }
-    advance(set, k);
-  };
-  while (set < sets) {
-    step(l[0]);
-    step(l[1]);
-  }
-}
-
-// ----------------------------------------------------------- input gradient
+// ------------------------------------------- input gradient of one or two rows
 // dx^T = W^T g^T on the tensor cores: tiles of 16 columns of the weight by 16 of
-// its rows, the codes as the exact bf16 values q - z, against 8 columns of
-// (g s)^T, whose fp32 values enter as three bf16 parts (24 bits).  A CTA takes one
-// slab of columns and a share of the rows, and leaves its sums for the join.
-struct Bwd {
-  Q4 w;
-  const void *g, *x;
-  int64_t ldg, ldx, m;
-  int g_dtype, x_dtype, scale_dtype, silu;
-  void* dx;
-  int64_t lddx;
-  float* dbias;
-  float* part;   // [splits][m][128 slabs]
-  int splits;
-  int64_t per;   // rows of the weight to a CTA, a multiple of 16
-};
-constexpr int kBwdPackedRows = 2;  // three parts of two rows fit eight columns
-// rows of the weight whose g and scales are staged at a time
-template <bool PACKED>
-constexpr int kStageRows = PACKED ? 768 : 256;
-template <int NT, bool PACKED>
-constexpr int kStageCols = PACKED ? kBwdPackedRows : NT * 8;
-constexpr int larger(int a, int b) { return a > b ? a : b; }
-template <int NT, int IW, bool PACKED>
-constexpr int kBwdSmem = larger((kStageCols<NT, PACKED> + 4) * kStageRows<PACKED> * 4, 2 * IW * NT * 8 * 128 * 4);
-// IW words of a lane's four (32 columns each) are this warp's: 4 / IW warps share
-// a block of 16 rows, and the 2 IW groups of such warps take blocks in turn.
-template <int NT, int IW, bool PACKED>
-__global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) q4_backward_kernel(Bwd a) {
+// its rows, the codes as the exact bf16 values q - z, against eight columns of
+// (g s)^T, whose fp32 values enter as three bf16 parts (24 bits): part p of row m is
+// column 3 m + p.  A CTA takes one slab of columns and a share of the rows, and
+// leaves its sums for the join.
+using Bwd = Q4Bwd;
+constexpr int kBwdFewRows = 2;
+constexpr int kStageBlocks = 48;  // blocks of 16 rows of the weight whose parts are staged at a time
+int few_smem(int variants) { return std::max(kStageBlocks * (variants * 256 + 4 * 4 * 8), 8 * 8 * 128 * 4); }
+
+// Each warp takes every eighth block of 16 rows.  The parts of g s for a block
+// (and for each of the slab's groups, `variants`) are formed once, in the order in
+// which the lanes read them.
+__global__ void __launch_bounds__(kThreads, 2) q4_few_backward_kernel(Bwd a) {
   extern __shared__ __align__(16) uint8_t smem[];
-  constexpr int kShare = 4 / IW, kTurns = 2 * IW, kRows = kStageRows<PACKED>, kBlocks = kRows / 16;
-  constexpr int kStaged = kStageCols<NT, PACKED>;
+  constexpr int kTurns = kThreads / 32;
   pdl_wait();
   const Q4& w = a.w;
-  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, warp = warp_index();
-  const int first_word = (warp % kShare) * IW, turn = warp / kShare;
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, turn = warp_index();
   const int slab = blockIdx.x;
-  const int64_t chunk = blockIdx.z, m0 = chunk * kChunk;
   const int64_t begin = blockIdx.y * a.per, end = min(w.n, begin + a.per);
-  if (a.dbias != nullptr && slab == 0 && chunk == 0)
+  if (a.dbias != nullptr && slab == 0)
     for (int64_t n = begin + threadIdx.x; n < end; n += kThreads) {
       float v = 0.f;
       for (int64_t m = 0; m < a.m; ++m) v += value_at(a.g_dtype, a.g, m * a.ldg + n);
       a.dbias[n] = v;
     }
   if (a.dx == nullptr) return;
-  float4* gs = reinterpret_cast<float4*>(smem);           // [block][column][t]: rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9
-  float4* ss = gs + kBlocks * kStaged * 4;  // [block][word][t]
-  float acc[IW][2][NT][4];
+  const int variants = 128 >> w.group_log, variant_log = 7 - w.group_log, word_log = w.group_log - 5;
+  uint2* bs = reinterpret_cast<uint2*>(smem);        // [block][variant][lane]
+  uint2* zs = bs + kStageBlocks * variants * 32;     // [block][variant][t]: 128 + z of the rows, as bf16
+  float acc[4][2][4];
 #pragma unroll
-  for (int i = 0; i < IW; ++i)
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][n][e] = 0.f;
+      for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.f;
   struct Load {
-    uint32_t q[4][IW];
-    uint32_t z[4];  // zero points of the words, a byte each
+    uint4 q[4];
   };
-  const int per_slab = 128 >> w.group_log;
-  auto row_of = [&](int64_t block, int r) { return block * 16 + 2 * t + (r & 1) + (r >> 1) * 8; };
   const int64_t blocks_end = (end + 15) / 16;
   auto fetch = [&](Load& l, int64_t block) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int64_t row = min(row_of(block, r), w.n - 1);
-      const int64_t at = (row * w.slabs + slab) * 16 + 4 * (g & 3) + first_word;
-      if (ACID_IN_BOUNDS(kSiteQ4, at + IW - 1, w.n * w.slabs * 16)) {
-        const uint32_t* p = w.packed + at;
-        if constexpr (IW == 4) {
-          const uint4 v = *reinterpret_cast<const uint4*>(p);
-          l.q[r][0] = v.x; l.q[r][1] = v.y; l.q[r][2] = v.z; l.q[r][3] = v.w;
-        } else if constexpr (IW == 2) {
-          const uint2 v = *reinterpret_cast<const uint2*>(p);
-          l.q[r][0] = v.x; l.q[r][1] = v.y;
-        } else {
-          l.q[r][0] = *p;
-        }
-      }
-      if (w.zeros != nullptr) {
-        l.z[r] = 0;
-#pragma unroll
-        for (int i = 0; i < IW; ++i) {
-          const int64_t z = row * w.groups + min(slab * per_slab + ((first_word + i) >> (w.group_log - 5)), w.groups - 1);
-          if (ACID_IN_BOUNDS(kSiteQ4, z, w.n * w.groups)) l.z[r] |= (uint32_t)w.zeros[z] << (8 * i);
-        }
-      }
+      const int64_t row = min(block * 16 + 2 * t + (r & 1) + (r >> 1) * 8, w.n - 1);
+      const int64_t at = (row * w.slabs + slab) * 16 + 4 * (g & 3);
+      if (ACID_IN_BOUNDS(kSiteQ4, at + 3, w.n * w.slabs * 16)) l.q[r] = *reinterpret_cast<const uint4*>(w.packed + at);
     }
   };
   // eight halves of a word's columns of two rows: which half the lane takes
   const uint32_t half = g < 4 ? 0x5410u : 0x7632u;
   auto compute = [&](const Load& l, int block) {
+    uint2 b;
 #pragma unroll
-    for (int i = 0; i < IW; ++i) {
-      uint32_t b[NT][3][2];
-      const float4 s = ss[(block * 4 + first_word + i) * 4 + t];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (!PACKED || g < 3 * kBwdPackedRows) v = gs[(block * kStaged + (PACKED ? g / 3 : n * 8 + g)) * 4 + t];
-        float f[4] = {v.x * s.x, v.y * s.y, v.z * s.z, v.w * s.w};
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-          for (int part = 0; part < 3; ++part) {
-            const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * h], f[2 * h + 1]);
-            const float lo = __low2float(p), hi = __high2float(p);
-            b[n][part][h] = bits(p);
-            f[2 * h] = isfinite(lo) ? f[2 * h] - lo : 0.f;
-            f[2 * h + 1] = isfinite(hi) ? f[2 * h + 1] - hi : 0.f;
-          }
-          if constexpr (PACKED) {  // column 3 m + part
-            const int part = g % 3;
-            b[n][0][h] = part == 0 ? b[n][0][h] : part == 1 ? b[n][1][h] : b[n][2][h];
-          }
-        }
-      }
-      uint32_t q01 = __byte_perm(l.q[0][i], l.q[1][i], half), q89 = __byte_perm(l.q[2][i], l.q[3][i], half);
-      uint32_t z01 = 0x43084308u, z89 = 0x43084308u;  // 128 + z
-      if (w.zeros != nullptr) {
-        z01 = 0x43004300u | (l.z[0] >> (8 * i) & 15u) | (l.z[1] >> (8 * i) & 15u) << 16;
-        z89 = 0x43004300u | (l.z[2] >> (8 * i) & 15u) | (l.z[3] >> (8 * i) & 15u) << 16;
-      }
+    for (int i = 0; i < 4; ++i) {
+      const int at = block * variants + (i >> word_log);
+      if (i == 0 || variants > 1) b = bs[at * 32 + lane];
+      auto word = [&](int r) { return i == 0 ? l.q[r].x : i == 1 ? l.q[r].y : i == 2 ? l.q[r].z : l.q[r].w; };
+      uint32_t q01 = __byte_perm(word(0), word(1), half), q89 = __byte_perm(word(2), word(3), half);
+      uint2 z = make_uint2(0x43084308u, 0x43084308u);  // 128 + 8
+      if (w.zeros != nullptr) z = zs[at * 4 + t];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         uint32_t d[4];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {  // the code in the low bits of the bf16 128
-          d[e] = bits(__hsub2(bf162_of((q01 & 0x000f000fu) | 0x43004300u), bf162_of(z01)));
-          d[2 + e] = bits(__hsub2(bf162_of((q89 & 0x000f000fu) | 0x43004300u), bf162_of(z89)));
+          d[e] = bits(__hsub2(bf162_of((q01 & 0x000f000fu) | 0x43004300u), bf162_of(z.x)));
+          d[2 + e] = bits(__hsub2(bf162_of((q89 & 0x000f000fu) | 0x43004300u), bf162_of(z.y)));
           q01 >>= 4;
           q89 >>= 4;
         }
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int part = 0; part < (PACKED ? 1 : 3); ++part)
-            mma_bf16(acc[i][j][n], d[0], d[1], d[2], d[3], b[n][part][0], b[n][part][1]);
+        mma_bf16(acc[i][j], d[0], d[1], d[2], d[3], b.x, b.y);
       }
     }
   };
-  constexpr int kAhead = PACKED ? 3 : IW == 4 ? 2 : 4;
-  static_assert(kBlocks % (kTurns * kAhead) == 0, "a stage is a whole number of rounds of every warp's ring");
+  constexpr int kAhead = 3;
+  static_assert(kStageBlocks % (kTurns * kAhead) == 0, "a stage is a whole number of rounds of every warp's ring");
   Load l[kAhead];
   int64_t fetched = begin / 16 + turn;
 #pragma unroll
   for (int k = 0; k < kAhead; ++k, fetched += kTurns)
     if (fetched < blocks_end) fetch(l[k], fetched);
-  for (int64_t base = begin; base < end; base += kRows) {
+  for (int64_t base = begin; base < end; base += kStageBlocks * 16) {
     __syncthreads();
-    // g and scales of the next rows; zeros past the end
-    for (int i = threadIdx.x; i < kStaged * kRows; i += kThreads) {
-      const int col = i / kRows, r = i % kRows;
-      const int64_t n = base + r, m = m0 + col;
-      const float v = n < end && m < a.m ? value_at(a.g_dtype, a.g, m * a.ldg + n) : 0.f;
-      const int b = r / 16, q = r % 8 / 2, e = r % 2 + (r % 16) / 8 * 2;
-      reinterpret_cast<float*>(gs + (b * kStaged + col) * 4 + q)[e] = v;
-    }
-    for (int i = threadIdx.x; i < 4 * kRows; i += kThreads) {
-      const int word = i % 4, r = i / 4;
-      const int64_t n = base + r;
-      float v = 0.f;
-      if (n < end) {
-        const int64_t at = n * w.groups + min(slab * per_slab + (word >> (w.group_log - 5)), w.groups - 1);
-        if (ACID_IN_BOUNDS(kSiteQ4, at, w.n * w.groups)) v = value_at(a.scale_dtype, w.scales, at);
+    const int blocks = (int)(min((int64_t)kStageBlocks * 16, end - base) + 15) / 16;
+    // parts of g s, zeros past the end; a thread takes four rows of a block and one row of g
+    for (int i = threadIdx.x; i < blocks * variants * 4 * kBwdFewRows; i += kThreads) {
+      const int q = i & 3, m = (i >> 2) % kBwdFewRows, bv = (i >> 2) / kBwdFewRows;
+      const int v = bv & (variants - 1), b = bv >> variant_log;
+      const int64_t n0 = base + b * 16 + 2 * q;
+      float f[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int64_t n = n0 + (r & 1) + (r >> 1) * 8;
+        f[r] = 0.f;
+        if (n < end && m < a.m) {
+          const int64_t at = n * w.groups + min(slab * variants + v, w.groups - 1);
+          f[r] = value_at(a.g_dtype, a.g, m * a.ldg + n);
+          if (ACID_IN_BOUNDS(kSiteQ4, at, w.n * w.groups)) f[r] *= value_at(a.scale_dtype, w.scales, at);
+        }
       }
-      const int b = r / 16, q = r % 8 / 2, e = r % 2 + (r % 16) / 8 * 2;
-      reinterpret_cast<float*>(ss + (b * 4 + word) * 4 + q)[e] = v;
+#pragma unroll
+      for (int part = 0; part < 3; ++part) {
+        uint32_t h[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
+          const float x = __low2float(p), y = __high2float(p);
+          h[e] = bits(p);
+          f[2 * e] = isfinite(x) ? f[2 * e] - x : 0.f;  // nothing is left of an infinity or a NaN
+          f[2 * e + 1] = isfinite(y) ? f[2 * e + 1] - y : 0.f;
+        }
+        bs[(b * variants + v) * 32 + (3 * m + part) * 4 + q] = make_uint2(h[0], h[1]);
+      }
     }
+    if (base == begin)  // columns that no part uses
+      for (int i = threadIdx.x; i < kStageBlocks * variants * 8; i += kThreads) bs[i / 8 * 32 + 24 + i % 8] = make_uint2(0, 0);
+    if (w.zeros != nullptr)
+      for (int i = threadIdx.x; i < blocks * variants * 4; i += kThreads) {
+        const int q = i & 3, v = (i >> 2) & (variants - 1), b = (i >> 2) >> variant_log;
+        uint32_t z[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int64_t n = min(base + b * 16 + 2 * q + (r & 1) + (r >> 1) * 8, w.n - 1);
+          const int64_t at = n * w.groups + min(slab * variants + v, w.groups - 1);
+          z[r] = ACID_IN_BOUNDS(kSiteQ4, at, w.n * w.groups) ? w.zeros[at] & 15u : 8u;
+        }
+        zs[i] = make_uint2(0x43004300u | z[0] | z[1] << 16, 0x43004300u | z[2] | z[3] << 16);
+      }
     __syncthreads();
-    const int blocks = (int)(min((int64_t)kRows, end - base) + 15) / 16;  // kAhead of them are fetched
 #pragma unroll 1
-    for (int k0 = turn; k0 < kBlocks; k0 += kTurns * kAhead)
+    for (int k0 = turn; k0 < kStageBlocks; k0 += kTurns * kAhead)
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         if (k0 + k * kTurns < blocks) compute(l[k], k0 + k * kTurns);
@@ -700,32 +402,27 @@ __global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) q4_backward_kernel(
         fetched += kTurns;
       }
   }
-  // the turns' sums, then the CTA's share
+  // the warps' sums, then the CTA's share
   __syncthreads();
-  constexpr int kCols = NT * 8;
-  float* red = reinterpret_cast<float*>(smem);  // [turn][column][128]
+  float* red = reinterpret_cast<float*>(smem);  // [warp][column][128]
 #pragma unroll
-  for (int i = 0; i < IW; ++i)
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int c = 32 * (first_word + i) + 8 * (g & 3) + 4 * (g >> 2) + 2 * j;
-          *reinterpret_cast<float2*>(red + (turn * kCols + n * 8 + 2 * t + e) * 128 + c) =
-              make_float2(acc[i][j][n][e], acc[i][j][n][2 + e]);
-        }
+      for (int e = 0; e < 2; ++e) {
+        const int c = 32 * i + 8 * (g & 3) + 4 * (g >> 2) + 2 * j;
+        *reinterpret_cast<float2*>(red + (turn * 8 + 2 * t + e) * 128 + c) = make_float2(acc[i][j][e], acc[i][j][2 + e]);
+      }
   __syncthreads();
-  const int rows = (int)min((int64_t)(PACKED ? kBwdPackedRows : kCols), a.m - m0);
-  for (int i = threadIdx.x; i < rows * 128; i += kThreads) {
+  for (int i = threadIdx.x; i < (int)a.m * 128; i += kThreads) {
     const int m = i / 128, c = i % 128;
     float v = 0.f;
     for (int u = 0; u < kTurns; ++u)
 #pragma unroll
-      for (int part = 0; part < (PACKED ? 3 : 1); ++part) v += red[(u * kCols + (PACKED ? 3 * m + part : m)) * 128 + c];
-    const int64_t at = (blockIdx.y * a.m + m0 + m) * w.slabs * 128 + slab * 128 + c;
-    if (ACID_IN_BOUNDS(kSiteQ4, at, a.splits * a.m * w.slabs * 128)) a.part[at] = v;
+      for (int part = 0; part < 3; ++part) v += red[(u * 8 + 3 * m + part) * 128 + c];
+    const int64_t at = (blockIdx.y * a.m + m) * w.slabs * 128 + slab * 128 + c;
+    if (ACID_IN_BOUNDS(kSiteQ4, at, a.shares * a.m * w.slabs * 128)) a.part[at] = v;
   }
 }
 
@@ -737,7 +434,7 @@ __global__ void __launch_bounds__(kThreads) q4_backward_join_kernel(Bwd a) {
   if (c >= a.w.k) return;
   float v = 0.f;
 #pragma unroll 8
-  for (int b = 0; b < a.splits; ++b) v += a.part[(b * a.m + m) * width + c];
+  for (int b = 0; b < a.shares; ++b) v += a.part[(b * a.m + m) * width + c];
   if (a.silu) {
     const float x = value_at(a.x_dtype, a.x, m * a.ldx + c), e = 1.f / (1.f + expf(-x));
     v *= e * (1.f + x * (1.f - e));
@@ -764,18 +461,30 @@ __device__ __forceinline__ float max_or_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
-// Code of v in 0 .. 15: rint(v / s) + z.  The quotient comes from a product with
-// inv = 1 / s, off by less than 2^-22 of it, and is rounded to even by the sum with
-// 1.5 2^23; only within 1e-4 of the middle of two codes (and where inv is no use)
-// does the division decide.
-__device__ __forceinline__ uint32_t code_of(float v, float s, float inv, int z) {
+// Codes of eight values in 0 .. 15, rint(v / s) + z.  The quotient comes from a
+// product with inv = 1 / s, off by less than 2^-22 of it, and is rounded to even by
+// the sum with 1.5 2^23; a word with a value within 1e-4 of the middle of two codes (or
+// where inv is no use) is formed by divisions.
+__device__ __noinline__ uint32_t divided_codes(float4 lo, float4 hi, float s, int z) {
+  const float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  uint32_t word = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)  // (a NaN becomes the lowest code)
+    word |= (uint32_t)fminf(fmaxf(rintf(v[j] / s) + (float)z, 0.f), 15.f) << (4 * j);
+  return word;
+}
+__device__ __forceinline__ uint32_t codes_of(const float (&v)[8], float s, float inv, int z) {
   constexpr float kRound = 12582912.f;
-  float q = v * inv, r = q + kRound;
-  if (!(fabsf(q - (r - kRound)) < 0.4999f)) {
-    q = fminf(fmaxf(rintf(v / s), -64.f), 64.f);  // (a NaN becomes -64)
-    r = q + kRound;
+  uint32_t word = 0;
+  bool sure = true;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float q = v[j] * inv, r = q + kRound;
+    sure = sure && fabsf(q - (r - kRound)) < 0.4999f;
+    word |= (uint32_t)min(max((int)(__float_as_uint(r) - __float_as_uint(kRound)) + z, 0), 15) << (4 * j);
   }
-  return (uint32_t)min(max((int)(__float_as_uint(r) - __float_as_uint(kRound)) + z, 0), 15);
+  if (sure) return word;
+  return divided_codes(make_float4(v[0], v[1], v[2], v[3]), make_float4(v[4], v[5], v[6], v[7]), s, z);
 }
 
 template <typename TW, typename TS>
@@ -827,9 +536,7 @@ __global__ void __launch_bounds__(kThreads) q4_quantize_kernel(const TW* W, int6
     io<TS>::st(&st, asym ? (hi + lo) / 15.f : hi / 7.f);
     const float s = io<TS>::ld(&st), div = s == 0.f ? 1.f : s, inv = 1.f / div;
     const int z = asym ? (int)fminf(fmaxf(rintf(lo / div), 0.f), 15.f) : 8;
-    uint32_t q = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) q |= code_of(v[u][j], div, inv, z) << (4 * j);
+    const uint32_t q = codes_of(v[u], div, inv, z);
     if (octet < w.slabs * 16) {
       const int64_t p = row * w.slabs * 16 + column_word(octet);
       if (ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.slabs * 16)) packed[p] = q;
@@ -951,39 +658,28 @@ Q4 q4_args(const acid_q4_weight& w) {
           (w.k + w.group - 1) >> log};
 }
 
-// n tiles that a kernel is built for
-int tiles_for(int64_t m) {
-  const int nt = (int)((std::min<int64_t>(m, kChunk) + 7) / 8);
-  return nt <= 3 ? nt : nt <= 5 ? 5 : 8;
-}
-int64_t chunks_of(int64_t m) { return (m + kChunk - 1) / kChunk; }
-
 // Whether the CTAs prepare a(x) themselves: few rows, whose parts fit their shared memory twice an SM.
-bool packed_rows(int64_t m, int k) { return m <= kPackedRows && m * k <= 16384; }
-// Workspace of the product: the parts of a(x), then the powers of two.
-size_t parts_bytes(const acid_q4_weight& w, int64_t m) {
-  return packed_rows(m, w.k) ? 0 : (size_t)chunks_of(m) * ((w.k + 127) / 128) * tiles_for(m) * 4096;
-}
-size_t fwd_bytes(const acid_q4_weight& w, int64_t m) {
-  return packed_rows(m, w.k) ? 0 : parts_bytes(w, m) + (size_t)m * ((w.k + 127) / 128) * sizeof(float);
+bool few_rows(int64_t m, int k) { return m <= kPackedRows && m * k <= 16384; }
+size_t fwd_bytes(const Q4& w, int64_t m) {
+  return few_rows(m, w.k) ? 0 : q4_rows_parts_bytes(w, m) + q4_rows_back_bytes(w, m);
 }
 
-// CTAs that share a slab's rows in the input gradient.
-int bwd_splits(int64_t n, int slabs) {
-  const int64_t want = (304 + slabs - 1) / slabs, most = (n + 127) / 128;
-  return (int)std::max<int64_t>(1, std::min(want, most));
+// Rows of the weight to a CTA of the input gradient, shares of the sums and scans.
+int64_t bwd_per(const Q4& w, int64_t m) {
+  if (m > kBwdFewRows) return q4_rows_share(w);
+  const int64_t want = (304 + w.slabs - 1) / w.slabs, most = (w.n + 127) / 128;
+  const int64_t splits = std::max<int64_t>(1, std::min(want, most));
+  return ((w.n + splits - 1) / splits + 15) / 16 * 16;
 }
-int64_t bwd_per(int64_t n, int slabs) {
-  const int64_t splits = bwd_splits(n, slabs);
-  return ((n + splits - 1) / splits + 15) / 16 * 16;
+int bwd_shares(const Q4& w, int64_t m) {
+  const int64_t per = bwd_per(w, m);
+  return (int)((w.n + per - 1) / per) * (m > kBwdFewRows ? 2 : 1);
 }
-size_t bwd_bytes(const acid_q4_weight& w, int64_t m) {
-  const int slabs = (w.k + 127) / 128;
-  return (size_t)bwd_splits(w.n, slabs) * m * slabs * 128 * sizeof(float);
-}
-
-size_t workspace_bytes(const acid_q4_weight& w, int64_t m) {
-  return std::max<size_t>({16, fwd_bytes(w, m), bwd_bytes(w, m)});
+int bwd_scans(const Q4& w, int64_t m) { return m > kBwdFewRows ? (int)((w.n + kQ4ScanRows - 1) / kQ4ScanRows) : 0; }
+size_t bwd_part_bytes(const Q4& w, int64_t m) { return (size_t)bwd_shares(w, m) * m * w.slabs * 128 * sizeof(float); }
+size_t workspace_bytes(const acid_q4_weight& weight, int64_t m) {
+  const Q4 w = q4_args(weight);
+  return std::max<size_t>({16, fwd_bytes(w, m), bwd_part_bytes(w, m) + (size_t)bwd_scans(w, m) * (m + 1) * sizeof(float)});
 }
 
 // Warps of a CTA that share a row's columns: as many as give every SM eight warps
@@ -993,49 +689,24 @@ int sharing_warps(const Q4& w) {
   while (kw < 8 && 2 * kw <= w.slabs && (w.n + 31) / 32 * kw < 8 * num_sms()) kw *= 2;
   return kw;
 }
-template <typename TS, bool ZEROS>
+template <typename TS, bool ZEROS, int LOG>
 acid_status launch_few(Fwd a, cudaStream_t s) {
   static PerContext allowed;
   a.kw = sharing_warps(a.w);
   const int rw = kThreads / 32 / a.kw;
-  const size_t smem = (size_t)a.w.slabs * (512 * a.m + 4 * kPackedRows * (ZEROS ? 5 : 1)) +
+  const size_t smem = (size_t)a.w.slabs * (512 * a.m + 4 * kPackedRows * (ZEROS ? 5 : 1)) + 16 +
                       (a.kw == 1 ? 0 : 8 * kPackedRows * 33 * sizeof(float));
-  ACID_TRY(allow_smem(allowed, q4_few_kernel<TS, ZEROS>, 110 * 1024));
+  ACID_TRY(allow_smem(allowed, q4_few_kernel<TS, ZEROS, LOG>, 110 * 1024));
   const int64_t sets = ((a.w.n + 31) / 32 + rw - 1) / rw;
-  launch_pdl(q4_few_kernel<TS, ZEROS>, (unsigned)std::min<int64_t>(sets, (int64_t)num_sms() * 2), kThreads, smem, s, a);
+  launch_pdl(q4_few_kernel<TS, ZEROS, LOG>, (unsigned)std::min<int64_t>(sets, (int64_t)num_sms() * 2), kThreads, smem, s, a);
   ACID_CHECK_LAUNCH();
   return ACID_OK;
 }
-template <int NT, typename TS>
-acid_status launch_forward(Fwd a, cudaStream_t s) {
-  static PerContext allowed;
-  a.kw = sharing_warps(a.w);
-  const int rw = kThreads / 32 / a.kw;
-  const size_t smem = a.kw == 1 ? 0 : (size_t)8 * NT * 8 * 33 * sizeof(float);
-  ACID_TRY(allow_smem(allowed, q4_forward_kernel<NT, TS>, 8 * NT * 8 * 33 * sizeof(float)));
-  const int64_t sets = ((a.w.n + 31) / 32 + rw - 1) / rw;
-  const dim3 grid((unsigned)std::min<int64_t>(sets, (int64_t)num_sms() * (NT <= 2 ? 2 : 1)), (unsigned)chunks_of(a.m));
-  launch_pdl(q4_forward_kernel<NT, TS>, grid, kThreads, smem, s, a);
-  ACID_CHECK_LAUNCH();
-  return ACID_OK;
-}
-template <int NT>
-acid_status launch_parts_forward(const Fwd& a, bool half_scales, cudaStream_t s) {
-  const int64_t octets = a.m * a.w.slabs * 16;
-  launch_pdl(q4_parts_kernel<NT>, (unsigned)((octets + kThreads - 1) / kThreads), kThreads, 0, s, a);
-  ACID_CHECK_LAUNCH();
-  return half_scales ? launch_forward<NT, bf16>(a, s) : launch_forward<NT, float>(a, s);
-}
-
-template <int NT, int IW, bool PACKED>
-acid_status launch_backward(const Bwd& a, cudaStream_t s) {
-  static PerContext allowed;
-  const auto kernel = q4_backward_kernel<NT, IW, PACKED>;
-  ACID_TRY(allow_smem(allowed, kernel, kBwdSmem<NT, IW, PACKED>));
-  const dim3 grid(a.dx != nullptr ? a.w.slabs : 1, a.splits, a.dx != nullptr ? (unsigned)chunks_of(a.m) : 1);
-  launch_pdl(kernel, grid, kThreads, kBwdSmem<NT, IW, PACKED>, s, a);
-  ACID_CHECK_LAUNCH();
-  return ACID_OK;
+template <typename TS, bool ZEROS>
+acid_status launch_few(const Fwd& a, cudaStream_t s) {
+  return a.w.group_log == 5   ? launch_few<TS, ZEROS, 5>(a, s)
+         : a.w.group_log == 6 ? launch_few<TS, ZEROS, 6>(a, s)
+                              : launch_few<TS, ZEROS, 7>(a, s);
 }
 
 }  // namespace
@@ -1117,26 +788,21 @@ extern "C" acid_status acid_q4_linear_forward(int32_t x_dtype, const void* x, in
   ACID_TRY(check_matrix(x_dtype, x, ldx, weight->k, "x"));
   ACID_TRY(check_matrix(out_dtype, out, ldo, weight->n, "out"));
   ACID_REQUIRE(aligned(bias, 4), ACID_ERR_UNSUPPORTED, "acid_q4_linear_forward: bias must be 4-byte aligned");
-  const size_t need = fwd_bytes(*weight, M);
+  const Q4 w = q4_args(*weight);
+  const size_t need = fwd_bytes(w, M);
   ACID_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16)), ACID_ERR_WORKSPACE,
                "acid_q4_linear_forward: workspace null or not 16-byte aligned");
   ACID_REQUIRE(ws_bytes >= need, ACID_ERR_WORKSPACE,
                "acid_q4_linear_forward: workspace too small (need " + std::to_string(need) + ")");
-  Fwd a{q4_args(*weight), x, ldx, M, x_dtype, silu_input != 0, out_dtype, bias, out, ldo, static_cast<uint4*>(ws), nullptr, 1};
-  a.back = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + parts_bytes(*weight, M));
-  const bool h = weight->scale_dtype == ACID_BF16;
+  Fwd a{w, x, ldx, M, x_dtype, silu_input != 0, out_dtype, bias, out, ldo, static_cast<uint8_t*>(ws), nullptr, 1};
   cudaStream_t s = (cudaStream_t)stream;
-  if (need == 0) {
-    if (weight->zeros != nullptr) return h ? launch_few<bf16, true>(a, s) : launch_few<float, true>(a, s);
-    return h ? launch_few<bf16, false>(a, s) : launch_few<float, false>(a, s);
+  if (need != 0) {
+    a.back = reinterpret_cast<float*>(a.parts + q4_rows_parts_bytes(w, M));
+    return q4_rows_forward(a, weight->scale_dtype, s);
   }
-  switch (tiles_for(M)) {
-    case 1: return launch_parts_forward<1>(a, h, s);
-    case 2: return launch_parts_forward<2>(a, h, s);
-    case 3: return launch_parts_forward<3>(a, h, s);
-    case 5: return launch_parts_forward<5>(a, h, s);
-    default: return launch_parts_forward<8>(a, h, s);
-  }
+  const bool h = weight->scale_dtype == ACID_BF16;
+  if (weight->zeros != nullptr) return h ? launch_few<bf16, true>(a, s) : launch_few<float, true>(a, s);
+  return h ? launch_few<bf16, false>(a, s) : launch_few<float, false>(a, s);
 }
 
 extern "C" acid_status acid_q4_linear_workspace_size(const acid_q4_weight* weight, int64_t M, size_t* bytes) {
@@ -1173,23 +839,21 @@ extern "C" acid_status acid_q4_linear_backward(int32_t g_dtype, const void* g, i
     ACID_REQUIRE(ws_bytes >= need, ACID_ERR_WORKSPACE,
                  "acid_q4_linear_backward: workspace too small (need " + std::to_string(need) + ")");
   }
-  const int slabs = (weight->k + 127) / 128;
-  Bwd a{q4_args(*weight), g, x, ldg, ldx, M, g_dtype, x_dtype, weight->scale_dtype, silu_input != 0, dx, lddx, dbias,
-        static_cast<float*>(ws), 0, bwd_per(weight->n, slabs)};
-  a.splits = (int)((weight->n + a.per - 1) / a.per);
-  if (M <= kBwdPackedRows) {
-    ACID_TRY((launch_backward<1, 4, true>(a, s)));
+  const Q4 w = q4_args(*weight);
+  Bwd a{w, g, x, ldg, ldx, M, g_dtype, x_dtype, weight->scale_dtype, silu_input != 0, dx, lddx, dbias,
+        static_cast<float*>(ws), bwd_shares(w, M), bwd_per(w, M), nullptr, bwd_scans(w, M)};
+  if (M <= kBwdFewRows || dx == nullptr) {
+    static PerContext allowed;
+    ACID_TRY(allow_smem(allowed, q4_few_backward_kernel, few_smem(4)));
+    const dim3 grid(dx != nullptr ? w.slabs : 1, (unsigned)((w.n + a.per - 1) / a.per));
+    launch_pdl(q4_few_backward_kernel, grid, kThreads, few_smem(128 >> w.group_log), s, a);
+    ACID_CHECK_LAUNCH();
   } else {
-    switch (tiles_for(M)) {
-      case 1: ACID_TRY((launch_backward<1, 4, false>(a, s))); break;
-      case 2: ACID_TRY((launch_backward<2, 4, false>(a, s))); break;
-      case 3: ACID_TRY((launch_backward<3, 2, false>(a, s))); break;
-      case 5: ACID_TRY((launch_backward<5, 1, false>(a, s))); break;
-      default: ACID_TRY((launch_backward<8, 1, false>(a, s)));
-    }
+    a.top = a.part + bwd_part_bytes(w, M) / sizeof(float);
+    ACID_TRY(q4_rows_backward(a, s));
   }
   if (dx == nullptr) return ACID_OK;
-  launch_pdl(q4_backward_join_kernel, dim3((a.w.k + kThreads - 1) / kThreads, (unsigned)M), kThreads, 0, s, a);
+  launch_pdl(q4_backward_join_kernel, dim3((w.k + kThreads - 1) / kThreads, (unsigned)M), kThreads, 0, s, a);
   ACID_CHECK_LAUNCH();
   return ACID_OK;
 }
