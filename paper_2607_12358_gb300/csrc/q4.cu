@@ -79,6 +79,15 @@ __device__ __forceinline__ uint4 load_stream(const uint4* p) {
 using Fwd = Q4Fwd;
 constexpr int kPackedRows = 4;
 
+// The activated octet's values and the factor of their slab; 16 lanes in a row
+// hold a slab's octets.
+__device__ __forceinline__ float octet_of(const Fwd& a, int64_t m, int col, float (&v)[8]) {
+  float top = octet_values(a, m, col, v);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  return up_to_half(top);
+}
+
 // Where a warp reads its row tile: 32 rows g, g + 8, g + 16, g + 24 of a lane, rows
 // past the end as the last one.
 struct TileRows {

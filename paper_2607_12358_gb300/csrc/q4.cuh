@@ -34,8 +34,9 @@ __device__ __forceinline__ __half2 half2_of(uint32_t u) { return *reinterpret_ca
 __device__ __forceinline__ __nv_bfloat162 bf162_of(uint32_t u) { return *reinterpret_cast<__nv_bfloat162*>(&u); }
 
 // The product's operands.  The activated input enters as two halves, high and
-// low part, after a power of two that brings the largest value of each 128
-// columns of a row to 2^13 .. 2^14: together 22 bits of it.
+// low part, after a power of two that brings the largest value of each row (a few
+// rows: of each 128 columns of it) to 2^13 .. 2^14: together 22 bits of that value, and of
+// any down to 2^-16 of it.
 struct Q4Fwd {
   Q4 w;
   const void* x;
@@ -45,16 +46,15 @@ struct Q4Fwd {
   void* out;
   int64_t ldo;
   uint8_t* parts;  // past a few rows: the parts as the tensor cores read them
-  float* back;     // and the powers of two taken back
+  float* back;     // [m], and the powers of two taken back
   int kw;          // few rows: warps of a CTA that share a row's columns
 };
 // The power of two that brings `top` to 2^13 .. 2^14 (2^127 at most).
 __device__ __forceinline__ float up_to_half(float top) {
   return __uint_as_float(min(267u - (__float_as_uint(top) >> 23), 254u) << 23);
 }
-// The activated octet's eight values and the factor of their slab; 16 lanes in a
-// row hold a slab's octets.
-__device__ __forceinline__ float octet_of(const Q4Fwd& a, int64_t m, int col, float (&v)[8]) {
+// The activated octet's eight values; returns their largest (finite) magnitude.
+__device__ __forceinline__ float octet_values(const Q4Fwd& a, int64_t m, int col, float (&v)[8]) {
   float top = 0.f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -65,9 +65,7 @@ __device__ __forceinline__ float octet_of(const Q4Fwd& a, int64_t m, int col, fl
     }
     if (isfinite(v[j])) top = fmaxf(top, fabsf(v[j]));
   }
-#pragma unroll
-  for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  return up_to_half(top);
+  return top;
 }
 // High and low parts of an octet, columns j and j + 4 to a register.
 __device__ __forceinline__ void split_octet(const float (&v)[8], float by, uint4& hi, uint4& lo) {

@@ -16,7 +16,8 @@ namespace {
 
 using bf16 = __nv_bfloat16;
 constexpr int kThreads = 256;
-constexpr int kRowsThreads = 320;  // eight warps that make operands, an MMA warp and a copying warp
+constexpr int kRowsThreads = 320;  // product: eight warps that make operands, an MMA warp and a copying warp
+constexpr int kBackThreads = 416;  // gradient: eight and four warps that make operands, and an MMA warp
 
 // Instruction descriptor of kind::f16 with fp16 A and B, fp32 accumulator.
 __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool b_mn) {
@@ -57,25 +58,32 @@ constexpr int kSlabBytes = 16 * NT * 256;
 template <int NT>
 constexpr int kFwdSmem = kFwdRing * kSlabBytes<NT> + 8 * kCodeRing * 2048 + 256 + 1024;
 
+// One CTA to a row of a(x).
 template <int NT>
 __global__ void __launch_bounds__(kThreads) q4_parts_kernel(Q4Fwd a) {
+  __shared__ uint32_t largest;
   pdl_wait();
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int per_row = a.w.slabs * 16;
-  const int64_t m = i / per_row;
-  const int o = (int)(i - m * per_row), slab = o >> 4, word = (o >> 2) & 3, t = o & 3;
-  float v[8];
-  const float by = octet_of(a, m, o * 8, v);
-  if (m >= a.m) return;
-  uint4 hi, lo;
-  split_octet(v, by, hi, lo);
-  const int64_t chunk = m / kQ4Chunk;
-  const int n = (int)(m - chunk * kQ4Chunk), unit = (word & 1) * 4 + t;
-  // octets in the order of the codes in a lane: words 32 columns by 32, in them the lanes' quarters
-  uint8_t* p = a.parts + (chunk * a.w.slabs + slab) * kSlabBytes<NT> + (word >> 1) * (16 * NT * 128);
-  *reinterpret_cast<uint4*>(p + n * 128 + ((unit ^ (n & 7)) << 4)) = hi;
-  *reinterpret_cast<uint4*>(p + (8 * NT + n) * 128 + ((unit ^ (n & 7)) << 4)) = lo;
-  if ((o & 15) == 0) a.back[(chunk * a.w.slabs + slab) * 8 * NT + n] = 1.f / by;
+  const int64_t m = blockIdx.x, chunk = m / kQ4Chunk;
+  const int n = (int)(m - chunk * kQ4Chunk), octets = a.w.slabs * 16;
+  if (threadIdx.x == 0) largest = 0;
+  __syncthreads();
+  float v[8], top = 0.f;
+  for (int o = threadIdx.x; o < octets; o += kThreads) top = fmaxf(top, octet_values(a, m, o * 8, v));
+  const uint32_t t = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
+  if ((threadIdx.x & 31) == 0) atomicMax(&largest, t);
+  __syncthreads();
+  const float by = up_to_half(__uint_as_float(largest));
+  if (threadIdx.x == 0) a.back[m] = 1.f / by;
+  for (int o = threadIdx.x; o < octets; o += kThreads) {
+    if (octets > kThreads) octet_values(a, m, o * 8, v);  // (else they are still there)
+    uint4 hi, lo;
+    split_octet(v, by, hi, lo);
+    const int slab = o >> 4, word = (o >> 2) & 3, unit = (word & 1) * 4 + (o & 3);
+    // octets in the order of the codes in a lane: words 32 columns by 32, in them the lanes' quarters
+    uint8_t* p = a.parts + (chunk * a.w.slabs + slab) * kSlabBytes<NT> + (word >> 1) * (16 * NT * 128);
+    *reinterpret_cast<uint4*>(p + n * 128 + ((unit ^ (n & 7)) << 4)) = hi;
+    *reinterpret_cast<uint4*>(p + (8 * NT + n) * 128 + ((unit ^ (n & 7)) << 4)) = lo;
+  }
 }
 
 template <int NT, typename TS>
@@ -198,11 +206,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
     };
     for (int i = 0; i < kCodeRing - 1; ++i) copy();
     uint64_t total[NT][4];  // pairs of the row's sums
-    const float* backs = a.back + chunk * w.slabs * kHalf;
     bool ok = true;
     uint32_t u = 0;
-    // Adds the sums of step `step`, whose scale is s and whose slab's powers are at bk.
-    auto take = [&](uint32_t step, float s, const float* bk) -> bool {
+    // Adds the sums of step `step`, whose scale is s.
+    auto take = [&](uint32_t step, float s) -> bool {
       if (!mbar_wait_warp(&d_full[tile], step & 1)) return false;
       tc_fence_after();
       constexpr int kBatch = NT <= 5 ? NT : 4;
@@ -219,19 +226,14 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
           tc_fence_before();
           mbar_arrive(&d_empty[tile]);
         }
+        const uint64_t s2 = f2_pack(s, s);
 #pragma unroll
         for (int n = 0; n < kBatch; ++n)
 #pragma unroll
-          for (int e = 0; e < 4; e += 2) {
-            const float4 b = *reinterpret_cast<const float4*>(bk + (n0 + n) * 8 + 2 * e);
-            const uint64_t f[2] = {f2_pack(b.x * s, b.y * s), f2_pack(b.z * s, b.w * s)};
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const int j = 2 * (e + h);
-              const uint64_t x = f2_add(f2_pack(__uint_as_float(hi[n][j]), __uint_as_float(hi[n][j + 1])),
-                                        f2_pack(__uint_as_float(lo[n][j]), __uint_as_float(lo[n][j + 1])));
-              total[n0 + n][e + h] = f2_fma(x, f[h], total[n0 + n][e + h]);
-            }
+          for (int e = 0; e < 4; ++e) {
+            const uint64_t x = f2_add(f2_pack(__uint_as_float(hi[n][2 * e]), __uint_as_float(hi[n][2 * e + 1])),
+                                      f2_pack(__uint_as_float(lo[n][2 * e]), __uint_as_float(lo[n][2 * e + 1])));
+            total[n0 + n][e] = f2_fma(x, s2, total[n0 + n][e]);
           }
       }
       return true;
@@ -243,8 +245,22 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) total[n][e] = 0;
+      // scales and zero points of a slab's groups, a slab ahead
+      float scales[4];
+      uint8_t zeros[4];
+      auto look = [&](int slab) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (i >= per_slab) break;
+          const int64_t p = at + min(slab * per_slab + i, w.groups - 1);
+          if (!ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.groups)) continue;
+          scales[i] = io<TS>::ld(static_cast<const TS*>(w.scales) + p);
+          if (w.zeros != nullptr) zeros[i] = w.zeros[p];
+        }
+      };
+      look(0);
       float scale = 0.f;  // of the step whose sums are not taken yet
-      const float* bk = nullptr;
+      bool pending = false;
       for (int slab = 0; ok && slab < w.slabs; ++slab) {
         cp_async_wait<kCodeRing - 2>();
         __syncwarp();
@@ -253,17 +269,23 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
         for (int c = 0; c < 4; ++c) q[c] = *reinterpret_cast<const uint4*>(mine + st * 2048 + place(lane, c));
         copy();
         st = st + 1 == kCodeRing ? 0 : st + 1;
+        float s[4];
+        uint32_t z[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int within = i & (words - 1);
-          const int64_t group_at = at + min(slab * per_slab + i / words, w.groups - 1);
-          uint32_t z = 8;
-          if (w.zeros != nullptr && ACID_IN_BOUNDS(kSiteQ4, group_at, w.n * w.groups)) z = w.zeros[group_at];
+          s[i] = scales[i];
+          z[i] = w.zeros != nullptr ? zeros[i] : 8u;
+        }
+        if (slab + 1 < w.slabs) look(slab + 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int within = i & (words - 1), of = words == 4 ? 0 : words == 2 ? i >> 1 : i;
+          const uint32_t zero = of == 0 ? z[0] : of == 1 ? z[1] : of == 2 ? z[2] : z[3];
           uint32_t d[16];
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             uint32_t h[4];
-            halves_of(i == 0 ? q[c].x : i == 1 ? q[c].y : i == 2 ? q[c].z : q[c].w, z, h);
+            halves_of(i == 0 ? q[c].x : i == 1 ? q[c].y : i == 2 ? q[c].z : q[c].w, zero, h);
 #pragma unroll
             for (int j = 0; j < 4; ++j) d[4 * c + j] = h[j];
           }
@@ -272,16 +294,14 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
           tmem_wait_st();
           tc_fence_before();
           mbar_arrive(&a_full[tile * 2 + (u & 1)]);
-          float s = 0.f;
-          if (ACID_IN_BOUNDS(kSiteQ4, group_at, w.n * w.groups)) s = io<TS>::ld(static_cast<const TS*>(w.scales) + group_at);
           // the sums of the step before, while this one's are formed
-          if (bk != nullptr && ok) ok = take(u - 1, scale, bk);
-          scale = s;
-          bk = backs + slab * kHalf;
+          if (pending && ok) ok = take(u - 1, scale);
+          pending = true;
+          scale = of == 0 ? s[0] : of == 1 ? s[1] : of == 2 ? s[2] : s[3];
           ++u;
         }
       }
-      if (ok) ok = take(u - 1, scale, bk);
+      if (ok) ok = take(u - 1, scale);
       if (!ok || row >= w.n) continue;
       const float bias = a.bias != nullptr ? a.bias[row] : 0.f;
 #pragma unroll
@@ -291,8 +311,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
           const int64_t m = m0 + 8 * n + 2 * e;
           float x, y;
           f2_unpack(total[n][e], x, y);
-          if (m < a.m) put_value(a.out_dtype, a.out, m * a.ldo + row, x + bias);
-          if (m + 1 < a.m) put_value(a.out_dtype, a.out, (m + 1) * a.ldo + row, y + bias);
+          if (m < a.m) put_value(a.out_dtype, a.out, m * a.ldo + row, fmaf(x, a.back[m], bias));
+          if (m + 1 < a.m) put_value(a.out_dtype, a.out, (m + 1) * a.ldo + row, fmaf(y, a.back[m + 1], bias));
         }
     }
     cp_async_wait<0>();
@@ -370,7 +390,7 @@ __global__ void __launch_bounds__(kThreads) q4_scan_kernel(Q4Bwd a) {
 }
 
 template <typename TG, typename TS>
-__global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_backward_kernel(Q4Bwd a) {
+__global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd a) {
   extern __shared__ uint8_t smem_raw[];
   using L = BwdSmem;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -383,7 +403,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_backward_kernel(Q4Bwd
   const int warp = warp_index(), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&a_full[i], 128);
+      mbar_init(&a_full[i], 256);
       mbar_init(&a_empty[i], 1);
       mbar_init(&w_full[i], 128);
       mbar_init(&w_empty[i], 1);
@@ -392,7 +412,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_backward_kernel(Q4Bwd
     mbar_init(drain, 1);
     mbar_fence_init();
   }
-  if (warp == 8) tmem_alloc(tmem_slot, 512);
+  if (warp == 12) tmem_alloc(tmem_slot, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -407,7 +427,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_backward_kernel(Q4Bwd
   const uint32_t kDCol = 0, kACol = variants == 4 ? 256 : 128;
   const int d_step = variants == 1 ? 0 : 64;  // a group's sums are 128 columns, or the 64 of its box
 
-  if (warp == 8) {
+  if (warp == 12) {
     // ------------------------------------------------------------- MMA issuer
     const bool leader = elect_one();
     const uint32_t idesc = idesc_f16_f32(128, variants == 1 ? 128 : 64, true);
@@ -436,26 +456,25 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_backward_kernel(Q4Bwd
       mma_commit(drain);
       mbar_wait(drain, 0);
     }
-  } else if (warp >= 4 && warp < 8) {
+  } else if (warp >= 8) {
     // ------------------------------------------- codes into shared memory, 32 rows of a block to a warp
     const int g = lane >> 2, t = lane & 3, odd = g & 1;
     struct Load {
       uint4 q[4];
-      uint32_t z[4];  // zero points of the slab's groups, a byte each
+      uint8_t z[4][4];  // zero points of the slab's groups
     };
     auto fetch = [&](Load& l, int b) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int64_t row = min(begin + b * 128 + (warp - 4) * 32 + g + 8 * q, w.n - 1);
+        const int64_t row = min(begin + b * 128 + (warp - 8) * 32 + g + 8 * q, w.n - 1);
         const int64_t at = (row * w.slabs + slab) * 16 + 4 * t;
         if (ACID_IN_BOUNDS(kSiteQ4, at + 3, w.n * w.slabs * 16)) l.q[q] = *reinterpret_cast<const uint4*>(w.packed + at);
-        l.z[q] = 0x08080808u;
-        if (w.zeros != nullptr) {
-          l.z[q] = 0;
-          for (int v = 0; v < variants; ++v) {
-            const int64_t z = row * w.groups + min(slab * variants + v, w.groups - 1);
-            if (ACID_IN_BOUNDS(kSiteQ4, z, w.n * w.groups)) l.z[q] |= (uint32_t)w.zeros[z] << (8 * v);
-          }
+        if (w.zeros == nullptr) continue;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          if (v >= variants) break;
+          const int64_t z = row * w.groups + min(slab * variants + v, w.groups - 1);
+          if (ACID_IN_BOUNDS(kSiteQ4, z, w.n * w.groups)) l.z[q][v] = w.zeros[z];
         }
       }
     };
@@ -468,14 +487,19 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_backward_kernel(Q4Bwd
       if (b >= 2 && !mbar_wait_warp(&w_empty[wb], ((b >> 1) - 1) & 1)) { ok = false; break; }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int row = (warp - 4) * 32 + g + 8 * q;
+        const int row = (warp - 8) * 32 + g + 8 * q;
         // neighbouring rows take their words in another order, so that their units lie in different banks
         const uint4 v = odd ? make_uint4(l.q[q].y, l.q[q].x, l.q[q].w, l.q[q].z) : l.q[q];
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
           const int i = s ^ odd, unit = (i & 1) * 4 + t;
           uint32_t h[4];
-          halves_of(s == 0 ? v.x : s == 1 ? v.y : s == 2 ? v.z : v.w, l.z[q] >> (8 * (i >> word_log)) & 15u, h);
+          uint32_t z = 8;
+          if (w.zeros != nullptr) {
+            const int of = i >> word_log;
+            z = (of == 0 ? l.z[q][0] : of == 1 ? l.z[q][1] : of == 2 ? l.z[q][2] : l.z[q][3]) & 15u;
+          }
+          halves_of(s == 0 ? v.x : s == 1 ? v.y : s == 2 ? v.z : v.w, z, h);
           *reinterpret_cast<uint4*>(smem + wb * L::kCodes + (i >> 1) * (L::kCodes / 2) + row * 128 + ((unit ^ (row & 7)) << 4)) =
               make_uint4(h[0], h[1], h[2], h[3]);
         }
@@ -484,10 +508,11 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_backward_kernel(Q4Bwd
       fence_proxy_async_smem();
       mbar_arrive(&w_full[wb]);
     }
-  } else if (warp < 4) {
-    // ----------------------------------------------- parts of g s, then the sums
-    const int tid = threadIdx.x, m = (warp & 1) * 32 + lane;
-    const bool low = warp >= 2, active = (warp & 1) * 32 < rows;
+  } else {
+    // ----------------------------------------------- parts of g s, then the sums: two warps to a quarter of the lanes,
+    // half of the block's rows each
+    const int tid = threadIdx.x & 127, half = warp >> 2, m = (warp & 1) * 32 + lane;
+    const bool low = (warp & 2) != 0, active = (warp & 1) * 32 < rows;
     // the powers of two
     float gt = 0.f, st = 0.f;
     for (int i = 0; i < a.scans; ++i) {
@@ -496,39 +521,58 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_backward_kernel(Q4Bwd
     }
     const float up = up_to_half(gt);                                                       // |g| to 2^13 .. 2^14
     const float one = __uint_as_float(max(254 - (int)(__float_as_uint(st) >> 23), 1) << 23);  // scales to 1 .. 2
-    // row n of the block to thread n: g by columns, scales by groups
+    // Row n of the block to thread n, or n + 128: g by its rows (every other one), scales by groups (the same).  Scales
+    // are looked at a block before they are stored.
     auto copy = [&](int b) {
       const int64_t n = begin + b * 128 + tid;
       float* gd = gs + (b & 1) * (L::kG / 4) + tid;
       if constexpr (sizeof(TG) == 4) {
         const float* src = static_cast<const float*>(a.g) + m0 * a.ldg + (n < end ? n : begin);
-        for (int i = 0; i < rows; ++i) cp_async<4>(gd + i * L::kGStride, src + i * a.ldg, n < end);
+#pragma unroll 4
+        for (int i = half; i < rows; i += 2) cp_async<4>(gd + i * L::kGStride, src + i * a.ldg, n < end);
       } else {
-        for (int i = 0; i < rows; ++i)
+#pragma unroll 8
+        for (int i = half; i < rows; i += 2)
           gd[i * L::kGStride] = n < end ? io<TG>::ld(static_cast<const TG*>(a.g) + (m0 + i) * a.ldg + n) : 0.f;
       }
       cp_async_commit();
-      for (int v = 0; v < variants; ++v) {
-        float s = 0.f;
-        if (n < end) {
-          const int64_t at = n * w.groups + min(slab * variants + v, w.groups - 1);
-          if (ACID_IN_BOUNDS(kSiteQ4, at, w.n * w.groups)) s = io<TS>::ld(static_cast<const TS*>(w.scales) + at) * one;
-        }
-        ss[((b & 1) * 4 + v) * 128 + tid] = s;
+    };
+    float sv[2];
+    auto look = [&](int b) {
+      const int64_t n = begin + b * 128 + tid;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int v = half + 2 * j;
+        sv[j] = 0.f;
+        if (v >= variants || n >= end || b >= blocks) continue;
+        const int64_t at = n * w.groups + min(slab * variants + v, w.groups - 1);
+        if (ACID_IN_BOUNDS(kSiteQ4, at, w.n * w.groups)) sv[j] = io<TS>::ld(static_cast<const TS*>(w.scales) + at);
       }
     };
+    auto store = [&](int b) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (half + 2 * j < variants) ss[((b & 1) * 4 + half + 2 * j) * 128 + tid] = sv[j] * one;
+    };
     copy(0);
-    const uint32_t quad = (uint32_t)(warp * 32) << 16;
+    look(0);
+    store(0);
+    look(1);
+    const uint32_t quad = (uint32_t)((warp & 3) * 32) << 16;
     bool ok = true;
     const uint64_t up2 = f2_pack(up, up);
     for (int b = 0; b < blocks; ++b) {
       cp_async_wait<0>();
-      // block b is there, and nobody reads the other buffer any more; after a wait ran out the four warps leave together
-      if (!group_all(1, 128, ok)) {
+      // block b is there, and nobody reads the other buffer any more; after a wait ran out the eight warps leave together
+      if (!group_all(1, 256, ok)) {
         ok = false;
         break;
       }
-      if (b + 1 < blocks) copy(b + 1);
+      if (b + 1 < blocks) {
+        copy(b + 1);
+        store(b + 1);
+        look(b + 2);
+      }
       const int ab = b % a_bufs;
       if (b >= a_bufs) ok = mbar_wait_warp(&a_empty[ab], (b / a_bufs - 1) & 1);
       if (active && ok) {
@@ -537,7 +581,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_backward_kernel(Q4Bwd
           const float* sr = ss + ((b & 1) * 4 + v) * 128;
           const uint32_t to = tmem + quad + kACol + (ab * variants + v) * 64;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
+          for (int e4 = 0; e4 < 2; ++e4) {
+            const int c = 2 * half + e4;
             uint32_t d[16];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -572,27 +617,29 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_backward_kernel(Q4Bwd
       const float down = 1.f / up, per_s = 1.f / one;
       float* out = a.part + ((blockIdx.y * 2 + low) * a.m + m0 + m) * w.slabs * 128 + slab * 128;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {  // 32 columns
-        const int v = variants == 4 ? c : 0;
+      for (int e = 0; e < 2; ++e) {  // 32 columns
+        const int c = 2 * half + e, v = variants == 4 ? c : 0;
         uint32_t r[32];
         tmem_ld32(tmem + quad + kDCol + (variants == 4 ? v * 64 + (c & 1) * 32 : c * 32), r);
         tmem_wait_ld();
         const int64_t at = ((blockIdx.y * 2 + low) * a.m + m0 + m) * w.slabs * 128 + slab * 128 + c * 32;
-        if (m >= rows || !ACID_IN_BOUNDS(kSiteQ4, at + 31, a.shares * a.m * w.slabs * 128)) continue;
+        if (m < rows && ACID_IN_BOUNDS(kSiteQ4, at + 31, a.shares * a.m * w.slabs * 128)) {
 #pragma unroll
-        for (int o = 0; o < 4; ++o) {  // an octet's columns j and j + 4 lie side by side
-          float f[8];
+          for (int o = 0; o < 4; ++o) {  // an octet's columns j and j + 4 lie side by side
+            float f[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(r[8 * o + j]) * down * per_s;
-          *reinterpret_cast<float4*>(out + c * 32 + o * 8) = make_float4(f[0], f[2], f[4], f[6]);
-          *reinterpret_cast<float4*>(out + c * 32 + o * 8 + 4) = make_float4(f[1], f[3], f[5], f[7]);
+            for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(r[8 * o + j]) * down * per_s;
+            *reinterpret_cast<float4*>(out + c * 32 + o * 8) = make_float4(f[0], f[2], f[4], f[6]);
+            *reinterpret_cast<float4*>(out + c * 32 + o * 8 + 4) = make_float4(f[1], f[3], f[5], f[7]);
+          }
         }
+        __syncwarp();
       }
     }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 8) {
+  if (warp == 12) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
@@ -618,8 +665,7 @@ acid_status launch_forward(const Q4Fwd& a, cudaStream_t s) {
 }
 template <int NT>
 acid_status launch_forward(const Q4Fwd& a, int scale_dtype, cudaStream_t s) {
-  const int64_t octets = a.m * a.w.slabs * 16;
-  launch_pdl(q4_parts_kernel<NT>, (unsigned)((octets + kThreads - 1) / kThreads), kThreads, 0, s, a);
+  launch_pdl(q4_parts_kernel<NT>, (unsigned)a.m, kThreads, 0, s, a);
   ACID_CHECK_LAUNCH();
   return scale_dtype == ACID_BF16 ? launch_forward<NT, bf16>(a, s) : launch_forward<NT, float>(a, s);
 }
@@ -629,7 +675,7 @@ acid_status launch_backward(const Q4Bwd& a, cudaStream_t s) {
   static PerContext allowed;
   ACID_TRY(allow_smem(allowed, q4_rows_backward_kernel<TG, TS>, BwdSmem::kBytes));
   const dim3 grid(a.w.slabs, (unsigned)((a.w.n + a.per - 1) / a.per), (unsigned)chunks_of(a.m));
-  launch_pdl(q4_rows_backward_kernel<TG, TS>, grid, kRowsThreads, BwdSmem::kBytes, s, a);
+  launch_pdl(q4_rows_backward_kernel<TG, TS>, grid, kBackThreads, BwdSmem::kBytes, s, a);
   ACID_CHECK_LAUNCH();
   return ACID_OK;
 }
@@ -639,8 +685,8 @@ acid_status launch_backward(const Q4Bwd& a, cudaStream_t s) {
 size_t q4_rows_parts_bytes(const Q4& w, int64_t m) {
   return (size_t)chunks_of(m) * w.slabs * tiles_for(m) * kSlabBytes<1>;
 }
-size_t q4_rows_back_bytes(const Q4& w, int64_t m) {
-  return (size_t)chunks_of(m) * w.slabs * tiles_for(m) * 8 * sizeof(float);
+size_t q4_rows_back_bytes(const Q4&, int64_t m) {
+  return (size_t)m * sizeof(float);
 }
 
 acid_status q4_rows_forward(const Q4Fwd& a, int scale_dtype, cudaStream_t s) {
