@@ -55,13 +55,6 @@ __device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                         uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ uint4 load_stream(const uint4* p) {
   uint4 v;
   asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
@@ -268,187 +261,6 @@ __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
     step(l[0]);
     step(l[1]);
   }
-}
-
-// ------------------------------------------- input gradient of one or two rows
-// dx^T = W^T g^T on the tensor cores: tiles of 16 columns of the weight by 16 of
-// its rows, the codes as the exact bf16 values q - z, against eight columns of
-// (g s)^T, whose fp32 values enter as three bf16 parts (24 bits): part p of row m is
-// column 3 m + p.  A CTA takes one slab of columns and a share of the rows, and
-// leaves its sums for the join.
-using Bwd = Q4Bwd;
-constexpr int kBwdFewRows = 2;
-constexpr int kStageBlocks = 48;  // blocks of 16 rows of the weight whose parts are staged at a time
-int few_smem(int variants) { return std::max(kStageBlocks * (variants * 256 + 4 * 4 * 8), 8 * 8 * 128 * 4); }
-
-// Each warp takes every eighth block of 16 rows.  The parts of g s for a block
-// (and for each of the slab's groups, `variants`) are formed once, in the order in
-// which the lanes read them.
-__global__ void __launch_bounds__(kThreads, 2) q4_few_backward_kernel(Bwd a) {
-  extern __shared__ __align__(16) uint8_t smem[];
-  constexpr int kTurns = kThreads / 32;
-  pdl_wait();
-  const Q4& w = a.w;
-  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, turn = warp_index();
-  const int slab = blockIdx.x;
-  const int64_t begin = blockIdx.y * a.per, end = min(w.n, begin + a.per);
-  if (a.dbias != nullptr && slab == 0)
-    for (int64_t n = begin + threadIdx.x; n < end; n += kThreads) {
-      float v = 0.f;
-      for (int64_t m = 0; m < a.m; ++m) v += value_at(a.g_dtype, a.g, m * a.ldg + n);
-      a.dbias[n] = v;
-    }
-  if (a.dx == nullptr) return;
-  const int variants = 128 >> w.group_log, variant_log = 7 - w.group_log, word_log = w.group_log - 5;
-  uint2* bs = reinterpret_cast<uint2*>(smem);        // [block][variant][lane]
-  uint2* zs = bs + kStageBlocks * variants * 32;     // [block][variant][t]: 128 + z of the rows, as bf16
-  float acc[4][2][4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.f;
-  struct Load {
-    uint4 q[4];
-  };
-  const int64_t blocks_end = (end + 15) / 16;
-  auto fetch = [&](Load& l, int64_t block) {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int64_t row = min(block * 16 + 2 * t + (r & 1) + (r >> 1) * 8, w.n - 1);
-      const int64_t at = (row * w.slabs + slab) * 16 + 4 * (g & 3);
-      if (ACID_IN_BOUNDS(kSiteQ4, at + 3, w.n * w.slabs * 16)) l.q[r] = *reinterpret_cast<const uint4*>(w.packed + at);
-    }
-  };
-  // eight halves of a word's columns of two rows: which half the lane takes
-  const uint32_t half = g < 4 ? 0x5410u : 0x7632u;
-  auto compute = [&](const Load& l, int block) {
-    uint2 b;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int at = block * variants + (i >> word_log);
-      if (i == 0 || variants > 1) b = bs[at * 32 + lane];
-      auto word = [&](int r) { return i == 0 ? l.q[r].x : i == 1 ? l.q[r].y : i == 2 ? l.q[r].z : l.q[r].w; };
-      uint32_t q01 = __byte_perm(word(0), word(1), half), q89 = __byte_perm(word(2), word(3), half);
-      uint2 z = make_uint2(0x43084308u, 0x43084308u);  // 128 + 8
-      if (w.zeros != nullptr) z = zs[at * 4 + t];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        uint32_t d[4];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {  // the code in the low bits of the bf16 128
-          d[e] = bits(__hsub2(bf162_of((q01 & 0x000f000fu) | 0x43004300u), bf162_of(z.x)));
-          d[2 + e] = bits(__hsub2(bf162_of((q89 & 0x000f000fu) | 0x43004300u), bf162_of(z.y)));
-          q01 >>= 4;
-          q89 >>= 4;
-        }
-        mma_bf16(acc[i][j], d[0], d[1], d[2], d[3], b.x, b.y);
-      }
-    }
-  };
-  constexpr int kAhead = 3;
-  static_assert(kStageBlocks % (kTurns * kAhead) == 0, "a stage is a whole number of rounds of every warp's ring");
-  Load l[kAhead];
-  int64_t fetched = begin / 16 + turn;
-#pragma unroll
-  for (int k = 0; k < kAhead; ++k, fetched += kTurns)
-    if (fetched < blocks_end) fetch(l[k], fetched);
-  for (int64_t base = begin; base < end; base += kStageBlocks * 16) {
-    __syncthreads();
-    const int blocks = (int)(min((int64_t)kStageBlocks * 16, end - base) + 15) / 16;
-    // parts of g s, zeros past the end; a thread takes four rows of a block and one row of g
-    for (int i = threadIdx.x; i < blocks * variants * 4 * kBwdFewRows; i += kThreads) {
-      const int q = i & 3, m = (i >> 2) % kBwdFewRows, bv = (i >> 2) / kBwdFewRows;
-      const int v = bv & (variants - 1), b = bv >> variant_log;
-      const int64_t n0 = base + b * 16 + 2 * q;
-      float f[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int64_t n = n0 + (r & 1) + (r >> 1) * 8;
-        f[r] = 0.f;
-        if (n < end && m < a.m) {
-          const int64_t at = n * w.groups + min(slab * variants + v, w.groups - 1);
-          f[r] = value_at(a.g_dtype, a.g, m * a.ldg + n);
-          if (ACID_IN_BOUNDS(kSiteQ4, at, w.n * w.groups)) f[r] *= value_at(a.scale_dtype, w.scales, at);
-        }
-      }
-#pragma unroll
-      for (int part = 0; part < 3; ++part) {
-        uint32_t h[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
-          const float x = __low2float(p), y = __high2float(p);
-          h[e] = bits(p);
-          f[2 * e] = isfinite(x) ? f[2 * e] - x : 0.f;  // nothing is left of an infinity or a NaN
-          f[2 * e + 1] = isfinite(y) ? f[2 * e + 1] - y : 0.f;
-        }
-        bs[(b * variants + v) * 32 + (3 * m + part) * 4 + q] = make_uint2(h[0], h[1]);
-      }
-    }
-    if (base == begin)  // columns that no part uses
-      for (int i = threadIdx.x; i < kStageBlocks * variants * 8; i += kThreads) bs[i / 8 * 32 + 24 + i % 8] = make_uint2(0, 0);
-    if (w.zeros != nullptr)
-      for (int i = threadIdx.x; i < blocks * variants * 4; i += kThreads) {
-        const int q = i & 3, v = (i >> 2) & (variants - 1), b = (i >> 2) >> variant_log;
-        uint32_t z[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int64_t n = min(base + b * 16 + 2 * q + (r & 1) + (r >> 1) * 8, w.n - 1);
-          const int64_t at = n * w.groups + min(slab * variants + v, w.groups - 1);
-          z[r] = ACID_IN_BOUNDS(kSiteQ4, at, w.n * w.groups) ? w.zeros[at] & 15u : 8u;
-        }
-        zs[i] = make_uint2(0x43004300u | z[0] | z[1] << 16, 0x43004300u | z[2] | z[3] << 16);
-      }
-    __syncthreads();
-#pragma unroll 1
-    for (int k0 = turn; k0 < kStageBlocks; k0 += kTurns * kAhead)
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        if (k0 + k * kTurns < blocks) compute(l[k], k0 + k * kTurns);
-        if (fetched < blocks_end) fetch(l[k], fetched);
-        fetched += kTurns;
-      }
-  }
-  // the warps' sums, then the CTA's share
-  __syncthreads();
-  float* red = reinterpret_cast<float*>(smem);  // [warp][column][128]
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int c = 32 * i + 8 * (g & 3) + 4 * (g >> 2) + 2 * j;
-        *reinterpret_cast<float2*>(red + (turn * 8 + 2 * t + e) * 128 + c) = make_float2(acc[i][j][e], acc[i][j][2 + e]);
-      }
-  __syncthreads();
-  for (int i = threadIdx.x; i < (int)a.m * 128; i += kThreads) {
-    const int m = i / 128, c = i % 128;
-    float v = 0.f;
-    for (int u = 0; u < kTurns; ++u)
-#pragma unroll
-      for (int part = 0; part < 3; ++part) v += red[(u * 8 + 3 * m + part) * 128 + c];
-    const int64_t at = (blockIdx.y * a.m + m) * w.slabs * 128 + slab * 128 + c;
-    if (ACID_IN_BOUNDS(kSiteQ4, at, a.shares * a.m * w.slabs * 128)) a.part[at] = v;
-  }
-}
-
-// Joins the shares in their order and takes the activation's gradient.
-__global__ void __launch_bounds__(kThreads) q4_backward_join_kernel(Bwd a) {
-  pdl_wait();
-  const int c = blockIdx.x * kThreads + threadIdx.x;
-  const int64_t m = blockIdx.y, width = (int64_t)a.w.slabs * 128;
-  if (c >= a.w.k) return;
-  float v = 0.f;
-#pragma unroll 8
-  for (int b = 0; b < a.shares; ++b) v += a.part[(b * a.m + m) * width + c];
-  if (a.silu) {
-    const float x = value_at(a.x_dtype, a.x, m * a.ldx + c), e = 1.f / (1.f + expf(-x));
-    v *= e * (1.f + x * (1.f - e));
-  }
-  put_value(a.x_dtype, a.dx, m * a.lddx + c, v);
 }
 
 // ---------------------------------------------------------------- quantiser
@@ -669,26 +481,9 @@ Q4 q4_args(const acid_q4_weight& w) {
 
 // Whether the CTAs prepare a(x) themselves: few rows, whose parts fit their shared memory twice an SM.
 bool few_rows(int64_t m, int k) { return m <= kPackedRows && m * k <= 16384; }
-size_t fwd_bytes(const Q4& w, int64_t m) {
-  return few_rows(m, w.k) ? 0 : q4_rows_parts_bytes(w, m) + q4_rows_back_bytes(w, m);
-}
-
-// Rows of the weight to a CTA of the input gradient, shares of the sums and scans.
-int64_t bwd_per(const Q4& w, int64_t m) {
-  if (m > kBwdFewRows) return q4_rows_share(w);
-  const int64_t want = (304 + w.slabs - 1) / w.slabs, most = (w.n + 127) / 128;
-  const int64_t splits = std::max<int64_t>(1, std::min(want, most));
-  return ((w.n + splits - 1) / splits + 15) / 16 * 16;
-}
-int bwd_shares(const Q4& w, int64_t m) {
-  const int64_t per = bwd_per(w, m);
-  return (int)((w.n + per - 1) / per) * (m > kBwdFewRows ? 2 : 1);
-}
-int bwd_scans(const Q4& w, int64_t m) { return m > kBwdFewRows ? (int)((w.n + kQ4ScanRows - 1) / kQ4ScanRows) : 0; }
-size_t bwd_part_bytes(const Q4& w, int64_t m) { return (size_t)bwd_shares(w, m) * m * w.slabs * 128 * sizeof(float); }
-size_t workspace_bytes(const acid_q4_weight& weight, int64_t m) {
-  const Q4 w = q4_args(weight);
-  return std::max<size_t>({16, fwd_bytes(w, m), bwd_part_bytes(w, m) + (size_t)bwd_scans(w, m) * (m + 1) * sizeof(float)});
+size_t fwd_bytes(const Q4& w, int64_t m) { return few_rows(m, w.k) ? 0 : q4_rows_forward_bytes(w, m); }
+size_t workspace_bytes(const Q4& w, int64_t m) {
+  return std::max<size_t>({16, fwd_bytes(w, m), m > 0 ? q4_backward_bytes(w, m) : 0});
 }
 
 // Warps of a CTA that share a row's columns: as many as give every SM eight warps
@@ -803,12 +598,9 @@ extern "C" acid_status acid_q4_linear_forward(int32_t x_dtype, const void* x, in
                "acid_q4_linear_forward: workspace null or not 16-byte aligned");
   ACID_REQUIRE(ws_bytes >= need, ACID_ERR_WORKSPACE,
                "acid_q4_linear_forward: workspace too small (need " + std::to_string(need) + ")");
-  Fwd a{w, x, ldx, M, x_dtype, silu_input != 0, out_dtype, bias, out, ldo, static_cast<uint8_t*>(ws), nullptr, 1};
+  Fwd a{w, x, ldx, M, x_dtype, silu_input != 0, out_dtype, bias, out, ldo, nullptr, nullptr, 1};
   cudaStream_t s = (cudaStream_t)stream;
-  if (need != 0) {
-    a.back = reinterpret_cast<float*>(a.parts + q4_rows_parts_bytes(w, M));
-    return q4_rows_forward(a, weight->scale_dtype, s);
-  }
+  if (need != 0) return q4_rows_forward(a, ws, weight->scale_dtype, s);
   const bool h = weight->scale_dtype == ACID_BF16;
   if (weight->zeros != nullptr) return h ? launch_few<bf16, true>(a, s) : launch_few<float, true>(a, s);
   return h ? launch_few<bf16, false>(a, s) : launch_few<float, false>(a, s);
@@ -819,7 +611,7 @@ extern "C" acid_status acid_q4_linear_workspace_size(const acid_q4_weight* weigh
   ACID_TRY(check_weight(weight));
   ACID_REQUIRE(bytes != nullptr && M >= 0 && M <= kMostRows, ACID_ERR_INVALID_ARG,
                "acid_q4_linear_workspace_size: bad argument");
-  *bytes = workspace_bytes(*weight, M);
+  *bytes = workspace_bytes(q4_args(*weight), M);
   return ACID_OK;
 }
 
@@ -844,25 +636,10 @@ extern "C" acid_status acid_q4_linear_backward(int32_t g_dtype, const void* g, i
     if (silu_input) ACID_TRY(check_matrix(x_dtype, x, ldx, weight->k, "x"));
     ACID_REQUIRE(ws != nullptr && aligned(ws, 16), ACID_ERR_WORKSPACE,
                  "acid_q4_linear_backward: workspace null or not 16-byte aligned");
-    const size_t need = workspace_bytes(*weight, M);
+    const size_t need = workspace_bytes(q4_args(*weight), M);
     ACID_REQUIRE(ws_bytes >= need, ACID_ERR_WORKSPACE,
                  "acid_q4_linear_backward: workspace too small (need " + std::to_string(need) + ")");
   }
-  const Q4 w = q4_args(*weight);
-  Bwd a{w, g, x, ldg, ldx, M, g_dtype, x_dtype, weight->scale_dtype, silu_input != 0, dx, lddx, dbias,
-        static_cast<float*>(ws), bwd_shares(w, M), bwd_per(w, M), nullptr, bwd_scans(w, M)};
-  if (M <= kBwdFewRows || dx == nullptr) {
-    static PerContext allowed;
-    ACID_TRY(allow_smem(allowed, q4_few_backward_kernel, few_smem(4)));
-    const dim3 grid(dx != nullptr ? w.slabs : 1, (unsigned)((w.n + a.per - 1) / a.per));
-    launch_pdl(q4_few_backward_kernel, grid, kThreads, few_smem(128 >> w.group_log), s, a);
-    ACID_CHECK_LAUNCH();
-  } else {
-    a.top = a.part + bwd_part_bytes(w, M) / sizeof(float);
-    ACID_TRY(q4_rows_backward(a, s));
-  }
-  if (dx == nullptr) return ACID_OK;
-  launch_pdl(q4_backward_join_kernel, dim3((w.k + kThreads - 1) / kThreads, (unsigned)M), kThreads, 0, s, a);
-  ACID_CHECK_LAUNCH();
-  return ACID_OK;
+  const Q4Bwd a{q4_args(*weight), g, x, ldg, ldx, M, g_dtype, x_dtype, weight->scale_dtype, silu_input != 0, dx, lddx, dbias};
+  return q4_backward(a, ws, s);
 }

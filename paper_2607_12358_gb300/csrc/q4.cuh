@@ -108,20 +108,20 @@ struct Q4Bwd {
   void* dx;
   int64_t lddx;
   float* dbias;
-  float* part;   // [shares][m][128 slabs]
-  int shares;    // of the sums, joined in their order
-  int64_t per;   // rows of the weight to a CTA
-  float* top;    // past a few rows: [scans][1 + m] largest scale and |g| of each scanned run of the weight's rows
-  int scans;
+  // of the call's workspace
+  float* part;     // [shares][m][128 slabs]: sums, joined in their order
+  uint8_t* parts;  // g as the tensor cores read it
+  float* back;     // [shares / 2][m]: the powers of two taken back
+  uint32_t* top;   // largest scales
+  int shares;
+  int64_t per;     // rows of the weight to a CTA
 };
-constexpr int kQ4Chunk = 64;       // rows of x that a kernel of many rows takes at a time
-constexpr int kQ4ScanRows = 1024;  // rows of the weight to a scan
+constexpr int kQ4Chunk = 64;  // rows of x that a kernel of many rows takes at a time
 
-// Many rows (q4_rows.cu): tcgen05 kernels.
-size_t q4_rows_parts_bytes(const Q4& w, int64_t m);
-size_t q4_rows_back_bytes(const Q4& w, int64_t m);
-acid_status q4_rows_forward(const Q4Fwd& a, int scale_dtype, cudaStream_t s);
-int64_t q4_rows_share(const Q4& w);  // rows of the weight to a CTA of the gradient
-acid_status q4_rows_backward(const Q4Bwd& a, cudaStream_t s);
+// q4_rows.cu: tcgen05 kernels.
+size_t q4_rows_forward_bytes(const Q4& w, int64_t m);
+acid_status q4_rows_forward(Q4Fwd a, void* workspace, int scale_dtype, cudaStream_t s);
+size_t q4_backward_bytes(const Q4& w, int64_t m);
+acid_status q4_backward(Q4Bwd a, void* workspace, cudaStream_t s);
 
 }  // namespace acid

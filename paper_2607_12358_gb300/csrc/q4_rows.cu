@@ -16,8 +16,7 @@ namespace {
 
 using bf16 = __nv_bfloat16;
 constexpr int kThreads = 256;
-constexpr int kRowsThreads = 320;  // product: eight warps that make operands, an MMA warp and a copying warp
-constexpr int kBackThreads = 416;  // gradient: eight and four warps that make operands, and an MMA warp
+constexpr int kRowsThreads = 576;  // product: 16 warps that make operands, an MMA warp and a copying warp
 
 // Instruction descriptor of kind::f16 with fp16 A and B, fp32 accumulator.
 __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool b_mn) {
@@ -35,6 +34,17 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+// One arrival for the warp, after what all its lanes did.
+__device__ __forceinline__ void arrive_warp(uint64_t* bar, bool leader) {
+  __syncwarp();
+  if (leader) mbar_arrive(bar);
+}
+__device__ __forceinline__ uint4 load_codes(const uint32_t* p) { return *reinterpret_cast<const uint4*>(p); }
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
                    smem_u32(dst)),
@@ -42,21 +52,54 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                : "memory");
 }
 
+// A word's eight columns as two halves each, s (q - z) in s = sh + sl: the product
+// with sh rounded to a half, and what is left of it (exact: sh (q - z) has 15 bits
+// at most) with sl's part: 22 bits together.
+template <bool LOW>  // whether sl is there (scales of more than a half's 11 bits)
+__device__ __forceinline__ void scaled_halves(uint32_t word, uint32_t z, uint32_t sh, uint32_t sl, uint32_t* hi, uint32_t* lo) {
+  uint32_t d[4];
+  halves_of(word, z, d);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const __half2 c = half2_of(d[j]), h = __hmul2(c, half2_of(sh));
+    __half2 l = __hfma2(c, half2_of(sh), __hneg2(h));
+    if constexpr (LOW) l = __hfma2(c, half2_of(sl), l);
+    hi[j] = bits(h);
+    lo[j] = bits(l);
+  }
+}
+// sh and sl of a scale after its power of two, each in both halves.
+__device__ __forceinline__ void split_scale(float s, uint32_t& sh, uint32_t& sl) {
+  const __half h = __float2half_rn(s);
+  sh = bits(__half2half2(h));
+  sl = bits(__half2half2(__float2half_rn(s - __half2float(h))));
+}
+// The power of two that brings the largest scale, `top` in bits, to 2^10 .. 2^11 (2^127
+// at most): values below 2^15, and what is left of them far above a half's least.
+__device__ __forceinline__ float up_to_scale(uint32_t top) {
+  return __uint_as_float((uint32_t)min(264 - (int)(top >> 23), 254) << 23);
+}
+__device__ __forceinline__ uint32_t finite_bits(float v) { return isfinite(v) ? __float_as_uint(fabsf(v)) : 0u; }
+
 // ------------------------------------------------------------------ product
-// D[128 rows of the weight, 16 NT] = codes x parts^T for each group of columns,
-// the codes as the exact halves q - z in tensor memory (a row to a lane, where the
-// lane's thread writes them), the parts of a(x) in shared memory (8 NT rows of high
-// parts, then of low parts).  The same threads read the group's sums back, a row to a
-// thread, and add them to the row's totals times its scale and the parts' powers of
-// two.  A CTA has two tiles of 128 rows, whose four warps each run on their own.
+// D[128 rows of the weight, 16 NT] = values x parts^T, the values as two halves in
+// tensor memory (a row to a lane, where the lane's thread writes them, after a power
+// of two of the row), the parts of a(x) in shared memory (8 NT rows of high parts,
+// then of low parts).  The tensor cores' sums lose up to 2^-23 of themselves at each
+// addition, always towards zero, so that they are read back after each slab (12
+// additions on a sum of its size) and added up in fp32 by the rows' threads: over 65536
+// columns left in tensor memory a sum was 1.7e-4 off.  A CTA has two tiles of 128
+// rows; each of their lanes belongs to two threads, which share its words and its
+// sums: with one, two warps a scheduler left half of the issue slots empty (36864 x
+// 3072, 34 rows: 42 us).
 constexpr int kFwdRing = 4;   // slabs of parts in shared memory
-constexpr int kCodeRing = 3;  // slabs of a warp's 32 rows of codes
+constexpr int kCodeRing = 4;  // slabs of a warp's share of 32 rows of codes
 // Bytes of a slab's parts: two boxes of 64 columns, rows of 128 bytes whose
 // 16-byte units are swizzled as the tensor cores read them.
 template <int NT>
 constexpr int kSlabBytes = 16 * NT * 256;
 template <int NT>
-constexpr int kFwdSmem = kFwdRing * kSlabBytes<NT> + 8 * kCodeRing * 2048 + 256 + 1024;
+constexpr int kFwdSmem = kFwdRing * kSlabBytes<NT> + 16 * kCodeRing * 1024 + 256 + 1024;
 
 // One CTA to a row of a(x).
 template <int NT>
@@ -92,13 +135,14 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* ring = smem;
   uint8_t* codes = ring + kFwdRing * kSlabBytes<NT>;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(codes + 8 * kCodeRing * 2048);
-  uint64_t *b_full = bars, *b_empty = bars + kFwdRing;                           // [ring]
-  uint64_t *a_full = b_empty + kFwdRing, *d_full = a_full + 4, *d_empty = d_full + 2;  // [tile][2], [tile], [tile]
-  uint64_t* drain = d_empty + 2;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(codes + 16 * kCodeRing * 1024);
+  uint64_t *b_full = bars, *b_empty = bars + kFwdRing;                                      // [ring]
+  uint64_t *a_full = b_empty + kFwdRing, *a_empty = a_full + 4;                             // [tile][2]
+  uint64_t *d_full = a_empty + 4, *d_empty = d_full + 2, *drain = d_empty + 2;              // [tile]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   constexpr int kCols = 16 * NT, kHalf = 8 * NT;
-  constexpr uint32_t kACol = 0, kDCol = 256;  // tensor memory: codes [tile][2][64], sums [tile][<= 128]
+  // tensor memory: values [tile][2 buffers][high, low][32] of 64 columns, sums [tile][<= 128]
+  constexpr uint32_t kACol = 0, kDCol = 256;
   const Q4& w = a.w;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -106,15 +150,18 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
       mbar_init(&b_full[i], 1);
       mbar_init(&b_empty[i], 1);
     }
-    for (int i = 0; i < 4; ++i) mbar_init(&a_full[i], 128);
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&a_full[i], 8);
+      mbar_init(&a_empty[i], 1);
+    }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&d_full[i], 1);
-      mbar_init(&d_empty[i], 128);
+      mbar_init(&d_empty[i], 8);
     }
     mbar_init(drain, 1);
     mbar_fence_init();
   }
-  if (warp == 8) tmem_alloc(tmem_slot, 512);
+  if (warp == 16) tmem_alloc(tmem_slot, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -122,11 +169,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
   pdl_wait();
 
   const int64_t sets = (w.n + 255) / 256, chunk = blockIdx.y, m0 = chunk * kQ4Chunk;
-  const int group = 1 << w.group_log, per_slab = 128 >> w.group_log;
-  const int words = group / 32;  // of 32 columns, to a group
   const uint8_t* parts = a.parts + chunk * w.slabs * kSlabBytes<NT>;
 
-  if (warp == 9) {
+  if (warp == 17) {
     if (lane == 0) {  // ------------------------------------------ copies of the parts
       int issued = 0;
       bool ok = true;
@@ -142,32 +187,38 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
         for (int j = issued > kFwdRing ? issued - kFwdRing : 0; j < issued; ++j)
           mbar_wait(&b_full[j % kFwdRing], (j / kFwdRing) & 1);
     }
-  } else if (warp == 8) {
+  } else if (warp == 16) {
     // ------------------------------------------------------------- MMA issuer
     const bool leader = elect_one();
     constexpr uint32_t idesc = idesc_f16_f32(128, kCols, false);
     const uint64_t bdesc = smem_desc_sw128(smem_u32(ring), 16, 1024);
     bool ok = true;
-    uint32_t u = 0;  // steps (groups of columns)
+    constexpr uint32_t idesc_low = idesc_f16_f32(128, (kHalf + 15) / 16 * 16, false);  // low values: high parts are enough
+    uint32_t u = 0;  // steps of 64 columns
     int v = 0;       // slabs
     for (int64_t set = blockIdx.x; ok && set < sets; set += gridDim.x)
       for (int slab = 0; ok && slab < w.slabs; ++slab, ++v) {
         const int st = v % kFwdRing;
         if (!mbar_wait_warp(&b_full[st], (v / kFwdRing) & 1)) { ok = false; break; }
-        const uint64_t slot = bdesc + (uint64_t)((st * kSlabBytes<NT>) >> 4);
-        for (int i = 0; ok && i < per_slab; ++i, ++u)
+        for (int h = 0; ok && h < 2; ++h, ++u)
           for (int tile = 0; tile < 2; ++tile) {
             if (!mbar_wait_warp(&a_full[tile * 2 + (u & 1)], (u >> 1) & 1)) { ok = false; break; }
-            if (u > 0 && !mbar_wait_warp(&d_empty[tile], (u - 1) & 1)) { ok = false; break; }
+            if (h == 0 && v > 0 && !mbar_wait_warp(&d_empty[tile], (v - 1) & 1)) { ok = false; break; }
             tc_fence_after();
             if (leader) {
               const uint32_t d = tmem + kDCol + tile * 128, c = tmem + kACol + tile * 128 + (u & 1) * 64;
-              for (int k = 0; k < group / 16; ++k) {
-                const int kk = i * (group / 16) + k;  // 16 columns of the slab
-                mma_bf16_ts(d, c + k * 8, slot + (uint64_t)(((kk >> 2) * (kCols * 128) + (kk & 3) * 32) >> 4), idesc, k != 0);
-              }
-              if (i == per_slab - 1 && tile == 1) mma_commit(&b_empty[st]);
-              mma_commit(&d_full[tile]);
+              const uint64_t slot = bdesc + (uint64_t)((st * kSlabBytes<NT> + h * (kCols * 128)) >> 4);
+              if (h == 0)  // clears all columns; the low values come first, on small sums
+                mma_bf16_ts(d, c + 32, slot, idesc, false);
+              else
+                mma_bf16_ts(d, c + 32, slot, idesc_low, true);
+#pragma unroll
+              for (int k = 1; k < 4; ++k) mma_bf16_ts(d, c + 32 + k * 8, slot + (uint64_t)((k * 32) >> 4), idesc_low, true);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) mma_bf16_ts(d, c + k * 8, slot + (uint64_t)((k * 32) >> 4), idesc, true);
+              if (h == 1 && tile == 1) mma_commit(&b_empty[st]);
+              mma_commit(&a_empty[tile * 2 + (u & 1)]);
+              if (h == 1) mma_commit(&d_full[tile]);
             }
             __syncwarp();
           }
@@ -177,74 +228,90 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
       mbar_wait(drain, 0);
     }
   } else {
-    // ----------------------- codes into tensor memory, sums out of it: warps 0-3 tile 0, 4-7 tile 1
-    const int tile = warp >> 2, g = lane >> 2, t = lane & 3;
+    // ------------------- values into tensor memory, sums out of it: warps 0-7 tile 0, 8-15 tile 1; in a tile two warps
+    // to a quarter of the lanes, which share the words and the columns of the sums
+    const int tile = warp >> 3, half = (warp >> 2) & 1;
+    const bool leader = elect_one();
     const uint32_t quad = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t c_addr = tmem + quad + kACol + tile * 128, d_addr = tmem + quad + kDCol + tile * 128;
-    uint8_t* mine = codes + warp * kCodeRing * 2048;
-    // A lane copies 16 bytes of the rows g, g + 8, g + 16, g + 24 of the warp's 32 (64 bytes of a row together) and
-    // reads its own row back; the units of a row are exchanged so that eight rows' reads lie in different banks.
-    auto place = [](int row, int unit) { return row * 64 + ((unit ^ ((row >> 1) & 3)) << 4); };
+    const uint32_t c_addr = tmem + quad + kACol + tile * 128 + half * 8, d_addr = tmem + quad + kDCol + tile * 128;
+    uint8_t* mine = codes + warp * kCodeRing * 1024;
+    const int per_slab = 128 >> w.group_log, word_log = w.group_log - 5;
+    const int row_in_set = tile * 128 + (warp & 3) * 32;
+    // A lane copies 16 bytes of two of the warp's 32 rows (32 bytes of a row together) and reads its own row back; the
+    // units of every other four rows are exchanged, so that eight rows' reads lie in different banks.
+    auto place = [](int row, int unit) { return row * 32 + ((unit ^ ((row >> 2) & 1)) << 4); };
     int64_t fset = blockIdx.x;
     int fslab = 0, fst = 0;
+    const uint32_t* src[2] = {};
+    auto aim = [&] {  // the copies' rows in set fset
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int64_t row = min(fset * 256 + row_in_set + (lane >> 1) + 16 * q, w.n - 1);
+        src[q] = w.packed + row * w.slabs * 16 + 8 * half + 4 * (lane & 1);
+      }
+    };
+    aim();
     auto copy = [&] {
       if (fset < sets) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int64_t row = min(fset * 256 + warp * 32 + g + 8 * q, w.n - 1);
-          const int64_t at = (row * w.slabs + fslab) * 16 + 4 * t;
-          const bool in = ACID_IN_BOUNDS(kSiteQ4, at + 3, w.n * w.slabs * 16);
-          cp_async<16>(mine + fst * 2048 + place(g + 8 * q, t), w.packed + (in ? at : 0), in);
+        for (int q = 0; q < 2; ++q) {
+          const bool in = ACID_IN_BOUNDS(kSiteQ4, src[q] - w.packed + 3, w.n * w.slabs * 16);
+          cp_async<16>(mine + fst * 1024 + place((lane >> 1) + 16 * q, lane & 1), in ? src[q] : w.packed, in);
+          src[q] += 16;
         }
         if (++fslab == w.slabs) {
           fslab = 0;
           fset += gridDim.x;
+          aim();
         }
       }
       cp_async_commit();
       fst = fst + 1 == kCodeRing ? 0 : fst + 1;
     };
     for (int i = 0; i < kCodeRing - 1; ++i) copy();
-    uint64_t total[NT][4];  // pairs of the row's sums
     bool ok = true;
-    uint32_t u = 0;
-    // Adds the sums of step `step`, whose scale is s.
-    auto take = [&](uint32_t step, float s) -> bool {
-      if (!mbar_wait_warp(&d_full[tile], step & 1)) return false;
+    uint32_t u = 0, taken = 0;  // steps of 64 columns; slabs whose sums were read back
+    int st = 0;
+    constexpr int kMine = (NT + 1) / 2;  // column tiles of a thread's sums: the first ones, or the rest
+    const int n_first = half * kMine;
+    uint64_t total[kMine][4];  // pairs of the row's sums
+    auto take = [&]() -> bool {
+      if (!mbar_wait_warp(&d_full[tile], taken & 1)) return false;
+      ++taken;
       tc_fence_after();
-      constexpr int kBatch = NT <= 5 ? NT : 4;
+      constexpr int kBatch = kMine < 3 ? kMine : kMine == 3 ? 3 : 2;
 #pragma unroll
-      for (int n0 = 0; n0 < NT; n0 += kBatch) {
+      for (int n0 = 0; n0 < kMine; n0 += kBatch) {
         uint32_t hi[kBatch][8], lo[kBatch][8];
 #pragma unroll
-        for (int n = 0; n < kBatch; ++n) {
-          tmem_ld8(d_addr + (n0 + n) * 8, hi[n]);
-          tmem_ld8(d_addr + kHalf + (n0 + n) * 8, lo[n]);
+        for (int n = 0; n < kBatch; ++n) {  // (an odd tile count: the last one is read twice)
+          const int c = min(n_first + n0 + n, NT - 1) * 8;
+          tmem_ld8(d_addr + c, hi[n]);
+          tmem_ld8(d_addr + kHalf + c, lo[n]);
         }
         tmem_wait_ld();
-        if (n0 + kBatch == NT) {
+        if (n0 + kBatch == kMine) {
           tc_fence_before();
-          mbar_arrive(&d_empty[tile]);
+          arrive_warp(&d_empty[tile], leader);
         }
-        const uint64_t s2 = f2_pack(s, s);
 #pragma unroll
         for (int n = 0; n < kBatch; ++n)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint64_t x = f2_add(f2_pack(__uint_as_float(hi[n][2 * e]), __uint_as_float(hi[n][2 * e + 1])),
-                                      f2_pack(__uint_as_float(lo[n][2 * e]), __uint_as_float(lo[n][2 * e + 1])));
-            total[n0 + n][e] = f2_fma(x, s2, total[n0 + n][e]);
-          }
+          for (int e = 0; e < 4; ++e)
+            total[n0 + n][e] =
+                f2_add(total[n0 + n][e],
+                       f2_add(f2_pack(__uint_as_float(hi[n][2 * e]), __uint_as_float(hi[n][2 * e + 1])),
+                              f2_pack(__uint_as_float(lo[n][2 * e]), __uint_as_float(lo[n][2 * e + 1]))));
       }
       return true;
     };
-    int st = 0;
     for (int64_t set = blockIdx.x; ok && set < sets; set += gridDim.x) {
-      const int64_t row = set * 256 + warp * 32 + lane, at = min(row, w.n - 1) * w.groups;
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < kMine; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) total[n][e] = 0;
+      const int64_t row = set * 256 + row_in_set + lane, at = min(row, w.n - 1) * w.groups;
+      const TS* scale = static_cast<const TS*>(w.scales) + at;
       // scales and zero points of a slab's groups, a slab ahead
       float scales[4];
       uint8_t zeros[4];
@@ -252,203 +319,253 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if (i >= per_slab) break;
-          const int64_t p = at + min(slab * per_slab + i, w.groups - 1);
-          if (!ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.groups)) continue;
-          scales[i] = io<TS>::ld(static_cast<const TS*>(w.scales) + p);
-          if (w.zeros != nullptr) zeros[i] = w.zeros[p];
+          const int p = min(slab * per_slab + i, w.groups - 1);
+          if (!ACID_IN_BOUNDS(kSiteQ4, at + p, w.n * w.groups)) continue;
+          scales[i] = io<TS>::ld(scale + p);
+          if (w.zeros != nullptr) zeros[i] = w.zeros[at + p];
         }
       };
       look(0);
-      float scale = 0.f;  // of the step whose sums are not taken yet
-      bool pending = false;
+      // the row's power of two
+      uint32_t top = 0;
+#pragma unroll 8
+      for (int i = 0; i < w.groups; ++i)
+        if (ACID_IN_BOUNDS(kSiteQ4, at + i, w.n * w.groups)) top = max(top, finite_bits(io<TS>::ld(scale + i)));
+      const float one = up_to_scale(top);
       for (int slab = 0; ok && slab < w.slabs; ++slab) {
         cp_async_wait<kCodeRing - 2>();
         __syncwarp();
-        uint4 q[4];  // q[t]: words of the columns 32 i + 8 t
+        uint4 q[2];  // words of the columns 32 i + 16 half + 8 c
 #pragma unroll
-        for (int c = 0; c < 4; ++c) q[c] = *reinterpret_cast<const uint4*>(mine + st * 2048 + place(lane, c));
+        for (int c = 0; c < 2; ++c) q[c] = *reinterpret_cast<const uint4*>(mine + st * 1024 + place(lane, c));
         copy();
         st = st + 1 == kCodeRing ? 0 : st + 1;
-        float s[4];
-        uint32_t z[4];
+        uint32_t sh[4], sl[4], z[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          s[i] = scales[i];
-          z[i] = w.zeros != nullptr ? zeros[i] : 8u;
+          if (i >= per_slab) break;
+          split_scale(scales[i] * one, sh[i], sl[i]);
+          z[i] = w.zeros != nullptr ? zeros[i] & 15u : 8u;
         }
         if (slab + 1 < w.slabs) look(slab + 1);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int within = i & (words - 1), of = words == 4 ? 0 : words == 2 ? i >> 1 : i;
-          const uint32_t zero = of == 0 ? z[0] : of == 1 ? z[1] : of == 2 ? z[2] : z[3];
-          uint32_t d[16];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t h[4];
-            halves_of(i == 0 ? q[c].x : i == 1 ? q[c].y : i == 2 ? q[c].z : q[c].w, zero, h);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) d[4 * c + j] = h[j];
+          if ((i & 1) == 0) {  // a step of 64 columns: its buffer is free
+            if (u >= 2 && ok) ok = mbar_wait_warp(&a_empty[tile * 2 + (u & 1)], ((u >> 1) - 1) & 1);
           }
-          tmem_st16(c_addr + (u & 1) * 64 + within * 16, d);
-          if (within != words - 1) continue;
+          const int of = i >> word_log;
+          const uint32_t h = of == 0 ? sh[0] : of == 1 ? sh[1] : of == 2 ? sh[2] : sh[3];
+          const uint32_t l = of == 0 ? sl[0] : of == 1 ? sl[1] : of == 2 ? sl[2] : sl[3];
+          const uint32_t zero = of == 0 ? z[0] : of == 1 ? z[1] : of == 2 ? z[2] : z[3];
+          uint32_t hi[8], lo[8];
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+            scaled_halves<sizeof(TS) == 4>(i == 0 ? q[c].x : i == 1 ? q[c].y : i == 2 ? q[c].z : q[c].w, zero, h, l,
+                                           hi + 4 * c, lo + 4 * c);
+          if (ok) {
+            tmem_st8(c_addr + (u & 1) * 64 + (i & 1) * 16, hi);
+            tmem_st8(c_addr + (u & 1) * 64 + 32 + (i & 1) * 16, lo);
+          }
+          if ((i & 1) == 0) continue;
           tmem_wait_st();
           tc_fence_before();
-          mbar_arrive(&a_full[tile * 2 + (u & 1)]);
-          // the sums of the step before, while this one's are formed
-          if (pending && ok) ok = take(u - 1, scale);
-          pending = true;
-          scale = of == 0 ? s[0] : of == 1 ? s[1] : of == 2 ? s[2] : s[3];
+          arrive_warp(&a_full[tile * 2 + (u & 1)], leader);
           ++u;
+          // the sums of the slab before, while this one's are formed
+          if (i == 1 && slab > 0 && ok) ok = take();
         }
       }
-      if (ok) ok = take(u - 1, scale);
+      if (ok) ok = take();
       if (!ok || row >= w.n) continue;
-      const float bias = a.bias != nullptr ? a.bias[row] : 0.f;
+      const float bias = a.bias != nullptr ? a.bias[row] : 0.f, down = 1.f / one;
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < kMine; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int64_t m = m0 + 8 * n + 2 * e;
+          const int64_t m = m0 + 8 * (n_first + n) + 2 * e;
+          if (n_first + n >= NT) continue;
           float x, y;
           f2_unpack(total[n][e], x, y);
-          if (m < a.m) put_value(a.out_dtype, a.out, m * a.ldo + row, fmaf(x, a.back[m], bias));
-          if (m + 1 < a.m) put_value(a.out_dtype, a.out, (m + 1) * a.ldo + row, fmaf(y, a.back[m + 1], bias));
+          if (m < a.m) put_value(a.out_dtype, a.out, m * a.ldo + row, fmaf(x * down, a.back[m], bias));
+          if (m + 1 < a.m) put_value(a.out_dtype, a.out, (m + 1) * a.ldo + row, fmaf(y * down, a.back[m + 1], bias));
         }
     }
     cp_async_wait<0>();
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 8) {
+  if (warp == 16) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
 }
 
 // ----------------------------------------------------------- input gradient
-// D[2 x 64 parts of g s, 128 columns] += parts x codes for 128 rows of the weight at a
-// time.  (g s), a power of two that brings its largest value below 2^15, and
-// two halves of it are formed by the threads of a lane of tensor memory (row m of
-// g: lane m its high parts, lane 64 + m its low parts), once for each of the slab's
-// groups; the codes, exact halves q - z, are written to shared memory, where they
-// are the second operand as they lie (columns together).  Sums stay in tensor memory
-// over all of a CTA's rows.
-struct BwdSmem {
-  static constexpr int kCodes = 128 * 256;                // [box of 64 columns][128 rows][128 bytes]
-  static constexpr int kGStride = 132;                    // floats of a row of g: 128 and a shift of the banks
-  static constexpr int kG = kQ4Chunk * kGStride * 4;
-  static constexpr int kOffG = 2 * kCodes, kOffS = kOffG + 2 * kG, kOffBar = kOffS + 2 * 4 * 128 * 4;
-  static constexpr int kBytes = kOffBar + 256 + 1024;
+// D[2 x 64 parts of g, 128 columns] += parts x values for 128 rows of the weight at a
+// time.  The parts of g (row m: lane m its high halves, lane 64 + m its low halves)
+// come from q4_back_parts_kernel and go to tensor memory; the values, two halves
+// each, are written to shared memory, where they are the second operand as they lie
+// (columns together).  A block's sums are read back and added up in fp32, as in the
+// product, while the next block's are formed.
+//   Bound by shared memory: a block's values are 64 KB written and 64 KB read, 1024
+// clocks.
+constexpr int kBackThreads = 576;  // 16 warps that make operands and read sums, an MMA warp and a copying warp
+constexpr int kBackRing = 3;  // blocks of a warp's eight rows of codes
+struct BackSmem {
+  static constexpr int kPart = 128 * 256;    // [box of 64 columns][128 rows][128 bytes]
+  static constexpr int kBuffer = 2 * kPart;  // high, low
+  static constexpr int kParts = 16 * 2 * kQ4Chunk * 16;  // a block of g's parts
+  static constexpr int kOffParts = 2 * kBuffer, kOffCodes = kOffParts + 2 * kParts;
+  static constexpr int kOffBar = kOffCodes + 16 * kBackRing * 512, kBytes = kOffBar + 256 + 1024;
 };
+constexpr int kTopRuns = 8;  // parts of a share's scales that are scanned by a CTA each
 
-// Largest scale and largest |g| of each row over runs of kQ4ScanRows rows of the
-// weight (blockIdx.y: a chunk of g's rows), and the bias's gradient.
-__global__ void __launch_bounds__(kThreads) q4_scan_kernel(Q4Bwd a) {
-  __shared__ uint32_t top[1 + kQ4Chunk];  // bits of non-negative floats
+__device__ __forceinline__ void bias_of(const Q4Bwd& a, int64_t n) {
+  float sum = 0.f;
+#pragma unroll 8
+  for (int64_t m = 0; m < a.m; ++m) sum += value_at(a.g_dtype, a.g, m * a.ldg + n);
+  a.dbias[n] = sum;
+}
+// The bias's gradient alone.
+__global__ void __launch_bounds__(kThreads) q4_bias_kernel(Q4Bwd a) {
   pdl_wait();
-  const int lane = threadIdx.x & 31;
-  const bool first = blockIdx.y == 0;
-  const int64_t n0 = (int64_t)blockIdx.x * kQ4ScanRows, n1 = min(a.w.n, n0 + kQ4ScanRows);
-  const int64_t m0 = (int64_t)blockIdx.y * kQ4Chunk, m1 = min(a.m, m0 + kQ4Chunk);
-  if (threadIdx.x <= kQ4Chunk) top[threadIdx.x] = 0;
-  __syncthreads();
-  auto bits_of = [](float v) { return isfinite(v) ? __float_as_uint(fabsf(v)) : 0u; };
-  if (first) {
-    uint32_t s = 0;
-    for (int64_t i = n0 * a.w.groups + threadIdx.x; i < n1 * a.w.groups; i += kThreads)
-      if (ACID_IN_BOUNDS(kSiteQ4, i, a.w.n * a.w.groups)) s = max(s, bits_of(value_at(a.scale_dtype, a.w.scales, i)));
-    s = __reduce_max_sync(0xffffffffu, s);
-    if (lane == 0) atomicMax(&top[0], s);
-  }
-  constexpr int kPer = kQ4ScanRows / kThreads;
-  float sum[kPer] = {};
-#pragma unroll 4
-  for (int64_t m = m0; m < m1; ++m) {
-    uint32_t t = 0;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int64_t n = n0 + j * kThreads + threadIdx.x;
-      const float v = n < n1 ? value_at(a.g_dtype, a.g, m * a.ldg + n) : 0.f;
-      sum[j] += v;
-      t = max(t, bits_of(v));
-    }
-    t = __reduce_max_sync(0xffffffffu, t);
-    if (lane == 0) atomicMax(&top[1 + m - m0], t);
-  }
-  if (first && a.dbias != nullptr)
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int64_t n = n0 + j * kThreads + threadIdx.x;
-      if (n >= n1) continue;
-      for (int64_t m = m1; m < a.m; ++m) sum[j] += value_at(a.g_dtype, a.g, m * a.ldg + n);
-      a.dbias[n] = sum[j];
-    }
-  __syncthreads();
-  float* out = a.top + blockIdx.x * (a.m + 1);
-  if (first && threadIdx.x == 0) out[0] = __uint_as_float(top[0]);
-  if (threadIdx.x < m1 - m0) out[1 + m0 + threadIdx.x] = __uint_as_float(top[1 + threadIdx.x]);
+  for (int64_t n = (int64_t)blockIdx.x * kThreads + threadIdx.x; n < a.w.n; n += (int64_t)gridDim.x * kThreads) bias_of(a, n);
 }
 
-template <typename TG, typename TS>
+// For each share of the weight's rows (blockIdx.x): the parts of a row of g, after
+// a power of two of the row and share (y < m); the largest scale of a part of the share
+// (the next kTopRuns); the bias's gradient of 256 rows (the rest).
+//   parts: [chunk][run of 8 rows of the weight][2][rows of the chunk][8]
+__global__ void __launch_bounds__(kThreads) q4_back_parts_kernel(Q4Bwd a) {
+  __shared__ uint32_t largest;
+  pdl_wait();
+  const int64_t begin = blockIdx.x * a.per, end = min(a.w.n, begin + a.per), y = blockIdx.y;
+  if (y >= a.m + kTopRuns) {
+    const int64_t step = (gridDim.y - a.m - kTopRuns) * kThreads;
+    for (int64_t n = begin + (y - a.m - kTopRuns) * kThreads + threadIdx.x; n < end; n += step) bias_of(a, n);
+    return;
+  }
+  if (threadIdx.x == 0) largest = 0;
+  __syncthreads();
+  uint32_t top = 0;
+  auto join = [&] {
+    top = __reduce_max_sync(0xffffffffu, top);
+    if ((threadIdx.x & 31) == 0) atomicMax(&largest, top);
+    __syncthreads();
+  };
+  if (y >= a.m) {
+    const int64_t run = y - a.m, all = (end - begin) * a.w.groups, per = (all + kTopRuns - 1) / kTopRuns;
+    const int64_t i0 = begin * a.w.groups + run * per, i1 = begin * a.w.groups + min(all, (run + 1) * per);
+#pragma unroll 8
+    for (int64_t i = i0 + threadIdx.x; i < i1; i += kThreads)
+      if (ACID_IN_BOUNDS(kSiteQ4, i, a.w.n * a.w.groups)) top = max(top, finite_bits(value_at(a.scale_dtype, a.w.scales, i)));
+    join();
+    if (threadIdx.x == 0) a.top[blockIdx.x * kTopRuns + run] = largest;
+    return;
+  }
+  const int64_t m = y, chunk = m / kQ4Chunk, rows = min((int64_t)kQ4Chunk, a.m - chunk * kQ4Chunk), r = m - chunk * kQ4Chunk;
+#pragma unroll 8
+  for (int64_t n = begin + threadIdx.x; n < end; n += kThreads)
+    top = max(top, finite_bits(value_at(a.g_dtype, a.g, m * a.ldg + n)));
+  join();
+  const float up = up_to_half(__uint_as_float(largest));
+  if (threadIdx.x == 0) a.back[blockIdx.x * a.m + m] = 1.f / up;
+  // runs of eight rows of the weight; the last block of a share is filled with zeros
+  const int64_t runs = (min(begin + a.per, (a.w.n + 127) / 128 * 128) - begin) / 8, all_runs = (a.w.n + 127) / 128 * 16;
+  for (int64_t i = threadIdx.x; i < runs; i += kThreads) {
+    const int64_t n0 = begin + i * 8;
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float v0 = n0 + 2 * j < end ? value_at(a.g_dtype, a.g, m * a.ldg + n0 + 2 * j) * up : 0.f;
+      const float v1 = n0 + 2 * j + 1 < end ? value_at(a.g_dtype, a.g, m * a.ldg + n0 + 2 * j + 1) * up : 0.f;
+      const __half2 p = __floats2half2_rn(v0, v1);
+      const float2 f = __half22float2(p);
+      h[j] = bits(p);
+      // nothing is left of an infinity or a NaN
+      l[j] = bits(__floats2half2_rn(isfinite(f.x) ? v0 - f.x : 0.f, isfinite(f.y) ? v1 - f.y : 0.f));
+    }
+    uint4* out = reinterpret_cast<uint4*>(a.parts) + chunk * all_runs * 2 * kQ4Chunk + (n0 / 8) * 2 * rows + r;
+    out[0] = make_uint4(h[0], h[1], h[2], h[3]);
+    out[rows] = make_uint4(l[0], l[1], l[2], l[3]);
+  }
+}
+
+template <typename TS>
 __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd a) {
   extern __shared__ uint8_t smem_raw[];
-  using L = BwdSmem;
+  using L = BackSmem;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  float* gs = reinterpret_cast<float*>(smem + L::kOffG);  // [2][64][kGStride]
-  float* ss = reinterpret_cast<float*>(smem + L::kOffS);  // [2][group of the slab][128]
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kOffBar);
-  uint64_t *a_full = bars, *a_empty = bars + 2, *w_full = bars + 4, *w_empty = bars + 6, *done = bars + 8, *drain = bars + 9;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 10);
+  uint64_t *full = bars, *empty = bars + 2, *d_empty = bars + 4, *p_full = bars + 6, *p_empty = bars + 8;  // [buffer]
+  uint64_t* drain = bars + 10;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 11);
   const Q4& w = a.w;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&a_full[i], 256);
-      mbar_init(&a_empty[i], 1);
-      mbar_init(&w_full[i], 128);
-      mbar_init(&w_empty[i], 1);
+      mbar_init(&full[i], 16);
+      mbar_init(&empty[i], 1);
+      mbar_init(&d_empty[i], 16);
+      mbar_init(&p_full[i], 1);
+      mbar_init(&p_empty[i], 16);
     }
-    mbar_init(done, 1);
     mbar_init(drain, 1);
     mbar_fence_init();
   }
-  if (warp == 12) tmem_alloc(tmem_slot, 512);
+  if (warp == 16) tmem_alloc(tmem_slot, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   pdl_wait();
 
-  const int slab = blockIdx.x, variants = 128 >> w.group_log;
-  const int64_t begin = blockIdx.y * a.per, end = min(w.n, begin + a.per), m0 = (int64_t)blockIdx.z * kQ4Chunk;
+  const int slab = blockIdx.x;
+  const int64_t begin = blockIdx.y * a.per, end = min(w.n, begin + a.per), chunk = blockIdx.z, m0 = chunk * kQ4Chunk;
   const int rows = (int)min((int64_t)kQ4Chunk, a.m - m0), blocks = (int)((end - begin + 127) / 128);
-  // tensor memory: sums [128], or [4][64] of which half is used; parts [buffer][group][64]
-  const int a_bufs = variants == 4 ? 1 : 2;
-  const uint32_t kDCol = 0, kACol = variants == 4 ? 256 : 128;
-  const int d_step = variants == 1 ? 0 : 64;  // a group's sums are 128 columns, or the 64 of its box
+  constexpr uint32_t kDCol = 0, kACol = 256;  // tensor memory: sums [2 buffers][128], parts [2 buffers][64]
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < kTopRuns; ++i) top = max(top, a.top[blockIdx.y * kTopRuns + i]);
+  const float one = up_to_scale(top);
 
-  if (warp == 12) {
+  const int64_t all_runs = (w.n + 127) / 128 * 16;
+  if (warp == 17) {
+    if (lane == 0) {  // ------------------------------------------ copies of g's parts
+      const uint8_t* src = a.parts + (chunk * all_runs * 2 * kQ4Chunk + begin / 8 * 2 * rows) * 16;
+      const uint32_t bytes = 16 * 2 * rows * 16;
+      int b = 0;
+      for (; b < blocks; ++b) {
+        const int i = b & 1;
+        if (b >= 2 && !mbar_wait(&p_empty[i], ((b >> 1) - 1) & 1)) break;
+        mbar_expect_tx(&p_full[i], bytes);
+        bulk_load(smem + L::kOffParts + i * L::kParts, src + (int64_t)b * bytes, bytes, &p_full[i]);
+      }
+      // after a wait ran out: the last copies have landed before the CTA leaves
+      if (b < blocks)
+        for (int j = b > 2 ? b - 2 : 0; j < b; ++j) mbar_wait(&p_full[j & 1], (j >> 1) & 1);
+    }
+  } else if (warp == 16) {
     // ------------------------------------------------------------- MMA issuer
     const bool leader = elect_one();
-    const uint32_t idesc = idesc_f16_f32(128, variants == 1 ? 128 : 64, true);
-    const uint64_t bdesc = smem_desc_sw128(smem_u32(smem), L::kCodes / 2, 1024);
+    constexpr uint32_t idesc = idesc_f16_f32(128, 128, true);
+    const uint64_t bdesc = smem_desc_sw128(smem_u32(smem), L::kPart / 2, 1024);
     bool ok = true;
     for (int b = 0; ok && b < blocks; ++b) {
-      const int ab = b % a_bufs, wb = b & 1;
-      if (!mbar_wait_warp(&a_full[ab], (b / a_bufs) & 1)) { ok = false; break; }
-      if (!mbar_wait_warp(&w_full[wb], (b >> 1) & 1)) { ok = false; break; }
+      const int i = b & 1;
+      if (!mbar_wait_warp(&full[i], (b >> 1) & 1)) { ok = false; break; }
+      if (b >= 2 && !mbar_wait_warp(&d_empty[i], ((b >> 1) - 1) & 1)) { ok = false; break; }
       tc_fence_after();
       if (leader) {
-        for (int v = 0; v < variants; ++v) {
-          const int box = variants == 1 ? 0 : variants == 2 ? v : v >> 1;
-          const uint64_t slot = bdesc + (uint64_t)((wb * L::kCodes + box * (L::kCodes / 2)) >> 4);
+#pragma unroll
+        for (int part = 1; part >= 0; --part) {  // the low values first, on small sums
+          const uint64_t slot = bdesc + (uint64_t)((i * L::kBuffer + part * L::kPart) >> 4);
+#pragma unroll
           for (int k = 0; k < 8; ++k)
-            mma_bf16_ts(tmem + kDCol + v * d_step, tmem + kACol + (ab * variants + v) * 64 + k * 8,
-                        slot + (uint64_t)((k * 16 * 128) >> 4), idesc, b != 0 || k != 0);
+            mma_bf16_ts(tmem + kDCol + i * 128, tmem + kACol + i * 64 + k * 8, slot + (uint64_t)((k * 16 * 128) >> 4), idesc,
+                        part == 0 || k != 0);
         }
-        mma_commit(&a_empty[ab]);
-        mma_commit(&w_empty[wb]);
-        if (b == blocks - 1) mma_commit(done);
+        mma_commit(&empty[i]);
       }
       __syncwarp();
     }
@@ -456,200 +573,173 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
       mma_commit(drain);
       mbar_wait(drain, 0);
     }
-  } else if (warp >= 8) {
-    // ------------------------------------------- codes into shared memory, 32 rows of a block to a warp
-    const int g = lane >> 2, t = lane & 3, odd = g & 1;
-    struct Load {
-      uint4 q[4];
-      uint8_t z[4][4];  // zero points of the slab's groups
-    };
-    auto fetch = [&](Load& l, int b) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int64_t row = min(begin + b * 128 + (warp - 8) * 32 + g + 8 * q, w.n - 1);
-        const int64_t at = (row * w.slabs + slab) * 16 + 4 * t;
-        if (ACID_IN_BOUNDS(kSiteQ4, at + 3, w.n * w.slabs * 16)) l.q[q] = *reinterpret_cast<const uint4*>(w.packed + at);
-        if (w.zeros == nullptr) continue;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          if (v >= variants) break;
-          const int64_t z = row * w.groups + min(slab * variants + v, w.groups - 1);
-          if (ACID_IN_BOUNDS(kSiteQ4, z, w.n * w.groups)) l.z[q][v] = w.zeros[z];
-        }
-      }
-    };
-    const int word_log = w.group_log - 5;
-    bool ok = true;
-    Load l;
-    fetch(l, 0);
-    for (int b = 0; ok && b < blocks; ++b) {
-      const int wb = b & 1;
-      if (b >= 2 && !mbar_wait_warp(&w_empty[wb], ((b >> 1) - 1) & 1)) { ok = false; break; }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int row = (warp - 8) * 32 + g + 8 * q;
-        // neighbouring rows take their words in another order, so that their units lie in different banks
-        const uint4 v = odd ? make_uint4(l.q[q].y, l.q[q].x, l.q[q].w, l.q[q].z) : l.q[q];
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          const int i = s ^ odd, unit = (i & 1) * 4 + t;
-          uint32_t h[4];
-          uint32_t z = 8;
-          if (w.zeros != nullptr) {
-            const int of = i >> word_log;
-            z = (of == 0 ? l.z[q][0] : of == 1 ? l.z[q][1] : of == 2 ? l.z[q][2] : l.z[q][3]) & 15u;
-          }
-          halves_of(s == 0 ? v.x : s == 1 ? v.y : s == 2 ? v.z : v.w, z, h);
-          *reinterpret_cast<uint4*>(smem + wb * L::kCodes + (i >> 1) * (L::kCodes / 2) + row * 128 + ((unit ^ (row & 7)) << 4)) =
-              make_uint4(h[0], h[1], h[2], h[3]);
-        }
-      }
-      if (b + 1 < blocks) fetch(l, b + 1);
-      fence_proxy_async_smem();
-      mbar_arrive(&w_full[wb]);
-    }
   } else {
-    // ----------------------------------------------- parts of g s, then the sums: two warps to a quarter of the lanes,
-    // half of the block's rows each
-    const int tid = threadIdx.x & 127, half = warp >> 2, m = (warp & 1) * 32 + lane;
-    const bool low = (warp & 2) != 0, active = (warp & 1) * 32 < rows;
-    // the powers of two
-    float gt = 0.f, st = 0.f;
-    for (int i = 0; i < a.scans; ++i) {
-      st = fmaxf(st, a.top[(int64_t)i * (a.m + 1)]);
-      if (m < rows) gt = fmaxf(gt, a.top[(int64_t)i * (a.m + 1) + 1 + m0 + m]);
-    }
-    const float up = up_to_half(gt);                                                       // |g| to 2^13 .. 2^14
-    const float one = __uint_as_float(max(254 - (int)(__float_as_uint(st) >> 23), 1) << 23);  // scales to 1 .. 2
-    // Row n of the block to thread n, or n + 128: g by its rows (every other one), scales by groups (the same).  Scales
-    // are looked at a block before they are stored.
-    auto copy = [&](int b) {
-      const int64_t n = begin + b * 128 + tid;
-      float* gd = gs + (b & 1) * (L::kG / 4) + tid;
-      if constexpr (sizeof(TG) == 4) {
-        const float* src = static_cast<const float*>(a.g) + m0 * a.ldg + (n < end ? n : begin);
-#pragma unroll 4
-        for (int i = half; i < rows; i += 2) cp_async<4>(gd + i * L::kGStride, src + i * a.ldg, n < end);
-      } else {
-#pragma unroll 8
-        for (int i = half; i < rows; i += 2)
-          gd[i * L::kGStride] = n < end ? io<TG>::ld(static_cast<const TG*>(a.g) + (m0 + i) * a.ldg + n) : 0.f;
+    // ------------------- a warp's eight rows of a block's values into shared memory, a quarter of its lanes' parts into
+    // tensor memory, and a quarter of the columns of their sums out of it
+    const int quarter = warp >> 2, m = (warp & 1) * 32 + lane, g = lane >> 2, t = lane & 3, odd = g & 1;
+    const bool low = (warp & 2) != 0, active = (warp & 1) * 32 < rows, leader = elect_one();
+    const uint32_t quad = (uint32_t)((warp & 3) * 32) << 16;
+    const int variants = 128 >> w.group_log, word_log = w.group_log - 5;
+    uint8_t* mine = smem + L::kOffCodes + warp * kBackRing * 512;
+    // a lane's own 16 bytes of its row, some blocks ahead
+    auto row_of = [&](int b) { return min(begin + b * 128 + warp * 8 + g, w.n - 1); };
+    int fetched = 0, fst = 0;
+    auto copy = [&] {
+      if (fetched < blocks) {
+        const int64_t at = (row_of(fetched) * w.slabs + slab) * 16 + 4 * t;
+        const bool in = ACID_IN_BOUNDS(kSiteQ4, at + 3, w.n * w.slabs * 16);
+        cp_async<16>(mine + fst * 512 + lane * 16, w.packed + (in ? at : 0), in);
+        ++fetched;
       }
       cp_async_commit();
+      fst = fst + 1 == kBackRing ? 0 : fst + 1;
     };
-    float sv[2];
-    auto look = [&](int b) {
-      const int64_t n = begin + b * 128 + tid;
+    for (int i = 0; i < kBackRing - 1; ++i) copy();
+    // its scales and zero points, two blocks ahead
+    struct Look {
+      float s[4];
+      uint8_t z[4];
+    };
+    auto look = [&](Look& l, int b) {
+      if (b >= blocks) return;
+      const int64_t at = row_of(b) * w.groups;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int v = half + 2 * j;
-        sv[j] = 0.f;
-        if (v >= variants || n >= end || b >= blocks) continue;
-        const int64_t at = n * w.groups + min(slab * variants + v, w.groups - 1);
-        if (ACID_IN_BOUNDS(kSiteQ4, at, w.n * w.groups)) sv[j] = io<TS>::ld(static_cast<const TS*>(w.scales) + at);
+      for (int v = 0; v < 4; ++v) {
+        if (v >= variants) break;
+        const int p = min(slab * variants + v, w.groups - 1);
+        if (!ACID_IN_BOUNDS(kSiteQ4, at + p, w.n * w.groups)) continue;
+        l.s[v] = io<TS>::ld(static_cast<const TS*>(w.scales) + at + p);
+        if (w.zeros != nullptr) l.z[v] = w.zeros[at + p];
       }
     };
-    auto store = [&](int b) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-        if (half + 2 * j < variants) ss[((b & 1) * 4 + half + 2 * j) * 128 + tid] = sv[j] * one;
-    };
-    copy(0);
-    look(0);
-    store(0);
-    look(1);
-    const uint32_t quad = (uint32_t)((warp & 3) * 32) << 16;
     bool ok = true;
-    const uint64_t up2 = f2_pack(up, up);
-    for (int b = 0; b < blocks; ++b) {
-      cp_async_wait<0>();
-      // block b is there, and nobody reads the other buffer any more; after a wait ran out the eight warps leave together
-      if (!group_all(1, 256, ok)) {
-        ok = false;
-        break;
-      }
-      if (b + 1 < blocks) {
-        copy(b + 1);
-        store(b + 1);
-        look(b + 2);
-      }
-      const int ab = b % a_bufs;
-      if (b >= a_bufs) ok = mbar_wait_warp(&a_empty[ab], (b / a_bufs - 1) & 1);
-      if (active && ok) {
-        const float* gr = gs + (b & 1) * (L::kG / 4) + m * L::kGStride;
-        for (int v = 0; v < variants; ++v) {
-          const float* sr = ss + ((b & 1) * 4 + v) * 128;
-          const uint32_t to = tmem + quad + kACol + (ab * variants + v) * 64;
+    int st = 0;
+    uint64_t total[16];  // pairs of a quarter of the slab's columns
 #pragma unroll
-          for (int e4 = 0; e4 < 2; ++e4) {
-            const int c = 2 * half + e4;
-            uint32_t d[16];
+    for (int i = 0; i < 16; ++i) total[i] = 0;
+    auto take = [&](int b) {  // the sums of block b
+      ok = mbar_wait_warp(&empty[b & 1], (b >> 1) & 1);
+      if (!ok) return;
+      tc_fence_after();
+      if (active) {
+        uint32_t r[32];
+        tmem_ld32(tmem + quad + kDCol + (b & 1) * 128 + quarter * 32, r);
+        tmem_wait_ld();
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const float4 x = *reinterpret_cast<const float4*>(gr + c * 32 + j * 4);
-              const float4 y = *reinterpret_cast<const float4*>(sr + c * 32 + j * 4);
-              const uint64_t p[2] = {f2_mul(f2_mul(f2_pack(x.x, x.y), up2), f2_pack(y.x, y.y)),
-                                     f2_mul(f2_mul(f2_pack(x.z, x.w), up2), f2_pack(y.z, y.w))};
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                float f0, f1;
-                f2_unpack(p[e], f0, f1);
-                __half2 h = __floats2half2_rn(f0, f1);
-                if (low) {
-                  const float2 f = __half22float2(h);
-                  h = __floats2half2_rn(f0 - f.x, f1 - f.y);
-                }
-                d[2 * j + e] = bits(h);
-              }
-            }
-            tmem_st16(to + c * 16, d);
-          }
-        }
-        tmem_wait_st();
+        for (int i = 0; i < 16; ++i)
+          total[i] = f2_add(total[i], f2_pack(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])));
       }
       tc_fence_before();
-      mbar_arrive(&a_full[ab]);
+      arrive_warp(&d_empty[b & 1], leader);
+    };
+    auto block = [&](Look& l, int b) {
+      const int i = b & 1;
+      if (b >= 2) take(b - 2);  // the tensor cores are done with these buffers
+      if (ok) ok = mbar_wait_warp(&p_full[i], (b >> 1) & 1);
+      if (!ok) return;
+      if (active) {
+        const uint4* p = reinterpret_cast<const uint4*>(smem + L::kOffParts + i * L::kParts) +
+                         quarter * 4 * 2 * rows + (low ? rows : 0) + min(m, rows - 1);
+        uint32_t d[16];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint4 x = p[j * 2 * rows];
+          d[4 * j] = x.x;
+          d[4 * j + 1] = x.y;
+          d[4 * j + 2] = x.z;
+          d[4 * j + 3] = x.w;
+        }
+        tmem_st16(tmem + quad + kACol + i * 64 + quarter * 16, d);
+      }
+      arrive_warp(&p_empty[i], leader);
+      cp_async_wait<kBackRing - 2>();
+      const uint4 q = *reinterpret_cast<const uint4*>(mine + st * 512 + lane * 16);
+      st = st + 1 == kBackRing ? 0 : st + 1;
+      copy();
+      uint32_t sh[4], sl[4], z[4];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        if (v >= variants) break;
+        split_scale(l.s[v] * one, sh[v], sl[v]);
+        z[v] = w.zeros != nullptr ? l.z[v] & 15u : 8u;
+      }
+      look(l, b + 2);
+      // neighbouring rows take their words in another order, so that their units lie in different banks
+      const uint4 v = odd ? make_uint4(q.y, q.x, q.w, q.z) : q;
+      const int row = warp * 8 + g;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const int word = s ^ odd, unit = (word & 1) * 4 + t, of = word >> word_log;
+        const uint32_t h = of == 0 ? sh[0] : of == 1 ? sh[1] : of == 2 ? sh[2] : sh[3];
+        const uint32_t lw = of == 0 ? sl[0] : of == 1 ? sl[1] : of == 2 ? sl[2] : sl[3];
+        const uint32_t zero = of == 0 ? z[0] : of == 1 ? z[1] : of == 2 ? z[2] : z[3];
+        uint32_t hi[4], lo[4];
+        scaled_halves<sizeof(TS) == 4>(s == 0 ? v.x : s == 1 ? v.y : s == 2 ? v.z : v.w, zero, h, lw, hi, lo);
+        uint8_t* to = smem + i * L::kBuffer + (s >> 1) * (L::kPart / 2) + row * 128 + ((unit ^ (row & 7)) << 4);
+        *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4*>(to + L::kPart) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      fence_proxy_async_smem();
+      arrive_warp(&full[i], leader);
+    };
+    Look l[2];
+    look(l[0], 0);
+    look(l[1], 1);
+    for (int b = 0; ok && b < blocks; b += 2) {
+      block(l[0], b);
+      if (ok && b + 1 < blocks) block(l[1], b + 1);
     }
     cp_async_wait<0>();
-    if (ok) ok = mbar_wait_warp(done, 0);
-    tc_fence_after();
-    if (ok && active) {
-      const float down = 1.f / up, per_s = 1.f / one;
-      float* out = a.part + ((blockIdx.y * 2 + low) * a.m + m0 + m) * w.slabs * 128 + slab * 128;
+    if (ok && blocks > 1) take(blocks - 2);
+    if (ok) take(blocks - 1);
+    if (ok && m < rows) {
+      const float down = a.back[blockIdx.y * a.m + m0 + m], per_s = 1.f / one;
+      const int64_t at = ((blockIdx.y * 2 + low) * a.m + m0 + m) * w.slabs * 128 + slab * 128 + quarter * 32;
+      if (ACID_IN_BOUNDS(kSiteQ4, at + 31, a.shares * a.m * w.slabs * 128)) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {  // 32 columns
-        const int c = 2 * half + e, v = variants == 4 ? c : 0;
-        uint32_t r[32];
-        tmem_ld32(tmem + quad + kDCol + (variants == 4 ? v * 64 + (c & 1) * 32 : c * 32), r);
-        tmem_wait_ld();
-        const int64_t at = ((blockIdx.y * 2 + low) * a.m + m0 + m) * w.slabs * 128 + slab * 128 + c * 32;
-        if (m < rows && ACID_IN_BOUNDS(kSiteQ4, at + 31, a.shares * a.m * w.slabs * 128)) {
+        for (int o = 0; o < 4; ++o) {  // an octet's columns j and j + 4 lie side by side
+          float f[8];
 #pragma unroll
-          for (int o = 0; o < 4; ++o) {  // an octet's columns j and j + 4 lie side by side
-            float f[8];
+          for (int j = 0; j < 4; ++j) f2_unpack(total[4 * o + j], f[2 * j], f[2 * j + 1]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(r[8 * o + j]) * down * per_s;
-            *reinterpret_cast<float4*>(out + c * 32 + o * 8) = make_float4(f[0], f[2], f[4], f[6]);
-            *reinterpret_cast<float4*>(out + c * 32 + o * 8 + 4) = make_float4(f[1], f[3], f[5], f[7]);
-          }
+          for (int j = 0; j < 8; ++j) f[j] = f[j] * down * per_s;
+          *reinterpret_cast<float4*>(a.part + at + o * 8) = make_float4(f[0], f[2], f[4], f[6]);
+          *reinterpret_cast<float4*>(a.part + at + o * 8 + 4) = make_float4(f[1], f[3], f[5], f[7]);
         }
-        __syncwarp();
       }
     }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 12) {
+  if (warp == 16) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
+}
+
+// Joins the shares in their order and takes the activation's gradient.
+__global__ void __launch_bounds__(128) q4_backward_join_kernel(Q4Bwd a) {
+  pdl_wait();
+  const int c = blockIdx.x * 128 + threadIdx.x;
+  const int64_t m = blockIdx.y, width = (int64_t)a.w.slabs * 128;
+  if (c >= a.w.k) return;
+  float v = 0.f;
+#pragma unroll 8
+  for (int b = 0; b < a.shares; ++b) v += a.part[(b * a.m + m) * width + c];
+  if (a.silu) {
+    const float x = value_at(a.x_dtype, a.x, m * a.ldx + c), e = 1.f / (1.f + expf(-x));
+    v *= e * (1.f + x * (1.f - e));
+  }
+  put_value(a.x_dtype, a.dx, m * a.lddx + c, v);
 }
 
 // --------------------------------------------------------------------- host
 // Column tiles of eight that the product's kernel is built for.
 int tiles_for(int64_t m) {
   const int nt = (int)((std::min<int64_t>(m, kQ4Chunk) + 7) / 8);
-  return nt <= 3 ? nt : nt <= 5 ? 5 : 8;
+  return nt <= 2 ? nt : nt <= 5 ? 5 : 8;
 }
 int64_t chunks_of(int64_t m) { return (m + kQ4Chunk - 1) / kQ4Chunk; }
 
@@ -670,14 +760,37 @@ acid_status launch_forward(const Q4Fwd& a, int scale_dtype, cudaStream_t s) {
   return scale_dtype == ACID_BF16 ? launch_forward<NT, bf16>(a, s) : launch_forward<NT, float>(a, s);
 }
 
-template <typename TG, typename TS>
+template <typename TS>
 acid_status launch_backward(const Q4Bwd& a, cudaStream_t s) {
   static PerContext allowed;
-  ACID_TRY(allow_smem(allowed, q4_rows_backward_kernel<TG, TS>, BwdSmem::kBytes));
+  ACID_TRY(allow_smem(allowed, q4_rows_backward_kernel<TS>, BackSmem::kBytes));
   const dim3 grid(a.w.slabs, (unsigned)((a.w.n + a.per - 1) / a.per), (unsigned)chunks_of(a.m));
-  launch_pdl(q4_rows_backward_kernel<TG, TS>, grid, kBackThreads, BwdSmem::kBytes, s, a);
+  launch_pdl(q4_rows_backward_kernel<TS>, grid, kBackThreads, BackSmem::kBytes, s, a);
   ACID_CHECK_LAUNCH();
   return ACID_OK;
+}
+
+// Rows of the weight to a CTA of the gradient, in whole blocks of 128, and the
+// CTAs that share a slab's rows: as many CTAs as an SM each has.
+int64_t share_rows(const Q4& w) {
+  const int64_t want = std::max(1, 152 / w.slabs), per = (w.n + want - 1) / want;
+  return (per + 127) / 128 * 128;
+}
+int64_t shares_of(const Q4& w) { return (w.n + share_rows(w) - 1) / share_rows(w); }
+
+// Workspace of the gradient: sums of each share, parts of g, powers of two, largest scales.
+struct BackSpace {
+  size_t parts, back, top, all;
+};
+BackSpace back_space(const Q4& w, int64_t m) {
+  BackSpace b;
+  const size_t shares = (size_t)shares_of(w), runs = (size_t)(w.n + 127) / 128 * 16;
+  b.parts = shares * 2 * m * w.slabs * 128 * sizeof(float);
+  const int64_t last = m - (chunks_of(m) - 1) * kQ4Chunk;  // rows of the last chunk
+  b.back = b.parts + ((size_t)(chunks_of(m) - 1) * kQ4Chunk + last) * runs * 2 * 16;
+  b.top = b.back + shares * m * sizeof(float);
+  b.all = b.top + shares * kTopRuns * sizeof(uint32_t);
+  return b;
 }
 
 }  // namespace
@@ -685,32 +798,43 @@ acid_status launch_backward(const Q4Bwd& a, cudaStream_t s) {
 size_t q4_rows_parts_bytes(const Q4& w, int64_t m) {
   return (size_t)chunks_of(m) * w.slabs * tiles_for(m) * kSlabBytes<1>;
 }
-size_t q4_rows_back_bytes(const Q4&, int64_t m) {
-  return (size_t)m * sizeof(float);
-}
+size_t q4_rows_forward_bytes(const Q4& w, int64_t m) { return q4_rows_parts_bytes(w, m) + (size_t)m * sizeof(float); }
 
-acid_status q4_rows_forward(const Q4Fwd& a, int scale_dtype, cudaStream_t s) {
+acid_status q4_rows_forward(Q4Fwd a, void* workspace, int scale_dtype, cudaStream_t s) {
+  a.parts = static_cast<uint8_t*>(workspace);
+  a.back = reinterpret_cast<float*>(a.parts + q4_rows_parts_bytes(a.w, a.m));
   switch (tiles_for(a.m)) {
     case 1: return launch_forward<1>(a, scale_dtype, s);
     case 2: return launch_forward<2>(a, scale_dtype, s);
-    case 3: return launch_forward<3>(a, scale_dtype, s);
     case 5: return launch_forward<5>(a, scale_dtype, s);
     default: return launch_forward<8>(a, scale_dtype, s);
   }
 }
 
-// As many CTAs as an SM each has, in whole blocks of 128 rows.
-int64_t q4_rows_share(const Q4& w) {
-  const int64_t want = std::max(1, 152 / w.slabs), per = (w.n + want - 1) / want;
-  return (per + 127) / 128 * 128;
-}
+size_t q4_backward_bytes(const Q4& w, int64_t m) { return back_space(w, m).all; }
 
-acid_status q4_rows_backward(const Q4Bwd& a, cudaStream_t s) {
-  launch_pdl(q4_scan_kernel, dim3(a.scans, (unsigned)chunks_of(a.m)), kThreads, 0, s, a);
+acid_status q4_backward(Q4Bwd a, void* workspace, cudaStream_t s) {
+  if (a.dx == nullptr) {
+    launch_pdl(q4_bias_kernel, (unsigned)std::min<int64_t>((a.w.n + kThreads - 1) / kThreads, 1 << 16), kThreads, 0, s, a);
+    ACID_CHECK_LAUNCH();
+    return ACID_OK;
+  }
+  const BackSpace b = back_space(a.w, a.m);
+  uint8_t* base = static_cast<uint8_t*>(workspace);
+  a.part = static_cast<float*>(workspace);
+  a.parts = base + b.parts;
+  a.back = reinterpret_cast<float*>(base + b.back);
+  a.top = reinterpret_cast<uint32_t*>(base + b.top);
+  a.per = share_rows(a.w);
+  const int64_t shares = shares_of(a.w);
+  a.shares = (int)shares * 2;
+  const int64_t bias_ctas = a.dbias != nullptr ? std::min<int64_t>((a.per + kThreads - 1) / kThreads, 1024) : 0;
+  launch_pdl(q4_back_parts_kernel, dim3((unsigned)shares, (unsigned)(a.m + kTopRuns + bias_ctas)), kThreads, 0, s, a);
   ACID_CHECK_LAUNCH();
-  if (a.g_dtype == ACID_BF16)
-    return a.scale_dtype == ACID_BF16 ? launch_backward<bf16, bf16>(a, s) : launch_backward<bf16, float>(a, s);
-  return a.scale_dtype == ACID_BF16 ? launch_backward<float, bf16>(a, s) : launch_backward<float, float>(a, s);
+  ACID_TRY(a.scale_dtype == ACID_BF16 ? launch_backward<bf16>(a, s) : launch_backward<float>(a, s));
+  launch_pdl(q4_backward_join_kernel, dim3((a.w.k + 127) / 128, (unsigned)a.m), 128, 0, s, a);
+  ACID_CHECK_LAUNCH();
+  return ACID_OK;
 }
 
 }  // namespace acid
