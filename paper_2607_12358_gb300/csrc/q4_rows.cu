@@ -2,6 +2,7 @@
 // or steps): the product and its input gradient on tcgen05.
 #include <algorithm>
 #include <string>
+#include <type_traits>
 
 #include "q4.cuh"
 
@@ -52,20 +53,28 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                : "memory");
 }
 
-// A word's eight columns as two halves each, s (q - z) in s = sh + sl: the product
-// with sh rounded to a half, and what is left of it (exact: sh (q - z) has 15 bits
-// at most) with sl's part: 22 bits together.
-template <bool LOW>  // whether sl is there (scales of more than a half's 11 bits)
-__device__ __forceinline__ void scaled_halves(uint32_t word, uint32_t z, uint32_t sh, uint32_t sl, uint32_t* hi, uint32_t* lo) {
+// How a value s (q - z) enters the gradient's product, by what its bits need.
+enum Values {
+  kOneHalf,     // bf16 scale, z = 8: 8 bits times 3 (q - 8 is -8 .. 7): exact in a half
+  kTwoHalves,   // bf16 scale, any z: 12 bits: a half and what is left of it
+  kThreeTerms   // fp32 scale, itself two halves sh + sl
+};
+// A word's eight columns: the product with sh rounded to a half, and what is left of
+// it (exact: sh (q - z) has 15 bits at most) with sl's part: 22 bits together.
+template <Values KIND>
+__device__ __forceinline__ void scaled_halves(uint32_t word, uint32_t z1, uint32_t z64, uint32_t sh, uint32_t sl,
+                                              uint32_t (&hi)[4], uint32_t (&lo)[4]) {
   uint32_t d[4];
-  halves_of(word, z, d);
+  halves_of(word, z1, z64, d);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const __half2 c = half2_of(d[j]), h = __hmul2(c, half2_of(sh));
-    __half2 l = __hfma2(c, half2_of(sh), __hneg2(h));
-    if constexpr (LOW) l = __hfma2(c, half2_of(sl), l);
     hi[j] = bits(h);
-    lo[j] = bits(l);
+    if constexpr (KIND != kOneHalf) {
+      __half2 l = __hfma2(c, half2_of(sh), __hneg2(h));
+      if constexpr (KIND == kThreeTerms) l = __hfma2(c, half2_of(sl), l);
+      lo[j] = bits(l);
+    }
   }
 }
 // sh and sl of a scale after its power of two, each in both halves.
@@ -82,16 +91,16 @@ __device__ __forceinline__ float up_to_scale(uint32_t top) {
 __device__ __forceinline__ uint32_t finite_bits(float v) { return isfinite(v) ? __float_as_uint(fabsf(v)) : 0u; }
 
 // ------------------------------------------------------------------ product
-// D[128 rows of the weight, 16 NT] = values x parts^T, the values as two halves in
-// tensor memory (a row to a lane, where the lane's thread writes them, after a power
-// of two of the row), the parts of a(x) in shared memory (8 NT rows of high parts,
-// then of low parts).  The tensor cores' sums lose up to 2^-23 of themselves at each
-// addition, always towards zero, so that they are read back after each slab (12
-// additions on a sum of its size) and added up in fp32 by the rows' threads: over 65536
-// columns left in tensor memory a sum was 1.7e-4 off.  A CTA has two tiles of 128
-// rows; each of their lanes belongs to two threads, which share its words and its
-// sums: with one, two warps a scheduler left half of the issue slots empty (36864 x
-// 3072, 34 rows: 42 us).
+// D[128 rows of the weight, 16 NT] = codes x parts^T for each group of columns, the
+// codes as the exact halves q - z in tensor memory (a row to a lane, where the lane's
+// threads write them), the parts of a(x) in shared memory (8 NT rows of high parts,
+// then of low parts).  The same threads read the group's sums back and add them in
+// fp32 to the row's totals, times its scale.  (The scale as part of the operand, a
+// value in two halves, would spare that only where sums may stay in tensor memory: the
+// tensor cores' sums lose up to 2^-23 of themselves at each addition, always towards
+// zero, 1.7e-4 over 65536 columns.  It costs more instructions and twice the MMAs.)
+//   A CTA has two tiles of 128 rows; each of their lanes belongs to two threads,
+// which share its words and its sums.  Issue slots bound it: 36864 x 3072, 34 rows.
 constexpr int kFwdRing = 4;   // slabs of parts in shared memory
 constexpr int kCodeRing = 4;  // slabs of a warp's share of 32 rows of codes
 // Bytes of a slab's parts: two boxes of 64 columns, rows of 128 bytes whose
@@ -129,20 +138,23 @@ __global__ void __launch_bounds__(kThreads) q4_parts_kernel(Q4Fwd a) {
   }
 }
 
-template <int NT, typename TS>
-__global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd a) {
+template <int NT, int LOG>
+__global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd a, int scale_dtype) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* ring = smem;
   uint8_t* codes = ring + kFwdRing * kSlabBytes<NT>;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(codes + 16 * kCodeRing * 1024);
-  uint64_t *b_full = bars, *b_empty = bars + kFwdRing;                                      // [ring]
-  uint64_t *a_full = b_empty + kFwdRing, *a_empty = a_full + 4;                             // [tile][2]
-  uint64_t *d_full = a_empty + 4, *d_empty = d_full + 2, *drain = d_empty + 2;              // [tile]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   constexpr int kCols = 16 * NT, kHalf = 8 * NT;
-  // tensor memory: values [tile][2 buffers][high, low][32] of 64 columns, sums [tile][<= 128]
-  constexpr uint32_t kACol = 0, kDCol = 256;
+  // A step is 64 columns or a group of 32; a group's sums are there after kSteps of them.
+  constexpr int kWords = LOG == 5 ? 1 : 2, kPerSlab = 4 / kWords, kSteps = LOG == 7 ? 2 : 1, kGroups = 128 >> LOG;
+  // tensor memory: codes [tile][2 buffers][32], sums [tile][buffers]
+  constexpr int kSums = NT <= 5 ? 2 : 1, kDStride = NT <= 5 ? 96 : 128;
+  constexpr uint32_t kACol = 0, kDCol = 128;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(codes + 16 * kCodeRing * 1024);
+  uint64_t *b_full = bars, *b_empty = bars + kFwdRing;                          // [ring]
+  uint64_t *a_full = b_empty + kFwdRing, *a_empty = a_full + 4;                 // [tile][2]
+  uint64_t *d_full = a_empty + 4, *d_empty = d_full + 4, *drain = d_empty + 4;  // [tile][2]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   const Q4& w = a.w;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -153,8 +165,6 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
     for (int i = 0; i < 4; ++i) {
       mbar_init(&a_full[i], 8);
       mbar_init(&a_empty[i], 1);
-    }
-    for (int i = 0; i < 2; ++i) {
       mbar_init(&d_full[i], 1);
       mbar_init(&d_empty[i], 8);
     }
@@ -193,49 +203,50 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
     constexpr uint32_t idesc = idesc_f16_f32(128, kCols, false);
     const uint64_t bdesc = smem_desc_sw128(smem_u32(ring), 16, 1024);
     bool ok = true;
-    constexpr uint32_t idesc_low = idesc_f16_f32(128, (kHalf + 15) / 16 * 16, false);  // low values: high parts are enough
-    uint32_t u = 0;  // steps of 64 columns
-    int v = 0;       // slabs
+    uint32_t u = 0, e = 0;  // steps, groups
+    int v = 0;              // slabs
     for (int64_t set = blockIdx.x; ok && set < sets; set += gridDim.x)
       for (int slab = 0; ok && slab < w.slabs; ++slab, ++v) {
         const int st = v % kFwdRing;
         if (!mbar_wait_warp(&b_full[st], (v / kFwdRing) & 1)) { ok = false; break; }
-        for (int h = 0; ok && h < 2; ++h, ++u)
+        for (int h = 0; ok && h < kPerSlab; ++h, ++u) {
+          const bool first = kSteps == 1 || h == 0, last = kSteps == 1 || h == 1;
+          const int db = e % kSums;
           for (int tile = 0; tile < 2; ++tile) {
             if (!mbar_wait_warp(&a_full[tile * 2 + (u & 1)], (u >> 1) & 1)) { ok = false; break; }
-            if (h == 0 && v > 0 && !mbar_wait_warp(&d_empty[tile], (v - 1) & 1)) { ok = false; break; }
+            if (first && e >= kSums && !mbar_wait_warp(&d_empty[tile * 2 + db], (e / kSums - 1) & 1)) { ok = false; break; }
             tc_fence_after();
             if (leader) {
-              const uint32_t d = tmem + kDCol + tile * 128, c = tmem + kACol + tile * 128 + (u & 1) * 64;
-              const uint64_t slot = bdesc + (uint64_t)((st * kSlabBytes<NT> + h * (kCols * 128)) >> 4);
-              if (h == 0)  // clears all columns; the low values come first, on small sums
-                mma_bf16_ts(d, c + 32, slot, idesc, false);
-              else
-                mma_bf16_ts(d, c + 32, slot, idesc_low, true);
+              const uint32_t d = tmem + kDCol + (tile * kSums + db) * kDStride, c = tmem + kACol + tile * 64 + (u & 1) * 32;
+              const uint64_t slot = bdesc + (uint64_t)((st * kSlabBytes<NT>) >> 4);
 #pragma unroll
-              for (int k = 1; k < 4; ++k) mma_bf16_ts(d, c + 32 + k * 8, slot + (uint64_t)((k * 32) >> 4), idesc_low, true);
-#pragma unroll
-              for (int k = 0; k < 4; ++k) mma_bf16_ts(d, c + k * 8, slot + (uint64_t)((k * 32) >> 4), idesc, true);
-              if (h == 1 && tile == 1) mma_commit(&b_empty[st]);
+              for (int k = 0; k < 2 * kWords; ++k) {
+                const int kk = h * 2 * kWords + k;  // 16 columns of the slab
+                mma_bf16_ts(d, c + k * 8, slot + (uint64_t)(((kk >> 2) * (kCols * 128) + (kk & 3) * 32) >> 4), idesc,
+                            !first || k != 0);
+              }
+              if (h == kPerSlab - 1 && tile == 1) mma_commit(&b_empty[st]);
               mma_commit(&a_empty[tile * 2 + (u & 1)]);
-              if (h == 1) mma_commit(&d_full[tile]);
+              if (last) mma_commit(&d_full[tile * 2 + db]);
             }
             __syncwarp();
           }
+          if (last) ++e;
+        }
       }
     if (!ok && leader) {
       mma_commit(drain);
       mbar_wait(drain, 0);
     }
   } else {
-    // ------------------- values into tensor memory, sums out of it: warps 0-7 tile 0, 8-15 tile 1; in a tile two warps
+    // ------------------- codes into tensor memory, sums out of it: warps 0-7 tile 0, 8-15 tile 1; in a tile two warps
     // to a quarter of the lanes, which share the words and the columns of the sums
     const int tile = warp >> 3, half = (warp >> 2) & 1;
     const bool leader = elect_one();
     const uint32_t quad = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t c_addr = tmem + quad + kACol + tile * 128 + half * 8, d_addr = tmem + quad + kDCol + tile * 128;
+    const uint32_t c_addr = tmem + quad + kACol + tile * 64 + half * 8;
+    const uint32_t d_addr = tmem + quad + kDCol + tile * kSums * kDStride;
     uint8_t* mine = codes + warp * kCodeRing * 1024;
-    const int per_slab = 128 >> w.group_log, word_log = w.group_log - 5;
     const int row_in_set = tile * 128 + (warp & 3) * 32;
     // A lane copies 16 bytes of two of the warp's 32 rows (32 bytes of a row together) and reads its own row back; the
     // units of every other four rows are exchanged, so that eight rows' reads lie in different banks.
@@ -266,44 +277,48 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
         }
       }
       cp_async_commit();
-      fst = fst + 1 == kCodeRing ? 0 : fst + 1;
+      fst = (fst + 1) % kCodeRing;
     };
     for (int i = 0; i < kCodeRing - 1; ++i) copy();
     bool ok = true;
-    uint32_t u = 0, taken = 0;  // steps of 64 columns; slabs whose sums were read back
+    uint32_t u = 0, taken = 0;  // steps; groups whose sums were read back
     int st = 0;
     constexpr int kMine = (NT + 1) / 2;  // column tiles of a thread's sums: the first ones, or the rest
     const int n_first = half * kMine;
     uint64_t total[kMine][4];  // pairs of the row's sums
-    auto take = [&]() -> bool {
-      if (!mbar_wait_warp(&d_full[tile], taken & 1)) return false;
+    // Adds the oldest group's sums, whose scale is s.
+    auto take = [&](float s) {
+      const int db = taken % kSums;
+      ok = mbar_wait_warp(&d_full[tile * 2 + db], (taken / kSums) & 1);
       ++taken;
+      if (!ok) return;
       tc_fence_after();
       constexpr int kBatch = kMine < 3 ? kMine : kMine == 3 ? 3 : 2;
+      const uint64_t s2 = f2_pack(s, s);
 #pragma unroll
       for (int n0 = 0; n0 < kMine; n0 += kBatch) {
         uint32_t hi[kBatch][8], lo[kBatch][8];
 #pragma unroll
         for (int n = 0; n < kBatch; ++n) {  // (an odd tile count: the last one is read twice)
-          const int c = min(n_first + n0 + n, NT - 1) * 8;
+          const int c = db * kDStride + min(n_first + n0 + n, NT - 1) * 8;
           tmem_ld8(d_addr + c, hi[n]);
           tmem_ld8(d_addr + kHalf + c, lo[n]);
         }
         tmem_wait_ld();
         if (n0 + kBatch == kMine) {
           tc_fence_before();
-          arrive_warp(&d_empty[tile], leader);
+          arrive_warp(&d_empty[tile * 2 + db], leader);
         }
 #pragma unroll
         for (int n = 0; n < kBatch; ++n)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             total[n0 + n][e] =
-                f2_add(total[n0 + n][e],
+                f2_fma(s2,
                        f2_add(f2_pack(__uint_as_float(hi[n][2 * e]), __uint_as_float(hi[n][2 * e + 1])),
-                              f2_pack(__uint_as_float(lo[n][2 * e]), __uint_as_float(lo[n][2 * e + 1]))));
+                              f2_pack(__uint_as_float(lo[n][2 * e]), __uint_as_float(lo[n][2 * e + 1]))),
+                       total[n0 + n][e]);
       }
-      return true;
     };
     for (int64_t set = blockIdx.x; ok && set < sets; set += gridDim.x) {
 #pragma unroll
@@ -311,27 +326,20 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
 #pragma unroll
         for (int e = 0; e < 4; ++e) total[n][e] = 0;
       const int64_t row = set * 256 + row_in_set + lane, at = min(row, w.n - 1) * w.groups;
-      const TS* scale = static_cast<const TS*>(w.scales) + at;
       // scales and zero points of a slab's groups, a slab ahead
-      float scales[4];
-      uint8_t zeros[4];
+      float scales[kGroups];
+      uint8_t zeros[kGroups];
       auto look = [&](int slab) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (i >= per_slab) break;
-          const int p = min(slab * per_slab + i, w.groups - 1);
-          if (!ACID_IN_BOUNDS(kSiteQ4, at + p, w.n * w.groups)) continue;
-          scales[i] = io<TS>::ld(scale + p);
-          if (w.zeros != nullptr) zeros[i] = w.zeros[at + p];
+        for (int i = 0; i < kGroups; ++i) {
+          const int64_t p = at + min(slab * kGroups + i, w.groups - 1);
+          if (!ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.groups)) continue;
+          scales[i] = value_at(scale_dtype, w.scales, p);
+          if (w.zeros != nullptr) zeros[i] = w.zeros[p];
         }
       };
       look(0);
-      // the row's power of two
-      uint32_t top = 0;
-#pragma unroll 8
-      for (int i = 0; i < w.groups; ++i)
-        if (ACID_IN_BOUNDS(kSiteQ4, at + i, w.n * w.groups)) top = max(top, finite_bits(io<TS>::ld(scale + i)));
-      const float one = up_to_scale(top);
+      float scale = 0.f;  // of the group whose sums are not taken yet
       for (int slab = 0; ok && slab < w.slabs; ++slab) {
         cp_async_wait<kCodeRing - 2>();
         __syncwarp();
@@ -339,45 +347,48 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
 #pragma unroll
         for (int c = 0; c < 2; ++c) q[c] = *reinterpret_cast<const uint4*>(mine + st * 1024 + place(lane, c));
         copy();
-        st = st + 1 == kCodeRing ? 0 : st + 1;
-        uint32_t sh[4], sl[4], z[4];
+        st = (st + 1) % kCodeRing;
+        float s[kGroups];
+        uint32_t z1[kGroups], z64[kGroups];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (i >= per_slab) break;
-          split_scale(scales[i] * one, sh[i], sl[i]);
-          z[i] = w.zeros != nullptr ? zeros[i] & 15u : 8u;
+        for (int i = 0; i < kGroups; ++i) {
+          const uint32_t z = (w.zeros != nullptr ? zeros[i] & 15u : 8u) * 0x00010001u;
+          s[i] = scales[i];
+          z1[i] = 0x64006400u | z;
+          z64[i] = 0x54005400u | z << 4;
         }
         if (slab + 1 < w.slabs) look(slab + 1);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if ((i & 1) == 0) {  // a step of 64 columns: its buffer is free
-            if (u >= 2 && ok) ok = mbar_wait_warp(&a_empty[tile * 2 + (u & 1)], ((u >> 1) - 1) & 1);
-          }
-          const int of = i >> word_log;
-          const uint32_t h = of == 0 ? sh[0] : of == 1 ? sh[1] : of == 2 ? sh[2] : sh[3];
-          const uint32_t l = of == 0 ? sl[0] : of == 1 ? sl[1] : of == 2 ? sl[2] : sl[3];
-          const uint32_t zero = of == 0 ? z[0] : of == 1 ? z[1] : of == 2 ? z[2] : z[3];
-          uint32_t hi[8], lo[8];
+        for (int h = 0; h < kPerSlab; ++h) {
+          if (u >= 2 && ok) ok = mbar_wait_warp(&a_empty[tile * 2 + (u & 1)], ((u >> 1) - 1) & 1);
+          const int of = (h * kWords) >> (LOG - 5);
 #pragma unroll
-          for (int c = 0; c < 2; ++c)
-            scaled_halves<sizeof(TS) == 4>(i == 0 ? q[c].x : i == 1 ? q[c].y : i == 2 ? q[c].z : q[c].w, zero, h, l,
-                                           hi + 4 * c, lo + 4 * c);
-          if (ok) {
-            tmem_st8(c_addr + (u & 1) * 64 + (i & 1) * 16, hi);
-            tmem_st8(c_addr + (u & 1) * 64 + 32 + (i & 1) * 16, lo);
+          for (int word = 0; word < kWords; ++word) {
+            const int i = h * kWords + word;
+            uint32_t d[8];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              uint32_t x[4];
+              halves_of(i == 0 ? q[c].x : i == 1 ? q[c].y : i == 2 ? q[c].z : q[c].w, z1[of], z64[of], x);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) d[4 * c + j] = x[j];
+            }
+            if (ok) tmem_st8(c_addr + (u & 1) * 32 + word * 16, d);
           }
-          if ((i & 1) == 0) continue;
           tmem_wait_st();
           tc_fence_before();
           arrive_warp(&a_full[tile * 2 + (u & 1)], leader);
           ++u;
-          // the sums of the slab before, while this one's are formed
-          if (i == 1 && slab > 0 && ok) ok = take();
+          // the sums of the group before, while this one's are formed
+          if (h % kSteps == 0) {
+            if (ok && (h > 0 || slab > 0)) take(scale);
+            scale = s[of];
+          }
         }
       }
-      if (ok) ok = take();
+      if (ok) take(scale);
       if (!ok || row >= w.n) continue;
-      const float bias = a.bias != nullptr ? a.bias[row] : 0.f, down = 1.f / one;
+      const float bias = a.bias != nullptr ? a.bias[row] : 0.f;
 #pragma unroll
       for (int n = 0; n < kMine; ++n)
 #pragma unroll
@@ -386,8 +397,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
           if (n_first + n >= NT) continue;
           float x, y;
           f2_unpack(total[n][e], x, y);
-          if (m < a.m) put_value(a.out_dtype, a.out, m * a.ldo + row, fmaf(x * down, a.back[m], bias));
-          if (m + 1 < a.m) put_value(a.out_dtype, a.out, (m + 1) * a.ldo + row, fmaf(y * down, a.back[m + 1], bias));
+          if (m < a.m) put_value(a.out_dtype, a.out, m * a.ldo + row, fmaf(x, a.back[m], bias));
+          if (m + 1 < a.m) put_value(a.out_dtype, a.out, (m + 1) * a.ldo + row, fmaf(y, a.back[m + 1], bias));
         }
     }
     cp_async_wait<0>();
@@ -491,8 +502,10 @@ __global__ void __launch_bounds__(kThreads) q4_back_parts_kernel(Q4Bwd a) {
   }
 }
 
-template <typename TS>
+template <Values KIND, int LOG>
 __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd a) {
+  using TS = std::conditional_t<KIND == kThreeTerms, float, bf16>;
+  constexpr int kGroups = 128 >> LOG;
   extern __shared__ uint8_t smem_raw[];
   using L = BackSmem;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -558,12 +571,12 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
       tc_fence_after();
       if (leader) {
 #pragma unroll
-        for (int part = 1; part >= 0; --part) {  // the low values first, on small sums
+        for (int part = KIND == kOneHalf ? 0 : 1; part >= 0; --part) {  // the low values first, on small sums
           const uint64_t slot = bdesc + (uint64_t)((i * L::kBuffer + part * L::kPart) >> 4);
 #pragma unroll
           for (int k = 0; k < 8; ++k)
             mma_bf16_ts(tmem + kDCol + i * 128, tmem + kACol + i * 64 + k * 8, slot + (uint64_t)((k * 16 * 128) >> 4), idesc,
-                        part == 0 || k != 0);
+                        (part == 0 && KIND != kOneHalf) || k != 0);
         }
         mma_commit(&empty[i]);
       }
@@ -579,7 +592,6 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
     const int quarter = warp >> 2, m = (warp & 1) * 32 + lane, g = lane >> 2, t = lane & 3, odd = g & 1;
     const bool low = (warp & 2) != 0, active = (warp & 1) * 32 < rows, leader = elect_one();
     const uint32_t quad = (uint32_t)((warp & 3) * 32) << 16;
-    const int variants = 128 >> w.group_log, word_log = w.group_log - 5;
     uint8_t* mine = smem + L::kOffCodes + warp * kBackRing * 512;
     // a lane's own 16 bytes of its row, some blocks ahead
     auto row_of = [&](int b) { return min(begin + b * 128 + warp * 8 + g, w.n - 1); };
@@ -597,19 +609,18 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
     for (int i = 0; i < kBackRing - 1; ++i) copy();
     // its scales and zero points, two blocks ahead
     struct Look {
-      float s[4];
-      uint8_t z[4];
+      float s[kGroups];
+      uint8_t z[kGroups];
     };
     auto look = [&](Look& l, int b) {
       if (b >= blocks) return;
       const int64_t at = row_of(b) * w.groups;
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        if (v >= variants) break;
-        const int p = min(slab * variants + v, w.groups - 1);
-        if (!ACID_IN_BOUNDS(kSiteQ4, at + p, w.n * w.groups)) continue;
-        l.s[v] = io<TS>::ld(static_cast<const TS*>(w.scales) + at + p);
-        if (w.zeros != nullptr) l.z[v] = w.zeros[at + p];
+      for (int v = 0; v < kGroups; ++v) {
+        const int64_t p = at + min(slab * kGroups + v, w.groups - 1);
+        if (!ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.groups)) continue;
+        l.s[v] = io<TS>::ld(static_cast<const TS*>(w.scales) + p);
+        if (KIND != kOneHalf && w.zeros != nullptr) l.z[v] = w.zeros[p];
       }
     };
     bool ok = true;
@@ -622,12 +633,13 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
       if (!ok) return;
       tc_fence_after();
       if (active) {
-        uint32_t r[32];
-        tmem_ld32(tmem + quad + kDCol + (b & 1) * 128 + quarter * 32, r);
+        uint32_t r[4][8];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld8(tmem + quad + kDCol + (b & 1) * 128 + quarter * 32 + c * 8, r[c]);
         tmem_wait_ld();
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          total[i] = f2_add(total[i], f2_pack(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])));
+          total[i] = f2_add(total[i], f2_pack(__uint_as_float(r[i >> 2][2 * (i & 3)]), __uint_as_float(r[i >> 2][2 * (i & 3) + 1])));
       }
       tc_fence_before();
       arrive_warp(&d_empty[b & 1], leader);
@@ -656,28 +668,32 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
       const uint4 q = *reinterpret_cast<const uint4*>(mine + st * 512 + lane * 16);
       st = st + 1 == kBackRing ? 0 : st + 1;
       copy();
-      uint32_t sh[4], sl[4], z[4];
+      uint32_t sh[kGroups], sl[kGroups], z1[kGroups], z64[kGroups];
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        if (v >= variants) break;
+      for (int v = 0; v < kGroups; ++v) {
         split_scale(l.s[v] * one, sh[v], sl[v]);
-        z[v] = w.zeros != nullptr ? l.z[v] & 15u : 8u;
+        const uint32_t z = (KIND != kOneHalf && w.zeros != nullptr ? l.z[v] & 15u : 8u) * 0x00010001u;
+        z1[v] = 0x64006400u | z;
+        z64[v] = 0x54005400u | z << 4;
       }
       look(l, b + 2);
       // neighbouring rows take their words in another order, so that their units lie in different banks
       const uint4 v = odd ? make_uint4(q.y, q.x, q.w, q.z) : q;
       const int row = warp * 8 + g;
+      uint8_t* to = smem + i * L::kBuffer;
+      const int at = row * 128 + (((odd * 4 + t) ^ (row & 7)) << 4);  // unit of word 0 or 1
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        const int word = s ^ odd, unit = (word & 1) * 4 + t, of = word >> word_log;
-        const uint32_t h = of == 0 ? sh[0] : of == 1 ? sh[1] : of == 2 ? sh[2] : sh[3];
-        const uint32_t lw = of == 0 ? sl[0] : of == 1 ? sl[1] : of == 2 ? sl[2] : sl[3];
-        const uint32_t zero = of == 0 ? z[0] : of == 1 ? z[1] : of == 2 ? z[2] : z[3];
+        // word s ^ odd: its group, and the unit beside the first one's for the second of a box
+        const int even_of = s >> (LOG - 5), odd_of = (s ^ 1) >> (LOG - 5);
+        const bool other = odd != 0 && even_of != odd_of;
         uint32_t hi[4], lo[4];
-        scaled_halves<sizeof(TS) == 4>(s == 0 ? v.x : s == 1 ? v.y : s == 2 ? v.z : v.w, zero, h, lw, hi, lo);
-        uint8_t* to = smem + i * L::kBuffer + (s >> 1) * (L::kPart / 2) + row * 128 + ((unit ^ (row & 7)) << 4);
-        *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        *reinterpret_cast<uint4*>(to + L::kPart) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        scaled_halves<KIND>(s == 0 ? v.x : s == 1 ? v.y : s == 2 ? v.z : v.w, other ? z1[odd_of] : z1[even_of],
+                            other ? z64[odd_of] : z64[even_of], other ? sh[odd_of] : sh[even_of],
+                            other ? sl[odd_of] : sl[even_of], hi, lo);
+        uint8_t* p = to + (at ^ ((s & 1) * 64)) + (s >> 1) * (L::kPart / 2);
+        *reinterpret_cast<uint4*>(p) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        if constexpr (KIND != kOneHalf) *reinterpret_cast<uint4*>(p + L::kPart) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
       }
       tmem_wait_st();
       tc_fence_before();
@@ -743,13 +759,13 @@ int tiles_for(int64_t m) {
 }
 int64_t chunks_of(int64_t m) { return (m + kQ4Chunk - 1) / kQ4Chunk; }
 
-template <int NT, typename TS>
-acid_status launch_forward(const Q4Fwd& a, cudaStream_t s) {
+template <int NT, int LOG>
+acid_status launch_forward(const Q4Fwd& a, int scale_dtype, cudaStream_t s) {
   static PerContext allowed;
-  ACID_TRY(allow_smem(allowed, q4_rows_forward_kernel<NT, TS>, kFwdSmem<NT>));
+  ACID_TRY(allow_smem(allowed, q4_rows_forward_kernel<NT, LOG>, kFwdSmem<NT>));
   const int64_t sets = (a.w.n + 255) / 256;
   const dim3 grid((unsigned)std::min<int64_t>(sets, num_sms()), (unsigned)chunks_of(a.m));
-  launch_pdl(q4_rows_forward_kernel<NT, TS>, grid, kRowsThreads, kFwdSmem<NT>, s, a);
+  launch_pdl(q4_rows_forward_kernel<NT, LOG>, grid, kRowsThreads, kFwdSmem<NT>, s, a, scale_dtype);
   ACID_CHECK_LAUNCH();
   return ACID_OK;
 }
@@ -757,17 +773,25 @@ template <int NT>
 acid_status launch_forward(const Q4Fwd& a, int scale_dtype, cudaStream_t s) {
   launch_pdl(q4_parts_kernel<NT>, (unsigned)a.m, kThreads, 0, s, a);
   ACID_CHECK_LAUNCH();
-  return scale_dtype == ACID_BF16 ? launch_forward<NT, bf16>(a, s) : launch_forward<NT, float>(a, s);
+  return a.w.group_log == 5   ? launch_forward<NT, 5>(a, scale_dtype, s)
+         : a.w.group_log == 6 ? launch_forward<NT, 6>(a, scale_dtype, s)
+                              : launch_forward<NT, 7>(a, scale_dtype, s);
 }
 
-template <typename TS>
+template <Values KIND, int LOG>
 acid_status launch_backward(const Q4Bwd& a, cudaStream_t s) {
   static PerContext allowed;
-  ACID_TRY(allow_smem(allowed, q4_rows_backward_kernel<TS>, BackSmem::kBytes));
+  ACID_TRY(allow_smem(allowed, q4_rows_backward_kernel<KIND, LOG>, BackSmem::kBytes));
   const dim3 grid(a.w.slabs, (unsigned)((a.w.n + a.per - 1) / a.per), (unsigned)chunks_of(a.m));
-  launch_pdl(q4_rows_backward_kernel<TS>, grid, kBackThreads, BackSmem::kBytes, s, a);
+  launch_pdl(q4_rows_backward_kernel<KIND, LOG>, grid, kBackThreads, BackSmem::kBytes, s, a);
   ACID_CHECK_LAUNCH();
   return ACID_OK;
+}
+template <Values KIND>
+acid_status launch_backward(const Q4Bwd& a, cudaStream_t s) {
+  return a.w.group_log == 5   ? launch_backward<KIND, 5>(a, s)
+         : a.w.group_log == 6 ? launch_backward<KIND, 6>(a, s)
+                              : launch_backward<KIND, 7>(a, s);
 }
 
 // Rows of the weight to a CTA of the gradient, in whole blocks of 128, and the
@@ -831,7 +855,9 @@ acid_status q4_backward(Q4Bwd a, void* workspace, cudaStream_t s) {
   const int64_t bias_ctas = a.dbias != nullptr ? std::min<int64_t>((a.per + kThreads - 1) / kThreads, 1024) : 0;
   launch_pdl(q4_back_parts_kernel, dim3((unsigned)shares, (unsigned)(a.m + kTopRuns + bias_ctas)), kThreads, 0, s, a);
   ACID_CHECK_LAUNCH();
-  ACID_TRY(a.scale_dtype == ACID_BF16 ? launch_backward<bf16>(a, s) : launch_backward<float>(a, s));
+  ACID_TRY(a.scale_dtype != ACID_BF16     ? launch_backward<kThreeTerms>(a, s)
+           : a.w.zeros != nullptr ? launch_backward<kTwoHalves>(a, s)
+                                  : launch_backward<kOneHalf>(a, s));
   launch_pdl(q4_backward_join_kernel, dim3((a.w.k + 127) / 128, (unsigned)a.m), 128, 0, s, a);
   ACID_CHECK_LAUNCH();
   return ACID_OK;
