@@ -264,28 +264,13 @@ __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
 }
 
 // ---------------------------------------------------------------- quantiser
-// A lane takes eight columns of a row (one word), a warp 32 such octets of one
-// row at a time: two slabs, whose groups are 4, 8 or 16 lanes.
-constexpr int kUnits = 4;  // octet runs of a warp, all loaded before the first is worked on
-struct Runs {
-  int64_t n;    // runs: n rows of per_row
-  int per_row;
-};
-__host__ __device__ inline Runs runs_of(int64_t rows, int k) {
-  const int per_row = (k + 255) / 256;
-  return {rows * per_row, per_row};
-}
-
 // the larger of two values; a NaN wins
 __device__ __forceinline__ float max_or_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
-// Codes of eight values in 0 .. 15, rint(v / s) + z.  The quotient comes from a
-// product with inv = 1 / s, off by less than 2^-22 of it, and is rounded to even by
-// the sum with 1.5 2^23; a word with a value within 1e-4 of the middle of two codes (or
-// where inv is no use) is formed by divisions.
+// Codes of eight values in 0 .. 15, rint(v / s) + z, by divisions.
 __device__ __noinline__ uint32_t divided_codes(float4 lo, float4 hi, float s, int z) {
   const float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
   uint32_t word = 0;
@@ -294,86 +279,107 @@ __device__ __noinline__ uint32_t divided_codes(float4 lo, float4 hi, float s, in
     word |= (uint32_t)fminf(fmaxf(rintf(v[j] / s) + (float)z, 0.f), 15.f) << (4 * j);
   return word;
 }
+// The same with one division a group: the quotient comes from a product with
+// inv = 1 / s, off by less than 2^-22 of it, and is rounded to even by the sum with 1.5 2^23,
+// whose last bits are then the code's; the eight are gathered by one addition each,
+// the constant bits above them taken out at the end.  A word with a value within
+// 1e-4 of the middle of two codes (or where inv is no use) is formed by divisions.
+//   Quotients lie in -7.03 .. 7.03 without zero points (s may be rounded down by 2^-8):
+// no code is clamped; with them the largest may come out as 16.
+template <bool ZEROS>
 __device__ __forceinline__ uint32_t codes_of(const float (&v)[8], float s, float inv, int z) {
   constexpr float kRound = 12582912.f;
+  const uint64_t inv2 = f2_pack(inv, inv), up = f2_pack(kRound, kRound), down = f2_pack(-kRound, -kRound);
+  const uint64_t minus = f2_pack(-1.f, -1.f);
+  const float most = kRound + (float)(15 - z);
   uint32_t word = 0;
-  bool sure = true;
+  float off = 0.f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float q = v[j] * inv, r = q + kRound;
-    sure = sure && fabsf(q - (r - kRound)) < 0.4999f;
-    word |= (uint32_t)min(max((int)(__float_as_uint(r) - __float_as_uint(kRound)) + z, 0), 15) << (4 * j);
+  for (int j = 6; j >= 0; j -= 2) {
+    const uint64_t q = f2_mul(f2_pack(v[j], v[j + 1]), inv2), r = f2_add(q, up);
+    float a, b, x, y;
+    f2_unpack(f2_fma(f2_add(r, down), minus, q), a, b);
+    off = max_or_nan(off, max_or_nan(fabsf(a), fabsf(b)));
+    f2_unpack(r, x, y);
+    if (ZEROS) {
+      x = fminf(x, most);
+      y = fminf(y, most);
+    }
+    word = word * 16u + __float_as_uint(y);
+    word = word * 16u + __float_as_uint(x);
   }
-  if (sure) return word;
+  if (off < 0.4999f) return word - (0x4B400000u - (uint32_t)z) * 0x11111111u;
   return divided_codes(make_float4(v[0], v[1], v[2], v[3]), make_float4(v[4], v[5], v[6], v[7]), s, z);
 }
 
-template <typename TW, typename TS>
+// 8 values of the weight, zeros past its columns.
+template <typename TW>
+__device__ __forceinline__ void weight8(const TW* p, int cols, bool wide, float (&v)[8]) {
+  if (wide && cols >= 8) {
+    load8(p, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < cols ? io<TW>::ld(p + j) : 0.f;
+  }
+}
+// A thread takes 32 columns of a row (four words); a group is one, two or four
+// threads.  HBM would bound it (36864 x 3072 bf16: 42 us); what a thread does once,
+// two divisions and the places of its columns, weighed most with eight columns each
+// (183 us).
+template <typename TW, typename TS, bool ZEROS>
 __global__ void __launch_bounds__(kThreads) q4_quantize_kernel(const TW* W, int64_t ldw, Q4 w, uint32_t* packed,
                                                                TS* scales, uint8_t* zeros, bool wide) {
   pdl_wait();
-  const int lane = threadIdx.x & 31;
-  const Runs runs = runs_of(w.n, w.k);
-  const int64_t first = ((int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * kUnits;
-  const bool asym = zeros != nullptr;
-  const int span = 1 << (w.group_log - 3);  // lanes of a group
-  float v[kUnits][8];
-  int64_t row = first / runs.per_row;
-  int at = (int)(first - row * runs.per_row);
-  const int64_t row0 = row;
-  const int at0 = at;
+  const int per_row = w.slabs * 4;
+  const int64_t unit = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t row = unit / per_row;
+  const int block = (int)(unit - row * per_row), col = block * 32;
+  const bool in = row < w.n && ACID_IN_BOUNDS(kSiteQ4, row, w.n);
+  const TW* src = W + (in ? row * ldw + col : 0);
+  float v[4][8], hi = 0.f, lo = 0.f;  // max(w, 0) and -min(w, 0), or max |w|
 #pragma unroll
-  for (int u = 0; u < kUnits; ++u) {
-    const int col = (at * 32 + lane) * 8;
-    const bool in = first + u < runs.n;
-    if (in && wide && col + 8 <= w.k && ACID_IN_BOUNDS(kSiteQ4, row, w.n)) {
-      load8(W + row * ldw + col, v[u]);
-    } else {
+  for (int t = 0; t < 4; ++t) weight8(src + 8 * t, in ? w.k - col - 8 * t : 0, wide, v[t]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[u][j] = in && col + j < w.k ? io<TW>::ld(W + row * ldw + col + j) : 0.f;
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      hi = max_or_nan(hi, ZEROS ? v[t][j] : fabsf(v[t][j]));
+      if (ZEROS) lo = max_or_nan(lo, -v[t][j]);
     }
-    if (++at == runs.per_row) {
-      at = 0;
-      ++row;
+  for (int o = 1; o < 1 << (w.group_log - 5); o <<= 1) {
+    hi = max_or_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    if (ZEROS) lo = max_or_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+  }
+  TS st;
+  io<TS>::st(&st, ZEROS ? (hi + lo) / 15.f : hi / 7.f);
+  const float s = io<TS>::ld(&st), div = s == 0.f ? 1.f : s, inv = 1.f / div;
+  const int z = ZEROS ? (int)fminf(fmaxf(rintf(lo / div), 0.f), 15.f) : 8;
+  if (!in) return;
+  // word 4 t + i of the slab holds the octet t of its 32 columns i
+  uint32_t* out = packed + row * w.slabs * 16 + (block >> 2) * 16 + (block & 3);
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+    if (ACID_IN_BOUNDS(kSiteQ4, out + 4 * t - packed, w.n * w.slabs * 16)) out[4 * t] = codes_of<ZEROS>(v[t], div, inv, z);
+  if ((block & ((1 << (w.group_log - 5)) - 1)) == 0 && col < w.k) {
+    const int64_t p = row * w.groups + (col >> w.group_log);
+    if (ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.groups)) {
+      scales[p] = st;
+      if (ZEROS) zeros[p] = (uint8_t)z;
     }
   }
-  row = row0;
-  at = at0;
-#pragma unroll
-  for (int u = 0; u < kUnits; ++u) {
-    if (first + u >= runs.n) break;
-    const int octet = at * 32 + lane, col = octet * 8;
-    float hi = 0.f, lo = 0.f;  // max(w, 0) and -min(w, 0), or max |w|
-#pragma unroll
-    for (int j = 0; j < 8; ++j) hi = max_or_nan(hi, asym ? v[u][j] : fabsf(v[u][j]));
-    if (asym)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) lo = max_or_nan(lo, -v[u][j]);
-    for (int o = span >> 1; o > 0; o >>= 1) {
-      hi = max_or_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-      if (asym) lo = max_or_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    }
-    TS st;
-    io<TS>::st(&st, asym ? (hi + lo) / 15.f : hi / 7.f);
-    const float s = io<TS>::ld(&st), div = s == 0.f ? 1.f : s, inv = 1.f / div;
-    const int z = asym ? (int)fminf(fmaxf(rintf(lo / div), 0.f), 15.f) : 8;
-    const uint32_t q = codes_of(v[u], div, inv, z);
-    if (octet < w.slabs * 16) {
-      const int64_t p = row * w.slabs * 16 + column_word(octet);
-      if (ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.slabs * 16)) packed[p] = q;
-    }
-    if ((lane & (span - 1)) == 0 && col < w.k) {
-      const int64_t p = row * w.groups + (col >> w.group_log);
-      if (ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.groups)) {
-        scales[p] = st;
-        if (asym) zeros[p] = (uint8_t)z;
-      }
-    }
-    if (++at == runs.per_row) {
-      at = 0;
-      ++row;
-    }
-  }
+}
+
+// ------------------------------------------------------------------- values
+// A lane takes eight columns of a row (one word), a warp 32 such octets of one
+// row at a time.  HBM bounds it: 36864 x 3072 to fp32 in 76 us.
+constexpr int kUnits = 4;  // octet runs of a warp, all loaded before the first is worked on
+struct Runs {
+  int64_t n;    // runs: n rows of per_row
+  int per_row;
+};
+__host__ __device__ inline Runs runs_of(int64_t rows, int k) {
+  const int per_row = (k + 255) / 256;
+  return {rows * per_row, per_row};
 }
 
 // 32 bytes with one store where the address allows it: a lane's own sector.
@@ -534,15 +540,15 @@ extern "C" acid_status acid_q4_quantize(int32_t w_dtype, const void* W, int64_t 
   cudaStream_t s = (cudaStream_t)stream;
   const Q4 w = q4_args(*weight);
   const bool wide = aligned(W, 16) && ldw % 8 == 0;
-  const int64_t per_cta = kThreads / 32 * kUnits;
-  const unsigned grid = (unsigned)((runs_of(w.n, w.k).n + per_cta - 1) / per_cta);
+  const unsigned grid = (unsigned)((w.n * w.slabs * 4 + kThreads - 1) / kThreads);
   auto packed = static_cast<uint32_t*>(const_cast<void*>(weight->packed));
   auto scales = const_cast<void*>(weight->scales);
   auto zeros = const_cast<uint8_t*>(weight->zeros);
   auto launch = [&](auto* src, auto* sc) {
-    launch_pdl(q4_quantize_kernel<std::remove_const_t<std::remove_pointer_t<decltype(src)>>,
-                                  std::remove_pointer_t<decltype(sc)>>,
-               grid, kThreads, 0, s, src, ldw, w, packed, sc, zeros, wide);
+    using TW = std::remove_const_t<std::remove_pointer_t<decltype(src)>>;
+    using TS = std::remove_pointer_t<decltype(sc)>;
+    launch_pdl(zeros != nullptr ? q4_quantize_kernel<TW, TS, true> : q4_quantize_kernel<TW, TS, false>, grid, kThreads, 0,
+               s, src, ldw, w, packed, sc, zeros, wide);
   };
   auto by_scale = [&](auto* src) {
     if (weight->scale_dtype == ACID_BF16)
