@@ -15,7 +15,7 @@ ACID_BOUNDS_READER(take_bounds_site)
 namespace {
 
 using bf16 = __nv_bfloat16;
-constexpr int kMaxWidth = 4096;           // 8 warps of 16 columns a lane
+constexpr int kMaxWidth = 4096;  // 8 warps of 16 columns a lane
 constexpr int kMaxWarps = kMaxWidth / 512;
 
 // What both directions read, as the kernels see it.
@@ -60,13 +60,22 @@ struct SiteBwd {
   int64_t per;   // rows of a CTA
 };
 
-// A thread's 16 columns: two octets, 8 (tid + j blockDim) ..., as eight fp32
-// pairs, so that one instruction does the arithmetic of two columns.  Octets
-// past the row's end hold zeros all through.
+// A thread's columns: 8 V of them in runs of E, E (tid + j blockDim) ..., as fp32
+// pairs, so that one instruction does the arithmetic of two columns.  E is such
+// that a warp's loads and stores of a run are contiguous: 8 where both types are
+// bf16, else 4 (with fp32 in runs of 8 each access takes half of its 32-byte sectors:
+// 32760 x 1536 fp32 stream 114 us, its gradient 226).  Runs past the row's end hold
+// zeros all through.
+//   V is 2; 1 for rows of at most 256 columns, which are one warp's then (26 Mi elements
+// of 256 columns, bf16: 68 us, 82 with half of the warp's lanes; their gradient 132,
+// 178).
+template <int V>
 struct Cols {
-  uint64_t v[8];
+  uint64_t v[4 * V];
 };
-#define FOR_PAIRS _Pragma("unroll") for (int i = 0; i < 8; ++i)
+template <int V>
+constexpr int kMostThreads = V == 1 ? 32 : kMaxWidth / 16;
+#define FOR_PAIRS _Pragma("unroll") for (int i = 0; i < 4 * V; ++i)
 __device__ __forceinline__ uint64_t f2_same(float x) { return f2_pack(x, x); }
 __device__ __forceinline__ float f2_total(uint64_t x) {
   float a, b;
@@ -74,58 +83,72 @@ __device__ __forceinline__ float f2_total(uint64_t x) {
   return a + b;
 }
 // Sum of the pairs.
-__device__ __forceinline__ float total(const uint64_t (&p)[8]) {
-  return f2_total(f2_add(f2_add(f2_add(p[0], p[1]), f2_add(p[2], p[3])), f2_add(f2_add(p[4], p[5]), f2_add(p[6], p[7]))));
+template <int V>
+__device__ __forceinline__ float total(const Cols<V>& a) {
+  uint64_t s[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s[i] = V == 2 ? f2_add(a.v[i], a.v[4 * V - 4 + i]) : a.v[i];
+  return f2_total(f2_add(f2_add(s[0], s[1]), f2_add(s[2], s[3])));
 }
-__device__ __forceinline__ float total(const Cols& a) { return total(a.v); }
 // Sum of the products.
-__device__ __forceinline__ float dot(const Cols& a, const Cols& b) {
+template <int V>
+__device__ __forceinline__ float dot(const Cols<V>& a, const Cols<V>& b) {
   uint64_t s = f2_mul(a.v[0], b.v[0]), t = f2_mul(a.v[1], b.v[1]);
 #pragma unroll
-  for (int i = 2; i < 8; i += 2) {
+  for (int i = 2; i < 4 * V; i += 2) {
     s = f2_fma(a.v[i], b.v[i], s);
     t = f2_fma(a.v[i + 1], b.v[i + 1], t);
   }
   return f2_total(f2_add(s, t));
 }
 
+template <int V, int E>
 struct Place {
-  int c[2], d;  // first column of each octet
-  bool on[2];
+  static constexpr int kRuns = 8 * V / E;
+  int c[kRuns], d;  // first column of each run
+  bool on[kRuns];
 };
-__device__ __forceinline__ Place place(int d) {
-  const int c0 = threadIdx.x * 8, c1 = c0 + blockDim.x * 8;
-  return {{c0, c1}, d, {c0 < d, c1 < d}};
-}
-__device__ __forceinline__ void fill(Cols& a, int j, float x) {
+template <int V, int E>
+__device__ __forceinline__ Place<V, E> place(int d) {
+  Place<V, E> at;
+  at.d = d;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) a.v[4 * j + i] = f2_same(x);
+  for (int j = 0; j < at.kRuns; ++j) {
+    at.c[j] = (threadIdx.x + j * blockDim.x) * E;
+    at.on[j] = at.c[j] < d;
+  }
+  return at;
 }
 // Columns of a vector; `none` in all of the row's where there is none.
-__device__ __forceinline__ Cols vec(const float* p, const Place& at, float none) {
-  Cols a;
+template <int V, int E>
+__device__ __forceinline__ Cols<V> vec(const float* p, const Place<V, E>& at, float none) {
+  Cols<V> a;
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    if (!at.on[j] || p == nullptr) {
-      fill(a, j, at.on[j] ? none : 0.f);
-    } else if (ACID_IN_BOUNDS(kSiteNormSite, at.c[j] + 7, at.d)) {
-      const float4 lo = *reinterpret_cast<const float4*>(p + at.c[j]);
-      const float4 hi = *reinterpret_cast<const float4*>(p + at.c[j] + 4);
-      a.v[4 * j] = f2_pack(lo.x, lo.y);
-      a.v[4 * j + 1] = f2_pack(lo.z, lo.w);
-      a.v[4 * j + 2] = f2_pack(hi.x, hi.y);
-      a.v[4 * j + 3] = f2_pack(hi.z, hi.w);
+  for (int j = 0; j < at.kRuns; ++j) {
+    uint64_t* v = a.v + j * (E / 2);
+    const float fill = at.on[j] ? none : 0.f;
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) v[i] = f2_same(fill);
+    if (!at.on[j] || p == nullptr || !ACID_IN_BOUNDS(kSiteNormSite, at.c[j] + E - 1, at.d)) continue;
+#pragma unroll
+    for (int i = 0; i < E / 4; ++i) {
+      const float4 x = *reinterpret_cast<const float4*>(p + at.c[j] + 4 * i);
+      v[2 * i] = f2_pack(x.x, x.y);
+      v[2 * i + 1] = f2_pack(x.z, x.w);
     }
   }
   return a;
 }
-__device__ __forceinline__ void times(Cols& a, const Cols& b) { FOR_PAIRS a.v[i] = f2_mul(a.v[i], b.v[i]); }
-__device__ __forceinline__ void plus(Cols& a, float x, const Place& at) {
-  FOR_PAIRS a.v[i] = f2_add(a.v[i], f2_same(at.on[i >> 2] ? x : 0.f));
+template <int V>
+__device__ __forceinline__ void times(Cols<V>& a, const Cols<V>& b) { FOR_PAIRS a.v[i] = f2_mul(a.v[i], b.v[i]); }
+template <int V, int E>
+__device__ __forceinline__ void plus(Cols<V>& a, float x, const Place<V, E>& at) {
+  FOR_PAIRS a.v[i] = f2_add(a.v[i], f2_same(at.on[i / (E / 2)] ? x : 0.f));
 }
 // branch_scale times the gate's columns of a group.
-__device__ __forceinline__ Cols gate_cols(const Site& s, int64_t m, const Place& at) {
-  Cols g = vec(s.gate ? s.gate + m : nullptr, at, 1.f);
+template <int V, int E>
+__device__ __forceinline__ Cols<V> gate_cols(const Site& s, int64_t m, const Place<V, E>& at) {
+  Cols<V> g = vec(s.gate ? s.gate + m : nullptr, at, 1.f);
   FOR_PAIRS {
     if (s.tanh && s.gate) {
       float lo, hi;
@@ -137,25 +160,31 @@ __device__ __forceinline__ Cols gate_cols(const Site& s, int64_t m, const Place&
   return g;
 }
 // 1 + scale of a group.
-__device__ __forceinline__ Cols scale_cols(const Site& s, int64_t m, const Place& at) {
-  Cols a = vec(s.scale ? s.scale + m : nullptr, at, 0.f);
+template <int V, int E>
+__device__ __forceinline__ Cols<V> scale_cols(const Site& s, int64_t m, const Place<V, E>& at) {
+  Cols<V> a = vec(s.scale ? s.scale + m : nullptr, at, 0.f);
   plus(a, 1.f, at);
   return a;
 }
 
-template <typename T>
-__device__ __forceinline__ void store_pairs(T* p, const uint64_t* v) {
-  float f[8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) f2_unpack(v[i], f[2 * i], f[2 * i + 1]);
-  store8(p, f);
-}
 // To a row of the operand, whose first element is `row`.
-template <typename T>
-__device__ __forceinline__ void put(T* row, const Place& at, const Cols& a, int64_t r, int64_t rows) {
+template <typename T, int V, int E>
+__device__ __forceinline__ void put(T* row, const Place<V, E>& at, const Cols<V>& a, int64_t r, int64_t rows) {
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
-    if (at.on[j] && ACID_IN_BOUNDS(kSiteNormSite, r, rows)) store_pairs(row + at.c[j], a.v + 4 * j);
+  for (int j = 0; j < at.kRuns; ++j) {
+    float f[E];
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) f2_unpack(a.v[j * (E / 2) + i], f[2 * i], f[2 * i + 1]);
+    if (!at.on[j] || !ACID_IN_BOUNDS(kSiteNormSite, r, rows)) continue;
+    T* p = row + at.c[j];
+    if constexpr (E == 8) {
+      store8(p, f);
+    } else if constexpr (sizeof(T) == 4) {
+      *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    } else {
+      *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
+    }
+  }
 }
 
 // Sums of N values over the CTA; every thread gets them.  The first shuffles
@@ -207,91 +236,124 @@ __device__ __forceinline__ Reducer reducer(float4 (*red)[kMaxWarps]) {
 
 // A thread's own ring of row pieces in shared memory: it copies the columns
 // that it will work on and nobody else reads them, so that waiting for its own
-// copies is all the synchronisation there is.  A stage is planes of 16 bytes a
-// thread.
-template <typename T>
-constexpr int kPlanes = sizeof(T);  // of 16 columns
-template <typename T>
-__device__ __forceinline__ void stage(uint8_t* mine, int plane, const T* row, const Place& at, int64_t r, int64_t rows) {
-  constexpr int kOctet = kPlanes<T> / 2;
+// copies is all the synchronisation there is.  A stage is a plane for each run of
+// each operand: a warp's copies go to consecutive addresses (with a thread's pieces
+// side by side they took longer: 32760 x 1536 128 us, not 112).  Pieces of runs past the
+// row's end are zeros from the start.
+template <typename T, int V>
+constexpr int kBytes = 8 * V * sizeof(T);  // of a thread's columns
+template <typename T, int V, int E>
+__device__ __forceinline__ void stage(uint8_t* plane, const T* row, const Place<V, E>& at, int64_t r, int64_t rows) {
+  constexpr int kRun = E * sizeof(T);
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
-    if (at.on[j] && ACID_IN_BOUNDS(kSiteNormSite, r, rows))
-#pragma unroll
-      for (int i = 0; i < kOctet; ++i)
-        cp_async<16>(mine + (plane + j * kOctet + i) * blockDim.x * 16,
-                     reinterpret_cast<const uint8_t*>(row + at.c[j]) + 16 * i, true);
-}
-template <typename T>
-__device__ __forceinline__ Cols unstage(const uint8_t* mine, int plane, const Place& at) {
-  constexpr int kOctet = kPlanes<T> / 2;
-  Cols a;
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    if (!at.on[j]) {
-      fill(a, j, 0.f);
-      continue;
+  for (int j = 0; j < at.kRuns; ++j)
+    if (at.on[j] && ACID_IN_BOUNDS(kSiteNormSite, r, rows)) {
+      const uint32_t to = smem_u32(plane + (threadIdx.x + j * blockDim.x) * kRun);
+      if constexpr (kRun == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row + at.c[j]) : "memory");
+      else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(row + at.c[j]) : "memory");
     }
-    const uint8_t* q = mine + (plane + j * kOctet) * blockDim.x * 16;
-    uint64_t* v = a.v + 4 * j;
-    if constexpr (sizeof(T) == 2) {
+}
+template <typename T, int V, int E>
+__device__ __forceinline__ Cols<V> unstage(const uint8_t* plane) {
+  constexpr int kRun = E * sizeof(T), kRuns = 8 * V / E;
+  Cols<V> a;
+#pragma unroll
+  for (int j = 0; j < kRuns; ++j) {
+    const uint8_t* q = plane + (threadIdx.x + j * blockDim.x) * kRun;
+    uint64_t* v = a.v + j * (E / 2);
+    if constexpr (sizeof(T) == 4) {
+      const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(q);
+      v[0] = x.x;
+      v[1] = x.y;
+    } else if constexpr (E == 8) {
       const uint4 u = *reinterpret_cast<const uint4*>(q);
       v[0] = f2_pack(bf16_lo(u.x), bf16_hi(u.x));
       v[1] = f2_pack(bf16_lo(u.y), bf16_hi(u.y));
       v[2] = f2_pack(bf16_lo(u.z), bf16_hi(u.z));
       v[3] = f2_pack(bf16_lo(u.w), bf16_hi(u.w));
     } else {
-      const ulonglong2 lo = *reinterpret_cast<const ulonglong2*>(q);
-      const ulonglong2 hi = *reinterpret_cast<const ulonglong2*>(q + blockDim.x * 16);
-      v[0] = lo.x;
-      v[1] = lo.y;
-      v[2] = hi.x;
-      v[3] = hi.y;
+      const uint2 u = *reinterpret_cast<const uint2*>(q);
+      v[0] = f2_pack(bf16_lo(u.x), bf16_hi(u.x));
+      v[1] = f2_pack(bf16_lo(u.y), bf16_hi(u.y));
     }
   }
   return a;
 }
+// Zeros in the thread's pieces of an operand.
+template <typename T, int V, int E>
+__device__ __forceinline__ void clear_plane(uint8_t* plane) {
+  constexpr int kRun = E * sizeof(T);
+#pragma unroll
+  for (int j = 0; j < 8 * V / E; ++j) {
+    uint8_t* q = plane + (threadIdx.x + j * blockDim.x) * kRun;
+    *reinterpret_cast<uint2*>(q) = make_uint2(0, 0);
+    if constexpr (kRun == 16) *reinterpret_cast<uint2*>(q + 8) = make_uint2(0, 0);
+  }
+}
+template <typename TS, typename TB>
+constexpr int kRunOf = sizeof(TS) + sizeof(TB) == 4 ? 8 : 4;
 
-// A CTA takes a row at a time; row k of CTA b is b start + k step, k < count.
+// r = res x + branch gate (N_post(y) post_w), u = N_pre(r) pre_w (1 + scale) + shift.
+// A CTA takes a row at a time; row k of CTA b is b start + k step, k < count: rows that
+// lie apart where there is one group (the CTAs then work on one stretch of memory),
+// adjoining ones where a CTA would change its group's vectors at each row otherwise.
+// Each operand passes once, so the bytes bound it; a few rows in flight a CTA and two or
+// more CTAs an SM keep the memory busy through the two or three sums of a row.  fp32
+// stream, bf16 branch, RMS and layer norm: 32760 x 1536 105 us (85% of a copy's rate),
+// 67576 x 3072 with a group of 3276 rows a frame 252 us (97%); one row 3.5 us, which is a
+// launch and three sums' latency.
 constexpr int kFwdStages = 4;
-template <typename TS, typename TB, bool BRANCH>
-__global__ void __launch_bounds__(32 * kMaxWarps, 2) site_forward_kernel(SiteFwd a, int64_t start, int64_t step,
-                                                                        uint32_t count) {
+template <typename TS, typename TB, bool BRANCH, int V>
+__global__ void __launch_bounds__(kMostThreads<V>, V == 1 ? 16 : 2) site_forward_kernel(SiteFwd a, int64_t start, int64_t step, uint32_t count) {
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float4 red[2][kMaxWarps];
-  pdl_wait();
+  constexpr int E = kRunOf<TS, TB>, kX = kBytes<TS, V>, kStage = kX + (BRANCH ? kBytes<TB, V> : 0);
   const Site& s = a.s;
-  const Place at = place(s.d);
+  const Place<V, E> at = place<V, E>(s.d);
+  uint8_t* mine = ring;
+  const int unit = blockDim.x, stage_bytes = kStage * unit;
+  if (!at.on[at.kRuns - 1])
+    for (int k = 0; k < kFwdStages; ++k) {
+      clear_plane<TS, V, E>(ring + k * stage_bytes);
+      if constexpr (BRANCH) clear_plane<TB, V, E>(ring + k * stage_bytes + kX * unit);
+    }
   Reducer sums = reducer(red);
+  pdl_wait();
   const float d = (float)s.d, per_d = 1.f / d;
   int64_t row = blockIdx.x * start;
   const uint32_t n = row < s.rows ? (uint32_t)min((int64_t)count, (s.rows - 1 - row) / step + 1) : 0;
-  constexpr int kStage = kPlanes<TS> + (BRANCH ? kPlanes<TB> : 0);
-  uint8_t* mine = ring + threadIdx.x * 16;
-  const int stride = kStage * blockDim.x * 16;
   int64_t ahead = row;  // the next row to be copied
+  const TS* xp = static_cast<const TS*>(a.x) + row * a.ldx;
+  const TB* yp = static_cast<const TB*>(a.y) + (BRANCH ? row * a.ldy : 0);
   uint32_t copied = 0;
-  int to = 0;
+  uint8_t* to = mine;
   auto issue = [&] {
     if (copied < n) {
-      stage(mine + to * stride, 0, static_cast<const TS*>(a.x) + ahead * a.ldx, at, ahead, s.rows);
-      if constexpr (BRANCH)
-        stage(mine + to * stride, kPlanes<TS>, static_cast<const TB*>(a.y) + ahead * a.ldy, at, ahead, s.rows);
+      stage<TS, V, E>(to, xp, at, ahead, s.rows);
+      xp += step * a.ldx;
+      if constexpr (BRANCH) {
+        stage<TB, V, E>(to + kX * unit, yp, at, ahead, s.rows);
+        yp += step * a.ldy;
+      }
       ahead += step;
       ++copied;
     }
-    to = to + 1 == kFwdStages ? 0 : to + 1;
+    to = to == mine + (kFwdStages - 1) * stage_bytes ? mine : to + stage_bytes;
     cp_async_commit();
   };
   for (int k = 0; k < kFwdStages - 1; ++k) issue();
   const bool wants_mean = s.pre == ACID_NORM_LAYER && a.u != nullptr;
-  int st = 0;
+  const uint8_t* from = mine;
+  TS* rp = static_cast<TS*>(a.r) + (a.r != nullptr ? row * a.ldr : 0);
+  TB* up = static_cast<TB*>(a.u) + (a.u != nullptr ? row * a.ldu : 0);
   for (uint32_t k = 0; k < n;) {
     // the rows of one group
     const int64_t g = group_of(s, row), m = g * s.ld_mod;
     const uint32_t stop = (uint32_t)min((int64_t)n, k + (group_end(s, g) - 1 - row) / step + 1);
-    Cols gw, sc = scale_cols(s, m, at);  // gate and post_w, (1 + scale) and pre_w, shift
-    const Cols sh = vec(s.shift ? s.shift + m : nullptr, at, 0.f);
+    Cols<V> gw, sc = scale_cols(s, m, at);  // gate and post_w, (1 + scale) and pre_w, shift
+    const Cols<V> sh = vec(s.shift ? s.shift + m : nullptr, at, 0.f);
     times(sc, vec(s.pre_w, at, 1.f));
     if constexpr (BRANCH) {
       gw = gate_cols(s, m, at);
@@ -299,12 +361,12 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) site_forward_kernel(SiteFwd
     }
     for (; k < stop; ++k, row += step) {
       cp_async_wait<kFwdStages - 2>();
-      Cols r = unstage<TS>(mine + st * stride, 0, at);
-      FOR_PAIRS r.v[i] = f2_mul(r.v[i], f2_same(s.res));
+      Cols<V> r = unstage<TS, V, E>(from);
       float mean = 0.f;
       if constexpr (BRANCH) {
-        Cols y = unstage<TB>(mine + st * stride, kPlanes<TS>, at);
+        Cols<V> y = unstage<TB, V, E>(from + kX * unit);
         issue();
+        FOR_PAIRS r.v[i] = f2_mul(r.v[i], f2_same(s.res));
         if (s.post == ACID_NORM_LAYER) plus(y, -(sums.sum<1>(total(y)).x / d), at);
         // the sum of r comes with the branch's sum of squares, from those of x and of g w y
         const float sq = dot(y, y);
@@ -318,10 +380,14 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) site_forward_kernel(SiteFwd
         FOR_PAIRS r.v[i] = f2_fma(f2_same(inv), y.v[i], r.v[i]);
       } else {
         issue();
+        FOR_PAIRS r.v[i] = f2_mul(r.v[i], f2_same(s.res));
         if (wants_mean) mean = sums.sum<1>(total(r)).x / d;
       }
-      st = st + 1 == kFwdStages ? 0 : st + 1;
-      if (a.r != nullptr) put(static_cast<TS*>(a.r) + row * a.ldr, at, r, row, s.rows);
+      from = from == mine + (kFwdStages - 1) * stage_bytes ? mine : from + stage_bytes;
+      if (a.r != nullptr) {
+        put(rp, at, r, row, s.rows);
+        rp += step * a.ldr;
+      }
       if (a.u == nullptr) continue;
       if (s.pre != ACID_NORM_NONE) {
         if (s.pre == ACID_NORM_LAYER) plus(r, -mean, at);
@@ -329,7 +395,8 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) site_forward_kernel(SiteFwd
         FOR_PAIRS r.v[i] = f2_mul(r.v[i], f2_same(inv));
       }
       FOR_PAIRS r.v[i] = f2_fma(r.v[i], sc.v[i], sh.v[i]);
-      put(static_cast<TB*>(a.u) + row * a.ldu, at, r, row, s.rows);
+      put(up, at, r, row, s.rows);
+      up += step * a.ldu;
     }
   }
 }
@@ -348,14 +415,15 @@ __device__ __forceinline__ void put_sum(const SiteBwd& a, int which, int64_t g, 
   out[g * a.ld_dmod + c] = v;
 }
 // The same for a thread's columns.
-__device__ __forceinline__ void put_sums(const SiteBwd& a, int which, int64_t g, int64_t m, const Place& at, Cols v) {
+template <int V, int E>
+__device__ __forceinline__ void put_sums(const SiteBwd& a, int which, int64_t g, int64_t m, const Place<V, E>& at, Cols<V> v) {
   const Site& s = a.s;
   float* out = which == 0 ? a.dshift : which == 1 ? a.dscale : a.dgate;
   if (out == nullptr) return;
   if (which == 1) times(v, vec(s.pre_w, at, 1.f));
   if (which == 2) {
     times(v, vec(s.post_w, at, 1.f));
-    const Cols t = vec(s.tanh && s.gate ? s.gate + m : nullptr, at, 0.f);
+    const Cols<V> t = vec(s.tanh && s.gate ? s.gate + m : nullptr, at, 0.f);
     FOR_PAIRS {
       float lo, hi;
       f2_unpack(t.v[i], lo, hi);
@@ -371,66 +439,84 @@ __device__ __forceinline__ void put_sums(const SiteBwd& a, int which, int64_t g,
 // over the rows of its group in registers.  A group that lies in the CTA's rows
 // is finished here; of one that reaches over their edge the sums go to the
 // CTA's slot 2 b (the group began earlier) or 2 b + 1 (it begins here), and
-// site_join_kernel adds the slots.
-// (two stages where four fp32 rows of 4096 columns have to fit)
-template <typename TS, typename TB>
-constexpr int kBwdStages = sizeof(TS) + sizeof(TB) == 8 ? 2 : 3;
-template <typename TS, typename TB>
-__global__ void __launch_bounds__(384, 1) site_backward_kernel(SiteBwd a) {
-  constexpr int kStages = kBwdStages<TS, TB>;
+// site_join_kernel adds the slots.  A row's four sums go together, so that it waits for
+// the CTA two or three times.  The bytes bound it from some thousand rows on: 32760 x 1536,
+// fp32 stream, bf16 branch 170 us (79% of a copy's rate); 226 x 1920 13 us with the
+// second kernel, of which the launches' and the sums' latency is nearly all.
+constexpr int kBwdStages = 3;
+template <typename TS, typename TB, int V>
+__global__ void __launch_bounds__(kMostThreads<V>, V == 1 ? 12 : 1) site_backward_kernel(SiteBwd a) {
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float4 red[2][kMaxWarps];
-  pdl_wait();
+  constexpr int E = kRunOf<TS, TB>, kS = kBytes<TS, V>, kB = kBytes<TB, V>, kR = 0, kDr = kS, kY = 2 * kS, kDu = kY + kB;
+  constexpr int kStage = kDu + kB;
   const Site& s = a.s;
-  const Place at = place(s.d);
+  const Place<V, E> at = place<V, E>(s.d);
+  uint8_t* mine = ring;
+  const int unit = blockDim.x, stage_bytes = kStage * unit;
+  ulonglong2* wsum = reinterpret_cast<ulonglong2*>(ring + kBwdStages * stage_bytes) + threadIdx.x;  // [4 V]
+  const bool weights = a.dpre_w != nullptr || a.dpost_w != nullptr;
+  // absent operands and columns past the row are zeros
+  if (!at.on[at.kRuns - 1] || a.du == nullptr || a.dr == nullptr || a.y == nullptr)
+    for (int k = 0; k < kBwdStages; ++k) {
+      uint8_t* p = ring + k * stage_bytes;
+      clear_plane<TS, V, E>(p + kR * unit);
+      clear_plane<TS, V, E>(p + kDr * unit);
+      clear_plane<TB, V, E>(p + kY * unit);
+      clear_plane<TB, V, E>(p + kDu * unit);
+    }
+  for (int i = 0; weights && i < 4 * V; ++i) wsum[i * blockDim.x] = make_ulonglong2(0, 0);
   Reducer sums = reducer(red);
+  pdl_wait();
   const float d = (float)s.d, per_d = 1.f / d;
   const int64_t begin = blockIdx.x * a.per, end = min(s.rows, begin + a.per);
-  constexpr int kR = 0, kDr = kPlanes<TS>, kY = 2 * kPlanes<TS>, kDu = kY + kPlanes<TB>, kStage = kDu + kPlanes<TB>;
-  uint8_t* mine = ring + threadIdx.x * 16;
-  const int stride = kStage * blockDim.x * 16;
-  ulonglong2* wsum = reinterpret_cast<ulonglong2*>(ring + kStages * stride) + threadIdx.x;  // 8 planes of 4 columns
   int64_t ahead = begin;
-  int to = 0;
+  const TS *rp = static_cast<const TS*>(a.r) + (a.du ? begin * a.ldr : 0), *drp = static_cast<const TS*>(a.dr) + (a.dr ? begin * a.lddr : 0);
+  const TB *dup = static_cast<const TB*>(a.du) + (a.du ? begin * a.lddu : 0), *yp = static_cast<const TB*>(a.y) + (a.y ? begin * a.ldy : 0);
+  TS* dxp = static_cast<TS*>(a.dx) + (a.dx ? begin * a.lddx : 0);
+  TB* dyp = static_cast<TB*>(a.dy) + (a.dy ? begin * a.lddy : 0);
+  uint8_t* to = mine;
   auto issue = [&] {
     if (ahead < end) {
-      uint8_t* p = mine + to * stride;
       if (a.du != nullptr) {
-        stage(p, kR, static_cast<const TS*>(a.r) + ahead * a.ldr, at, ahead, s.rows);
-        stage(p, kDu, static_cast<const TB*>(a.du) + ahead * a.lddu, at, ahead, s.rows);
+        stage<TS, V, E>(to + kR * unit, rp, at, ahead, s.rows);
+        stage<TB, V, E>(to + kDu * unit, dup, at, ahead, s.rows);
+        rp += a.ldr;
+        dup += a.lddu;
       }
-      if (a.dr != nullptr) stage(p, kDr, static_cast<const TS*>(a.dr) + ahead * a.lddr, at, ahead, s.rows);
-      if (a.y != nullptr) stage(p, kY, static_cast<const TB*>(a.y) + ahead * a.ldy, at, ahead, s.rows);
+      if (a.dr != nullptr) {
+        stage<TS, V, E>(to + kDr * unit, drp, at, ahead, s.rows);
+        drp += a.lddr;
+      }
+      if (a.y != nullptr) {
+        stage<TB, V, E>(to + kY * unit, yp, at, ahead, s.rows);
+        yp += a.ldy;
+      }
       ++ahead;
     }
-    to = to + 1 == kStages ? 0 : to + 1;
+    to = to == mine + (kBwdStages - 1) * stage_bytes ? mine : to + stage_bytes;
     cp_async_commit();
   };
-  for (int k = 0; k < kStages - 1; ++k) issue();
-  const bool weights = a.dpre_w != nullptr || a.dpost_w != nullptr;
-  for (int i = 0; weights && i < 8; ++i) wsum[i * blockDim.x] = make_ulonglong2(0, 0);
-  const Cols zero = {};
-  int st = 0;
+  for (int k = 0; k < kBwdStages - 1; ++k) issue();
+  const uint8_t* from = mine;
   for (int64_t row = begin; row < end;) {
-    const int64_t g = group_of(s, row), m = g * s.ld_mod, from = row, last = min(end, group_end(s, g));
-    Cols A = {}, S = {}, T = {}, sc = scale_cols(s, m, at), gw = gate_cols(s, m, at);
+    const int64_t g = group_of(s, row), m = g * s.ld_mod, first = row, last = min(end, group_end(s, g));
+    Cols<V> A = {}, S = {}, T = {}, sc = scale_cols(s, m, at), gw = gate_cols(s, m, at);
     times(sc, vec(s.pre_w, at, 1.f));
     times(gw, vec(s.post_w, at, 1.f));
     for (; row < last; ++row) {
-      cp_async_wait<kStages - 2>();
-      const uint8_t* p = mine + st * stride;
-      Cols n = a.du != nullptr ? unstage<TS>(p, kR, at) : zero, du = a.du != nullptr ? unstage<TB>(p, kDu, at) : zero;
-      Cols y = a.y != nullptr ? unstage<TB>(p, kY, at) : zero, dr = a.dr != nullptr ? unstage<TS>(p, kDr, at) : zero;
+      cp_async_wait<kBwdStages - 2>();
+      Cols<V> n = unstage<TS, V, E>(from + kR * unit), du = unstage<TB, V, E>(from + kDu * unit);
+      Cols<V> y = unstage<TB, V, E>(from + kY * unit), dr = unstage<TS, V, E>(from + kDr * unit);
       issue();
-      st = st + 1 == kStages ? 0 : st + 1;
+      from = from == mine + (kBwdStages - 1) * stage_bytes ? mine : from + stage_bytes;
       if (s.pre == ACID_NORM_LAYER || s.post == ACID_NORM_LAYER) {
         const float4 t = sums.sum<2>(total(n), total(y));
         if (s.pre == ACID_NORM_LAYER) plus(n, -(t.x / d), at);
         if (s.post == ACID_NORM_LAYER) plus(y, -(t.y / d), at);
       }
       FOR_PAIRS A.v[i] = f2_add(A.v[i], du.v[i]);
-      // S takes du n before du becomes dn = du (1 + scale) pre_w, so the root comes first
-      Cols dn = du;
+      Cols<V> dn = du;
       times(dn, sc);
       float in = 1.f, ip = 1.f, mean = 0.f, along = 0.f;
       if (s.pre != ACID_NORM_NONE || s.post != ACID_NORM_NONE) {
@@ -442,20 +528,22 @@ __global__ void __launch_bounds__(384, 1) site_backward_kernel(SiteBwd a) {
         }
         if (s.post != ACID_NORM_NONE) ip = rsqrtf(fmaf(t.y, per_d, s.eps));
       }
+      // dr += in (dn - mean - along n); S takes du in n
       FOR_PAIRS {
         S.v[i] = f2_fma(f2_mul(du.v[i], f2_same(in)), n.v[i], S.v[i]);
         dn.v[i] = f2_fma(n.v[i], f2_same(-along), dn.v[i]);
       }
-      plus(dn, -mean, at);
+      if (s.pre == ACID_NORM_LAYER) plus(dn, -mean, at);
       FOR_PAIRS {
         dr.v[i] = f2_fma(f2_same(in), dn.v[i], dr.v[i]);
         y.v[i] = f2_mul(y.v[i], f2_same(ip));
         T.v[i] = f2_fma(dr.v[i], y.v[i], T.v[i]);
       }
       if (a.dx != nullptr) {
-        Cols o;
+        Cols<V> o;
         FOR_PAIRS o.v[i] = f2_mul(dr.v[i], f2_same(s.res));
-        put(static_cast<TS*>(a.dx) + row * a.lddx, at, o, row, s.rows);
+        put(dxp, at, o, row, s.rows);
+        dxp += a.lddx;
       }
       if (a.dy == nullptr) continue;
       times(dr, gw);
@@ -465,19 +553,20 @@ __global__ void __launch_bounds__(384, 1) site_backward_kernel(SiteBwd a) {
         if (s.post == ACID_NORM_LAYER) plus(dr, -t.x * per_d, at);
         FOR_PAIRS dr.v[i] = f2_mul(dr.v[i], f2_same(ip));
       }
-      put(static_cast<TB*>(a.dy) + row * a.lddy, at, dr, row, s.rows);
+      put(dyp, at, dr, row, s.rows);
+      dyp += a.lddy;
     }
     if (weights) {  // dpre_w gathers (1 + scale) S, dpost_w branch_scale gate T
-      const Cols f = scale_cols(s, m, at), h = gate_cols(s, m, at);
+      const Cols<V> f = scale_cols(s, m, at), h = gate_cols(s, m, at);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < 2 * V; ++i) {
         ulonglong2& p = wsum[i * blockDim.x];
-        ulonglong2& q = wsum[(4 + i) * blockDim.x];
+        ulonglong2& q = wsum[(2 * V + i) * blockDim.x];
         p = make_ulonglong2(f2_fma(f.v[2 * i], S.v[2 * i], p.x), f2_fma(f.v[2 * i + 1], S.v[2 * i + 1], p.y));
         q = make_ulonglong2(f2_fma(h.v[2 * i], T.v[2 * i], q.x), f2_fma(h.v[2 * i + 1], T.v[2 * i + 1], q.y));
       }
     }
-    const bool starts = group_begin(s, g) == from, ends = group_end(s, g) == last;
+    const bool starts = group_begin(s, g) == first, ends = group_end(s, g) == last;
     if (starts && ends) {
       put_sums(a, 0, g, m, at, A);
       put_sums(a, 1, g, m, at, S);
@@ -494,10 +583,10 @@ __global__ void __launch_bounds__(384, 1) site_backward_kernel(SiteBwd a) {
   float* wp = a.wpart + (int64_t)blockIdx.x * 2 * s.d;
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
-    Cols v;
+    Cols<V> v;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const ulonglong2 p = wsum[(4 * w + i) * blockDim.x];
+    for (int i = 0; i < 2 * V; ++i) {
+      const ulonglong2 p = wsum[(2 * V * w + i) * blockDim.x];
       v.v[2 * i] = p.x;
       v.v[2 * i + 1] = p.y;
     }
@@ -613,9 +702,9 @@ Site site_args(const acid_norm_site& s) {
   return a;
 }
 
-int threads_for(int d) { return (d + 511) / 512 * 32; }
+int threads_for(int d, int v) { return (d + 256 * v - 1) / (256 * v) * 32; }
 
-constexpr size_t kMaxSmem = 200 * 1024;
+constexpr size_t kMaxSmem = 224 * 1024;
 // CTAs that an SM keeps of a kernel with so much shared memory; sets the kernel
 // up in the context.  (An occupancy query at each launch would take longer than
 // the smallest kernels.)
@@ -648,20 +737,24 @@ struct FwdLaunch {
 };
 template <typename TS, typename TB>
 struct RunFwd {
-  static acid_status run(const FwdLaunch& l) { return l.a.y != nullptr ? go<true>(l) : go<false>(l); }
-  template <bool BRANCH>
+  static acid_status run(const FwdLaunch& l) {
+    if (l.a.s.d <= 256) return l.a.y != nullptr ? go<true, 1>(l) : go<false, 1>(l);
+    return l.a.y != nullptr ? go<true, 2>(l) : go<false, 2>(l);
+  }
+  template <bool BRANCH, int V>
   static acid_status go(const FwdLaunch& l) {
     static PerContext known;
     const Site& s = l.a.s;
-    const int threads = threads_for(s.d);
-    const size_t smem = (size_t)kFwdStages * threads * 16 * (kPlanes<TS> + (BRANCH ? kPlanes<TB> : 0));
+    const int threads = threads_for(s.d, V);
+    const size_t smem = (size_t)threads * kFwdStages * (kBytes<TS, V> + (BRANCH ? kBytes<TB, V> : 0));
+    const auto kernel = site_forward_kernel<TS, TB, BRANCH, V>;
     int fit;
-    ACID_TRY(ctas_per_sm(known, site_forward_kernel<TS, TB, BRANCH>, threads, smem, &fit));
+    ACID_TRY(ctas_per_sm(known, kernel, threads, smem, &fit));
     const int64_t most = (int64_t)num_sms() * fit;
     const int64_t ctas = std::min(s.rows, most), per = (s.rows + ctas - 1) / ctas;
     const bool strided = s.groups == 1;
-    launch_pdl(site_forward_kernel<TS, TB, BRANCH>, (unsigned)(strided ? ctas : (s.rows + per - 1) / per), threads,
-               smem, l.s, l.a, strided ? int64_t(1) : per, strided ? ctas : int64_t(1), (uint32_t)per);
+    launch_pdl(kernel, (unsigned)(strided ? ctas : (s.rows + per - 1) / per), threads, smem, l.s, l.a,
+               strided ? int64_t(1) : per, strided ? ctas : int64_t(1), (uint32_t)per);
     ACID_CHECK_LAUNCH();
     return ACID_OK;
   }
@@ -672,19 +765,21 @@ struct BwdLaunch {
 };
 template <typename TS, typename TB>
 struct RunBwd {
-  static acid_status run(const BwdLaunch& l) {
+  static acid_status run(const BwdLaunch& l) { return l.a.s.d <= 256 ? go<1>(l) : go<2>(l); }
+  template <int V>
+  static acid_status go(const BwdLaunch& l) {
     static PerContext known;
     SiteBwd a = l.a;
     const Site& s = a.s;
-    const int threads = threads_for(s.d);
-    const size_t smem = (size_t)threads * (kBwdStages<TS, TB> * 16 * 2 * (kPlanes<TS> + kPlanes<TB>) + 128);
+    const int threads = threads_for(s.d, V);
+    const size_t smem = (size_t)threads * (kBwdStages * 2 * (kBytes<TS, V> + kBytes<TB, V>) + 64 * V);
     int fit;
-    ACID_TRY(ctas_per_sm(known, site_backward_kernel<TS, TB>, threads, smem, &fit));
+    ACID_TRY(ctas_per_sm(known, site_backward_kernel<TS, TB, V>, threads, smem, &fit));
     const int64_t most = std::min<int64_t>(kMaxCtas, (int64_t)num_sms() * fit);
     a.per = std::max<int64_t>(1, (s.rows + most - 1) / most);
     const int ctas = (int)((s.rows + a.per - 1) / a.per);
     a.wpart = a.part + part_bytes(s.d, ctas) / sizeof(float);
-    launch_pdl(site_backward_kernel<TS, TB>, ctas, threads, smem, l.s, a);
+    launch_pdl(site_backward_kernel<TS, TB, V>, ctas, threads, smem, l.s, a);
     ACID_CHECK_LAUNCH();
     const bool weights = a.dpre_w != nullptr || a.dpost_w != nullptr;
     const bool vectors = a.dgate != nullptr || a.dscale != nullptr || a.dshift != nullptr;
