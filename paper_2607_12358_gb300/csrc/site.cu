@@ -302,7 +302,7 @@ constexpr int kRunOf = sizeof(TS) + sizeof(TB) == 4 ? 8 : 4;
 // Each operand passes once, so the bytes bound it; a few rows in flight a CTA and two or
 // more CTAs an SM keep the memory busy through the two or three sums of a row.  fp32
 // stream, bf16 branch, RMS and layer norm: 32760 x 1536 105 us (85% of a copy's rate),
-// 67576 x 3072 with a group of 3276 rows a frame 252 us (97%); one row 3.5 us, which is a
+// 67576 x 3072, both bf16, a group of 2040 rows a frame, 252 us (97%); one row 3.5 us, which is a
 // launch and three sums' latency.
 constexpr int kFwdStages = 4;
 template <typename TS, typename TB, bool BRANCH, int V>
