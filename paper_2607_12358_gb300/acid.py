@@ -10,6 +10,7 @@ leaves all allocation to the caller.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 from dataclasses import dataclass, field
 
@@ -349,6 +350,11 @@ def norm_site_workspace_size(site: A.acid_norm_site) -> int:
     return b.value
 
 
+@functools.lru_cache(maxsize=1024)
+def _site_bytes(rows, d):  # the size goes by these alone
+    return norm_site_workspace_size(A.acid_norm_site(rows=rows, d=d))
+
+
 def acid_norm_site_backward(du: torch.Tensor | None, r: torch.Tensor | None, y: torch.Tensor | None = None, *,
                             dr: torch.Tensor | None = None, gate: torch.Tensor | None = None,
                             scale: torch.Tensor | None = None, shift: torch.Tensor | None = None,
@@ -408,7 +414,7 @@ def acid_norm_site_backward(du: torch.Tensor | None, r: torch.Tensor | None, y: 
             t = out["dpre_w"] = _empty(d, dtype=_F32, device=dev)
             dpre = t.data_ptr()
     if workspace is None:
-        workspace = _empty(norm_site_workspace_size(site), dtype=torch.uint8, device=dev)
+        workspace = _empty(_site_bytes(rows, d), dtype=torch.uint8, device=dev)
     grads = A.acid_norm_site_grads(dx.data_ptr(), lddx, dyp, lddy, dgate, dscale, dshift, d, dpost, dpre)
     status = load().acid_norm_site_backward(C.byref(site), dup, lddu, rp, ldr, yp, ldy, drp, lddr, C.byref(grads),
                                             workspace.data_ptr(), workspace.numel(), _stream(stream))

@@ -431,11 +431,17 @@ struct BackSmem {
 };
 constexpr int kTopRuns = 8;  // parts of a share's scales that are scanned by a CTA each
 
+// What each addition rounds off is added up beside the sum (exact: the difference of the
+// operands' and the sum's parts), so that terms that cancel leave a sum as good as its terms.
 __device__ __forceinline__ void bias_of(const Q4Bwd& a, int64_t n) {
-  float sum = 0.f;
+  float sum = 0.f, off = 0.f;
 #pragma unroll 8
-  for (int64_t m = 0; m < a.m; ++m) sum += value_at(a.g_dtype, a.g, m * a.ldg + n);
-  a.dbias[n] = sum;
+  for (int64_t m = 0; m < a.m; ++m) {
+    const float v = value_at(a.g_dtype, a.g, m * a.ldg + n), t = sum + v, part = t - sum;
+    off += (sum - (t - part)) + (v - part);
+    sum = t;
+  }
+  a.dbias[n] = isfinite(sum) ? sum + off : sum;
 }
 // The bias's gradient alone.
 __global__ void __launch_bounds__(kThreads) q4_bias_kernel(Q4Bwd a) {
