@@ -282,24 +282,34 @@ __device__ __noinline__ uint32_t divided_codes(float4 lo, float4 hi, float s, in
 // The same with one division a group: the quotient comes from a product with
 // inv = 1 / s, off by less than 2^-22 of it, and is rounded to even by the sum with 1.5 2^23,
 // whose last bits are then the code's; the eight are gathered by one addition each,
-// the constant bits above them taken out at the end.  A word with a value within
-// 1e-4 of the middle of two codes (or where inv is no use) is formed by divisions.
+// the constant bits above them taken out at the end.
+//   A quotient near the middle of two codes depends on its last bits.  Where value and
+// scale are bf16 (SHORT) it is the middle m or at least 2^-9 off it (v - m s is a multiple
+// of half the last place of s), and the middle itself is met often; the remainder v - q s
+// (one fma, exact) takes the product's error out, so that it comes out exactly.  Otherwise a
+// word with a value within 1e-4 of a middle is formed by divisions, as are those whose
+// scale is no ordinary number.
 //   Quotients lie in -7.03 .. 7.03 without zero points (s may be rounded down by 2^-8):
 // no code is clamped; with them the largest may come out as 16.
-template <bool ZEROS>
+template <bool ZEROS, bool SHORT>
 __device__ __forceinline__ uint32_t codes_of(const float (&v)[8], float s, float inv, int z) {
   constexpr float kRound = 12582912.f;
   const uint64_t inv2 = f2_pack(inv, inv), up = f2_pack(kRound, kRound), down = f2_pack(-kRound, -kRound);
-  const uint64_t minus = f2_pack(-1.f, -1.f);
+  const uint64_t minus = f2_pack(-1.f, -1.f), minus_s = f2_pack(-s, -s);
   const float most = kRound + (float)(15 - z);
   uint32_t word = 0;
   float off = 0.f;
 #pragma unroll
   for (int j = 6; j >= 0; j -= 2) {
-    const uint64_t q = f2_mul(f2_pack(v[j], v[j + 1]), inv2), r = f2_add(q, up);
-    float a, b, x, y;
-    f2_unpack(f2_fma(f2_add(r, down), minus, q), a, b);
-    off = max_or_nan(off, max_or_nan(fabsf(a), fabsf(b)));
+    const uint64_t v2 = f2_pack(v[j], v[j + 1]);
+    uint64_t q = f2_mul(v2, inv2);
+    if (SHORT) q = f2_fma(f2_fma(q, minus_s, v2), inv2, q);
+    const uint64_t r = f2_add(q, up);
+    float x, y;
+    if (!SHORT) {
+      f2_unpack(f2_fma(f2_add(r, down), minus, q), x, y);
+      off = max_or_nan(off, max_or_nan(fabsf(x), fabsf(y)));
+    }
     f2_unpack(r, x, y);
     if (ZEROS) {
       x = fminf(x, most);
@@ -308,70 +318,150 @@ __device__ __forceinline__ uint32_t codes_of(const float (&v)[8], float s, float
     word = word * 16u + __float_as_uint(y);
     word = word * 16u + __float_as_uint(x);
   }
-  if (off < 0.4999f) return word - (0x4B400000u - (uint32_t)z) * 0x11111111u;
+  const bool sure = SHORT ? s >= 0x1p-90f && s <= 0x1p90f : off < 0.4999f;
+  if (sure) return word - (0x4B400000u - (uint32_t)z) * 0x11111111u;
   return divided_codes(make_float4(v[0], v[1], v[2], v[3]), make_float4(v[4], v[5], v[6], v[7]), s, z);
 }
 
-// 8 values of the weight, zeros past its columns.
+// 8 values of the weight as they lie in memory, zeros past its columns.
 template <typename TW>
-__device__ __forceinline__ void weight8(const TW* p, int cols, bool wide, float (&v)[8]) {
-  if (wide && cols >= 8) {
-    load8(p, v);
-  } else {
+struct Octet {
+  uint4 bits[sizeof(TW) / 2];
+  __device__ __forceinline__ void load(const TW* p, int cols, bool wide) {
+    if (wide && cols >= 8) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j < cols ? io<TW>::ld(p + j) : 0.f;
-  }
-}
-// A thread takes 32 columns of a row (four words); a group is one, two or four
-// threads.  HBM would bound it (36864 x 3072 bf16: 42 us); what a thread does once,
-// two divisions and the places of its columns, weighed most with eight columns each
-// (183 us).
-template <typename TW, typename TS, bool ZEROS>
-__global__ void __launch_bounds__(kThreads) q4_quantize_kernel(const TW* W, int64_t ldw, Q4 w, uint32_t* packed,
-                                                               TS* scales, uint8_t* zeros, bool wide) {
-  pdl_wait();
-  const int per_row = w.slabs * 4;
-  const int64_t unit = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t row = unit / per_row;
-  const int block = (int)(unit - row * per_row), col = block * 32;
-  const bool in = row < w.n && ACID_IN_BOUNDS(kSiteQ4, row, w.n);
-  const TW* src = W + (in ? row * ldw + col : 0);
-  float v[4][8], hi = 0.f, lo = 0.f;  // max(w, 0) and -min(w, 0), or max |w|
-#pragma unroll
-  for (int t = 0; t < 4; ++t) weight8(src + 8 * t, in ? w.k - col - 8 * t : 0, wide, v[t]);
-#pragma unroll
-  for (int t = 0; t < 4; ++t)
+      for (int i = 0; i < (int)sizeof(TW) / 2; ++i) bits[i] = reinterpret_cast<const uint4*>(p)[i];
+      return;
+    }
+    uint32_t u[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      hi = max_or_nan(hi, ZEROS ? v[t][j] : fabsf(v[t][j]));
-      if (ZEROS) lo = max_or_nan(lo, -v[t][j]);
+      if constexpr (sizeof(TW) == 4)
+        u[j] = j < cols ? __float_as_uint(p[j]) : 0u;
+      else
+        u[j] = j < cols ? __bfloat16_as_ushort(p[j]) : 0u;
     }
-  for (int o = 1; o < 1 << (w.group_log - 5); o <<= 1) {
-    hi = max_or_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    if (ZEROS) lo = max_or_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    if constexpr (sizeof(TW) == 4) {
+      bits[0] = make_uint4(u[0], u[1], u[2], u[3]);
+      bits[1] = make_uint4(u[4], u[5], u[6], u[7]);
+    } else {
+      bits[0] = make_uint4(u[0] | u[1] << 16, u[2] | u[3] << 16, u[4] | u[5] << 16, u[6] | u[7] << 16);
+    }
   }
-  TS st;
-  io<TS>::st(&st, ZEROS ? (hi + lo) / 15.f : hi / 7.f);
-  const float s = io<TS>::ld(&st), div = s == 0.f ? 1.f : s, inv = 1.f / div;
-  const int z = ZEROS ? (int)fminf(fmaxf(rintf(lo / div), 0.f), 15.f) : 8;
-  if (!in) return;
-  // word 4 t + i of the slab holds the octet t of its 32 columns i
-  uint32_t* out = packed + row * w.slabs * 16 + (block >> 2) * 16 + (block & 3);
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    const uint32_t* u = reinterpret_cast<const uint32_t*>(bits);
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
-    if (ACID_IN_BOUNDS(kSiteQ4, out + 4 * t - packed, w.n * w.slabs * 16)) out[4 * t] = codes_of<ZEROS>(v[t], div, inv, z);
-  if ((block & ((1 << (w.group_log - 5)) - 1)) == 0 && col < w.k) {
-    const int64_t p = row * w.groups + (col >> w.group_log);
-    if (ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.groups)) {
-      scales[p] = st;
-      if (ZEROS) zeros[p] = (uint8_t)z;
+    for (int j = 0; j < 8; ++j)
+      v[j] = sizeof(TW) == 4 ? __uint_as_float(u[j]) : j % 2 ? bf16_hi(u[j / 2]) : bf16_lo(u[j / 2]);
+  }
+};
+// Four lanes take 128 columns of a row, each of them the octets t, t + 4, t + 8 and t + 12:
+// their loads lie together and a lane's four words do too (with 32 adjoining columns a
+// lane, 16-byte pieces 64 bytes apart, 36864 x 3072 took 88 us).  The four share 128 >> LOG
+// groups: the exchange that finds the largest values hands each group to lanes that do its
+// two divisions, once for 32 columns, and hand them round.
+//   A CTA's threads go on by `rows` rows and `slabs` slabs, with the next columns' loads
+// ahead of the work (without: 70 us).  HBM bounds it: 36864 x 3072, groups of 128, from bf16
+// 45 us (93% of a copy's rate), from fp32 80 us (94%); with fp32 scales of bf16 values,
+// whose middles are divided out, 91 us.
+template <typename TW, typename TS, bool ZEROS, int LOG>
+__global__ void __launch_bounds__(kThreads) q4_quantize_kernel(const TW* W, int64_t ldw, Q4 w, uint32_t* packed,
+                                                               TS* scales, uint8_t* zeros, bool wide, int64_t rows,
+                                                               int slabs) {
+  pdl_wait();
+  constexpr int kGroups = 128 >> LOG;
+  const int t = threadIdx.x & 3;
+  int64_t next_row = (blockIdx.x * (kThreads / 4) + (threadIdx.x >> 2)) / w.slabs;
+  int next_slab = (int)((blockIdx.x * (kThreads / 4) + (threadIdx.x >> 2)) - next_row * w.slabs);
+  Octet<TW> next[4];
+  auto fetch = [&] {
+    const int col = next_slab * 128 + 8 * t;
+    const bool in = next_row < w.n && ACID_IN_BOUNDS(kSiteQ4, next_row, w.n);
+    const TW* src = W + (in ? next_row * ldw + col : 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) next[i].load(src + 32 * i, in ? w.k - col - 32 * i : 0, wide);
+  };
+  fetch();
+  // whole warps go on together: the shuffles need all lanes
+  for (;;) {
+    const int64_t row = next_row;
+    const int slab = next_slab;
+    const bool in = row < w.n;
+    if (!__any_sync(0xffffffffu, in)) break;
+    float v[4][8], hi[kGroups], lo[kGroups];  // max(w, 0) and -min(w, 0), or max |w|
+#pragma unroll
+    for (int i = 0; i < 4; ++i) next[i].values(v[i]);
+    next_row += rows;
+    next_slab += slabs;
+    if (next_slab >= w.slabs) {
+      next_slab -= w.slabs;
+      ++next_row;
+    }
+    fetch();
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) hi[g] = lo[g] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float &h = hi[i >> (LOG - 5)], &l = lo[i >> (LOG - 5)];
+        h = max_or_nan(h, ZEROS ? v[i][j] : fabsf(v[i][j]));
+        if (ZEROS) l = max_or_nan(l, -v[i][j]);
+      }
+    // lane t ends with group t & (kGroups - 1)
+    auto largest = [&](float (&x)[kGroups]) {
+      if constexpr (kGroups == 4) {
+        const bool up = t & 2;
+        const float a = __shfl_xor_sync(0xffffffffu, up ? x[0] : x[2], 2), b = __shfl_xor_sync(0xffffffffu, up ? x[1] : x[3], 2);
+        x[0] = max_or_nan(up ? x[2] : x[0], a);
+        x[1] = max_or_nan(up ? x[3] : x[1], b);
+      }
+      if constexpr (kGroups >= 2) {
+        const bool up = t & 1;
+        const float a = __shfl_xor_sync(0xffffffffu, up ? x[0] : x[1], 1);
+        x[0] = max_or_nan(up ? x[1] : x[0], a);
+      } else {
+        x[0] = max_or_nan(x[0], __shfl_xor_sync(0xffffffffu, x[0], 1));
+      }
+      if constexpr (kGroups <= 2) x[0] = max_or_nan(x[0], __shfl_xor_sync(0xffffffffu, x[0], 2));
+      return x[0];
+    };
+    const float top = largest(hi), low = ZEROS ? largest(lo) : 0.f;
+    TS st;
+    io<TS>::st(&st, ZEROS ? (top + low) / 15.f : top / 7.f);
+    const float s = io<TS>::ld(&st), div = s == 0.f ? 1.f : s, inv = 1.f / div;
+    const int z = ZEROS ? (int)fminf(fmaxf(rintf(low / div), 0.f), 15.f) : 8;
+    // word 4 t + i of the slab holds the octet t of its 32 columns i
+    constexpr bool kShort = sizeof(TW) == 2 && sizeof(TS) == 2;
+    uint32_t words[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      constexpr uint32_t kAll = 0xffffffffu;
+      const int of = i >> (LOG - 5);
+      if (kGroups == 1)
+        words[i] = codes_of<ZEROS, kShort>(v[i], div, inv, z);
+      else
+        words[i] = codes_of<ZEROS, kShort>(v[i], __shfl_sync(kAll, div, of, 4), __shfl_sync(kAll, inv, of, 4),
+                                   ZEROS ? __shfl_sync(kAll, z, of, 4) : 8);
+    }
+    if (!in) continue;
+    const int64_t at = (row * w.slabs + slab) * 16 + 4 * t;
+    if (ACID_IN_BOUNDS(kSiteQ4, at + 3, w.n * w.slabs * 16))
+      *reinterpret_cast<uint4*>(packed + at) = make_uint4(words[0], words[1], words[2], words[3]);
+    const int group = slab * kGroups + t;
+    if (t < kGroups && group < w.groups) {
+      const int64_t p = row * w.groups + group;
+      if (ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.groups)) {
+        scales[p] = st;
+        if (ZEROS) zeros[p] = (uint8_t)z;
+      }
     }
   }
 }
 
 // ------------------------------------------------------------------- values
 // A lane takes eight columns of a row (one word), a warp 32 such octets of one
-// row at a time.  HBM bounds it: 36864 x 3072 to fp32 in 76 us.
+// row at a time.  HBM bounds it: 36864 x 3072 to fp32 in 75 us (89% of a copy's rate).
 constexpr int kUnits = 4;  // octet runs of a warp, all loaded before the first is worked on
 struct Runs {
   int64_t n;    // runs: n rows of per_row
@@ -540,15 +630,25 @@ extern "C" acid_status acid_q4_quantize(int32_t w_dtype, const void* W, int64_t 
   cudaStream_t s = (cudaStream_t)stream;
   const Q4 w = q4_args(*weight);
   const bool wide = aligned(W, 16) && ldw % 8 == 0;
-  const unsigned grid = (unsigned)((w.n * w.slabs * 4 + kThreads - 1) / kThreads);
+  const int64_t units = kThreads / 4, all = (w.n * w.slabs + units - 1) / units;  // 128 columns of a row, by four threads
+  const int64_t most = (int64_t)num_sms() * (w_dtype == ACID_BF16 ? 3 : 2), turns = (all + most - 1) / most;
+  const unsigned grid = (unsigned)((all + turns - 1) / turns);
+  const int64_t step = grid * units, rows = step / w.slabs;
+  const int slabs = (int)(step - rows * w.slabs);
   auto packed = static_cast<uint32_t*>(const_cast<void*>(weight->packed));
   auto scales = const_cast<void*>(weight->scales);
   auto zeros = const_cast<uint8_t*>(weight->zeros);
   auto launch = [&](auto* src, auto* sc) {
     using TW = std::remove_const_t<std::remove_pointer_t<decltype(src)>>;
     using TS = std::remove_pointer_t<decltype(sc)>;
-    launch_pdl(zeros != nullptr ? q4_quantize_kernel<TW, TS, true> : q4_quantize_kernel<TW, TS, false>, grid, kThreads, 0,
-               s, src, ldw, w, packed, sc, zeros, wide);
+    auto with = [&](auto log) {
+      constexpr int LOG = decltype(log)::value;
+      launch_pdl(zeros != nullptr ? q4_quantize_kernel<TW, TS, true, LOG> : q4_quantize_kernel<TW, TS, false, LOG>, grid,
+                 kThreads, 0, s, src, ldw, w, packed, sc, zeros, wide, rows, slabs);
+    };
+    w.group_log == 5   ? with(std::integral_constant<int, 5>())
+    : w.group_log == 6 ? with(std::integral_constant<int, 6>())
+                       : with(std::integral_constant<int, 7>());
   };
   auto by_scale = [&](auto* src) {
     if (weight->scale_dtype == ACID_BF16)

@@ -102,6 +102,35 @@ def test_wide(acid):
     check_both(acid, 3, 70001, 256, 32, False, BF, F32, F32, True)
 
 
+def test_offsets_past_32_bits(acid):
+    """Products, their gradients and values past element 2^31, against the definition in 64 bits at both ends."""
+    n, k, m = 1 << 20, 64, 2050
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    scales = torch.empty(n, 2, device=DEV).uniform_(0.003, 0.009, generator=gen)
+    q = acid.Q4Weight(torch.randint(0, 256, (n, 64), device=DEV, generator=gen, dtype=torch.uint8), scales, None, n, k, 32)
+    w = acid.acid_q4_dequantize(q).double()
+    x = randn(m, k, seed=6)
+    out = acid.acid_q4_linear_forward(x, q, out_dtype=BF)
+    for rows in (slice(0, 3), slice(m - 5, m)):
+        for cols in (slice(0, 300), slice(n - 300, n)):
+            close(out[rows, cols], f64(x[rows].double() @ w[cols].T), TOL[BF], (rows, cols))
+    dx, db = acid.acid_q4_linear_backward(out, q)
+    at = torch.tensor([0, 1, m // 2, m - 2, m - 1], device=DEV)
+    close(dx[at], f64(out[at].double() @ w), TOL[F32], "dx")
+    cols = slice(n - 300, n)
+    close(db[cols], f64(out[:, cols].double().sum(0)), 5e-6, "dbias")
+    n, k = (1 << 16) + 3, 65536  # 2^32 codes and more
+    packed = torch.randint(0, 256, (n, k // 2), device=DEV, generator=gen, dtype=torch.uint8)
+    scales = torch.empty(n, k // 128, device=DEV, dtype=BF).uniform_(0.003, 0.009, generator=gen)
+    q = acid.Q4Weight(packed, scales, None, n, k, 128)
+    tail = acid.Q4Weight(packed[-5:], scales[-5:], None, 5, k, 128)
+    v = acid.acid_q4_dequantize(q, dtype=BF)
+    assert torch.equal(v[-5:], acid.acid_q4_dequantize(tail, dtype=BF))
+    x = randn(1, k, seed=7)
+    y = acid.acid_q4_linear_forward(x, q)
+    close(y[:, -5:], f64(x.double() @ acid.acid_q4_dequantize(tail).double().T), TOL[F32], "long rows")
+
+
 def test_values_of_x(acid):
     """Rows of zeros, of very large and very small values; an infinity or a NaN stays in its row."""
     q, w = weight(acid, 200, 512, 64, False, seed=4)
@@ -184,6 +213,30 @@ def test_quantiser(acid, wdt, scale_dtype, group, zeros):
         out = torch.full((n, k + 5), 7.0, device=DEV)
         acid.acid_q4_dequantize(q, out=out[:, 2:-3])
         assert torch.equal(out[:, 2:-3], got) and (out[:, :2] == 7).all() and (out[:, -3:] == 7).all()
+
+
+@pytest.mark.parametrize("wdt,scale_dtype", [(BF, BF), (BF, F32), (F32, BF), (F32, F32)])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_quantiser_at_the_middles_of_codes(acid, wdt, scale_dtype, zeros):
+    """Values at halves of the scale, some a last place off them, scales from subnormal to 2^120; rows that wide loads
+    can read, and their copy a column further on."""
+    rng = np.random.default_rng(11)
+    n, k = 126, 520
+    size = np.exp2(np.arange(n) * 2.0 - 131) * (1 + rng.integers(0, 16, n) / 16)
+    v = rng.integers(-14, 15, (n, k)) / 2
+    v[:, ::32] = 7  # each group's largest, so that its scale is the row's size
+    near = rng.integers(-1, 2, (n, k)) * (rng.random((n, k)) < 0.3)
+    w = torch.from_numpy((v * (1 + near * 2.0 ** -23) * size[:, None]).astype(np.float32)).to(DEV, wdt)
+    rnd = lambda s: torch.from_numpy(s).to(scale_dtype).float().numpy()  # noqa: E731
+    for group in (32, 64, 128):
+        codes, scales, zs = O.q4_quantize(w.float().cpu().numpy(), group, zeros, rnd)
+        for shift in (0, 1):
+            there = torch.zeros(n, k + 8, device=DEV, dtype=wdt)[:, shift:shift + k]
+            there.copy_(w)
+            q = acid.acid_q4_quantize(there, group, zeros=zeros, scale_dtype=scale_dtype)
+            assert (q.scales.float().cpu().numpy() == scales).all()
+            assert (O.q4_unpack(q.packed.cpu().numpy(), k) == codes).all()
+            assert zs is None or (q.zeros.cpu().numpy() == zs).all()
 
 
 def test_quantiser_of_values_that_are_not_finite(acid):
