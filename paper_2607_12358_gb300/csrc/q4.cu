@@ -582,11 +582,15 @@ size_t workspace_bytes(const Q4& w, int64_t m) {
   return std::max<size_t>({16, fwd_bytes(w, m), m > 0 ? q4_backward_bytes(w, m) : 0});
 }
 
-// Warps of a CTA that share a row's columns: as many as give every SM eight warps
-// where the rows alone would not.
+// Warps of a CTA that share a row's columns: as many as give every SM eight warps where
+// the rows alone would not, and up to four while an SM's sixteen warps have less than two
+// turns each, which then come out more evenly (a row of x, groups of 128: 46080 x 1536
+// with four 12.4 us, with one 16.3; 80000 x 1920 with two 26.4, with one 32.3; beyond, the
+// sums' exchange costs as much as it gains: 138240 x 3072 58.3 and 55.6).
 int sharing_warps(const Q4& w) {
+  const int64_t tiles = (w.n + 31) / 32, sms = num_sms();
   int kw = 1;
-  while (kw < 8 && 2 * kw <= w.slabs && (w.n + 31) / 32 * kw < 8 * num_sms()) kw *= 2;
+  while (kw < 8 && 2 * kw <= w.slabs && (tiles * kw < 8 * sms || (kw < 4 && tiles * kw < 28 * sms))) kw *= 2;
   return kw;
 }
 template <typename TS, bool ZEROS, int LOG>

@@ -17,7 +17,7 @@ namespace {
 
 using bf16 = __nv_bfloat16;
 constexpr int kThreads = 256;
-constexpr int kRowsThreads = 576;  // product: 16 warps that make operands, an MMA warp and a copying warp
+constexpr int kRowsThreads = 608;  // product: 16 warps that make operands, two MMA warps and a copying warp
 
 // Instruction descriptor of kind::f16 with fp16 A and B, fp32 accumulator.
 __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool b_mn) {
@@ -35,17 +35,11 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
-               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-               : "memory");
-}
 // One arrival for the warp, after what all its lanes did.
 __device__ __forceinline__ void arrive_warp(uint64_t* bar, bool leader) {
   __syncwarp();
   if (leader) mbar_arrive(bar);
 }
-__device__ __forceinline__ uint4 load_codes(const uint32_t* p) { return *reinterpret_cast<const uint4*>(p); }
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
                    smem_u32(dst)),
@@ -91,27 +85,32 @@ __device__ __forceinline__ float up_to_scale(uint32_t top) {
 __device__ __forceinline__ uint32_t finite_bits(float v) { return isfinite(v) ? __float_as_uint(fabsf(v)) : 0u; }
 
 // ------------------------------------------------------------------ product
-// D[128 rows of the weight, 16 NT] = codes x parts^T for each group of columns, the
+// D[128 rows of the weight, 16 NB] = codes x parts^T for each group of columns, the
 // codes as the exact halves q - z in tensor memory (a row to a lane, where the lane's
-// threads write them), the parts of a(x) in shared memory (8 NT rows of high parts,
-// then of low parts).  The same threads read the group's sums back and add them in
-// fp32 to the row's totals, times its scale.  (The scale as part of the operand, a
+// threads write them), the parts of a(x) in shared memory (16 NB rows of high parts,
+// then of low parts, which go first into the same sums).  The same threads read the
+// group's sums back and add them in fp32 to the row's totals, times its scale.  (The scale as part of the operand, a
 // value in two halves, would spare that only where sums may stay in tensor memory: the
 // tensor cores' sums lose up to 2^-23 of themselves at each addition, always towards
 // zero, 1.7e-4 over 65536 columns.  It costs more instructions and twice the MMAs.)
-//   A CTA has two tiles of 128 rows; each of their lanes belongs to two threads,
-// which share its words and its sums.  Issue slots bound it: 36864 x 3072, 34 rows.
+//   A CTA has two tiles of 128 rows.  Each of their lanes belongs to two threads, which
+// take the codes of every other slab of 128 columns (with half of each slab's the same
+// waits and fences came twice as often) and half of the columns of all sums.  The
+// chain of waits from a slab's codes to its sums bounds it, then the instructions that
+// make the operands: 36864 x 3072, groups of 128, 34 rows 29 us, of which the MMAs by
+// themselves are 20; groups of 64 36 us, of 32 59 us; 8 rows 26 us.  (One thread issuing
+// for both tiles in steps of 64 columns: 37 us.)
 constexpr int kFwdRing = 4;   // slabs of parts in shared memory
-constexpr int kCodeRing = 4;  // slabs of a warp's share of 32 rows of codes
+constexpr int kCodeRing = 2;  // a warp's slabs of its 32 rows of codes
 // Bytes of a slab's parts: two boxes of 64 columns, rows of 128 bytes whose
 // 16-byte units are swizzled as the tensor cores read them.
-template <int NT>
-constexpr int kSlabBytes = 16 * NT * 256;
-template <int NT>
-constexpr int kFwdSmem = kFwdRing * kSlabBytes<NT> + 16 * kCodeRing * 1024 + 256 + 1024;
+template <int NB>
+constexpr int kSlabBytes = 32 * NB * 256;
+template <int NB>
+constexpr int kFwdSmem = kFwdRing * kSlabBytes<NB> + 16 * kCodeRing * 2048 + 512 + 1024;
 
 // One CTA to a row of a(x).
-template <int NT>
+template <int NB>
 __global__ void __launch_bounds__(kThreads) q4_parts_kernel(Q4Fwd a) {
   __shared__ uint32_t largest;
   pdl_wait();
@@ -132,43 +131,46 @@ __global__ void __launch_bounds__(kThreads) q4_parts_kernel(Q4Fwd a) {
     split_octet(v, by, hi, lo);
     const int slab = o >> 4, word = (o >> 2) & 3, unit = (word & 1) * 4 + (o & 3);
     // octets in the order of the codes in a lane: words 32 columns by 32, in them the lanes' quarters
-    uint8_t* p = a.parts + (chunk * a.w.slabs + slab) * kSlabBytes<NT> + (word >> 1) * (16 * NT * 128);
+    uint8_t* p = a.parts + (chunk * a.w.slabs + slab) * kSlabBytes<NB> + (word >> 1) * (32 * NB * 128);
     *reinterpret_cast<uint4*>(p + n * 128 + ((unit ^ (n & 7)) << 4)) = hi;
-    *reinterpret_cast<uint4*>(p + (8 * NT + n) * 128 + ((unit ^ (n & 7)) << 4)) = lo;
+    *reinterpret_cast<uint4*>(p + (16 * NB + n) * 128 + ((unit ^ (n & 7)) << 4)) = lo;
   }
 }
 
-template <int NT, int LOG>
+template <int NB, int LOG>
 __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd a, int scale_dtype) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* ring = smem;
-  uint8_t* codes = ring + kFwdRing * kSlabBytes<NT>;
-  constexpr int kCols = 16 * NT, kHalf = 8 * NT;
-  // A step is 64 columns or a group of 32; a group's sums are there after kSteps of them.
-  constexpr int kWords = LOG == 5 ? 1 : 2, kPerSlab = 4 / kWords, kSteps = LOG == 7 ? 2 : 1, kGroups = 128 >> LOG;
-  // tensor memory: codes [tile][2 buffers][32], sums [tile][buffers]
-  constexpr int kSums = NT <= 5 ? 2 : 1, kDStride = NT <= 5 ? 96 : 128;
-  constexpr uint32_t kACol = 0, kDCol = 128;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(codes + 16 * kCodeRing * 1024);
-  uint64_t *b_full = bars, *b_empty = bars + kFwdRing;                          // [ring]
-  uint64_t *a_full = b_empty + kFwdRing, *a_empty = a_full + 4;                 // [tile][2]
-  uint64_t *d_full = a_empty + 4, *d_empty = d_full + 4, *drain = d_empty + 4;  // [tile][2]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  uint8_t* codes = ring + kFwdRing * kSlabBytes<NB>;
+  constexpr int kCols = 16 * NB;
+  constexpr int kGroups = 128 >> LOG;  // of a slab
+  // tensor memory: codes [tile][2 buffers][64], sums [tile][buffers]
+  constexpr int kSums = NB <= 2 ? 4 : 2, kDStride = 128 / kSums;
+  constexpr uint32_t kACol = 0, kDCol = 256;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(codes + 16 * kCodeRing * 2048);
+  uint64_t *b_full = bars, *b_empty = bars + kFwdRing;                 // [ring]
+  uint64_t *a_full = b_empty + kFwdRing, *a_empty = a_full + 4;        // [tile][2]
+  uint64_t *d_full = a_empty + 4, *d_empty = d_full + 2 * kSums;       // [tile][buffer]
+  uint64_t* drain = d_empty + 2 * kSums;                               // [tile]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 2);
   const Q4& w = a.w;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kFwdRing; ++i) {
       mbar_init(&b_full[i], 1);
-      mbar_init(&b_empty[i], 1);
+      mbar_init(&b_empty[i], 2);
     }
     for (int i = 0; i < 4; ++i) {
-      mbar_init(&a_full[i], 8);
+      mbar_init(&a_full[i], 4);
       mbar_init(&a_empty[i], 1);
+    }
+    for (int i = 0; i < 2 * kSums; ++i) {
       mbar_init(&d_full[i], 1);
       mbar_init(&d_empty[i], 8);
     }
-    mbar_init(drain, 1);
+    mbar_init(&drain[0], 1);
+    mbar_init(&drain[1], 1);
     mbar_fence_init();
   }
   if (warp == 16) tmem_alloc(tmem_slot, 512);
@@ -179,9 +181,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
   pdl_wait();
 
   const int64_t sets = (w.n + 255) / 256, chunk = blockIdx.y, m0 = chunk * kQ4Chunk;
-  const uint8_t* parts = a.parts + chunk * w.slabs * kSlabBytes<NT>;
+  const uint8_t* parts = a.parts + chunk * w.slabs * kSlabBytes<NB>;
 
-  if (warp == 17) {
+  if (warp == 18) {
     if (lane == 0) {  // ------------------------------------------ copies of the parts
       int issued = 0;
       bool ok = true;
@@ -189,140 +191,128 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
         for (int slab = 0; slab < w.slabs; ++slab, ++issued) {
           const int st = issued % kFwdRing;
           if (issued >= kFwdRing && !mbar_wait(&b_empty[st], (issued / kFwdRing - 1) & 1)) { ok = false; break; }
-          mbar_expect_tx(&b_full[st], kSlabBytes<NT>);
-          bulk_load(ring + st * kSlabBytes<NT>, parts + (int64_t)slab * kSlabBytes<NT>, kSlabBytes<NT>, &b_full[st]);
+          mbar_expect_tx(&b_full[st], kSlabBytes<NB>);
+          bulk_load(ring + st * kSlabBytes<NB>, parts + (int64_t)slab * kSlabBytes<NB>, kSlabBytes<NB>, &b_full[st]);
         }
       // after a wait ran out: the last copies have landed before the CTA leaves
       if (!ok)
         for (int j = issued > kFwdRing ? issued - kFwdRing : 0; j < issued; ++j)
           mbar_wait(&b_full[j % kFwdRing], (j / kFwdRing) & 1);
     }
-  } else if (warp == 16) {
-    // ------------------------------------------------------------- MMA issuer
-    const bool leader = elect_one();
-    constexpr uint32_t idesc = idesc_f16_f32(128, kCols, false);
-    const uint64_t bdesc = smem_desc_sw128(smem_u32(ring), 16, 1024);
-    bool ok = true;
-    uint32_t u = 0, e = 0;  // steps, groups
-    int v = 0;              // slabs
-    for (int64_t set = blockIdx.x; ok && set < sets; set += gridDim.x)
-      for (int slab = 0; ok && slab < w.slabs; ++slab, ++v) {
-        const int st = v % kFwdRing;
-        if (!mbar_wait_warp(&b_full[st], (v / kFwdRing) & 1)) { ok = false; break; }
-        for (int h = 0; ok && h < kPerSlab; ++h, ++u) {
-          const bool first = kSteps == 1 || h == 0, last = kSteps == 1 || h == 1;
-          const int db = e % kSums;
-          for (int tile = 0; tile < 2; ++tile) {
-            if (!mbar_wait_warp(&a_full[tile * 2 + (u & 1)], (u >> 1) & 1)) { ok = false; break; }
-            if (first && e >= kSums && !mbar_wait_warp(&d_empty[tile * 2 + db], (e / kSums - 1) & 1)) { ok = false; break; }
-            tc_fence_after();
-            if (leader) {
-              const uint32_t d = tmem + kDCol + (tile * kSums + db) * kDStride, c = tmem + kACol + tile * 64 + (u & 1) * 32;
-              const uint64_t slot = bdesc + (uint64_t)((st * kSlabBytes<NT>) >> 4);
+  } else if (warp >= 16) {
+    // ------------------------------------------------------------- MMA issuers, a tile each
+    if (elect_one()) {
+      const int tile = warp - 16;
+      constexpr uint32_t idesc = idesc_f16_f32(128, kCols, false);
+      const uint64_t bdesc = smem_desc_sw128(smem_u32(ring), 16, 1024);
+      bool ok = true;
+      uint32_t v = 0, e = 0;  // slabs, groups
+      for (int64_t set = blockIdx.x; ok && set < sets; set += gridDim.x)
+        for (int slab = 0; ok && slab < w.slabs; ++slab, ++v) {
+          const int st = v % kFwdRing, ab = tile * 2 + (v & 1);
+          ok = mbar_wait(&b_full[st], (v / kFwdRing) & 1) && mbar_wait(&a_full[ab], (v >> 1) & 1);
+          const uint64_t slot = bdesc + (uint64_t)((st * kSlabBytes<NB>) >> 4);
 #pragma unroll
-              for (int k = 0; k < 2 * kWords; ++k) {
-                const int kk = h * 2 * kWords + k;  // 16 columns of the slab
-                mma_bf16_ts(d, c + k * 8, slot + (uint64_t)(((kk >> 2) * (kCols * 128) + (kk & 3) * 32) >> 4), idesc,
-                            !first || k != 0);
-              }
-              if (h == kPerSlab - 1 && tile == 1) mma_commit(&b_empty[st]);
-              mma_commit(&a_empty[tile * 2 + (u & 1)]);
-              if (last) mma_commit(&d_full[tile * 2 + db]);
-            }
-            __syncwarp();
+          for (int g = 0; g < kGroups; ++g, ++e) {
+            const int db = tile * kSums + e % kSums;
+            if (ok && e >= kSums) ok = mbar_wait(&d_empty[db], (e / kSums - 1) & 1);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int part = 1; part >= 0; --part)  // the low parts first, on smaller sums
+#pragma unroll
+              for (int k = g * (8 / kGroups); k < (g + 1) * (8 / kGroups); ++k)  // 16 columns of the slab
+                mma_bf16_ts(tmem + kDCol + db * kDStride, tmem + kACol + ab * 64 + k * 8,
+                            slot + (uint64_t)(((k >> 2) * (2 * kCols * 128) + part * (kCols * 128) + (k & 3) * 32) >> 4), idesc,
+                            part == 0 || k != g * (8 / kGroups));
+            mma_commit(&d_full[db]);
           }
-          if (last) ++e;
+          if (ok) {
+            mma_commit(&a_empty[ab]);
+            mma_commit(&b_empty[st]);
+          }
         }
+      if (!ok) {
+        mma_commit(&drain[tile]);
+        mbar_wait(&drain[tile], 0);
       }
-    if (!ok && leader) {
-      mma_commit(drain);
-      mbar_wait(drain, 0);
     }
+    __syncwarp();
   } else {
     // ------------------- codes into tensor memory, sums out of it: warps 0-7 tile 0, 8-15 tile 1; in a tile two warps
-    // to a quarter of the lanes, which share the words and the columns of the sums
+    // to a quarter of the lanes, which take every other slab's codes and share the columns of all sums
     const int tile = warp >> 3, half = (warp >> 2) & 1;
     const bool leader = elect_one();
     const uint32_t quad = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t c_addr = tmem + quad + kACol + tile * 64 + half * 8;
-    const uint32_t d_addr = tmem + quad + kDCol + tile * kSums * kDStride;
-    uint8_t* mine = codes + warp * kCodeRing * 1024;
+    const uint32_t c_addr = tmem + quad + kACol + tile * 128 + half * 64;
+    const uint32_t d_addr = tmem + quad + kDCol + tile * 128 + half * 8 * NB;
+    uint64_t *my_full = &a_full[tile * 2 + half], *my_empty = &a_empty[tile * 2 + half];
+    uint8_t* mine = codes + warp * kCodeRing * 2048;
     const int row_in_set = tile * 128 + (warp & 3) * 32;
-    // A lane copies 16 bytes of two of the warp's 32 rows (32 bytes of a row together) and reads its own row back; the
-    // units of every other four rows are exchanged, so that eight rows' reads lie in different banks.
-    auto place = [](int row, int unit) { return row * 32 + ((unit ^ ((row >> 2) & 1)) << 4); };
+    // A lane copies 16 bytes of four of the warp's 32 rows (64 bytes of a row together) and reads its own row back; the
+    // units change places from pair to pair of rows, so that eight rows' reads lie in different banks.
+    auto place = [](int row, int unit) { return row * 64 + ((unit ^ ((row >> 1) & 3)) << 4); };
     int64_t fset = blockIdx.x;
-    int fslab = 0, fst = 0;
-    const uint32_t* src[2] = {};
-    auto aim = [&] {  // the copies' rows in set fset
+    int fslab = 0, fst = 0, st = 0;
+    const uint32_t* src[4] = {};
+    auto aim = [&] {  // the copies' rows in set fset; those past the end are the last one
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const int64_t row = min(fset * 256 + row_in_set + (lane >> 1) + 16 * q, w.n - 1);
-        src[q] = w.packed + row * w.slabs * 16 + 8 * half + 4 * (lane & 1);
+      for (int q = 0; q < 4; ++q)
+        src[q] = w.packed + min(fset * 256 + row_in_set + (lane >> 2) + 8 * q, w.n - 1) * w.slabs * 16 + 4 * (lane & 3);
+    };
+    // The warp's next slab: every other one of all that the CTA has.
+    auto forward = [&](int by) {
+      fslab += by;
+      while (fslab >= w.slabs && fset < sets) {
+        fslab -= w.slabs;
+        fset += gridDim.x;
+        aim();
       }
     };
     aim();
+    forward(half);
     auto copy = [&] {
       if (fset < sets) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const bool in = ACID_IN_BOUNDS(kSiteQ4, src[q] - w.packed + 3, w.n * w.slabs * 16);
-          cp_async<16>(mine + fst * 1024 + place((lane >> 1) + 16 * q, lane & 1), in ? src[q] : w.packed, in);
-          src[q] += 16;
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t* from = src[q] + fslab * 16;
+          const bool in = ACID_IN_BOUNDS(kSiteQ4, from - w.packed + 3, w.n * w.slabs * 16);
+          cp_async<16>(mine + fst * 2048 + place((lane >> 2) + 8 * q, lane & 3), in ? from : w.packed, in);
         }
-        if (++fslab == w.slabs) {
-          fslab = 0;
-          fset += gridDim.x;
-          aim();
-        }
+        forward(2);
       }
       cp_async_commit();
-      fst = (fst + 1) % kCodeRing;
+      fst ^= 1;
     };
-    for (int i = 0; i < kCodeRing - 1; ++i) copy();
+    copy();
+    copy();
     bool ok = true;
-    uint32_t u = 0, taken = 0;  // steps; groups whose sums were read back
-    int st = 0;
-    constexpr int kMine = (NT + 1) / 2;  // column tiles of a thread's sums: the first ones, or the rest
-    const int n_first = half * kMine;
-    uint64_t total[kMine][4];  // pairs of the row's sums
+    uint32_t v = 0, taken = 0;  // slabs; groups whose sums were read back
+    constexpr int kEarly = kGroups > kSums ? kGroups - kSums : 0;
+    uint64_t total[NB][4];  // pairs of the row's sums: half of the columns
     // Adds the oldest group's sums, whose scale is s.
     auto take = [&](float s) {
       const int db = taken % kSums;
-      ok = mbar_wait_warp(&d_full[tile * 2 + db], (taken / kSums) & 1);
+      ok = mbar_wait_warp(&d_full[tile * kSums + db], (taken / kSums) & 1);
       ++taken;
       if (!ok) return;
       tc_fence_after();
-      constexpr int kBatch = kMine < 3 ? kMine : kMine == 3 ? 3 : 2;
       const uint64_t s2 = f2_pack(s, s);
+      uint32_t r[NB][8];
 #pragma unroll
-      for (int n0 = 0; n0 < kMine; n0 += kBatch) {
-        uint32_t hi[kBatch][8], lo[kBatch][8];
+      for (int n = 0; n < NB; ++n) tmem_ld8(d_addr + db * kDStride + n * 8, r[n]);
+      tmem_wait_ld();
+      tc_fence_before();
+      arrive_warp(&d_empty[tile * kSums + db], leader);
 #pragma unroll
-        for (int n = 0; n < kBatch; ++n) {  // (an odd tile count: the last one is read twice)
-          const int c = db * kDStride + min(n_first + n0 + n, NT - 1) * 8;
-          tmem_ld8(d_addr + c, hi[n]);
-          tmem_ld8(d_addr + kHalf + c, lo[n]);
-        }
-        tmem_wait_ld();
-        if (n0 + kBatch == kMine) {
-          tc_fence_before();
-          arrive_warp(&d_empty[tile * 2 + db], leader);
-        }
+      for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int n = 0; n < kBatch; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            total[n0 + n][e] =
-                f2_fma(s2,
-                       f2_add(f2_pack(__uint_as_float(hi[n][2 * e]), __uint_as_float(hi[n][2 * e + 1])),
-                              f2_pack(__uint_as_float(lo[n][2 * e]), __uint_as_float(lo[n][2 * e + 1]))),
-                       total[n0 + n][e]);
-      }
+        for (int e = 0; e < 4; ++e)
+          total[n][e] = f2_fma(s2, f2_pack(__uint_as_float(r[n][2 * e]), __uint_as_float(r[n][2 * e + 1])), total[n][e]);
     };
     for (int64_t set = blockIdx.x; ok && set < sets; set += gridDim.x) {
 #pragma unroll
-      for (int n = 0; n < kMine; ++n)
+      for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) total[n][e] = 0;
       const int64_t row = set * 256 + row_in_set + lane, at = min(row, w.n - 1) * w.groups;
@@ -339,62 +329,69 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
         }
       };
       look(0);
-      float scale = 0.f;  // of the group whose sums are not taken yet
-      for (int slab = 0; ok && slab < w.slabs; ++slab) {
-        cp_async_wait<kCodeRing - 2>();
-        __syncwarp();
-        uint4 q[2];  // words of the columns 32 i + 16 half + 8 c
-#pragma unroll
-        for (int c = 0; c < 2; ++c) q[c] = *reinterpret_cast<const uint4*>(mine + st * 1024 + place(lane, c));
-        copy();
-        st = (st + 1) % kCodeRing;
-        float s[kGroups];
+      float s[kGroups] = {};
+      for (int slab = 0; ok && slab < w.slabs; ++slab, ++v) {
+        float before[kGroups];  // the scales of the slab whose sums are not taken yet
         uint32_t z1[kGroups], z64[kGroups];
 #pragma unroll
         for (int i = 0; i < kGroups; ++i) {
           const uint32_t z = (w.zeros != nullptr ? zeros[i] & 15u : 8u) * 0x00010001u;
+          before[i] = s[i];
           s[i] = scales[i];
           z1[i] = 0x64006400u | z;
           z64[i] = 0x54005400u | z << 4;
         }
         if (slab + 1 < w.slabs) look(slab + 1);
+        // the sums of the slab before, while this one's are formed: the groups whose buffers that slab's others wait for
+        // come ahead of the codes
+        if (slab > 0)
 #pragma unroll
-        for (int h = 0; h < kPerSlab; ++h) {
-          if (u >= 2 && ok) ok = mbar_wait_warp(&a_empty[tile * 2 + (u & 1)], ((u >> 1) - 1) & 1);
-          const int of = (h * kWords) >> (LOG - 5);
+          for (int i = 0; i < kEarly; ++i)
+            if (ok) take(before[i]);
+        if (!ok) break;
+        if ((v & 1) == half) {
+          cp_async_wait<kCodeRing - 1>();
+          __syncwarp();
+          uint4 q[4];  // words of the columns 32 i + 8 c
 #pragma unroll
-          for (int word = 0; word < kWords; ++word) {
-            const int i = h * kWords + word;
-            uint32_t d[8];
+          for (int c = 0; c < 4; ++c) q[c] = *reinterpret_cast<const uint4*>(mine + st * 2048 + place(lane, c));
+          __syncwarp();
+          copy();
+          st ^= 1;
+          if (v >= 2) ok = mbar_wait_warp(my_empty, ((v >> 1) - 1) & 1);
+          if (!ok) break;
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
+          for (int i = 0; i < 4; ++i) {
+            const int of = i >> (LOG - 5);
+            uint32_t d[16];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
               uint32_t x[4];
               halves_of(i == 0 ? q[c].x : i == 1 ? q[c].y : i == 2 ? q[c].z : q[c].w, z1[of], z64[of], x);
 #pragma unroll
               for (int j = 0; j < 4; ++j) d[4 * c + j] = x[j];
             }
-            if (ok) tmem_st8(c_addr + (u & 1) * 32 + word * 16, d);
+            tmem_st16(c_addr + i * 16, d);
           }
           tmem_wait_st();
           tc_fence_before();
-          arrive_warp(&a_full[tile * 2 + (u & 1)], leader);
-          ++u;
-          // the sums of the group before, while this one's are formed
-          if (h % kSteps == 0) {
-            if (ok && (h > 0 || slab > 0)) take(scale);
-            scale = s[of];
-          }
+          arrive_warp(my_full, leader);
         }
+        if (slab > 0)
+#pragma unroll
+          for (int i = kEarly; i < kGroups; ++i)
+            if (ok) take(before[i]);
       }
-      if (ok) take(scale);
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i)
+        if (ok) take(s[i]);
       if (!ok || row >= w.n) continue;
       const float bias = a.bias != nullptr ? a.bias[row] : 0.f;
 #pragma unroll
-      for (int n = 0; n < kMine; ++n)
+      for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int64_t m = m0 + 8 * (n_first + n) + 2 * e;
-          if (n_first + n >= NT) continue;
+          const int64_t m = m0 + 8 * (half * NB + n) + 2 * e;
           float x, y;
           f2_unpack(total[n][e], x, y);
           if (m < a.m) put_value(a.out_dtype, a.out, m * a.ldo + row, fmaf(x, a.back[m], bias));
@@ -758,30 +755,27 @@ __global__ void __launch_bounds__(128) q4_backward_join_kernel(Q4Bwd a) {
 }
 
 // --------------------------------------------------------------------- host
-// Column tiles of eight that the product's kernel is built for.
-int tiles_for(int64_t m) {
-  const int nt = (int)((std::min<int64_t>(m, kQ4Chunk) + 7) / 8);
-  return nt <= 2 ? nt : nt <= 5 ? 5 : 8;
-}
+// Sixteens of rows of x that the product's kernel takes at a time.
+int sixteens_of(int64_t m) { return (int)((std::min<int64_t>(m, kQ4Chunk) + 15) / 16); }
 int64_t chunks_of(int64_t m) { return (m + kQ4Chunk - 1) / kQ4Chunk; }
 
-template <int NT, int LOG>
+template <int NB, int LOG>
 acid_status launch_forward(const Q4Fwd& a, int scale_dtype, cudaStream_t s) {
   static PerContext allowed;
-  ACID_TRY(allow_smem(allowed, q4_rows_forward_kernel<NT, LOG>, kFwdSmem<NT>));
+  ACID_TRY(allow_smem(allowed, q4_rows_forward_kernel<NB, LOG>, kFwdSmem<NB>));
   const int64_t sets = (a.w.n + 255) / 256;
   const dim3 grid((unsigned)std::min<int64_t>(sets, num_sms()), (unsigned)chunks_of(a.m));
-  launch_pdl(q4_rows_forward_kernel<NT, LOG>, grid, kRowsThreads, kFwdSmem<NT>, s, a, scale_dtype);
+  launch_pdl(q4_rows_forward_kernel<NB, LOG>, grid, kRowsThreads, kFwdSmem<NB>, s, a, scale_dtype);
   ACID_CHECK_LAUNCH();
   return ACID_OK;
 }
-template <int NT>
+template <int NB>
 acid_status launch_forward(const Q4Fwd& a, int scale_dtype, cudaStream_t s) {
-  launch_pdl(q4_parts_kernel<NT>, (unsigned)a.m, kThreads, 0, s, a);
+  launch_pdl(q4_parts_kernel<NB>, (unsigned)a.m, kThreads, 0, s, a);
   ACID_CHECK_LAUNCH();
-  return a.w.group_log == 5   ? launch_forward<NT, 5>(a, scale_dtype, s)
-         : a.w.group_log == 6 ? launch_forward<NT, 6>(a, scale_dtype, s)
-                              : launch_forward<NT, 7>(a, scale_dtype, s);
+  return a.w.group_log == 5   ? launch_forward<NB, 5>(a, scale_dtype, s)
+         : a.w.group_log == 6 ? launch_forward<NB, 6>(a, scale_dtype, s)
+                              : launch_forward<NB, 7>(a, scale_dtype, s);
 }
 
 template <Values KIND, int LOG>
@@ -826,18 +820,18 @@ BackSpace back_space(const Q4& w, int64_t m) {
 }  // namespace
 
 size_t q4_rows_parts_bytes(const Q4& w, int64_t m) {
-  return (size_t)chunks_of(m) * w.slabs * tiles_for(m) * kSlabBytes<1>;
+  return (size_t)chunks_of(m) * w.slabs * sixteens_of(m) * kSlabBytes<1>;
 }
 size_t q4_rows_forward_bytes(const Q4& w, int64_t m) { return q4_rows_parts_bytes(w, m) + (size_t)m * sizeof(float); }
 
 acid_status q4_rows_forward(Q4Fwd a, void* workspace, int scale_dtype, cudaStream_t s) {
   a.parts = static_cast<uint8_t*>(workspace);
   a.back = reinterpret_cast<float*>(a.parts + q4_rows_parts_bytes(a.w, a.m));
-  switch (tiles_for(a.m)) {
+  switch (sixteens_of(a.m)) {
     case 1: return launch_forward<1>(a, scale_dtype, s);
     case 2: return launch_forward<2>(a, scale_dtype, s);
-    case 5: return launch_forward<5>(a, scale_dtype, s);
-    default: return launch_forward<8>(a, scale_dtype, s);
+    case 3: return launch_forward<3>(a, scale_dtype, s);
+    default: return launch_forward<4>(a, scale_dtype, s);
   }
 }
 
