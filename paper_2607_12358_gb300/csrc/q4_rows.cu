@@ -71,11 +71,10 @@ __device__ __forceinline__ void scaled_halves(uint32_t word, uint32_t z1, uint32
     }
   }
 }
-// sh and sl of a scale after its power of two, each in both halves.
-__device__ __forceinline__ void split_scale(float s, uint32_t& sh, uint32_t& sl) {
+// sh and, in the upper half, sl of a scale after its power of two.
+__device__ __forceinline__ uint32_t split_scale(float s) {
   const __half h = __float2half_rn(s);
-  sh = bits(__half2half2(h));
-  sl = bits(__half2half2(__float2half_rn(s - __half2float(h))));
+  return bits(__halves2half2(h, __float2half_rn(s - __half2float(h))));
 }
 // The power of two that brings the largest scale, `top` in bits, to 2^10 .. 2^11 (2^127
 // at most): values below 2^15, and what is left of them far above a half's least.
@@ -415,16 +414,21 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
 // each, are written to shared memory, where they are the second operand as they lie
 // (columns together).  A block's sums are read back and added up in fp32, as in the
 // product, while the next block's are formed.
-//   Bound by shared memory: a block's values are 64 KB written and 64 KB read, 1024
-// clocks.
-constexpr int kBackThreads = 576;  // 16 warps that make operands and read sums, an MMA warp and a copying warp
+//   A block's values are 64 KB written to shared memory and 64 KB read, and its MMAs take
+// 1024 clocks; the instructions that make the values and the chain of waits around them
+// bound it, at about twice that: 34 rows, 18432 x 3072, groups of 64 with fp32 scales and
+// zero points 43 us, 36864 x 3072, groups of 128 with bf16 scales 55 us; one row, 9216 x
+// 1536 13 us with the kernels before and after it.  (The scales, a line of memory to each
+// row, loaded by the warps that use them: 47 and 69 us.)
+constexpr int kBackThreads = 640;  // 16 warps that make operands and read sums, one for MMAs, one for g's parts, two for scales
 constexpr int kBackRing = 3;  // blocks of a warp's eight rows of codes
 struct BackSmem {
   static constexpr int kPart = 128 * 256;    // [box of 64 columns][128 rows][128 bytes]
   static constexpr int kBuffer = 2 * kPart;  // high, low
   static constexpr int kParts = 16 * 2 * kQ4Chunk * 16;  // a block of g's parts
   static constexpr int kOffParts = 2 * kBuffer, kOffCodes = kOffParts + 2 * kParts;
-  static constexpr int kOffBar = kOffCodes + 16 * kBackRing * 512, kBytes = kOffBar + 256 + 1024;
+  static constexpr int kOffScales = kOffCodes + 16 * kBackRing * 512;  // of two blocks
+  static constexpr int kOffBar = kOffScales + 2 * 128 * 4 * 8, kBytes = kOffBar + 256 + 1024;
 };
 constexpr int kTopRuns = 8;  // parts of a share's scales that are scanned by a CTA each
 
@@ -513,9 +517,9 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
   using L = BackSmem;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kOffBar);
-  uint64_t *full = bars, *empty = bars + 2, *d_empty = bars + 4, *p_full = bars + 6, *p_empty = bars + 8;  // [buffer]
-  uint64_t* drain = bars + 10;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 11);
+  uint64_t *full = bars, *empty = bars + 2, *d_empty = bars + 4, *p_full = bars + 6, *p_empty = bars + 8, *s_full = bars + 10;  // [buffer]
+  uint64_t* drain = bars + 12;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 13);
   const Q4& w = a.w;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -525,6 +529,7 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
       mbar_init(&d_empty[i], 16);
       mbar_init(&p_full[i], 1);
       mbar_init(&p_empty[i], 16);
+      mbar_init(&s_full[i], 2);
     }
     mbar_init(drain, 1);
     mbar_fence_init();
@@ -560,6 +565,48 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
       // after a wait ran out: the last copies have landed before the CTA leaves
       if (b < blocks)
         for (int j = b > 2 ? b - 2 : 0; j < b; ++j) mbar_wait(&p_full[j & 1], (j >> 1) & 1);
+    }
+  } else if (warp >= 18) {
+    // ------------------- a block's scales in their two halves, and its zero points: half of the rows to a warp, a lane has
+    // one of the slab's groups, two blocks ahead in its registers
+    constexpr int kMine = 2 * kGroups, kApart = 32 / kGroups;  // rows of a lane, and between them
+    struct Look {
+      float s[kMine];
+      uint8_t z[kMine];
+    };
+    const int64_t apart = (int64_t)kApart * w.groups;
+    int64_t row = begin + (warp - 18) * 64 + lane / kGroups;
+    int64_t at = row * w.groups + min(slab * kGroups + lane % kGroups, w.groups - 1);
+    auto look = [&](Look& l) {  // the next block's
+#pragma unroll
+      for (int j = 0; j < kMine; ++j) {
+        const int64_t p = row + j * kApart < w.n ? at + j * apart : 0;  // rows past the end: any
+        if (!ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.groups)) continue;
+        l.s[j] = io<TS>::ld(static_cast<const TS*>(w.scales) + p);
+        if (KIND != kOneHalf && w.zeros != nullptr) l.z[j] = w.zeros[p];
+      }
+      row += 128;
+      at += (int64_t)128 * w.groups;
+    };
+    uint2* to = reinterpret_cast<uint2*>(smem + L::kOffScales) + (warp - 18) * 64 * kGroups + lane;
+    bool ok = true;
+    auto put = [&](Look& l, int b) {
+      // (the block before last has been read when its values are there)
+      if (b >= 2) ok = mbar_wait_warp(&full[b & 1], ((b >> 1) - 1) & 1);
+      if (!ok) return;
+#pragma unroll
+      for (int j = 0; j < kMine; ++j)
+        to[(b & 1) * 128 * kGroups + 32 * j] =
+            make_uint2(split_scale(l.s[j] * one), KIND != kOneHalf && w.zeros != nullptr ? l.z[j] & 15u : 8u);
+      if (b + 2 < blocks) look(l);
+      arrive_warp(&s_full[b & 1], lane == 0);
+    };
+    Look l[2];
+    look(l[0]);
+    if (blocks > 1) look(l[1]);
+    for (int b = 0; ok && b < blocks; b += 2) {
+      put(l[0], b);
+      if (ok && b + 1 < blocks) put(l[1], b + 1);
     }
   } else if (warp == 16) {
     // ------------------------------------------------------------- MMA issuer
@@ -597,35 +644,24 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
     const uint32_t quad = (uint32_t)((warp & 3) * 32) << 16;
     uint8_t* mine = smem + L::kOffCodes + warp * kBackRing * 512;
     // a lane's own 16 bytes of its row, some blocks ahead
-    auto row_of = [&](int b) { return min(begin + b * 128 + warp * 8 + g, w.n - 1); };
+    int64_t crow = begin + warp * 8 + g;
+    const uint32_t* src = w.packed + (crow * w.slabs + slab) * 16 + 4 * t;
+    const int64_t src_step = (int64_t)128 * 16 * w.slabs;
     int fetched = 0, fst = 0;
     auto copy = [&] {
       if (fetched < blocks) {
-        const int64_t at = (row_of(fetched) * w.slabs + slab) * 16 + 4 * t;
-        const bool in = ACID_IN_BOUNDS(kSiteQ4, at + 3, w.n * w.slabs * 16);
-        cp_async<16>(mine + fst * 512 + lane * 16, w.packed + (in ? at : 0), in);
+        // (rows past the end, against parts of zero, are the first one)
+        const uint32_t* from = crow < w.n ? src : w.packed;
+        const bool in = ACID_IN_BOUNDS(kSiteQ4, from - w.packed + 3, w.n * w.slabs * 16);
+        cp_async<16>(mine + fst * 512 + lane * 16, in ? from : w.packed, in);
+        crow += 128;
+        src += src_step;
         ++fetched;
       }
       cp_async_commit();
       fst = fst + 1 == kBackRing ? 0 : fst + 1;
     };
     for (int i = 0; i < kBackRing - 1; ++i) copy();
-    // its scales and zero points, two blocks ahead
-    struct Look {
-      float s[kGroups];
-      uint8_t z[kGroups];
-    };
-    auto look = [&](Look& l, int b) {
-      if (b >= blocks) return;
-      const int64_t at = row_of(b) * w.groups;
-#pragma unroll
-      for (int v = 0; v < kGroups; ++v) {
-        const int64_t p = at + min(slab * kGroups + v, w.groups - 1);
-        if (!ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.groups)) continue;
-        l.s[v] = io<TS>::ld(static_cast<const TS*>(w.scales) + p);
-        if (KIND != kOneHalf && w.zeros != nullptr) l.z[v] = w.zeros[p];
-      }
-    };
     bool ok = true;
     int st = 0;
     uint64_t total[16];  // pairs of a quarter of the slab's columns
@@ -647,7 +683,7 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
       tc_fence_before();
       arrive_warp(&d_empty[b & 1], leader);
     };
-    auto block = [&](Look& l, int b) {
+    auto block = [&](int b) {
       const int i = b & 1;
       if (b >= 2) take(b - 2);  // the tensor cores are done with these buffers
       if (ok) ok = mbar_wait_warp(&p_full[i], (b >> 1) & 1);
@@ -672,14 +708,16 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
       st = st + 1 == kBackRing ? 0 : st + 1;
       copy();
       uint32_t sh[kGroups], sl[kGroups], z1[kGroups], z64[kGroups];
+      ok = mbar_wait_warp(&s_full[i], (b >> 1) & 1);
+      if (!ok) return;
 #pragma unroll
       for (int v = 0; v < kGroups; ++v) {
-        split_scale(l.s[v] * one, sh[v], sl[v]);
-        const uint32_t z = (KIND != kOneHalf && w.zeros != nullptr ? l.z[v] & 15u : 8u) * 0x00010001u;
-        z1[v] = 0x64006400u | z;
-        z64[v] = 0x54005400u | z << 4;
+        const uint2 x = reinterpret_cast<const uint2*>(smem + L::kOffScales)[(i * 128 + warp * 8 + g) * kGroups + v];
+        sh[v] = __byte_perm(x.x, 0, 0x1010);
+        sl[v] = __byte_perm(x.x, 0, 0x3232);
+        z1[v] = 0x64006400u | x.y * 0x00010001u;
+        z64[v] = 0x54005400u | x.y * 0x00100010u;
       }
-      look(l, b + 2);
       // neighbouring rows take their words in another order, so that their units lie in different banks
       const uint4 v = odd ? make_uint4(q.y, q.x, q.w, q.z) : q;
       const int row = warp * 8 + g;
@@ -703,13 +741,7 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
       fence_proxy_async_smem();
       arrive_warp(&full[i], leader);
     };
-    Look l[2];
-    look(l[0], 0);
-    look(l[1], 1);
-    for (int b = 0; ok && b < blocks; b += 2) {
-      block(l[0], b);
-      if (ok && b + 1 < blocks) block(l[1], b + 1);
-    }
+    for (int b = 0; ok && b < blocks; ++b) block(b);
     cp_async_wait<0>();
     if (ok && blocks > 1) take(blocks - 2);
     if (ok) take(blocks - 1);
