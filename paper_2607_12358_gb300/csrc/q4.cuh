@@ -48,7 +48,6 @@ struct Q4Fwd {
   uint8_t* parts;  // past a few rows: the parts as the tensor cores read them
   float* back;     // [m], and the powers of two taken back
   int kw;          // few rows: warps of a CTA that share a row's columns
-  bool wide;       // codes on a 32-byte boundary
 };
 // The power of two that brings `top` to 2^13 .. 2^14 (2^127 at most).
 __device__ __forceinline__ float up_to_half(float top) {

@@ -17,7 +17,6 @@ namespace {
 
 using bf16 = __nv_bfloat16;
 constexpr int kThreads = 256;
-constexpr int kRowsThreads = 608;  // product: 16 warps that make operands, two MMA warps and a copying warp
 
 // Instruction descriptor of kind::f16 with fp16 A and B, fp32 accumulator.
 __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool b_mn) {
@@ -35,6 +34,9 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+// Lets the next kernel's CTAs start beside this one's (they wait for its end before they
+// read): for a kernel that leaves most SMs free.
+__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;"); }
 // One arrival for the warp, after what all its lanes did.
 __device__ __forceinline__ void arrive_warp(uint64_t* bar, bool leader) {
   __syncwarp();
@@ -92,13 +94,13 @@ __device__ __forceinline__ uint32_t finite_bits(float v) { return isfinite(v) ? 
 // value in two halves, would spare that only where sums may stay in tensor memory: the
 // tensor cores' sums lose up to 2^-23 of themselves at each addition, always towards
 // zero, 1.7e-4 over 65536 columns.  It costs more instructions and twice the MMAs.)
-//   A CTA has two tiles of 128 rows.  Each of their lanes belongs to two threads, which
-// take the codes of every other slab of 128 columns (with half of each slab's the same
-// waits and fences came twice as often) and half of the columns of all sums.  The
+//   A CTA has two tiles of 128 rows, or one.  Each of their lanes belongs to two threads,
+// which take the codes of every other slab of 128 columns (with half of each slab's the
+// same waits and fences came twice as often) and half of the columns of all sums.  The
 // chain of waits from a slab's codes to its sums bounds it, then the instructions that
-// make the operands: 36864 x 3072, groups of 128, 34 rows 29 us, of which the MMAs by
-// themselves are 20; groups of 64 36 us, of 32 59 us; 8 rows 26 us.  (One thread issuing
-// for both tiles in steps of 64 columns: 37 us.)
+// make the operands.  34 rows, 36864 x 3072: groups of 128 27 us (35% of a copy's rate), of
+// 64 33 us, of 32 56 us; 8 rows 23 us; 18432 x 3072, groups of 64 22 us.  (One thread
+// issuing for both tiles in steps of 64 columns, two tiles always: 37, 44, 75, 32, 43 us.)
 constexpr int kFwdRing = 4;   // slabs of parts in shared memory
 constexpr int kCodeRing = 2;  // a warp's slabs of its 32 rows of codes
 // Bytes of a slab's parts: two boxes of 64 columns, rows of 128 bytes whose
@@ -107,25 +109,29 @@ template <int NB>
 constexpr int kSlabBytes = 32 * NB * 256;
 template <int NB>
 constexpr int kFwdSmem = kFwdRing * kSlabBytes<NB> + 16 * kCodeRing * 2048 + 512 + 1024;
+// Of a CTA with so many tiles: to each eight warps that make operands and one for MMAs; one that copies parts.
+constexpr int fwd_threads(int tiles) { return (9 * tiles + 1) * 32; }
 
 // One CTA to a row of a(x).
+constexpr int kPartThreads = 512;
 template <int NB>
-__global__ void __launch_bounds__(kThreads) q4_parts_kernel(Q4Fwd a) {
+__global__ void __launch_bounds__(kPartThreads) q4_parts_kernel(Q4Fwd a) {
   __shared__ uint32_t largest;
   pdl_wait();
+  pdl_trigger();
   const int64_t m = blockIdx.x, chunk = m / kQ4Chunk;
   const int n = (int)(m - chunk * kQ4Chunk), octets = a.w.slabs * 16;
   if (threadIdx.x == 0) largest = 0;
   __syncthreads();
   float v[8], top = 0.f;
-  for (int o = threadIdx.x; o < octets; o += kThreads) top = fmaxf(top, octet_values(a, m, o * 8, v));
+  for (int o = threadIdx.x; o < octets; o += kPartThreads) top = fmaxf(top, octet_values(a, m, o * 8, v));
   const uint32_t t = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
   if ((threadIdx.x & 31) == 0) atomicMax(&largest, t);
   __syncthreads();
   const float by = up_to_half(__uint_as_float(largest));
   if (threadIdx.x == 0) a.back[m] = 1.f / by;
-  for (int o = threadIdx.x; o < octets; o += kThreads) {
-    if (octets > kThreads) octet_values(a, m, o * 8, v);  // (else they are still there)
+  for (int o = threadIdx.x; o < octets; o += kPartThreads) {
+    if (octets > kPartThreads) octet_values(a, m, o * 8, v);  // (else they are still there)
     uint4 hi, lo;
     split_octet(v, by, hi, lo);
     const int slab = o >> 4, word = (o >> 2) & 3, unit = (word & 1) * 4 + (o & 3);
@@ -136,8 +142,8 @@ __global__ void __launch_bounds__(kThreads) q4_parts_kernel(Q4Fwd a) {
   }
 }
 
-template <int NB, int LOG>
-__global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd a, int scale_dtype) {
+template <int NB, int LOG, int TILES>
+__global__ void __launch_bounds__(fwd_threads(TILES), 1) q4_rows_forward_kernel(Q4Fwd a, int scale_dtype) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* ring = smem;
@@ -158,7 +164,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kFwdRing; ++i) {
       mbar_init(&b_full[i], 1);
-      mbar_init(&b_empty[i], 2);
+      mbar_init(&b_empty[i], TILES);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(&a_full[i], 4);
@@ -172,17 +178,18 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
     mbar_init(&drain[1], 1);
     mbar_fence_init();
   }
-  if (warp == 16) tmem_alloc(tmem_slot, 512);
+  if (warp == 8 * TILES) tmem_alloc(tmem_slot, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   pdl_wait();
 
-  const int64_t sets = (w.n + 255) / 256, chunk = blockIdx.y, m0 = chunk * kQ4Chunk;
+  constexpr int kSetRows = 128 * TILES;
+  const int64_t sets = (w.n + kSetRows - 1) / kSetRows, chunk = blockIdx.y, m0 = chunk * kQ4Chunk;
   const uint8_t* parts = a.parts + chunk * w.slabs * kSlabBytes<NB>;
 
-  if (warp == 18) {
+  if (warp == 9 * TILES) {
     if (lane == 0) {  // ------------------------------------------ copies of the parts
       int issued = 0;
       bool ok = true;
@@ -198,10 +205,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
         for (int j = issued > kFwdRing ? issued - kFwdRing : 0; j < issued; ++j)
           mbar_wait(&b_full[j % kFwdRing], (j / kFwdRing) & 1);
     }
-  } else if (warp >= 16) {
+  } else if (warp >= 8 * TILES) {
     // ------------------------------------------------------------- MMA issuers, a tile each
     if (elect_one()) {
-      const int tile = warp - 16;
+      const int tile = warp - 8 * TILES;
       constexpr uint32_t idesc = idesc_f16_f32(128, kCols, false);
       const uint64_t bdesc = smem_desc_sw128(smem_u32(ring), 16, 1024);
       bool ok = true;
@@ -257,7 +264,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
     auto aim = [&] {  // the copies' rows in set fset; those past the end are the last one
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        src[q] = w.packed + min(fset * 256 + row_in_set + (lane >> 2) + 8 * q, w.n - 1) * w.slabs * 16 + 4 * (lane & 3);
+        src[q] = w.packed + min(fset * kSetRows + row_in_set + (lane >> 2) + 8 * q, w.n - 1) * w.slabs * 16 + 4 * (lane & 3);
     };
     // The warp's next slab: every other one of all that the CTA has.
     auto forward = [&](int by) {
@@ -314,7 +321,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
       for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) total[n][e] = 0;
-      const int64_t row = set * 256 + row_in_set + lane, at = min(row, w.n - 1) * w.groups;
+      const int64_t row = set * kSetRows + row_in_set + lane, at = min(row, w.n - 1) * w.groups;
       // scales and zero points of a slab's groups, a slab ahead
       float scales[kGroups];
       uint8_t zeros[kGroups];
@@ -401,7 +408,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) q4_rows_forward_kernel(Q4Fwd 
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 16) {
+  if (warp == 8 * TILES) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
@@ -791,19 +798,26 @@ __global__ void __launch_bounds__(128) q4_backward_join_kernel(Q4Bwd a) {
 int sixteens_of(int64_t m) { return (int)((std::min<int64_t>(m, kQ4Chunk) + 15) / 16); }
 int64_t chunks_of(int64_t m) { return (m + kQ4Chunk - 1) / kQ4Chunk; }
 
-template <int NB, int LOG>
+template <int NB, int LOG, int TILES>
 acid_status launch_forward(const Q4Fwd& a, int scale_dtype, cudaStream_t s) {
   static PerContext allowed;
-  ACID_TRY(allow_smem(allowed, q4_rows_forward_kernel<NB, LOG>, kFwdSmem<NB>));
-  const int64_t sets = (a.w.n + 255) / 256;
+  ACID_TRY(allow_smem(allowed, q4_rows_forward_kernel<NB, LOG, TILES>, kFwdSmem<NB>));
+  const int64_t sets = (a.w.n + 128 * TILES - 1) / (128 * TILES);
   const dim3 grid((unsigned)std::min<int64_t>(sets, num_sms()), (unsigned)chunks_of(a.m));
-  launch_pdl(q4_rows_forward_kernel<NB, LOG>, grid, kRowsThreads, kFwdSmem<NB>, s, a, scale_dtype);
+  launch_pdl(q4_rows_forward_kernel<NB, LOG, TILES>, grid, fwd_threads(TILES), kFwdSmem<NB>, s, a, scale_dtype);
   ACID_CHECK_LAUNCH();
   return ACID_OK;
 }
+// One tile to a CTA where every tile has an SM to itself (34 rows, 4608 x 3072, groups of
+// 64: 21 us, with two tiles 32), else two (36864 x 3072, groups of 128 27 us, one by one 33).
+template <int NB, int LOG>
+acid_status launch_forward(const Q4Fwd& a, int scale_dtype, cudaStream_t s) {
+  return (a.w.n + 127) / 128 <= num_sms() ? launch_forward<NB, LOG, 1>(a, scale_dtype, s)
+                                          : launch_forward<NB, LOG, 2>(a, scale_dtype, s);
+}
 template <int NB>
 acid_status launch_forward(const Q4Fwd& a, int scale_dtype, cudaStream_t s) {
-  launch_pdl(q4_parts_kernel<NB>, (unsigned)a.m, kThreads, 0, s, a);
+  launch_pdl(q4_parts_kernel<NB>, (unsigned)a.m, kPartThreads, 0, s, a);
   ACID_CHECK_LAUNCH();
   return a.w.group_log == 5   ? launch_forward<NB, 5>(a, scale_dtype, s)
          : a.w.group_log == 6 ? launch_forward<NB, 6>(a, scale_dtype, s)
