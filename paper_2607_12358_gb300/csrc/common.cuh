@@ -201,6 +201,9 @@ constexpr bool kBoundsChecked = false;
 // ---------------------------------------------------------------------------
 // Waits until the kernel before this one has completed.
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Lets the next kernel's CTAs start beside this one's (they wait for its end before they
+// read): where that kernel is small, or this one leaves most SMs free.
+__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;"); }
 
 // ---------------------------------------------------------------------------
 // Numeric helpers

@@ -34,9 +34,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
-// Lets the next kernel's CTAs start beside this one's (they wait for its end before they
-// read): for a kernel that leaves most SMs free.
-__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;"); }
 // One arrival for the warp, after what all its lanes did.
 __device__ __forceinline__ void arrive_warp(uint64_t* bar, bool leader) {
   __syncwarp();

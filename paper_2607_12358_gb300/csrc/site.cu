@@ -441,8 +441,9 @@ __device__ __forceinline__ void put_sums(const SiteBwd& a, int which, int64_t g,
 // CTA's slot 2 b (the group began earlier) or 2 b + 1 (it begins here), and
 // site_join_kernel adds the slots.  A row's four sums go together, so that it waits for
 // the CTA two or three times.  The bytes bound it from some thousand rows on: 32760 x 1536,
-// fp32 stream, bf16 branch 170 us (79% of a copy's rate); 226 x 1920 13 us with the
-// second kernel, of which the launches' and the sums' latency is nearly all.
+// fp32 stream, bf16 branch, a group of 1560 rows 145 us (92% of a copy's rate), with the
+// second kernel 155; 226 x 1920 5 and 12.6 us, of which the launches' and the sums'
+// latency is nearly all.
 constexpr int kBwdStages = 3;
 template <typename TS, typename TB, int V>
 __global__ void __launch_bounds__(kMostThreads<V>, V == 1 ? 12 : 1) site_backward_kernel(SiteBwd a) {
@@ -594,32 +595,42 @@ __global__ void __launch_bounds__(kMostThreads<V>, V == 1 ? 12 : 1) site_backwar
   }
 }
 
-// Adds the CTAs' slots in the CTAs' order.  A job is one vector of one group
-// that reaches over an edge (jobs counted by groups, or by CTAs where these are
-// fewer: the group that begins in the CTA and leaves it), or one of the two
-// weights' gradients.  `segs` warps share a job's slots, a lane takes a column.
+// Adds the CTAs' slots in the CTAs' order.  A job is one vector of one group that
+// reaches over an edge (counted by groups, or by CTAs where these are fewer: the
+// group that begins in the CTA and leaves it), or one of the two weights' gradients.
+// `segs` warps share a job's slots, a lane takes a column.  The groups' jobs come first,
+// in `ctas_v` CTAs down the grid, and share by the CTAs that a group reaches over; the
+// weights' by all CTAs.  (As many warps for each group's as for the weights': 700 rows of
+// 1536, each its own group, 170 us in all, now 19.)
 constexpr int kJoinWarps = 16;
-__global__ void __launch_bounds__(32 * kJoinWarps) site_join_kernel(SiteBwd a, int ctas, int jobs, int segs,
-                                                                   bool by_cta) {
+struct Join {
+  int jobs, segs;  // of each vector
+  int ctas_v, segs_w;
+  int ctas;        // of site_backward_kernel
+  bool by_cta;
+};
+__global__ void __launch_bounds__(32 * kJoinWarps) site_join_kernel(SiteBwd a, Join n) {
   __shared__ float part[kJoinWarps][32];
   pdl_wait();
   const Site& s = a.s;
+  const bool rows = blockIdx.y < n.ctas_v;
+  const int segs = rows ? n.segs : n.segs_w, y = rows ? blockIdx.y : blockIdx.y - n.ctas_v;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, seg = warp % segs;
-  const int c = blockIdx.x * 32 + lane, d = s.d, job = blockIdx.y * (kJoinWarps / segs) + warp / segs;
-  const int which = job / jobs;  // 0 .. 2: dshift, dscale, dgate; 3, 4: dpre_w, dpost_w
+  const int c = blockIdx.x * 32 + lane, d = s.d, job = y * (kJoinWarps / segs) + warp / segs;
+  const int which = rows ? job / n.jobs : 3 + job;  // 0 .. 2: dshift, dscale, dgate; 3, 4: dpre_w, dpost_w
   int64_t g = 0, lo = 0, hi = -1;  // slots lo .. hi
   if (which < 3) {
-    const int64_t i = job - which * jobs;
-    g = by_cta ? group_of(s, min(s.rows, (i + 1) * a.per) - 1) : i;
+    const int64_t i = job - which * n.jobs;
+    g = n.by_cta ? group_of(s, min(s.rows, (i + 1) * a.per) - 1) : i;
     lo = group_begin(s, g) / a.per;
     hi = (group_end(s, g) - 1) / a.per;
-    if (lo == hi || (by_cta && lo != i)) hi = lo - 1;  // finished by its CTA, or another job's
-  } else if (job - 3 * jobs < 2) {
-    hi = ctas - 1;
+    if (lo == hi || (n.by_cta && lo != i)) hi = lo - 1;  // finished by its CTA, or another job's
+  } else if (!rows && which < 5) {
+    hi = n.ctas - 1;
   }
   float v = 0.f;
   if (c < d) {
-    const float* base = which < 3 ? a.part + which * d : a.wpart + (job - 3 * jobs) * d;
+    const float* base = which < 3 ? a.part + which * d : a.wpart + (which - 3) * d;
     const int64_t width = which < 3 ? 6 * (int64_t)d : 2 * (int64_t)d;
 #pragma unroll 8
     for (int64_t k = lo + seg; k <= hi; k += segs)
@@ -633,7 +644,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) site_join_kernel(SiteBwd a, i
   if (which < 3) {
     put_sum(a, which, g, c, t);
   } else {
-    float* out = job - 3 * jobs == 0 ? a.dpre_w : a.dpost_w;
+    float* out = which == 3 ? a.dpre_w : a.dpost_w;
     if (out != nullptr) out[c] = t;
   }
 }
@@ -785,15 +796,21 @@ struct RunBwd {
     const bool vectors = a.dgate != nullptr || a.dscale != nullptr || a.dshift != nullptr;
     // does any group reach over an edge?
     const int64_t head = s.first > 0 ? s.first : 0, longest = std::max(head, std::min(s.group, s.rows - head));
-    if (!weights && (!vectors || (longest == 1))) return ACID_OK;
-    const bool by_cta = s.groups > ctas;
-    const int jobs = by_cta ? ctas : (int)s.groups;
-    const int64_t span = std::max<int64_t>(longest / a.per + 2, weights ? ctas : 0);
-    int segs = 1;
-    while (segs < kJoinWarps && segs * 8 < span) segs *= 2;
-    const int per_cta = kJoinWarps / segs;
-    launch_pdl(site_join_kernel, dim3((s.d + 31) / 32, (3 * jobs + 2 + per_cta - 1) / per_cta), 32 * kJoinWarps, 0, l.s, a,
-               ctas, jobs, segs, by_cta);
+    const bool over = vectors && longest > 1;
+    if (!weights && !over) return ACID_OK;
+    auto share = [](int64_t slots) {  // warps for so many slots
+      int segs = 1;
+      while (segs < kJoinWarps && segs * 8 < slots) segs *= 2;
+      return segs;
+    };
+    Join n{1, 1, 0, share(ctas), ctas, s.groups > ctas};
+    if (over) {
+      n.jobs = n.by_cta ? ctas : (int)s.groups;
+      n.segs = share(std::min<int64_t>(ctas, longest / a.per + 2));
+      n.ctas_v = (3 * n.jobs * n.segs + kJoinWarps - 1) / kJoinWarps;
+    }
+    const int ctas_w = weights ? (2 * n.segs_w + kJoinWarps - 1) / kJoinWarps : 0;
+    launch_pdl(site_join_kernel, dim3((s.d + 31) / 32, n.ctas_v + ctas_w), 32 * kJoinWarps, 0, l.s, a, n);
     ACID_CHECK_LAUNCH();
     return ACID_OK;
   }
