@@ -397,8 +397,8 @@ acid_status acid_q4_dequantize(const acid_q4_weight* weight, int32_t out_dtype, 
 
 /* out[M, N] = a(x[M, K]) W^T + bias for a few rows (timestep embeddings of the
  * branches, frames or steps), a = identity, or SiLU if silu_input.  Sums in fp32;
- * an fp32 a(x) enters the products to within 2^-22 of the largest value in
- * its 128 columns (those of one packed slab).
+ * a(x) enters the products as two halves, to within 2^-22 of the largest value
+ * of its row (without a workspace: of its 128 columns, those of one packed slab).
  *   x      device [M, K], row stride ldx, x_dtype.
  *   bias   device fp32 [N] or NULL.
  *   out    device [M, N], row stride ldo, out_dtype.
@@ -422,8 +422,13 @@ acid_status acid_q4_linear_workspace_size(const acid_q4_weight* weight, int64_t 
  *          may be NULL without silu_input.
  *   dx     device [M, K], row stride lddx, x_dtype, or NULL.
  *   dbias  device fp32 [N], or NULL.  Not both NULL.
+ * Sums in fp32.  The weight's rows are shared out among CTAs; g enters the
+ * products to within 2^-22 of its row's largest value in a share, and s (q - z)
+ * to within 2^-22 of itself, or 2^-35 of the share's largest scale where that is
+ * more (bf16 scales without zero points: exactly).
  * Deterministic, as acid_norm_site_backward.  workspace: device, 16-byte
- * aligned.  M = 0 writes zeros to dbias. */
+ * aligned, acid_q4_linear_workspace_size bytes; not used without dx.  0 <= M <=
+ * 32768; M = 0 writes zeros to dbias. */
 acid_status acid_q4_linear_backward(int32_t g_dtype, const void* g, int64_t ldg, int64_t M,
                                     const acid_q4_weight* weight, int32_t x_dtype, const void* x, int64_t ldx,
                                     int32_t silu_input, void* dx, int64_t lddx, float* dbias, void* workspace,
