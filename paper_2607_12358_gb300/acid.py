@@ -35,12 +35,13 @@ def _dtype(t: torch.Tensor) -> int:
 # The current stream's handle without building a Stream object: 0.3 us against
 # 2.9 us, a third of a small call's whole host time.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # the arguments are on a device already
 
 
 def _stream(stream=None) -> int:
     if stream is None:
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(_current_device())
         return torch.cuda.current_stream().cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
@@ -262,23 +263,17 @@ def _rows_of(name: str, t: torch.Tensor, rows: int, d: int, dtype) -> int:
     return ld[0] if rows > 1 else d
 
 
-def _group_vectors(gate, scale, shift, groups, d):
-    """(pointers, row stride) of the vectors of a site's groups."""
-    ld, ptrs = 0, []
-    for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
-        if t is None:
-            ptrs.append(None)
-            continue
-        st, shape = t.stride(), t.shape
-        if t.dtype is not _F32 or not t.is_cuda or st[-1] != 1 or not (
-                shape == (groups, d) or (groups == 1 and shape == (d,))):
-            raise ValueError(f"{name} must be a CUDA fp32 tensor [{groups}, {d}] with contiguous rows")
-        if groups > 1:
-            if ld and ld != st[0]:
-                raise ValueError("gate, scale and shift must have one row stride")
-            ld = st[0]
-        ptrs.append(t.data_ptr())
-    return ptrs, ld
+def _group_vector(name: str, t: torch.Tensor, groups: int, d: int, ld: int) -> int:
+    """Row stride of the vectors t of a site's groups; ld: that of the ones before (0: none)."""
+    st, shape = t.stride(), t.shape
+    if t.dtype is not _F32 or not t.is_cuda or st[-1] != 1 or not (
+            shape == (groups, d) or (groups == 1 and shape == (d,))):
+        raise ValueError(f"{name} must be a CUDA fp32 tensor [{groups}, {d}] with contiguous rows")
+    if groups == 1:
+        return d
+    if ld and ld != st[0]:
+        raise ValueError("gate, scale and shift must have one row stride")
+    return st[0]
 
 
 def _column_vector(name: str, t: torch.Tensor, d: int):
@@ -294,11 +289,20 @@ def _site(rows, d, stream_dtype, branch_dtype, gate, scale, shift, post_w, pre_w
     """(C descriptor of a site, its groups) after a check of the vectors' shapes."""
     if not 0 <= first_rows <= rows or group_rows < 0:
         raise ValueError("need 0 <= first_rows <= rows and group_rows >= 0")
-    groups = norm_site_groups(rows, first_rows, group_rows)
-    ptrs, ld = _group_vectors(gate, scale, shift, groups, d)
+    groups, ld = norm_site_groups(rows, first_rows, group_rows), 0
+    gp = cp = hp = ap = bp = None
+    if gate is not None:
+        ld, gp = _group_vector("gate", gate, groups, d, 0), gate.data_ptr()
+    if scale is not None:
+        ld, cp = _group_vector("scale", scale, groups, d, ld), scale.data_ptr()
+    if shift is not None:
+        ld, hp = _group_vector("shift", shift, groups, d, ld), shift.data_ptr()
+    if post_w is not None:
+        ap = _column_vector("post_w", post_w, d)
+    if pre_w is not None:
+        bp = _column_vector("pre_w", pre_w, d)
     return A.acid_norm_site(rows, d, _DT[stream_dtype], _DT[branch_dtype], _NORM[post_norm], _NORM[pre_norm],
-                            gate_tanh, eps, res_scale, branch_scale, first_rows, group_rows, ptrs[0], ptrs[1], ptrs[2],
-                            ld, _column_vector("post_w", post_w, d), _column_vector("pre_w", pre_w, d)), groups
+                            gate_tanh, eps, res_scale, branch_scale, first_rows, group_rows, gp, cp, hp, ld, ap, bp), groups
 
 
 def acid_norm_site_forward(x: torch.Tensor, y: torch.Tensor | None = None, *, gate: torch.Tensor | None = None,
@@ -447,9 +451,18 @@ class Q4Weight:
         if zeros is not None and (zeros.dtype is not torch.uint8 or not zeros.is_cuda or not zeros.is_contiguous()
                                   or zeros.numel() != number):
             raise ValueError("zeros must be a contiguous CUDA uint8 tensor [n, ceil(k / group)]")
+        self._set(packed, scales, zeros, n, k, group)
+
+    def _set(self, packed, scales, zeros, n, k, group):
         self.packed, self.scales, self.zeros, self.n, self.k, self.group = packed, scales, zeros, n, k, group
         self.struct = A.acid_q4_weight(packed.data_ptr(), scales.data_ptr(),
-                                       None if zeros is None else zeros.data_ptr(), n, k, group, _DT[sdt])
+                                       None if zeros is None else zeros.data_ptr(), n, k, group, _DT[scales.dtype])
+
+    @classmethod
+    def _of(cls, *parts):  # of tensors made here
+        self = cls.__new__(cls)
+        self._set(*parts)
+        return self
 
 
 def _matrix(name: str, t: torch.Tensor, rows: int, cols: int) -> int:
@@ -470,19 +483,31 @@ def acid_q4_quantize(w: torch.Tensor, group: int = 128, zeros: bool = False, sca
     if group not in (32, 64, 128):
         raise ValueError("group must be 32, 64 or 128")
     per_row = -(-k // group)
-    q = Q4Weight(torch.empty((n, 64 * -(-k // 128)), dtype=torch.uint8, device=w.device),
-                 torch.empty((n, per_row), dtype=scale_dtype, device=w.device),
-                 torch.empty((n, per_row), dtype=torch.uint8, device=w.device) if zeros else None, n, k, group)
-    check(load().acid_q4_quantize(_DT[w.dtype], w.data_ptr(), ld, C.byref(q.struct), _stream(stream)))
+    if scale_dtype not in _DT:
+        raise TypeError(f"unsupported dtype {scale_dtype}")
+    dev = w.device
+    packed = _empty((n, 64 * -(-k // 128)), dtype=torch.uint8, device=dev)
+    scales = _empty((n, per_row), dtype=scale_dtype, device=dev)
+    q = Q4Weight._of(packed, scales, _empty((n, per_row), dtype=torch.uint8, device=dev) if zeros else None, n, k, group)
+    status = load().acid_q4_quantize(_DT[w.dtype], w.data_ptr(), ld, C.byref(q.struct), _stream(stream))
+    if status:
+        check(status)
     return q
 
 
 def acid_q4_dequantize(weight: Q4Weight, dtype=torch.float32, out: torch.Tensor | None = None,
                        stream=None) -> torch.Tensor:
     """The weight's values s (q - z) as a [n, k] tensor."""
-    out = torch.empty((weight.n, weight.k), dtype=dtype, device=weight.packed.device) if out is None else out
-    ld = _matrix("out", out, weight.n, weight.k)
-    check(load().acid_q4_dequantize(C.byref(weight.struct), _DT[out.dtype], out.data_ptr(), ld, _stream(stream)))
+    ld = weight.k
+    if out is None:
+        if dtype not in _DT:
+            raise TypeError(f"unsupported dtype {dtype}")
+        out = _empty((weight.n, ld), dtype=dtype, device=weight.packed.device)
+    else:
+        ld = _matrix("out", out, weight.n, ld)
+    status = load().acid_q4_dequantize(C.byref(weight.struct), _DT[out.dtype], out.data_ptr(), ld, _stream(stream))
+    if status:
+        check(status)
     return out
 
 
@@ -501,7 +526,7 @@ def acid_q4_linear_forward(x: torch.Tensor, weight: Q4Weight, bias: torch.Tensor
         out_dtype = out.dtype
         ldo = _matrix("out", out, m, n)
     if workspace is None and (m > 4 or m * k > 16384):
-        workspace = _empty(q4_linear_workspace_size(weight, m), dtype=torch.uint8, device=x.device)
+        workspace = _empty(_q4_bytes(n, k, m), dtype=torch.uint8, device=x.device)
     if workspace is not None:
         ws, nws = workspace.data_ptr(), workspace.numel()
     status = load().acid_q4_linear_forward(_DT[x.dtype], x.data_ptr(), ldx, m, C.byref(weight.struct), bp, silu,
@@ -514,6 +539,13 @@ def acid_q4_linear_forward(x: torch.Tensor, weight: Q4Weight, bias: torch.Tensor
 def q4_linear_workspace_size(weight: Q4Weight, m: int) -> int:
     b = C.c_size_t()
     check(load().acid_q4_linear_workspace_size(C.byref(weight.struct), int(m), C.byref(b)))
+    return b.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _q4_bytes(n, k, m):  # the size goes by these alone
+    b = C.c_size_t()
+    check(load().acid_q4_linear_workspace_size(C.byref(A.acid_q4_weight(n=n, k=k, group=128)), m, C.byref(b)))
     return b.value
 
 
@@ -543,7 +575,7 @@ def acid_q4_linear_backward(g: torch.Tensor, weight: Q4Weight, x: torch.Tensor |
     if dx is not None:
         dxp = dx.data_ptr()
         if workspace is None:
-            workspace = _empty(q4_linear_workspace_size(weight, m), dtype=torch.uint8, device=dev)
+            workspace = _empty(_q4_bytes(n, k, m), dtype=torch.uint8, device=dev)
         ws, nws = workspace.data_ptr(), workspace.numel()
     status = load().acid_q4_linear_backward(_DT[g.dtype], g.data_ptr(), ldg, m, C.byref(weight.struct), _DT[dx_dtype], xp,
                                             ldx, silu, dxp, lddx, bp, ws, nws, _stream(stream))
