@@ -35,7 +35,7 @@ def random_weights(d: int, hidden: int, seed: int = 0, device="cuda") -> dict:
     gen = torch.Generator(device=device).manual_seed(seed)
 
     def normal(*shape, std=1.0, dtype=torch.float32):
-        return (std * torch.randn(*shape, device=device, generator=gen)).to(dtype)
+        return (std * torch.randn(*shape, device=device, dtype=torch.float32, generator=gen)).to(dtype)
 
     w = dict(mod_w=normal(6 * d, d, std=0.02), mod_b=normal(6 * d, std=0.1), w1=1 + normal(d, std=0.1),
              w2=1 + normal(d, std=0.1))
@@ -163,10 +163,13 @@ def main(argv=None):
     a = ap.parse_args(argv)
     weights = random_weights(a.d, a.hidden or 4 * a.d, a.seed)
     gen = torch.Generator(device="cuda").manual_seed(a.seed + 1)
-    x = torch.randn(a.frames * a.tokens, a.d, device="cuda", generator=gen)
+
+    def normal(*shape):
+        return torch.randn(*shape, device="cuda", dtype=torch.float32, generator=gen)
+
+    x = normal(a.frames * a.tokens, a.d)
     # embeddings of neighbouring timesteps: a common part, and a tenth of its size of their own
-    temb = torch.randn(1, a.d, device="cuda", generator=gen) + 0.1 * torch.randn(a.frames, a.d, device="cuda",
-                                                                                 generator=gen)
+    temb = normal(1, a.d) + 0.1 * normal(a.frames, a.d)
     full = AdaLNBlock(weights, a.heads, group=None)
     want, seen = full.forward(x, temb, a.tokens, keep=True)
     block = AdaLNBlock(weights, a.heads, a.group, a.zeros)

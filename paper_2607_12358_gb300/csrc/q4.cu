@@ -16,8 +16,6 @@ namespace {
 constexpr int kThreads = 256;
 using bf16 = __nv_bfloat16;
 
-// First of the eight columns that word `w` of a row holds.
-__device__ __forceinline__ int word_column(int w) { return (w >> 4) * 128 + (w & 3) * 32 + ((w >> 2) & 3) * 8; }
 // The word that holds the columns 8 o .. 8 o + 7.
 __device__ __forceinline__ int column_word(int o) { return (o & ~15) + ((o & 3) << 2) + ((o >> 2) & 3); }
 

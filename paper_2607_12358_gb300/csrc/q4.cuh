@@ -31,7 +31,6 @@ __device__ __forceinline__ uint32_t bits(H2 h) {
   return *reinterpret_cast<uint32_t*>(&h);
 }
 __device__ __forceinline__ __half2 half2_of(uint32_t u) { return *reinterpret_cast<__half2*>(&u); }
-__device__ __forceinline__ __nv_bfloat162 bf162_of(uint32_t u) { return *reinterpret_cast<__nv_bfloat162*>(&u); }
 
 // The product's operands.  The activated input enters as two halves, high and
 // low part, after a power of two that brings the largest value of each row (a few

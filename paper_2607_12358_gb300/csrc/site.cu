@@ -659,7 +659,6 @@ int64_t num_groups(const acid_norm_site& s) {
 
 bool known_dtype(int t) { return t == ACID_BF16 || t == ACID_FP32; }
 bool known_norm(int k) { return k == ACID_NORM_NONE || k == ACID_NORM_RMS || k == ACID_NORM_LAYER; }
-size_t bytes_of(int dtype) { return dtype == ACID_BF16 ? 2 : 4; }
 
 acid_status check_site(const acid_norm_site* s) {
   ACID_REQUIRE(s != nullptr, ACID_ERR_INVALID_ARG, "norm_site: null site");

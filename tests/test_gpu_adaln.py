@@ -18,6 +18,15 @@ torch = pytest.importorskip("torch")
 D, HEADS, HIDDEN, FRAMES, TOKENS = 256, 2, 512, 3, 37
 
 
+@pytest.fixture(autouse=True)
+def fp32_by_default():
+    """Whatever default another module of the run has set."""
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 @pytest.fixture(scope="module")
 def adaln():
     import __graft_entry__ as g
@@ -35,8 +44,9 @@ def f64(t):
 def inputs(adaln):
     w = adaln.random_weights(D, HIDDEN, seed=3)
     gen = torch.Generator(device="cuda").manual_seed(4)
-    x = torch.randn(FRAMES * TOKENS, D, device="cuda", generator=gen)
-    temb = torch.randn(1, D, device="cuda", generator=gen) + 0.1 * torch.randn(FRAMES, D, device="cuda", generator=gen)
+    normal = lambda *s: torch.randn(*s, device="cuda", dtype=torch.float32, generator=gen)  # noqa: E731
+    x = normal(FRAMES * TOKENS, D)
+    temb = normal(1, D) + 0.1 * normal(FRAMES, D)
     return w, x, temb
 
 

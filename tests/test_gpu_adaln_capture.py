@@ -8,6 +8,15 @@ torch = pytest.importorskip("torch")
 DEV = "cuda"
 
 
+@pytest.fixture(autouse=True)
+def fp32_by_default():
+    """Whatever default another module of the run has set."""
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 @pytest.fixture(scope="module")
 def acid():
     import __graft_entry__ as g
@@ -22,7 +31,7 @@ def acid():
 def test_captured_calls_equal_eager_calls(acid, groups):
     d, rows = 1536, 600
     gen = torch.Generator(device=DEV).manual_seed(9)
-    rand = lambda *s, dt=torch.float32, std=1.0: (std * torch.randn(*s, device=DEV, generator=gen)).to(dt)  # noqa: E731
+    rand = lambda *s, dt=torch.float32, std=1.0: (std * torch.randn(*s, device=DEV, dtype=torch.float32, generator=gen)).to(dt)  # noqa: E731
     temb, x, y = rand(groups, d), rand(rows, d), rand(rows, d, dt=torch.bfloat16)
     q = acid.acid_q4_quantize(rand(3 * d, d, std=0.02), 64, True)
     bias, w, other = rand(3 * d, std=0.1), rand(d), torch.cuda.Stream()
@@ -53,8 +62,8 @@ def test_captured_calls_equal_eager_calls(acid, groups):
         calls()
     held = dict(back)  # the graph's own outputs
     for seed in (1, 2, 3):
-        temb.copy_(torch.randn(groups, d, device=DEV, generator=gen))
-        x.copy_(torch.randn(rows, d, device=DEV, generator=gen))
+        temb.copy_(rand(groups, d))
+        x.copy_(rand(rows, d))
         calls()
         torch.cuda.synchronize()
         want = [t.clone() for t in (mod, r, u, dtemb, *back.values())]

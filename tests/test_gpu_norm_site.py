@@ -20,6 +20,15 @@ TYPES = {"bf16": (torch.bfloat16, torch.bfloat16), "mixed": (torch.float32, torc
          "fp32": (torch.float32, torch.float32), "wide": (torch.bfloat16, torch.float32)}
 
 
+@pytest.fixture(autouse=True)
+def fp32_by_default():
+    """Whatever default another module of the run has set."""
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 @pytest.fixture(scope="module")
 def acid():
     import __graft_entry__ as g

@@ -19,6 +19,15 @@ TOL = {torch.float32: 5e-6, torch.bfloat16: 2.0 ** -8 + 5e-6}
 BF, F32 = torch.bfloat16, torch.float32
 
 
+@pytest.fixture(autouse=True)
+def fp32_by_default():
+    """Whatever default another module of the run has set."""
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 @pytest.fixture(scope="module")
 def acid():
     import __graft_entry__ as g
