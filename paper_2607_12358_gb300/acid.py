@@ -252,7 +252,21 @@ def norm_site_groups(rows: int, first_rows: int = 0, group_rows: int = 0) -> int
 # These calls are a few microseconds of GPU work on small sites, so their checks are written to cost little: plain
 # comparisons on the way through, the messages formed only where one fails.
 _F32 = torch.float32
-_empty = torch.empty
+
+
+def _empty_on(stream):
+    """torch.empty for a call on ``stream``: memory of that stream's pool, so that neither work that another stream still
+    has to do on a freed block nor that stream's next allocation meets the call's own work."""
+    if stream is None:
+        return torch.empty
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream))
+
+    def empty(*size, **how):
+        with torch.cuda.stream(stream):
+            return torch.empty(*size, **how)
+
+    return empty
 
 
 def _rows_of(name: str, t: torch.Tensor, rows: int, d: int, dtype) -> int:
@@ -316,6 +330,7 @@ def acid_norm_site_forward(x: torch.Tensor, y: torch.Tensor | None = None, *, ga
     g = gate or tanh(gate).  x, r [rows, d] of the stream's dtype, y, u of the branch's (branch_dtype where y is None);
     gate, scale, shift fp32 [groups, d] (norm_site_groups).  r and u are allocated unless given (r may be x, u may be
     y); want_r / want_u False leave one out (None)."""
+    empty = _empty_on(stream)
     xdt = x.dtype
     if x.dim() != 2 or xdt not in _DT:
         raise ValueError("x must be a [rows, d] tensor of bf16 or fp32")
@@ -333,11 +348,11 @@ def acid_norm_site_forward(x: torch.Tensor, y: torch.Tensor | None = None, *, ga
     if r is not None:
         ldr = _rows_of("r", r, rows, d, xdt)
     elif want_r:
-        r = _empty((rows, d), dtype=xdt, device=x.device)
+        r = empty((rows, d), dtype=xdt, device=x.device)
     if u is not None:
         ldu = _rows_of("u", u, rows, d, bdt)
     elif want_u:
-        u = _empty((rows, d), dtype=bdt, device=x.device)
+        u = empty((rows, d), dtype=bdt, device=x.device)
     if r is not None:
         rp = r.data_ptr()
     if u is not None:
@@ -370,6 +385,7 @@ def acid_norm_site_backward(du: torch.Tensor | None, r: torch.Tensor | None, y: 
     """Gradients of acid_norm_site_forward from du (of u) and dr (of r), with the forward call's r and y and its other
     arguments: a dict of dx, dy and, with ``vectors``, dgate, dscale, dshift [groups, d], dpost_w, dpre_w [d] (those
     whose input is given; dshift where scale or shift is)."""
+    empty = _empty_on(stream)
     like = dr if r is None else r
     if like is None or like.dim() != 2 or like.dtype not in _DT:
         raise ValueError("need r or dr, [rows, d] of bf16 or fp32")
@@ -384,7 +400,7 @@ def acid_norm_site_backward(du: torch.Tensor | None, r: torch.Tensor | None, y: 
     lddu = ldr = ldy = lddr = lddx = lddy = d
     out = {}
     if dx is None:
-        dx = _empty((rows, d), dtype=sdt, device=dev)
+        dx = empty((rows, d), dtype=sdt, device=dev)
     else:
         lddx = _rows_of("dx", dx, rows, d, sdt)
     out["dx"] = dx
@@ -395,30 +411,30 @@ def acid_norm_site_backward(du: torch.Tensor | None, r: torch.Tensor | None, y: 
     if y is not None:
         ldy, yp = _rows_of("y", y, rows, d, bdt), y.data_ptr()
         if dy is None:
-            dy = _empty((rows, d), dtype=bdt, device=dev)
+            dy = empty((rows, d), dtype=bdt, device=dev)
         else:
             lddy = _rows_of("dy", dy, rows, d, bdt)
         out["dy"] = dy
         dyp = dy.data_ptr()
         if vectors and gate is not None:
-            t = out["dgate"] = _empty((groups, d), dtype=_F32, device=dev)
+            t = out["dgate"] = empty((groups, d), dtype=_F32, device=dev)
             dgate = t.data_ptr()
         if vectors and post_w is not None:
-            t = out["dpost_w"] = _empty(d, dtype=_F32, device=dev)
+            t = out["dpost_w"] = empty(d, dtype=_F32, device=dev)
             dpost = t.data_ptr()
     if du is not None:
         lddu, dup = _rows_of("du", du, rows, d, bdt), du.data_ptr()
         if vectors and scale is not None:
-            t = out["dscale"] = _empty((groups, d), dtype=_F32, device=dev)
+            t = out["dscale"] = empty((groups, d), dtype=_F32, device=dev)
             dscale = t.data_ptr()
         if vectors and (scale is not None or shift is not None):
-            t = out["dshift"] = _empty((groups, d), dtype=_F32, device=dev)
+            t = out["dshift"] = empty((groups, d), dtype=_F32, device=dev)
             dshift = t.data_ptr()
         if vectors and pre_w is not None:
-            t = out["dpre_w"] = _empty(d, dtype=_F32, device=dev)
+            t = out["dpre_w"] = empty(d, dtype=_F32, device=dev)
             dpre = t.data_ptr()
     if workspace is None:
-        workspace = _empty(_site_bytes(rows, d), dtype=torch.uint8, device=dev)
+        workspace = empty(_site_bytes(rows, d), dtype=torch.uint8, device=dev)
     grads = A.acid_norm_site_grads(dx.data_ptr(), lddx, dyp, lddy, dgate, dscale, dshift, d, dpost, dpre)
     status = load().acid_norm_site_backward(C.byref(site), dup, lddu, rp, ldr, yp, ldy, drp, lddr, C.byref(grads),
                                             workspace.data_ptr(), workspace.numel(), _stream(stream))
@@ -476,6 +492,7 @@ def _matrix(name: str, t: torch.Tensor, rows: int, cols: int) -> int:
 def acid_q4_quantize(w: torch.Tensor, group: int = 128, zeros: bool = False, scale_dtype=torch.bfloat16,
                      stream=None) -> Q4Weight:
     """w [n, k] (bf16 or fp32) in 4 bits with a scale, and with ``zeros`` a zero point, for each ``group`` columns."""
+    empty = _empty_on(stream)
     if w.dim() != 2:
         raise ValueError("w must be a matrix")
     n, k = w.shape
@@ -486,9 +503,9 @@ def acid_q4_quantize(w: torch.Tensor, group: int = 128, zeros: bool = False, sca
     if scale_dtype not in _DT:
         raise TypeError(f"unsupported dtype {scale_dtype}")
     dev = w.device
-    packed = _empty((n, 64 * -(-k // 128)), dtype=torch.uint8, device=dev)
-    scales = _empty((n, per_row), dtype=scale_dtype, device=dev)
-    q = Q4Weight._of(packed, scales, _empty((n, per_row), dtype=torch.uint8, device=dev) if zeros else None, n, k, group)
+    packed = empty((n, 64 * -(-k // 128)), dtype=torch.uint8, device=dev)
+    scales = empty((n, per_row), dtype=scale_dtype, device=dev)
+    q = Q4Weight._of(packed, scales, empty((n, per_row), dtype=torch.uint8, device=dev) if zeros else None, n, k, group)
     status = load().acid_q4_quantize(_DT[w.dtype], w.data_ptr(), ld, C.byref(q.struct), _stream(stream))
     if status:
         check(status)
@@ -498,11 +515,12 @@ def acid_q4_quantize(w: torch.Tensor, group: int = 128, zeros: bool = False, sca
 def acid_q4_dequantize(weight: Q4Weight, dtype=torch.float32, out: torch.Tensor | None = None,
                        stream=None) -> torch.Tensor:
     """The weight's values s (q - z) as a [n, k] tensor."""
+    empty = _empty_on(stream)
     ld = weight.k
     if out is None:
         if dtype not in _DT:
             raise TypeError(f"unsupported dtype {dtype}")
-        out = _empty((weight.n, ld), dtype=dtype, device=weight.packed.device)
+        out = empty((weight.n, ld), dtype=dtype, device=weight.packed.device)
     else:
         ld = _matrix("out", out, weight.n, ld)
     status = load().acid_q4_dequantize(C.byref(weight.struct), _DT[out.dtype], out.data_ptr(), ld, _stream(stream))
@@ -517,16 +535,17 @@ def acid_q4_linear_forward(x: torch.Tensor, weight: Q4Weight, bias: torch.Tensor
     """out [m, n] = a(x [m, k]) W^T + bias, a = SiLU with ``silu``; bias fp32 [n].  ``workspace``:
     q4_linear_workspace_size bytes, not needed up to four rows with
     m k <= 16384."""
+    empty = _empty_on(stream)
     m, n, k = x.shape[0], weight.n, weight.k
     ldx, ldo = _matrix("x", x, m, k), n
     bp, ws, nws = _column_vector("bias", bias, n), None, 0
     if out is None:
-        out = _empty((m, n), dtype=out_dtype, device=x.device)
+        out = empty((m, n), dtype=out_dtype, device=x.device)
     else:
         out_dtype = out.dtype
         ldo = _matrix("out", out, m, n)
     if workspace is None and (m > 4 or m * k > 16384):
-        workspace = _empty(_q4_bytes(n, k, m), dtype=torch.uint8, device=x.device)
+        workspace = empty(_q4_bytes(n, k, m), dtype=torch.uint8, device=x.device)
     if workspace is not None:
         ws, nws = workspace.data_ptr(), workspace.numel()
     status = load().acid_q4_linear_forward(_DT[x.dtype], x.data_ptr(), ldx, m, C.byref(weight.struct), bp, silu,
@@ -554,6 +573,7 @@ def acid_q4_linear_backward(g: torch.Tensor, weight: Q4Weight, x: torch.Tensor |
                             dx_dtype=torch.float32, workspace: torch.Tensor | None = None, stream=None):
     """(dx [m, k], dbias [n]) of acid_q4_linear_forward from g [m, n], the gradient of its output, and x, its input
     (needed with ``silu``; dx has its dtype, dx_dtype without it).  want_dx / want_dbias False leave one out (None)."""
+    empty = _empty_on(stream)
     m, n, k, dev = g.shape[0], weight.n, weight.k, g.device
     ldg = _matrix("g", g, m, n)
     xp = dxp = bp = ws = dbias = None
@@ -563,7 +583,7 @@ def acid_q4_linear_backward(g: torch.Tensor, weight: Q4Weight, x: torch.Tensor |
     elif silu and want_dx:
         raise ValueError("silu needs x")
     if want_dbias:
-        dbias = _empty(n, dtype=_F32, device=dev)
+        dbias = empty(n, dtype=_F32, device=dev)
         bp = dbias.data_ptr()
     if dx is not None:
         lddx = _matrix("dx", dx, m, k)
@@ -571,11 +591,11 @@ def acid_q4_linear_backward(g: torch.Tensor, weight: Q4Weight, x: torch.Tensor |
             raise ValueError("dx must have the dtype of x")
         dx_dtype = dx.dtype
     elif want_dx:
-        dx = _empty((m, k), dtype=dx_dtype, device=dev)
+        dx = empty((m, k), dtype=dx_dtype, device=dev)
     if dx is not None:
         dxp = dx.data_ptr()
         if workspace is None:
-            workspace = _empty(_q4_bytes(n, k, m), dtype=torch.uint8, device=dev)
+            workspace = empty(_q4_bytes(n, k, m), dtype=torch.uint8, device=dev)
         ws, nws = workspace.data_ptr(), workspace.numel()
     status = load().acid_q4_linear_backward(_DT[g.dtype], g.data_ptr(), ldg, m, C.byref(weight.struct), _DT[dx_dtype], xp,
                                             ldx, silu, dxp, lddx, bp, ws, nws, _stream(stream))

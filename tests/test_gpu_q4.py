@@ -257,6 +257,33 @@ def test_quantiser_of_values_that_are_not_finite(acid):
         assert bad.nonzero().tolist() == [[1, 0], [2, 3], [3, 1]]
 
 
+def test_memory_of_a_given_stream(acid):
+    """A call on a stream that is not the current one takes its outputs and workspace from that stream's memory, whether
+    the stream is given as an object or by its handle."""
+    def pool(t):
+        return next(b["stream"] for b in torch.cuda.memory_snapshot()
+                    if b["address"] <= t.data_ptr() < b["address"] + b["total_size"])
+
+    side, x = torch.cuda.Stream(), randn(20, 256, seed=3)
+    y = x.to(BF)
+    gate = randn(1, 256, seed=4)
+    torch.cuda.synchronize()
+    for stream in (side, side.cuda_stream):
+        q = acid.acid_q4_quantize(randn(64, 256, seed=5), 64, True, stream=stream)
+        torch.cuda.synchronize()
+        w = acid.acid_q4_dequantize(q, stream=stream)
+        out = acid.acid_q4_linear_forward(x, q, stream=stream)
+        dx, db = acid.acid_q4_linear_backward(out, q, stream=stream)
+        r, u = acid.acid_norm_site_forward(x, y, gate=gate, stream=stream)
+        g = acid.acid_norm_site_backward(u, r, y, gate=gate, stream=stream)
+        torch.cuda.synchronize()
+        for t in (q.packed, q.scales, q.zeros, w, out, dx, db, r, u, *g.values()):
+            assert pool(t) == side.cuda_stream
+        close(out, f64(x) @ f64(w).T, TOL[F32])
+        assert torch.equal(r, acid.acid_norm_site_forward(x, y, gate=gate)[0])
+    assert pool(acid.acid_q4_linear_forward(x, q)) == torch.cuda.current_stream().cuda_stream
+
+
 def test_empty_and_refusals(acid):
     q, w = weight(acid, 96, 128, 64, True)
     n = acid.launch_count()
