@@ -397,8 +397,8 @@ acid_status acid_q4_dequantize(const acid_q4_weight* weight, int32_t out_dtype, 
 
 /* out[M, N] = a(x[M, K]) W^T + bias for a few rows (timestep embeddings of the
  * branches, frames or steps), a = identity, or SiLU if silu_input.  Sums in fp32;
- * a(x) enters the products as two halves, to within 2^-22 of the largest value
- * of its row (without a workspace: of its 128 columns, those of one packed slab).
+ * a(x) enters the products to within 2^-22 of the largest value of its row
+ * (without a workspace: of its 128 columns, those of one packed slab).
  *   x      device [M, K], row stride ldx, x_dtype.
  *   bias   device fp32 [N] or NULL.
  *   out    device [M, N], row stride ldo, out_dtype.

@@ -96,11 +96,13 @@ __device__ __forceinline__ TileRows tile_rows(const Q4& w, int64_t tile, int g, 
   return r;
 }
 
-// A few rows: the codes enter as q - 8 and a zero point by the sum of a(x) over
-// the group, sum x (q - z) = sum x (q - 8) + (8 - z) sum x.  A CTA's warps split a row tile's slabs among kw of them, and 8 / kw
-// row tiles are neighbours.  A lane reads 16 bytes of four rows: word i of them
-// holds its columns of the slab's 32 columns i, so that four lanes' words make a
-// tile's step of 16 columns twice.
+// Two to four rows: the codes enter as q - 8 and a zero point by the sum of a(x) over
+// the group, sum x (q - z) = sum x (q - 8) + (8 - z) sum x.  A CTA's warps split a row
+// tile's slabs among kw of them, and 8 / kw row tiles are neighbours.  A lane reads 16
+// bytes of four rows: word i of them holds its columns of the slab's 32 columns i, so
+// that four lanes' words make a tile's step of 16 columns twice.
+//   Issue slots bound it, 425 instructions a warp for 32 rows of 128 columns, of which 144
+// convert codes: 276480 x 1536, groups of 128, four rows 57 us (58% of a copy's rate).
 template <typename TS, bool ZEROS, int LOG>
 __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
   constexpr int kWords = 1 << (LOG - 5);  // of 32 columns, to a group
@@ -251,6 +253,211 @@ __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
     if (++k == mine) {
       finish();
       clear();
+      k = 0;
+      set += gridDim.x;
+    }
+  };
+  while (set < sets) {
+    step(l[0]);
+    step(l[1]);
+  }
+}
+
+// ------------------------------------------------------- product with one row
+// One row on whole numbers.  The activated values of 128 columns, times the power of two
+// that brings the largest to 2^22 .. 2^23, are rounded to v = 2^16 h + 2^8 m + l (h signed,
+// m and l unsigned bytes: to within 2^-23 of the largest), and four codes meet four
+// bytes of each in one instruction (dot product of bytes).  A lane's part of a group's sum
+// of v (q - z) is exact: it has 31 bits up to 16 columns, where the three sums may wrap on
+// the way, and is put together from two parts in fp32 beyond.  What is not finite is left
+// out there and comes in at the end.
+//   The tensor cores' tile has room for four rows; for one, most of it is empty, and its
+// codes have to become halves first: 9 instructions for eight codes, here 3, and 6 for
+// their products.  HBM bounds it at groups of 128, 276480 x 1536 43 us (76% of a copy's
+// rate; by the kernel above 54), and the byte products' pipe comes near: groups of 64
+// with zero points 53 us (65%; 65).  9216 x 1536 5 us, a launch and the loads' latency.
+struct OneSmem {
+  size_t low, sums, back, red, odd, all;  // behind the high bytes, uint4 [16 slabs]
+};
+__host__ __device__ inline OneSmem one_smem(int slabs, int groups_of_slab) {
+  OneSmem o;
+  o.low = (size_t)slabs * 16 * 16;              // uint2 [16 slabs]
+  o.sums = o.low + (size_t)slabs * 16 * 8;      // int2 [slab][group][4]
+  o.back = o.sums + (size_t)slabs * groups_of_slab * 32;
+  o.red = o.back + (size_t)slabs * 4;
+  o.odd = o.red + 8 * 33 * 4;
+  o.all = o.odd + 16;
+  return o;
+}
+// The products with the values that are not finite.
+template <typename TS>
+__device__ __noinline__ float odd_products(const Fwd& a, int64_t row) {
+  float sum = 0.f;
+  for (int o = 0; o * 8 < a.w.k; ++o) {
+    float v[8];
+    octet_values(a, 0, o * 8, v);
+    const uint32_t word = word_at(a.w, row, column_word(o));
+    for (int j = 0; j < 8; ++j)
+      if (!isfinite(v[j]))
+        sum += v[j] * (scale_at<TS>(a.w, row, o * 8 + j) * (float)((int)(word >> (4 * j) & 15u) - zero_at(a.w, row, o * 8 + j)));
+  }
+  return sum;
+}
+template <typename TS, bool ZEROS, int LOG>
+__global__ void __launch_bounds__(kThreads, 2) q4_one_kernel(Fwd a) {
+  constexpr int kWords = 1 << (LOG - 5), per_slab = 4 / kWords;  // words of 32 columns to a group; groups to a slab
+  extern __shared__ __align__(16) uint8_t smem[];
+  const Q4& w = a.w;
+  const OneSmem at_smem = one_smem(w.slabs, per_slab);
+  uint4* high = reinterpret_cast<uint4*>(smem);                     // [octet]: h and m of the even columns and the odd ones
+  uint2* low = reinterpret_cast<uint2*>(smem + at_smem.low);        // [octet]: l
+  int2* vsum = reinterpret_cast<int2*>(smem + at_smem.sums);        // [slab][group][t]: sums of h, and of 2^8 m + l
+  float* back = reinterpret_cast<float*>(smem + at_smem.back);      // [slab]
+  float* red = reinterpret_cast<float*>(smem + at_smem.red);        // [8 warps][33]
+  int* odd = reinterpret_cast<int*>(smem + at_smem.odd);
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, warp = warp_index();
+  const int kw = a.kw, rw = kThreads / 32 / kw, kwarp = warp % kw, rwarp = warp / kw;
+  const int64_t tiles = (w.n + 31) / 32, sets = (tiles + rw - 1) / rw;
+  const int mine = (w.slabs - kwarp + kw - 1) / kw;  // slabs of this warp
+  const int lane_group = t / kWords;
+  struct Load {
+    uint4 q[4];
+    float s[4];
+    uint8_t z[4];
+  };
+  if (threadIdx.x == 0) *odd = 0;
+  __syncthreads();
+  pdl_wait();
+  // this warp's steps (row set, slab), two fetched ahead
+  int64_t set = blockIdx.x, fset = set;
+  int k = 0, fslab = kwarp;
+  TileRows at = tile_rows(w, fset * rw + rwarp, g, t);
+  auto next = [&](Load& l) {
+    if (fset < sets) {
+      const int group = min(fslab * per_slab + lane_group, w.groups - 1);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint4* p = at.q[q] + fslab * 4;
+        if (ACID_IN_BOUNDS(kSiteQ4, (p - reinterpret_cast<const uint4*>(w.packed)) * 4 + 3, w.n * w.slabs * 16))
+          l.q[q] = load_stream(p);
+        if (ACID_IN_BOUNDS(kSiteQ4, at.s[q] + group, w.n * w.groups)) {
+          l.s[q] = io<TS>::ld(static_cast<const TS*>(w.scales) + at.s[q] + group);
+          if constexpr (ZEROS) l.z[q] = w.zeros[at.s[q] + group];
+        }
+      }
+    }
+    fslab += kw;
+    if (fslab >= w.slabs) {
+      fslab = kwarp;
+      fset += gridDim.x;
+      if (fset < sets) at = tile_rows(w, fset * rw + rwarp, g, t);
+    }
+  };
+  Load l[2];
+  next(l[0]);
+  next(l[1]);
+  // the bytes of a(x), while the first weights are on their way
+  for (int base = threadIdx.x & ~31; base < w.slabs * 16; base += kThreads) {
+    const int o = base + lane;  // the octet 4 i + t of a slab's 16 lanes
+    float v[8];
+    float top = octet_values(a, 0, o * 8, v);
+#pragma unroll
+    for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+    const float by = __uint_as_float(min(276u - (__float_as_uint(top) >> 23), 254u) << 23);
+    uint32_t d[6] = {};  // h, m, l of the even columns and of the odd ones
+    int sh = 0, sl = 0;
+    bool bad = false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      bad = bad || !isfinite(v[j]);
+      const int n = isfinite(v[j]) ? min(__float2int_rn(v[j] * by), (1 << 23) - 1) : 0;
+      sh += n >> 16;
+      sl += n & 0xffff;
+#pragma unroll
+      for (int b = 0; b < 3; ++b) d[2 * b + j % 2] |= ((uint32_t)n >> (16 - 8 * b) & 255u) << (8 * (j / 2));
+    }
+#pragma unroll
+    for (int x = 4; x < 4 * kWords; x <<= 1) {
+      sh += __shfl_xor_sync(0xffffffffu, sh, x);
+      sl += __shfl_xor_sync(0xffffffffu, sl, x);
+    }
+    if (o < w.slabs * 16) {
+      high[o] = make_uint4(d[0], d[1], d[2], d[3]);
+      low[o] = make_uint2(d[4], d[5]);
+      const int i = (o >> 2) & 3, slab = o >> 4;
+      if (i % kWords == 0) vsum[(slab * per_slab + i / kWords) * 4 + (o & 3)] = make_int2(sh, sl);
+      if ((o & 15) == 0) back[slab] = 1.f / by;
+      if (bad) *odd = 1;
+    }
+  }
+  __syncthreads();
+  float sum[4] = {};  // rows g + 8 q of the tile, this lane's columns
+  auto compute = [&](const Load& l, int slab) {
+    const float bk = back[slab];
+    int h[4], m[4], lw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint4 hm = high[(slab * 4 + i) * 4 + t];
+      const uint2 lo = low[(slab * 4 + i) * 4 + t];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t word = i == 0 ? l.q[q].x : i == 1 ? l.q[q].y : i == 2 ? l.q[q].z : l.q[q].w;
+        const uint32_t even = word & 0x0f0f0f0fu, uneven = word >> 4 & 0x0f0f0f0fu;
+        if (i % kWords == 0) h[q] = m[q] = lw[q] = 0;
+        h[q] = __dp4a((int)uneven, (int)hm.y, __dp4a((int)even, (int)hm.x, h[q]));
+        m[q] = (int)__dp4a(uneven, hm.w, __dp4a(even, hm.z, (uint32_t)m[q]));
+        lw[q] = (int)__dp4a(uneven, lo.y, __dp4a(even, lo.x, (uint32_t)lw[q]));
+      }
+      if ((i + 1) % kWords == 0) {  // the group ends
+        const int from = (lane & ~3) | i / kWords * kWords;  // a lane that has its scale
+        const int2 vs = vsum[(slab * per_slab + i / kWords) * 4 + t];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float s = kWords == 4 ? l.s[q] : __shfl_sync(0xffffffffu, l.s[q], from);
+          const int z = !ZEROS ? 8 : kWords == 4 ? l.z[q] : __shfl_sync(0xffffffffu, (int)l.z[q], from);
+          const int r = m[q] * 256 + lw[q] - z * vs.y;
+          float v;
+          if constexpr (kWords == 4)
+            v = fmaf((float)(h[q] - z * vs.x), 65536.f, (float)r);
+          else
+            v = (float)(int)((uint32_t)(h[q] - z * vs.x) * 65536u + (uint32_t)r);
+          sum[q] = fmaf(s, v * bk, sum[q]);
+        }
+      }
+    }
+  };
+  auto put = [&](int64_t row, float v) {
+    if (row >= w.n) return;
+    if (*odd) v += odd_products<TS>(a, row);
+    put_value(a.out_dtype, a.out, row, v + (a.bias != nullptr ? a.bias[row] : 0.f));
+  };
+  auto finish = [&] {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], 1);
+      sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], 2);
+    }
+    const float v = t == 0 ? sum[0] : t == 1 ? sum[1] : t == 2 ? sum[2] : sum[3];
+    sum[0] = sum[1] = sum[2] = sum[3] = 0.f;
+    if (kw == 1) {
+      put((set * rw + rwarp) * 32 + 8 * t + g, v);
+      return;
+    }
+    __syncthreads();  // the buffer's last readers are done
+    red[warp * 33 + 8 * t + g] = v;
+    __syncthreads();
+    for (int i = threadIdx.x; i < rw * 32; i += kThreads) {
+      float all = 0.f;
+      for (int j = 0; j < kw; ++j) all += red[((i >> 5) * kw + j) * 33 + (i & 31)];
+      put((set * rw + (i >> 5)) * 32 + (i & 31), all);
+    }
+  };
+  auto step = [&](Load& cur) {
+    if (set >= sets) return;
+    compute(cur, kwarp + k * kw);
+    next(cur);
+    if (++k == mine) {
+      finish();
       k = 0;
       set += gridDim.x;
     }
@@ -583,8 +790,8 @@ size_t workspace_bytes(const Q4& w, int64_t m) {
 // Warps of a CTA that share a row's columns: as many as give every SM eight warps where
 // the rows alone would not, and up to four while an SM's sixteen warps have less than two
 // turns each, which then come out more evenly (a row of x, groups of 128: 46080 x 1536
-// with four 12.4 us, with one 16.3; 80000 x 1920 with two 26.4, with one 32.3; beyond, the
-// sums' exchange costs as much as it gains: 138240 x 3072 58.3 and 55.6).
+// with four 10.9 us, with one 13.5; 80000 x 1920 with two 20.4, with one 25.4; beyond, the
+// sums' exchange costs more than it gains: 138240 x 3072 48.2 and 44.1).
 int sharing_warps(const Q4& w) {
   const int64_t tiles = (w.n + 31) / 32, sms = num_sms();
   int kw = 1;
@@ -600,6 +807,14 @@ acid_status launch_few(Fwd a, cudaStream_t s) {
                       (a.kw == 1 ? 0 : 8 * kPackedRows * 33 * sizeof(float));
   ACID_TRY(allow_smem(allowed, q4_few_kernel<TS, ZEROS, LOG>, 110 * 1024));
   const int64_t sets = ((a.w.n + 31) / 32 + rw - 1) / rw;
+  if (a.m == 1) {
+    static PerContext allowed_one;
+    const size_t one = one_smem(a.w.slabs, 128 >> LOG).all;
+    ACID_TRY(allow_smem(allowed_one, q4_one_kernel<TS, ZEROS, LOG>, 110 * 1024));
+    launch_pdl(q4_one_kernel<TS, ZEROS, LOG>, (unsigned)std::min<int64_t>(sets, (int64_t)num_sms() * 2), kThreads, one, s, a);
+    ACID_CHECK_LAUNCH();
+    return ACID_OK;
+  }
   launch_pdl(q4_few_kernel<TS, ZEROS, LOG>, (unsigned)std::min<int64_t>(sets, (int64_t)num_sms() * 2), kThreads, smem, s, a);
   ACID_CHECK_LAUNCH();
   return ACID_OK;

@@ -173,6 +173,46 @@ def test_values_of_x(acid):
     assert torch.isfinite(dx).all() and (dx[0] == 0).all()
 
 
+@pytest.mark.parametrize("group,zeros,scale_dtype", [(128, False, BF), (128, True, F32), (64, True, BF), (64, False, F32),
+                                                     (32, True, BF), (32, False, BF)])
+@pytest.mark.parametrize("n,k", [(1, 1), (5, 40), (33, 129), (100, 512), (3000, 384), (70001, 256), (40, 16384)])
+def test_one_row(acid, group, zeros, scale_dtype, n, k):
+    check_both(acid, 1, n, k, group, zeros, scale_dtype, F32, F32, True)
+    check_both(acid, 1, n, k, group, zeros, scale_dtype, BF, BF, False, bias=False)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_values_of_one_row(acid, group):
+    """Codes, zero points and inputs at the ends of their ranges; sizes of a(x); what is not finite."""
+    n, k = 64, 400
+    rng = np.random.default_rng(group)
+    per_row = -(-k // group)
+    codes, z = rng.choice([0, 15], (n, k)), rng.choice([0, 15], (n, per_row))
+    codes[0], z[0], codes[1], z[1] = 0, 15, 15, 0  # the largest sums of either sign
+    scales = np.full((n, per_row), 0.0078125)
+    q = acid.Q4Weight(torch.from_numpy(O.q4_pack(codes)).to(DEV), torch.from_numpy(scales).to(DEV, F32),
+                      torch.from_numpy(z.astype(np.uint8)).to(DEV), n, k, group)
+    w = O.q4_values(codes, scales, z, group)
+    for size in (1.0, 1e30, 1e-30):
+        for x in (np.full(k, 1.9999999), np.full(k, -2.0), np.full(k, 2.0), rng.choice([-1.0, 1.9999999], k)):
+            t = torch.from_numpy((x * size).astype(np.float32))[None].to(DEV)
+            got, want = acid.acid_q4_linear_forward(t, q), O.q4_linear(f64(t), w)
+            # 2^-23 of the largest value a column, and fp32 sums of the terms
+            assert (np.abs(f64(got) - want) <= 5e-6 * np.abs(f64(t)) @ np.abs(w).T).all()
+    x = randn(1, k, seed=8)
+    x[0, 200:] = 0.0
+    x[0, :128] *= 1e-9  # another 128 columns
+    close(acid.acid_q4_linear_forward(x, q), O.q4_linear(f64(x), w), TOL[F32])
+    assert (acid.acid_q4_linear_forward(torch.zeros(1, k, device=DEV), q) == 0).all()
+    for values in ({5: float("inf")}, {5: float("nan")}, {5: float("inf"), 300: -float("inf")}):
+        y = x.clone()
+        for c, v in values.items():
+            y[0, c] = v
+        with np.errstate(invalid="ignore"):
+            want = O.q4_linear(f64(y), w)
+        np.testing.assert_array_equal(f64(acid.acid_q4_linear_forward(y, q)), want)
+
+
 def test_strides_streams_and_bits(acid):
     n, k, m = 1000, 1536, 7
     q, w = weight(acid, n, k, 128, True, seed=8)
