@@ -434,7 +434,7 @@ struct BackSmem {
   static constexpr int kOffScales = kOffCodes + 16 * kBackRing * 512;  // of two blocks
   static constexpr int kOffBar = kOffScales + 2 * 128 * 4 * 8, kBytes = kOffBar + 256 + 1024;
 };
-constexpr int kTopRuns = 8;  // parts of a share's scales that are scanned by a CTA each
+constexpr int kTopRuns = 32;  // parts of a share's scales that are scanned by a CTA each
 
 // What each addition rounds off is added up beside the sum (exact: the difference of the
 // operands' and the sum's parts), so that terms that cancel leave a sum as good as its terms.
@@ -549,10 +549,7 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
   const int64_t begin = blockIdx.y * a.per, end = min(w.n, begin + a.per), chunk = blockIdx.z, m0 = chunk * kQ4Chunk;
   const int rows = (int)min((int64_t)kQ4Chunk, a.m - m0), blocks = (int)((end - begin + 127) / 128);
   constexpr uint32_t kDCol = 0, kACol = 256;  // tensor memory: sums [2 buffers][128], parts [2 buffers][64]
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < kTopRuns; ++i) top = max(top, a.top[blockIdx.y * kTopRuns + i]);
-  const float one = up_to_scale(top);
+  const float one = up_to_scale(__reduce_max_sync(0xffffffffu, a.top[blockIdx.y * kTopRuns + lane]));
 
   const int64_t all_runs = (w.n + 127) / 128 * 16;
   if (warp == 17) {
