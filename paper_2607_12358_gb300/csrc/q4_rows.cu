@@ -1,5 +1,5 @@
 // 4-bit weights against many rows (tens of timestep embeddings: frames, branches
-// or steps): the product and its input gradient on tcgen05.
+// or steps): the product and its input gradient on tcgen05; the gradient of one row.
 #include <algorithm>
 #include <string>
 #include <type_traits>
@@ -421,9 +421,9 @@ __global__ void __launch_bounds__(fwd_threads(TILES), 1) q4_rows_forward_kernel(
 //   A block's values are 64 KB written to shared memory and 64 KB read, and its MMAs take
 // 1024 clocks; the instructions that make the values and the chain of waits around them
 // bound it, at about twice that: 34 rows, 18432 x 3072, groups of 64 with fp32 scales and
-// zero points 43 us, 36864 x 3072, groups of 128 with bf16 scales 55 us; one row, 9216 x
-// 1536 13 us with the kernels before and after it.  (The scales, a line of memory to each
-// row, loaded by the warps that use them: 47 and 69 us.)
+// zero points 40 us, 36864 x 3072, groups of 128 with bf16 scales 54 us, with the kernels
+// before and after it.  (The scales, a line of memory to each row, loaded by the warps
+// that use them: 47 and 69 us.)
 constexpr int kBackThreads = 640;  // 16 warps that make operands and read sums, one for MMAs, one for g's parts, two for scales
 constexpr int kBackRing = 3;  // blocks of a warp's eight rows of codes
 struct BackSmem {
@@ -771,6 +771,127 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
   }
 }
 
+// --------------------------------------------- input gradient of one row
+// dx of one row of g on the FP32 pipes: a lane takes a row's 32 columns of a slab (16
+// bytes), eight rows to a warp, and keeps the columns' sums over its rows.  A code in bits
+// 4 e .. 4 e + 3 of the last bits of 2^23 is 16^e q without a conversion; 2^23 + 16^e z is
+// taken off (exact), and the column's 16^e at the end.  The lanes', the warps' and
+// (q4_backward_join_kernel) the shares' sums are added in order.
+//   In the kernel above one row of g fills 2 of 128 lanes, and there are three launches for
+// two: 276480 x 1536, groups of 64 with zero points 119 us (29% of a copy's rate; 194
+// above), 9216 x 1536, groups of 128 10 us (14).  The instructions bound it, two a code and
+// 50 a row for its scales and places; two rows took as long as above.
+constexpr int kOneBackCtas = 2;  // of an SM
+template <typename TS, bool ZEROS, int LOG>
+__global__ void __launch_bounds__(kThreads, kOneBackCtas) q4_one_backward_kernel(Q4Bwd a) {
+  constexpr int kGroups = 128 >> LOG, kAhead = 4;
+  __shared__ float red[kThreads / 32][128];
+  pdl_wait();
+  const Q4& w = a.w;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, slab = blockIdx.x;
+  const int64_t begin = blockIdx.y * a.per, end = min(w.n, begin + a.per);
+  struct Load {
+    uint4 q;
+    float s[kGroups], g;
+    uint8_t z[kGroups];
+  };
+  // this lane's next row: rows past the end are the first one against 0
+  int64_t row = begin + warp * 8 + g;
+  const int64_t q0 = (begin * w.slabs + slab) * 16 + 4 * t, s0 = begin * w.groups;
+  int64_t qi = q0 + (int64_t)(warp * 8 + g) * w.slabs * 16, si = s0 + (int64_t)(warp * 8 + g) * w.groups;
+  int group[kGroups];
+#pragma unroll
+  for (int v = 0; v < kGroups; ++v) group[v] = min(slab * kGroups + v, w.groups - 1);
+  auto look = [&](Load& l) {
+    const bool in = row < end;
+    const int64_t q = in ? qi : q0, s = in ? si : s0;
+    if (ACID_IN_BOUNDS(kSiteQ4, q + 3, w.n * w.slabs * 16)) {
+      const uint32_t* p = w.packed + q;
+      asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                   : "=r"(l.q.x), "=r"(l.q.y), "=r"(l.q.z), "=r"(l.q.w)
+                   : "l"(p));
+    }
+#pragma unroll
+    for (int v = 0; v < kGroups; ++v) {
+      if (!ACID_IN_BOUNDS(kSiteQ4, s + group[v], w.n * w.groups)) continue;
+      l.s[v] = io<TS>::ld(static_cast<const TS*>(w.scales) + s + group[v]);
+      if constexpr (ZEROS) l.z[v] = w.zeros[s + group[v]];
+    }
+    l.g = in ? value_at(a.g_dtype, a.g, row) : 0.f;
+    row += 64;
+    qi += (int64_t)64 * w.slabs * 16;
+    si += (int64_t)64 * w.groups;
+  };
+  constexpr float kOne = 8388608.f;  // 2^23
+  const uint64_t one2 = f2_pack(kOne, kOne), minus = f2_pack(-1.f, -1.f);
+  // 16^e of a word's pairs of columns: fields 0 .. 4, and 5 .. 7 shifted down
+  const uint64_t power[4] = {f2_pack(1.f, 16.f), f2_pack(256.f, 4096.f), f2_pack(65536.f, 1.f), f2_pack(16.f, 256.f)};
+  uint64_t sum[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[i][j] = 0;
+  auto add = [&](const Load& l) {
+    uint64_t off[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int v = i >> (LOG - 5);
+      if (i == 0 || (ZEROS && i % (1 << (LOG - 5)) == 0)) {  // -(2^23 + 16^e z)
+        const float z = ZEROS ? (float)l.z[v] : 8.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) off[j] = f2_mul(f2_fma(f2_pack(z, z), power[j], one2), minus);
+      }
+      const float c = l.s[v] * l.g;
+      const uint64_t c2 = f2_pack(c, c);
+      const uint32_t x = i == 0 ? l.q.x : i == 1 ? l.q.y : i == 2 ? l.q.z : l.q.w, y = x >> 20;
+      auto code = [](uint32_t u, int e) { return __uint_as_float((u & (15u << (4 * e))) | 0x4B000000u); };
+      const uint64_t q[4] = {f2_pack(code(x, 0), code(x, 1)), f2_pack(code(x, 2), code(x, 3)), f2_pack(code(x, 4), code(y, 0)),
+                             f2_pack(code(y, 1), code(y, 2))};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum[i][j] = f2_fma(c2, f2_add(q[j], off[j]), sum[i][j]);
+    }
+  };
+  Load l[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) look(l[i]);
+  const int64_t steps = (end - begin + 63) / 64;
+  for (int64_t i = 0; i < steps; i += kAhead)
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {  // (steps past the last one add zeros)
+      add(l[j]);
+      look(l[j]);
+    }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float x, y, px, py;
+      f2_unpack(sum[i][j], x, y);
+      f2_unpack(power[j], px, py);
+      x /= px;  // (powers of two)
+      y /= py;
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) {
+        x += __shfl_xor_sync(0xffffffffu, x, o);
+        y += __shfl_xor_sync(0xffffffffu, y, o);
+      }
+      if (g == 0) {
+        red[warp][32 * i + 8 * t + 2 * j] = x;
+        red[warp][32 * i + 8 * t + 2 * j + 1] = y;
+      }
+    }
+  __syncthreads();
+  if (threadIdx.x < 128) {
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < kThreads / 32; ++i) v += red[i][threadIdx.x];
+    const int64_t at = ((int64_t)blockIdx.y * w.slabs + slab) * 128 + threadIdx.x;
+    if (ACID_IN_BOUNDS(kSiteQ4, at, (int64_t)a.shares * w.slabs * 128)) a.part[at] = v;
+  }
+  if (a.dbias != nullptr && slab == 0)
+    for (int64_t n = begin + threadIdx.x; n < end; n += kThreads) bias_of(a, n);
+}
+
 // Joins the shares in their order and takes the activation's gradient.
 __global__ void __launch_bounds__(128) q4_backward_join_kernel(Q4Bwd a) {
   pdl_wait();
@@ -842,6 +963,22 @@ int64_t share_rows(const Q4& w) {
 }
 int64_t shares_of(const Q4& w) { return (w.n + share_rows(w) - 1) / share_rows(w); }
 
+// Rows of the weight to a CTA of one row's gradient.
+int64_t one_share_rows(const Q4& w) {
+  const int64_t want = std::max(1, kOneBackCtas * 152 / w.slabs), per = (w.n + want - 1) / want;
+  return (per + 63) / 64 * 64;
+}
+template <typename TS, bool ZEROS>
+acid_status launch_one_backward(const Q4Bwd& a, cudaStream_t s) {
+  const dim3 grid(a.w.slabs, (unsigned)a.shares);
+  const auto kernel = a.w.group_log == 5   ? q4_one_backward_kernel<TS, ZEROS, 5>
+                      : a.w.group_log == 6 ? q4_one_backward_kernel<TS, ZEROS, 6>
+                                           : q4_one_backward_kernel<TS, ZEROS, 7>;
+  launch_pdl(kernel, grid, kThreads, 0, s, a);
+  ACID_CHECK_LAUNCH();
+  return ACID_OK;
+}
+
 // Workspace of the gradient: sums of each share, parts of g, powers of two, largest scales.
 struct BackSpace {
   size_t parts, back, top, all;
@@ -854,6 +991,7 @@ BackSpace back_space(const Q4& w, int64_t m) {
   b.back = b.parts + ((size_t)(chunks_of(m) - 1) * kQ4Chunk + last) * runs * 2 * 16;
   b.top = b.back + shares * m * sizeof(float);
   b.all = b.top + shares * kTopRuns * sizeof(uint32_t);
+  if (m == 1) b.all = (size_t)((w.n + one_share_rows(w) - 1) / one_share_rows(w)) * w.slabs * 128 * sizeof(float);
   return b;
 }
 
@@ -892,6 +1030,16 @@ acid_status q4_backward(Q4Bwd a, void* workspace, cudaStream_t s) {
   a.per = share_rows(a.w);
   const int64_t shares = shares_of(a.w);
   a.shares = (int)shares * 2;
+  if (a.m == 1) {
+    a.per = one_share_rows(a.w);
+    a.shares = (int)((a.w.n + a.per - 1) / a.per);
+    const bool h = a.scale_dtype == ACID_BF16;
+    ACID_TRY(a.w.zeros != nullptr ? (h ? launch_one_backward<bf16, true>(a, s) : launch_one_backward<float, true>(a, s))
+                                  : (h ? launch_one_backward<bf16, false>(a, s) : launch_one_backward<float, false>(a, s)));
+    launch_pdl(q4_backward_join_kernel, dim3((a.w.k + 127) / 128, (unsigned)a.m), 128, 0, s, a);
+    ACID_CHECK_LAUNCH();
+    return ACID_OK;
+  }
   const int64_t bias_ctas = a.dbias != nullptr ? std::min<int64_t>((a.per + kThreads - 1) / kThreads, 1024) : 0;
   launch_pdl(q4_back_parts_kernel, dim3((unsigned)shares, (unsigned)(a.m + kTopRuns + bias_ctas)), kThreads, 0, s, a);
   ACID_CHECK_LAUNCH();

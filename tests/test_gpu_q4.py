@@ -213,6 +213,25 @@ def test_values_of_one_row(acid, group):
         np.testing.assert_array_equal(f64(acid.acid_q4_linear_forward(y, q)), want)
 
 
+@pytest.mark.parametrize("group,zeros", [(128, False), (64, True), (32, True)])
+def test_gradient_of_one_row(acid, group, zeros):
+    """Sizes of g from row to row of the weight, and what is not finite, where a product with 0 is not a number."""
+    q, w = weight(acid, 700, 300, group, zeros, seed=9)
+    for size in (1e30, 1e-30):
+        g = randn(1, 700, seed=2) * size
+        close(acid.acid_q4_linear_backward(g, q)[0], O.q4_linear_grad(f64(g), w)[0], TOL[F32], size)
+    g = randn(1, 700, seed=3)
+    g[0, 100:] *= 1e-6
+    close(acid.acid_q4_linear_backward(g, q)[0], O.q4_linear_grad(f64(g), w)[0], TOL[F32])
+    for at, value in ((3, float("inf")), (699, -float("inf")), (64, float("nan"))):
+        h = g.clone()
+        h[0, at] = value
+        with np.errstate(invalid="ignore"):
+            want = O.q4_linear_grad(f64(h), w)[0]
+        np.testing.assert_array_equal(f64(acid.acid_q4_linear_backward(h, q)[0]), want)
+    assert (acid.acid_q4_linear_backward(torch.zeros(1, 700, device=DEV), q)[0] == 0).all()
+
+
 def test_strides_streams_and_bits(acid):
     n, k, m = 1000, 1536, 7
     q, w = weight(acid, n, k, 128, True, seed=8)
