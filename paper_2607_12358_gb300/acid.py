@@ -482,11 +482,11 @@ class Q4Weight:
 
 
 def _matrix(name: str, t: torch.Tensor, rows: int, cols: int) -> int:
-    """Row stride of an operand [rows, cols]."""
+    """Row stride of an operand [rows, cols], as it is: rows that overlap (one expanded to many: 0) are refused by the call."""
     ld = t.stride()
     if t.dtype not in _DT or not t.is_cuda or t.shape != (rows, cols) or (ld[1] != 1 and cols > 1):
         raise ValueError(f"{name} must be a CUDA tensor [{rows}, {cols}] of bf16 or fp32 with contiguous rows")
-    return max(ld[0], cols) if rows > 1 else cols
+    return ld[0] if rows > 1 else cols
 
 
 def acid_q4_quantize(w: torch.Tensor, group: int = 128, zeros: bool = False, scale_dtype=torch.bfloat16,

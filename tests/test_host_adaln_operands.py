@@ -1,0 +1,64 @@
+"""Operands of the norm sites and the 4-bit operators that their kernels cannot take, through the Python binding on the
+CPU: stand-ins for tensors, whose addresses nothing reads, because the call is refused first."""
+
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+BF, F32 = torch.bfloat16, torch.float32
+
+
+class Operand:
+    """What the binding asks of a CUDA tensor."""
+
+    is_cuda, device = True, torch.device("cpu")
+
+    def __init__(self, shape, stride=None, dtype=F32):
+        self.shape, self.dtype = torch.Size(shape), dtype
+        self.strides = stride or (*(math.prod(shape[i + 1:]) for i in range(len(shape) - 1)), 1)
+
+    def stride(self):
+        return self.strides
+
+    def is_contiguous(self):
+        return True
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return math.prod(self.shape)
+
+    def data_ptr(self):
+        return 0x10000000
+
+
+@pytest.fixture()
+def acid(monkeypatch):
+    import __graft_entry__ as g
+
+    g.build()
+    from paper_2607_12358_gb300 import acid as a
+
+    monkeypatch.setattr(a, "_raw_stream", lambda device: 0)
+    monkeypatch.setattr(a, "_current_device", lambda: 0)
+    return a
+
+
+def test_rows_that_overlap(acid):
+    """One row expanded to many has a row stride of 0; the kernels step by at least a row."""
+    q = acid.Q4Weight(Operand((96, 64), dtype=torch.uint8), Operand((96, 2)), None, 96, 128, 64)
+    ws = Operand((1 << 20,), dtype=torch.uint8)
+    for m in (3, 34):
+        x, out = Operand((m, 128)), Operand((m, 96))
+        for stride in ((0, 1), (95, 1)):
+            row, wide = Operand((m, 96), stride), Operand((m, 128), stride)
+            for call in (lambda: acid.acid_q4_linear_forward(wide, q, out=out, workspace=ws),
+                         lambda: acid.acid_q4_linear_forward(x, q, out=row, workspace=ws),
+                         lambda: acid.acid_q4_linear_backward(row, q, dx=x, want_dbias=False, workspace=ws),
+                         lambda: acid.acid_q4_linear_backward(out, q, wide, silu=True, dx=x, want_dbias=False, workspace=ws),
+                         lambda: acid.acid_q4_linear_backward(out, q, dx=wide, want_dbias=False, workspace=ws),
+                         lambda: acid.acid_q4_quantize(wide), lambda: acid.acid_q4_dequantize(q, out=Operand((96, 128), stride))):
+                with pytest.raises(acid.A.AcidError, match="row stride"):
+                    call()
