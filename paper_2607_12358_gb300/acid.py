@@ -278,14 +278,14 @@ def _rows_of(name: str, t: torch.Tensor, rows: int, d: int, dtype) -> int:
 
 
 def _group_vector(name: str, t: torch.Tensor, groups: int, d: int, ld: int) -> int:
-    """Row stride of the vectors t of a site's groups; ld: that of the ones before (0: none)."""
+    """Row stride of the vectors t of a site's groups; ld: that of the ones before (-1: none)."""
     st, shape = t.stride(), t.shape
     if t.dtype is not _F32 or not t.is_cuda or st[-1] != 1 or not (
             shape == (groups, d) or (groups == 1 and shape == (d,))):
         raise ValueError(f"{name} must be a CUDA fp32 tensor [{groups}, {d}] with contiguous rows")
     if groups == 1:
         return d
-    if ld and ld != st[0]:
+    if ld != st[0] and ld >= 0:
         raise ValueError("gate, scale and shift must have one row stride")
     return st[0]
 
@@ -303,10 +303,10 @@ def _site(rows, d, stream_dtype, branch_dtype, gate, scale, shift, post_w, pre_w
     """(C descriptor of a site, its groups) after a check of the vectors' shapes."""
     if not 0 <= first_rows <= rows or group_rows < 0:
         raise ValueError("need 0 <= first_rows <= rows and group_rows >= 0")
-    groups, ld = norm_site_groups(rows, first_rows, group_rows), 0
+    groups, ld = norm_site_groups(rows, first_rows, group_rows), -1
     gp = cp = hp = ap = bp = None
     if gate is not None:
-        ld, gp = _group_vector("gate", gate, groups, d, 0), gate.data_ptr()
+        ld, gp = _group_vector("gate", gate, groups, d, ld), gate.data_ptr()
     if scale is not None:
         ld, cp = _group_vector("scale", scale, groups, d, ld), scale.data_ptr()
     if shift is not None:

@@ -1,0 +1,24 @@
+"""Norm sites where single values decide.  Tolerances are those of test_gpu_norm_site.py."""
+
+import numpy as np
+import pytest
+
+import oracle.adaln_oracle as O
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+from test_gpu_norm_site import DEV, SUM_TOL, TOL, TYPES, acid, both, close, f64, fp32_by_default, make  # noqa: E402, F401
+
+
+def test_vectors_with_strides_of_their_own(acid):
+    """One row stride serves gate, scale and shift: a vector that is repeated by a stride of 0 beside others is refused,
+    whichever it is, and so are three of them."""
+    t, vec = make(12, 256, "mixed", seed=1, groups=3)
+    one = torch.zeros(1, 256, device=DEV).expand(3, 256)
+    for name in ("gate", "scale", "shift"):
+        with pytest.raises(ValueError, match="one row stride"):
+            acid.acid_norm_site_forward(t["x"], t["y"], group_rows=4, **{k: vec[k] for k in ("gate", "scale", "shift")} | {name: one})
+    for names in (("gate",), ("gate", "scale", "shift")):
+        with pytest.raises(acid.A.AcidError):
+            acid.acid_norm_site_forward(t["x"], t["y"], group_rows=4, **{k: one for k in names})

@@ -62,3 +62,16 @@ def test_rows_that_overlap(acid):
                          lambda: acid.acid_q4_quantize(wide), lambda: acid.acid_q4_dequantize(q, out=Operand((96, 128), stride))):
                 with pytest.raises(acid.A.AcidError, match="row stride"):
                     call()
+
+
+@pytest.mark.parametrize("first", [0, 1, 2])
+def test_vectors_that_repeat_by_their_stride(acid, first):
+    """A vector of stride 0 beside one of another stride: one stride is given for both."""
+    names = ("gate", "scale", "shift")
+    x, y = Operand((12, 256)), Operand((12, 256), dtype=BF)
+    vec = {n: Operand((3, 256), (0, 1) if i == first else (768, 1)) for i, n in enumerate(names)}
+    for some in (names, (names[first], names[first - 1])):
+        with pytest.raises(ValueError, match="one row stride"):
+            acid.acid_norm_site_forward(x, y, r=x, u=y, group_rows=4, **{n: vec[n] for n in some})
+    with pytest.raises(acid.A.AcidError, match="ld_mod"):
+        acid.acid_norm_site_forward(x, y, r=x, u=y, group_rows=4, **{names[first]: vec[names[first]]})
