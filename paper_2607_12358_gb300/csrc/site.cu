@@ -651,9 +651,13 @@ __global__ void __launch_bounds__(32 * kJoinWarps) site_join_kernel(SiteBwd a, J
 
 constexpr int kMaxCtas = 2048;  // of the backward pass (workspace)
 
+// Rows of a group after the first rows: no more than there are, so that sums with it stay in range.
+int64_t group_length(const acid_norm_site& s) {
+  const int64_t rest = std::max<int64_t>(s.rows - s.first_rows, 1);
+  return s.group_rows > 0 ? std::min(s.group_rows, rest) : rest;
+}
 int64_t num_groups(const acid_norm_site& s) {
-  const int64_t rest = s.rows - s.first_rows;
-  const int64_t group = s.group_rows > 0 ? s.group_rows : std::max<int64_t>(rest, 1);
+  const int64_t rest = s.rows - s.first_rows, group = group_length(s);
   return (s.first_rows > 0) + (rest + group - 1) / group;
 }
 
@@ -694,7 +698,7 @@ Site site_args(const acid_norm_site& s) {
   Site a;
   a.rows = s.rows;
   a.first = s.first_rows;
-  a.group = s.group_rows > 0 ? s.group_rows : std::max<int64_t>(s.rows - s.first_rows, 1);
+  a.group = group_length(s);
   a.d = s.d;
   a.post = s.post_norm;
   a.pre = s.pre_norm;

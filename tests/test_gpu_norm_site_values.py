@@ -22,3 +22,15 @@ def test_vectors_with_strides_of_their_own(acid):
     for names in (("gate",), ("gate", "scale", "shift")):
         with pytest.raises(acid.A.AcidError):
             acid.acid_norm_site_forward(t["x"], t["y"], group_rows=4, **{k: one for k in names})
+
+
+@pytest.mark.parametrize("first", [0, 1, 40])
+def test_groups_longer_than_the_rows(acid, first):
+    """A group of any length holds the rows that there are."""
+    t, vec = make(41, 520, "mixed", seed=2, groups=acid.norm_site_groups(41, first, 0))
+    how = dict(first_rows=first)
+    r, u, g = both(acid, t, vec, how)
+    for group in (41, 1 << 62, (1 << 63) - 1):
+        assert acid.norm_site_groups(41, first, group) == vec["gate"].shape[0]
+        r2, u2, g2 = both(acid, t, vec, dict(how, group_rows=group))
+        assert torch.equal(r, r2) and torch.equal(u, u2) and all(torch.equal(g[k], g2[k]) for k in g)

@@ -75,3 +75,13 @@ def test_vectors_that_repeat_by_their_stride(acid, first):
             acid.acid_norm_site_forward(x, y, r=x, u=y, group_rows=4, **{n: vec[n] for n in some})
     with pytest.raises(acid.A.AcidError, match="ld_mod"):
         acid.acid_norm_site_forward(x, y, r=x, u=y, group_rows=4, **{names[first]: vec[names[first]]})
+
+
+def test_groups_longer_than_the_rows(acid):
+    """Lengths up to the largest number count like the rows that there are, in the library as in the binding."""
+    A, n = acid.A, acid.C.c_int64()
+    for rows, first, group in ((10, 0, 10), (10, 0, 1 << 62), (10, 0, (1 << 63) - 1), (10, 1, (1 << 63) - 1),
+                               (10, 10, (1 << 63) - 1), (1 << 39, 5, (1 << 63) - 1), (0, 0, (1 << 63) - 1)):
+        site = A.acid_norm_site(rows=rows, d=256, first_rows=first, group_rows=group)
+        acid.check(acid.load().acid_norm_site_groups(acid.C.byref(site), acid.C.byref(n)))
+        assert n.value == acid.norm_site_groups(rows, first, group) == (first > 0) + (rows > first), (rows, first, group)
