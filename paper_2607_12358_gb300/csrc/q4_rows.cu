@@ -581,9 +581,12 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
     auto look = [&](Look& l) {  // the next block's
 #pragma unroll
       for (int j = 0; j < kMine; ++j) {
-        const int64_t p = row + j * kApart < w.n ? at + j * apart : 0;  // rows past the end: any
+        const bool in = row + j * kApart < w.n;
+        const int64_t p = in ? at + j * apart : 0;
         if (!ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.groups)) continue;
         l.s[j] = io<TS>::ld(static_cast<const TS*>(w.scales) + p);
+        // (rows past the end meet parts of zero; another row's scale may be far above the share's, and not fit a half)
+        if (!in) l.s[j] = 0.f;
         if (KIND != kOneHalf && w.zeros != nullptr) l.z[j] = w.zeros[p];
       }
       row += 128;

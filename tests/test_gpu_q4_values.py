@@ -37,3 +37,15 @@ def test_rows_that_overlap_are_refused(acid):
                     call()
     with pytest.raises(acid.A.AcidError, match="row stride"):
         acid.acid_q4_dequantize(q, out=torch.zeros(1, 128, device=DEV).expand(96, 128))
+
+
+@pytest.mark.parametrize("m", [2, 65])
+@pytest.mark.parametrize("group,zeros,scale_dtype", KINDS)
+def test_first_scales_far_above_the_last(acid, m, group, zeros, scale_dtype):
+    """The gradient's last block of 128 rows is not full; the weight's first scales are 2^12 times those of its rows."""
+    q, w = weight(acid, 700, 100, group, zeros, scale_dtype, seed=3)
+    q.scales[0] *= 4096.0
+    w[0] *= 4096.0
+    g = randn(m, 700, seed=1)
+    g[:, 0] = 0.0
+    close(acid.acid_q4_linear_backward(g, q)[0], O.q4_linear_grad(f64(g), w)[0], TOL[F32])
