@@ -899,7 +899,11 @@ extern "C" acid_status acid_norm_site_backward(const acid_norm_site* site, const
   const size_t need = workspace_bytes(*site);
   ACID_REQUIRE(ws_bytes >= need, ACID_ERR_WORKSPACE,
                "acid_norm_site_backward: workspace too small (need " + std::to_string(need) + ")");
-  const BwdLaunch l{{site_args(*site), du, r, y, dr, lddu, ldr, ldy, lddr, o.dx, o.dy, o.lddx, o.lddy, o.dgate, o.dscale,
+  acid_norm_site used = *site;
+  // Without du or y their norms have no part in the gradients: the kernel finds zeros there, whose norm is none at eps 0.
+  if (du == nullptr) used.pre_norm = ACID_NORM_NONE;
+  if (y == nullptr) used.post_norm = ACID_NORM_NONE;
+  const BwdLaunch l{{site_args(used), du, r, y, dr, lddu, ldr, ldy, lddr, o.dx, o.dy, o.lddx, o.lddy, o.dgate, o.dscale,
                      o.dshift, o.dpost_w, o.dpre_w, o.ld_dmod, static_cast<float*>(ws), nullptr, 1},
                     s};
   return by_types<RunBwd>(*site, l);

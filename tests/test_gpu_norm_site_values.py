@@ -34,3 +34,19 @@ def test_groups_longer_than_the_rows(acid, first):
         assert acid.norm_site_groups(41, first, group) == vec["gate"].shape[0]
         r2, u2, g2 = both(acid, t, vec, dict(how, group_rows=group))
         assert torch.equal(r, r2) and torch.equal(u, u2) and all(torch.equal(g[k], g2[k]) for k in g)
+
+
+@pytest.mark.parametrize("pre", ["none", "rms", "layer"])
+@pytest.mark.parametrize("branch", [True, False])
+def test_no_epsilon_without_du(acid, pre, branch):
+    """Where u was not formed its norm has no part in the gradients, with an epsilon of 0 too."""
+    for types in TYPES:
+        t, vec = make(33, 520, types, seed=5)
+        how = dict(pre_norm=pre, post_norm="rms", eps=0.0, res_scale=0.9)
+        some = {k: vec[k] for k in (("gate", "post_w") if branch else ())}
+        y = t["y"] if branch else None
+        g = acid.acid_norm_site_backward(None, None, y, dr=t["dr"], **some, **how)
+        ref = O.norm_site_grad(None, None, f64(y), f64(t["dr"]), **{k: f64(v) for k, v in some.items()}, **how)
+        assert set(g) == ({"dx", "dy", "dgate", "dpost_w"} if branch else {"dx"})
+        for k, v in g.items():
+            close(v.reshape(ref[k].shape), ref[k], TOL[v.dtype] if k in ("dx", "dy") else SUM_TOL, (types, k))
