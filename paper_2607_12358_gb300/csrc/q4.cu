@@ -96,8 +96,24 @@ __device__ __forceinline__ TileRows tile_rows(const Q4& w, int64_t tile, int g, 
   return r;
 }
 
+// The products of row m's values that are not finite with a row of the weight.
+template <typename TS>
+__device__ __noinline__ float odd_products(const Fwd& a, int64_t m, int64_t row) {
+  float sum = 0.f;
+  for (int o = 0; o * 8 < a.w.k; ++o) {
+    float v[8];
+    octet_values(a, m, o * 8, v);
+    const uint32_t word = word_at(a.w, row, column_word(o));
+    for (int j = 0; j < 8; ++j)
+      if (!isfinite(v[j]))
+        sum += v[j] * (scale_at<TS>(a.w, row, o * 8 + j) * (float)((int)(word >> (4 * j) & 15u) - zero_at(a.w, row, o * 8 + j)));
+  }
+  return sum;
+}
+
 // Two to four rows: the codes enter as q - 8 and a zero point by the sum of a(x) over
-// the group, sum x (q - z) = sum x (q - 8) + (8 - z) sum x.  A CTA's warps split a row
+// the group, sum x (q - z) = sum x (q - 8) + (8 - z) sum x.  (Values that are not finite are
+// left out there, and come in at the end times q - z.)  A CTA's warps split a row
 // tile's slabs among kw of them, and 8 / kw row tiles are neighbours.  A lane reads 16
 // bytes of four rows: word i of them holds its columns of the slab's 32 columns i, so
 // that four lanes' words make a tile's step of 16 columns twice.
@@ -155,6 +171,7 @@ __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
   next(l[0]);
   next(l[1]);
   // a(x) in parts, while the first weights are on their way
+  bool odd = false;  // with zero points: values that are not finite
   {
     const int per_row = w.slabs * 16, all = per_row * rows;
     for (int base = threadIdx.x & ~31; base < all; base += kThreads) {
@@ -164,7 +181,13 @@ __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
       float sum = 0.f;
       if constexpr (ZEROS) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum += v[j];
+        for (int j = 0; j < 8; ++j) {
+          if (!isfinite(v[j])) {
+            odd = true;
+            v[j] = 0.f;
+          }
+          sum += v[j];
+        }
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
       }
@@ -178,7 +201,7 @@ __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
       if (ZEROS && (o & 3) == 0) xsum[(o >> 2) * kPackedRows + m] = sum;
     }
     if (threadIdx.x == 0) *none = make_uint4(0, 0, 0, 0);
-    __syncthreads();
+    odd = __syncthreads_or(odd);
   }
   float sum[2][2];  // row t of the input, rows g + 8 h + 16 r of the tile
   auto clear = [&] { sum[0][0] = sum[0][1] = sum[1][0] = sum[1][1] = 0.f; };
@@ -261,6 +284,15 @@ __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
     step(l[0]);
     step(l[1]);
   }
+  if (!ZEROS || !odd) return;
+  // a row with values that are not finite is their products' sum; of other rows that sum is 0
+  __syncthreads();
+  for (set = blockIdx.x; set < sets; set += gridDim.x)
+    for (int i = threadIdx.x; i < rw * rows * 32; i += kThreads) {
+      const int64_t row = (set * rw + i / (rows * 32)) * 32 + (i & 31);
+      const float v = row < w.n ? odd_products<TS>(a, (i >> 5) % rows, row) : 0.f;
+      if (!isfinite(v)) put(row, (i >> 5) % rows, v);
+    }
 }
 
 // ------------------------------------------------------- product with one row
@@ -288,20 +320,6 @@ __host__ __device__ inline OneSmem one_smem(int slabs, int groups_of_slab) {
   o.odd = o.red + 8 * 33 * 4;
   o.all = o.odd + 16;
   return o;
-}
-// The products with the values that are not finite.
-template <typename TS>
-__device__ __noinline__ float odd_products(const Fwd& a, int64_t row) {
-  float sum = 0.f;
-  for (int o = 0; o * 8 < a.w.k; ++o) {
-    float v[8];
-    octet_values(a, 0, o * 8, v);
-    const uint32_t word = word_at(a.w, row, column_word(o));
-    for (int j = 0; j < 8; ++j)
-      if (!isfinite(v[j]))
-        sum += v[j] * (scale_at<TS>(a.w, row, o * 8 + j) * (float)((int)(word >> (4 * j) & 15u) - zero_at(a.w, row, o * 8 + j)));
-  }
-  return sum;
 }
 template <typename TS, bool ZEROS, int LOG>
 __global__ void __launch_bounds__(kThreads, 2) q4_one_kernel(Fwd a) {
@@ -428,7 +446,7 @@ __global__ void __launch_bounds__(kThreads, 2) q4_one_kernel(Fwd a) {
   };
   auto put = [&](int64_t row, float v) {
     if (row >= w.n) return;
-    if (*odd) v += odd_products<TS>(a, row);
+    if (*odd) v += odd_products<TS>(a, 0, row);
     put_value(a.out_dtype, a.out, row, v + (a.bias != nullptr ? a.bias[row] : 0.f));
   };
   auto finish = [&] {

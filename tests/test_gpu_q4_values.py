@@ -49,3 +49,27 @@ def test_first_scales_far_above_the_last(acid, m, group, zeros, scale_dtype):
     g = randn(m, 700, seed=1)
     g[:, 0] = 0.0
     close(acid.acid_q4_linear_backward(g, q)[0], O.q4_linear_grad(f64(g), w)[0], TOL[F32])
+
+
+@pytest.mark.parametrize("m", [1, 2, 3, 4, 5, 17])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("silu", [False, True])
+def test_inputs_that_are_not_finite(acid, m, group, zeros, silu):
+    """An infinity gives what the definition gives, whatever its code and zero point, and the other rows keep their bits."""
+    for n, k in ((40, 100), (40, 400)):
+        q, w = weight(acid, n, k, group, zeros, F32, seed=k)
+        x = randn(m, k, seed=m)
+        ref = acid.acid_q4_linear_forward(x, q, silu=silu)
+        bad = x.clone()
+        bad[0, 7] = float("inf")
+        if m > 2:
+            bad[1, 64], bad[1, k - 1] = -float("inf"), float("inf")
+        if m > 3:
+            bad[2, 33] = float("nan")
+        got = acid.acid_q4_linear_forward(bad, q, silu=silu)
+        with np.errstate(invalid="ignore"):
+            want = O.q4_linear(f64(bad), w, silu=silu)
+        rows = ~torch.isfinite(bad).all(1).cpu().numpy()
+        np.testing.assert_array_equal(f64(got)[rows], want[rows])
+        assert (f64(got)[~rows] == f64(ref)[~rows]).all()
