@@ -110,7 +110,7 @@ struct Q4Bwd {
   // of the call's workspace
   float* part;     // [shares][m][128 slabs]: sums, joined in their order
   uint8_t* parts;  // g as the tensor cores read it
-  float* back;     // [shares / 2][m]: the powers of two taken back
+  float* back;     // [shares / 2][m]: the powers of two taken back; negative: g has values there that are not finite
   uint32_t* top;   // largest scales
   int shares;
   int64_t per;     // rows of the weight to a CTA

@@ -456,10 +456,13 @@ __global__ void __launch_bounds__(kThreads) q4_bias_kernel(Q4Bwd a) {
 
 // For each share of the weight's rows (blockIdx.x): the parts of a row of g, after
 // a power of two of the row and share (y < m); the largest scale of a part of the share
-// (the next kTopRuns); the bias's gradient of 256 rows (the rest).
+// (the next kTopRuns); the bias's gradient of 256 rows (the rest).  What is not finite in g
+// has parts of 0 (an infinity times a value's low half, mostly 0, would be NaN): the power
+// of two is negative then, and odd_gradient adds it.
 //   parts: [chunk][run of 8 rows of the weight][2][rows of the chunk][8]
 __global__ void __launch_bounds__(kThreads) q4_back_parts_kernel(Q4Bwd a) {
   __shared__ uint32_t largest;
+  __shared__ bool odd;
   pdl_wait();
   const int64_t begin = blockIdx.x * a.per, end = min(a.w.n, begin + a.per), y = blockIdx.y;
   if (y >= a.m + kTopRuns) {
@@ -467,7 +470,10 @@ __global__ void __launch_bounds__(kThreads) q4_back_parts_kernel(Q4Bwd a) {
     for (int64_t n = begin + (y - a.m - kTopRuns) * kThreads + threadIdx.x; n < end; n += step) bias_of(a, n);
     return;
   }
-  if (threadIdx.x == 0) largest = 0;
+  if (threadIdx.x == 0) {
+    largest = 0;
+    odd = false;
+  }
   __syncthreads();
   uint32_t top = 0;
   auto join = [&] {
@@ -487,11 +493,14 @@ __global__ void __launch_bounds__(kThreads) q4_back_parts_kernel(Q4Bwd a) {
   }
   const int64_t m = y, chunk = m / kQ4Chunk, rows = min((int64_t)kQ4Chunk, a.m - chunk * kQ4Chunk), r = m - chunk * kQ4Chunk;
 #pragma unroll 8
-  for (int64_t n = begin + threadIdx.x; n < end; n += kThreads)
-    top = max(top, finite_bits(value_at(a.g_dtype, a.g, m * a.ldg + n)));
+  for (int64_t n = begin + threadIdx.x; n < end; n += kThreads) {
+    const float v = value_at(a.g_dtype, a.g, m * a.ldg + n);
+    top = max(top, finite_bits(v));
+    if (!isfinite(v)) odd = true;
+  }
   join();
   const float up = up_to_half(__uint_as_float(largest));
-  if (threadIdx.x == 0) a.back[blockIdx.x * a.m + m] = 1.f / up;
+  if (threadIdx.x == 0) a.back[blockIdx.x * a.m + m] = odd ? -1.f / up : 1.f / up;
   // runs of eight rows of the weight; the last block of a share is filled with zeros
   const int64_t runs = (min(begin + a.per, (a.w.n + 127) / 128 * 128) - begin) / 8, all_runs = (a.w.n + 127) / 128 * 16;
   for (int64_t i = threadIdx.x; i < runs; i += kThreads) {
@@ -499,18 +508,35 @@ __global__ void __launch_bounds__(kThreads) q4_back_parts_kernel(Q4Bwd a) {
     uint32_t h[4], l[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float v0 = n0 + 2 * j < end ? value_at(a.g_dtype, a.g, m * a.ldg + n0 + 2 * j) * up : 0.f;
-      const float v1 = n0 + 2 * j + 1 < end ? value_at(a.g_dtype, a.g, m * a.ldg + n0 + 2 * j + 1) * up : 0.f;
+      float v0 = n0 + 2 * j < end ? value_at(a.g_dtype, a.g, m * a.ldg + n0 + 2 * j) * up : 0.f;
+      float v1 = n0 + 2 * j + 1 < end ? value_at(a.g_dtype, a.g, m * a.ldg + n0 + 2 * j + 1) * up : 0.f;
+      if (!isfinite(v0)) v0 = 0.f;
+      if (!isfinite(v1)) v1 = 0.f;
       const __half2 p = __floats2half2_rn(v0, v1);
       const float2 f = __half22float2(p);
       h[j] = bits(p);
-      // nothing is left of an infinity or a NaN
-      l[j] = bits(__floats2half2_rn(isfinite(f.x) ? v0 - f.x : 0.f, isfinite(f.y) ? v1 - f.y : 0.f));
+      l[j] = bits(__floats2half2_rn(v0 - f.x, v1 - f.y));
     }
     uint4* out = reinterpret_cast<uint4*>(a.parts) + chunk * all_runs * 2 * kQ4Chunk + (n0 / 8) * 2 * rows + r;
     out[0] = make_uint4(h[0], h[1], h[2], h[3]);
     out[rows] = make_uint4(l[0], l[1], l[2], l[3]);
   }
+}
+
+// What the values of row m of g that are not finite add to column c of dx, over a share's rows of the weight.
+__device__ __noinline__ float odd_gradient(const Q4Bwd& a, int64_t m, int c, int64_t begin, int64_t end) {
+  const Q4& w = a.w;
+  const int in_slab = c & 127, word = (c >> 7) * 16 + 4 * (in_slab % 32 / 8) + in_slab / 32, shift = 4 * (c % 8);
+  float sum = 0.f;
+  for (int64_t n = begin; n < end && !isnan(sum); ++n) {
+    const float v = value_at(a.g_dtype, a.g, m * a.ldg + n);
+    if (isfinite(v)) continue;
+    const int64_t i = n * w.groups + (c >> w.group_log), p = n * w.slabs * 16 + word;
+    if (!ACID_IN_BOUNDS(kSiteQ4, i, w.n * w.groups) || !ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.slabs * 16)) continue;
+    const int z = w.zeros != nullptr ? w.zeros[i] : 8;
+    sum += v * (value_at(a.scale_dtype, w.scales, i) * (float)((int)(w.packed[p] >> shift & 15u) - z));
+  }
+  return sum;
 }
 
 template <Values KIND, int LOG>
@@ -750,7 +776,7 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
     if (ok && blocks > 1) take(blocks - 2);
     if (ok) take(blocks - 1);
     if (ok && m < rows) {
-      const float down = a.back[blockIdx.y * a.m + m0 + m], per_s = 1.f / one;
+      const float back = a.back[blockIdx.y * a.m + m0 + m], down = fabsf(back), per_s = 1.f / one;
       const int64_t at = ((blockIdx.y * 2 + low) * a.m + m0 + m) * w.slabs * 128 + slab * 128 + quarter * 32;
       if (ACID_IN_BOUNDS(kSiteQ4, at + 31, a.shares * a.m * w.slabs * 128)) {
 #pragma unroll
@@ -763,6 +789,9 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
           *reinterpret_cast<float4*>(a.part + at + o * 8) = make_float4(f[0], f[2], f[4], f[6]);
           *reinterpret_cast<float4*>(a.part + at + o * 8 + 4) = make_float4(f[1], f[3], f[5], f[7]);
         }
+        const int c0 = slab * 128 + quarter * 32;
+        if (back < 0.f && !low)
+          for (int c = 0; c < min(32, w.k - c0); ++c) a.part[at + c] += odd_gradient(a, m0 + m, c0 + c, begin, end);
       }
     }
   }

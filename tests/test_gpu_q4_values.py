@@ -73,3 +73,28 @@ def test_inputs_that_are_not_finite(acid, m, group, zeros, silu):
         rows = ~torch.isfinite(bad).all(1).cpu().numpy()
         np.testing.assert_array_equal(f64(got)[rows], want[rows])
         assert (f64(got)[~rows] == f64(ref)[~rows]).all()
+
+
+@pytest.mark.parametrize("m", [1, 2, 5, 65])
+@pytest.mark.parametrize("group,zeros,scale_dtype", KINDS)
+def test_gradients_that_are_not_finite(acid, m, group, zeros, scale_dtype):
+    """The same for the gradient of the output: rows of dx that meet an infinity or a NaN, and the others' bits."""
+    for n, k in ((300, 200), (700, 100)):
+        q, w = weight(acid, n, k, group, zeros, scale_dtype, seed=n)
+        g = randn(m, n, seed=m)
+        ref, ref_bias = acid.acid_q4_linear_backward(g, q)
+        bad = g.clone()
+        bad[0, 3] = float("inf")
+        if m > 1:
+            bad[m - 1, 5], bad[m - 1, n - 1] = float("inf"), -float("inf")
+        if m > 2:
+            bad[1, 129] = float("nan")
+        dx, db = acid.acid_q4_linear_backward(bad, q)
+        with np.errstate(invalid="ignore"):
+            want, want_bias = O.q4_linear_grad(f64(bad), w)
+        rows = ~torch.isfinite(bad).all(1).cpu().numpy()
+        np.testing.assert_array_equal(f64(dx)[rows], want[rows])
+        assert (f64(dx)[~rows] == f64(ref)[~rows]).all()
+        cols = ~np.isfinite(want_bias)
+        np.testing.assert_array_equal(f64(db)[cols], want_bias[cols])
+        assert (f64(db)[~cols] == f64(ref_bias)[~cols]).all()
