@@ -96,24 +96,56 @@ __device__ __forceinline__ TileRows tile_rows(const Q4& w, int64_t tile, int g, 
   return r;
 }
 
-// The products of row m's values that are not finite with a row of the weight.
+// Row m of a(x) times a row of the weight, value by value.
 template <typename TS>
-__device__ __noinline__ float odd_products(const Fwd& a, int64_t m, int64_t row) {
+__device__ __noinline__ float plain_product(const Fwd& a, int64_t m, int64_t row) {
   float sum = 0.f;
-  for (int o = 0; o * 8 < a.w.k; ++o) {
-    float v[8];
-    octet_values(a, m, o * 8, v);
-    const uint32_t word = word_at(a.w, row, column_word(o));
-    for (int j = 0; j < 8; ++j)
-      if (!isfinite(v[j]))
-        sum += v[j] * (scale_at<TS>(a.w, row, o * 8 + j) * (float)((int)(word >> (4 * j) & 15u) - zero_at(a.w, row, o * 8 + j)));
+  for (int col = 0; col < a.w.k; col += 32) {
+    float part = 0.f;
+    for (int o = col / 8; o < col / 8 + 4 && o * 8 < a.w.k; ++o) {
+      float v[8];
+      octet_values(a, m, o * 8, v);
+      const uint32_t word = word_at(a.w, row, column_word(o));
+      const float s = scale_at<TS>(a.w, row, col);
+      const int z = zero_at(a.w, row, col);
+      for (int j = 0; j < 8 && o * 8 + j < a.w.k; ++j) part += v[j] * (s * (float)((int)(word >> (4 * j) & 15u) - z));
+    }
+    sum += part;
   }
   return sum;
 }
+// Values that the kernels' sums cannot serve: each warp notes those that it met, one entry a warp.
+enum Special { kInfinite = 1, kLarge = 2 };  // not finite; so large that a sum may pass the largest number where the result does not
+__device__ __forceinline__ void note_special(int* noted, bool infinite, float by) {
+  // (65536 values below 2^82 times 15 stay far from it)
+  const int it = (infinite ? kInfinite : 0) | (by < 0x1p-60f ? kLarge : 0), all = __reduce_or_sync(0xffffffffu, it);
+  if ((threadIdx.x & 31) == 0) noted[threadIdx.x >> 5] = all;
+}
+// Behind the kernels' loops: the CTA's results that are not finite, or should not be, value by value.
+template <typename TS>
+__device__ __noinline__ void special_results(const Fwd& a, int rw, bool infinite) {
+  __syncthreads();
+  const int rows = (int)a.m;
+  const int64_t tiles = (a.w.n + 31) / 32, sets = (tiles + rw - 1) / rw;
+  for (int64_t set = blockIdx.x; set < sets; set += gridDim.x)
+    for (int i = threadIdx.x; i < rw * rows * 32; i += kThreads) {
+      const int64_t row = (set * rw + i / (rows * 32)) * 32 + (i & 31), m = (i >> 5) % rows, at = m * a.ldo + row;
+      if (row >= a.w.n) continue;
+      const bool bad = !isfinite(value_at(a.out_dtype, a.out, at));
+      if (!infinite && !bad) continue;
+      const float v = plain_product<TS>(a, m, row);
+      if (bad || !isfinite(v)) put_value(a.out_dtype, a.out, at, v + (a.bias != nullptr ? a.bias[row] : 0.f));
+    }
+}
+template <typename TS>
+__device__ __forceinline__ void look_at_special(const Fwd& a, int rw, const int* noted) {
+  const int all = __reduce_or_sync(0xffffffffu, noted[threadIdx.x & 7]);
+  if (all != 0) special_results<TS>(a, rw, all & kInfinite);
+}
 
 // Two to four rows: the codes enter as q - 8 and a zero point by the sum of a(x) over
-// the group, sum x (q - z) = sum x (q - 8) + (8 - z) sum x.  (Values that are not finite are
-// left out there, and come in at the end times q - z.)  A CTA's warps split a row
+// the group, sum x (q - z) = sum x (q - 8) + (8 - z) sum x (without values that are not finite:
+// special_results).  A CTA's warps split a row
 // tile's slabs among kw of them, and 8 / kw row tiles are neighbours.  A lane reads 16
 // bytes of four rows: word i of them holds its columns of the slab's 32 columns i, so
 // that four lanes' words make a tile's step of 16 columns twice.
@@ -131,7 +163,8 @@ __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
   float* back = reinterpret_cast<float*>(smem + (size_t)w.slabs * 16 * cols * 16);  // [slab][row]
   float* xsum = back + w.slabs * kPackedRows;                                     // [slab][32 columns][row]
   uint4* none = reinterpret_cast<uint4*>(xsum + (ZEROS ? 4 * w.slabs * kPackedRows : 0));  // zeros
-  float* red = reinterpret_cast<float*>(none + 1);                                // [8 warps][row][33]
+  int* noted = reinterpret_cast<int*>(none + 1);                                  // [8 warps]
+  float* red = reinterpret_cast<float*>(none + 3);                                // [8 warps][row][33]
   const int64_t tiles = (w.n + 31) / 32, sets = (tiles + rw - 1) / rw;
   const int mine = (w.slabs - kwarp + kw - 1) / kw;  // slabs of this warp
   constexpr int per_slab = 4 / kWords;
@@ -171,19 +204,21 @@ __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
   next(l[0]);
   next(l[1]);
   // a(x) in parts, while the first weights are on their way
-  bool odd = false;  // with zero points: values that are not finite
   {
+    bool infinite = false;  // (with zero points; else such values go through the sums)
+    float least = 1.f;
     const int per_row = w.slabs * 16, all = per_row * rows;
     for (int base = threadIdx.x & ~31; base < all; base += kThreads) {
       const int i = base + lane, m = i / per_row, o = i - m * per_row;
       float v[8];
       const float by = octet_of(a, m, o * 8, v);
+      least = fminf(least, by);
       float sum = 0.f;
       if constexpr (ZEROS) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           if (!isfinite(v[j])) {
-            odd = true;
+            infinite = true;
             v[j] = 0.f;
           }
           sum += v[j];
@@ -201,7 +236,8 @@ __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
       if (ZEROS && (o & 3) == 0) xsum[(o >> 2) * kPackedRows + m] = sum;
     }
     if (threadIdx.x == 0) *none = make_uint4(0, 0, 0, 0);
-    odd = __syncthreads_or(odd);
+    note_special(noted, infinite, least);
+    __syncthreads();
   }
   float sum[2][2];  // row t of the input, rows g + 8 h + 16 r of the tile
   auto clear = [&] { sum[0][0] = sum[0][1] = sum[1][0] = sum[1][1] = 0.f; };
@@ -284,15 +320,7 @@ __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
     step(l[0]);
     step(l[1]);
   }
-  if (!ZEROS || !odd) return;
-  // a row with values that are not finite is their products' sum; of other rows that sum is 0
-  __syncthreads();
-  for (set = blockIdx.x; set < sets; set += gridDim.x)
-    for (int i = threadIdx.x; i < rw * rows * 32; i += kThreads) {
-      const int64_t row = (set * rw + i / (rows * 32)) * 32 + (i & 31);
-      const float v = row < w.n ? odd_products<TS>(a, (i >> 5) % rows, row) : 0.f;
-      if (!isfinite(v)) put(row, (i >> 5) % rows, v);
-    }
+  look_at_special<TS>(a, rw, noted);
 }
 
 // ------------------------------------------------------- product with one row
@@ -302,14 +330,14 @@ __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
 // bytes of each in one instruction (dot product of bytes).  A lane's part of a group's sum
 // of v (q - z) is exact: it has 31 bits up to 16 columns, where the three sums may wrap on
 // the way, and is put together from two parts in fp32 beyond.  What is not finite is left
-// out there and comes in at the end.
+// out there (special_results).
 //   The tensor cores' tile has room for four rows; for one, most of it is empty, and its
 // codes have to become halves first: 9 instructions for eight codes, here 3, and 6 for
 // their products.  HBM bounds it at groups of 128, 276480 x 1536 43 us (76% of a copy's
 // rate; by the kernel above 54), and the byte products' pipe comes near: groups of 64
 // with zero points 53 us (65%; 65).  9216 x 1536 5 us, a launch and the loads' latency.
 struct OneSmem {
-  size_t low, sums, back, red, odd, all;  // behind the high bytes, uint4 [16 slabs]
+  size_t low, sums, back, red, noted, all;  // behind the high bytes, uint4 [16 slabs]
 };
 __host__ __device__ inline OneSmem one_smem(int slabs, int groups_of_slab) {
   OneSmem o;
@@ -317,8 +345,8 @@ __host__ __device__ inline OneSmem one_smem(int slabs, int groups_of_slab) {
   o.sums = o.low + (size_t)slabs * 16 * 8;      // int2 [slab][group][4]
   o.back = o.sums + (size_t)slabs * groups_of_slab * 32;
   o.red = o.back + (size_t)slabs * 4;
-  o.odd = o.red + 8 * 33 * 4;
-  o.all = o.odd + 16;
+  o.noted = o.red + 8 * 33 * 4;
+  o.all = o.noted + 32;
   return o;
 }
 template <typename TS, bool ZEROS, int LOG>
@@ -332,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, 2) q4_one_kernel(Fwd a) {
   int2* vsum = reinterpret_cast<int2*>(smem + at_smem.sums);        // [slab][group][t]: sums of h, and of 2^8 m + l
   float* back = reinterpret_cast<float*>(smem + at_smem.back);      // [slab]
   float* red = reinterpret_cast<float*>(smem + at_smem.red);        // [8 warps][33]
-  int* odd = reinterpret_cast<int*>(smem + at_smem.odd);
+  int* noted = reinterpret_cast<int*>(smem + at_smem.noted);        // [8 warps]
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, warp = warp_index();
   const int kw = a.kw, rw = kThreads / 32 / kw, kwarp = warp % kw, rwarp = warp / kw;
   const int64_t tiles = (w.n + 31) / 32, sets = (tiles + rw - 1) / rw;
@@ -343,8 +371,6 @@ __global__ void __launch_bounds__(kThreads, 2) q4_one_kernel(Fwd a) {
     float s[4];
     uint8_t z[4];
   };
-  if (threadIdx.x == 0) *odd = 0;
-  __syncthreads();
   pdl_wait();
   // this warp's steps (row set, slab), two fetched ahead
   int64_t set = blockIdx.x, fset = set;
@@ -375,6 +401,8 @@ __global__ void __launch_bounds__(kThreads, 2) q4_one_kernel(Fwd a) {
   next(l[0]);
   next(l[1]);
   // the bytes of a(x), while the first weights are on their way
+  bool infinite = false;
+  float least = 1.f;
   for (int base = threadIdx.x & ~31; base < w.slabs * 16; base += kThreads) {
     const int o = base + lane;  // the octet 4 i + t of a slab's 16 lanes
     float v[8];
@@ -382,12 +410,12 @@ __global__ void __launch_bounds__(kThreads, 2) q4_one_kernel(Fwd a) {
 #pragma unroll
     for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
     const float by = __uint_as_float(min(276u - (__float_as_uint(top) >> 23), 254u) << 23);
+    least = fminf(least, by);
     uint32_t d[6] = {};  // h, m, l of the even columns and of the odd ones
     int sh = 0, sl = 0;
-    bool bad = false;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      bad = bad || !isfinite(v[j]);
+      infinite = infinite || !isfinite(v[j]);
       const int n = isfinite(v[j]) ? min(__float2int_rn(v[j] * by), (1 << 23) - 1) : 0;
       sh += n >> 16;
       sl += n & 0xffff;
@@ -405,9 +433,9 @@ __global__ void __launch_bounds__(kThreads, 2) q4_one_kernel(Fwd a) {
       const int i = (o >> 2) & 3, slab = o >> 4;
       if (i % kWords == 0) vsum[(slab * per_slab + i / kWords) * 4 + (o & 3)] = make_int2(sh, sl);
       if ((o & 15) == 0) back[slab] = 1.f / by;
-      if (bad) *odd = 1;
     }
   }
+  note_special(noted, infinite, least);
   __syncthreads();
   float sum[4] = {};  // rows g + 8 q of the tile, this lane's columns
   auto compute = [&](const Load& l, int slab) {
@@ -445,9 +473,7 @@ __global__ void __launch_bounds__(kThreads, 2) q4_one_kernel(Fwd a) {
     }
   };
   auto put = [&](int64_t row, float v) {
-    if (row >= w.n) return;
-    if (*odd) v += odd_products<TS>(a, 0, row);
-    put_value(a.out_dtype, a.out, row, v + (a.bias != nullptr ? a.bias[row] : 0.f));
+    if (row < w.n) put_value(a.out_dtype, a.out, row, v + (a.bias != nullptr ? a.bias[row] : 0.f));
   };
   auto finish = [&] {
 #pragma unroll
@@ -484,6 +510,7 @@ __global__ void __launch_bounds__(kThreads, 2) q4_one_kernel(Fwd a) {
     step(l[0]);
     step(l[1]);
   }
+  look_at_special<TS>(a, rw, noted);
 }
 
 // ---------------------------------------------------------------- quantiser
@@ -821,7 +848,7 @@ acid_status launch_few(Fwd a, cudaStream_t s) {
   static PerContext allowed;
   a.kw = sharing_warps(a.w);
   const int rw = kThreads / 32 / a.kw;
-  const size_t smem = (size_t)a.w.slabs * (512 * a.m + 4 * kPackedRows * (ZEROS ? 5 : 1)) + 16 +
+  const size_t smem = (size_t)a.w.slabs * (512 * a.m + 4 * kPackedRows * (ZEROS ? 5 : 1)) + 48 +
                       (a.kw == 1 ? 0 : 8 * kPackedRows * 33 * sizeof(float));
   ACID_TRY(allow_smem(allowed, q4_few_kernel<TS, ZEROS, LOG>, 110 * 1024));
   const int64_t sets = ((a.w.n + 31) / 32 + rw - 1) / rw;

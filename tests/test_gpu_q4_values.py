@@ -98,3 +98,27 @@ def test_gradients_that_are_not_finite(acid, m, group, zeros, scale_dtype):
         cols = ~np.isfinite(want_bias)
         np.testing.assert_array_equal(f64(db)[cols], want_bias[cols])
         assert (f64(db)[~cols] == f64(ref_bias)[~cols]).all()
+
+
+def positive(acid, n, k, group, zeros, scale_dtype):
+    """A weight of positive values, 0.005 to 0.05, and the values."""
+    rng = np.random.default_rng(n + k)
+    per_row = -(-k // group)
+    z = np.full((n, per_row), 5 if zeros else 8)
+    codes = rng.integers(9, 16, (n, k))
+    scales = torch.full((n, per_row), 0.005, device=DEV).to(scale_dtype)
+    q = acid.Q4Weight(torch.from_numpy(O.q4_pack(codes)).to(DEV), scales,
+                      torch.from_numpy(z.astype(np.uint8)).to(DEV) if zeros else None, n, k, group)
+    return q, O.q4_values(codes, f64(scales), z, group)
+
+
+@pytest.mark.parametrize("m", [1, 2, 4, 5])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_products_near_the_largest_number(acid, m, group, zeros):
+    """Results of 1e38, whose sums before the scales would be past the largest number."""
+    for n, k in ((40, 100), (40, 256)):
+        q, w = positive(acid, n, k, group, zeros, F32)
+        x = 1e37 * (0.5 + 0.5 * torch.rand(m, k, device=DEV, generator=torch.Generator(DEV).manual_seed(m)))
+        close(acid.acid_q4_linear_forward(x, q), O.q4_linear(f64(x), w), TOL[F32], (n, k))
+        close(acid.acid_q4_linear_forward(-x, q), O.q4_linear(f64(-x), w), TOL[F32], (n, k))
