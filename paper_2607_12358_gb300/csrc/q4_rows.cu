@@ -458,7 +458,7 @@ __global__ void __launch_bounds__(kThreads) q4_bias_kernel(Q4Bwd a) {
 // a power of two of the row and share (y < m); the largest scale of a part of the share
 // (the next kTopRuns); the bias's gradient of 256 rows (the rest).  What is not finite in g
 // has parts of 0 (an infinity times a value's low half, mostly 0, would be NaN): the power
-// of two is negative then, and odd_gradient adds it.
+// of two is negative then, and plain_gradient adds it.
 //   parts: [chunk][run of 8 rows of the weight][2][rows of the chunk][8]
 __global__ void __launch_bounds__(kThreads) q4_back_parts_kernel(Q4Bwd a) {
   __shared__ uint32_t largest;
@@ -523,20 +523,25 @@ __global__ void __launch_bounds__(kThreads) q4_back_parts_kernel(Q4Bwd a) {
   }
 }
 
-// What the values of row m of g that are not finite add to column c of dx, over a share's rows of the weight.
-__device__ __noinline__ float odd_gradient(const Q4Bwd& a, int64_t m, int c, int64_t begin, int64_t end) {
+// Column c of row m of g W over a share's rows of the weight, value by value: all of them, or those of g that are not
+// finite alone.
+__device__ __noinline__ float plain_gradient(const Q4Bwd& a, int64_t m, int c, int64_t begin, int64_t end, bool all) {
   const Q4& w = a.w;
   const int in_slab = c & 127, word = (c >> 7) * 16 + 4 * (in_slab % 32 / 8) + in_slab / 32, shift = 4 * (c % 8);
-  float sum = 0.f;
-  for (int64_t n = begin; n < end && !isnan(sum); ++n) {
+  float sum = 0.f, part = 0.f;
+  for (int64_t n = begin; n < end && !isnan(sum + part); ++n) {
     const float v = value_at(a.g_dtype, a.g, m * a.ldg + n);
-    if (isfinite(v)) continue;
+    if (!all && isfinite(v)) continue;
     const int64_t i = n * w.groups + (c >> w.group_log), p = n * w.slabs * 16 + word;
     if (!ACID_IN_BOUNDS(kSiteQ4, i, w.n * w.groups) || !ACID_IN_BOUNDS(kSiteQ4, p, w.n * w.slabs * 16)) continue;
     const int z = w.zeros != nullptr ? w.zeros[i] : 8;
-    sum += v * (value_at(a.scale_dtype, w.scales, i) * (float)((int)(w.packed[p] >> shift & 15u) - z));
+    part += v * (value_at(a.scale_dtype, w.scales, i) * (float)((int)(w.packed[p] >> shift & 15u) - z));
+    if ((n & 63) == 63) {
+      sum += part;
+      part = 0.f;
+    }
   }
-  return sum;
+  return sum + part;
 }
 
 template <Values KIND, int LOG>
@@ -776,7 +781,8 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
     if (ok && blocks > 1) take(blocks - 2);
     if (ok) take(blocks - 1);
     if (ok && m < rows) {
-      const float back = a.back[blockIdx.y * a.m + m0 + m], down = fabsf(back), per_s = 1.f / one;
+      const float back = a.back[blockIdx.y * a.m + m0 + m], per_s = 1.f / one;
+      const float less = fminf(fabsf(back), per_s), more = fmaxf(fabsf(back), per_s);  // (the other way a large g overflows)
       const int64_t at = ((blockIdx.y * 2 + low) * a.m + m0 + m) * w.slabs * 128 + slab * 128 + quarter * 32;
       if (ACID_IN_BOUNDS(kSiteQ4, at + 31, a.shares * a.m * w.slabs * 128)) {
 #pragma unroll
@@ -785,13 +791,13 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
 #pragma unroll
           for (int j = 0; j < 4; ++j) f2_unpack(total[4 * o + j], f[2 * j], f[2 * j + 1]);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = f[j] * down * per_s;
+          for (int j = 0; j < 8; ++j) f[j] = f[j] * less * more;
           *reinterpret_cast<float4*>(a.part + at + o * 8) = make_float4(f[0], f[2], f[4], f[6]);
           *reinterpret_cast<float4*>(a.part + at + o * 8 + 4) = make_float4(f[1], f[3], f[5], f[7]);
         }
         const int c0 = slab * 128 + quarter * 32;
         if (back < 0.f && !low)
-          for (int c = 0; c < min(32, w.k - c0); ++c) a.part[at + c] += odd_gradient(a, m0 + m, c0 + c, begin, end);
+          for (int c = 0; c < min(32, w.k - c0); ++c) a.part[at + c] += plain_gradient(a, m0 + m, c0 + c, begin, end, false);
       }
     }
   }
@@ -917,6 +923,8 @@ __global__ void __launch_bounds__(kThreads, kOneBackCtas) q4_one_backward_kernel
     float v = 0.f;
 #pragma unroll
     for (int i = 0; i < kThreads / 32; ++i) v += red[i][threadIdx.x];
+    // (16^e times a sum may pass the largest number where the sum does not)
+    if (!isfinite(v) && slab * 128 + threadIdx.x < w.k) v = plain_gradient(a, 0, slab * 128 + threadIdx.x, begin, end, true);
     const int64_t at = ((int64_t)blockIdx.y * w.slabs + slab) * 128 + threadIdx.x;
     if (ACID_IN_BOUNDS(kSiteQ4, at, (int64_t)a.shares * w.slabs * 128)) a.part[at] = v;
   }

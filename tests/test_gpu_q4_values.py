@@ -122,3 +122,14 @@ def test_products_near_the_largest_number(acid, m, group, zeros):
         x = 1e37 * (0.5 + 0.5 * torch.rand(m, k, device=DEV, generator=torch.Generator(DEV).manual_seed(m)))
         close(acid.acid_q4_linear_forward(x, q), O.q4_linear(f64(x), w), TOL[F32], (n, k))
         close(acid.acid_q4_linear_forward(-x, q), O.q4_linear(f64(-x), w), TOL[F32], (n, k))
+
+
+@pytest.mark.parametrize("m", [1, 2, 65])
+@pytest.mark.parametrize("group,zeros,scale_dtype", KINDS)
+def test_gradients_near_the_largest_number(acid, m, group, zeros, scale_dtype):
+    """The same for the input's gradient."""
+    for n, k in ((40, 100), (300, 200)):
+        q, w = positive(acid, n, k, group, zeros, scale_dtype)
+        g = 1e37 * (0.5 + 0.5 * torch.rand(m, n, device=DEV, generator=torch.Generator(DEV).manual_seed(m)))
+        for v in (g, -g):
+            close(acid.acid_q4_linear_backward(v, q, want_dbias=False)[0], O.q4_linear_grad(f64(v), w)[0], TOL[F32], (n, k))
