@@ -260,7 +260,8 @@ def _empty_on(stream):
     if stream is None:
         return torch.empty
     if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream))
+        handle = _stream(stream)  # (0 as an external stream would be one of PyTorch's own pool)
+        stream = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
 
     def empty(*size, **how):
         with torch.cuda.stream(stream):

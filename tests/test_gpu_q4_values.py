@@ -133,3 +133,26 @@ def test_gradients_near_the_largest_number(acid, m, group, zeros, scale_dtype):
         g = 1e37 * (0.5 + 0.5 * torch.rand(m, n, device=DEV, generator=torch.Generator(DEV).manual_seed(m)))
         for v in (g, -g):
             close(acid.acid_q4_linear_backward(v, q, want_dbias=False)[0], O.q4_linear_grad(f64(v), w)[0], TOL[F32], (n, k))
+
+
+def test_default_stream_by_its_handle(acid):
+    """Handle 0 is the default stream, and its memory is what a call on it takes, whatever stream is current."""
+    def pool(t):
+        return next(b["stream"] for b in torch.cuda.memory_snapshot()
+                    if b["address"] <= t.data_ptr() < b["address"] + b["total_size"])
+
+    x, y, gate = randn(20, 256, seed=3), randn(20, 256, dtype=BF, seed=2), randn(1, 256, seed=4)
+    wf = randn(64, 256, seed=5)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        for stream in (0, torch.cuda.default_stream()):
+            q = acid.acid_q4_quantize(wf, 64, True, stream=stream)
+            w = acid.acid_q4_dequantize(q, stream=stream)
+            out = acid.acid_q4_linear_forward(x, q, stream=stream)
+            dx, db = acid.acid_q4_linear_backward(out, q, stream=stream)
+            r, u = acid.acid_norm_site_forward(x, y, gate=gate, stream=stream)
+            g = acid.acid_norm_site_backward(u, r, y, gate=gate, stream=stream)
+            torch.cuda.synchronize()
+            for t in (q.packed, q.scales, q.zeros, w, out, dx, db, r, u, *g.values()):
+                assert pool(t) == 0
+            close(out, f64(x) @ f64(w).T, TOL[F32])
