@@ -401,6 +401,13 @@ __global__ void __launch_bounds__(kMostThreads<V>, V == 1 ? 16 : 2) site_forward
   }
 }
 
+// The slope 1 - tanh^2 of a gate, 4 e / (1 + e)^2 with e = exp(-2 |x|): 1 - tanh^2 itself has
+// nothing left of it where the gate is past 9.
+__device__ __forceinline__ float tanh_slope(float x) {
+  const float e = expf(-2.f * fabsf(x)), f = 1.f + e;
+  return __fdividef(4.f * e, f * f);
+}
+
 // Gradients of the site's vectors for one group from the raw sums
 // sum du, sum du n and sum dr p over its rows (which = 0, 1, 2): one column.
 __device__ __forceinline__ void put_sum(const SiteBwd& a, int which, int64_t g, int c, float v) {
@@ -409,8 +416,7 @@ __device__ __forceinline__ void put_sum(const SiteBwd& a, int which, int64_t g, 
   if (out == nullptr || !ACID_IN_BOUNDS(kSiteNormSite, c, s.d)) return;
   if (which == 1 && s.pre_w != nullptr) v *= s.pre_w[c];
   if (which == 2) {
-    const float th = s.tanh && s.gate ? tanhf(s.gate[g * s.ld_mod + c]) : 0.f;
-    v *= s.branch * (1.f - th * th) * (s.post_w != nullptr ? s.post_w[c] : 1.f);
+    v *= s.branch * (s.tanh && s.gate ? tanh_slope(s.gate[g * s.ld_mod + c]) : 1.f) * (s.post_w != nullptr ? s.post_w[c] : 1.f);
   }
   out[g * a.ld_dmod + c] = v;
 }
@@ -423,13 +429,14 @@ __device__ __forceinline__ void put_sums(const SiteBwd& a, int which, int64_t g,
   if (which == 1) times(v, vec(s.pre_w, at, 1.f));
   if (which == 2) {
     times(v, vec(s.post_w, at, 1.f));
-    const Cols<V> t = vec(s.tanh && s.gate ? s.gate + m : nullptr, at, 0.f);
-    FOR_PAIRS {
-      float lo, hi;
-      f2_unpack(t.v[i], lo, hi);
-      lo = tanhf(lo);
-      hi = tanhf(hi);
-      v.v[i] = f2_mul(v.v[i], f2_pack(s.branch * (1.f - lo * lo), s.branch * (1.f - hi * hi)));
+    FOR_PAIRS v.v[i] = f2_mul(v.v[i], f2_same(s.branch));
+    if (s.tanh && s.gate) {
+      const Cols<V> t = vec(s.gate + m, at, 0.f);
+      FOR_PAIRS {
+        float lo, hi;
+        f2_unpack(t.v[i], lo, hi);
+        v.v[i] = f2_mul(v.v[i], f2_pack(tanh_slope(lo), tanh_slope(hi)));
+      }
     }
   }
   put(out + g * a.ld_dmod, at, v, g, s.groups);

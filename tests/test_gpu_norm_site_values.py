@@ -50,3 +50,17 @@ def test_no_epsilon_without_du(acid, pre, branch):
         assert set(g) == ({"dx", "dy", "dgate", "dpost_w"} if branch else {"dx"})
         for k, v in g.items():
             close(v.reshape(ref[k].shape), ref[k], TOL[v.dtype] if k in ("dx", "dy") else SUM_TOL, (types, k))
+
+
+@pytest.mark.parametrize("rows,group", [(1, 0), (5, 1), (700, 0), (700, 100)])
+def test_slope_of_gates_far_out(acid, rows, group):
+    """dgate of tanh gates from -10 to 10, column by column: the terms have one sign, so that a column's sum is as good as
+    they are (2e-6), and the slope adds an exponential (2^-22) and four roundings (2^-24 each)."""
+    d, groups = 520, acid.norm_site_groups(rows, 0, group)
+    t, _ = make(rows, d, "fp32", seed=rows, vectors=False, weights=False)
+    y, dr = t["y"].abs() + 0.1, t["dr"].abs() + 0.01
+    gate = torch.linspace(-10, 10, d, device=DEV).repeat(groups, 1)
+    how = dict(gate_tanh=True, group_rows=group, pre_norm="none")
+    g = acid.acid_norm_site_backward(None, None, y, dr=dr, gate=gate, **how)
+    want = O.norm_site_grad(None, None, f64(y), f64(dr), gate=f64(gate), **how)["dgate"]
+    assert (np.abs(f64(g["dgate"]) - want) <= (SUM_TOL if rows > 5 else 3e-6) * want).all()
