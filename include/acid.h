@@ -421,7 +421,7 @@ acid_status acid_q4_linear_workspace_size(const acid_q4_weight* weight, int64_t 
  *   x      device [M, K], row stride ldx, x_dtype: the forward call's input;
  *          may be NULL without silu_input.
  *   dx     device [M, K], row stride lddx, x_dtype, or NULL.
- *   dbias  device fp32 [N], or NULL.  Not both NULL.
+ *   dbias  device fp32 [N], or NULL.  Not both NULL (but for M = 0, where dx has no elements).
  * Sums in fp32.  The weight's rows are shared out among CTAs; g enters the
  * products to within 2^-22 of its row's largest value in a share, and s (q - z)
  * to within 2^-22 of itself, or 2^-35 of the share's largest scale where that is

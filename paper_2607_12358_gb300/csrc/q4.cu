@@ -990,7 +990,8 @@ extern "C" acid_status acid_q4_linear_backward(int32_t g_dtype, const void* g, i
   clear_error();
   ACID_TRY(check_weight(weight));
   ACID_REQUIRE(M >= 0 && M <= kMostRows, ACID_ERR_INVALID_ARG, "acid_q4_linear_backward: need 0 <= M <= 32768");
-  ACID_REQUIRE(dx != nullptr || dbias != nullptr, ACID_ERR_INVALID_ARG, "acid_q4_linear_backward: need dx or dbias");
+  ACID_REQUIRE(M == 0 || dx != nullptr || dbias != nullptr, ACID_ERR_INVALID_ARG,
+               "acid_q4_linear_backward: need dx or dbias");
   ACID_REQUIRE(aligned(dbias, 4), ACID_ERR_UNSUPPORTED, "acid_q4_linear_backward: dbias must be 4-byte aligned");
   cudaStream_t s = (cudaStream_t)stream;
   if (M == 0) {

@@ -156,3 +156,10 @@ def test_default_stream_by_its_handle(acid):
             for t in (q.packed, q.scales, q.zeros, w, out, dx, db, r, u, *g.values()):
                 assert pool(t) == 0
             close(out, f64(x) @ f64(w).T, TOL[F32])
+
+
+def test_gradient_of_no_rows(acid):
+    """Without rows dx is empty, and may be all that is asked for."""
+    q, _ = weight(acid, 96, 128, 64, True)
+    dx, db = acid.acid_q4_linear_backward(torch.zeros(0, 96, device=DEV), q, want_dbias=False)
+    assert dx.shape == (0, 128) and db is None
