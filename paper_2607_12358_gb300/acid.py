@@ -299,6 +299,13 @@ def _column_vector(name: str, t: torch.Tensor, d: int):
     return t.data_ptr()
 
 
+def _workspace(t: torch.Tensor):
+    """(address, bytes) of a workspace that the caller gave."""
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA tensor")
+    return t.data_ptr(), t.numel()
+
+
 def _site(rows, d, stream_dtype, branch_dtype, gate, scale, shift, post_w, pre_w, post_norm, pre_norm, eps, res_scale,
           branch_scale, gate_tanh, first_rows, group_rows):
     """(C descriptor of a site, its groups) after a check of the vectors' shapes."""
@@ -436,9 +443,10 @@ def acid_norm_site_backward(du: torch.Tensor | None, r: torch.Tensor | None, y: 
             dpre = t.data_ptr()
     if workspace is None:
         workspace = empty(_site_bytes(rows, d), dtype=torch.uint8, device=dev)
+    ws, nws = _workspace(workspace)
     grads = A.acid_norm_site_grads(dx.data_ptr(), lddx, dyp, lddy, dgate, dscale, dshift, d, dpost, dpre)
     status = load().acid_norm_site_backward(C.byref(site), dup, lddu, rp, ldr, yp, ldy, drp, lddr, C.byref(grads),
-                                            workspace.data_ptr(), workspace.numel(), _stream(stream))
+                                            ws, nws, _stream(stream))
     if status:
         check(status)
     return out
@@ -548,7 +556,7 @@ def acid_q4_linear_forward(x: torch.Tensor, weight: Q4Weight, bias: torch.Tensor
     if workspace is None and (m > 4 or m * k > 16384):
         workspace = empty(_q4_bytes(n, k, m), dtype=torch.uint8, device=x.device)
     if workspace is not None:
-        ws, nws = workspace.data_ptr(), workspace.numel()
+        ws, nws = _workspace(workspace)
     status = load().acid_q4_linear_forward(_DT[x.dtype], x.data_ptr(), ldx, m, C.byref(weight.struct), bp, silu,
                                            _DT[out_dtype], out.data_ptr(), ldo, ws, nws, _stream(stream))
     if status:
@@ -597,7 +605,7 @@ def acid_q4_linear_backward(g: torch.Tensor, weight: Q4Weight, x: torch.Tensor |
         dxp = dx.data_ptr()
         if workspace is None:
             workspace = empty(_q4_bytes(n, k, m), dtype=torch.uint8, device=dev)
-        ws, nws = workspace.data_ptr(), workspace.numel()
+        ws, nws = _workspace(workspace)
     status = load().acid_q4_linear_backward(_DT[g.dtype], g.data_ptr(), ldg, m, C.byref(weight.struct), _DT[dx_dtype], xp,
                                             ldx, silu, dxp, lddx, bp, ws, nws, _stream(stream))
     if status:

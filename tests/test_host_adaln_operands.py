@@ -85,3 +85,17 @@ def test_groups_longer_than_the_rows(acid):
         site = A.acid_norm_site(rows=rows, d=256, first_rows=first, group_rows=group)
         acid.check(acid.load().acid_norm_site_groups(acid.C.byref(site), acid.C.byref(n)))
         assert n.value == acid.norm_site_groups(rows, first, group) == (first > 0) + (rows > first), (rows, first, group)
+
+
+def test_workspaces_on_the_host(acid):
+    """A workspace that the GPU cannot write as one piece is refused like any other operand."""
+    q = acid.Q4Weight(Operand((96, 64), dtype=torch.uint8), Operand((96, 2)), None, 96, 128, 64)
+    x, g, row = Operand((34, 128)), Operand((34, 96)), Operand((34, 256))
+    for bad in ("is_cuda", "is_contiguous"):
+        ws = Operand((1 << 20,), dtype=torch.uint8)
+        setattr(ws, bad, False if bad == "is_cuda" else lambda: False)
+        for call in (lambda: acid.acid_q4_linear_forward(x, q, out=g, workspace=ws),
+                     lambda: acid.acid_q4_linear_backward(g, q, dx=x, want_dbias=False, workspace=ws),
+                     lambda: acid.acid_norm_site_backward(row, row, row, dx=row, dy=row, workspace=ws)):
+            with pytest.raises(ValueError, match="workspace must be"):
+                call()
