@@ -656,8 +656,6 @@ __global__ void __launch_bounds__(32 * kJoinWarps) site_join_kernel(SiteBwd a, J
   }
 }
 
-constexpr int kMaxCtas = 2048;  // of the backward pass (workspace)
-
 // Rows of a group after the first rows: no more than there are, so that sums with it stay in range.
 int64_t group_length(const acid_norm_site& s) {
   const int64_t rest = std::max<int64_t>(s.rows - s.first_rows, 1);
@@ -724,6 +722,10 @@ Site site_args(const acid_norm_site& s) {
 }
 
 int threads_for(int d, int v) { return (d + 256 * v - 1) / (256 * v) * 32; }
+// Columns of a thread in eights (Cols).
+int eights_for(int d) { return d <= 256 ? 1 : 2; }
+// CTAs of the backward pass that a workspace has slots for: 13 warps an SM (registers leave room for 8 to 12).
+int max_ctas(int d) { return 2048 / (threads_for(d, eights_for(d)) / 32); }
 
 constexpr size_t kMaxSmem = 224 * 1024;
 // CTAs that an SM keeps of a kernel with so much shared memory; sets the kernel
@@ -759,7 +761,7 @@ struct FwdLaunch {
 template <typename TS, typename TB>
 struct RunFwd {
   static acid_status run(const FwdLaunch& l) {
-    if (l.a.s.d <= 256) return l.a.y != nullptr ? go<true, 1>(l) : go<false, 1>(l);
+    if (eights_for(l.a.s.d) == 1) return l.a.y != nullptr ? go<true, 1>(l) : go<false, 1>(l);
     return l.a.y != nullptr ? go<true, 2>(l) : go<false, 2>(l);
   }
   template <bool BRANCH, int V>
@@ -786,7 +788,7 @@ struct BwdLaunch {
 };
 template <typename TS, typename TB>
 struct RunBwd {
-  static acid_status run(const BwdLaunch& l) { return l.a.s.d <= 256 ? go<1>(l) : go<2>(l); }
+  static acid_status run(const BwdLaunch& l) { return eights_for(l.a.s.d) == 1 ? go<1>(l) : go<2>(l); }
   template <int V>
   static acid_status go(const BwdLaunch& l) {
     static PerContext known;
@@ -796,7 +798,7 @@ struct RunBwd {
     const size_t smem = (size_t)threads * (kBwdStages * 2 * (kBytes<TS, V> + kBytes<TB, V>) + 64 * V);
     int fit;
     ACID_TRY(ctas_per_sm(known, site_backward_kernel<TS, TB, V>, threads, smem, &fit));
-    const int64_t most = std::min<int64_t>(kMaxCtas, (int64_t)num_sms() * fit);
+    const int64_t most = std::min<int64_t>(max_ctas(s.d), (int64_t)num_sms() * fit);
     a.per = std::max<int64_t>(1, (s.rows + most - 1) / most);
     const int ctas = (int)((s.rows + a.per - 1) / a.per);
     a.wpart = a.part + part_bytes(s.d, ctas) / sizeof(float);
@@ -827,7 +829,7 @@ struct RunBwd {
 };
 
 size_t workspace_bytes(const acid_norm_site& s) {
-  const int ctas = (int)std::min<int64_t>(kMaxCtas, std::max<int64_t>(s.rows, 1));
+  const int ctas = (int)std::min<int64_t>(max_ctas(s.d), std::max<int64_t>(s.rows, 1));
   return part_bytes(s.d, ctas) + (size_t)ctas * 2 * s.d * sizeof(float);
 }
 

@@ -99,3 +99,12 @@ def test_workspaces_on_the_host(acid):
                      lambda: acid.acid_norm_site_backward(row, row, row, dx=row, dy=row, workspace=ws)):
             with pytest.raises(ValueError, match="workspace must be"):
                 call()
+
+
+def test_workspace_of_a_site(acid):
+    """Slots of the CTAs that a width lets run, some 34 MB at most."""
+    b = acid.C.c_size_t()
+    for d in (8, 256, 264, 512, 1000, 1536, 1920, 4096):
+        site = acid.A.acid_norm_site(rows=1 << 39, d=d)
+        acid.check(acid.load().acid_norm_site_workspace_size(acid.C.byref(site), acid.C.byref(b)))
+        assert 0 < b.value <= 34 << 20, d
