@@ -402,8 +402,8 @@ acid_status acid_q4_dequantize(const acid_q4_weight* weight, int32_t out_dtype, 
  *   x      device [M, K], row stride ldx, x_dtype.
  *   bias   device fp32 [N] or NULL.
  *   out    device [M, N], row stride ldo, out_dtype.
- *   workspace  device, 16-byte aligned, acid_q4_linear_workspace_size bytes (the
- *          parts of a(x) that the tensor cores multiply); not used up to 4
+ *   workspace  device, 16-byte aligned, acid_q4_linear_forward_workspace_size
+ *          bytes (the parts of a(x) that the tensor cores multiply): 0 up to 4
  *          rows of M K <= 16384, where it may be NULL.
  * 0 <= M <= 32768 (0 returns ACID_OK without a launch); past 64 rows the weight
  * is read once for each 64. */
@@ -412,7 +412,10 @@ acid_status acid_q4_linear_forward(int32_t x_dtype, const void* x, int64_t ldx, 
                                    int32_t out_dtype, void* out, int64_t ldo, void* workspace,
                                    size_t workspace_bytes, acid_stream_t stream);
 
-/* Bytes of device workspace that the product and its gradient need for M rows. */
+/* Bytes of device workspace that the product alone needs for M rows. */
+acid_status acid_q4_linear_forward_workspace_size(const acid_q4_weight* weight, int64_t M, size_t* bytes);
+
+/* Bytes of device workspace that serve the product and its gradient for M rows. */
 acid_status acid_q4_linear_workspace_size(const acid_q4_weight* weight, int64_t M, size_t* bytes);
 
 /* Gradients of acid_q4_linear_forward for a frozen weight:

@@ -132,6 +132,7 @@ _PROTOS = {
     "acid_q4_dequantize": (C.c_int, [_Q4, C.c_int32, _P, C.c_int64, _P]),
     "acid_q4_linear_forward": (C.c_int, [C.c_int32, _P, C.c_int64, C.c_int64, _Q4, _P, C.c_int32, C.c_int32, _P,
                                          C.c_int64, _P, C.c_size_t, _P]),
+    "acid_q4_linear_forward_workspace_size": (C.c_int, [_Q4, C.c_int64, C.POINTER(C.c_size_t)]),
     "acid_q4_linear_workspace_size": (C.c_int, [_Q4, C.c_int64, C.POINTER(C.c_size_t)]),
     "acid_q4_linear_backward": (C.c_int, [C.c_int32, _P, C.c_int64, C.c_int64, _Q4, C.c_int32, _P, C.c_int64,
                                           C.c_int32, _P, C.c_int64, _P, _P, C.c_size_t, _P]),

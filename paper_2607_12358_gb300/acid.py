@@ -542,8 +542,7 @@ def acid_q4_linear_forward(x: torch.Tensor, weight: Q4Weight, bias: torch.Tensor
                            out: torch.Tensor | None = None, out_dtype=torch.float32,
                            workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """out [m, n] = a(x [m, k]) W^T + bias, a = SiLU with ``silu``; bias fp32 [n].  ``workspace``:
-    q4_linear_workspace_size bytes, not needed up to four rows with
-    m k <= 16384."""
+    q4_linear_forward_workspace_size bytes (q4_linear_workspace_size serves the gradient too)."""
     empty = _empty_on(stream)
     m, n, k = x.shape[0], weight.n, weight.k
     ldx, ldo = _matrix("x", x, m, k), n
@@ -554,7 +553,7 @@ def acid_q4_linear_forward(x: torch.Tensor, weight: Q4Weight, bias: torch.Tensor
         out_dtype = out.dtype
         ldo = _matrix("out", out, m, n)
     if workspace is None and (m > 4 or m * k > 16384):
-        workspace = empty(_q4_bytes(n, k, m), dtype=torch.uint8, device=x.device)
+        workspace = empty(_q4_forward_bytes(n, k, m), dtype=torch.uint8, device=x.device)
     if workspace is not None:
         ws, nws = _workspace(workspace)
     status = load().acid_q4_linear_forward(_DT[x.dtype], x.data_ptr(), ldx, m, C.byref(weight.struct), bp, silu,
@@ -564,6 +563,12 @@ def acid_q4_linear_forward(x: torch.Tensor, weight: Q4Weight, bias: torch.Tensor
     return out
 
 
+def q4_linear_forward_workspace_size(weight: Q4Weight, m: int) -> int:
+    b = C.c_size_t()
+    check(load().acid_q4_linear_forward_workspace_size(C.byref(weight.struct), int(m), C.byref(b)))
+    return b.value
+
+
 def q4_linear_workspace_size(weight: Q4Weight, m: int) -> int:
     b = C.c_size_t()
     check(load().acid_q4_linear_workspace_size(C.byref(weight.struct), int(m), C.byref(b)))
@@ -571,7 +576,14 @@ def q4_linear_workspace_size(weight: Q4Weight, m: int) -> int:
 
 
 @functools.lru_cache(maxsize=1024)
-def _q4_bytes(n, k, m):  # the size goes by these alone
+def _q4_forward_bytes(n, k, m):  # the sizes go by these alone
+    b = C.c_size_t()
+    check(load().acid_q4_linear_forward_workspace_size(C.byref(A.acid_q4_weight(n=n, k=k, group=128)), m, C.byref(b)))
+    return b.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _q4_bytes(n, k, m):
     b = C.c_size_t()
     check(load().acid_q4_linear_workspace_size(C.byref(A.acid_q4_weight(n=n, k=k, group=128)), m, C.byref(b)))
     return b.value

@@ -974,6 +974,15 @@ extern "C" acid_status acid_q4_linear_forward(int32_t x_dtype, const void* x, in
   return h ? launch_few<bf16, false>(a, s) : launch_few<float, false>(a, s);
 }
 
+extern "C" acid_status acid_q4_linear_forward_workspace_size(const acid_q4_weight* weight, int64_t M, size_t* bytes) {
+  clear_error();
+  ACID_TRY(check_weight(weight));
+  ACID_REQUIRE(bytes != nullptr && M >= 0 && M <= kMostRows, ACID_ERR_INVALID_ARG,
+               "acid_q4_linear_forward_workspace_size: bad argument");
+  *bytes = fwd_bytes(q4_args(*weight), M);
+  return ACID_OK;
+}
+
 extern "C" acid_status acid_q4_linear_workspace_size(const acid_q4_weight* weight, int64_t M, size_t* bytes) {
   clear_error();
   ACID_TRY(check_weight(weight));

@@ -163,3 +163,16 @@ def test_gradient_of_no_rows(acid):
     q, _ = weight(acid, 96, 128, 64, True)
     dx, db = acid.acid_q4_linear_backward(torch.zeros(0, 96, device=DEV), q, want_dbias=False)
     assert dx.shape == (0, 128) and db is None
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 300, 1000), (34, 700, 384), (130, 129, 256), (2, 96, 16384)])
+def test_product_stays_in_its_workspace(acid, m, n, k):
+    """The bytes of acid_q4_linear_forward_workspace_size are enough, and none past them is written."""
+    q, w = weight(acid, n, k, 64, True)
+    x = randn(m, k, seed=m)
+    size = acid.q4_linear_forward_workspace_size(q, m)
+    assert 0 < size <= acid.q4_linear_workspace_size(q, m)
+    ws = torch.full((size + 4096,), 77, dtype=torch.uint8, device=DEV)
+    out = acid.acid_q4_linear_forward(x, q, workspace=ws[:size])
+    close(out, O.q4_linear(f64(x), w), TOL[F32])
+    assert (ws[size:] == 77).all() and torch.equal(out, acid.acid_q4_linear_forward(x, q))

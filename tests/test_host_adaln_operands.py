@@ -108,3 +108,18 @@ def test_workspace_of_a_site(acid):
         site = acid.A.acid_norm_site(rows=1 << 39, d=d)
         acid.check(acid.load().acid_norm_site_workspace_size(acid.C.byref(site), acid.C.byref(b)))
         assert 0 < b.value <= 34 << 20, d
+
+
+def test_workspace_of_a_product(acid):
+    """The parts of its input, whatever the weight's rows, and not the sums and parts of its gradient."""
+    A, b = acid.A, acid.C.c_size_t()
+    for n, k, m in ((36864, 1920, 34), (276480, 1536, 64), (36864, 1920, 2048), (9216, 1536, 5)):
+        w = A.acid_q4_weight(n=n, k=k, group=64)
+        acid.check(acid.load().acid_q4_linear_forward_workspace_size(acid.C.byref(w), m, acid.C.byref(b)))
+        most = (m + 64) * (-(-k // 128) * 512 + 4)  # two halves of each value, whole tiles
+        assert m * k * 4 <= b.value <= most, (n, k, m)
+        acid.check(acid.load().acid_q4_linear_workspace_size(acid.C.byref(w), m, acid.C.byref(b)))
+        assert b.value > most  # the gradient's too
+    for m, want in ((0, 0), (1, 0), (4, 0), (-1, None), (32769, None)):
+        status = acid.load().acid_q4_linear_forward_workspace_size(acid.C.byref(w), m, acid.C.byref(b))
+        assert status == (A.ACID_ERR_INVALID_ARG if want is None else A.ACID_OK) and (want is None or b.value == want)
