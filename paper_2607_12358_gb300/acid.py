@@ -548,6 +548,8 @@ def acid_q4_linear_forward(x: torch.Tensor, weight: Q4Weight, bias: torch.Tensor
     ldx, ldo = _matrix("x", x, m, k), n
     bp, ws, nws = _column_vector("bias", bias, n), None, 0
     if out is None:
+        if out_dtype not in _DT:
+            raise TypeError(f"unsupported dtype {out_dtype}")
         out = empty((m, n), dtype=out_dtype, device=x.device)
     else:
         out_dtype = out.dtype
@@ -612,6 +614,8 @@ def acid_q4_linear_backward(g: torch.Tensor, weight: Q4Weight, x: torch.Tensor |
             raise ValueError("dx must have the dtype of x")
         dx_dtype = dx.dtype
     elif want_dx:
+        if dx_dtype not in _DT:
+            raise TypeError(f"unsupported dtype {dx_dtype}")
         dx = empty((m, k), dtype=dx_dtype, device=dev)
     if dx is not None:
         dxp = dx.data_ptr()

@@ -123,3 +123,14 @@ def test_workspace_of_a_product(acid):
     for m, want in ((0, 0), (1, 0), (4, 0), (-1, None), (32769, None)):
         status = acid.load().acid_q4_linear_forward_workspace_size(acid.C.byref(w), m, acid.C.byref(b))
         assert status == (A.ACID_ERR_INVALID_ARG if want is None else A.ACID_OK) and (want is None or b.value == want)
+
+
+def test_types_of_results(acid):
+    """A type that no kernel writes is refused as the other calls refuse it."""
+    q = acid.Q4Weight(Operand((96, 64), dtype=torch.uint8), Operand((96, 2)), None, 96, 128, 64)
+    x, g, ws = Operand((34, 128)), Operand((34, 96)), Operand((1 << 20,), dtype=torch.uint8)
+    for call in (lambda: acid.acid_q4_linear_forward(x, q, out_dtype=torch.float16, workspace=ws),
+                 lambda: acid.acid_q4_linear_backward(g, q, dx_dtype=torch.float16, workspace=ws),
+                 lambda: acid.acid_q4_dequantize(q, torch.float16)):
+        with pytest.raises(TypeError, match="unsupported dtype"):
+            call()
