@@ -845,22 +845,21 @@ int sharing_warps(const Q4& w) {
 }
 template <typename TS, bool ZEROS, int LOG>
 acid_status launch_few(Fwd a, cudaStream_t s) {
-  static PerContext allowed;
   a.kw = sharing_warps(a.w);
   const int rw = kThreads / 32 / a.kw;
-  const size_t smem = (size_t)a.w.slabs * (512 * a.m + 4 * kPackedRows * (ZEROS ? 5 : 1)) + 48 +
-                      (a.kw == 1 ? 0 : 8 * kPackedRows * 33 * sizeof(float));
-  ACID_TRY(allow_smem(allowed, q4_few_kernel<TS, ZEROS, LOG>, 110 * 1024));
   const int64_t sets = ((a.w.n + 31) / 32 + rw - 1) / rw;
+  const unsigned grid = (unsigned)std::min<int64_t>(sets, (int64_t)num_sms() * 2);
   if (a.m == 1) {
-    static PerContext allowed_one;
-    const size_t one = one_smem(a.w.slabs, 128 >> LOG).all;
-    ACID_TRY(allow_smem(allowed_one, q4_one_kernel<TS, ZEROS, LOG>, 110 * 1024));
-    launch_pdl(q4_one_kernel<TS, ZEROS, LOG>, (unsigned)std::min<int64_t>(sets, (int64_t)num_sms() * 2), kThreads, one, s, a);
-    ACID_CHECK_LAUNCH();
-    return ACID_OK;
+    static PerContext allowed;
+    ACID_TRY(allow_smem(allowed, q4_one_kernel<TS, ZEROS, LOG>, 110 * 1024));
+    launch_pdl(q4_one_kernel<TS, ZEROS, LOG>, grid, kThreads, one_smem(a.w.slabs, 128 >> LOG).all, s, a);
+  } else {
+    static PerContext allowed;
+    const size_t smem = (size_t)a.w.slabs * (512 * a.m + 4 * kPackedRows * (ZEROS ? 5 : 1)) + 48 +
+                        (a.kw == 1 ? 0 : 8 * kPackedRows * 33 * sizeof(float));
+    ACID_TRY(allow_smem(allowed, q4_few_kernel<TS, ZEROS, LOG>, 110 * 1024));
+    launch_pdl(q4_few_kernel<TS, ZEROS, LOG>, grid, kThreads, smem, s, a);
   }
-  launch_pdl(q4_few_kernel<TS, ZEROS, LOG>, (unsigned)std::min<int64_t>(sets, (int64_t)num_sms() * 2), kThreads, smem, s, a);
   ACID_CHECK_LAUNCH();
   return ACID_OK;
 }
