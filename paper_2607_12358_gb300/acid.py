@@ -442,8 +442,11 @@ def acid_norm_site_backward(du: torch.Tensor | None, r: torch.Tensor | None, y: 
             t = out["dpre_w"] = empty(d, dtype=_F32, device=dev)
             dpre = t.data_ptr()
     if workspace is None:
-        workspace = empty(_site_bytes(rows, d), dtype=torch.uint8, device=dev)
-    ws, nws = _workspace(workspace)
+        nws = _site_bytes(rows, d)
+        workspace = empty(nws, dtype=torch.uint8, device=dev)
+        ws = workspace.data_ptr()
+    else:
+        ws, nws = _workspace(workspace)
     grads = A.acid_norm_site_grads(dx.data_ptr(), lddx, dyp, lddy, dgate, dscale, dshift, d, dpost, dpre)
     status = load().acid_norm_site_backward(C.byref(site), dup, lddu, rp, ldr, yp, ldy, drp, lddr, C.byref(grads),
                                             ws, nws, _stream(stream))
@@ -554,10 +557,12 @@ def acid_q4_linear_forward(x: torch.Tensor, weight: Q4Weight, bias: torch.Tensor
     else:
         out_dtype = out.dtype
         ldo = _matrix("out", out, m, n)
-    if workspace is None and (m > 4 or m * k > 16384):
-        workspace = empty(_q4_forward_bytes(n, k, m), dtype=torch.uint8, device=x.device)
     if workspace is not None:
         ws, nws = _workspace(workspace)
+    elif m > 4 or m * k > 16384:
+        nws = _q4_forward_bytes(n, k, m)
+        workspace = empty(nws, dtype=torch.uint8, device=x.device)
+        ws = workspace.data_ptr()
     status = load().acid_q4_linear_forward(_DT[x.dtype], x.data_ptr(), ldx, m, C.byref(weight.struct), bp, silu,
                                            _DT[out_dtype], out.data_ptr(), ldo, ws, nws, _stream(stream))
     if status:
@@ -620,8 +625,11 @@ def acid_q4_linear_backward(g: torch.Tensor, weight: Q4Weight, x: torch.Tensor |
     if dx is not None:
         dxp = dx.data_ptr()
         if workspace is None:
-            workspace = empty(_q4_bytes(n, k, m), dtype=torch.uint8, device=dev)
-        ws, nws = _workspace(workspace)
+            nws = _q4_bytes(n, k, m)
+            workspace = empty(nws, dtype=torch.uint8, device=dev)
+            ws = workspace.data_ptr()
+        else:
+            ws, nws = _workspace(workspace)
     status = load().acid_q4_linear_backward(_DT[g.dtype], g.data_ptr(), ldg, m, C.byref(weight.struct), _DT[dx_dtype], xp,
                                             ldx, silu, dxp, lddx, bp, ws, nws, _stream(stream))
     if status:
