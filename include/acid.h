@@ -398,7 +398,8 @@ acid_status acid_q4_dequantize(const acid_q4_weight* weight, int32_t out_dtype, 
 /* out[M, N] = a(x[M, K]) W^T + bias for a few rows (timestep embeddings of the
  * branches, frames or steps), a = identity, or SiLU if silu_input.  Sums in fp32;
  * a(x) enters the products to within 2^-22 of the largest value of its row
- * (without a workspace: of its 128 columns, those of one packed slab).
+ * (without a workspace: of its 128 columns, those of one packed slab), or 2^-128
+ * where that is more.  An infinity or a NaN in a row gives what the formula gives.
  *   x      device [M, K], row stride ldx, x_dtype.
  *   bias   device fp32 [N] or NULL.
  *   out    device [M, N], row stride ldo, out_dtype.
@@ -427,8 +428,9 @@ acid_status acid_q4_linear_workspace_size(const acid_q4_weight* weight, int64_t 
  *   dbias  device fp32 [N], or NULL.  Not both NULL (but for M = 0, where dx has no elements).
  * Sums in fp32.  The weight's rows are shared out among CTAs; g enters the
  * products to within 2^-22 of its row's largest value in a share, and s (q - z)
- * to within 2^-22 of itself, or 2^-35 of the share's largest scale where that is
- * more (bf16 scales without zero points: exactly).
+ * to within 2^-22 of itself (bf16 scales without zero points: exactly), or 2^-35 of
+ * the share's largest scale where that is more.  One row of g enters as it is.  An
+ * infinity or a NaN in g gives what the formula gives.
  * Deterministic, as acid_norm_site_backward.  workspace: device, 16-byte
  * aligned, acid_q4_linear_workspace_size bytes; not used without dx.  0 <= M <=
  * 32768; M = 0 writes zeros to dbias. */

@@ -47,7 +47,8 @@ def random_weights(d: int, hidden: int, seed: int = 0, device="cuda") -> dict:
 
 class AdaLNBlock:
     """The block above.  ``group`` and ``zeros``: how the modulation's weight is quantised (acid_q4_quantize); ``group``
-    None keeps it in full precision.  The bias ``mod_b`` is the block's own copy, so that it can be calibrated."""
+    None keeps it in full precision.  The bias ``mod_b`` is the block's own copy, so that it can be calibrated; so is the
+    attention's workspace: a block runs on one stream at a time."""
 
     def __init__(self, weights: dict, heads: int, group: int | None = 64, zeros: bool = True):
         self.w, self.heads, self.d = weights, heads, weights["out"].shape[0]

@@ -149,8 +149,10 @@ __device__ __forceinline__ void look_at_special(const Fwd& a, int rw, const int*
 // tile's slabs among kw of them, and 8 / kw row tiles are neighbours.  A lane reads 16
 // bytes of four rows: word i of them holds its columns of the slab's 32 columns i, so
 // that four lanes' words make a tile's step of 16 columns twice.
-//   Issue slots bound it, 425 instructions a warp for 32 rows of 128 columns, of which 144
-// convert codes: 276480 x 1536, groups of 128, four rows 57 us (58% of a copy's rate).
+//   Instructions bound it, 425 a warp for 32 rows of 128 columns, of which 144 convert codes
+// (two rows: issue 61 to 66% busy, the integer pipe 60 to 63%, DRAM 42 to 46%): 276480 x 1536,
+// groups of 128, two rows 56 us, four 57 to 58 (56% of a copy's rate); groups of 64 with zero
+// points 66 and 67 us.
 template <typename TS, bool ZEROS, int LOG>
 __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
   constexpr int kWords = 1 << (LOG - 5);  // of 32 columns, to a group
@@ -333,9 +335,11 @@ __global__ void __launch_bounds__(kThreads, 2) q4_few_kernel(Fwd a) {
 // out there (special_results).
 //   The tensor cores' tile has room for four rows; for one, most of it is empty, and its
 // codes have to become halves first: 9 instructions for eight codes, here 3, and 6 for
-// their products.  HBM bounds it at groups of 128, 276480 x 1536 43 us (76% of a copy's
-// rate; by the kernel above 54), and the byte products' pipe comes near: groups of 64
-// with zero points 53 us (65%; 65).  9216 x 1536 5 us, a launch and the loads' latency.
+// their products.  276480 x 1536, groups of 128 43 us (76% of a copy's rate; by the kernel
+// above 54), of 64 with zero points 53 us (65%; 65).  No unit is full there: the pipe of the
+// byte products is 61% busy, issue 62 to 64%, DRAM (under a profiler) 60 and 52%; sixteen
+// warps an SM with two loads ahead each wait for memory and for that pipe in turn.
+// 9216 x 1536 5 us, a launch and the loads' latency.
 struct OneSmem {
   size_t low, sums, back, red, noted, all;  // behind the high bytes, uint4 [16 slabs]
 };
@@ -533,7 +537,8 @@ __device__ __noinline__ uint32_t divided_codes(float4 lo, float4 hi, float s, in
 // inv = 1 / s, off by less than 2^-22 of it, and is rounded to even by the sum with 1.5 2^23,
 // whose last bits are then the code's; the eight are gathered by one addition each,
 // the constant bits above them taken out at the end.
-//   A quotient near the middle of two codes depends on its last bits.  Where value and
+//   A quotient near the middle of two codes depends on its last bits (they are corrected by
+// the remainder, after Markstein).  Where value and
 // scale are bf16 (SHORT) it is the middle m or at least 2^-9 off it (v - m s is a multiple
 // of half the last place of s), and the middle itself is met often; the remainder v - q s
 // (one fma, exact) takes the product's error out, so that it comes out exactly.  Otherwise a

@@ -816,9 +816,10 @@ __global__ void __launch_bounds__(kBackThreads, 1) q4_rows_backward_kernel(Q4Bwd
 // taken off (exact), and the column's 16^e at the end.  The lanes', the warps' and
 // (q4_backward_join_kernel) the shares' sums are added in order.
 //   In the kernel above one row of g fills 2 of 128 lanes, and there are three launches for
-// two: 276480 x 1536, groups of 64 with zero points 119 us (29% of a copy's rate; 194
-// above), 9216 x 1536, groups of 128 10 us (14).  The instructions bound it, two a code and
-// 50 a row for its scales and places; two rows took as long as above.
+// two: 276480 x 1536, groups of 64 with zero points 113 to 119 us over several GPUs (29 to
+// 31% of a copy's rate; 194 above), of 128 without 96, 9216 x 1536, groups of 128 10 us (14).
+// The instructions bound it, two a code and 50 a row for its scales and places (the integer
+// pipe 68% busy, issue 55 to 60%, DRAM 26 to 28%); two rows took as long as above.
 constexpr int kOneBackCtas = 2;  // of an SM
 template <typename TS, bool ZEROS, int LOG>
 __global__ void __launch_bounds__(kThreads, kOneBackCtas) q4_one_backward_kernel(Q4Bwd a) {
@@ -996,7 +997,8 @@ acid_status launch_backward(const Q4Bwd& a, cudaStream_t s) {
 }
 
 // Rows of the weight to a CTA of the gradient, in whole blocks of 128, and the
-// CTAs that share a slab's rows: as many CTAs as an SM each has.
+// CTAs that share a slab's rows: as many CTAs as an SM each has.  (152 and not the device's
+// SMs: the workspace and the order of the sums go by the weight's shape alone.)
 int64_t share_rows(const Q4& w) {
   const int64_t want = std::max(1, 152 / w.slabs), per = (w.n + want - 1) / want;
   return (per + 127) / 128 * 128;
