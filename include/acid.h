@@ -399,7 +399,8 @@ acid_status acid_q4_dequantize(const acid_q4_weight* weight, int32_t out_dtype, 
  * branches, frames or steps), a = identity, or SiLU if silu_input.  Sums in fp32;
  * a(x) enters the products to within 2^-22 of the largest value of its row
  * (without a workspace: of its 128 columns, those of one packed slab), or 2^-128
- * where that is more.  An infinity or a NaN in a row gives what the formula gives.
+ * where that is more; in two to four rows without a workspace q - 8 and 8 - z meet
+ * it each by itself.  An infinity or a NaN in a row gives what the formula gives.
  *   x      device [M, K], row stride ldx, x_dtype.
  *   bias   device fp32 [N] or NULL.
  *   out    device [M, N], row stride ldo, out_dtype.
