@@ -114,10 +114,12 @@ __device__ __noinline__ float plain_product(const Fwd& a, int64_t m, int64_t row
   }
   return sum;
 }
-// Values that the kernels' sums cannot serve: each warp notes those that it met, one entry a warp.
-enum Special { kInfinite = 1, kLarge = 2 };  // not finite; so large that a sum may pass the largest number where the result does not
+// Values that the kernels' sums cannot serve: not finite, or so large that a sum may pass the
+// largest number where the result does not.  Each warp notes what it met, one entry a warp.
+enum Special { kInfinite = 1, kLarge = 2 };
 __device__ __forceinline__ void note_special(int* noted, bool infinite, float by) {
-  // (65536 values below 2^82 times 15 stay far from it)
+  // (by, the least power of two that a value was brought down with; 65536 values below 2^82
+  // times 15 stay far from the largest number)
   const int it = (infinite ? kInfinite : 0) | (by < 0x1p-60f ? kLarge : 0), all = __reduce_or_sync(0xffffffffu, it);
   if ((threadIdx.x & 31) == 0) noted[threadIdx.x >> 5] = all;
 }
@@ -144,9 +146,9 @@ __device__ __forceinline__ void look_at_special(const Fwd& a, int rw, const int*
 }
 
 // Two to four rows: the codes enter as q - 8 and a zero point by the sum of a(x) over
-// the group, sum x (q - z) = sum x (q - 8) + (8 - z) sum x (without values that are not finite:
-// special_results).  A CTA's warps split a row
-// tile's slabs among kw of them, and 8 / kw row tiles are neighbours.  A lane reads 16
+// the group, sum x (q - z) = sum x (q - 8) + (8 - z) sum x (without values that are not
+// finite, whose two shares may have either sign: special_results).  A CTA's warps split a
+// row tile's slabs among kw of them, and 8 / kw row tiles are neighbours.  A lane reads 16
 // bytes of four rows: word i of them holds its columns of the slab's 32 columns i, so
 // that four lanes' words make a tile's step of 16 columns twice.
 //   Instructions bound it, 425 a warp for 32 rows of 128 columns, of which 144 convert codes
