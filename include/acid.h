@@ -262,6 +262,118 @@ acid_status acid_layernorm_mod(int32_t x_dtype, const void* x, int32_t y_dtype, 
                                float eps, acid_stream_t stream);
 
 /* ------------------------------------------------------------------------ */
+/* Rotary positions with several axes                                        */
+/* ------------------------------------------------------------------------ */
+
+/* A rotation of the query and key heads by positions with up to four axes (latent
+ * frame, row, column).  Axis a turns axis_dim[a] columns of every head: its pair j
+ * by the angle  position[a] * theta[a]^(-2j / axis_dim[a]).  The axes' pairs follow
+ * each other; with R columns turned in all, pair p is columns (2p, 2p + 1), or
+ * (p, p + R/2) with `halves`; columns from R on pass through.  (x1, x2) becomes
+ * (x1 cos - x2 sin, x1 sin + x2 cos), formed in fp32 and rounded once; the angle is
+ * right to 2^-22 of a turn at any position below 2^24.  acid_dit_block_forward
+ * rotates inside its QKV projection; these calls serve callers composing their own
+ * blocks, other position schemes, and gradients. */
+typedef struct {
+  int64_t rows;              /* >= 0, at most 2^31 */
+  int32_t heads, head_dim;   /* head_dim a multiple of 8, <= 256 */
+  int32_t dtype;             /* acid_dtype */
+  int32_t axes;              /* 1 .. 4 */
+  int32_t axis_dim[4];       /* even, > 0; R = their sum <= head_dim, a multiple of 8 (halves: of 16) */
+  float theta[4];            /* > 0, one for each axis */
+  int32_t halves;
+  int64_t first_rows;        /* rows [0, first_rows) are not turned (the text of a joint sequence) */
+  const float* positions;    /* device fp32 [rows, axes], row stride ld_pos; NULL: the grid's */
+  int64_t ld_pos;
+  int32_t grid[4];           /* places along each axis: row first_rows + n is place n (row-major, the last axis
+                                fastest) of the grid, which repeats (a batch of clips) */
+  float origin[4];           /* added to the grid's positions (a later chunk of a clip) */
+} acid_rope;
+
+/* out = the rotation of x, both device [rows, heads * head_dim] with row strides
+ * ldx, ldo, 16-byte aligned, strides multiples of 8.  out may be x (one stride: in
+ * place); no other overlap.  rows = 0 returns ACID_OK without a launch. */
+acid_status acid_rope_forward(const acid_rope* rope, const void* x, int64_t ldx, void* out, int64_t ldo,
+                              acid_stream_t stream);
+
+/* dx = the gradient of x from dout, that of out: the rotation taken back.  The
+ * same rules; dx may be dout. */
+acid_status acid_rope_backward(const acid_rope* rope, const void* dout, int64_t lddo, void* dx, int64_t lddx,
+                               acid_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Attention with row sums, and its gradient                                 */
+/* ------------------------------------------------------------------------ */
+
+/* Attention over several sequences, with key heads shared by query heads and
+ * windows of frames: what training, distillation and frame by frame generation
+ * around the caches need beside acid_attention_forward.  Query head h reads key
+ * head h / (heads / kv_heads).
+ * Sequences: rows [first, end) of the queries attend to rows [first, end) of the
+ * keys.  Bounds lie in order and do not overlap (gaps are padding); one sequence
+ * without bounds has all rows.  Rows of no sequence are neither used (they may hold
+ * anything) nor written.  A bound outside the operand is cut to it.
+ * Frames: frame_rows > 0 makes frames of so many rows of each sequence.  Query row i
+ * is at position i + q_first (q_first -1: so that the last query is at the last
+ * key), and a frame sees the keys of frames_before frames before it, its own and
+ * frames_after after it (-1: all).  frame_rows 1 and frames_after 0 is the causal
+ * mask of single rows.
+ * A query row that sees no key has out 0 and lse -inf, and no part in gradients.
+ * A value that is not finite in a row of a sequence may reach all of that
+ * sequence's results. */
+typedef struct {
+  int64_t nq, nk;            /* rows of the operands, 0 .. 2^30 */
+  int32_t dtype;             /* acid_dtype of all matrices */
+  int32_t heads, kv_heads;   /* heads a multiple of kv_heads */
+  int32_t head_dim;          /* 64 or 128; fp32: 32, 64, 96 or 128 */
+  float scale;               /* of the scores, 1 / sqrt(head_dim) as a rule */
+  int32_t sequences;         /* 1 .. 65535 */
+  const int32_t* q_bounds;   /* device int32 [sequences, 2]: first row, row past the last; 8-byte aligned; */
+  const int32_t* k_bounds;   /* NULL: all rows (one sequence only) */
+  int64_t frame_rows;        /* 0: every row sees all keys of its sequence */
+  int32_t frames_before, frames_after;
+  int64_t q_first;
+} acid_mha;
+
+/* Bytes of device workspace that the calls need (may be 0). */
+acid_status acid_mha_forward_workspace_size(const acid_mha* mha, size_t* bytes);
+acid_status acid_mha_backward_workspace_size(const acid_mha* mha, size_t* bytes);
+
+/* out = softmax(scale q k^T) v over the visible keys, and lse = the logarithm of
+ * each row's sum of exponentials, which acid_mha_backward reads.
+ *   q, out  device [nq, heads * head_dim], row strides ldq, ldo.
+ *   k, v    device [nk, kv_heads * head_dim], row strides ldk, ldv.
+ *   lse     device fp32 [heads, nq].
+ * Matrices are 16-byte aligned, row strides multiples of 8; out overlaps nothing.
+ * bf16 runs on tcgen05 (scores and sums in fp32, probabilities enter the second
+ * product in bf16, with errors of 2^-9 of themselves), fp32 on the FP32 pipes.
+ *   workspace  device, 16-byte aligned.
+ * The same call gives the same bits. */
+acid_status acid_mha_forward(const acid_mha* mha, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                             const void* v, int64_t ldv, void* out, int64_t ldo, float* lse, void* workspace,
+                             size_t workspace_bytes, acid_stream_t stream);
+
+/* Gradients that acid_mha_backward writes; NULL ones are left out, not all of them. */
+typedef struct {
+  void* dq; int64_t lddq;    /* device [nq, heads * head_dim] */
+  void* dk; int64_t lddk;    /* device [nk, kv_heads * head_dim] */
+  void* dv; int64_t lddv;    /* the same */
+} acid_mha_grads;
+
+/* Gradients of acid_mha_forward from dout, that of out (lse has none), with the
+ * forward call's operands and results.  The probabilities are formed again from
+ * lse.  With P the probabilities and D = sum over a row of dout out:
+ *     dv = P^T dout,   dS = P (dout v^T - D),   dq = scale dS k,   dk = scale dS^T q
+ * in fp32 sums; dk and dv are summed over the query heads that share a key head.
+ * In bf16, P and dS enter the products rounded to bf16.  Gradients overlap neither
+ * operands nor each other (they may be columns of one matrix).  Deterministic: no
+ * sum depends on the order in which parts finish. */
+acid_status acid_mha_backward(const acid_mha* mha, const void* dout, int64_t lddo, const void* q, int64_t ldq,
+                              const void* k, int64_t ldk, const void* v, int64_t ldv, const void* out, int64_t ldo,
+                              const float* lse, const acid_mha_grads* grads, void* workspace, size_t workspace_bytes,
+                              acid_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
 /* Norm sites: the gate, residual, norms and modulation between two branches */
 /* ------------------------------------------------------------------------ */
 

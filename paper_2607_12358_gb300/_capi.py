@@ -97,7 +97,26 @@ class acid_q4_weight(C.Structure):
                 ("group", C.c_int32), ("scale_dtype", C.c_int32)]
 
 
+class acid_rope(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("axes", C.c_int32), ("axis_dim", C.c_int32 * 4), ("theta", C.c_float * 4), ("halves", C.c_int32),
+                ("first_rows", C.c_int64), ("positions", _P), ("ld_pos", C.c_int64), ("grid", C.c_int32 * 4),
+                ("origin", C.c_float * 4)]
+
+
+class acid_mha(C.Structure):
+    _fields_ = [("nq", C.c_int64), ("nk", C.c_int64), ("dtype", C.c_int32), ("heads", C.c_int32),
+                ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("scale", C.c_float), ("sequences", C.c_int32),
+                ("q_bounds", _P), ("k_bounds", _P), ("frame_rows", C.c_int64), ("frames_before", C.c_int32),
+                ("frames_after", C.c_int32), ("q_first", C.c_int64)]
+
+
+class acid_mha_grads(C.Structure):
+    _fields_ = [("dq", _P), ("lddq", C.c_int64), ("dk", _P), ("lddk", C.c_int64), ("dv", _P), ("lddv", C.c_int64)]
+
+
 _SITE, _GRADS, _Q4 = C.POINTER(acid_norm_site), C.POINTER(acid_norm_site_grads), C.POINTER(acid_q4_weight)
+_ROPE, _MHA, _MHA_GRADS = C.POINTER(acid_rope), C.POINTER(acid_mha), C.POINTER(acid_mha_grads)
 _PROTOS = {
     "acid_last_error": (C.c_char_p, []),
     "acid_version": (C.c_char_p, []),
@@ -122,6 +141,14 @@ _PROTOS = {
                                          C.c_int64, C.c_int64, C.c_int32, C.c_int32, _P, C.c_size_t, _P]),
     "acid_attention_workspace_size": (C.c_int, [C.c_int32, C.POINTER(C.c_size_t)]),
     "acid_layernorm_mod": (C.c_int, [C.c_int32, _P, C.c_int32, _P, C.c_int64, C.c_int32, _P, _P, C.c_float, _P]),
+    "acid_rope_forward": (C.c_int, [_ROPE, _P, C.c_int64, _P, C.c_int64, _P]),
+    "acid_rope_backward": (C.c_int, [_ROPE, _P, C.c_int64, _P, C.c_int64, _P]),
+    "acid_mha_forward_workspace_size": (C.c_int, [_MHA, C.POINTER(C.c_size_t)]),
+    "acid_mha_backward_workspace_size": (C.c_int, [_MHA, C.POINTER(C.c_size_t)]),
+    "acid_mha_forward": (C.c_int, [_MHA, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P, _P,
+                                   C.c_size_t, _P]),
+    "acid_mha_backward": (C.c_int, [_MHA, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64,
+                                    _P, _MHA_GRADS, _P, C.c_size_t, _P]),
     "acid_norm_site_groups": (C.c_int, [_SITE, C.POINTER(C.c_int64)]),
     "acid_norm_site_forward": (C.c_int, [_SITE, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P]),
     "acid_norm_site_workspace_size": (C.c_int, [_SITE, C.POINTER(C.c_size_t)]),

@@ -456,6 +456,210 @@ def acid_norm_site_backward(du: torch.Tensor | None, r: torch.Tensor | None, y: 
 
 
 # ---------------------------------------------------------------------------
+# rotary positions with several axes
+# ---------------------------------------------------------------------------
+
+def _rope(call, x, heads, axes, theta, grid, origin, positions, first_rows, halves, out, stream):
+    empty = _empty_on(stream)
+    if x.dim() != 2 or x.dtype not in _DT:
+        raise ValueError("need a [rows, heads * head_dim] tensor of bf16 or fp32")
+    rows, width = x.shape
+    if heads < 1 or width % heads:
+        raise ValueError("the columns must be heads of one head_dim")
+    n = len(axes)
+    if not 1 <= n <= 4:
+        raise ValueError("need 1 to 4 axes")
+    thetas = (theta,) * n if isinstance(theta, (int, float)) else tuple(theta)
+    origin = (0.0,) * n if origin is None else tuple(origin)
+    if (grid is None) == (positions is None):
+        raise ValueError("need either grid or positions")
+    if len(thetas) != n or len(origin) != n or (grid is not None and len(grid) != n):
+        raise ValueError(f"theta, grid and origin must have {n} entries, as axes has")
+    pp, ld_pos = None, 0
+    if positions is not None:
+        ld_pos, pp = _rows_of("positions", positions, rows, n, _F32), positions.data_ptr()
+        grid = ()
+    ldx = _rows_of("x", x, rows, width, x.dtype)
+    if out is None:
+        out, ldo = empty((rows, width), dtype=x.dtype, device=x.device), width
+    else:
+        ldo = _rows_of("out", out, rows, width, x.dtype)
+    i4, f4 = C.c_int32 * 4, C.c_float * 4
+    desc = A.acid_rope(rows, heads, width // heads, _DT[x.dtype], n, i4(*axes), f4(*thetas), halves, first_rows, pp,
+                       ld_pos, i4(*grid), f4(*origin))
+    status = call(C.byref(desc), x.data_ptr(), ldx, out.data_ptr(), ldo, _stream(stream))
+    if status:
+        check(status)
+    return out
+
+
+def acid_rope_forward(x: torch.Tensor, heads: int, axes, *, theta=10000.0, grid=None, origin=None,
+                      positions: torch.Tensor | None = None, first_rows: int = 0, halves: bool = False,
+                      out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """x [rows, heads * head_dim] with every head's columns turned by the row's position along each axis: ``axes`` columns
+    an axis, frequencies theta^(-2j / columns) (one theta or one for each axis).  Positions are those of ``grid`` (row-major
+    over the rows from ``first_rows`` on, repeated, plus ``origin``) or ``positions`` fp32 [rows, axes].  ``halves`` pairs
+    column p with p + half of the turned ones instead of 2p with 2p + 1.  out may be x."""
+    return _rope(load().acid_rope_forward, x, heads, axes, theta, grid, origin, positions, first_rows, halves, out, stream)
+
+
+def acid_rope_backward(dout: torch.Tensor, heads: int, axes, *, theta=10000.0, grid=None, origin=None,
+                       positions: torch.Tensor | None = None, first_rows: int = 0, halves: bool = False,
+                       out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The gradient of acid_rope_forward's x from that of its output: the rotation taken back.  out may be dout."""
+    return _rope(load().acid_rope_backward, dout, heads, axes, theta, grid, origin, positions, first_rows, halves, out,
+                 stream)
+
+
+# ---------------------------------------------------------------------------
+# attention with row sums, and its gradient
+# ---------------------------------------------------------------------------
+
+def sequence_bounds(lengths, room: int = 0, device="cuda") -> torch.Tensor:
+    """int32 [sequences, 2] of first rows and rows past the last: sequences of these lengths one after the other, or each
+    at the start of ``room`` rows."""
+    out, at = [], 0
+    for n in lengths:
+        if n < 0 or (room and n > room):
+            raise ValueError("lengths must be >= 0 and fit the room")
+        out.append((at, at + n))
+        at += room or n
+    return torch.tensor(out, dtype=torch.int32).reshape(len(out), 2).to(device)
+
+
+def _mha_desc(q, k, heads, scale, q_bounds, k_bounds, frame_rows, frames_before, frames_after, q_first):
+    """(C description, query columns, key columns)."""
+    if q.dim() != 2 or k.dim() != 2 or q.dtype not in _DT:
+        raise ValueError("q and k must be [rows, heads * head_dim] tensors of bf16 or fp32")
+    if heads < 1 or q.shape[1] % heads or q.shape[1] == 0:
+        raise ValueError("the columns of q must be heads of one head_dim")
+    d = q.shape[1] // heads
+    kv_heads = k.shape[1] // d
+    if kv_heads < 1 or k.shape[1] != kv_heads * d or heads % kv_heads:
+        raise ValueError("the columns of k must be heads of q's head_dim, whose number divides heads")
+    seqs, ptrs = 1, [None, None]
+    for i, (name, b) in enumerate((("q_bounds", q_bounds), ("k_bounds", k_bounds))):
+        if b is None:
+            continue
+        if b.dtype is not torch.int32 or not b.is_cuda or b.dim() != 2 or b.shape[1] != 2 or not b.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous CUDA int32 tensor [sequences, 2]")
+        seqs, ptrs[i] = b.shape[0], b.data_ptr()
+    if q_bounds is not None and k_bounds is not None and q_bounds.shape != k_bounds.shape:
+        raise ValueError("q_bounds and k_bounds must have as many sequences")
+    return A.acid_mha(q.shape[0], k.shape[0], _DT[q.dtype], heads, kv_heads, d, d ** -0.5 if scale is None else scale, seqs,
+                      ptrs[0], ptrs[1], frame_rows, frames_before, frames_after, q_first), heads * d, kv_heads * d
+
+
+def mha_workspace_size(desc: A.acid_mha, backward: bool = False) -> int:
+    b = C.c_size_t()
+    f = load().acid_mha_backward_workspace_size if backward else load().acid_mha_forward_workspace_size
+    check(f(C.byref(desc), C.byref(b)))
+    return b.value
+
+
+def mha_workspace(q: torch.Tensor, k: torch.Tensor, heads: int, *, backward: bool = False,
+                  q_bounds: torch.Tensor | None = None, k_bounds: torch.Tensor | None = None) -> torch.Tensor:
+    """A workspace for acid_mha_forward or acid_mha_backward of operands of these shapes, with any window of frames."""
+    if k_bounds is None and q_bounds is not None:
+        k_bounds = q_bounds  # the size goes by their number
+    desc, _, _ = _mha_desc(q, k, heads, None, q_bounds, k_bounds, 0, -1, -1, 0)
+    return torch.empty(mha_workspace_size(desc, backward), dtype=torch.uint8, device=q.device)
+
+
+def _blank_on(stream, bounded):
+    """Allocates results: zeros where sequences may leave rows unwritten."""
+    empty = _empty_on(stream)
+    if not bounded:
+        return empty
+
+    def zeros(*size, **how):
+        t = empty(*size, **how)
+        if stream is None:
+            return t.zero_()
+        handle = _stream(stream)
+        with torch.cuda.stream(torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()):
+            return t.zero_()
+
+    return zeros
+
+
+def acid_mha_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, heads: int, *, scale: float | None = None,
+                     q_bounds: torch.Tensor | None = None, k_bounds: torch.Tensor | None = None, frame_rows: int = 0,
+                     frames_before: int = -1, frames_after: int = -1, q_first: int = 0, out: torch.Tensor | None = None,
+                     lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
+    """(out, lse): out = softmax(scale q k^T) v over each row's visible keys, lse fp32 [heads, nq] the logarithm of its sum.
+    q [nq, heads * head_dim], k, v [nk, kv_heads * head_dim] (head_dim is q's; scale 1 / sqrt(head_dim) unless given);
+    bounds int32 [sequences, 2] (sequence_bounds); with frame_rows, a row at position i + q_first (-1: the last query at
+    the last key) sees frames_before frames before its own and frames_after after it (-1: all).  out and lse are
+    allocated unless given (rows of no sequence are then 0)."""
+    desc, wq, wk = _mha_desc(q, k, heads, scale, q_bounds, k_bounds, frame_rows, frames_before, frames_after, q_first)
+    nq, nk, dt = q.shape[0], k.shape[0], q.dtype
+    ldq, ldk, ldv = _rows_of("q", q, nq, wq, dt), _rows_of("k", k, nk, wk, dt), _rows_of("v", v, nk, wk, dt)
+    blank, ldo = _blank_on(stream, q_bounds is not None), wq
+    if out is None:
+        out = blank((nq, wq), dtype=dt, device=q.device)
+    else:
+        ldo = _rows_of("out", out, nq, wq, dt)
+    if lse is None:
+        lse = blank((heads, nq), dtype=_F32, device=q.device)
+    elif lse.dtype is not _F32 or not lse.is_cuda or lse.shape != (heads, nq) or not lse.is_contiguous():
+        raise ValueError(f"lse must be a contiguous CUDA fp32 tensor [{heads}, {nq}]")
+    ws = nws = 0
+    if workspace is not None:
+        ws, nws = _workspace(workspace)
+    else:
+        nws = mha_workspace_size(desc)
+        if nws:
+            workspace = _empty_on(stream)(nws, dtype=torch.uint8, device=q.device)
+            ws = workspace.data_ptr()
+    status = load().acid_mha_forward(C.byref(desc), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
+                                     out.data_ptr(), ldo, lse.data_ptr(), ws, nws, _stream(stream))
+    if status:
+        check(status)
+    return out, lse
+
+
+def acid_mha_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                      lse: torch.Tensor, heads: int, *, scale: float | None = None, q_bounds: torch.Tensor | None = None,
+                      k_bounds: torch.Tensor | None = None, frame_rows: int = 0, frames_before: int = -1,
+                      frames_after: int = -1, q_first: int = 0, dq: torch.Tensor | None = None,
+                      dk: torch.Tensor | None = None, dv: torch.Tensor | None = None, want=("q", "k", "v"),
+                      workspace: torch.Tensor | None = None, stream=None):
+    """(dq, dk, dv) of acid_mha_forward from dout, that of out, with the forward call's operands, results and other
+    arguments.  Gradients are allocated unless given (rows of no sequence are then 0); those not in ``want`` are None."""
+    desc, wq, wk = _mha_desc(q, k, heads, scale, q_bounds, k_bounds, frame_rows, frames_before, frames_after, q_first)
+    nq, nk, dt = q.shape[0], k.shape[0], q.dtype
+    ldg, ldq, ldo = _rows_of("dout", dout, nq, wq, dt), _rows_of("q", q, nq, wq, dt), _rows_of("out", out, nq, wq, dt)
+    ldk, ldv = _rows_of("k", k, nk, wk, dt), _rows_of("v", v, nk, wk, dt)
+    if lse.dtype is not _F32 or not lse.is_cuda or lse.shape != (heads, nq) or not lse.is_contiguous():
+        raise ValueError(f"lse must be a contiguous CUDA fp32 tensor [{heads}, {nq}]")
+    grads, fields = [], []
+    for name, given, rows, width, bounded in (("q", dq, nq, wq, q_bounds is not None),
+                                              ("k", dk, nk, wk, k_bounds is not None),
+                                              ("v", dv, nk, wk, k_bounds is not None)):
+        ld = width
+        if given is not None:
+            ld = _rows_of("d" + name, given, rows, width, dt)
+        elif name in want:
+            given = _blank_on(stream, bounded)((rows, width), dtype=dt, device=q.device)
+        grads.append(given)
+        fields += [_ptr(given), ld]
+    if workspace is not None:
+        ws, nws = _workspace(workspace)
+    else:
+        nws = mha_workspace_size(desc, True)
+        workspace = _empty_on(stream)(nws, dtype=torch.uint8, device=q.device)
+        ws = workspace.data_ptr()
+    fields = A.acid_mha_grads(*fields)
+    status = load().acid_mha_backward(C.byref(desc), dout.data_ptr(), ldg, q.data_ptr(), ldq, k.data_ptr(), ldk,
+                                      v.data_ptr(), ldv, out.data_ptr(), ldo, lse.data_ptr(), C.byref(fields), ws, nws,
+                                      _stream(stream))
+    if status:
+        check(status)
+    return tuple(grads)
+
+
+# ---------------------------------------------------------------------------
 # modulation projections with 4-bit weights
 # ---------------------------------------------------------------------------
 

@@ -23,6 +23,9 @@ BoundsRecord take_bounds_site();
 BoundsRecord take_bounds_q4();
 unsigned int take_device_error_q4_rows();
 BoundsRecord take_bounds_q4_rows();
+BoundsRecord take_bounds_rope();
+BoundsRecord take_bounds_mha();
+BoundsRecord take_bounds_mha_f32();
 
 namespace {
 thread_local std::string t_last_error;
@@ -226,8 +229,9 @@ extern "C" acid_status acid_bounds_report(int32_t* checked, int64_t* site, int64
   clear_error();
   ACID_REQUIRE(checked && site && index && extent, ACID_ERR_INVALID_ARG, "acid_bounds_report: null argument");
   ACID_CUDA(cudaDeviceSynchronize());
-  const BoundsRecord recs[7] = {take_bounds_elementwise(), take_bounds_gemm(), take_bounds_attention(), take_bounds_site(),
-                                take_bounds_q4(),          take_bounds_q4_rows(), take_bounds_capi()};
+  const BoundsRecord recs[] = {take_bounds_elementwise(), take_bounds_gemm(), take_bounds_attention(), take_bounds_site(),
+                               take_bounds_q4(),          take_bounds_q4_rows(), take_bounds_rope(), take_bounds_mha(),
+                               take_bounds_mha_f32(),     take_bounds_capi()};
   *checked = kBoundsChecked ? 1 : 0;
   *site = *index = *extent = 0;
   for (const BoundsRecord& r : recs) {

@@ -1,0 +1,130 @@
+// What the kernels of acid_mha_forward and acid_mha_backward share: the shape of
+// a call as the device sees it, its sequences, and which rows see which.
+#pragma once
+
+#include <stdint.h>
+
+#include "common.cuh"
+#include "internal.h"
+
+namespace acid {
+
+// Rows are 32-bit (at most kMhaMaxRows); offsets into matrices are 64-bit.
+constexpr int64_t kMhaMaxRows = (int64_t)1 << 30;
+constexpr int kStatRows = 128;  // query rows of a slot of the row statistics (MhaStats)
+
+struct MhaShape {
+  int nq, nk, heads, kv_heads, group;  // group: query heads that share a key head
+  int seqs;
+  const int2 *qb, *kb;  // [seqs] {first row, row past the last}; null: all rows
+  int frame, before, after, q_first;
+};
+
+// One sequence's rows: queries [q0, q0 + nq), keys [k0, k0 + nk).
+struct MhaSeq {
+  int q0, nq, k0, nk;
+};
+
+// A bound as the device reads it: inside the matrix and in order, whatever the
+// array holds, so that no access leaves the operands.
+__device__ __forceinline__ void mha_bound(const int2* b, int i, int n, int& first, int& rows) {
+  const int2 v = b != nullptr ? __ldg(b + i) : make_int2(0, n);
+  first = min(max(v.x, 0), n);
+  rows = min(max(v.y, first), n) - first;
+}
+__device__ __forceinline__ MhaSeq mha_seq(const MhaShape& s, int i) {
+  MhaSeq q;
+  mha_bound(s.qb, i, s.nq, q.q0, q.nq);
+  mha_bound(s.kb, i, s.nk, q.k0, q.nk);
+  return q;
+}
+
+// Slots of tiles of `tile` rows.  Sequence i begins at slot first / tile + i, so
+// that each has as many slots as it can need (and one may stay empty) without a
+// table or a scan of the lengths before it: ceil(len / tile) <=
+// (first + len) / tile - first / tile + 1.
+__host__ __device__ __forceinline__ int mha_slots(int rows, int seqs, bool bounded, int tile) {
+  return bounded ? rows / tile + seqs : (rows + tile - 1) / tile;
+}
+// First slot of sequence i, whose first row is `first`.
+__device__ __forceinline__ int mha_slot0(const int2* b, int i, int first, int tile) {
+  return b != nullptr ? first / tile + i : 0;
+}
+// The sequence and its tile at a slot of the queries or keys; false: an empty slot.
+template <int TILE, bool KEYS>
+__device__ __forceinline__ bool mha_slot(const MhaShape& s, int slot, MhaSeq& seq, int& index, int& tile) {
+  const int2* b = KEYS ? s.kb : s.qb;
+  int lo = 0;
+  if (b != nullptr) {
+    const int n = KEYS ? s.nk : s.nq;
+    for (int hi = s.seqs; hi - lo > 1;) {
+      const int mid = (lo + hi) >> 1;
+      if (min(max(__ldg(b + mid).x, 0), n) / TILE + mid <= slot) lo = mid;
+      else hi = mid;
+    }
+  }
+  index = lo;
+  seq = mha_seq(s, lo);
+  tile = slot - mha_slot0(b, lo, KEYS ? seq.k0 : seq.q0, TILE);
+  const int rows = KEYS ? seq.nk : seq.nq;
+  return tile >= 0 && tile < (rows + TILE - 1) / TILE;
+}
+
+__device__ __forceinline__ int floor_div(int a, int b) { return a >= 0 ? a / b : -((b - 1 - a) / b); }
+__device__ __forceinline__ int clamp_row(int64_t v, int n) { return (int)min(max(v, (int64_t)0), (int64_t)n); }
+
+// Position of a sequence's first query among its keys.
+__device__ __forceinline__ int mha_first(const MhaShape& s, const MhaSeq& q) {
+  return s.q_first >= 0 ? s.q_first : q.nk - q.nq;
+}
+// Keys [lo, hi) of the sequence that its query row i sees, and queries [lo, hi)
+// that see its key row j.  Both bounds grow with the row.
+__device__ __forceinline__ void mha_keys_of(const MhaShape& s, const MhaSeq& q, int i, int& lo, int& hi) {
+  lo = 0;
+  hi = q.nk;
+  if (s.frame == 0) return;
+  const int64_t at = floor_div(i + mha_first(s, q), s.frame);
+  if (s.before >= 0) lo = clamp_row((at - s.before) * s.frame, q.nk);
+  if (s.after >= 0) hi = clamp_row((at + s.after + 1) * s.frame, q.nk);
+}
+__device__ __forceinline__ void mha_queries_of(const MhaShape& s, const MhaSeq& q, int j, int& lo, int& hi) {
+  lo = 0;
+  hi = q.nq;
+  if (s.frame == 0) return;
+  const int64_t at = j / s.frame, first = mha_first(s, q);
+  if (s.after >= 0) lo = clamp_row((at - s.after) * s.frame - first, q.nq);
+  if (s.before >= 0) hi = clamp_row((at + s.before + 1) * s.frame - first, q.nq);
+}
+
+// Row statistics of the backward pass, [heads][slots][2][kStatRows] floats: -lse
+// (in the unit of the kernels' exponential) and the sum of dout out over the head's
+// columns.  Rows past a sequence's end and rows that see no key hold -inf and 0,
+// which makes their probabilities 0.
+__host__ __device__ __forceinline__ int64_t mha_stat_offset(int head, int slots, int slot) {
+  return ((int64_t)head * slots + slot) * (2 * kStatRows);
+}
+
+// A call of either direction.
+struct MhaArgs {
+  MhaShape shape;
+  int dtype, head_dim;
+  float scale;
+  const void *q, *k, *v;
+  int64_t ldq, ldk, ldv;
+  void* out;  // forward: written; backward: read
+  int64_t ldo;
+  float* lse;
+  const void* dout;
+  int64_t lddo;
+  void *dq, *dk, *dv;
+  int64_t lddq, lddk, lddv;
+  float* stats;
+  void* part;
+  size_t part_bytes;
+};
+
+// mha_f32.cu: the FP32 pipes
+acid_status mha_forward_simt(const MhaArgs& a, cudaStream_t s);
+acid_status mha_backward_simt(const MhaArgs& a, cudaStream_t s);
+
+}  // namespace acid
