@@ -128,7 +128,9 @@ MhaArgs common_args(const acid_mha& m) {
 int stat_slots(const acid_mha& m) { return mha_slots((int)m.nq, m.sequences, m.q_bounds != nullptr, kStatRows); }
 size_t stat_bytes(const acid_mha& m) { return (size_t)mha_stat_offset(m.heads, stat_slots(m), 0) * sizeof(float); }
 
-size_t forward_bytes(const acid_mha&) { return 0; }
+size_t forward_bytes(const acid_mha& m) {
+  return m.dtype == ACID_BF16 && m.nq > 0 ? mha_forward_tc_bytes(common_args(m)) : 0;
+}
 size_t backward_bytes(const acid_mha& m) { return stat_bytes(m); }
 
 acid_status check_workspace(const void* ws, size_t bytes, size_t need, const char* call) {
@@ -186,7 +188,7 @@ extern "C" acid_status acid_mha_forward(const acid_mha* mha, const void* q, int6
   a.lse = lse;
   a.part = ws;
   a.part_bytes = ws_bytes;
-  return mha_forward_simt(a, (cudaStream_t)stream);
+  return m.dtype == ACID_BF16 ? mha_forward_tc(a, (cudaStream_t)stream) : mha_forward_simt(a, (cudaStream_t)stream);
 }
 
 extern "C" acid_status acid_mha_backward(const acid_mha* mha, const void* dout, int64_t lddo, const void* q, int64_t ldq,
