@@ -27,7 +27,8 @@ BUILD_DEBUG = os.path.join(PKG, "_build_debug")
 LIB_DEBUG = os.path.join(PKG, "libacid_gb300_debug.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["capi.cu", "elementwise.cu", "gemm.cu", "attention.cu", "block.cu", "loop.cu", "site.cu", "q4.cu", "q4_rows.cu",
-           "rope.cu", "mha.cu", "mha_f32.cu", "mha_forward.cu", "noalloc.cu"]
+           "rope.cu", "mha.cu", "mha_f32.cu", "mha_forward.cu", "mha_backward.cu",
+           "noalloc.cu"]
 
 
 def nvcc() -> str:

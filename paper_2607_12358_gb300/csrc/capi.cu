@@ -28,6 +28,8 @@ BoundsRecord take_bounds_mha();
 BoundsRecord take_bounds_mha_f32();
 BoundsRecord take_bounds_mha_forward();
 unsigned int take_device_error_mha_forward();
+BoundsRecord take_bounds_mha_backward();
+unsigned int take_device_error_mha_backward();
 
 namespace {
 thread_local std::string t_last_error;
@@ -233,7 +235,8 @@ extern "C" acid_status acid_bounds_report(int32_t* checked, int64_t* site, int64
   ACID_CUDA(cudaDeviceSynchronize());
   const BoundsRecord recs[] = {take_bounds_elementwise(), take_bounds_gemm(), take_bounds_attention(), take_bounds_site(),
                                take_bounds_q4(),          take_bounds_q4_rows(), take_bounds_rope(), take_bounds_mha(),
-                               take_bounds_mha_f32(),     take_bounds_mha_forward(), take_bounds_capi()};
+                               take_bounds_mha_f32(),     take_bounds_mha_forward(),
+                               take_bounds_mha_backward(), take_bounds_capi()};
   *checked = kBoundsChecked ? 1 : 0;
   *site = *index = *extent = 0;
   for (const BoundsRecord& r : recs) {
@@ -276,7 +279,7 @@ extern "C" acid_status acid_check_device_error(void) {
   ACID_CUDA(cudaDeviceSynchronize());
   const unsigned int flag = take_device_error_elementwise() | take_device_error_gemm() |
                             take_device_error_attention() | take_device_error_q4_rows() | take_device_error_mha_forward() |
-                            take_device_error_capi();
+                            take_device_error_mha_backward() | take_device_error_capi();
   if (flag) {
     set_error("a bounded device-side wait timed out");
     return ACID_ERR_TIMEOUT;

@@ -75,6 +75,8 @@ acid_status check_mha(const acid_mha* m) {
   else
     ACID_REQUIRE(m->head_dim > 0 && m->head_dim % 32 == 0 && m->head_dim <= 128, ACID_ERR_UNSUPPORTED,
                  "mha fp32: head_dim must be 32, 64, 96 or 128");
+  ACID_REQUIRE((std::max(m->nq, m->nk) / 128 + 65536) * m->heads <= (int64_t)1 << 32, ACID_ERR_UNSUPPORTED,
+               "mha: too many rows and heads");
   ACID_REQUIRE(isfinite(m->scale), ACID_ERR_INVALID_ARG, "mha: scale must be finite");
   ACID_REQUIRE(m->sequences >= 1 && m->sequences <= 65535, ACID_ERR_INVALID_ARG, "mha: need 1 to 65535 sequences");
   ACID_REQUIRE(m->sequences == 1 || (m->q_bounds != nullptr && m->k_bounds != nullptr), ACID_ERR_INVALID_ARG,
@@ -131,7 +133,9 @@ size_t stat_bytes(const acid_mha& m) { return (size_t)mha_stat_offset(m.heads, s
 size_t forward_bytes(const acid_mha& m) {
   return m.dtype == ACID_BF16 && m.nq > 0 ? mha_forward_tc_bytes(common_args(m)) : 0;
 }
-size_t backward_bytes(const acid_mha& m) { return stat_bytes(m); }
+size_t backward_bytes(const acid_mha& m) {
+  return stat_bytes(m) + (m.dtype == ACID_BF16 ? mha_backward_tc_bytes(common_args(m)) : 0);
+}
 
 acid_status check_workspace(const void* ws, size_t bytes, size_t need, const char* call) {
   if (need == 0) return ACID_OK;
@@ -188,7 +192,7 @@ extern "C" acid_status acid_mha_forward(const acid_mha* mha, const void* q, int6
   a.lse = lse;
   a.part = ws;
   a.part_bytes = ws_bytes;
-  return m.dtype == ACID_BF16 ? mha_forward_tc(a, (cudaStream_t)stream) : mha_forward_simt(a, (cudaStream_t)stream);
+  return m.dtype == ACID_BF16 ? mha_forward_tc(a, (cudaStream_t)stream) : mha_forward_f32(a, (cudaStream_t)stream);
 }
 
 extern "C" acid_status acid_mha_backward(const acid_mha* mha, const void* dout, int64_t lddo, const void* q, int64_t ldq,
@@ -234,13 +238,15 @@ extern "C" acid_status acid_mha_backward(const acid_mha* mha, const void* dout, 
   a.dv = m.nk > 0 ? o.dv : nullptr;
   a.lddv = o.lddv;
   a.stats = static_cast<float*>(ws);
+  a.part = static_cast<uint8_t*>(ws) + stat_bytes(m);
   if (m.nq > 0) {
-    const StatArgs t{a.shape, out, dout, ldo, lddo, lse, a.stats, m.head_dim, stat_slots(m), 1.0f};
+    const StatArgs t{a.shape, out, dout, ldo, lddo, lse, a.stats, m.head_dim, stat_slots(m),
+                     m.dtype == ACID_BF16 ? 1.4426950408889634f : 1.0f};
     int lanes = 4;
     while (lanes * 8 < m.head_dim) lanes *= 2;
     launch_pdl(m.dtype == ACID_BF16 ? mha_stats_kernel<__nv_bfloat16> : mha_stats_kernel<float>,
                dim3(t.slots, m.heads), kThreads, 0, s, t, lanes);
     ACID_CHECK_LAUNCH();
   }
-  return mha_backward_simt(a, s);
+  return m.dtype == ACID_BF16 ? mha_backward_tc(a, s) : mha_backward_f32(a, s);
 }

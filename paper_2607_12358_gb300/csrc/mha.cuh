@@ -126,8 +126,11 @@ struct MhaArgs {
 // mha_forward.cu: bf16 on tcgen05.  Bytes of scratch (part) that the call needs.
 size_t mha_forward_tc_bytes(const MhaArgs& a);
 acid_status mha_forward_tc(const MhaArgs& a, cudaStream_t s);
+// mha_backward.cu: the same of the gradient.
+size_t mha_backward_tc_bytes(const MhaArgs& a);
+acid_status mha_backward_tc(const MhaArgs& a, cudaStream_t s);
 // mha_f32.cu: the FP32 pipes
-acid_status mha_forward_simt(const MhaArgs& a, cudaStream_t s);
-acid_status mha_backward_simt(const MhaArgs& a, cudaStream_t s);
+acid_status mha_forward_f32(const MhaArgs& a, cudaStream_t s);
+acid_status mha_backward_f32(const MhaArgs& a, cudaStream_t s);
 
 }  // namespace acid

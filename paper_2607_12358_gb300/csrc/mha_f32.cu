@@ -13,10 +13,10 @@ namespace {
 
 constexpr int kGroups = 4, kCols = 32, kThreads = 128 * kGroups;  // groups of four warps; rows of a streamed tile
 
-// N rows of D values of T as fp32 (row stride lds in shared memory); rows outside
-// [0, valid) are zeros.
-template <typename T, int D, int N>
-__device__ __forceinline__ void load_rows(float* dst, int lds, const T* src, int64_t ld, int valid, int tid,
+// N rows of D values (row stride lds in shared memory); rows outside [0, valid) are
+// zeros.
+template <int D, int N>
+__device__ __forceinline__ void load_rows(float* dst, int lds, const float* src, int64_t ld, int valid, int tid,
                                           int threads) {
   for (int i = tid; i < N * (D / 8); i += threads) {
     const int r = i / (D / 8), c = (i % (D / 8)) * 8;
@@ -69,7 +69,7 @@ __device__ __forceinline__ void accumulate(const float* p, int ldp, const float*
   }
 }
 
-struct SimtArgs {
+struct F32Args {
   MhaShape s;
   const void *q, *k, *v, *o, *dout;
   int64_t ldq, ldk, ldv, ldo, lddo;
@@ -81,7 +81,7 @@ struct SimtArgs {
 };
 
 template <int D, int ROWS, int NSTREAM, int NP>
-struct SimtCfg {
+struct F32Cfg {
   static constexpr int LD = D + 4, LDP = kCols + 4;
   static constexpr int OFF_STREAM = 2 * ROWS * LD;                        // after the two stationary tiles
   static constexpr int STREAM = NSTREAM * kCols * LD + NP * ROWS * LDP + 2 * kCols;  // of one group
@@ -92,10 +92,10 @@ struct SimtCfg {
 // A CTA has 16 query rows of a head; its groups of four warps walk the key tiles
 // in turn with a running maximum and sum each, and their parts are joined through
 // shared memory.  A half-warp has two rows.
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) mha_forward_simt_kernel(const SimtArgs a) {
+template <int D>
+__global__ void __launch_bounds__(kThreads) mha_forward_f32_kernel(const F32Args a) {
   constexpr int ROWS = 16, R = 2;
-  using C = SimtCfg<D, ROWS, 2, 1>;
+  using C = F32Cfg<D, ROWS, 2, 1>;
   extern __shared__ __align__(16) float sm[];
   pdl_wait();
   const int g = threadIdx.x >> 7, t = threadIdx.x & 127, hw = t >> 4, kg = t & 15;
@@ -108,10 +108,10 @@ __global__ void __launch_bounds__(kThreads) mha_forward_simt_kernel(const SimtAr
   float* sk = sm + C::OFF_STREAM + g * C::STREAM;
   float* sv = sk + kCols * C::LD;
   float* sp = sv + kCols * C::LD + hw * R * C::LDP;
-  const T* q = static_cast<const T*>(a.q) + (int64_t)(seq.q0 + r0) * a.ldq + h * D;
-  const T* k = static_cast<const T*>(a.k) + (int64_t)seq.k0 * a.ldk + hk * D;
-  const T* v = static_cast<const T*>(a.v) + (int64_t)seq.k0 * a.ldv + hk * D;
-  load_rows<T, D, ROWS>(sq, C::LD, q, a.ldq, rows, threadIdx.x, kThreads);
+  const float* q = static_cast<const float*>(a.q) + (int64_t)(seq.q0 + r0) * a.ldq + h * D;
+  const float* k = static_cast<const float*>(a.k) + (int64_t)seq.k0 * a.ldk + hk * D;
+  const float* v = static_cast<const float*>(a.v) + (int64_t)seq.k0 * a.ldv + hk * D;
+  load_rows<D, ROWS>(sq, C::LD, q, a.ldq, rows, threadIdx.x, kThreads);
   __syncthreads();
   int lo[R], hi[R], first, last, none;
   mha_keys_of(a.s, seq, r0, first, none);
@@ -126,8 +126,8 @@ __global__ void __launch_bounds__(kThreads) mha_forward_simt_kernel(const SimtAr
   }
   for (int j = first / kCols + g; j * kCols < last; j += kGroups) {
     group_sync(1 + g, 128);  // the tiles before have been read
-    load_rows<T, D, kCols>(sk, C::LD, k + (int64_t)j * kCols * a.ldk, a.ldk, seq.nk - j * kCols, t, 128);
-    load_rows<T, D, kCols>(sv, C::LD, v + (int64_t)j * kCols * a.ldv, a.ldv, seq.nk - j * kCols, t, 128);
+    load_rows<D, kCols>(sk, C::LD, k + (int64_t)j * kCols * a.ldk, a.ldk, seq.nk - j * kCols, t, 128);
+    load_rows<D, kCols>(sv, C::LD, v + (int64_t)j * kCols * a.ldv, a.ldv, seq.nk - j * kCols, t, 128);
     group_sync(1 + g, 128);
     float s[R][2];
     products<D, R>(sq + hw * R * C::LD, sk, C::LD, kg, s);
@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(kThreads) mha_forward_simt_kernel(const SimtAr
     }
     const int64_t row = seq.q0 + r0 + r, at = row * a.ld1 + h * D + c;
     if (!ACID_IN_BOUNDS(kSiteMha, at, (int64_t)a.s.nq * a.ld1)) continue;
-    io<T>::st(static_cast<T*>(a.out1) + at, den > 0.f ? acc / den : den == 0.f ? 0.f : den);
+    static_cast<float*>(a.out1)[at] = den > 0.f ? acc / den : den == 0.f ? 0.f : den;
     if (c == 0) a.lse[(int64_t)h * a.s.nq + row] = den == 0.f ? -INFINITY : mx + logf(den);
   }
 }
@@ -199,10 +199,10 @@ __global__ void __launch_bounds__(kThreads) mha_forward_simt_kernel(const SimtAr
 //          group: rows are keys, columns queries; dk += ds^T q, dv += p^T dout;
 //   else   keeps q and dout, streams keys and values: dq += ds k.
 // The groups of four warps take the tiles in turn and their sums are joined in order.
-template <typename T, int D, bool KEYS>
-__global__ void __launch_bounds__(kThreads) mha_backward_simt_kernel(const SimtArgs a) {
+template <int D, bool KEYS>
+__global__ void __launch_bounds__(kThreads) mha_backward_f32_kernel(const F32Args a) {
   constexpr int ROWS = 16, R = 2;
-  using C = SimtCfg<D, ROWS, 2, 2>;
+  using C = F32Cfg<D, ROWS, 2, 2>;
   extern __shared__ __align__(16) float sm[];
   pdl_wait();
   const int g = threadIdx.x >> 7, t = threadIdx.x & 127, hw = t >> 4, kg = t & 15;
@@ -219,16 +219,16 @@ __global__ void __launch_bounds__(kThreads) mha_backward_simt_kernel(const SimtA
   float* sp = y2 + kCols * C::LD;
   float* sd = sp + ROWS * C::LDP;
   float* st = sd + ROWS * C::LDP;  // KEYS: the streamed rows' statistics
-  const T* q = static_cast<const T*>(a.q) + (int64_t)seq.q0 * a.ldq;
-  const T* k = static_cast<const T*>(a.k) + (int64_t)seq.k0 * a.ldk;
-  const T* v = static_cast<const T*>(a.v) + (int64_t)seq.k0 * a.ldv;
-  const T* dout = static_cast<const T*>(a.dout) + (int64_t)seq.q0 * a.lddo;
+  const float* q = static_cast<const float*>(a.q) + (int64_t)seq.q0 * a.ldq;
+  const float* k = static_cast<const float*>(a.k) + (int64_t)seq.k0 * a.ldk;
+  const float* v = static_cast<const float*>(a.v) + (int64_t)seq.k0 * a.ldv;
+  const float* dout = static_cast<const float*>(a.dout) + (int64_t)seq.q0 * a.lddo;
   if (KEYS) {
-    load_rows<T, D, ROWS>(x1, C::LD, k + (int64_t)r0 * a.ldk + hb * D, a.ldk, rows, threadIdx.x, kThreads);
-    load_rows<T, D, ROWS>(x2, C::LD, v + (int64_t)r0 * a.ldv + hb * D, a.ldv, rows, threadIdx.x, kThreads);
+    load_rows<D, ROWS>(x1, C::LD, k + (int64_t)r0 * a.ldk + hb * D, a.ldk, rows, threadIdx.x, kThreads);
+    load_rows<D, ROWS>(x2, C::LD, v + (int64_t)r0 * a.ldv + hb * D, a.ldv, rows, threadIdx.x, kThreads);
   } else {
-    load_rows<T, D, ROWS>(x1, C::LD, q + (int64_t)r0 * a.ldq + hb * D, a.ldq, rows, threadIdx.x, kThreads);
-    load_rows<T, D, ROWS>(x2, C::LD, dout + (int64_t)r0 * a.lddo + hb * D, a.lddo, rows, threadIdx.x, kThreads);
+    load_rows<D, ROWS>(x1, C::LD, q + (int64_t)r0 * a.ldq + hb * D, a.ldq, rows, threadIdx.x, kThreads);
+    load_rows<D, ROWS>(x2, C::LD, dout + (int64_t)r0 * a.lddo + hb * D, a.lddo, rows, threadIdx.x, kThreads);
   }
   __syncthreads();
   auto seen = [&](int row, int& lo, int& hi) {
@@ -256,15 +256,15 @@ __global__ void __launch_bounds__(kThreads) mha_backward_simt_kernel(const SimtA
     const int j = j0 + n % tiles, h = KEYS ? hb * a.s.group + n / tiles : hb / a.s.group, c0 = j * kCols;
     group_sync(1 + g, 128);  // the tiles before have been read
     if (KEYS) {
-      load_rows<T, D, kCols>(y1, C::LD, q + (int64_t)c0 * a.ldq + h * D, a.ldq, seq.nq - c0, t, 128);
-      load_rows<T, D, kCols>(y2, C::LD, dout + (int64_t)c0 * a.lddo + h * D, a.lddo, seq.nq - c0, t, 128);
+      load_rows<D, kCols>(y1, C::LD, q + (int64_t)c0 * a.ldq + h * D, a.ldq, seq.nq - c0, t, 128);
+      load_rows<D, kCols>(y2, C::LD, dout + (int64_t)c0 * a.lddo + h * D, a.lddo, seq.nq - c0, t, 128);
       if (t < 2 * kCols) {
         const float* at = a.stats + mha_stat_offset(h, a.stat_slots, slot0 + c0 / kStatRows) + c0 % kStatRows;
         st[t] = at[(t / kCols) * kStatRows + t % kCols];
       }
     } else {
-      load_rows<T, D, kCols>(y1, C::LD, k + (int64_t)c0 * a.ldk + h * D, a.ldk, seq.nk - c0, t, 128);
-      load_rows<T, D, kCols>(y2, C::LD, v + (int64_t)c0 * a.ldv + h * D, a.ldv, seq.nk - c0, t, 128);
+      load_rows<D, kCols>(y1, C::LD, k + (int64_t)c0 * a.ldk + h * D, a.ldk, seq.nk - c0, t, 128);
+      load_rows<D, kCols>(y2, C::LD, v + (int64_t)c0 * a.ldv + h * D, a.ldv, seq.nk - c0, t, 128);
     }
     group_sync(1 + g, 128);
     float s[R][2], dp[R][2];
@@ -301,55 +301,55 @@ __global__ void __launch_bounds__(kThreads) mha_backward_simt_kernel(const SimtA
       for (int gg = 0; gg < kGroups; ++gg) sum += mo[gg * ROWS * D + i];
       const int64_t at = (int64_t)(row0 + i / D) * ld + hb * D + i % D;
       if (!ACID_IN_BOUNDS(kSiteMha, at, (int64_t)(KEYS ? a.s.nk : a.s.nq) * ld)) continue;
-      io<T>::st(static_cast<T*>(out) + at, sum * by);
+      static_cast<float*>(out)[at] = sum * by;
     }
   };
   join(acc1, a.out1, a.ld1, (KEYS ? seq.k0 : seq.q0) + r0, a.scale);
   if (KEYS) join(acc2, a.out2, a.ld2, seq.k0 + r0, 1.f);
 }
 
-template <typename T, int D>
-acid_status forward(const MhaArgs& x, const SimtArgs& base, cudaStream_t s) {
+template <int D>
+acid_status forward(const MhaArgs& x, const F32Args& base, cudaStream_t s) {
   static PerContext allowed;
-  constexpr size_t smem = (size_t)SimtCfg<D, 16, 2, 1>::FLOATS * 4;
-  ACID_TRY(allow_smem(allowed, mha_forward_simt_kernel<T, D>, smem));
-  SimtArgs a = base;
+  constexpr size_t smem = (size_t)F32Cfg<D, 16, 2, 1>::FLOATS * 4;
+  ACID_TRY(allow_smem(allowed, mha_forward_f32_kernel<D>, smem));
+  F32Args a = base;
   a.out1 = x.out;
   a.ld1 = x.ldo;
   const dim3 grid(mha_slots(a.s.nq, a.s.seqs, a.s.qb != nullptr, 16), a.s.heads);
-  launch_pdl(mha_forward_simt_kernel<T, D>, grid, kThreads, smem, s, a);
+  launch_pdl(mha_forward_f32_kernel<D>, grid, kThreads, smem, s, a);
   ACID_CHECK_LAUNCH();
   return ACID_OK;
 }
 
-template <typename T, int D>
-acid_status backward(const MhaArgs& x, const SimtArgs& base, cudaStream_t s) {
+template <int D>
+acid_status backward(const MhaArgs& x, const F32Args& base, cudaStream_t s) {
   static PerContext allowed_k, allowed_q;
-  constexpr size_t smem = (size_t)SimtCfg<D, 16, 2, 2>::FLOATS * 4;
-  SimtArgs a = base;
+  constexpr size_t smem = (size_t)F32Cfg<D, 16, 2, 2>::FLOATS * 4;
+  F32Args a = base;
   if (x.dk != nullptr || x.dv != nullptr) {
-    ACID_TRY(allow_smem(allowed_k, mha_backward_simt_kernel<T, D, true>, smem));
+    ACID_TRY(allow_smem(allowed_k, mha_backward_f32_kernel<D, true>, smem));
     a.out1 = x.dk;
     a.ld1 = x.lddk;
     a.out2 = x.dv;
     a.ld2 = x.lddv;
     const dim3 grid(mha_slots(a.s.nk, a.s.seqs, a.s.kb != nullptr, 16), a.s.kv_heads);
-    launch_pdl(mha_backward_simt_kernel<T, D, true>, grid, kThreads, smem, s, a);
+    launch_pdl(mha_backward_f32_kernel<D, true>, grid, kThreads, smem, s, a);
     ACID_CHECK_LAUNCH();
   }
   if (x.dq != nullptr) {
-    ACID_TRY(allow_smem(allowed_q, mha_backward_simt_kernel<T, D, false>, smem));
+    ACID_TRY(allow_smem(allowed_q, mha_backward_f32_kernel<D, false>, smem));
     a.out1 = x.dq;
     a.ld1 = x.lddq;
     const dim3 grid(mha_slots(a.s.nq, a.s.seqs, a.s.qb != nullptr, 16), a.s.heads);
-    launch_pdl(mha_backward_simt_kernel<T, D, false>, grid, kThreads, smem, s, a);
+    launch_pdl(mha_backward_f32_kernel<D, false>, grid, kThreads, smem, s, a);
     ACID_CHECK_LAUNCH();
   }
   return ACID_OK;
 }
 
-SimtArgs base_args(const MhaArgs& x) {
-  SimtArgs a = {};
+F32Args base_args(const MhaArgs& x) {
+  F32Args a = {};
   a.s = x.shape;
   a.q = x.q;
   a.k = x.k;
@@ -370,24 +370,24 @@ SimtArgs base_args(const MhaArgs& x) {
 
 }  // namespace
 
-#define MHA_BY_HEAD_DIM(CALL)                                \
-  switch (x.head_dim) {                                      \
-    case 32: return CALL(float, 32);                         \
-    case 64: return x.dtype == ACID_FP32 ? CALL(float, 64) : CALL(__nv_bfloat16, 64);    \
-    case 96: return CALL(float, 96);                         \
-    default: return x.dtype == ACID_FP32 ? CALL(float, 128) : CALL(__nv_bfloat16, 128);  \
+acid_status mha_forward_f32(const MhaArgs& x, cudaStream_t s) {
+  const F32Args a = base_args(x);
+  switch (x.head_dim) {
+    case 32: return forward<32>(x, a, s);
+    case 64: return forward<64>(x, a, s);
+    case 96: return forward<96>(x, a, s);
+    default: return forward<128>(x, a, s);
   }
-
-acid_status mha_forward_simt(const MhaArgs& x, cudaStream_t s) {
-#define CALL(T, D) forward<T, D>(x, base_args(x), s)
-  MHA_BY_HEAD_DIM(CALL)
-#undef CALL
 }
 
-acid_status mha_backward_simt(const MhaArgs& x, cudaStream_t s) {
-#define CALL(T, D) backward<T, D>(x, base_args(x), s)
-  MHA_BY_HEAD_DIM(CALL)
-#undef CALL
+acid_status mha_backward_f32(const MhaArgs& x, cudaStream_t s) {
+  const F32Args a = base_args(x);
+  switch (x.head_dim) {
+    case 32: return backward<32>(x, a, s);
+    case 64: return backward<64>(x, a, s);
+    case 96: return backward<96>(x, a, s);
+    default: return backward<128>(x, a, s);
+  }
 }
 
 }  // namespace acid
