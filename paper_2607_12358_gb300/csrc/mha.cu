@@ -27,7 +27,7 @@ struct StatArgs {
   float unit;  // of the kernels' exponential: 1 for e, log2(e) for 2
 };
 
-// -lse and sum(dout out) of a slot's rows for one head (mha_stat_offset).  A row is
+// -lse and -sum(dout out) of a slot's rows for one head (mha_stat_offset).  A row is
 // `lanes` lanes of 8 columns.  HBM bound: it reads out and dout once.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) mha_stats_kernel(const StatArgs a, int lanes) {
@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(kThreads) mha_stats_kernel(const StatArgs a, i
     for (int off = lanes / 2; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
     if (part == 0) {
       to[r] = nlse;
-      to[kStatRows + r] = nlse == -INFINITY ? 0.f : sum;
+      to[kStatRows + r] = nlse == -INFINITY ? 0.f : -sum;
     }
   }
 }

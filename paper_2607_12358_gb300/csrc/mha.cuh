@@ -97,8 +97,8 @@ __device__ __forceinline__ void mha_queries_of(const MhaShape& s, const MhaSeq& 
 }
 
 // Row statistics of the backward pass, [heads][slots][2][kStatRows] floats: -lse
-// (in the unit of the kernels' exponential) and the sum of dout out over the head's
-// columns.  Rows past a sequence's end and rows that see no key hold -inf and 0,
+// (in the unit of the kernels' exponential) and less the sum of dout out over the
+// head's columns.  Rows past a sequence's end and rows that see no key hold -inf and 0,
 // which makes their probabilities 0.
 __host__ __device__ __forceinline__ int64_t mha_stat_offset(int head, int slots, int slot) {
   return ((int64_t)head * slots + slot) * (2 * kStatRows);

@@ -186,6 +186,14 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                : "memory");
 }
 
+// Four consecutive floats as two packed pairs.  (Through a generic pointer, which is
+// what the aligned base of dynamic shared memory is to the compiler, the same loads
+// take the path of global memory: 4726 rows, 30 x 64, keys stationary STEP1A us instead of
+// STEP1B.)
+__device__ __forceinline__ void lds_pairs(uint32_t addr, uint64_t& a, uint64_t& b) {
+  asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(addr));
+}
+
 // D[128 x 128] = A B^T over D columns, both K-major in shared memory.
 template <class C>
 __device__ __forceinline__ void mma_scores(uint32_t d, uint64_t adesc, uint64_t bdesc) {
@@ -404,20 +412,19 @@ __global__ void __launch_bounds__(kThreads, 1)
       seen(r0 + r, lo, hi);
       seen(r0, none, all_hi);
       seen(r0 + kTile - 1, all_lo, none);
-      float nlse = 0.f, delta = 0.f;
+      float nlse = 0.f, ndelta = 0.f;
       if (!KEYS) {
         const int slot = mha_slot0(a.s.qb, x.index, x.seq.q0, kStatRows) + x.tile;
         const float* st = a.stats + mha_stat_offset(x.head, a.stat_slots, slot);
         nlse = st[r];
-        delta = st[kStatRows + r];
+        ndelta = st[kStatRows + r];
       }
       // One step; MASK: some row does not see some streamed row.
       auto step = [&](int i, auto mask) -> bool {
         constexpr bool MASK = decltype(mask)::value;
         const int c0 = (x.j0 + (x.n0 + i) % x.tiles) * kTile + half * 64;
         const uint32_t s_at = base + C::S_COL + (g % C::NS) * 128 + half * 64, dp_at = base + C::DP_COL + half * 64;
-        const float* st = reinterpret_cast<const float*>(smem + C::OFF_STAT + (KEYS ? g % C::Y1S : 0) * kStatBytes) +
-                          half * 64;
+        const uint32_t st = smem_u32(smem + C::OFF_STAT + (KEYS ? g % C::Y1S : 0) * kStatBytes) + half * 256;
         if (!mbar_wait(&bar.s_full[g % C::NS], (g / C::NS) & 1)) return false;
         // (the statistics were written by the copy that the scores' operand came with: its own barrier
         // makes them visible to this thread; completed long before)
@@ -430,16 +437,22 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int c = 0; c < 64; c += 4) {
           uint64_t n01, n23;
-          if (KEYS) {
-            const float4 n = *reinterpret_cast<const float4*>(st + c);
-            n01 = f2_pack(n.x, n.y);
-            n23 = f2_pack(n.z, n.w);
-          } else {
-            n01 = n23 = f2_pack(nlse, nlse);
-          }
+          if (KEYS) lds_pairs(st + c * 4, n01, n23);
+          else n01 = n23 = f2_pack(nlse, nlse);
           f2_unpack(f2_fma(f2_pack(p[c], p[c + 1]), sc2, n01), p[c], p[c + 1]);
           f2_unpack(f2_fma(f2_pack(p[c + 2], p[c + 3]), sc2, n23), p[c + 2], p[c + 3]);
         }
+        float dp[64];
+        // dP is read behind P where it comes later than S, and beside the exponentials where
+        // it is there by then (queries stationary)
+        auto read_dp = [&]() -> bool {
+          if (!mbar_wait(bar.dp_full, g & 1)) return false;
+          tc_fence_after();
+#pragma unroll
+          for (int c = 0; c < 2; ++c) tmem_ld32(dp_at + c * 32, reinterpret_cast<uint32_t*>(dp + c * 32));
+          return true;
+        };
+        if (!KEYS && !read_dp()) return false;
 #pragma unroll
         for (int c = 0; c < 64; ++c) {
           p[c] = ex2_approx(p[c]);
@@ -453,12 +466,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_wait_st();
           tc_fence_before();
           mbar_arrive(bar.p_full);
+          if (!read_dp()) return false;
         }
-        if (!mbar_wait(bar.dp_full, g & 1)) return false;
-        tc_fence_after();
-        float dp[64];
-#pragma unroll
-        for (int c = 0; c < 2; ++c) tmem_ld32(dp_at + c * 32, reinterpret_cast<uint32_t*>(dp + c * 32));
         tmem_wait_ld();
         if constexpr (!KEYS) {
           tc_fence_before();
@@ -468,13 +477,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int c = 0; c < 64; c += 4) {
           uint64_t d01, d23;
-          if (KEYS) {
-            const float4 n = *reinterpret_cast<const float4*>(st + kStatRows + c);
-            d01 = f2_pack(-n.x, -n.y);
-            d23 = f2_pack(-n.z, -n.w);
-          } else {
-            d01 = d23 = f2_pack(-delta, -delta);
-          }
+          if (KEYS) lds_pairs(st + kStatRows * 4 + c * 4, d01, d23);
+          else d01 = d23 = f2_pack(ndelta, ndelta);
           float v[4];
           f2_unpack(f2_mul(f2_pack(p[c], p[c + 1]), f2_add(f2_pack(dp[c], dp[c + 1]), d01)), v[0], v[1]);
           f2_unpack(f2_mul(f2_pack(p[c + 2], p[c + 3]), f2_add(f2_pack(dp[c + 2], dp[c + 3]), d23)), v[2], v[3]);

@@ -275,11 +275,11 @@ __global__ void __launch_bounds__(kThreads) mha_backward_f32_kernel(const F32Arg
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int col = kg + 16 * c;
-        const float nlse = KEYS ? st[col] : nl[i], delta = KEYS ? st[kCols + col] : dl[i];
+        const float nlse = KEYS ? st[col] : nl[i], ndelta = KEYS ? st[kCols + col] : dl[i];
         const bool on = c0 + col >= lo[i] && c0 + col < hi[i];
         const float p = on ? expf(fmaf(s[i][c], a.scale, nlse)) : 0.f;
         if (KEYS) sp[(hw * R + i) * C::LDP + col] = p;
-        sd[(hw * R + i) * C::LDP + col] = on ? p * (dp[i][c] - delta) : 0.f;
+        sd[(hw * R + i) * C::LDP + col] = on ? p * (dp[i][c] + ndelta) : 0.f;
       }
     __syncwarp();
     accumulate<D, R>(sd + hw * R * C::LDP, C::LDP, y1, C::LD, kg, acc1);
