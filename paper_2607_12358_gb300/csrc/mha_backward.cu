@@ -115,7 +115,7 @@ struct BwdCfg {
   // S regions in tensor memory: with two, the next step's S is formed while this one's is
   // worked on.  Keys stationary at head dim 128: S, dP and two sums fill the 512 columns.
   static constexpr int NS = KEYS && D == 128 ? 1 : 2;
-  static constexpr int Y1S = NS + 1, Y2S = 2;
+  static constexpr int Y1S = D == 64 ? 4 : NS + 1, Y2S = D == 64 ? 4 : 2;
   static constexpr int SUMS = KEYS ? 2 : 1;
   static constexpr int OFF_X = 0, OFF_Y1 = 2 * T_BYTES, OFF_Y2 = OFF_Y1 + Y1S * T_BYTES;
   static constexpr int OFF_STAT = OFF_Y2 + Y2S * T_BYTES;
