@@ -40,68 +40,196 @@ struct BwdArgs {
   int64_t ld1, ld2;
   float scale, scale_log2;
   int slots, stat_slots, heads;  // of the stationary side
-  int full, splits, units;       // as in the forward pass: units from `full` on are shares of an item
-  float* part;                   // [split units][1 or 2][D / 4][128 rows][4]
+  int items;      // stationary tiles and heads
+  int full;       // items [0, full) go to the CTAs whole, one in turn; the others' steps are shared out
+  int alike;      // every item has the same steps
+  int longest;    // items with the most steps first (whole items under a window of frames)
+  float* part;    // [2 CTAs][1 or 2][D / 4][128 rows][4]: sums of an item's share
+  int4* record;   // [CTAs][2]: the item that begins in a CTA's share and ends in another's
 };
 
-// A CTA's unit: a stationary tile with the streamed tiles that see it.
+// What a CTA does at a time: a stationary tile, or a share of its steps.
 struct BwdUnit {
-  int head;         // of the stationary side
-  int row0, rows;   // first stationary row, rows left in its sequence
-  int j0, tiles;    // streamed tiles [j0, j0 + tiles) of the sequence, for each head of the group
-  int n0, steps;    // steps [n0, n0 + steps) of group * tiles
-  int part;         // slot of a share's partial sums, or -1
-  int tile, index;  // of and in the sequence
-  MhaSeq seq;
+  int head;        // of the stationary side
+  int row0, rows;  // first stationary row, rows of the tile
+  int r0, nq, nk;  // that row in its sequence, the sequence's rows
+  int y0;          // the sequence's first streamed row
+  int j0, tiles;   // streamed tiles [j0, j0 + tiles) of the sequence, for each head of the group
+  int n0, steps;   // steps [n0, n0 + steps) of group * tiles
+  int part;        // slot of a share's partial sums, or -1
+  int stat;        // keys stationary: slot of the sequence's first queries; else of this tile's
 };
 
-template <bool KEYS>
-__device__ __forceinline__ bool bwd_unit(const BwdArgs& a, int u, BwdUnit& x) {
-  int item = u, split = 0, slot;
-  x.part = -1;
-  if (u >= a.full) {
-    x.part = u - a.full;
-    item = a.full + x.part / a.splits;
-    split = x.part % a.splits;
-  }
-  if (a.s.frame == 0) {
+__device__ __forceinline__ void bwd_place(const BwdArgs& a, int item, int& slot, int& head, bool keys) {
+  if (!a.longest) {
     slot = item % a.slots;
-    x.head = item / a.slots;
-  } else {  // longest first under a causal window: the first keys, the last queries
+    head = item / a.slots;
+  } else {  // causal: the first keys, the last queries
     slot = item / a.heads;
-    if (!KEYS) slot = a.slots - 1 - slot;
-    x.head = item % a.heads;
+    if (!keys) slot = a.slots - 1 - slot;
+    head = item % a.heads;
   }
-  if (!mha_slot<kTile, KEYS>(a.s, slot, x.seq, x.index, x.tile)) return false;
-  const int r0 = x.tile * kTile, n = KEYS ? x.seq.nk : x.seq.nq;
-  x.row0 = (KEYS ? x.seq.k0 : x.seq.q0) + r0;
-  x.rows = n - r0;
+}
+// An item with all its steps (which may be none); false: an empty slot.
+template <bool KEYS>
+__device__ __forceinline__ bool bwd_item(const BwdArgs& a, int slot, int head, BwdUnit& x) {
+  MhaSeq seq;
+  int index, tile;
+  x.steps = 0;
+  if (!mha_slot<kTile, KEYS>(a.s, slot, seq, index, tile)) return false;
+  const int n = KEYS ? seq.nk : seq.nq;
+  x.head = head;
+  x.r0 = tile * kTile;
+  x.row0 = (KEYS ? seq.k0 : seq.q0) + x.r0;
+  x.rows = min(n - x.r0, kTile);
+  x.nq = seq.nq;
+  x.nk = seq.nk;
+  x.y0 = KEYS ? seq.q0 : seq.k0;
+  x.stat = mha_slot0(a.s.qb, index, seq.q0, kStatRows) + (KEYS ? 0 : tile);
   int lo, hi, none;
-  const int last = r0 + min(x.rows, kTile) - 1;
   if (KEYS) {
-    mha_queries_of(a.s, x.seq, r0, lo, none);
-    mha_queries_of(a.s, x.seq, last, none, hi);
+    mha_queries_of(a.s, seq, x.r0, lo, none);
+    mha_queries_of(a.s, seq, x.r0 + x.rows - 1, none, hi);
   } else {
-    mha_keys_of(a.s, x.seq, r0, lo, none);
-    mha_keys_of(a.s, x.seq, last, none, hi);
+    mha_keys_of(a.s, seq, x.r0, lo, none);
+    mha_keys_of(a.s, seq, x.r0 + x.rows - 1, none, hi);
   }
   x.j0 = lo / kTile;
   x.tiles = hi > lo ? (hi + kTile - 1) / kTile - x.j0 : 0;
-  const int total = x.tiles * (KEYS ? a.s.group : 1);
   x.n0 = 0;
-  x.steps = total;
-  if (x.part >= 0) {
-    x.n0 = (int)((int64_t)split * total / a.splits);
-    x.steps = (int)((int64_t)(split + 1) * total / a.splits) - x.n0;
-  }
+  x.steps = x.tiles * (KEYS ? a.s.group : 1);
+  x.part = -1;
   return true;
 }
+
+// The units of this CTA, in order, by its producer warp.  First whole items, one in
+// turn.  Then the steps of all other items, laid end to end head by head, in equal
+// shares: a share begins and ends inside an item as a rule, whose parts are joined by
+// mha_backward_join_kernel.  `scratch` holds the steps before each slot of a head.
+constexpr int kLeastSteps = 4;  // of a share
 template <bool KEYS>
-__device__ __forceinline__ bool next_bwd_unit(const BwdArgs& a, int& u, BwdUnit& x) {
-  for (; u < a.units; u += gridDim.x)
-    if (bwd_unit<KEYS>(a, u, x) && x.steps > 0) return true;
-  return false;
-}
+struct BwdWalk {
+  const BwdArgs& a;
+  int* scratch;
+  int lane;
+  int next;        // whole items; then the next shared one
+  bool shared = false;
+  int64_t s, from, to, base, work;  // first step of `next`; this share's steps
+  int shares, units = 0;
+  __device__ __forceinline__ BwdWalk(const BwdArgs& a_, int* scratch_, int lane_)
+      : a(a_), scratch(scratch_), lane(lane_), next(blockIdx.x) {}
+  __device__ __forceinline__ int64_t bound(int c) const { return base + work * c / shares; }
+
+  __device__ __forceinline__ void share_out() {
+    shared = true;
+    int total = 0;
+    BwdUnit x;
+    if (a.alike) {
+      bwd_item<KEYS>(a, 0, 0, x);
+      total = x.steps * a.slots;
+    } else {
+      for (int i = 0; i < a.slots; i += 32) {
+        int n = 0;
+        if (i + lane < a.slots) {
+          bwd_item<KEYS>(a, i + lane, 0, x);
+          n = x.steps;
+        }
+        int sum = n;
+#pragma unroll
+        for (int off = 1; off < 32; off *= 2) {
+          const int t = __shfl_up_sync(0xffffffffu, sum, off);
+          if (lane >= off) sum += t;
+        }
+        if (i + lane < a.slots) scratch[i + lane] = total + sum;  // up to and with this slot
+        total += __shfl_sync(0xffffffffu, sum, 31);
+      }
+      __syncwarp();
+    }
+    const int per = a.alike ? x.steps : 0;
+    auto upto = [&](int slot) { return slot < 0 ? 0 : a.alike ? (slot + 1) * per : scratch[slot]; };
+    const int head0 = a.full / a.slots, slot0 = a.full % a.slots;
+    base = (int64_t)head0 * total + upto(slot0 - 1);
+    work = (int64_t)a.heads * total - base;
+    shares = (int)max((int64_t)1, min((int64_t)gridDim.x, work / kLeastSteps));
+    if ((int)blockIdx.x >= shares) {
+      next = a.items;
+      from = to = 0;
+      return;
+    }
+    from = bound(blockIdx.x);
+    to = bound(blockIdx.x + 1);
+    if (blockIdx.x == 0) {
+      next = a.full;
+      s = base;
+    } else {  // the item that step `from` lies in
+      const int head = (int)(from / total), rest = (int)(from - (int64_t)head * total);
+      int lo = 0, hi = a.slots - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (upto(mid) > rest) hi = mid;
+        else lo = mid + 1;
+      }
+      next = head * a.slots + lo;
+      s = (int64_t)head * total + upto(lo - 1);
+    }
+    fence_proxy_async_smem();  // the scratch becomes a target of copies
+    __syncwarp();
+  }
+
+  // Gradients of rows that nothing sees, or that see nothing.
+  __device__ __forceinline__ void clear(const BwdUnit& x, int d) const {
+    for (int w = 0; w < (KEYS ? 2 : 1); ++w) {
+      __nv_bfloat16* out = w == 0 ? a.out1 : a.out2;
+      const int64_t ld = w == 0 ? a.ld1 : a.ld2;
+      for (int i = lane; out != nullptr && i < x.rows * (d / 8); i += 32) {
+        const int64_t at = (int64_t)(x.row0 + i / (d / 8)) * ld + x.head * d + i % (d / 8) * 8;
+        if (ACID_IN_BOUNDS(kSiteMha, at + 7, (KEYS ? a.s.nk : a.s.nq) * ld))
+          *reinterpret_cast<uint4*>(out + at) = make_uint4(0, 0, 0, 0);
+      }
+    }
+  }
+
+  // The next unit with steps; false: none.
+  __device__ __forceinline__ bool operator()(BwdUnit& x, int d) {
+    int slot, head;
+    for (; !shared && next < a.full; next += gridDim.x) {
+      bwd_place(a, next, slot, head, KEYS);
+      if (!bwd_item<KEYS>(a, slot, head, x)) continue;
+      if (x.steps == 0) {
+        clear(x, d);
+        continue;
+      }
+      next += gridDim.x;
+      return true;
+    }
+    if (a.full == a.items) return false;
+    if (!shared) share_out();
+    for (; next < a.items; ++next) {
+      bwd_place(a, next, slot, head, KEYS);
+      if (!bwd_item<KEYS>(a, slot, head, x)) continue;
+      if (x.steps == 0) {
+        clear(x, d);
+        continue;
+      }
+      if (s >= to) return false;
+      const int n = x.steps, n0 = (int)max((int64_t)0, from - s), n1 = (int)min((int64_t)n, to - s);
+      x.n0 = n0;
+      x.steps = n1 - n0;
+      if (n0 > 0 || n1 < n) x.part = 2 * blockIdx.x + (units > 0);
+      if (n0 == 0 && n1 < n && lane == 0) {
+        int last = blockIdx.x;
+        while (bound(last + 1) < s + n) ++last;
+        a.record[2 * blockIdx.x] = make_int4(x.rows, x.row0, x.head, x.part);
+        a.record[2 * blockIdx.x + 1] = make_int4(last, 0, 0, 0);
+      }
+      ++units;
+      s += n;
+      ++next;
+      return true;
+    }
+    return false;
+  }
+};
 
 // Shared memory: the two stationary tiles, rings of the two streamed operands, the
 // rows' statistics beside them, barriers.  Y1 (q or k) is read by the first product of
@@ -119,7 +247,9 @@ struct BwdCfg {
   static constexpr int SUMS = KEYS ? 2 : 1;
   static constexpr int OFF_X = 0, OFF_Y1 = 2 * T_BYTES, OFF_Y2 = OFF_Y1 + Y1S * T_BYTES;
   static constexpr int OFF_STAT = OFF_Y2 + Y2S * T_BYTES;
-  static constexpr int OFF_BAR = OFF_STAT + (KEYS ? Y1S * kStatBytes : 0);
+  static constexpr int UNITS = 4, UNIT_BYTES = 64;
+  static constexpr int OFF_UNIT = OFF_STAT + (KEYS ? Y1S * kStatBytes : 0);
+  static constexpr int OFF_BAR = OFF_UNIT + UNITS * UNIT_BYTES;
   static constexpr int SMEM = OFF_BAR + 512 + 1024;
   static_assert(SMEM <= 227 * 1024, "shared memory");
   static constexpr uint32_t S_COL = 0, DP_COL = NS * 128, SUM_COL = DP_COL + 128;
@@ -129,14 +259,15 @@ struct BwdCfg {
 
 template <class C>
 struct BwdBars {
-  uint64_t *x_full, *x_empty, *y1_full, *y1_empty, *y2_full, *y2_empty;
+  uint64_t *unit_full, *x_full, *x_empty, *y1_full, *y1_empty, *y2_full, *y2_empty;
   uint64_t *s_full, *dp_full, *dp_read, *p_full, *ds_full, *sum_full, *sum_empty, *edge, *drain;
   uint32_t* tmem_slot;
-  static constexpr int kCount = 2 + 2 * C::Y1S + 2 * C::Y2S + C::NS + 8;
+  static constexpr int kCount = 2 + 2 * C::Y1S + 2 * C::Y2S + C::NS + 10 + C::UNITS;
   static_assert(kCount * 8 + 4 <= 512, "barrier area");
   __device__ __forceinline__ explicit BwdBars(uint8_t* at) {
     uint64_t* b = reinterpret_cast<uint64_t*>(at);
     auto take = [&](int n) { uint64_t* r = b; b += n; return r; };
+    unit_full = take(C::UNITS);
     x_full = take(1);
     x_empty = take(1);
     y1_full = take(C::Y1S);
@@ -146,8 +277,10 @@ struct BwdBars {
     s_full = take(C::NS);
     dp_full = take(1);
     dp_read = take(1);
-    p_full = take(1);
-    ds_full = take(1);
+    // (two each: the workers may be a step ahead of the MMA warp, which can be held up by a
+    // tile that is still on its way)
+    p_full = take(2);
+    ds_full = take(2);
     sum_full = take(1);
     sum_empty = take(1);
     edge = take(1);
@@ -155,6 +288,7 @@ struct BwdBars {
     tmem_slot = reinterpret_cast<uint32_t*>(b);
   }
   __device__ __forceinline__ void init() const {
+    for (int i = 0; i < C::UNITS; ++i) mbar_init(&unit_full[i], 1);
     mbar_init(x_full, 1);
     mbar_init(x_empty, 1);
     for (int i = 0; i < C::Y1S; ++i) {
@@ -168,8 +302,10 @@ struct BwdBars {
     for (int i = 0; i < C::NS; ++i) mbar_init(&s_full[i], 1);
     mbar_init(dp_full, 1);
     mbar_init(dp_read, kWorkers);
-    mbar_init(p_full, kWorkers);
-    mbar_init(ds_full, kWorkers);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&p_full[i], kWorkers);
+      mbar_init(&ds_full[i], kWorkers);
+    }
     mbar_init(sum_full, 1);
     mbar_init(sum_empty, kWorkers);
     mbar_init(edge, 1);
@@ -186,10 +322,20 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                : "memory");
 }
 
+// 16 columns of 32-bit registers a lane to tensor memory.
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(
+          taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
 // Four consecutive floats as two packed pairs.  (Through a generic pointer, which is
 // what the aligned base of dynamic shared memory is to the compiler, the same loads
-// take the path of global memory: 4726 rows, 30 x 64, keys stationary STEP1A us instead of
-// STEP1B.)
+// take the path of global memory: keys stationary, 4726 rows, 30 x 64 348 us instead of
+// 305.)
 __device__ __forceinline__ void lds_pairs(uint32_t addr, uint64_t& a, uint64_t& b) {
   asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(addr));
 }
@@ -228,6 +374,29 @@ __device__ __forceinline__ void clear_tile_rows(uint8_t* tile, int valid, int la
   __syncwarp();
 }
 
+// 64 bytes of a row, a lane's own, by whole sectors where the address allows it.
+__device__ __forceinline__ void store_64_bytes(void* p, const uint32_t* w) {
+  if ((reinterpret_cast<uintptr_t>(p) & 31) == 0) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(static_cast<uint8_t*>(p) + 32 * i),
+                   "r"(w[8 * i]), "r"(w[8 * i + 1]), "r"(w[8 * i + 2]), "r"(w[8 * i + 3]), "r"(w[8 * i + 4]),
+                   "r"(w[8 * i + 5]), "r"(w[8 * i + 6]), "r"(w[8 * i + 7])
+                   : "memory");
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      static_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  }
+}
+
+// Columns [lo, hi) of 32 as bits.
+__device__ __forceinline__ uint32_t column_bits(int lo, int hi) {
+  lo = max(lo, 0);
+  hi = min(hi, 32);
+  return lo < hi ? (0xffffffffu >> (32 - hi)) & (0xffffffffu << lo) : 0u;
+}
+
 // X1, X2: the stationary operands (k, v or q, g); Y1, Y2: the streamed ones (q, g or
 // k, v).
 template <class C>
@@ -243,6 +412,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* sY1 = smem + C::OFF_Y1;
   uint8_t* sY2 = smem + C::OFF_Y2;
   const BwdBars<C> bar(smem + C::OFF_BAR);
+  int4* const entries = reinterpret_cast<int4*>(smem + C::OFF_UNIT);
+  auto entry = [&](int n) { return entries + n % C::UNITS * (C::UNIT_BYTES / 16); };
   const int warp = warp_index(), lane = threadIdx.x & 31;
   if (warp == 0 && lane == 0) {
     tma_prefetch_desc(&tmX1);
@@ -257,13 +428,23 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *bar.tmem_slot;
   pdl_wait();
+  if (threadIdx.x == 0 && a.full < a.items) a.record[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
 
   if (warp == 0) {  // -------------------------------------------- TMA producer
     bool ok = true;
-    int y1_done = 0, y2_done = 0, x_done = 0, edges = 0;
+    int y1_done = 0, y2_done = 0, x_done = 0, edges = 0, g = 0;
+    BwdWalk<KEYS> walk(a, reinterpret_cast<int*>(sY1), lane);
     BwdUnit x;
-    int u = blockIdx.x, g = 0;
-    for (; ok && next_bwd_unit<KEYS>(a, u, x); u += gridDim.x, ++x_done) {
+    for (; ok; ++x_done) {
+      const bool more = walk(x, D);
+      if (lane == 0) {
+        int4* e = entry(x_done);
+        e[0] = make_int4(more ? x.steps : 0, x.head, x.row0, x.rows);
+        e[1] = make_int4(x.r0, x.nq, x.nk, x.part);
+        e[2] = make_int4(x.j0, x.tiles, more ? x.n0 % x.tiles : 0, x.stat);
+        mbar_arrive(&bar.unit_full[x_done % C::UNITS]);
+      }
+      if (!more) break;
       if (x_done > 0 && !mbar_wait_warp(bar.x_empty, (x_done - 1) & 1)) { ok = false; break; }
       if (lane == 0) {
         mbar_expect_tx(bar.x_full, 2 * C::T_BYTES);
@@ -272,13 +453,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           tma_load_2d(sX + C::T_BYTES + c * C::CHUNK, &tmX2, bar.x_full, x.head * D + c * 64, x.row0);
         }
       }
-      const int seq0 = KEYS ? x.seq.q0 : x.seq.k0, n = KEYS ? x.seq.nq : x.seq.nk, all = KEYS ? a.s.nq : a.s.nk;
-      const int stat0 = KEYS ? mha_slot0(a.s.qb, x.index, x.seq.q0, kStatRows) : 0;
+      const int rows = KEYS ? x.nq : x.nk, all = KEYS ? a.s.nq : a.s.nk;
+      int jt = x.n0 % x.tiles, head = KEYS ? x.head * a.s.group + x.n0 / x.tiles : x.head / a.s.group;
       for (int i = 0; ok && i < x.steps; ++i, ++g) {
-        const int j = x.j0 + (x.n0 + i) % x.tiles;
-        const int head = KEYS ? x.head * a.s.group + (x.n0 + i) / x.tiles : x.head / a.s.group;
-        const int valid = n - j * kTile, row = seq0 + j * kTile;
-        const bool clear = valid < kTile && seq0 + n < all;
+        const int j = x.j0 + jt;
+        const int valid = rows - j * kTile, row = x.y0 + j * kTile;
+        const bool clear = valid < kTile && x.y0 + rows < all;
         // (the statistics of a tile's queries come with it: one kilobyte)
         auto load = [&](uint8_t* dst, const CUtensorMap* map, uint64_t* full, uint8_t* stat_dst) -> bool {
           uint64_t* to = clear ? bar.edge : full;
@@ -286,7 +466,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_expect_tx(to, C::T_BYTES + (stat_dst != nullptr ? kStatBytes : 0));
             for (int c = 0; c < C::CH; ++c) tma_load_2d(dst + c * C::CHUNK, map, to, head * D + c * 64, row);
             if (stat_dst != nullptr)
-              bulk_load(stat_dst, a.stats + mha_stat_offset(head, a.stat_slots, stat0 + j), kStatBytes, to);
+              bulk_load(stat_dst, a.stats + mha_stat_offset(head, a.stat_slots, x.stat + j), kStatBytes, to);
           }
           if (clear) {
             if (!mbar_wait_warp(bar.edge, edges++ & 1)) return false;
@@ -304,10 +484,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (r2 > 0 && !mbar_wait_warp(&bar.y2_empty[s2], (r2 - 1) & 1)) { ok = false; break; }
         if (!load(sY2 + s2 * C::T_BYTES, &tmY2, &bar.y2_full[s2], nullptr)) { ok = false; break; }
         y2_done = g + 1;
+        if (++jt == x.tiles) {
+          jt = 0;
+          ++head;
+        }
       }
     }
     if (!ok && lane == 0) {  // a wait ran out: the loads issued so far have landed before the CTA leaves
-      mbar_wait(bar.x_full, x_done & 1);
+      mbar_wait(bar.x_full, x_done & 1);  // (of a unit whose load was not issued: runs out too)
       for (int i = std::max(0, y1_done - C::Y1S); i < y1_done; ++i) mbar_wait(&bar.y1_full[i % C::Y1S], (i / C::Y1S) & 1);
       for (int i = std::max(0, y2_done - C::Y2S); i < y2_done; ++i) mbar_wait(&bar.y2_full[i % C::Y2S], (i / C::Y2S) & 1);
     }
@@ -320,13 +504,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint64_t y2m = smem_desc_sw128(smem_u32(sY2), C::CHUNK, 1024);
     auto at = [](uint64_t desc, int slot) { return desc + (uint64_t)((slot * C::T_BYTES) >> 4); };
     bool ok = true;
-    int u = blockIdx.x, units = 0, g0 = 0;
-    BwdUnit x;
-    for (; ok && next_bwd_unit<KEYS>(a, u, x); u += gridDim.x, ++units) {
+    int units = 0, g0 = 0;
+    for (; ok; ++units) {
+      if (!mbar_wait_warp(&bar.unit_full[units % C::UNITS], (units / C::UNITS) & 1)) { ok = false; break; }
+      // (a shuffle: a value that the compiler knows to be the same in all lanes)
+      const int steps = __shfl_sync(0xffffffffu, entry(units)->x, 0);
+      if (steps == 0) break;
       if (!mbar_wait_warp(bar.x_full, units & 1)) { ok = false; break; }
       auto scores = [&](int i) -> bool {  // S of step i
         const int g = g0 + i;
-        if (i >= x.steps) return true;
+        if (i >= steps) return true;
         if (!mbar_wait_warp(&bar.y1_full[g % C::Y1S], (g / C::Y1S) & 1)) return false;
         tc_fence_after();
         if (leader) {
@@ -338,25 +525,25 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       auto grads = [&](int i) -> bool {  // dP of step i
         const int g = g0 + i;
-        if (i >= x.steps) return true;
+        if (i >= steps) return true;
         if (!mbar_wait_warp(&bar.y2_full[g % C::Y2S], (g / C::Y2S) & 1)) return false;
         tc_fence_after();
         if (leader) {
           mma_scores<C>(tmem + C::DP_COL, x2, at(y2k, g % C::Y2S));
           mma_commit(bar.dp_full);
           if (!KEYS) mma_commit(&bar.y2_empty[g % C::Y2S]);
-          if (i == x.steps - 1) mma_commit(bar.x_empty);
+          if (i == steps - 1) mma_commit(bar.x_empty);
         }
         __syncwarp();
         return true;
       };
       ok = scores(0) && grads(0) && (C::NS == 1 || scores(1));
-      for (int i = 0; ok && i < x.steps; ++i) {
+      for (int i = 0; ok && i < steps; ++i) {
         const int g = g0 + i;
         if (i == 0 && units > 0 && !mbar_wait_warp(bar.sum_empty, (units - 1) & 1)) { ok = false; break; }
         if constexpr (KEYS) {
           // dv += P^T g, over S; then the next S may take the region
-          if (!mbar_wait_warp(bar.p_full, g & 1)) { ok = false; break; }
+          if (!mbar_wait_warp(&bar.p_full[g & 1], (g >> 1) & 1)) { ok = false; break; }
           tc_fence_after();
           if (leader) {
             mma_sum<C>(tmem + C::SUM_COL + D, tmem + C::S_COL + (g % C::NS) * 128, at(y2m, g % C::Y2S), i != 0);
@@ -364,32 +551,32 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           __syncwarp();
           if (!scores(i + C::NS)) { ok = false; break; }
-          if (!mbar_wait_warp(bar.ds_full, g & 1)) { ok = false; break; }
+          if (!mbar_wait_warp(&bar.ds_full[g & 1], (g >> 1) & 1)) { ok = false; break; }
           tc_fence_after();
           if (leader) {
             mma_sum<C>(tmem + C::SUM_COL, tmem + C::DP_COL, at(y1m, g % C::Y1S), i != 0);
             mma_commit(&bar.y1_empty[g % C::Y1S]);
-            if (i == x.steps - 1) mma_commit(bar.sum_full);
+            if (i == steps - 1) mma_commit(bar.sum_full);
           }
           __syncwarp();
           if (!grads(i + 1)) { ok = false; break; }
         } else {
           // the next dP as soon as this one has been read; dq += dS k, over S
-          if (i + 1 < x.steps) {
+          if (i + 1 < steps) {
             if (!mbar_wait_warp(bar.dp_read, g & 1) || !grads(i + 1)) { ok = false; break; }
           }
-          if (!mbar_wait_warp(bar.ds_full, g & 1)) { ok = false; break; }
+          if (!mbar_wait_warp(&bar.ds_full[g & 1], (g >> 1) & 1)) { ok = false; break; }
           tc_fence_after();
           if (leader) {
             mma_sum<C>(tmem + C::SUM_COL, tmem + C::S_COL + (g % C::NS) * 128, at(y1m, g % C::Y1S), i != 0);
             mma_commit(&bar.y1_empty[g % C::Y1S]);
-            if (i == x.steps - 1) mma_commit(bar.sum_full);
+            if (i == steps - 1) mma_commit(bar.sum_full);
           }
           __syncwarp();
           if (!scores(i + C::NS)) { ok = false; break; }
         }
       }
-      g0 += x.steps;
+      g0 += steps;
     }
     if (!ok && leader) drain_mmas(bar.drain);
   } else {  // ------------------------------------------- workers
@@ -399,30 +586,41 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t base = tmem + ((uint32_t)(q * 32) << 16);
     const uint64_t sc2 = f2_pack(a.scale_log2, a.scale_log2);
     bool ok = true;
-    int g = 0, sums = 0;
-    for (int u = blockIdx.x; ok && u < a.units; u += gridDim.x) {
-      BwdUnit x;
-      if (!bwd_unit<KEYS>(a, u, x)) continue;
-      const int last = (KEYS ? x.seq.nk : x.seq.nq) - 1, r0 = x.tile * kTile;
-      auto seen = [&](int row, int& lo, int& hi) {
-        if (KEYS) mha_queries_of(a.s, x.seq, min(row, last), lo, hi);
-        else mha_keys_of(a.s, x.seq, min(row, last), lo, hi);
-      };
-      int lo, hi, all_lo, all_hi, none;
-      seen(r0 + r, lo, hi);
-      seen(r0, none, all_hi);
-      seen(r0 + kTile - 1, all_lo, none);
-      float nlse = 0.f, ndelta = 0.f;
-      if (!KEYS) {
-        const int slot = mha_slot0(a.s.qb, x.index, x.seq.q0, kStatRows) + x.tile;
-        const float* st = a.stats + mha_stat_offset(x.head, a.stat_slots, slot);
+    int g = 0, steps = 0;
+    float nlse = 0.f, ndelta = 0.f;
+    // the unit's steps; queries stationary: its rows' statistics are on their way
+    auto fetch = [&](int n) -> bool {
+      if (!mbar_wait(&bar.unit_full[n % C::UNITS], (n / C::UNITS) & 1)) return false;
+      steps = entry(n)[0].x;
+      if (!KEYS && steps > 0) {
+        const float* st = a.stats + mha_stat_offset(entry(n)[0].y, a.stat_slots, entry(n)[2].w);
         nlse = st[r];
         ndelta = st[kStatRows + r];
       }
+      return true;
+    };
+    ok = __all_sync(0xffffffffu, fetch(0));
+    for (int n = 0; ok && steps > 0; ++n) {
+      const int4 e0 = entry(n)[0], e1 = entry(n)[1], e2 = entry(n)[2];
+      const int rows = e0.w, part = e1.w;
+      const MhaSeq seq{0, e1.y, 0, e1.z};
+      auto seen = [&](int row, int& lo, int& hi) {
+        if (KEYS) mha_queries_of(a.s, seq, e1.x + min(row, rows - 1), lo, hi);
+        else mha_keys_of(a.s, seq, e1.x + min(row, rows - 1), lo, hi);
+      };
+      int lo, hi, all_lo, all_hi, none;
+      seen(r, lo, hi);
+      seen(0, none, all_hi);
+      seen(kTile - 1, all_lo, none);
       // One step; MASK: some row does not see some streamed row.
-      auto step = [&](int i, auto mask) -> bool {
+      auto step = [&](int cc, auto mask) -> bool {
         constexpr bool MASK = decltype(mask)::value;
-        const int c0 = (x.j0 + (x.n0 + i) % x.tiles) * kTile + half * 64;
+        uint32_t bits[2] = {~0u, ~0u};
+        if (MASK) {
+          const int first = cc + half * 64;
+          bits[0] = column_bits(lo - first, hi - first);
+          bits[1] = column_bits(lo - first - 32, hi - first - 32);
+        }
         const uint32_t s_at = base + C::S_COL + (g % C::NS) * 128 + half * 64, dp_at = base + C::DP_COL + half * 64;
         const uint32_t st = smem_u32(smem + C::OFF_STAT + (KEYS ? g % C::Y1S : 0) * kStatBytes) + half * 256;
         if (!mbar_wait(&bar.s_full[g % C::NS], (g / C::NS) & 1)) return false;
@@ -452,11 +650,39 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int c = 0; c < 2; ++c) tmem_ld32(dp_at + c * 32, reinterpret_cast<uint32_t*>(dp + c * 32));
           return true;
         };
+        if constexpr (!KEYS && MASK) {  // (32 columns at a time: with the masks' registers more would spill)
+          if (!mbar_wait(bar.dp_full, g & 1)) return false;
+          tc_fence_after();
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            uint32_t pk[32];
+            tmem_ld32(dp_at + 32 * k, reinterpret_cast<uint32_t*>(dp));
+            tmem_wait_ld();
+            if (k == 1) {
+              tc_fence_before();
+              mbar_arrive(bar.dp_read);
+            }
+#pragma unroll
+            for (int c = 0; c < 32; ++c) p[32 * k + c] = bits[k] >> c & 1 ? ex2_approx(p[32 * k + c]) : 0.f;
+#pragma unroll
+            for (int c = 0; c < 32; c += 2) {
+              float v0, v1;
+              f2_unpack(f2_mul(f2_pack(p[32 * k + c], p[32 * k + c + 1]),
+                               f2_add(f2_pack(dp[c], dp[c + 1]), f2_pack(ndelta, ndelta))), v0, v1);
+              pk[c / 2] = pack_bf16(v0, v1);
+            }
+            tmem_st16(s_at + 16 * k, pk);
+          }
+          tmem_wait_st();
+          tc_fence_before();
+          mbar_arrive(&bar.ds_full[g & 1]);
+          return true;
+        }
         if (!KEYS && !read_dp()) return false;
 #pragma unroll
         for (int c = 0; c < 64; ++c) {
           p[c] = ex2_approx(p[c]);
-          if (MASK && (c0 + c < lo || c0 + c >= hi)) p[c] = 0.f;
+          if (MASK && !(bits[c / 32] >> (c % 32) & 1)) p[c] = 0.f;
         }
         if constexpr (KEYS) {
           uint32_t pk[32];
@@ -465,7 +691,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_st32(s_at, pk);
           tmem_wait_st();
           tc_fence_before();
-          mbar_arrive(bar.p_full);
+          mbar_arrive(&bar.p_full[g & 1]);
           if (!read_dp()) return false;
         }
         tmem_wait_ld();
@@ -482,69 +708,60 @@ __global__ void __launch_bounds__(kThreads, 1)
           float v[4];
           f2_unpack(f2_mul(f2_pack(p[c], p[c + 1]), f2_add(f2_pack(dp[c], dp[c + 1]), d01)), v[0], v[1]);
           f2_unpack(f2_mul(f2_pack(p[c + 2], p[c + 3]), f2_add(f2_pack(dp[c + 2], dp[c + 3]), d23)), v[2], v[3]);
-          if (MASK)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (c0 + c + k < lo || c0 + c + k >= hi) v[k] = 0.f;  // (0 times what may not be finite)
           pk[c / 2] = pack_bf16(v[0], v[1]);
           pk[c / 2 + 1] = pack_bf16(v[2], v[3]);
         }
         tmem_st32(KEYS ? dp_at : s_at, pk);
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(bar.ds_full);
+        mbar_arrive(&bar.ds_full[g & 1]);
         return true;
       };
-      for (int i = 0; i < x.steps; ++i, ++g) {
-        const int c0 = (x.j0 + (x.n0 + i) % x.tiles) * kTile;
+      const int begin0 = e2.x * kTile, end0 = begin0 + e2.y * kTile;
+      int cc = begin0 + e2.z * kTile;
+      for (int i = 0; i < steps; ++i, ++g) {
+        const int c0 = cc;
         // (streamed queries behind the sequence have probability 0 by their statistics)
-        const bool plain = c0 >= all_lo && (c0 + kTile <= all_hi || (KEYS && all_hi == x.seq.nq));
-        if (!(plain ? step(i, std::false_type{}) : step(i, std::true_type{}))) {
+        const bool plain = c0 >= all_lo && (c0 + kTile <= all_hi || (KEYS && all_hi == seq.nq));
+        if (!(plain ? step(cc, std::false_type{}) : step(cc, std::true_type{}))) {
           ok = false;
           break;
         }
+        cc = cc + kTile == end0 ? begin0 : cc + kTile;
       }
       // ------------------------------------------------ sums
-      if (ok && x.steps > 0) ok = mbar_wait(bar.sum_full, sums++ & 1);
+      if (ok) ok = fetch(n + 1) && mbar_wait(bar.sum_full, n & 1);
       ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
       tc_fence_after();
-      const bool mine = ok && r < x.rows;
+      constexpr int kChunks = C::SUMS * D / 64;  // of 32 columns, for each half
 #pragma unroll 1
-      for (int w = 0; w < C::SUMS; ++w) {
+      for (int k = 0; k < kChunks; ++k) {
+        const int w = (half * kChunks + k) / (D / 32), c = (half * kChunks + k) % (D / 32) * 32;
         __nv_bfloat16* out = w == 0 ? a.out1 : a.out2;
         const int64_t ld = w == 0 ? a.ld1 : a.ld2;
         const float by = w == 0 ? a.scale : 1.0f;
-#pragma unroll 1
-        for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
-          uint32_t o[32];
-          if (x.steps > 0) {
-            tmem_ld32(base + C::SUM_COL + w * D + c, o);
-            tmem_wait_ld();
-          } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = 0;
-          }
-          if (!ok) continue;
-          if (x.part >= 0) {
-            float* to = a.part + (((int64_t)x.part * C::SUMS + w) * (D / 4) + c / 4) * (kTile * 4) + r * 4;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              *reinterpret_cast<uint4*>(to + i * kTile * 4) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-            continue;
-          }
-          const int64_t at = (int64_t)(x.row0 + r) * ld + x.head * D + c;
-          if (!mine || out == nullptr || !ACID_IN_BOUNDS(kSiteMha, at + 31, (KEYS ? a.s.nk : a.s.nq) * ld)) continue;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            auto v = [&](int k) { return __uint_as_float(o[8 * i + k]) * by; };
-            reinterpret_cast<uint4*>(out + at)[i] =
-                make_uint4(pack_bf16(v(0), v(1)), pack_bf16(v(2), v(3)), pack_bf16(v(4), v(5)), pack_bf16(v(6), v(7)));
-          }
+        uint32_t o[32];
+        tmem_ld32(base + C::SUM_COL + w * D + c, o);
+        tmem_wait_ld();
+        if (k == kChunks - 1) {  // the sums have been read: the next unit's may begin
+          tc_fence_before();
+          mbar_arrive(bar.sum_empty);
         }
-      }
-      if (ok && x.steps > 0) {
-        tc_fence_before();
-        mbar_arrive(bar.sum_empty);
+        if (part >= 0) {
+          float* to = a.part + (((int64_t)part * C::SUMS + w) * (D / 4) + c / 4) * (kTile * 4) + r * 4;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            *reinterpret_cast<uint4*>(to + i * kTile * 4) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+          continue;
+        }
+        const int64_t at = (int64_t)(e0.z + r) * ld + e0.y * D + c;
+        if (r >= rows || out == nullptr || !ACID_IN_BOUNDS(kSiteMha, at + 31, (KEYS ? a.s.nk : a.s.nq) * ld)) continue;
+        uint32_t w16[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          w16[i] = pack_bf16(__uint_as_float(o[2 * i]) * by, __uint_as_float(o[2 * i + 1]) * by);
+        store_64_bytes(out + at, w16);
       }
     }
   }
@@ -556,57 +773,64 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-// Adds the shares of the split items in their order.  A thread has four columns of a
-// row; a warp 32 rows.
+// Adds the parts of the items that lie in several shares, in the shares' order: the
+// first in the share where the item begins, the others the first units of theirs.  A
+// thread has four columns of a row.
 template <int D, bool KEYS>
 __global__ void __launch_bounds__(256) mha_backward_join_kernel(const __grid_constant__ BwdArgs a) {
   constexpr int SUMS = KEYS ? 2 : 1;
   pdl_wait();
-  const int it = blockIdx.x, row = threadIdx.x & 127;
-  BwdUnit x;
-  if (!bwd_unit<KEYS>(a, a.full + it * a.splits, x) || row >= x.rows) return;
+  const int cta = blockIdx.x, row = threadIdx.x & 127;
+  const int4 e = a.record[2 * cta];  // {rows, row0, head, part}
+  if (row >= e.x) return;            // (no rows: no such item)
+  const int last = a.record[2 * cta + 1].x;
   const int idx = blockIdx.y * 2 + (threadIdx.x >> 7);  // quad of columns, of dk and then dv
   const int w = idx / (D / 4), c = idx % (D / 4) * 4;
   __nv_bfloat16* out = w == 0 ? a.out1 : a.out2;
   if (out == nullptr) return;
-  const float* p = a.part + ((int64_t)it * a.splits * SUMS * (D / 4) + idx) * (kTile * 4) + row * 4;
-  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s = 0; s < a.splits; ++s) {
-    const float4 v = *reinterpret_cast<const float4*>(p + (int64_t)s * SUMS * (D / 4) * (kTile * 4));
+  constexpr int64_t kPart = (int64_t)SUMS * (D / 4) * (kTile * 4);
+  const float* p = a.part + (int64_t)idx * (kTile * 4) + row * 4;
+  float4 sum = *reinterpret_cast<const float4*>(p + e.w * kPart);
+  for (int s = cta + 1; s <= last; ++s) {
+    const float4 v = *reinterpret_cast<const float4*>(p + 2 * s * kPart);
     sum.x += v.x;
     sum.y += v.y;
     sum.z += v.z;
     sum.w += v.w;
   }
   const float by = w == 0 ? a.scale : 1.0f;
-  const int64_t ld = w == 0 ? a.ld1 : a.ld2, at = (int64_t)(x.row0 + row) * ld + x.head * D + c;
+  const int64_t ld = w == 0 ? a.ld1 : a.ld2, at = (int64_t)(e.y + row) * ld + e.z * D + c;
   if (!ACID_IN_BOUNDS(kSiteMha, at + 3, (int64_t)(KEYS ? a.s.nk : a.s.nq) * ld)) return;
   *reinterpret_cast<uint2*>(out + at) = make_uint2(pack_bf16(sum.x * by, sum.y * by), pack_bf16(sum.z * by, sum.w * by));
 }
 
+// Which items go to the CTAs whole.  Fewer items than SMs: none, all their steps are
+// shared out evenly.  More: the CTAs take whole items, of one head after the other, so
+// that those at work at a time stream the same tiles out of L2 (8190 rows, 24 on 8 heads,
+// windows of five frames: 255 us, shared out evenly head by head 284); the last, partial
+// wave is shared out where all items are alike.  With sequences and windows lengths
+// differ, and many items even out.  Items of a few steps stay whole: a join takes as
+// long as three of them.
 struct BwdPlan {
-  int slots, items, full, splits;
+  int slots, items, full;
+  bool alike;
 };
-// As the forward pass: a few items are shared out so that they fill the GPU, and so is
-// the last wave of many where all are alike.
 BwdPlan bwd_plan(const MhaShape& s, bool keys, int sms) {
   BwdPlan p;
-  p.slots = mha_slots(keys ? s.nk : s.nq, s.seqs, (keys ? s.kb : s.qb) != nullptr, kTile);
+  const bool bounded = (keys ? s.kb : s.qb) != nullptr;
+  p.slots = mha_slots(keys ? s.nk : s.nq, s.seqs, bounded, kTile);
   p.items = p.slots * (keys ? s.kv_heads : s.heads);
+  p.alike = s.qb == nullptr && s.kb == nullptr && s.frame == 0;
+  const int64_t steps = ((int64_t)(keys ? s.nq : s.nk) / s.seqs + kTile - 1) / kTile * (keys ? s.group : 1);
   p.full = p.items;
-  p.splits = 1;
-  const int steps = ((keys ? s.nq : s.nk) / s.seqs + kTile - 1) / kTile * (keys ? s.group : 1);
-  const int whole = p.items / sms * sms, tail = p.items - whole;
-  const bool alike = s.seqs == 1 && s.frame == 0;
-  const int splits = tail > 0 ? std::min(sms / tail, steps / 2) : 1;
-  if ((whole == 0 || alike) && splits >= 2) {
-    p.full = whole;
-    p.splits = splits;
+  if (steps > 2 * kLeastSteps) {
+    if (p.items < sms) p.full = 0;
+    else if (p.alike) p.full = p.items / sms * sms;
   }
   return p;
 }
-size_t bwd_part_bytes(const BwdPlan& p, int sums, int d) {
-  return p.full < p.items ? (size_t)(p.items - p.full) * p.splits * sums * kTile * d * sizeof(float) : 0;
+size_t bwd_part_bytes(const BwdPlan& p, int sms, int sums, int d) {
+  return p.full < p.items ? (size_t)sms * (2 * sums * kTile * d * sizeof(float) + 2 * sizeof(int4)) : 0;
 }
 
 template <int D, bool KEYS>
@@ -623,7 +847,8 @@ acid_status launch(const MhaArgs& x, cudaStream_t s) {
   ACID_TRY(make_tmap_bf16(&tg, m.nq > 0 ? x.dout : any, nq, wq, x.lddo, kTile));
   ACID_TRY(make_tmap_bf16(&tk, m.nk > 0 ? x.k : any, nk, wk, x.ldk, kTile));
   ACID_TRY(make_tmap_bf16(&tv, m.nk > 0 ? x.v : any, nk, wk, x.ldv, kTile));
-  const BwdPlan p = bwd_plan(m, KEYS, num_sms());
+  const int sms = num_sms();
+  const BwdPlan p = bwd_plan(m, KEYS, sms);
   BwdArgs a = {};
   a.s = m;
   a.stats = x.stats;
@@ -636,15 +861,19 @@ acid_status launch(const MhaArgs& x, cudaStream_t s) {
   a.slots = p.slots;
   a.stat_slots = mha_slots(m.nq, m.seqs, m.qb != nullptr, kStatRows);
   a.heads = KEYS ? m.kv_heads : m.heads;
+  a.items = p.items;
   a.full = p.full;
-  a.splits = p.splits;
-  a.units = p.full + (p.items - p.full) * p.splits;
+  a.alike = p.alike;
+  a.longest = m.frame != 0 && p.full == p.items;
+  const bool shared = p.full < p.items;
+  const int ctas = shared ? sms : std::min(p.items, sms);
   a.part = static_cast<float*>(x.part);
-  launch_pdl(mha_backward_kernel<C>, std::min(a.units, num_sms()), kThreads, C::SMEM, s, KEYS ? tk : tq, KEYS ? tv : tg,
-             KEYS ? tq : tk, KEYS ? tg : tv, a);
+  a.record = reinterpret_cast<int4*>(a.part + (size_t)sms * 2 * C::SUMS * kTile * D);
+  launch_pdl(mha_backward_kernel<C>, ctas, kThreads, C::SMEM, s, KEYS ? tk : tq, KEYS ? tv : tg, KEYS ? tq : tk,
+             KEYS ? tg : tv, a);
   ACID_CHECK_LAUNCH();
-  if (p.full < p.items) {
-    launch_pdl(mha_backward_join_kernel<D, KEYS>, dim3(p.items - p.full, C::SUMS * D / 8), 256, 0, s, a);
+  if (shared) {
+    launch_pdl(mha_backward_join_kernel<D, KEYS>, dim3(ctas, C::SUMS * D / 8), 256, 0, s, a);
     ACID_CHECK_LAUNCH();
   }
   return ACID_OK;
@@ -654,8 +883,8 @@ acid_status launch(const MhaArgs& x, cudaStream_t s) {
 
 size_t mha_backward_tc_bytes(const MhaArgs& x) {
   const int sms = num_sms();
-  return std::max(bwd_part_bytes(bwd_plan(x.shape, true, sms), 2, x.head_dim),
-                  bwd_part_bytes(bwd_plan(x.shape, false, sms), 1, x.head_dim));
+  return std::max(bwd_part_bytes(bwd_plan(x.shape, true, sms), sms, 2, x.head_dim),
+                  bwd_part_bytes(bwd_plan(x.shape, false, sms), sms, 1, x.head_dim));
 }
 
 acid_status mha_backward_tc(const MhaArgs& x, cudaStream_t s) {
