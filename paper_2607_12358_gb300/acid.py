@@ -459,34 +459,42 @@ def acid_norm_site_backward(du: torch.Tensor | None, r: torch.Tensor | None, y: 
 # rotary positions with several axes
 # ---------------------------------------------------------------------------
 
-def _rope(call, x, heads, axes, theta, grid, origin, positions, first_rows, halves, out, stream):
-    empty = _empty_on(stream)
-    if x.dim() != 2 or x.dtype not in _DT:
-        raise ValueError("need a [rows, heads * head_dim] tensor of bf16 or fp32")
-    rows, width = x.shape
-    if heads < 1 or width % heads:
-        raise ValueError("the columns must be heads of one head_dim")
+@functools.lru_cache(maxsize=1024)
+def _rope_desc(rows, width, dtype, heads, axes, theta, grid, origin, first_rows, halves):
+    """The C description of a rotation, but for positions of the caller's own."""
     n = len(axes)
     if not 1 <= n <= 4:
         raise ValueError("need 1 to 4 axes")
-    thetas = (theta,) * n if isinstance(theta, (int, float)) else tuple(theta)
-    origin = (0.0,) * n if origin is None else tuple(origin)
-    if (grid is None) == (positions is None):
-        raise ValueError("need either grid or positions")
+    if heads < 1 or width % heads:
+        raise ValueError("the columns must be heads of one head_dim")
+    thetas = theta if isinstance(theta, tuple) else (theta,) * n
+    origin = (0.0,) * n if origin is None else origin
     if len(thetas) != n or len(origin) != n or (grid is not None and len(grid) != n):
         raise ValueError(f"theta, grid and origin must have {n} entries, as axes has")
-    pp, ld_pos = None, 0
-    if positions is not None:
-        ld_pos, pp = _rows_of("positions", positions, rows, n, _F32), positions.data_ptr()
-        grid = ()
-    ldx = _rows_of("x", x, rows, width, x.dtype)
-    if out is None:
-        out, ldo = empty((rows, width), dtype=x.dtype, device=x.device), width
-    else:
-        ldo = _rows_of("out", out, rows, width, x.dtype)
     i4, f4 = C.c_int32 * 4, C.c_float * 4
-    desc = A.acid_rope(rows, heads, width // heads, _DT[x.dtype], n, i4(*axes), f4(*thetas), halves, first_rows, pp,
-                       ld_pos, i4(*grid), f4(*origin))
+    return A.acid_rope(rows, heads, width // heads, _DT[dtype], n, i4(*axes), f4(*thetas), halves, first_rows, None, 0,
+                       i4(*(grid or ())), f4(*origin))
+
+
+def _rope(call, x, heads, axes, theta, grid, origin, positions, first_rows, halves, out, stream):
+    dtype = x.dtype
+    if x.dim() != 2 or dtype not in _DT:
+        raise ValueError("need a [rows, heads * head_dim] tensor of bf16 or fp32")
+    if (grid is None) == (positions is None):
+        raise ValueError("need either grid or positions")
+    rows, width = x.shape
+    desc = _rope_desc(rows, width, dtype, heads, tuple(axes), theta if isinstance(theta, float) else
+                      float(theta) if isinstance(theta, int) else tuple(theta), None if grid is None else tuple(grid),
+                      None if origin is None else tuple(origin), first_rows, halves)
+    if positions is not None:
+        ld = _rows_of("positions", positions, rows, desc.axes, _F32)
+        desc = A.acid_rope.from_buffer_copy(desc)
+        desc.positions, desc.ld_pos = positions.data_ptr(), ld
+    ldx = _rows_of("x", x, rows, width, dtype)
+    if out is None:
+        out, ldo = _empty_on(stream)((rows, width), dtype=dtype, device=x.device), width
+    else:
+        ldo = _rows_of("out", out, rows, width, dtype)
     status = call(C.byref(desc), x.data_ptr(), ldx, out.data_ptr(), ldo, _stream(stream))
     if status:
         check(status)
@@ -557,6 +565,24 @@ def mha_workspace_size(desc: A.acid_mha, backward: bool = False) -> int:
     return b.value
 
 
+@functools.lru_cache(maxsize=1024)
+def _mha_bytes(nq, nk, dtype, heads, kv_heads, d, seqs, q_bounded, k_bounded, windowed, backward):
+    """Workspace of a call: the size goes by these alone (an address that nothing reads stands for bounds)."""
+    return mha_workspace_size(A.acid_mha(nq, nk, dtype, heads, kv_heads, d, 1.0, seqs, 8 if q_bounded else None,
+                                         8 if k_bounded else None, windowed, 0, 0, 0), backward)
+
+
+def _mha_scratch(desc, backward, device, stream):
+    """(address, bytes, owner) of a workspace for the call."""
+    nws = _mha_bytes(desc.nq, desc.nk, desc.dtype, desc.heads, desc.kv_heads, desc.head_dim, desc.sequences,
+                     desc.q_bounds is not None, desc.k_bounds is not None,
+                     int(desc.frame_rows > 0 and (desc.frames_before >= 0 or desc.frames_after >= 0)), backward)
+    if not nws:
+        return None, 0, None
+    ws = _empty_on(stream)(nws, dtype=torch.uint8, device=device)
+    return ws.data_ptr(), nws, ws
+
+
 def mha_workspace(q: torch.Tensor, k: torch.Tensor, heads: int, *, backward: bool = False,
                   q_bounds: torch.Tensor | None = None, k_bounds: torch.Tensor | None = None) -> torch.Tensor:
     """A workspace for acid_mha_forward or acid_mha_backward of operands of these shapes, with any window of frames."""
@@ -604,14 +630,10 @@ def acid_mha_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, heads: i
         lse = blank((heads, nq), dtype=_F32, device=q.device)
     elif lse.dtype is not _F32 or not lse.is_cuda or lse.shape != (heads, nq) or not lse.is_contiguous():
         raise ValueError(f"lse must be a contiguous CUDA fp32 tensor [{heads}, {nq}]")
-    ws = nws = 0
     if workspace is not None:
         ws, nws = _workspace(workspace)
     else:
-        nws = mha_workspace_size(desc)
-        if nws:
-            workspace = _empty_on(stream)(nws, dtype=torch.uint8, device=q.device)
-            ws = workspace.data_ptr()
+        ws, nws, workspace = _mha_scratch(desc, False, q.device, stream)
     status = load().acid_mha_forward(C.byref(desc), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
                                      out.data_ptr(), ldo, lse.data_ptr(), ws, nws, _stream(stream))
     if status:
@@ -647,9 +669,7 @@ def acid_mha_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: t
     if workspace is not None:
         ws, nws = _workspace(workspace)
     else:
-        nws = mha_workspace_size(desc, True)
-        workspace = _empty_on(stream)(nws, dtype=torch.uint8, device=q.device)
-        ws = workspace.data_ptr()
+        ws, nws, workspace = _mha_scratch(desc, True, q.device, stream)
     fields = A.acid_mha_grads(*fields)
     status = load().acid_mha_backward(C.byref(desc), dout.data_ptr(), ldg, q.data_ptr(), ldq, k.data_ptr(), ldk,
                                       v.data_ptr(), ldv, out.data_ptr(), ldo, lse.data_ptr(), C.byref(fields), ws, nws,

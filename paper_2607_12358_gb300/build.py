@@ -28,7 +28,7 @@ LIB_DEBUG = os.path.join(PKG, "libacid_gb300_debug.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["capi.cu", "elementwise.cu", "gemm.cu", "attention.cu", "block.cu", "loop.cu", "site.cu", "q4.cu", "q4_rows.cu",
            "rope.cu", "mha.cu", "mha_f32.cu", "mha_forward.cu", "mha_backward.cu",
-           "noalloc.cu"]
+           "mha_few.cu", "noalloc.cu"]
 
 
 def nvcc() -> str:

@@ -26,6 +26,7 @@ BoundsRecord take_bounds_q4_rows();
 BoundsRecord take_bounds_rope();
 BoundsRecord take_bounds_mha();
 BoundsRecord take_bounds_mha_f32();
+BoundsRecord take_bounds_mha_few();
 BoundsRecord take_bounds_mha_forward();
 unsigned int take_device_error_mha_forward();
 BoundsRecord take_bounds_mha_backward();
@@ -236,7 +237,7 @@ extern "C" acid_status acid_bounds_report(int32_t* checked, int64_t* site, int64
   const BoundsRecord recs[] = {take_bounds_elementwise(), take_bounds_gemm(), take_bounds_attention(), take_bounds_site(),
                                take_bounds_q4(),          take_bounds_q4_rows(), take_bounds_rope(), take_bounds_mha(),
                                take_bounds_mha_f32(),     take_bounds_mha_forward(),
-                               take_bounds_mha_backward(), take_bounds_capi()};
+                               take_bounds_mha_backward(), take_bounds_mha_few(), take_bounds_capi()};
   *checked = kBoundsChecked ? 1 : 0;
   *site = *index = *extent = 0;
   for (const BoundsRecord& r : recs) {

@@ -131,7 +131,10 @@ int stat_slots(const acid_mha& m) { return mha_slots((int)m.nq, m.sequences, m.q
 size_t stat_bytes(const acid_mha& m) { return (size_t)mha_stat_offset(m.heads, stat_slots(m), 0) * sizeof(float); }
 
 size_t forward_bytes(const acid_mha& m) {
-  return m.dtype == ACID_BF16 && m.nq > 0 ? mha_forward_tc_bytes(common_args(m)) : 0;
+  const MhaArgs a = common_args(m);
+  if (m.nq == 0) return 0;
+  if (mha_few(a.shape)) return mha_few_bytes(a);
+  return m.dtype == ACID_BF16 ? mha_forward_tc_bytes(a) : 0;
 }
 size_t backward_bytes(const acid_mha& m) {
   return stat_bytes(m) + (m.dtype == ACID_BF16 ? mha_backward_tc_bytes(common_args(m)) : 0);
@@ -192,6 +195,7 @@ extern "C" acid_status acid_mha_forward(const acid_mha* mha, const void* q, int6
   a.lse = lse;
   a.part = ws;
   a.part_bytes = ws_bytes;
+  if (mha_few(a.shape)) return mha_forward_few(a, (cudaStream_t)stream);
   return m.dtype == ACID_BF16 ? mha_forward_tc(a, (cudaStream_t)stream) : mha_forward_f32(a, (cudaStream_t)stream);
 }
 

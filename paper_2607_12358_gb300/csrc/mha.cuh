@@ -70,6 +70,32 @@ __device__ __forceinline__ bool mha_slot(const MhaShape& s, int slot, MhaSeq& se
   return tile >= 0 && tile < (rows + TILE - 1) / TILE;
 }
 
+// Order in which CTAs take the items, one of `heads` and a slot each, in turn.
+//   By head: those at work at a time stream the same keys (or queries) out of L2.
+//   By slot, all heads of a slot together: a round of CTAs then has items of one
+// sequence or one frame, which are as long as each other, so that the rounds come out
+// even (4726, 2501 and 1013 rows, 30 heads: the longest CTA has 196 tiles instead of 225,
+// 184.5 on average).  Under a window the items with the most tiles come first: a causal
+// one's last queries, its first keys.
+enum MhaOrder : int { kByHead = 0, kBySlot = 1, kBySlotDown = 2 };
+__host__ __device__ __forceinline__ void mha_item(int order, int slots, int heads, int item, int& slot, int& head) {
+  if (order == kByHead) {
+    slot = item % slots;
+    head = item / slots;
+  } else {
+    slot = item / heads;
+    if (order == kBySlotDown) slot = slots - 1 - slot;
+    head = item % heads;
+  }
+}
+// By slot all heads' streamed rows are in use together; with sequences, whose items have
+// all of them to read, only where L2 holds them.
+inline int mha_order(const MhaShape& s, int d, bool queries_streamed, bool first_longest) {
+  const int64_t bytes = queries_streamed ? (int64_t)s.nq * s.heads * d * 4 : (int64_t)s.nk * s.kv_heads * d * 4;
+  if (s.frame != 0) return first_longest ? kBySlot : kBySlotDown;
+  return s.seqs > 1 && bytes <= (int64_t)80 << 20 ? kBySlot : kByHead;
+}
+
 __device__ __forceinline__ int floor_div(int a, int b) { return a >= 0 ? a / b : -((b - 1 - a) / b); }
 __device__ __forceinline__ int clamp_row(int64_t v, int n) { return (int)min(max(v, (int64_t)0), (int64_t)n); }
 
@@ -123,6 +149,10 @@ struct MhaArgs {
   size_t part_bytes;
 };
 
+// mha_few.cu: a few query rows.  Whether a call is one, and its bytes of scratch.
+bool mha_few(const MhaShape& s);
+size_t mha_few_bytes(const MhaArgs& a);
+acid_status mha_forward_few(const MhaArgs& a, cudaStream_t s);
 // mha_forward.cu: bf16 on tcgen05.  Bytes of scratch (part) that the call needs.
 size_t mha_forward_tc_bytes(const MhaArgs& a);
 acid_status mha_forward_tc(const MhaArgs& a, cudaStream_t s);

@@ -43,7 +43,7 @@ struct BwdArgs {
   int items;      // stationary tiles and heads
   int full;       // items [0, full) go to the CTAs whole, one in turn; the others' steps are shared out
   int alike;      // every item has the same steps
-  int longest;    // items with the most steps first (whole items under a window of frames)
+  int order;      // of the items (MhaOrder)
   float* part;    // [2 CTAs][1 or 2][D / 4][128 rows][4]: sums of an item's share
   int4* record;   // [CTAs][2]: the item that begins in a CTA's share and ends in another's
 };
@@ -60,16 +60,6 @@ struct BwdUnit {
   int stat;        // keys stationary: slot of the sequence's first queries; else of this tile's
 };
 
-__device__ __forceinline__ void bwd_place(const BwdArgs& a, int item, int& slot, int& head, bool keys) {
-  if (!a.longest) {
-    slot = item % a.slots;
-    head = item / a.slots;
-  } else {  // causal: the first keys, the last queries
-    slot = item / a.heads;
-    if (!keys) slot = a.slots - 1 - slot;
-    head = item % a.heads;
-  }
-}
 // An item with all its steps (which may be none); false: an empty slot.
 template <bool KEYS>
 __device__ __forceinline__ bool bwd_item(const BwdArgs& a, int slot, int head, BwdUnit& x) {
@@ -193,7 +183,7 @@ struct BwdWalk {
   __device__ __forceinline__ bool operator()(BwdUnit& x, int d) {
     int slot, head;
     for (; !shared && next < a.full; next += gridDim.x) {
-      bwd_place(a, next, slot, head, KEYS);
+      mha_item(a.order, a.slots, a.heads, next, slot, head);
       if (!bwd_item<KEYS>(a, slot, head, x)) continue;
       if (x.steps == 0) {
         clear(x, d);
@@ -205,7 +195,7 @@ struct BwdWalk {
     if (a.full == a.items) return false;
     if (!shared) share_out();
     for (; next < a.items; ++next) {
-      bwd_place(a, next, slot, head, KEYS);
+      mha_item(a.order, a.slots, a.heads, next, slot, head);
       if (!bwd_item<KEYS>(a, slot, head, x)) continue;
       if (x.steps == 0) {
         clear(x, d);
@@ -814,8 +804,9 @@ __global__ void __launch_bounds__(256) mha_backward_join_kernel(const __grid_con
 struct BwdPlan {
   int slots, items, full;
   bool alike;
+  int order;
 };
-BwdPlan bwd_plan(const MhaShape& s, bool keys, int sms) {
+BwdPlan bwd_plan(const MhaShape& s, int d, bool keys, int sms) {
   BwdPlan p;
   const bool bounded = (keys ? s.kb : s.qb) != nullptr;
   p.slots = mha_slots(keys ? s.nk : s.nq, s.seqs, bounded, kTile);
@@ -823,10 +814,12 @@ BwdPlan bwd_plan(const MhaShape& s, bool keys, int sms) {
   p.alike = s.qb == nullptr && s.kb == nullptr && s.frame == 0;
   const int64_t steps = ((int64_t)(keys ? s.nq : s.nk) / s.seqs + kTile - 1) / kTile * (keys ? s.group : 1);
   p.full = p.items;
+  p.order = kByHead;
   if (steps > 2 * kLeastSteps) {
     if (p.items < sms) p.full = 0;
     else if (p.alike) p.full = p.items / sms * sms;
   }
+  if (p.full == p.items) p.order = mha_order(s, d, keys, keys);
   return p;
 }
 size_t bwd_part_bytes(const BwdPlan& p, int sms, int sums, int d) {
@@ -848,7 +841,7 @@ acid_status launch(const MhaArgs& x, cudaStream_t s) {
   ACID_TRY(make_tmap_bf16(&tk, m.nk > 0 ? x.k : any, nk, wk, x.ldk, kTile));
   ACID_TRY(make_tmap_bf16(&tv, m.nk > 0 ? x.v : any, nk, wk, x.ldv, kTile));
   const int sms = num_sms();
-  const BwdPlan p = bwd_plan(m, KEYS, sms);
+  const BwdPlan p = bwd_plan(m, D, KEYS, sms);
   BwdArgs a = {};
   a.s = m;
   a.stats = x.stats;
@@ -864,7 +857,7 @@ acid_status launch(const MhaArgs& x, cudaStream_t s) {
   a.items = p.items;
   a.full = p.full;
   a.alike = p.alike;
-  a.longest = m.frame != 0 && p.full == p.items;
+  a.order = p.order;
   const bool shared = p.full < p.items;
   const int ctas = shared ? sms : std::min(p.items, sms);
   a.part = static_cast<float*>(x.part);
@@ -883,8 +876,8 @@ acid_status launch(const MhaArgs& x, cudaStream_t s) {
 
 size_t mha_backward_tc_bytes(const MhaArgs& x) {
   const int sms = num_sms();
-  return std::max(bwd_part_bytes(bwd_plan(x.shape, true, sms), sms, 2, x.head_dim),
-                  bwd_part_bytes(bwd_plan(x.shape, false, sms), sms, 1, x.head_dim));
+  return std::max(bwd_part_bytes(bwd_plan(x.shape, x.head_dim, true, sms), sms, 2, x.head_dim),
+                  bwd_part_bytes(bwd_plan(x.shape, x.head_dim, false, sms), sms, 1, x.head_dim));
 }
 
 acid_status mha_backward_tc(const MhaArgs& x, cudaStream_t s) {

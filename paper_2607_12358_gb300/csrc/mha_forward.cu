@@ -26,6 +26,7 @@ struct FwdArgs {
   int64_t ldo;
   float scale_log2;
   int slots;   // of query-tile pairs
+  int order;   // of the items (MhaOrder)
   int full;    // items that one CTA takes whole; the rest are split along their keys
   int splits;  // CTAs to a split item
   int units;
@@ -42,19 +43,6 @@ struct FwdUnit {
   MhaSeq seq;
 };
 
-// Items are taken slot by slot within a head (its keys stay in L2); with windows of
-// frames, whose tiles differ in length, from the last slot down, all heads of a slot
-// together, so that the longest items of a causal window come first.
-__device__ __forceinline__ void item_of(const FwdArgs& a, int u, int& slot, int& head) {
-  if (a.s.frame == 0) {
-    slot = u % a.slots;
-    head = u / a.slots;
-  } else {
-    slot = a.slots - 1 - u / a.s.heads;
-    head = u % a.s.heads;
-  }
-}
-
 // False: nothing there (an empty slot).
 template <class C>
 __device__ __forceinline__ bool fwd_unit(const FwdArgs& a, int u, FwdUnit& x) {
@@ -65,7 +53,7 @@ __device__ __forceinline__ bool fwd_unit(const FwdArgs& a, int u, FwdUnit& x) {
     item = a.full + x.part / a.splits;
     split = x.part % a.splits;
   }
-  item_of(a, item, slot, x.head);
+  mha_item(a.order, a.slots, a.s.heads, item, slot, x.head);
   if (!mha_slot<kBQ, false>(a.s, slot, x.seq, index, x.tile)) return false;
   const int r0 = x.tile * kBQ;
   x.q0 = x.seq.q0 + r0;
@@ -345,7 +333,7 @@ __global__ void __launch_bounds__(256) mha_merge_kernel(const __grid_constant__ 
   const int it = wrow / kBQ, rr = wrow % kBQ;
   int slot, head, index, tile;
   MhaSeq seq;
-  item_of(a, a.full + it, slot, head);
+  mha_item(a.order, a.slots, a.s.heads, a.full + it, slot, head);
   if (!mha_slot<kBQ, false>(a.s, slot, seq, index, tile) || tile * kBQ + rr >= seq.nq) return;
   const int64_t row = seq.q0 + tile * kBQ + rr;
   const float* ml = a.part_ml + ((int64_t)it * a.splits * kBQ + rr) * 2;
@@ -423,6 +411,7 @@ acid_status launch(const MhaArgs& x, cudaStream_t s) {
   a.ldo = x.ldo;
   a.scale_log2 = x.scale * 1.4426950408889634f;
   a.slots = p.slots;
+  a.order = mha_order(m, D, false, false);
   a.full = p.full;
   a.splits = p.splits;
   a.units = p.full + (p.items - p.full) * p.splits;

@@ -148,8 +148,10 @@ acid_status rope_entry(const acid_rope* r, const void* x, int64_t ldx, void* out
                  "rope: axes must have an even number of columns, no more than head_dim in all");
     ACID_REQUIRE(r->theta[ax] > 0 && isfinite(r->theta[ax]), ACID_ERR_INVALID_ARG,
                  "rope: theta must be positive and finite");
-    for (int j = 0; j < n / 2; ++j, ++a.pairs) {
-      const double turns = pow((double)r->theta[ax], -2.0 * j / n) / 6.283185307179586476925286766559;
+    // (a product a pair: 64 powers would take longer than the smallest calls' kernel)
+    const double ratio = pow((double)r->theta[ax], -2.0 / n);
+    double turns = 1.0 / 6.283185307179586476925286766559;
+    for (int j = 0; j < n / 2; ++j, ++a.pairs, turns *= ratio) {
       a.hi[a.pairs] = (float)turns;
       a.lo[a.pairs] = (float)(turns - (double)a.hi[a.pairs]);
       a.axis[a.pairs] = (uint8_t)ax;

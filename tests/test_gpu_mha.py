@@ -147,6 +147,16 @@ CASES = {
     "one row, one key, 128": ((B, 1, 1, 128, [1], [1]), {}),
     "one row, many keys": ((B, 3, 3, 128, [1], [1000]), {}),
     "many rows, one key": ((B, 2, 2, 64, [300], [1]), {}),
+    "two rows": ((B, 2, 2, 64, [2], [300]), {}),
+    "four rows, shared": ((B, 6, 2, 128, [4], [700]), {}),
+    "five rows": ((B, 2, 2, 128, [5], [700]), {}),
+    "one row, five heads on one": ((B, 5, 1, 64, [1], [513]), {}),
+    "one row each": ((B, 4, 2, 128, [1, 1, 0, 1, 1, 1], [300, 1, 50, 0, 64, 1000]), {}),
+    "a few rows each, padded": ((B, 4, 1, 64, [3, 1, 4, 0], [60, 64, 1, 13]), dict(room=64)),
+    "a few rows, behind": ((B, 2, 2, 64, [3], [100]), dict(behind=1)),
+    "a few rows, window": ((B, 2, 2, 128, [4], [400]), dict(frame=2, before=40, after=0, q_first=-1)),
+    "a few rows that see nothing": ((B, 2, 1, 64, [4], [60]), dict(frame=1, before=0, after=0, q_first=58)),
+    "one row, no scale": ((B, 2, 2, 64, [1], [200]), dict(scale=0.0)),
     "127": ((B, 1, 1, 128, [127], [127]), {}),
     "128": ((B, 1, 1, 128, [128], [128]), {}),
     "129": ((B, 2, 2, 64, [129], [129]), {}),
@@ -176,6 +186,10 @@ CASES = {
     "fp32 64": ((F, 4, 4, 64, [100], [100]), {}),
     "fp32 96, shared": ((F, 4, 2, 96, [33], [129]), {}),
     "fp32 128": ((F, 2, 2, 128, [130], [257]), {}),
+    "fp32 one of many": ((F, 4, 2, 96, [1], [900]), {}),
+    "fp32 one of many, 32": ((F, 3, 1, 32, [3], [300]), {}),
+    "fp32 one of many, 128": ((F, 8, 2, 128, [2], [300]), dict(frame=1, after=0, q_first=-1)),
+    "fp32 one each": ((F, 2, 2, 64, [1, 1, 1], [200, 3, 77]), dict(room=256)),
     "fp32 one": ((F, 1, 1, 32, [1], [1]), {}),
     "fp32 packed": ((F, 2, 1, 64, [5, 0, 40, 17], [17, 9, 33, 1]), {}),
     "fp32 padded": ((F, 2, 2, 64, [30, 50], [7, 48]), dict(room=64)),
