@@ -35,29 +35,41 @@ __global__ void __launch_bounds__(kThreads) mha_stats_kernel(const StatArgs a, i
   MhaSeq seq;
   int index, tile;
   if (!mha_slot<kStatRows, false>(a.s, blockIdx.x, seq, index, tile)) return;
-  const int h = blockIdx.y, part = threadIdx.x % lanes;
+  const int h = blockIdx.y, part = threadIdx.x % lanes, step = kThreads / lanes;
   float* to = a.stats + mha_stat_offset(h, a.slots, blockIdx.x);
-  for (int r = threadIdx.x / lanes; r < kStatRows; r += kThreads / lanes) {
-    const int i = tile * kStatRows + r;
-    float sum = 0.f, nlse = -INFINITY;
-    if (i < seq.nq) {
+  constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;  // rows whose loads are on the way together
+  for (int r0 = threadIdx.x / lanes; r0 < kStatRows; r0 += kAhead * step) {
+    MhaRaw<T> o[kAhead], g[kAhead];
+    float lse[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int i = tile * kStatRows + r0 + k * step;
+      o[k].zero();
+      g[k].zero();
+      lse[k] = -INFINITY;
+      if (i >= seq.nq || r0 + k * step >= kStatRows) continue;
       const int64_t row = seq.q0 + i;
       const int64_t at = row * a.ldo + h * a.d + part * 8, from = row * a.lddo + h * a.d + part * 8;
       if (part * 8 < a.d && ACID_IN_BOUNDS(kSiteMha, at + 7, (int64_t)a.s.nq * a.ldo) &&
           ACID_IN_BOUNDS(kSiteMha, from + 7, (int64_t)a.s.nq * a.lddo)) {
-        float o[8], g[8];
-        load8(static_cast<const T*>(a.out) + at, o);
-        load8(static_cast<const T*>(a.dout) + from, g);
-#pragma unroll
-        for (int c = 0; c < 8; ++c) sum = fmaf(o[c], g[c], sum);
+        o[k].load(static_cast<const T*>(a.out) + at);
+        g[k].load(static_cast<const T*>(a.dout) + from);
       }
-      const float lse = a.lse[(int64_t)h * a.s.nq + row];
-      if (lse != -INFINITY) nlse = -lse * a.unit;  // (a row that sees no key: probability 0)
+      lse[k] = a.lse[(int64_t)h * a.s.nq + row];
     }
-    for (int off = lanes / 2; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-    if (part == 0) {
-      to[r] = nlse;
-      to[kStatRows + r] = nlse == -INFINITY ? 0.f : -sum;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      float x[8], y[8], sum = 0.f;
+      o[k].get(x);
+      g[k].get(y);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) sum = fmaf(x[c], y[c], sum);
+      for (int off = lanes / 2; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+      const int r = r0 + k * step;
+      if (part == 0 && r < kStatRows) {
+        to[r] = lse[k] == -INFINITY ? -INFINITY : -lse[k] * a.unit;  // (a row that sees no key: probability 0)
+        to[kStatRows + r] = lse[k] == -INFINITY ? 0.f : -sum;
+      }
     }
   }
 }
@@ -75,10 +87,10 @@ acid_status check_mha(const acid_mha* m) {
   else
     ACID_REQUIRE(m->head_dim > 0 && m->head_dim % 32 == 0 && m->head_dim <= 128, ACID_ERR_UNSUPPORTED,
                  "mha fp32: head_dim must be 32, 64, 96 or 128");
-  ACID_REQUIRE((std::max(m->nq, m->nk) / 128 + 65536) * m->heads <= (int64_t)1 << 32, ACID_ERR_UNSUPPORTED,
-               "mha: too many rows and heads");
   ACID_REQUIRE(isfinite(m->scale), ACID_ERR_INVALID_ARG, "mha: scale must be finite");
   ACID_REQUIRE(m->sequences >= 1 && m->sequences <= 65535, ACID_ERR_INVALID_ARG, "mha: need 1 to 65535 sequences");
+  ACID_REQUIRE((std::max(m->nq, m->nk) / 64 + m->sequences + 1) * m->heads <= (int64_t)1 << 30, ACID_ERR_UNSUPPORTED,
+               "mha: too many rows and heads");
   ACID_REQUIRE(m->sequences == 1 || (m->q_bounds != nullptr && m->k_bounds != nullptr), ACID_ERR_INVALID_ARG,
                "mha: several sequences need the bounds of both queries and keys");
   ACID_REQUIRE(aligned(m->q_bounds, 8) && aligned(m->k_bounds, 8), ACID_ERR_UNSUPPORTED,

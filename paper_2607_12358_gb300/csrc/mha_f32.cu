@@ -1,6 +1,8 @@
 // Attention with row sums, and its gradient, on the FP32 pipes.
 #include <math.h>
 
+#include <algorithm>
+
 #define ACID_UNIT_WITHOUT_WAITS
 #include "mha.cuh"
 
@@ -13,17 +15,15 @@ namespace {
 
 constexpr int kGroups = 4, kCols = 32, kThreads = 128 * kGroups;  // groups of four warps; rows of a streamed tile
 
-// N rows of D values (row stride lds in shared memory); rows outside [0, valid) are
-// zeros.
+// N rows of D values (row stride lds in shared memory) on their way (cp.async); rows
+// outside [0, valid) are zeros.
 template <int D, int N>
 __device__ __forceinline__ void load_rows(float* dst, int lds, const float* src, int64_t ld, int valid, int tid,
                                           int threads) {
-  for (int i = tid; i < N * (D / 8); i += threads) {
-    const int r = i / (D / 8), c = (i % (D / 8)) * 8;
-    float v[8] = {};
-    if (r < valid) load8(src + (int64_t)r * ld + c, v);
-    *reinterpret_cast<float4*>(dst + r * lds + c) = make_float4(v[0], v[1], v[2], v[3]);
-    *reinterpret_cast<float4*>(dst + r * lds + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
+  for (int i = tid; i < N * (D / 4); i += threads) {
+    const int r = i / (D / 4), c = (i % (D / 4)) * 4;
+    const bool on = r < valid;
+    cp_async<16>(dst + r * lds + c, src + (on ? (int64_t)r * ld + c : 0), on);
   }
 }
 
@@ -52,19 +52,24 @@ template <int D, int R>
 __device__ __forceinline__ void accumulate(const float* p, int ldp, const float* b, int lds, int kg,
                                            float (&acc)[R][D / 16]) {
 #pragma unroll 2
-  for (int k = 0; k < kCols; ++k) {
-    float bv[D / 16];
+  for (int k0 = 0; k0 < kCols; k0 += 4) {
+    float4 pv[R];
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c) {
-      const float2 t = *reinterpret_cast<const float2*>(b + k * lds + 32 * c + 2 * kg);
-      bv[2 * c] = t.x;
-      bv[2 * c + 1] = t.y;
-    }
+    for (int i = 0; i < R; ++i) pv[i] = *reinterpret_cast<const float4*>(p + i * ldp + k0);
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const float w = p[i * ldp + k];
+    for (int kk = 0; kk < 4; ++kk) {
+      float2 bv[D / 32];
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) acc[i][c] = fmaf(w, bv[c], acc[i][c]);
+      for (int c = 0; c < D / 32; ++c) bv[c] = *reinterpret_cast<const float2*>(b + (k0 + kk) * lds + 32 * c + 2 * kg);
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const float w = kk == 0 ? pv[i].x : kk == 1 ? pv[i].y : kk == 2 ? pv[i].z : pv[i].w;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          acc[i][2 * c] = fmaf(w, bv[c].x, acc[i][2 * c]);
+          acc[i][2 * c + 1] = fmaf(w, bv[c].y, acc[i][2 * c + 1]);
+        }
+      }
     }
   }
 }
@@ -73,19 +78,24 @@ struct F32Args {
   MhaShape s;
   const void *q, *k, *v, *o, *dout;
   int64_t ldq, ldk, ldv, ldo, lddo;
-  void *out1, *out2;  // forward: out; keys: dk, dv; queries: dq
-  int64_t ld1, ld2;
+  void *out1, *out2, *out3;  // forward: out; backward: dk, dv, dq
+  int64_t ld1, ld2, ld3;
   float *lse, *stats;
   float scale;
   int stat_slots;
 };
 
-template <int D, int ROWS, int NSTREAM, int NP>
+// Shared memory, in floats: two stationary tiles; for each group BUFS buffers of two
+// streamed tiles and their rows' statistics, and NP tiles of products.  Up to head dim 64
+// the next tiles are on their way while a group works on its own.
+template <int D, int ROWS, int NP>
 struct F32Cfg {
-  static constexpr int LD = D + 4, LDP = kCols + 4;
-  static constexpr int OFF_STREAM = 2 * ROWS * LD;                        // after the two stationary tiles
-  static constexpr int STREAM = NSTREAM * kCols * LD + NP * ROWS * LDP + 2 * kCols;  // of one group
+  static constexpr int LD = D + 4, LDP = kCols + 4, BUFS = D <= 64 ? 2 : 1;
+  static constexpr int OFF_STREAM = 2 * ROWS * LD;
+  static constexpr int BUF = 2 * kCols * LD + 2 * kCols, STREAM = BUFS * BUF + NP * ROWS * LDP;
   static constexpr int FLOATS = OFF_STREAM + kGroups * STREAM;
+  static_assert(kGroups * ROWS * (D + 2) <= kGroups * STREAM, "the parts fit over the streamed tiles");
+  static_assert(FLOATS * 4 <= 227 * 1024, "shared memory");
 };
 
 // ----------------------------------------------------------------- forward
@@ -95,7 +105,7 @@ struct F32Cfg {
 template <int D>
 __global__ void __launch_bounds__(kThreads) mha_forward_f32_kernel(const F32Args a) {
   constexpr int ROWS = 16, R = 2;
-  using C = F32Cfg<D, ROWS, 2, 1>;
+  using C = F32Cfg<D, ROWS, 1>;
   extern __shared__ __align__(16) float sm[];
   pdl_wait();
   const int g = threadIdx.x >> 7, t = threadIdx.x & 127, hw = t >> 4, kg = t & 15;
@@ -105,14 +115,12 @@ __global__ void __launch_bounds__(kThreads) mha_forward_f32_kernel(const F32Args
   if (!mha_slot<ROWS, false>(a.s, blockIdx.x, seq, index, tile)) return;
   const int r0 = tile * ROWS, rows = min(ROWS, seq.nq - r0);
   float* sq = sm;
-  float* sk = sm + C::OFF_STREAM + g * C::STREAM;
-  float* sv = sk + kCols * C::LD;
-  float* sp = sv + kCols * C::LD + hw * R * C::LDP;
+  float* bufs = sm + C::OFF_STREAM + g * C::STREAM;
+  float* sp = bufs + C::BUFS * C::BUF + hw * R * C::LDP;
   const float* q = static_cast<const float*>(a.q) + (int64_t)(seq.q0 + r0) * a.ldq + h * D;
   const float* k = static_cast<const float*>(a.k) + (int64_t)seq.k0 * a.ldk + hk * D;
   const float* v = static_cast<const float*>(a.v) + (int64_t)seq.k0 * a.ldv + hk * D;
   load_rows<D, ROWS>(sq, C::LD, q, a.ldq, rows, threadIdx.x, kThreads);
-  __syncthreads();
   int lo[R], hi[R], first, last, none;
   mha_keys_of(a.s, seq, r0, first, none);
   mha_keys_of(a.s, seq, r0 + rows - 1, none, last);
@@ -124,11 +132,22 @@ __global__ void __launch_bounds__(kThreads) mha_forward_f32_kernel(const F32Args
     m[i] = -INFINITY;
     l[i] = 0.f;
   }
+  auto fetch = [&](int j, int buf) {  // tile j's keys and values, if there is one
+    float* to = bufs + buf * C::BUF;
+    if (j * kCols < last) {
+      load_rows<D, kCols>(to, C::LD, k + (int64_t)j * kCols * a.ldk, a.ldk, seq.nk - j * kCols, t, 128);
+      load_rows<D, kCols>(to + kCols * C::LD, C::LD, v + (int64_t)j * kCols * a.ldv, a.ldv, seq.nk - j * kCols, t, 128);
+    }
+    cp_async_commit();
+  };
+  int buf = 0;
+  fetch(first / kCols + g, 0);
+  cp_async_wait<0>();
+  __syncthreads();  // the query rows, and every group's first tiles
   for (int j = first / kCols + g; j * kCols < last; j += kGroups) {
-    group_sync(1 + g, 128);  // the tiles before have been read
-    load_rows<D, kCols>(sk, C::LD, k + (int64_t)j * kCols * a.ldk, a.ldk, seq.nk - j * kCols, t, 128);
-    load_rows<D, kCols>(sv, C::LD, v + (int64_t)j * kCols * a.ldv, a.ldv, seq.nk - j * kCols, t, 128);
-    group_sync(1 + g, 128);
+    if (C::BUFS == 2) fetch(j + kGroups, buf ^ 1);
+    const float* sk = bufs + buf * C::BUF;
+    const float* sv = sk + kCols * C::LD;
     float s[R][2];
     products<D, R>(sq + hw * R * C::LD, sk, C::LD, kg, s);
 #pragma unroll
@@ -157,6 +176,11 @@ __global__ void __launch_bounds__(kThreads) mha_forward_f32_kernel(const F32Args
     }
     __syncwarp();
     accumulate<D, R>(sp, C::LDP, sv, C::LD, kg, o);
+    group_sync(1 + g, 128);  // the tiles have been read
+    if (C::BUFS == 1) fetch(j + kGroups, 0);
+    cp_async_wait<0>();
+    group_sync(1 + g, 128);  // the next are there
+    if (C::BUFS == 2) buf ^= 1;
   }
   // ---- join: [group][ROWS][D] parts over the streamed tiles, then {m, l}
 #pragma unroll
@@ -200,25 +224,22 @@ __global__ void __launch_bounds__(kThreads) mha_forward_f32_kernel(const F32Args
 //   else   keeps q and dout, streams keys and values: dq += ds k.
 // The groups of four warps take the tiles in turn and their sums are joined in order.
 template <int D, bool KEYS>
-__global__ void __launch_bounds__(kThreads) mha_backward_f32_kernel(const F32Args a) {
+__device__ __forceinline__ void mha_backward_f32(const F32Args& a) {
   constexpr int ROWS = 16, R = 2;
-  using C = F32Cfg<D, ROWS, 2, 2>;
+  using C = F32Cfg<D, ROWS, 2>;
   extern __shared__ __align__(16) float sm[];
-  pdl_wait();
   const int g = threadIdx.x >> 7, t = threadIdx.x & 127, hw = t >> 4, kg = t & 15;
   const int hb = blockIdx.y;  // head of the rows that stay
   MhaSeq seq;
   int index, tile;
-  if (!mha_slot<ROWS, KEYS>(a.s, blockIdx.x, seq, index, tile)) return;
+  if (hb >= (KEYS ? a.s.kv_heads : a.s.heads) || !mha_slot<ROWS, KEYS>(a.s, blockIdx.x, seq, index, tile)) return;
   const int n_rows = KEYS ? seq.nk : seq.nq, r0 = tile * ROWS, rows = min(ROWS, n_rows - r0);
   const int slot0 = mha_slot0(a.s.qb, index, seq.q0, kStatRows);
   float* x1 = sm;
   float* x2 = sm + ROWS * C::LD;
-  float* y1 = sm + C::OFF_STREAM + g * C::STREAM;
-  float* y2 = y1 + kCols * C::LD;
-  float* sp = y2 + kCols * C::LD;
+  float* bufs = sm + C::OFF_STREAM + g * C::STREAM;
+  float* sp = bufs + C::BUFS * C::BUF;
   float* sd = sp + ROWS * C::LDP;
-  float* st = sd + ROWS * C::LDP;  // KEYS: the streamed rows' statistics
   const float* q = static_cast<const float*>(a.q) + (int64_t)seq.q0 * a.ldq;
   const float* k = static_cast<const float*>(a.k) + (int64_t)seq.k0 * a.ldk;
   const float* v = static_cast<const float*>(a.v) + (int64_t)seq.k0 * a.ldv;
@@ -230,7 +251,6 @@ __global__ void __launch_bounds__(kThreads) mha_backward_f32_kernel(const F32Arg
     load_rows<D, ROWS>(x1, C::LD, q + (int64_t)r0 * a.ldq + hb * D, a.ldq, rows, threadIdx.x, kThreads);
     load_rows<D, ROWS>(x2, C::LD, dout + (int64_t)r0 * a.lddo + hb * D, a.lddo, rows, threadIdx.x, kThreads);
   }
-  __syncthreads();
   auto seen = [&](int row, int& lo, int& hi) {
     if (KEYS) mha_queries_of(a.s, seq, row, lo, hi);
     else mha_keys_of(a.s, seq, row, lo, hi);
@@ -252,21 +272,36 @@ __global__ void __launch_bounds__(kThreads) mha_backward_f32_kernel(const F32Arg
   const int j0 = first / kCols, tiles = last > j0 * kCols ? (last + kCols - 1) / kCols - j0 : 0;
   const int total = tiles * (KEYS ? a.s.group : 1);
   float acc1[R][D / 16] = {}, acc2[R][D / 16] = {};
-  for (int n = g; n < total; n += kGroups) {
-    const int j = j0 + n % tiles, h = KEYS ? hb * a.s.group + n / tiles : hb / a.s.group, c0 = j * kCols;
-    group_sync(1 + g, 128);  // the tiles before have been read
-    if (KEYS) {
-      load_rows<D, kCols>(y1, C::LD, q + (int64_t)c0 * a.ldq + h * D, a.ldq, seq.nq - c0, t, 128);
-      load_rows<D, kCols>(y2, C::LD, dout + (int64_t)c0 * a.lddo + h * D, a.lddo, seq.nq - c0, t, 128);
-      if (t < 2 * kCols) {
-        const float* at = a.stats + mha_stat_offset(h, a.stat_slots, slot0 + c0 / kStatRows) + c0 % kStatRows;
-        st[t] = at[(t / kCols) * kStatRows + t % kCols];
+  // step n: tile j0 + n % tiles of the n / tiles-th head of the group
+  auto fetch = [&](int n, int buf) {
+    if (n < total) {
+      const int c0 = (j0 + n % tiles) * kCols, h = KEYS ? hb * a.s.group + n / tiles : hb / a.s.group;
+      float* y1 = bufs + buf * C::BUF;
+      float* y2 = y1 + kCols * C::LD;
+      if (KEYS) {
+        load_rows<D, kCols>(y1, C::LD, q + (int64_t)c0 * a.ldq + h * D, a.ldq, seq.nq - c0, t, 128);
+        load_rows<D, kCols>(y2, C::LD, dout + (int64_t)c0 * a.lddo + h * D, a.lddo, seq.nq - c0, t, 128);
+        if (t < 2 * kCols) {  // the streamed rows' statistics
+          const float* at = a.stats + mha_stat_offset(h, a.stat_slots, slot0 + c0 / kStatRows) + c0 % kStatRows;
+          cp_async<4>(y2 + kCols * C::LD + t, at + (t / kCols) * kStatRows + t % kCols, true);
+        }
+      } else {
+        load_rows<D, kCols>(y1, C::LD, k + (int64_t)c0 * a.ldk + h * D, a.ldk, seq.nk - c0, t, 128);
+        load_rows<D, kCols>(y2, C::LD, v + (int64_t)c0 * a.ldv + h * D, a.ldv, seq.nk - c0, t, 128);
       }
-    } else {
-      load_rows<D, kCols>(y1, C::LD, k + (int64_t)c0 * a.ldk + h * D, a.ldk, seq.nk - c0, t, 128);
-      load_rows<D, kCols>(y2, C::LD, v + (int64_t)c0 * a.ldv + h * D, a.ldv, seq.nk - c0, t, 128);
     }
-    group_sync(1 + g, 128);
+    cp_async_commit();
+  };
+  int buf = 0;
+  fetch(g, 0);
+  cp_async_wait<0>();
+  __syncthreads();  // the stationary rows, and every group's first tiles
+  for (int n = g; n < total; n += kGroups) {
+    if (C::BUFS == 2) fetch(n + kGroups, buf ^ 1);
+    const float* y1 = bufs + buf * C::BUF;
+    const float* y2 = y1 + kCols * C::LD;
+    const float* st = y2 + kCols * C::LD;
+    const int c0 = (j0 + n % tiles) * kCols;
     float s[R][2], dp[R][2];
     products<D, R>(x1 + hw * R * C::LD, y1, C::LD, kg, s);
     products<D, R>(x2 + hw * R * C::LD, y2, C::LD, kg, dp);
@@ -284,6 +319,11 @@ __global__ void __launch_bounds__(kThreads) mha_backward_f32_kernel(const F32Arg
     __syncwarp();
     accumulate<D, R>(sd + hw * R * C::LDP, C::LDP, y1, C::LD, kg, acc1);
     if (KEYS) accumulate<D, R>(sp + hw * R * C::LDP, C::LDP, y2, C::LD, kg, acc2);
+    group_sync(1 + g, 128);  // the tiles have been read
+    if (C::BUFS == 1) fetch(n + kGroups, 0);
+    cp_async_wait<0>();
+    group_sync(1 + g, 128);  // the next are there
+    if (C::BUFS == 2) buf ^= 1;
   }
   auto join = [&](const float (&acc)[R][D / 16], void* out, int64_t ld, int row0, float by) {
     __syncthreads();
@@ -304,14 +344,28 @@ __global__ void __launch_bounds__(kThreads) mha_backward_f32_kernel(const F32Arg
       static_cast<float*>(out)[at] = sum * by;
     }
   };
-  join(acc1, a.out1, a.ld1, (KEYS ? seq.k0 : seq.q0) + r0, a.scale);
-  if (KEYS) join(acc2, a.out2, a.ld2, seq.k0 + r0, 1.f);
+  if (KEYS) {
+    join(acc1, a.out1, a.ld1, seq.k0 + r0, a.scale);
+    join(acc2, a.out2, a.ld2, seq.k0 + r0, 1.f);
+  } else {
+    join(acc1, a.out3, a.ld3, seq.q0 + r0, a.scale);
+  }
+}
+
+// Both halves in one launch (blockIdx.z: `first` of them on): neither fills the GPU at the
+// sizes of the fp32 mode (256 rows, 4 heads of 64: 64 CTAs each; one after the other 35.7
+// us with the statistics, so F32A).
+template <int D>
+__global__ void __launch_bounds__(kThreads) mha_backward_f32_kernel(const F32Args a, int first) {
+  pdl_wait();
+  if (blockIdx.z + first == 0) mha_backward_f32<D, true>(a);
+  else mha_backward_f32<D, false>(a);
 }
 
 template <int D>
 acid_status forward(const MhaArgs& x, const F32Args& base, cudaStream_t s) {
   static PerContext allowed;
-  constexpr size_t smem = (size_t)F32Cfg<D, 16, 2, 1>::FLOATS * 4;
+  constexpr size_t smem = (size_t)F32Cfg<D, 16, 1>::FLOATS * 4;
   ACID_TRY(allow_smem(allowed, mha_forward_f32_kernel<D>, smem));
   F32Args a = base;
   a.out1 = x.out;
@@ -324,27 +378,23 @@ acid_status forward(const MhaArgs& x, const F32Args& base, cudaStream_t s) {
 
 template <int D>
 acid_status backward(const MhaArgs& x, const F32Args& base, cudaStream_t s) {
-  static PerContext allowed_k, allowed_q;
-  constexpr size_t smem = (size_t)F32Cfg<D, 16, 2, 2>::FLOATS * 4;
+  static PerContext allowed;
+  constexpr size_t smem = (size_t)F32Cfg<D, 16, 2>::FLOATS * 4;
+  ACID_TRY(allow_smem(allowed, mha_backward_f32_kernel<D>, smem));
   F32Args a = base;
-  if (x.dk != nullptr || x.dv != nullptr) {
-    ACID_TRY(allow_smem(allowed_k, mha_backward_f32_kernel<D, true>, smem));
-    a.out1 = x.dk;
-    a.ld1 = x.lddk;
-    a.out2 = x.dv;
-    a.ld2 = x.lddv;
-    const dim3 grid(mha_slots(a.s.nk, a.s.seqs, a.s.kb != nullptr, 16), a.s.kv_heads);
-    launch_pdl(mha_backward_f32_kernel<D, true>, grid, kThreads, smem, s, a);
-    ACID_CHECK_LAUNCH();
-  }
-  if (x.dq != nullptr) {
-    ACID_TRY(allow_smem(allowed_q, mha_backward_f32_kernel<D, false>, smem));
-    a.out1 = x.dq;
-    a.ld1 = x.lddq;
-    const dim3 grid(mha_slots(a.s.nq, a.s.seqs, a.s.qb != nullptr, 16), a.s.heads);
-    launch_pdl(mha_backward_f32_kernel<D, false>, grid, kThreads, smem, s, a);
-    ACID_CHECK_LAUNCH();
-  }
+  a.out1 = x.dk;
+  a.ld1 = x.lddk;
+  a.out2 = x.dv;
+  a.ld2 = x.lddv;
+  a.out3 = x.dq;
+  a.ld3 = x.lddq;
+  const bool keys = x.dk != nullptr || x.dv != nullptr, queries = x.dq != nullptr;
+  if (!keys && !queries) return ACID_OK;
+  const int kx = keys ? mha_slots(a.s.nk, a.s.seqs, a.s.kb != nullptr, 16) : 0;
+  const int qx = queries ? mha_slots(a.s.nq, a.s.seqs, a.s.qb != nullptr, 16) : 0;
+  const dim3 grid(std::max(kx, qx), queries ? a.s.heads : a.s.kv_heads, keys && queries ? 2 : 1);
+  launch_pdl(mha_backward_f32_kernel<D>, grid, kThreads, smem, s, a, keys ? 0 : 1);
+  ACID_CHECK_LAUNCH();
   return ACID_OK;
 }
 

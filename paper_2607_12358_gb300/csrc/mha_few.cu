@@ -41,29 +41,6 @@ template <> struct Base<float> {
   static __device__ __forceinline__ float lse(float m, float l) { return m + logf(l); }
 };
 
-// 8 columns of a row as they are loaded, and as fp32.
-template <typename T> struct Raw;
-template <> struct Raw<__nv_bfloat16> {
-  uint4 u;
-  __device__ __forceinline__ void zero() { u = make_uint4(0, 0, 0, 0); }
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { u = __ldg(reinterpret_cast<const uint4*>(p)); }
-  __device__ __forceinline__ void get(float* v) const {
-    v[0] = bf16_lo(u.x); v[1] = bf16_hi(u.x); v[2] = bf16_lo(u.y); v[3] = bf16_hi(u.y);
-    v[4] = bf16_lo(u.z); v[5] = bf16_hi(u.z); v[6] = bf16_lo(u.w); v[7] = bf16_hi(u.w);
-  }
-};
-template <> struct Raw<float> {
-  float4 a, b;
-  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
-  __device__ __forceinline__ void load(const float* p) {
-    a = __ldg(reinterpret_cast<const float4*>(p));
-    b = __ldg(reinterpret_cast<const float4*>(p + 4));
-  }
-  __device__ __forceinline__ void get(float* v) const {
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  }
-};
-
 // Running maximum, sum and output of R heads over a lane's 8 columns.
 template <typename T, int R>
 struct Running {
@@ -132,7 +109,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) mha_few_kernel(const __grid_co
   const T* kp = static_cast<const T*>(a.k) + (int64_t)seq.k0 * a.ldk + hk * D + col;
   const T* vp = static_cast<const T*>(a.v) + (int64_t)seq.k0 * a.ldv + hk * D + col;
   constexpr int kStep = kWarps * KEYS * BATCH;
-  Raw<T> kr[BATCH], vr[BATCH];
+  MhaRaw<T> kr[BATCH], vr[BATCH];
   auto fetch = [&](int j0) {
 #pragma unroll
     for (int b = 0; b < BATCH; ++b) {
@@ -148,7 +125,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) mha_few_kernel(const __grid_co
   int j0 = begin + warp * KEYS * BATCH + sub;
   fetch(j0);
   for (; j0 - sub < end; j0 += kStep) {
-    Raw<T> kc[BATCH], vc[BATCH];
+    MhaRaw<T> kc[BATCH], vc[BATCH];
 #pragma unroll
     for (int b = 0; b < BATCH; ++b) {
       kc[b] = kr[b];
