@@ -34,6 +34,8 @@ struct FwdArgs {
   float* part_ml;  // [split units][256][2]: reference max and sum
 };
 
+constexpr int kBarBytes = 768;  // barriers, units
+
 // What a CTA does at a time: an item, or a share of its key tiles.
 struct FwdUnit {
   int head, q0, rows, q_end;  // first row of the pair, rows left in the sequence from there, its last row's successor
@@ -73,13 +75,66 @@ __device__ __forceinline__ bool fwd_unit(const FwdArgs& a, int u, FwdUnit& x) {
   }
   return true;
 }
-// The CTA's next unit that has key tiles, from unit u on; false: none.
+// A unit without key tiles: rows that see no key.  By the producer's warp.
 template <class C>
-__device__ __forceinline__ bool next_unit(const FwdArgs& a, int& u, FwdUnit& x) {
-  for (; u < a.units; u += gridDim.x)
-    if (fwd_unit<C>(a, u, x) && x.tiles > 0) return true;
-  return false;
+__device__ __forceinline__ void write_empty(const FwdArgs& a, const FwdUnit& x, int lane) {
+  const int rows = min(x.rows, kBQ);
+  for (int r = lane; r < rows; r += 32) {
+    if (x.part >= 0) *reinterpret_cast<float2*>(a.part_ml + ((int64_t)x.part * kBQ + r) * 2) = make_float2(-INFINITY, 0.f);
+    else a.lse[(int64_t)x.head * a.s.nq + x.q0 + r] = -INFINITY;
+  }
+  if (x.part >= 0) return;
+  for (int i = lane; i < rows * (C::D / 8); i += 32) {
+    const int64_t at = (int64_t)(x.q0 + i / (C::D / 8)) * a.ldo + x.head * C::D + i % (C::D / 8) * 8;
+    if (ACID_IN_BOUNDS(kSiteMha, at + 7, (int64_t)a.s.nq * a.ldo))
+      *reinterpret_cast<uint4*>(a.out + at) = make_uint4(0, 0, 0, 0);
+  }
 }
+
+// The units of a CTA that have key tiles, as its producer warp finds them, in a ring in
+// shared memory: {key tiles (0: no more units), head, q0, q_end}, {first query row, queries
+// and keys of the sequence, first key tile}, {part}.  The other warps read what they need
+// when they need it, and every branch that goes by it is a vote.  With each warp forming its
+// units by itself, and branches on loaded values, which the compiler cannot know to be the
+// same in all lanes, descriptors, ring slots and loop counts left the uniform registers for
+// those beside a row's 128 scores: 4726 rows, 30 heads of 64 205 us instead of 164, 8192
+// rows, 12 heads of 128 330 instead of 271 (of that, votes alone 170 to 164 and 303 to 271).
+struct UnitRing {
+  static constexpr int kEntries = 4, kBytes = kEntries * (48 + 16);
+  int4* entries;
+  uint64_t *full, *empty;
+  __device__ __forceinline__ explicit UnitRing(uint8_t* at)
+      : entries(reinterpret_cast<int4*>(at)),
+        full(reinterpret_cast<uint64_t*>(at + kEntries * 48)),
+        empty(full + kEntries) {}
+  __device__ __forceinline__ void init() const {
+    for (int i = 0; i < kEntries; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 9);  // eight softmax warps, the MMA warp
+    }
+  }
+  __device__ __forceinline__ const volatile int* at(int n) const {
+    return reinterpret_cast<const volatile int*>(entries + n % kEntries * 3);
+  }
+  __device__ __forceinline__ bool wait(int n) const { return mbar_wait_warp(&full[n % kEntries], (n / kEntries) & 1); }
+  // By one lane, behind the warp's last read.
+  __device__ __forceinline__ void done(int n) const { mbar_arrive(&empty[n % kEntries]); }
+  // By the producer's warp: unit n, or that there is none.
+  __device__ __forceinline__ bool publish(int n, bool any, const FwdUnit& x, int lane) const {
+    if (n >= kEntries && !mbar_wait_warp(&empty[n % kEntries], (n / kEntries - 1) & 1)) return false;
+    if (lane == 0) {
+      int4* e = entries + n % kEntries * 3;
+      e[0] = any ? make_int4(x.tiles, x.head, x.q0, x.q_end) : make_int4(0, 0, 0, 0);
+      if (any) {
+        e[1] = make_int4(x.tile * kBQ, x.seq.nq, x.nk, x.j0);
+        e[2] = make_int4(x.part, 0, 0, 0);
+      }
+      mbar_arrive(&full[n % kEntries]);
+    }
+    __syncwarp();
+    return true;
+  }
+};
 
 // Rows [valid, ROWS) of a loaded tile (128-byte swizzled chunks of 64 columns) are
 // set to zero: rows of another sequence, or of none, that a product over keys would
@@ -105,7 +160,10 @@ __global__ void __launch_bounds__(kAttnThreads, C::CTAS_PER_SM)
   uint8_t* sK = smem + C::OFF_K;
   uint8_t* sV = smem + C::OFF_V;
   const AttnBars<C> bar(smem + C::OFF_BAR_P);
-  uint64_t* edge = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR_P + C::BAR_BYTES - 8);  // a V tile to be cleared
+  constexpr int kOffRing = (AttnBars<C>::kCount * 8 + 4 + 15) / 16 * 16;
+  static_assert(kOffRing + UnitRing::kBytes + 8 <= kBarBytes, "barrier area");
+  const UnitRing ring(smem + C::OFF_BAR_P + kOffRing);
+  uint64_t* edge = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR_P + kBarBytes - 8);  // a V tile to be cleared
   static_assert(AttnBars<C>::kCount * 8 + 16 <= C::BAR_BYTES, "barrier area");
 
   const int warp = warp_index(), lane = threadIdx.x & 31;
@@ -115,6 +173,7 @@ __global__ void __launch_bounds__(kAttnThreads, C::CTAS_PER_SM)
     tma_prefetch_desc(&tmV);
     tma_prefetch_desc(&tmO);
     mbar_init(edge, 1);
+    ring.init();
     bar.init();
   }
   if (warp == 1) tmem_alloc(bar.tmem_slot, C::TMEM_COLS);
@@ -127,9 +186,23 @@ __global__ void __launch_bounds__(kAttnThreads, C::CTAS_PER_SM)
   if (warp == 0) {  // -------------------------------------------- TMA producer
     bool ok = true;
     int k_done = 0, v_done = 0, edges = 0;
-    FwdUnit x;
+    FwdUnit x, next;
     int u = blockIdx.x, n = 0;  // n: the unit's number among those with key tiles
-    for (int g = 0; ok && next_unit<C>(a, u, x); u += gridDim.x, ++n) {
+    auto find = [&](FwdUnit& y) -> bool {
+      for (; u < a.units; u += gridDim.x) {
+        if (!fwd_unit<C>(a, u, y)) continue;
+        if (y.tiles > 0) {
+          u += gridDim.x;
+          return true;
+        }
+        write_empty<C>(a, y, lane);
+      }
+      return false;
+    };
+    // a unit is published while the one before it is loaded, behind its first tile
+    bool more = find(x);
+    ok = ring.publish(0, more, x, lane);
+    for (int g = 0; ok && more; x = next, ++n) {
       const int kcol = x.head / a.s.group * C::D;
       auto load_q = [&](int t) -> bool {
         if (n > 0 && !mbar_wait_warp(&bar.q_empty[t], (n - 1) & 1)) return false;
@@ -160,6 +233,10 @@ __global__ void __launch_bounds__(kAttnThreads, C::CTAS_PER_SM)
           load_kv_tile<C>(sV + st * C::KV_BYTES, &tmV, &bar.v_full[st], kcol, x.k0 + row);
         }
         v_done = g + 1;
+        if (j == 0) {
+          more = find(next);
+          if (!ring.publish(n + 1, more, next, lane)) { ok = false; break; }
+        }
       }
     }
     // after a wait ran out: the last K and V loads of each ring have landed
@@ -168,47 +245,57 @@ __global__ void __launch_bounds__(kAttnThreads, C::CTAS_PER_SM)
   } else if (warp == 1) {  // ------------------------------------- MMA issuer
     const bool leader = elect_one();
     const AttnMma<C> mma(bar, tmem, sQ, sK, sV);
-    // the next S to issue: step gs, query tile ts, key tile js of unit `xs`, its number ns
-    FwdUnit xs, xp;
-    int us = blockIdx.x, gs = 0, ts = 0, js = 0, ns = 0;
-    bool more = next_unit<C>(a, us, xs);
-    auto issue_s = [&]() -> bool {
-      if (!more) return true;
-      if (ts == 0 && !mbar_wait_warp(&bar.k_full[C::slot(gs)], C::round(gs) & 1)) return false;
-      if (js == 0 && !mbar_wait_warp(&bar.q_full[ts], ns & 1)) return false;
-      tc_fence_after();
-      if (leader) {
-        mma.s_step(ts, gs);
-        if (js == xs.tiles - 1) mma_commit(&bar.q_empty[ts]);
-      }
-      __syncwarp();
-      if (ts == 1) {
-        ++gs;
-        if (++js == xs.tiles) {
-          js = 0;
-          ++ns;
-          us += gridDim.x;
-          more = next_unit<C>(a, us, xs);
-        }
-      }
-      ts ^= 1;
+    // The unit whose S is to be issued next, and its tile js.  `last` keeps for the latest
+    // 32 steps whether a unit ends there: PV runs up to two steps behind.  The query tile is
+    // known where a step is issued, and with it the descriptors.
+    int js = 0, ns = 0, tiles = 0, end = 0;  // end: steps that there are, so far
+    bool more = false;
+    uint32_t last = 0;
+    auto read_unit = [&]() -> bool {
+      if (!ring.wait(ns)) return false;
+      tiles = ring.at(ns)[0];
+      more = __any_sync(0xffffffffu, tiles > 0);
+      if (leader) ring.done(ns);
       return true;
     };
-    bool ok = true;
-    for (int i = 0; ok && i < C::NB; ++i) ok = issue_s();
-    int u = blockIdx.x;
-    for (int g = 0; ok && next_unit<C>(a, u, xp); u += gridDim.x) {
-      for (int j = 0; ok && j < xp.tiles; ++j, ++g) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (!mbar_wait_warp(&bar.p_full[C::sb(t, g)], C::sp(t, g))) { ok = false; break; }
-          if (t == 0 && !mbar_wait_warp(&bar.v_full[C::slot(g)], C::round(g) & 1)) { ok = false; break; }
-          tc_fence_after();
-          if (leader) mma.pv_step(t, g, j != 0);
-          __syncwarp();
-          if (!issue_s()) { ok = false; break; }
-        }
+    auto issue_s = [&](int t, int g) -> bool {
+      if (!more) return true;
+      if (t == 0 && !mbar_wait_warp(&bar.k_full[C::slot(g)], C::round(g) & 1)) return false;
+      if (js == 0 && !mbar_wait_warp(&bar.q_full[t], ns & 1)) return false;
+      tc_fence_after();
+      const bool ends = __all_sync(0xffffffffu, js == tiles - 1);
+      if (leader) {
+        mma.s_step(t, g);
+        if (ends) mma_commit(&bar.q_empty[t]);
       }
+      __syncwarp();
+      if (t == 0) {
+        end = g + 1;
+        last = (last & ~(1u << (g & 31))) | ((uint32_t)ends << (g & 31));
+      } else if (!ends) {
+        ++js;
+      } else {
+        js = 0;
+        ++ns;
+        return read_unit();
+      }
+      return true;
+    };
+    bool ok = read_unit();
+#pragma unroll
+    for (int n = 0; n < C::NB; ++n) ok = ok && issue_s(n & 1, n >> 1);
+    bool first = true;
+    for (int g = 0; ok && g < end; ++g) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (!mbar_wait_warp(&bar.p_full[C::sb(t, g)], C::sp(t, g))) { ok = false; break; }
+        if (t == 0 && !mbar_wait_warp(&bar.v_full[C::slot(g)], C::round(g) & 1)) { ok = false; break; }
+        tc_fence_after();
+        if (leader) mma.pv_step(t, g, !first);
+        __syncwarp();
+        if (!issue_s((t + C::NB) & 1, g + (t + C::NB) / 2)) { ok = false; break; }
+      }
+      first = (last >> (g & 31)) & 1;
     }
     if (!ok && leader) drain_mmas(bar.drain);
   } else {  // ------------------- softmax: warps 2-5 tile a, 6-9 tile b
@@ -221,39 +308,48 @@ __global__ void __launch_bounds__(kAttnThreads, C::CTAS_PER_SM)
     uint8_t* stage = smem + C::OFF_STAGE_P + (warp - 2) * 2 * C::STAGE_BOX;
     int n_st = 0, g = 0;
     bool ok = true;
-    for (int u = blockIdx.x; ok && u < a.units; u += gridDim.x) {
-      FwdUnit x;
-      if (!fwd_unit<C>(a, u, x)) continue;
-      const int r0 = x.tile * kBQ, last = x.seq.nq - 1;
-      // keys that this row sees; those that all rows of the query tile see
-      int lo, hi, all_lo, all_hi, none;
-      mha_keys_of(a.s, x.seq, min(r0 + r, last), lo, hi);
-      mha_keys_of(a.s, x.seq, min(r0 + t * kTileQ, last), none, all_hi);
-      mha_keys_of(a.s, x.seq, min(r0 + t * kTileQ + kTileQ - 1, last), all_lo, none);
+    for (int n = 0;; ++n) {
+      if (!ring.wait(n)) { ok = false; break; }
+      const volatile int* e = ring.at(n);
+      auto word = [&](int i) { return __shfl_sync(0xffffffffu, e[i], 0); };
+      const int tiles = word(0);
+      if (__any_sync(0xffffffffu, tiles == 0)) break;
+      // keys that all rows of the query tile see
+      const int r0 = word(4), last = word(5) - 1;
+      const MhaSeq seq{0, last + 1, 0, word(6)};
+      int all_lo, all_hi, none, c0 = word(7) * C::BKV;
+      mha_keys_of(a.s, seq, min(r0 + t * kTileQ, last), none, all_hi);
+      mha_keys_of(a.s, seq, min(r0 + t * kTileQ + kTileQ - 1, last), all_lo, none);
       float m_run = -INFINITY, l_run = 0.f;
-      for (int j = 0; j < x.tiles; ++j, ++g) {
-        const int c0 = (x.j0 + j) * C::BKV;
+      for (int j = 0; j < tiles; ++j, ++g, c0 += C::BKV) {
         const bool fresh = m_run == -INFINITY;
-        const bool ok_j = c0 >= all_lo && c0 + C::BKV <= all_hi
-                              ? softmax_tile<C, kNoMask>(bar, t, g, fresh, 0, 0, s_base, o_addr, a.scale_log2, m_run,
-                                                         l_run)
-                              : softmax_tile<C, kRange>(bar, t, g, fresh, lo - c0, hi - c0, s_base, o_addr,
-                                                        a.scale_log2, m_run, l_run);
+        bool ok_j;
+        if (c0 >= all_lo && c0 + C::BKV <= all_hi) {
+          ok_j = softmax_tile<C, kNoMask>(bar, t, g, fresh, 0, 0, s_base, o_addr, a.scale_log2, m_run, l_run);
+        } else {  // the keys that this row sees (formed here, they are not kept through the other tiles)
+          const int nq = e[5];
+          int lo, hi;
+          mha_keys_of(a.s, MhaSeq{0, nq, 0, e[6]}, min(e[4] + r, nq - 1), lo, hi);
+          ok_j = softmax_tile<C, kRange>(bar, t, g, fresh, lo - c0, hi - c0, s_base, o_addr, a.scale_log2, m_run, l_run);
+        }
         if (!ok_j) {
           ok = false;
           break;
         }
       }
       // ------------------------------------------------ output: O_t / l
-      if (ok && x.tiles > 0) ok = mbar_wait(&bar.pv_done[C::sb(t, g - 1)], C::sp(t, g - 1));
+      if (ok) ok = mbar_wait(&bar.pv_done[C::sb(t, g - 1)], C::sp(t, g - 1));
       ok = __all_sync(0xffffffffu, ok);  // the unit loop continues for the whole warp or not at all
+      if (!ok) break;
       tc_fence_after();
-      const int row = x.q0 + r, row0 = x.q0 + t * kTileQ + q * 32;  // this warp's 32 rows start at row0
-      const bool mine = ok && row < x.q_end;
-      if (x.part >= 0) {
-        const int64_t slot = (int64_t)x.part * kBQ + r;
+      const int head = e[1], q0 = e[2], q_end = e[3], part = e[8];
+      __syncwarp();
+      if (lane == 0) ring.done(n);
+      const int row = q0 + r, row0 = q0 + t * kTileQ + q * 32;  // this warp's 32 rows start at row0
+      const bool mine = row < q_end;
+      if (__any_sync(0xffffffffu, part >= 0)) {
+        const int64_t slot = (int64_t)part * kBQ + r;
         if (mine) *reinterpret_cast<float2*>(a.part_ml + slot * 2) = make_float2(m_run, l_run);
-        if (x.tiles == 0) continue;
 #pragma unroll 1
         for (int c = 0; c < C::D; c += 32) {
           uint32_t o[32];
@@ -269,22 +365,17 @@ __global__ void __launch_bounds__(kAttnThreads, C::CTAS_PER_SM)
       }
       const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
       if (mine)
-        a.lse[(int64_t)x.head * a.s.nq + row] =
+        a.lse[(int64_t)head * a.s.nq + row] =
             l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * 0.6931471805599453f;
       // The warp's 32 x 32 box leaves through shared memory and one TMA store where its
       // rows end with the matrix's (which clips it) or lie in the sequence; else row by row.
-      const bool box_ok = row0 + 32 <= x.q_end || x.q_end == a.s.nq;
+      const bool box_ok = __any_sync(0xffffffffu, row0 + 32 <= q_end || q_end == a.s.nq);
 #pragma unroll 1
       for (int c = 0; c < C::D; c += 32) {
         uint32_t o[32];
-        if (x.tiles > 0) {
-          tmem_ld32(o_addr + c, o);
-          tmem_wait_ld();
-        } else {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] = 0;
-        }
-        if (!ok || row0 >= x.q_end) continue;  // warp-uniform
+        tmem_ld32(o_addr + c, o);
+        tmem_wait_ld();
+        if (__any_sync(0xffffffffu, row0 >= q_end)) continue;  // warp-uniform
         uint4 w[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -293,7 +384,7 @@ __global__ void __launch_bounds__(kAttnThreads, C::CTAS_PER_SM)
           w[k] = make_uint4(pack_bf16(v(0), v(1)), pack_bf16(v(2), v(3)), pack_bf16(v(4), v(5)), pack_bf16(v(6), v(7)));
         }
         if (!box_ok) {
-          const int64_t at = (int64_t)row * a.ldo + x.head * C::D + c;
+          const int64_t at = (int64_t)row * a.ldo + head * C::D + c;
           if (mine && ACID_IN_BOUNDS(kSiteMha, at + 31, (int64_t)a.s.nq * a.ldo))
 #pragma unroll
             for (int k = 0; k < 4; ++k) reinterpret_cast<uint4*>(a.out + at)[k] = w[k];
@@ -307,7 +398,7 @@ __global__ void __launch_bounds__(kAttnThreads, C::CTAS_PER_SM)
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
-          tma_store_2d(&tmO, box, x.head * C::D + c, row0);
+          tma_store_2d(&tmO, box, head * C::D + c, row0);
           bulk_commit_group();
         }
         ++n_st;
@@ -391,10 +482,13 @@ FwdPlan plan(const MhaArgs& x, int sms) {
 }
 
 template <class C>
+constexpr int kSmem = C::SMEM_P - C::BAR_BYTES + kBarBytes;
+
+template <class C>
 acid_status launch(const MhaArgs& x, cudaStream_t s) {
   constexpr int D = C::D;
   static PerContext allowed;
-  ACID_TRY(allow_smem(allowed, mha_forward_kernel<C>, C::SMEM_P));
+  ACID_TRY(allow_smem(allowed, mha_forward_kernel<C>, kSmem<C>));
   const MhaShape& m = x.shape;
   CUtensorMap tq, tk, tv, to;
   const int64_t wq = (int64_t)m.heads * D, wk = (int64_t)m.kv_heads * D;
@@ -417,7 +511,7 @@ acid_status launch(const MhaArgs& x, cudaStream_t s) {
   a.units = p.full + (p.items - p.full) * p.splits;
   a.part_o = static_cast<float*>(x.part);
   a.part_ml = a.part_o + (size_t)(p.items - p.full) * p.splits * kBQ * D;
-  launch_pdl(mha_forward_kernel<C>, std::min(a.units, num_sms() * C::CTAS_PER_SM), kAttnThreads, C::SMEM_P, s, tq, tk, tv,
+  launch_pdl(mha_forward_kernel<C>, std::min(a.units, num_sms() * C::CTAS_PER_SM), kAttnThreads, kSmem<C>, s, tq, tk, tv,
              to, a);
   ACID_CHECK_LAUNCH();
   if (p.full < p.items) {
