@@ -233,6 +233,7 @@ struct BwdCfg {
   // S regions in tensor memory: with two, the next step's S is formed while this one's is
   // worked on.  Keys stationary at head dim 128: S, dP and two sums fill the 512 columns.
   static constexpr int NS = KEYS && D == 128 ? 1 : 2;
+  static_assert(KEYS || NS == 2, "queries stationary: two regions");
   static constexpr int Y1S = D == 64 ? 4 : NS + 1, Y2S = D == 64 ? 4 : 2;
   static constexpr int SUMS = KEYS ? 2 : 1;
   static constexpr int OFF_X = 0, OFF_Y1 = 2 * T_BYTES, OFF_Y2 = OFF_Y1 + Y1S * T_BYTES;
@@ -494,79 +495,84 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint64_t y2m = smem_desc_sw128(smem_u32(sY2), C::CHUNK, 1024);
     auto at = [](uint64_t desc, int slot) { return desc + (uint64_t)((slot * C::T_BYTES) >> 4); };
     bool ok = true;
-    int units = 0, g0 = 0;
-    for (; ok; ++units) {
+    // Conditions that depend on a unit are votes here and in the workers: behind a branch that
+    // the compiler does not know to be the same in all lanes descriptors, ring slots and
+    // counters leave the uniform registers (dq 32760 rows, 12 x 128 5660 us instead of 5271;
+    // 4726 rows, 30 x 64 dk and dv 276 instead of 267, dq 214 instead of 198).
+    for (int units = 0, g = 0; ok; ++units) {
       if (!mbar_wait_warp(&bar.unit_full[units % C::UNITS], (units / C::UNITS) & 1)) { ok = false; break; }
-      // (a shuffle: a value that the compiler knows to be the same in all lanes)
-      const int steps = __shfl_sync(0xffffffffu, entry(units)->x, 0);
-      if (steps == 0) break;
+      const int steps = static_cast<const volatile int*>(&entry(units)->x)[0];
+      auto has = [&](int i) -> bool { return __any_sync(0xffffffffu, i < steps); };
+      if (!has(0)) break;
       if (!mbar_wait_warp(bar.x_full, units & 1)) { ok = false; break; }
-      auto scores = [&](int i) -> bool {  // S of step i
-        const int g = g0 + i;
-        if (i >= steps) return true;
-        if (!mbar_wait_warp(&bar.y1_full[g % C::Y1S], (g / C::Y1S) & 1)) return false;
+      auto scores = [&](int gs) -> bool {  // S of step gs
+        if (!mbar_wait_warp(&bar.y1_full[gs % C::Y1S], (gs / C::Y1S) & 1)) return false;
         tc_fence_after();
         if (leader) {
-          mma_scores<C>(tmem + C::S_COL + (g % C::NS) * 128, x1, at(y1k, g % C::Y1S));
-          mma_commit(&bar.s_full[g % C::NS]);
+          mma_scores<C>(tmem + C::S_COL + (gs % C::NS) * 128, x1, at(y1k, gs % C::Y1S));
+          mma_commit(&bar.s_full[gs % C::NS]);
         }
         __syncwarp();
         return true;
       };
-      auto grads = [&](int i) -> bool {  // dP of step i
-        const int g = g0 + i;
-        if (i >= steps) return true;
-        if (!mbar_wait_warp(&bar.y2_full[g % C::Y2S], (g / C::Y2S) & 1)) return false;
+      auto grads = [&](int gs, bool last) -> bool {  // dP of step gs; last: of the unit
+        if (!mbar_wait_warp(&bar.y2_full[gs % C::Y2S], (gs / C::Y2S) & 1)) return false;
         tc_fence_after();
         if (leader) {
-          mma_scores<C>(tmem + C::DP_COL, x2, at(y2k, g % C::Y2S));
+          mma_scores<C>(tmem + C::DP_COL, x2, at(y2k, gs % C::Y2S));
           mma_commit(bar.dp_full);
-          if (!KEYS) mma_commit(&bar.y2_empty[g % C::Y2S]);
-          if (i == steps - 1) mma_commit(bar.x_empty);
+          if (!KEYS) mma_commit(&bar.y2_empty[gs % C::Y2S]);
+          if (last) mma_commit(bar.x_empty);
         }
         __syncwarp();
         return true;
       };
-      ok = scores(0) && grads(0) && (C::NS == 1 || scores(1));
-      for (int i = 0; ok && i < steps; ++i) {
-        const int g = g0 + i;
-        if (i == 0 && units > 0 && !mbar_wait_warp(bar.sum_empty, (units - 1) & 1)) { ok = false; break; }
+      bool more = has(1), first = true;  // a step behind this one
+      ok = scores(g) && grads(g, !more) && (C::NS == 1 || !more || scores(g + 1));
+      if (ok && units > 0) ok = mbar_wait_warp(bar.sum_empty, (units - 1) & 1);
+      for (int i = 0; ok; ++i, ++g) {
+        const bool more2 = has(i + 2);
         if constexpr (KEYS) {
           // dv += P^T g, over S; then the next S may take the region
           if (!mbar_wait_warp(&bar.p_full[g & 1], (g >> 1) & 1)) { ok = false; break; }
           tc_fence_after();
           if (leader) {
-            mma_sum<C>(tmem + C::SUM_COL + D, tmem + C::S_COL + (g % C::NS) * 128, at(y2m, g % C::Y2S), i != 0);
+            mma_sum<C>(tmem + C::SUM_COL + D, tmem + C::S_COL + (g % C::NS) * 128, at(y2m, g % C::Y2S), !first);
             mma_commit(&bar.y2_empty[g % C::Y2S]);
           }
           __syncwarp();
-          if (!scores(i + C::NS)) { ok = false; break; }
+          if ((C::NS == 1 ? more : more2) && !scores(g + C::NS)) { ok = false; break; }
           if (!mbar_wait_warp(&bar.ds_full[g & 1], (g >> 1) & 1)) { ok = false; break; }
           tc_fence_after();
           if (leader) {
-            mma_sum<C>(tmem + C::SUM_COL, tmem + C::DP_COL, at(y1m, g % C::Y1S), i != 0);
+            mma_sum<C>(tmem + C::SUM_COL, tmem + C::DP_COL, at(y1m, g % C::Y1S), !first);
             mma_commit(&bar.y1_empty[g % C::Y1S]);
-            if (i == steps - 1) mma_commit(bar.sum_full);
+            if (!more) mma_commit(bar.sum_full);
           }
           __syncwarp();
-          if (!grads(i + 1)) { ok = false; break; }
+          if (more && !grads(g + 1, !more2)) { ok = false; break; }
         } else {
           // the next dP as soon as this one has been read; dq += dS k, over S
-          if (i + 1 < steps) {
-            if (!mbar_wait_warp(bar.dp_read, g & 1) || !grads(i + 1)) { ok = false; break; }
+          if (more) {
+            if (!mbar_wait_warp(bar.dp_read, g & 1) || !grads(g + 1, !more2)) { ok = false; break; }
           }
           if (!mbar_wait_warp(&bar.ds_full[g & 1], (g >> 1) & 1)) { ok = false; break; }
           tc_fence_after();
           if (leader) {
-            mma_sum<C>(tmem + C::SUM_COL, tmem + C::S_COL + (g % C::NS) * 128, at(y1m, g % C::Y1S), i != 0);
+            mma_sum<C>(tmem + C::SUM_COL, tmem + C::S_COL + (g % C::NS) * 128, at(y1m, g % C::Y1S), !first);
             mma_commit(&bar.y1_empty[g % C::Y1S]);
-            if (i == steps - 1) mma_commit(bar.sum_full);
+            if (!more) mma_commit(bar.sum_full);
           }
           __syncwarp();
-          if (!scores(i + C::NS)) { ok = false; break; }
+          if (more2 && !scores(g + C::NS)) { ok = false; break; }
         }
+        first = false;
+        if (!more) {
+          ++g;
+          break;
+        }
+        more = more2;
       }
-      g0 += steps;
     }
     if (!ok && leader) drain_mmas(bar.drain);
   } else {  // ------------------------------------------- workers
@@ -590,7 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       return true;
     };
     ok = __all_sync(0xffffffffu, fetch(0));
-    for (int n = 0; ok && steps > 0; ++n) {
+    for (int n = 0; ok && __any_sync(0xffffffffu, steps > 0); ++n) {
       const int4 e0 = entry(n)[0], e1 = entry(n)[1], e2 = entry(n)[2];
       const int rows = e0.w, part = e1.w;
       const MhaSeq seq{0, e1.y, 0, e1.z};
@@ -709,11 +715,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       const int begin0 = e2.x * kTile, end0 = begin0 + e2.y * kTile;
       int cc = begin0 + e2.z * kTile;
-      for (int i = 0; i < steps; ++i, ++g) {
+      for (int i = 0; __any_sync(0xffffffffu, i < steps); ++i, ++g) {
         const int c0 = cc;
         // (streamed queries behind the sequence have probability 0 by their statistics)
         const bool plain = c0 >= all_lo && (c0 + kTile <= all_hi || (KEYS && all_hi == seq.nq));
-        if (!(plain ? step(cc, std::false_type{}) : step(cc, std::true_type{}))) {
+        if (!(__any_sync(0xffffffffu, plain) ? step(cc, std::false_type{}) : step(cc, std::true_type{}))) {
           ok = false;
           break;
         }
@@ -738,7 +744,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           tc_fence_before();
           mbar_arrive(bar.sum_empty);
         }
-        if (part >= 0) {
+        if (__any_sync(0xffffffffu, part >= 0)) {
           float* to = a.part + (((int64_t)part * C::SUMS + w) * (D / 4) + c / 4) * (kTile * 4) + r * 4;
 #pragma unroll
           for (int i = 0; i < 8; ++i)
