@@ -55,7 +55,7 @@ struct BwdUnit {
   int r0, nq, nk;  // that row in its sequence, the sequence's rows
   int y0;          // the sequence's first streamed row
   int j0, tiles;   // streamed tiles [j0, j0 + tiles) of the sequence, for each head of the group
-  int n0, steps;   // steps [n0, n0 + steps) of group * tiles
+  int n0, steps;   // steps [n0, n0 + steps) of group * tiles, which come back to 0 at their end
   int part;        // slot of a share's partial sums, or -1
   int stat;        // keys stationary: slot of the sequence's first queries; else of this tile's
 };
@@ -108,7 +108,7 @@ struct BwdWalk {
   int shares, units = 0;
   __device__ __forceinline__ BwdWalk(const BwdArgs& a_, int* scratch_, int lane_)
       : a(a_), scratch(scratch_), lane(lane_), next(blockIdx.x) {}
-  __device__ __forceinline__ int64_t bound(int c) const { return base + work * c / shares; }
+  __device__ __forceinline__ int64_t bound(int64_t c) const { return base + work * c / shares; }
 
   __device__ __forceinline__ void share_out() {
     shared = true;
@@ -203,7 +203,14 @@ struct BwdWalk {
       }
       if (s >= to) return false;
       const int n = x.steps, n0 = (int)max((int64_t)0, from - s), n1 = (int)min((int64_t)n, to - s);
-      x.n0 = n0;
+      // An item's tiles are taken round its end, the first one where the first share inside
+      // the item begins: the CTAs that work on a head then stream the same tiles at a time,
+      // all but one out of L2 (32760 queries, 301 and 512 keys, 12 x 128: 709 MB from HBM in
+      // 140 us without, 220 MB in 121 us with it).
+      int64_t c = (s - base) * shares / work;
+      while (bound(c) < s) ++c;
+      const int turn = bound(c) < s + n ? (int)(bound(c) - s) : 0;
+      x.n0 = n0 >= turn ? n0 - turn : n0 - turn + n;
       x.steps = n1 - n0;
       if (n0 > 0 || n1 < n) x.part = 2 * blockIdx.x + (units > 0);
       if (n0 == 0 && n1 < n && lane == 0) {
@@ -446,6 +453,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       const int rows = KEYS ? x.nq : x.nk, all = KEYS ? a.s.nq : a.s.nk;
       int jt = x.n0 % x.tiles, head = KEYS ? x.head * a.s.group + x.n0 / x.tiles : x.head / a.s.group;
+      const int heads_end = (x.head + 1) * a.s.group;  // of a key head's queries
       for (int i = 0; ok && i < x.steps; ++i, ++g) {
         const int j = x.j0 + jt;
         const int valid = rows - j * kTile, row = x.y0 + j * kTile;
@@ -477,7 +485,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         y2_done = g + 1;
         if (++jt == x.tiles) {
           jt = 0;
-          ++head;
+          if (KEYS && ++head == heads_end) head -= a.s.group;
         }
       }
     }
