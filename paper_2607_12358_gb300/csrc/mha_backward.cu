@@ -779,7 +779,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // Adds the parts of the items that lie in several shares, in the shares' order: the
 // first in the share where the item begins, the others the first units of theirs.  A
-// thread has four columns of a row.
+// thread has 16 columns of a row.
 template <int D, bool KEYS>
 __global__ void __launch_bounds__(256) mha_backward_join_kernel(const __grid_constant__ BwdArgs a) {
   constexpr int SUMS = KEYS ? 2 : 1;
@@ -788,24 +788,34 @@ __global__ void __launch_bounds__(256) mha_backward_join_kernel(const __grid_con
   const int4 e = a.record[2 * cta];  // {rows, row0, head, part}
   if (row >= e.x) return;            // (no rows: no such item)
   const int last = a.record[2 * cta + 1].x;
-  const int idx = blockIdx.y * 2 + (threadIdx.x >> 7);  // quad of columns, of dk and then dv
-  const int w = idx / (D / 4), c = idx % (D / 4) * 4;
+  const int idx = blockIdx.y * 2 + (threadIdx.x >> 7);  // 16 columns, of dk and then dv
+  const int w = idx / (D / 16), c = idx % (D / 16) * 16;
   __nv_bfloat16* out = w == 0 ? a.out1 : a.out2;
   if (out == nullptr) return;
   constexpr int64_t kPart = (int64_t)SUMS * (D / 4) * (kTile * 4);
-  const float* p = a.part + (int64_t)idx * (kTile * 4) + row * 4;
-  float4 sum = *reinterpret_cast<const float4*>(p + e.w * kPart);
+  const float* p = a.part + (int64_t)idx * (kTile * 16) + row * 4;
+  float4 sum[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sum[k] = *reinterpret_cast<const float4*>(p + e.w * kPart + k * kTile * 4);
   for (int s = cta + 1; s <= last; ++s) {
-    const float4 v = *reinterpret_cast<const float4*>(p + 2 * s * kPart);
-    sum.x += v.x;
-    sum.y += v.y;
-    sum.z += v.z;
-    sum.w += v.w;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float4 v = *reinterpret_cast<const float4*>(p + 2 * s * kPart + k * kTile * 4);
+      sum[k].x += v.x;
+      sum[k].y += v.y;
+      sum[k].z += v.z;
+      sum[k].w += v.w;
+    }
   }
   const float by = w == 0 ? a.scale : 1.0f;
   const int64_t ld = w == 0 ? a.ld1 : a.ld2, at = (int64_t)(e.y + row) * ld + e.z * D + c;
-  if (!ACID_IN_BOUNDS(kSiteMha, at + 3, (int64_t)(KEYS ? a.s.nk : a.s.nq) * ld)) return;
-  *reinterpret_cast<uint2*>(out + at) = make_uint2(pack_bf16(sum.x * by, sum.y * by), pack_bf16(sum.z * by, sum.w * by));
+  if (!ACID_IN_BOUNDS(kSiteMha, at + 15, (int64_t)(KEYS ? a.s.nk : a.s.nq) * ld)) return;
+  auto two = [&](const float4& v) { return make_uint2(pack_bf16(v.x * by, v.y * by), pack_bf16(v.z * by, v.w * by)); };
+#pragma unroll
+  for (int k = 0; k < 4; k += 2) {
+    const uint2 lo = two(sum[k]), hi = two(sum[k + 1]);
+    *reinterpret_cast<uint4*>(out + at + 4 * k) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+  }
 }
 
 // Which items go to the CTAs whole.  Fewer items than SMs: none, all their steps are
@@ -880,7 +890,7 @@ acid_status launch(const MhaArgs& x, cudaStream_t s) {
              KEYS ? tg : tv, a);
   ACID_CHECK_LAUNCH();
   if (shared) {
-    launch_pdl(mha_backward_join_kernel<D, KEYS>, dim3(ctas, C::SUMS * D / 8), 256, 0, s, a);
+    launch_pdl(mha_backward_join_kernel<D, KEYS>, dim3(ctas, C::SUMS * D / 32), 256, 0, s, a);
     ACID_CHECK_LAUNCH();
   }
   return ACID_OK;
