@@ -96,6 +96,14 @@ inline int mha_order(const MhaShape& s, int d, bool queries_streamed, bool first
   return s.seqs > 1 && bytes <= (int64_t)80 << 20 ? kBySlot : kByHead;
 }
 
+// The item that this CTA takes in a turn: the turns go through the CTAs forwards and
+// backwards alternately, so that items which get shorter from one to the next come out
+// even (32760 rows causal in 21 frames, 12 heads: 1988 us, always forwards 2087).
+__device__ __forceinline__ int mha_turn(int turn) {
+  const int n = gridDim.x;
+  return turn * n + (turn & 1 ? n - 1 - (int)blockIdx.x : (int)blockIdx.x);
+}
+
 __device__ __forceinline__ int floor_div(int a, int b) { return a >= 0 ? a / b : -((b - 1 - a) / b); }
 __device__ __forceinline__ int clamp_row(int64_t v, int n) { return (int)min(max(v, (int64_t)0), (int64_t)n); }
 

@@ -102,12 +102,13 @@ struct BwdWalk {
   const BwdArgs& a;
   int* scratch;
   int lane;
-  int next;        // whole items; then the next shared one
+  int turn = 0;    // of the whole items
+  int next = 0;    // shared item
   bool shared = false;
   int64_t s, from, to, base, work;  // first step of `next`; this share's steps
   int shares, units = 0;
   __device__ __forceinline__ BwdWalk(const BwdArgs& a_, int* scratch_, int lane_)
-      : a(a_), scratch(scratch_), lane(lane_), next(blockIdx.x) {}
+      : a(a_), scratch(scratch_), lane(lane_) {}
   __device__ __forceinline__ int64_t bound(int64_t c) const { return base + work * c / shares; }
 
   __device__ __forceinline__ void share_out() {
@@ -182,15 +183,12 @@ struct BwdWalk {
   // The next unit with steps; false: none.
   __device__ __forceinline__ bool operator()(BwdUnit& x, int d) {
     int slot, head;
-    for (; !shared && next < a.full; next += gridDim.x) {
+    while (!shared && (next = mha_turn(turn)) < a.full) {
+      ++turn;
       mha_item(a.order, a.slots, a.heads, next, slot, head);
       if (!bwd_item<KEYS>(a, slot, head, x)) continue;
-      if (x.steps == 0) {
-        clear(x, d);
-        continue;
-      }
-      next += gridDim.x;
-      return true;
+      if (x.steps > 0) return true;
+      clear(x, d);
     }
     if (a.full == a.items) return false;
     if (!shared) share_out();

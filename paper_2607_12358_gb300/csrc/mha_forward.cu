@@ -187,14 +187,12 @@ __global__ void __launch_bounds__(kAttnThreads, C::CTAS_PER_SM)
     bool ok = true;
     int k_done = 0, v_done = 0, edges = 0;
     FwdUnit x, next;
-    int u = blockIdx.x, n = 0;  // n: the unit's number among those with key tiles
+    int turn = 0, n = 0;  // n: the unit's number among those with key tiles
     auto find = [&](FwdUnit& y) -> bool {
-      for (; u < a.units; u += gridDim.x) {
+      for (int u; (u = mha_turn(turn)) < a.units; ) {
+        ++turn;
         if (!fwd_unit<C>(a, u, y)) continue;
-        if (y.tiles > 0) {
-          u += gridDim.x;
-          return true;
-        }
+        if (y.tiles > 0) return true;
         write_empty<C>(a, y, lane);
       }
       return false;
