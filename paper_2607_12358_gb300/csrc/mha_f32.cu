@@ -354,7 +354,7 @@ __device__ __forceinline__ void mha_backward_f32(const F32Args& a) {
 
 // Both halves in one launch (blockIdx.z: `first` of them on): neither fills the GPU at the
 // sizes of the fp32 mode (256 rows, 4 heads of 64: 64 CTAs each; one after the other 35.7
-// us with the statistics, so F32A).
+// us with the statistics, so 19).
 template <int D>
 __global__ void __launch_bounds__(kThreads) mha_backward_f32_kernel(const F32Args a, int first) {
   pdl_wait();

@@ -19,6 +19,15 @@ DEV = "cuda"
 W = 2.0 ** -24
 
 
+@pytest.fixture(autouse=True)
+def fp32_by_default():
+    """Whatever default another module of the run has set."""
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 @pytest.fixture(scope="module")
 def acid():
     import __graft_entry__ as g
