@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import math
+from operator import index
 from dataclasses import dataclass, field
 
 import numpy as np
@@ -483,9 +484,9 @@ def _rope(call, x, heads, axes, theta, grid, origin, positions, first_rows, halv
     if (grid is None) == (positions is None):
         raise ValueError("need either grid or positions")
     rows, width = x.shape
-    desc = _rope_desc(rows, width, dtype, heads, tuple(axes), theta if isinstance(theta, float) else
+    desc = _rope_desc(rows, width, dtype, index(heads), tuple(axes), theta if isinstance(theta, float) else
                       float(theta) if isinstance(theta, int) else tuple(theta), None if grid is None else tuple(grid),
-                      None if origin is None else tuple(origin), first_rows, halves)
+                      None if origin is None else tuple(origin), index(first_rows), bool(halves))
     if positions is not None:
         ld = _rows_of("positions", positions, rows, desc.axes, _F32)
         desc = A.acid_rope.from_buffer_copy(desc)
@@ -535,27 +536,39 @@ def sequence_bounds(lengths, room: int = 0, device="cuda") -> torch.Tensor:
     return torch.tensor(out, dtype=torch.int32).reshape(len(out), 2).to(device)
 
 
+@functools.lru_cache(maxsize=1024)
+def _mha_shape(nq, wq, nk, wk, dtype, heads, scale, seqs, frame_rows, frames_before, frames_after, q_first):
+    """The C description of a call, but for the bounds' addresses; query columns, key columns."""
+    if heads < 1 or wq % heads or wq == 0:
+        raise ValueError("the columns of q must be heads of one head_dim")
+    d = wq // heads
+    kv_heads = wk // d
+    if kv_heads < 1 or wk != kv_heads * d or heads % kv_heads:
+        raise ValueError("the columns of k must be heads of q's head_dim, whose number divides heads")
+    return A.acid_mha(nq, nk, _DT[dtype], heads, kv_heads, d, d ** -0.5 if scale is None else scale, seqs, None, None,
+                      frame_rows, frames_before, frames_after, q_first), heads * d, kv_heads * d
+
+
 def _mha_desc(q, k, heads, scale, q_bounds, k_bounds, frame_rows, frames_before, frames_after, q_first):
     """(C description, query columns, key columns)."""
     if q.dim() != 2 or k.dim() != 2 or q.dtype not in _DT:
         raise ValueError("q and k must be [rows, heads * head_dim] tensors of bf16 or fp32")
-    if heads < 1 or q.shape[1] % heads or q.shape[1] == 0:
-        raise ValueError("the columns of q must be heads of one head_dim")
-    d = q.shape[1] // heads
-    kv_heads = k.shape[1] // d
-    if kv_heads < 1 or k.shape[1] != kv_heads * d or heads % kv_heads:
-        raise ValueError("the columns of k must be heads of q's head_dim, whose number divides heads")
-    seqs, ptrs = 1, [None, None]
-    for i, (name, b) in enumerate((("q_bounds", q_bounds), ("k_bounds", k_bounds))):
+    (nq, wq), (nk, wk), seqs = q.shape, k.shape, 1
+    for name, b in (("q_bounds", q_bounds), ("k_bounds", k_bounds)):
         if b is None:
             continue
         if b.dtype is not torch.int32 or not b.is_cuda or b.dim() != 2 or b.shape[1] != 2 or not b.is_contiguous():
             raise ValueError(f"{name} must be a contiguous CUDA int32 tensor [sequences, 2]")
-        seqs, ptrs[i] = b.shape[0], b.data_ptr()
+        seqs = b.shape[0]
     if q_bounds is not None and k_bounds is not None and q_bounds.shape != k_bounds.shape:
         raise ValueError("q_bounds and k_bounds must have as many sequences")
-    return A.acid_mha(q.shape[0], k.shape[0], _DT[q.dtype], heads, kv_heads, d, d ** -0.5 if scale is None else scale, seqs,
-                      ptrs[0], ptrs[1], frame_rows, frames_before, frames_after, q_first), heads * d, kv_heads * d
+    # (plain numbers: a key of the cache must not be an object that can change)
+    desc, wq, wk = _mha_shape(nq, wq, nk, wk, q.dtype, index(heads), None if scale is None else float(scale), seqs,
+                              index(frame_rows), index(frames_before), index(frames_after), index(q_first))
+    if q_bounds is not None or k_bounds is not None:
+        desc = A.acid_mha.from_buffer_copy(desc)
+        desc.q_bounds, desc.k_bounds = _ptr(q_bounds), _ptr(k_bounds)
+    return desc, wq, wk
 
 
 def mha_workspace_size(desc: A.acid_mha, backward: bool = False) -> int:
