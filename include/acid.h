@@ -354,6 +354,13 @@ acid_status acid_mha_forward(const acid_mha* mha, const void* q, int64_t ldq, co
                              const void* v, int64_t ldv, void* out, int64_t ldo, float* lse, void* workspace,
                              size_t workspace_bytes, acid_stream_t stream);
 
+/* Zeros in the rows that acid_mha_forward and acid_mha_backward leave as they are,
+ * those of no sequence: of up to two matrices of the queries' rows (out, dq) or, with
+ * `keys`, of the keys' (dk, dv), and of lse (queries only).  NULL ones are left out.
+ * The operands' rules; other rows are not touched. */
+acid_status acid_mha_clear_padding(const acid_mha* mha, int32_t keys, void* a, int64_t lda, void* b, int64_t ldb,
+                                   float* lse, acid_stream_t stream);
+
 /* Gradients that acid_mha_backward writes; NULL ones are left out, not all of them. */
 typedef struct {
   void* dq; int64_t lddq;    /* device [nq, heads * head_dim] */

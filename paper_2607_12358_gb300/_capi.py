@@ -145,6 +145,7 @@ _PROTOS = {
     "acid_rope_backward": (C.c_int, [_ROPE, _P, C.c_int64, _P, C.c_int64, _P]),
     "acid_mha_forward_workspace_size": (C.c_int, [_MHA, C.POINTER(C.c_size_t)]),
     "acid_mha_backward_workspace_size": (C.c_int, [_MHA, C.POINTER(C.c_size_t)]),
+    "acid_mha_clear_padding": (C.c_int, [_MHA, C.c_int32, _P, C.c_int64, _P, C.c_int64, _P, _P]),
     "acid_mha_forward": (C.c_int, [_MHA, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P, _P,
                                    C.c_size_t, _P]),
     "acid_mha_backward": (C.c_int, [_MHA, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64,

@@ -605,21 +605,13 @@ def mha_workspace(q: torch.Tensor, k: torch.Tensor, heads: int, *, backward: boo
     return torch.empty(mha_workspace_size(desc, backward), dtype=torch.uint8, device=q.device)
 
 
-def _blank_on(stream, bounded):
-    """Allocates results: zeros where sequences may leave rows unwritten."""
-    empty = _empty_on(stream)
-    if not bounded:
-        return empty
-
-    def zeros(*size, **how):
-        t = empty(*size, **how)
-        if stream is None:
-            return t.zero_()
-        handle = _stream(stream)
-        with torch.cuda.stream(torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()):
-            return t.zero_()
-
-    return zeros
+def _clear_padding(desc, keys, a, b, ld, lse, stream):
+    """Zeros in the rows of no sequence of results that a call has allocated."""
+    if a is None and b is None and lse is None:
+        return
+    status = load().acid_mha_clear_padding(C.byref(desc), keys, _ptr(a), ld, _ptr(b), ld, _ptr(lse), _stream(stream))
+    if status:
+        check(status)
 
 
 def acid_mha_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, heads: int, *, scale: float | None = None,
@@ -634,19 +626,21 @@ def acid_mha_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, heads: i
     desc, wq, wk = _mha_desc(q, k, heads, scale, q_bounds, k_bounds, frame_rows, frames_before, frames_after, q_first)
     nq, nk, dt = q.shape[0], k.shape[0], q.dtype
     ldq, ldk, ldv = _rows_of("q", q, nq, wq, dt), _rows_of("k", k, nk, wk, dt), _rows_of("v", v, nk, wk, dt)
-    blank, ldo = _blank_on(stream, q_bounds is not None), wq
+    empty, ldo, new_out, new_lse = _empty_on(stream), wq, None, None
     if out is None:
-        out = blank((nq, wq), dtype=dt, device=q.device)
+        out = new_out = empty((nq, wq), dtype=dt, device=q.device)
     else:
         ldo = _rows_of("out", out, nq, wq, dt)
     if lse is None:
-        lse = blank((heads, nq), dtype=_F32, device=q.device)
+        lse = new_lse = empty((heads, nq), dtype=_F32, device=q.device)
     elif lse.dtype is not _F32 or not lse.is_cuda or lse.shape != (heads, nq) or not lse.is_contiguous():
         raise ValueError(f"lse must be a contiguous CUDA fp32 tensor [{heads}, {nq}]")
     if workspace is not None:
         ws, nws = _workspace(workspace)
     else:
         ws, nws, workspace = _mha_scratch(desc, False, q.device, stream)
+    if q_bounds is not None:
+        _clear_padding(desc, 0, new_out, None, wq, new_lse, stream)
     status = load().acid_mha_forward(C.byref(desc), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
                                      out.data_ptr(), ldo, lse.data_ptr(), ws, nws, _stream(stream))
     if status:
@@ -668,21 +662,24 @@ def acid_mha_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: t
     ldk, ldv = _rows_of("k", k, nk, wk, dt), _rows_of("v", v, nk, wk, dt)
     if lse.dtype is not _F32 or not lse.is_cuda or lse.shape != (heads, nq) or not lse.is_contiguous():
         raise ValueError(f"lse must be a contiguous CUDA fp32 tensor [{heads}, {nq}]")
-    grads, fields = [], []
-    for name, given, rows, width, bounded in (("q", dq, nq, wq, q_bounds is not None),
-                                              ("k", dk, nk, wk, k_bounds is not None),
-                                              ("v", dv, nk, wk, k_bounds is not None)):
-        ld = width
+    grads, new, fields, empty = [], [], [], _empty_on(stream)
+    for name, given, rows, width in (("q", dq, nq, wq), ("k", dk, nk, wk), ("v", dv, nk, wk)):
+        ld, made = width, None
         if given is not None:
             ld = _rows_of("d" + name, given, rows, width, dt)
         elif name in want:
-            given = _blank_on(stream, bounded)((rows, width), dtype=dt, device=q.device)
+            given = made = empty((rows, width), dtype=dt, device=q.device)
         grads.append(given)
+        new.append(made)
         fields += [_ptr(given), ld]
     if workspace is not None:
         ws, nws = _workspace(workspace)
     else:
         ws, nws, workspace = _mha_scratch(desc, True, q.device, stream)
+    if q_bounds is not None:
+        _clear_padding(desc, 0, new[0], None, wq, None, stream)
+    if k_bounds is not None:
+        _clear_padding(desc, 1, new[1], new[2], wk, None, stream)
     fields = A.acid_mha_grads(*fields)
     status = load().acid_mha_backward(C.byref(desc), dout.data_ptr(), ldg, q.data_ptr(), ldq, k.data_ptr(), ldk,
                                       v.data_ptr(), ldv, out.data_ptr(), ldo, lse.data_ptr(), C.byref(fields), ws, nws,

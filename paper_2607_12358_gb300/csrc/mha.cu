@@ -74,6 +74,41 @@ __global__ void __launch_bounds__(kThreads) mha_stats_kernel(const StatArgs a, i
   }
 }
 
+// Zeros in the rows of no sequence, a warp a row.  Results that a caller has not allocated
+// are zero there; zeroing them whole wrote 33 MB and took 10 us of 234 at 4726 + 2501 + 1013
+// rows, 30 heads of 64.
+struct PaddingArgs {
+  const int2* bounds;
+  int seqs, rows, heads;
+  int width;  // bytes of a row
+  uint8_t *a, *b;
+  int64_t lda, ldb;  // bytes
+  float* lse;
+};
+__global__ void __launch_bounds__(kThreads) mha_padding_kernel(const PaddingArgs p) {
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  if (row >= p.rows) return;
+  int lo = 0;  // the last sequence that begins at or before the row
+  for (int hi = p.seqs; hi - lo > 1;) {
+    const int mid = (lo + hi) >> 1;
+    if (__ldg(p.bounds + mid).x <= row) lo = mid;
+    else hi = mid;
+  }
+  int first, n;
+  mha_bound(p.bounds, lo, p.rows, first, n);
+  if (row >= first && row < (int64_t)first + n) return;
+  for (int i = lane * 16; i < p.width; i += 512) {
+    if (p.a != nullptr && ACID_IN_BOUNDS(kSiteMha, row * p.lda + i + 15, p.rows * p.lda))
+      *reinterpret_cast<uint4*>(p.a + row * p.lda + i) = make_uint4(0, 0, 0, 0);
+    if (p.b != nullptr && ACID_IN_BOUNDS(kSiteMha, row * p.ldb + i + 15, p.rows * p.ldb))
+      *reinterpret_cast<uint4*>(p.b + row * p.ldb + i) = make_uint4(0, 0, 0, 0);
+  }
+  if (p.lse != nullptr)
+    for (int h = lane; h < p.heads; h += 32) p.lse[(int64_t)h * p.rows + row] = 0.f;
+}
+
 acid_status check_mha(const acid_mha* m) {
   ACID_REQUIRE(m != nullptr, ACID_ERR_INVALID_ARG, "mha: null description");
   ACID_REQUIRE(m->dtype == ACID_BF16 || m->dtype == ACID_FP32, ACID_ERR_INVALID_ARG, "mha: unknown dtype");
@@ -265,4 +300,27 @@ extern "C" acid_status acid_mha_backward(const acid_mha* mha, const void* dout, 
     ACID_CHECK_LAUNCH();
   }
   return m.dtype == ACID_BF16 ? mha_backward_tc(a, s) : mha_backward_f32(a, s);
+}
+
+extern "C" acid_status acid_mha_clear_padding(const acid_mha* mha, int32_t keys, void* a, int64_t lda, void* b,
+                                              int64_t ldb, float* lse, acid_stream_t stream) {
+  clear_error();
+  ACID_TRY(check_mha(mha));
+  const acid_mha& m = *mha;
+  const int64_t rows = keys ? m.nk : m.nq;
+  const int heads = keys ? m.kv_heads : m.heads;
+  ACID_TRY(check_gradient(m, a, lda, rows, heads, "a"));
+  ACID_TRY(check_gradient(m, b, ldb, rows, heads, "b"));
+  ACID_REQUIRE(aligned(lse, 4) && (lse == nullptr || !keys), ACID_ERR_INVALID_ARG,
+               "acid_mha_clear_padding: lse not aligned, or with the keys' rows");
+  const int32_t* bounds = keys ? m.k_bounds : m.q_bounds;
+  if (bounds == nullptr || rows == 0 || (a == nullptr && b == nullptr && lse == nullptr)) return ACID_OK;
+  const int64_t size = m.dtype == ACID_BF16 ? 2 : 4;
+  ACID_REQUIRE(heads * m.head_dim * size <= INT32_MAX, ACID_ERR_UNSUPPORTED, "acid_mha_clear_padding: rows too wide");
+  const PaddingArgs p{reinterpret_cast<const int2*>(bounds), m.sequences, (int)rows, heads, (int)(heads * m.head_dim * size),
+                      static_cast<uint8_t*>(a), static_cast<uint8_t*>(b), lda * size, ldb * size, lse};
+  launch_pdl(mha_padding_kernel, (unsigned)((rows + kThreads / 32 - 1) / (kThreads / 32)), kThreads, 0,
+             (cudaStream_t)stream, p);
+  ACID_CHECK_LAUNCH();
+  return ACID_OK;
 }

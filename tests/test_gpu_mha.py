@@ -276,3 +276,30 @@ def test_no_rows(acid):
     assert not out.any() and torch.isneginf(lse).all()
     dq, dk, dv = acid.acid_mha_backward(k, k, q, q, out, lse, 2)
     assert not dq.any() and dk.shape == (0, 128)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("room, behind", [(0, 0), (64, 0), (64, 37), (0, 5)])
+def test_allocated_results_are_zero_in_padding(acid, dtype, room, behind):
+    """Results that the call allocates: zeros in the rows of no sequence; given ones are left as they are there."""
+    c = Case(dtype, 4, 2, 64, [30, 0, 64, 1], [64, 5, 0, 33], room=room, behind=behind, seed=5)
+    q, k, v, g = (c.gpu(np.nan_to_num(t)) for t in (c.q, c.k, c.v, c.g))
+    used = {}
+    for n, rows, bs in (("q", c.nq, c.qb), ("k", c.nk, c.kb)):
+        used[n] = torch.zeros(rows, dtype=torch.bool, device=DEV)
+        for a, e in bs:
+            used[n][a:e] = True
+    torch.cuda.empty_cache()
+    junk = [torch.full((1 << 18,), float("nan"), device=DEV) for _ in range(4)]
+    torch.cuda.synchronize()
+    del junk  # (what the results are allocated from)
+    out, lse = acid.acid_mha_forward(q, k, v, c.heads, **c.how(acid))
+    assert not out[~used["q"]].any() and not lse[:, ~used["q"]].any()
+    assert not torch.isnan(out).any() and not torch.isnan(lse).any()
+    grads = acid.acid_mha_backward(g, q, k, v, out, lse, c.heads, **c.how(acid))
+    for n, t in zip("qkk", grads):
+        assert not t[~used[n]].any() and not torch.isnan(t).any()
+    given = torch.full_like(out, SENTINEL)
+    _, lse2 = acid.acid_mha_forward(q, k, v, c.heads, out=given, **c.how(acid))
+    assert (given[~used["q"]] == SENTINEL).all() and torch.equal(given[used["q"]], out[used["q"]])
+    assert torch.equal(lse2, lse)

@@ -193,3 +193,19 @@ def test_binding_refuses():
     assert acid.sequence_bounds([3, 2], 4, device="cpu").tolist() == [[0, 3], [4, 6]]
     with pytest.raises(ValueError):
         acid.sequence_bounds([5], 4, device="cpu")
+
+
+def test_clearing_of_padding_refuses(lib):
+    def call(m, keys=0, a=P, lda=256, b=None, ldb=0, lse=None):
+        return lib.STATUS_NAMES[lib.load().acid_mha_clear_padding(C.byref(m), keys, a, lda, b, ldb, lse, None)]
+
+    m = mha(lib, heads=4, kv_heads=2, head_dim=64, sequences=2, q_bounds=P, k_bounds=P)
+    assert call(m, lda=255) == "ACID_ERR_INVALID_ARG"
+    assert call(m, lda=260) == "ACID_ERR_UNSUPPORTED"
+    assert call(m, a=P + 8) == "ACID_ERR_UNSUPPORTED"
+    assert call(m, b=P, ldb=128) == "ACID_ERR_INVALID_ARG"
+    assert call(m, lse=P + 2) == "ACID_ERR_INVALID_ARG"
+    assert call(m, keys=1, a=P, lda=128, lse=P) == "ACID_ERR_INVALID_ARG"
+    assert call(mha(lib, head_dim=80)) == "ACID_ERR_UNSUPPORTED"
+    assert call(m, a=None) == "ACID_OK"  # nothing to clear
+    assert call(mha(lib, heads=4, kv_heads=2, head_dim=64)) == "ACID_OK"  # no padding
