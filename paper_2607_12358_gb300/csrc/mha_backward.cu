@@ -19,6 +19,7 @@
 
 #include "attention.cuh"
 #include "mha.cuh"
+#include "mha_shares.h"
 
 namespace acid {
 
@@ -96,74 +97,62 @@ __device__ __forceinline__ bool bwd_item(const BwdArgs& a, int slot, int head, B
 // The units of this CTA, in order, by its producer warp.  First whole items, one in
 // turn.  Then the steps of all other items, laid end to end head by head, in equal
 // shares: a share begins and ends inside an item as a rule, whose parts are joined by
-// mha_backward_join_kernel.  `scratch` holds the steps before each slot of a head.
+// mha_backward_join_kernel.  `scratch` holds a head's steps up to and with each slot
+// (uneven items are shared out only where they are fewer than the SMs).
 constexpr int kLeastSteps = 4;  // of a share
+struct BwdUpto {
+  const int64_t* scratch;
+  int64_t per;  // of every slot, or -1: see scratch
+  __device__ __forceinline__ int64_t operator()(int slot) const { return per >= 0 ? (slot + 1) * per : scratch[slot]; }
+};
 template <bool KEYS>
 struct BwdWalk {
   const BwdArgs& a;
-  int* scratch;
+  int64_t* scratch;
   int lane;
   int turn = 0;    // of the whole items
   int next = 0;    // shared item
   bool shared = false;
-  int64_t s, from, to, base, work;  // first step of `next`; this share's steps
-  int shares, units = 0;
-  __device__ __forceinline__ BwdWalk(const BwdArgs& a_, int* scratch_, int lane_)
+  int64_t s, from, to;  // first step of `next`; this share's steps
+  StepShares<BwdUpto> share;
+  int units = 0;
+  __device__ __forceinline__ BwdWalk(const BwdArgs& a_, int64_t* scratch_, int lane_)
       : a(a_), scratch(scratch_), lane(lane_) {}
-  __device__ __forceinline__ int64_t bound(int64_t c) const { return base + work * c / shares; }
 
   __device__ __forceinline__ void share_out() {
     shared = true;
-    int total = 0;
     BwdUnit x;
+    int per = -1;
     if (a.alike) {
       bwd_item<KEYS>(a, 0, 0, x);
-      total = x.steps * a.slots;
+      per = x.steps;
     } else {
+      int64_t total = 0;
       for (int i = 0; i < a.slots; i += 32) {
-        int n = 0;
+        int64_t sum = 0;
         if (i + lane < a.slots) {
           bwd_item<KEYS>(a, i + lane, 0, x);
-          n = x.steps;
+          sum = x.steps;
         }
-        int sum = n;
 #pragma unroll
         for (int off = 1; off < 32; off *= 2) {
-          const int t = __shfl_up_sync(0xffffffffu, sum, off);
+          const int64_t t = __shfl_up_sync(0xffffffffu, (long long)sum, off);
           if (lane >= off) sum += t;
         }
-        if (i + lane < a.slots) scratch[i + lane] = total + sum;  // up to and with this slot
-        total += __shfl_sync(0xffffffffu, sum, 31);
+        if (i + lane < a.slots) scratch[i + lane] = total + sum;
+        total += __shfl_sync(0xffffffffu, (long long)sum, 31);
       }
       __syncwarp();
     }
-    const int per = a.alike ? x.steps : 0;
-    auto upto = [&](int slot) { return slot < 0 ? 0 : a.alike ? (slot + 1) * per : scratch[slot]; };
-    const int head0 = a.full / a.slots, slot0 = a.full % a.slots;
-    base = (int64_t)head0 * total + upto(slot0 - 1);
-    work = (int64_t)a.heads * total - base;
-    shares = (int)max((int64_t)1, min((int64_t)gridDim.x, work / kLeastSteps));
-    if ((int)blockIdx.x >= shares) {
+    share = StepShares<BwdUpto>(BwdUpto{scratch, per}, a.heads, a.slots, a.full, gridDim.x, kLeastSteps);
+    if ((int)blockIdx.x >= share.shares) {
       next = a.items;
       from = to = 0;
       return;
     }
-    from = bound(blockIdx.x);
-    to = bound(blockIdx.x + 1);
-    if (blockIdx.x == 0) {
-      next = a.full;
-      s = base;
-    } else {  // the item that step `from` lies in
-      const int head = (int)(from / total), rest = (int)(from - (int64_t)head * total);
-      int lo = 0, hi = a.slots - 1;
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (upto(mid) > rest) hi = mid;
-        else lo = mid + 1;
-      }
-      next = head * a.slots + lo;
-      s = (int64_t)head * total + upto(lo - 1);
-    }
+    from = share.bound(blockIdx.x);
+    to = share.bound(blockIdx.x + 1);
+    share.begin(blockIdx.x, next, s);
     fence_proxy_async_smem();  // the scratch becomes a target of copies
     __syncwarp();
   }
@@ -207,15 +196,15 @@ struct BwdWalk {
       // the item begins: the CTAs that work on a head then stream the same tiles at a time,
       // all but one out of L2 (32760 queries, 301 and 512 keys, 12 x 128: 709 MB from HBM in
       // 140 us without, 220 MB in 121 us with it).
-      int64_t c = (s - base) * shares / work;
-      while (bound(c) < s) ++c;
-      const int turn = bound(c) < s + n ? (int)(bound(c) - s) : 0;
+      int64_t c = (s - share.base) * share.shares / share.work;
+      while (share.bound(c) < s) ++c;
+      const int turn = share.bound(c) < s + n ? (int)(share.bound(c) - s) : 0;
       x.n0 = n0 >= turn ? n0 - turn : n0 - turn + n;
       x.steps = n1 - n0;
       if (n0 > 0 || n1 < n) x.part = 2 * blockIdx.x + (units > 0);
       if (n0 == 0 && n1 < n && lane == 0) {
         int last = blockIdx.x;
-        while (bound(last + 1) < s + n) ++last;
+        while (share.bound(last + 1) < s + n) ++last;
         a.record[2 * blockIdx.x] = make_int4(x.rows, x.row0, x.head, x.part);
         a.record[2 * blockIdx.x + 1] = make_int4(last, 0, 0, 0);
       }
@@ -431,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 0) {  // -------------------------------------------- TMA producer
     bool ok = true;
     int y1_done = 0, y2_done = 0, x_done = 0, edges = 0, g = 0;
-    BwdWalk<KEYS> walk(a, reinterpret_cast<int*>(sY1), lane);
+    BwdWalk<KEYS> walk(a, reinterpret_cast<int64_t*>(sY1), lane);
     BwdUnit x;
     for (; ok; ++x_done) {
       const bool more = walk(x, D);
