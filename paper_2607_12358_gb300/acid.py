@@ -484,9 +484,11 @@ def _rope(call, x, heads, axes, theta, grid, origin, positions, first_rows, halv
     if (grid is None) == (positions is None):
         raise ValueError("need either grid or positions")
     rows, width = x.shape
-    desc = _rope_desc(rows, width, dtype, index(heads), tuple(axes), theta if isinstance(theta, float) else
-                      float(theta) if isinstance(theta, int) else tuple(theta), None if grid is None else tuple(grid),
-                      None if origin is None else tuple(origin), index(first_rows), bool(halves))
+    # (plain numbers: a key of the cache must not be an object that can change)
+    desc = _rope_desc(rows, width, dtype, index(heads), tuple(map(index, axes)),
+                      float(theta) if isinstance(theta, (float, int)) else tuple(map(float, theta)),
+                      None if grid is None else tuple(map(index, grid)),
+                      None if origin is None else tuple(map(float, origin)), index(first_rows), bool(halves))
     if positions is not None:
         ld = _rows_of("positions", positions, rows, desc.axes, _F32)
         desc = A.acid_rope.from_buffer_copy(desc)
