@@ -600,11 +600,14 @@ def _mha_scratch(desc, backward, device, stream):
 
 def mha_workspace(q: torch.Tensor, k: torch.Tensor, heads: int, *, backward: bool = False,
                   q_bounds: torch.Tensor | None = None, k_bounds: torch.Tensor | None = None) -> torch.Tensor:
-    """A workspace for acid_mha_forward or acid_mha_backward of operands of these shapes, with any window of frames."""
-    if k_bounds is None and q_bounds is not None:
-        k_bounds = q_bounds  # the size goes by their number
-    desc, _, _ = _mha_desc(q, k, heads, None, q_bounds, k_bounds, 0, -1, -1, 0)
-    return torch.empty(mha_workspace_size(desc, backward), dtype=torch.uint8, device=q.device)
+    """A workspace for acid_mha_forward or acid_mha_backward of operands of these shapes, with any window of frames; of
+    bounds the number of sequences counts (one: a call with bounds of either side, both or none)."""
+    desc = A.acid_mha.from_buffer_copy(_mha_desc(q, k, heads, None, q_bounds, k_bounds, 0, -1, -1, 0)[0])
+    nws = 0
+    # (an address that nothing reads stands for bounds: they add a slot to a side's items, with which it may need less)
+    for desc.q_bounds, desc.k_bounds in ((8, 8),) if desc.sequences > 1 else ((None, None), (8, None), (None, 8), (8, 8)):
+        nws = max(nws, mha_workspace_size(desc, backward))
+    return torch.empty(nws, dtype=torch.uint8, device=q.device)
 
 
 def _clear_padding(desc, keys, a, b, ld, lse, stream):

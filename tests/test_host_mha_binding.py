@@ -42,3 +42,41 @@ def test_rotation_of_values_that_change_in_place(acid, monkeypatch, name):
             want[at][0] = moving.item()
             assert seen.pop() == want
             moving += 2
+
+
+def sizes(nq, nk, heads, kv_heads, d, backward, sequences=1):
+    """Bytes that the library asks for, of each call on such operands."""
+    from paper_2607_12358_gb300 import _capi as A, acid
+
+    bounded = [(8, 8)] if sequences > 1 else [(None, None), (8, None), (None, 8), (8, 8)]  # (addresses that nothing reads)
+    for q, k in bounded:
+        for window in (dict(frames_before=-1, frames_after=-1), dict(frame_rows=7, frames_before=1, frames_after=0)):
+            m = A.acid_mha(nq=nq, nk=nk, dtype=A.ACID_BF16, heads=heads, kv_heads=kv_heads, head_dim=d, scale=1.0,
+                           sequences=sequences, q_bounds=q, k_bounds=k, **window)
+            yield acid.mha_workspace_size(m, backward)
+
+
+def bounds(sequences):
+    """What the binding looks at of a tensor of bounds on a GPU."""
+    return SimpleNamespace(dtype=torch.int32, is_cuda=True, shape=(sequences, 2), dim=lambda: 2, is_contiguous=lambda: True,
+                           data_ptr=lambda: 8)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("heads, kv_heads, d", [(4, 4, 128), (8, 4, 64), (1, 1, 64)])
+def test_workspace_covers_every_call(acid, heads, kv_heads, d, backward):
+    """Bounds add a slot to the items.  Where the items reach the number of SMs with it no scratch is needed, while the
+    call without bounds, which has fewer, shares out all its steps: the helper's workspace does for both."""
+    rows = [1, 3, 77, 8192]
+    for sms in (148, 152):  # (148 stands for them where there is no GPU to ask)
+        rows += [128 * n for h in {heads, kv_heads} for n in (sms // h - 1, sms // h, sms // h + 1)]
+    for nq in rows:
+        q = torch.empty(nq, heads * d, dtype=torch.bfloat16)
+        for nk in [0] + rows:
+            k = torch.empty(nk, kv_heads * d, dtype=torch.bfloat16)
+            for given in ({}, dict(q_bounds=bounds(1)), dict(k_bounds=bounds(1)), dict(q_bounds=bounds(1), k_bounds=bounds(1))):
+                room = acid.mha_workspace(q, k, heads, backward=backward, **given)
+                assert room.numel() >= max(sizes(nq, nk, heads, kv_heads, d, backward)), (nq, nk, list(given))
+            for given in (dict(q_bounds=bounds(3)), dict(k_bounds=bounds(3))):
+                room = acid.mha_workspace(q, k, heads, backward=backward, **given)
+                assert room.numel() >= max(sizes(nq, nk, heads, kv_heads, d, backward, 3)), (nq, nk, list(given))
