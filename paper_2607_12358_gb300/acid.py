@@ -581,15 +581,16 @@ def mha_workspace_size(desc: A.acid_mha, backward: bool = False) -> int:
 
 
 @functools.lru_cache(maxsize=1024)
-def _mha_bytes(nq, nk, dtype, heads, kv_heads, d, seqs, q_bounded, k_bounded, windowed, backward):
-    """Workspace of a call: the size goes by these alone (an address that nothing reads stands for bounds)."""
+def _mha_bytes(device, nq, nk, dtype, heads, kv_heads, d, seqs, q_bounded, k_bounded, windowed, backward):
+    """Workspace of a call: the size goes by these alone (the device's SMs; an address that nothing reads stands for
+    bounds)."""
     return mha_workspace_size(A.acid_mha(nq, nk, dtype, heads, kv_heads, d, 1.0, seqs, 8 if q_bounded else None,
                                          8 if k_bounded else None, windowed, 0, 0, 0), backward)
 
 
 def _mha_scratch(desc, backward, device, stream):
     """(address, bytes, owner) of a workspace for the call."""
-    nws = _mha_bytes(desc.nq, desc.nk, desc.dtype, desc.heads, desc.kv_heads, desc.head_dim, desc.sequences,
+    nws = _mha_bytes(_current_device(), desc.nq, desc.nk, desc.dtype, desc.heads, desc.kv_heads, desc.head_dim, desc.sequences,
                      desc.q_bounds is not None, desc.k_bounds is not None,
                      int(desc.frame_rows > 0 and (desc.frames_before >= 0 or desc.frames_after >= 0)), backward)
     if not nws:

@@ -80,3 +80,16 @@ def test_workspace_covers_every_call(acid, heads, kv_heads, d, backward):
             for given in (dict(q_bounds=bounds(3)), dict(k_bounds=bounds(3))):
                 room = acid.mha_workspace(q, k, heads, backward=backward, **given)
                 assert room.numel() >= max(sizes(nq, nk, heads, kv_heads, d, backward, 3)), (nq, nk, list(given))
+
+
+def test_workspace_of_the_device_that_the_call_runs_on(acid, monkeypatch):
+    """The size goes by the GPU's SMs: a second GPU's is its own, for the same shape."""
+    needs, given, device = {0: 1024, 1: 4096}, [], 0
+    lib = SimpleNamespace(acid_mha_forward=lambda *args: given.append(args[11]) or 0)
+    monkeypatch.setattr(acid, "load", lambda: lib)
+    monkeypatch.setattr(acid, "mha_workspace_size", lambda desc, backward=False: needs[device])
+    monkeypatch.setattr(acid, "_current_device", lambda: device)
+    x = torch.empty(200, 192, dtype=torch.bfloat16)
+    for device in (0, 1, 0, 1):
+        acid.acid_mha_forward(x, x, x, 3)
+        assert given.pop() == needs[device]
