@@ -57,7 +57,8 @@ __global__ void __launch_bounds__(kThreads) mha_stats_kernel(const StatArgs a, i
         o[k].load(static_cast<const T*>(a.out) + at);
         g[k].load(static_cast<const T*>(a.dout) + from);
       }
-      lse[k] = a.lse[(int64_t)h * a.s.nq + row];
+      if (ACID_IN_BOUNDS(kSiteMha, h * (int64_t)a.s.nq + row, (int64_t)a.s.heads * a.s.nq))
+        lse[k] = a.lse[(int64_t)h * a.s.nq + row];
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
@@ -68,7 +69,9 @@ __global__ void __launch_bounds__(kThreads) mha_stats_kernel(const StatArgs a, i
       for (int c = 0; c < 8; ++c) sum = fmaf(x[c], y[c], sum);
       for (int off = lanes / 2; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
       const int r = r0 + k * step;
-      if (part == 0 && r < kStatRows) {
+      if (part == 0 && r < kStatRows &&
+          ACID_IN_BOUNDS(kSiteMha, mha_stat_offset(h, a.slots, blockIdx.x) + kStatRows + r,
+                         mha_stat_offset(a.s.heads, a.slots, 0))) {
         to[r] = lse[k] == -INFINITY ? -INFINITY : -lse[k] * a.unit;  // (a row that sees no key: probability 0)
         to[kStatRows + r] = lse[k] == -INFINITY ? 0.f : -sum;
       }
@@ -92,14 +95,8 @@ __global__ void __launch_bounds__(kThreads) mha_padding_kernel(const PaddingArgs
   const int lane = threadIdx.x & 31;
   const int64_t row = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
   if (row >= p.rows) return;
-  int lo = 0;  // the last sequence that begins at or before the row
-  for (int hi = p.seqs; hi - lo > 1;) {
-    const int mid = (lo + hi) >> 1;
-    if (__ldg(p.bounds + mid).x <= row) lo = mid;
-    else hi = mid;
-  }
   int first, n;
-  mha_bound(p.bounds, lo, p.rows, first, n);
+  mha_bound(p.bounds, mha_sequence_of(p.bounds, p.seqs, row), p.seqs, p.rows, first, n);
   if (row >= first && row < (int64_t)first + n) return;
   for (int i = lane * 16; i < p.width; i += 512) {
     if (p.a != nullptr && ACID_IN_BOUNDS(kSiteMha, row * p.lda + i + 15, p.rows * p.lda))
@@ -108,7 +105,8 @@ __global__ void __launch_bounds__(kThreads) mha_padding_kernel(const PaddingArgs
       *reinterpret_cast<uint4*>(p.b + row * p.ldb + i) = make_uint4(0, 0, 0, 0);
   }
   if (p.lse != nullptr)
-    for (int h = lane; h < p.heads; h += 32) p.lse[(int64_t)h * p.rows + row] = 0.f;
+    for (int h = lane; h < p.heads; h += 32)
+      if (ACID_IN_BOUNDS(kSiteMha, h * (int64_t)p.rows + row, (int64_t)p.heads * p.rows)) p.lse[(int64_t)h * p.rows + row] = 0.f;
 }
 
 acid_status check_mha(const acid_mha* m) {
@@ -292,6 +290,7 @@ extern "C" acid_status acid_mha_backward(const acid_mha* mha, const void* dout, 
   a.lddv = o.lddv;
   a.stats = static_cast<float*>(ws);
   a.part = static_cast<uint8_t*>(ws) + stat_bytes(m);
+  a.part_bytes = ws_bytes - stat_bytes(m);
   if (m.nq > 0) {
     const StatArgs t{a.shape, out, dout, ldo, lddo, lse, a.stats, m.head_dim, stat_slots(m),
                      m.dtype == ACID_BF16 ? 1.4426950408889634f : 1.0f};

@@ -27,16 +27,28 @@ struct MhaSeq {
 
 // A bound as the device reads it: inside the matrix and in order, whatever the
 // array holds, so that no access leaves the operands.
-__device__ __forceinline__ void mha_bound(const int2* b, int i, int n, int& first, int& rows) {
-  const int2 v = b != nullptr ? __ldg(b + i) : make_int2(0, n);
+__device__ __forceinline__ void mha_bound(const int2* b, int i, int seqs, int n, int& first, int& rows) {
+  const int2 v = b != nullptr && ACID_IN_BOUNDS(kSiteMha, i, seqs) ? __ldg(b + i) : make_int2(0, n);
   first = min(max(v.x, 0), n);
   rows = min(max(v.y, first), n) - first;
 }
 __device__ __forceinline__ MhaSeq mha_seq(const MhaShape& s, int i) {
   MhaSeq q;
-  mha_bound(s.qb, i, s.nq, q.q0, q.nq);
-  mha_bound(s.kb, i, s.nk, q.k0, q.nk);
+  mha_bound(s.qb, i, s.seqs, s.nq, q.q0, q.nq);
+  mha_bound(s.kb, i, s.seqs, s.nk, q.k0, q.nk);
   return q;
+}
+
+// The last sequence that begins at or before a row: its own, if it is of one.
+__device__ __forceinline__ int mha_sequence_of(const int2* b, int seqs, int64_t row) {
+  int lo = 0;
+  if (b != nullptr)
+    for (int hi = seqs; hi - lo > 1;) {
+      const int mid = (lo + hi) >> 1;
+      if (__ldg(b + mid).x <= row) lo = mid;
+      else hi = mid;
+    }
+  return lo;
 }
 
 // Slots of tiles of `tile` rows.  Sequence i begins at slot first / tile + i, so
@@ -176,7 +188,7 @@ struct MhaArgs {
   void *dq, *dk, *dv;
   int64_t lddq, lddk, lddv;
   float* stats;
-  void* part;
+  void* part;  // scratch behind the statistics
   size_t part_bytes;
 };
 

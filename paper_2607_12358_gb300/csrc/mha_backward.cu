@@ -48,6 +48,7 @@ struct BwdArgs {
   int order;      // of the items (MhaOrder)
   float* part;    // [2 CTAs][1 or 2][D / 4][128 rows][4]: sums of an item's share
   int4* record;   // [CTAs][2]: the item that begins in a CTA's share and ends in another's
+  int64_t part_floats;  // room for parts
 };
 
 // What a CTA does at a time: a stationary tile, or a share of its steps.
@@ -453,8 +454,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (lane == 0) {
             mbar_expect_tx(to, C::T_BYTES + (stat_dst != nullptr ? kStatBytes : 0));
             for (int c = 0; c < C::CH; ++c) tma_load_2d(dst + c * C::CHUNK, map, to, head * D + c * 64, row);
-            if (stat_dst != nullptr)
-              bulk_load(stat_dst, a.stats + mha_stat_offset(head, a.stat_slots, x.stat + j), kStatBytes, to);
+            if (stat_dst != nullptr) {
+              const int64_t at = mha_stat_offset(head, a.stat_slots, x.stat + j);
+              const bool in = ACID_IN_BOUNDS(kSiteMha, at + 2 * kStatRows - 1, mha_stat_offset(a.s.heads, a.stat_slots, 0));
+              bulk_load(stat_dst, a.stats + (in ? at : 0), kStatBytes, to);  // (the barrier counts its bytes)
+            }
           }
           if (clear) {
             if (!mbar_wait_warp(bar.edge, edges++ & 1)) return false;
@@ -587,8 +591,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       steps = entry(n)[0].x;
       if (!KEYS && steps > 0) {
         const float* st = a.stats + mha_stat_offset(entry(n)[0].y, a.stat_slots, entry(n)[2].w);
-        nlse = st[r];
-        ndelta = st[kStatRows + r];
+        if (ACID_IN_BOUNDS(kSiteMha, st + kStatRows + r - a.stats, mha_stat_offset(a.s.heads, a.stat_slots, 0))) {
+          nlse = st[r];
+          ndelta = st[kStatRows + r];
+        }
       }
       return true;
     };
@@ -743,6 +749,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (__any_sync(0xffffffffu, part >= 0)) {
           float* to = a.part + (((int64_t)part * C::SUMS + w) * (D / 4) + c / 4) * (kTile * 4) + r * 4;
+          if (!ACID_IN_BOUNDS(kSiteMha, to + 7 * kTile * 4 + 3 - a.part, a.part_floats)) continue;
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             *reinterpret_cast<uint4*>(to + i * kTile * 4) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
@@ -783,6 +790,7 @@ __global__ void __launch_bounds__(256) mha_backward_join_kernel(const __grid_con
   if (out == nullptr) return;
   constexpr int64_t kPart = (int64_t)SUMS * (D / 4) * (kTile * 4);
   const float* p = a.part + (int64_t)idx * (kTile * 16) + row * 4;
+  if (!ACID_IN_BOUNDS(kSiteMha, p + max(e.w, 2 * last) * kPart + 3 * kTile * 4 + 3 - a.part, a.part_floats)) return;
   float4 sum[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) sum[k] = *reinterpret_cast<const float4*>(p + e.w * kPart + k * kTile * 4);
@@ -874,7 +882,8 @@ acid_status launch(const MhaArgs& x, cudaStream_t s) {
   const bool shared = p.full < p.items;
   const int ctas = shared ? sms : std::min(p.items, sms);
   a.part = static_cast<float*>(x.part);
-  a.record = reinterpret_cast<int4*>(a.part + (size_t)sms * 2 * C::SUMS * kTile * D);
+  a.part_floats = (int64_t)sms * 2 * C::SUMS * kTile * D;
+  a.record = reinterpret_cast<int4*>(a.part + a.part_floats);
   launch_pdl(mha_backward_kernel<C>, ctas, kThreads, C::SMEM, s, KEYS ? tk : tq, KEYS ? tv : tg, KEYS ? tq : tk,
              KEYS ? tg : tv, a);
   ACID_CHECK_LAUNCH();

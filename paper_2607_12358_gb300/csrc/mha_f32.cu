@@ -15,14 +15,22 @@ namespace {
 
 constexpr int kGroups = 4, kCols = 32, kThreads = 128 * kGroups;  // groups of four warps; rows of a streamed tile
 
-// N rows of D values (row stride lds in shared memory) on their way (cp.async); rows
-// outside [0, valid) are zeros.
+// A matrix in memory: [rows, ..] with row stride ld.
+struct Rows {
+  const float* p;
+  int64_t ld;
+  int rows;
+};
+// N rows of D values from (row, col) on their way (cp.async) to shared memory (row stride
+// lds there); rows outside [0, valid) are zeros.
 template <int D, int N>
-__device__ __forceinline__ void load_rows(float* dst, int lds, const float* src, int64_t ld, int valid, int tid,
+__device__ __forceinline__ void load_rows(float* dst, int lds, const Rows& m, int64_t row, int col, int valid, int tid,
                                           int threads) {
+  const float* src = m.p + row * m.ld + col;
+  const int64_t ld = m.ld;
   for (int i = tid; i < N * (D / 4); i += threads) {
     const int r = i / (D / 4), c = (i % (D / 4)) * 4;
-    const bool on = r < valid;
+    const bool on = r < valid && ACID_IN_BOUNDS(kSiteMha, (row + r) * ld + col + c + 3, m.rows * ld);
     cp_async<16>(dst + r * lds + c, src + (on ? (int64_t)r * ld + c : 0), on);
   }
 }
@@ -76,8 +84,8 @@ __device__ __forceinline__ void accumulate(const float* p, int ldp, const float*
 
 struct F32Args {
   MhaShape s;
-  const void *q, *k, *v, *o, *dout;
-  int64_t ldq, ldk, ldv, ldo, lddo;
+  const float *q, *k, *v, *dout;
+  int64_t ldq, ldk, ldv, lddo;
   void *out1, *out2, *out3;  // forward: out; backward: dk, dv, dq
   int64_t ld1, ld2, ld3;
   float *lse, *stats;
@@ -117,10 +125,8 @@ __global__ void __launch_bounds__(kThreads) mha_forward_f32_kernel(const F32Args
   float* sq = sm;
   float* bufs = sm + C::OFF_STREAM + g * C::STREAM;
   float* sp = bufs + C::BUFS * C::BUF + hw * R * C::LDP;
-  const float* q = static_cast<const float*>(a.q) + (int64_t)(seq.q0 + r0) * a.ldq + h * D;
-  const float* k = static_cast<const float*>(a.k) + (int64_t)seq.k0 * a.ldk + hk * D;
-  const float* v = static_cast<const float*>(a.v) + (int64_t)seq.k0 * a.ldv + hk * D;
-  load_rows<D, ROWS>(sq, C::LD, q, a.ldq, rows, threadIdx.x, kThreads);
+  const Rows q{a.q, a.ldq, a.s.nq}, k{a.k, a.ldk, a.s.nk}, v{a.v, a.ldv, a.s.nk};
+  load_rows<D, ROWS>(sq, C::LD, q, (int64_t)seq.q0 + r0, h * D, rows, threadIdx.x, kThreads);
   int lo[R], hi[R], first, last, none;
   mha_keys_of(a.s, seq, r0, first, none);
   mha_keys_of(a.s, seq, r0 + rows - 1, none, last);
@@ -135,8 +141,9 @@ __global__ void __launch_bounds__(kThreads) mha_forward_f32_kernel(const F32Args
   auto fetch = [&](int j, int buf) {  // tile j's keys and values, if there is one
     float* to = bufs + buf * C::BUF;
     if (j * kCols < last) {
-      load_rows<D, kCols>(to, C::LD, k + (int64_t)j * kCols * a.ldk, a.ldk, seq.nk - j * kCols, t, 128);
-      load_rows<D, kCols>(to + kCols * C::LD, C::LD, v + (int64_t)j * kCols * a.ldv, a.ldv, seq.nk - j * kCols, t, 128);
+      const int64_t row = (int64_t)seq.k0 + j * kCols;
+      load_rows<D, kCols>(to, C::LD, k, row, hk * D, seq.nk - j * kCols, t, 128);
+      load_rows<D, kCols>(to + kCols * C::LD, C::LD, v, row, hk * D, seq.nk - j * kCols, t, 128);
     }
     cp_async_commit();
   };
@@ -213,7 +220,8 @@ __global__ void __launch_bounds__(kThreads) mha_forward_f32_kernel(const F32Args
     const int64_t row = seq.q0 + r0 + r, at = row * a.ld1 + h * D + c;
     if (!ACID_IN_BOUNDS(kSiteMha, at, (int64_t)a.s.nq * a.ld1)) continue;
     static_cast<float*>(a.out1)[at] = den > 0.f ? acc / den : den == 0.f ? 0.f : den;
-    if (c == 0) a.lse[(int64_t)h * a.s.nq + row] = den == 0.f ? -INFINITY : mx + logf(den);
+    if (c == 0 && ACID_IN_BOUNDS(kSiteMha, h * (int64_t)a.s.nq + row, (int64_t)a.s.heads * a.s.nq))
+      a.lse[(int64_t)h * a.s.nq + row] = den == 0.f ? -INFINITY : mx + logf(den);
   }
 }
 
@@ -240,16 +248,14 @@ __device__ __forceinline__ void mha_backward_f32(const F32Args& a) {
   float* bufs = sm + C::OFF_STREAM + g * C::STREAM;
   float* sp = bufs + C::BUFS * C::BUF;
   float* sd = sp + ROWS * C::LDP;
-  const float* q = static_cast<const float*>(a.q) + (int64_t)seq.q0 * a.ldq;
-  const float* k = static_cast<const float*>(a.k) + (int64_t)seq.k0 * a.ldk;
-  const float* v = static_cast<const float*>(a.v) + (int64_t)seq.k0 * a.ldv;
-  const float* dout = static_cast<const float*>(a.dout) + (int64_t)seq.q0 * a.lddo;
+  const Rows q{a.q, a.ldq, a.s.nq}, dout{a.dout, a.lddo, a.s.nq}, k{a.k, a.ldk, a.s.nk}, v{a.v, a.ldv, a.s.nk};
+  const int64_t x0 = (KEYS ? seq.k0 : seq.q0) + (int64_t)r0, y0 = KEYS ? seq.q0 : seq.k0;  // rows in memory
   if (KEYS) {
-    load_rows<D, ROWS>(x1, C::LD, k + (int64_t)r0 * a.ldk + hb * D, a.ldk, rows, threadIdx.x, kThreads);
-    load_rows<D, ROWS>(x2, C::LD, v + (int64_t)r0 * a.ldv + hb * D, a.ldv, rows, threadIdx.x, kThreads);
+    load_rows<D, ROWS>(x1, C::LD, k, x0, hb * D, rows, threadIdx.x, kThreads);
+    load_rows<D, ROWS>(x2, C::LD, v, x0, hb * D, rows, threadIdx.x, kThreads);
   } else {
-    load_rows<D, ROWS>(x1, C::LD, q + (int64_t)r0 * a.ldq + hb * D, a.ldq, rows, threadIdx.x, kThreads);
-    load_rows<D, ROWS>(x2, C::LD, dout + (int64_t)r0 * a.lddo + hb * D, a.lddo, rows, threadIdx.x, kThreads);
+    load_rows<D, ROWS>(x1, C::LD, q, x0, hb * D, rows, threadIdx.x, kThreads);
+    load_rows<D, ROWS>(x2, C::LD, dout, x0, hb * D, rows, threadIdx.x, kThreads);
   }
   auto seen = [&](int row, int& lo, int& hi) {
     if (KEYS) mha_queries_of(a.s, seq, row, lo, hi);
@@ -264,9 +270,10 @@ __device__ __forceinline__ void mha_backward_f32(const F32Args& a) {
     const int row = r0 + min(hw * R + i, rows - 1);
     seen(row, lo[i], hi[i]);
     if (!KEYS) {
-      const float* at = a.stats + mha_stat_offset(hb, a.stat_slots, slot0 + row / kStatRows) + row % kStatRows;
-      nl[i] = at[0];
-      dl[i] = at[kStatRows];
+      const int64_t at = mha_stat_offset(hb, a.stat_slots, slot0 + row / kStatRows) + row % kStatRows;
+      const bool in = ACID_IN_BOUNDS(kSiteMha, at + kStatRows, mha_stat_offset(a.s.heads, a.stat_slots, 0));
+      nl[i] = in ? a.stats[at] : -INFINITY;
+      dl[i] = in ? a.stats[at + kStatRows] : 0.f;
     }
   }
   const int j0 = first / kCols, tiles = last > j0 * kCols ? (last + kCols - 1) / kCols - j0 : 0;
@@ -279,15 +286,17 @@ __device__ __forceinline__ void mha_backward_f32(const F32Args& a) {
       float* y1 = bufs + buf * C::BUF;
       float* y2 = y1 + kCols * C::LD;
       if (KEYS) {
-        load_rows<D, kCols>(y1, C::LD, q + (int64_t)c0 * a.ldq + h * D, a.ldq, seq.nq - c0, t, 128);
-        load_rows<D, kCols>(y2, C::LD, dout + (int64_t)c0 * a.lddo + h * D, a.lddo, seq.nq - c0, t, 128);
+        load_rows<D, kCols>(y1, C::LD, q, y0 + c0, h * D, seq.nq - c0, t, 128);
+        load_rows<D, kCols>(y2, C::LD, dout, y0 + c0, h * D, seq.nq - c0, t, 128);
         if (t < 2 * kCols) {  // the streamed rows' statistics
-          const float* at = a.stats + mha_stat_offset(h, a.stat_slots, slot0 + c0 / kStatRows) + c0 % kStatRows;
-          cp_async<4>(y2 + kCols * C::LD + t, at + (t / kCols) * kStatRows + t % kCols, true);
+          const int64_t at = mha_stat_offset(h, a.stat_slots, slot0 + c0 / kStatRows) + c0 % kStatRows +
+                             (t / kCols) * kStatRows + t % kCols;
+          if (ACID_IN_BOUNDS(kSiteMha, at, mha_stat_offset(a.s.heads, a.stat_slots, 0)))
+            cp_async<4>(y2 + kCols * C::LD + t, a.stats + at, true);
         }
       } else {
-        load_rows<D, kCols>(y1, C::LD, k + (int64_t)c0 * a.ldk + h * D, a.ldk, seq.nk - c0, t, 128);
-        load_rows<D, kCols>(y2, C::LD, v + (int64_t)c0 * a.ldv + h * D, a.ldv, seq.nk - c0, t, 128);
+        load_rows<D, kCols>(y1, C::LD, k, y0 + c0, h * D, seq.nk - c0, t, 128);
+        load_rows<D, kCols>(y2, C::LD, v, y0 + c0, h * D, seq.nk - c0, t, 128);
       }
     }
     cp_async_commit();
@@ -401,15 +410,13 @@ acid_status backward(const MhaArgs& x, const F32Args& base, cudaStream_t s) {
 F32Args base_args(const MhaArgs& x) {
   F32Args a = {};
   a.s = x.shape;
-  a.q = x.q;
-  a.k = x.k;
-  a.v = x.v;
-  a.o = x.out;
-  a.dout = x.dout;
+  a.q = static_cast<const float*>(x.q);
+  a.k = static_cast<const float*>(x.k);
+  a.v = static_cast<const float*>(x.v);
+  a.dout = static_cast<const float*>(x.dout);
   a.ldq = x.ldq;
   a.ldk = x.ldk;
   a.ldv = x.ldv;
-  a.ldo = x.ldo;
   a.lddo = x.lddo;
   a.lse = x.lse;
   a.stats = x.stats;

@@ -26,6 +26,7 @@ struct FewArgs {
   float scale;   // of the scores, in the exponential's unit
   int splits, chunks;  // shares of a row's keys; groups of R heads that share a key head
   float* part;   // [row][head][split][D + 2]: unnormalised output, reference max, sum
+  int64_t part_floats;
 };
 
 // Exponential and logarithm of a type's scores: base 2 by the hardware for bf16, e for fp32.
@@ -79,15 +80,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) mha_few_kernel(const __grid_co
   const bool on = col < D;  // (head dim 96: 12 of 16 lanes)
   const int row = blockIdx.z, hk = blockIdx.y / a.chunks, h0 = hk * a.s.group + blockIdx.y % a.chunks * R;
   const int heads = min(R, (hk + 1) * a.s.group - h0);
-  // the row's sequence: the last that begins at or before it
-  int lo = 0;
-  if (a.s.qb != nullptr)
-    for (int hi = a.s.seqs; hi - lo > 1;) {
-      const int mid = (lo + hi) >> 1;
-      if (__ldg(a.s.qb + mid).x <= row) lo = mid;
-      else hi = mid;
-    }
-  const MhaSeq seq = mha_seq(a.s, lo);
+  const MhaSeq seq = mha_seq(a.s, mha_sequence_of(a.s.qb, a.s.seqs, row));
   if (row < seq.q0 || row >= seq.q0 + seq.nq) return;  // of no sequence
   int first, last;
   mha_keys_of(a.s, seq, row - seq.q0, first, last);
@@ -116,7 +109,9 @@ __global__ void __launch_bounds__(32 * kWarps, 2) mha_few_kernel(const __grid_co
       const int j = j0 + b * KEYS;
       kr[b].zero();
       vr[b].zero();
-      if (on && j < end) {
+      const int64_t row = seq.k0 + (int64_t)j, at = hk * D + col + 7;
+      if (on && j < end && ACID_IN_BOUNDS(kSiteMha, row * a.ldk + at, (int64_t)a.s.nk * a.ldk) &&
+          ACID_IN_BOUNDS(kSiteMha, row * a.ldv + at, (int64_t)a.s.nk * a.ldv)) {
         kr[b].load(kp + (int64_t)j * a.ldk);
         vr[b].load(vp + (int64_t)j * a.ldv);
       }
@@ -203,7 +198,8 @@ __global__ void __launch_bounds__(32 * kWarps, 2) mha_few_kernel(const __grid_co
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) o += by[w] * joined[w][h][c];
       if (a.splits > 1) {
-        a.part[(hr * a.splits + blockIdx.x) * (D + 2) + c] = o;
+        const int64_t at = (hr * a.splits + blockIdx.x) * (D + 2) + c;
+        if (ACID_IN_BOUNDS(kSiteMha, at, a.part_floats)) a.part[at] = o;
       } else {
         const int64_t at = (int64_t)row * a.ldo + (h0 + h) * D + c;
         if (ACID_IN_BOUNDS(kSiteMha, at, (int64_t)a.s.nq * a.ldo))
@@ -212,10 +208,12 @@ __global__ void __launch_bounds__(32 * kWarps, 2) mha_few_kernel(const __grid_co
     }
     if (threadIdx.x == 0) {
       if (a.splits > 1) {
-        float* p = a.part + (hr * a.splits + blockIdx.x) * (D + 2) + D;
-        p[0] = m;
-        p[1] = l;
-      } else {
+        const int64_t at = (hr * a.splits + blockIdx.x) * (D + 2) + D;
+        if (ACID_IN_BOUNDS(kSiteMha, at + 1, a.part_floats)) {
+          a.part[at] = m;
+          a.part[at + 1] = l;
+        }
+      } else if (ACID_IN_BOUNDS(kSiteMha, (h0 + h) * (int64_t)a.s.nq + row, (int64_t)a.s.heads * a.s.nq)) {
         a.lse[(int64_t)(h0 + h) * a.s.nq + row] = l == 0.f ? -INFINITY : Base<T>::lse(m, l);
       }
     }
@@ -232,16 +230,11 @@ __global__ void __launch_bounds__(32 * kJoinWarps) mha_few_join_kernel(const __g
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int row = blockIdx.x / a.s.heads, h = blockIdx.x % a.s.heads;
   if (a.s.qb != nullptr) {  // rows of no sequence stay as they are
-    int lo = 0;
-    for (int hi = a.s.seqs; hi - lo > 1;) {
-      const int mid = (lo + hi) >> 1;
-      if (__ldg(a.s.qb + mid).x <= row) lo = mid;
-      else hi = mid;
-    }
-    const MhaSeq seq = mha_seq(a.s, lo);
+    const MhaSeq seq = mha_seq(a.s, mha_sequence_of(a.s.qb, a.s.seqs, row));
     if (row < seq.q0 || row >= seq.q0 + seq.nq) return;
   }
   const float* p = a.part + (int64_t)blockIdx.x * a.splits * (D + 2);
+  if (!ACID_IN_BOUNDS(kSiteMha, (blockIdx.x + (int64_t)1) * a.splits * (D + 2) - 1, a.part_floats)) return;
   float m = -INFINITY;
   for (int s = threadIdx.x; s < a.splits; s += 32 * kJoinWarps) m = fmaxf(m, p[(int64_t)s * (D + 2) + D]);
 #pragma unroll
@@ -275,7 +268,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) mha_few_join_kernel(const __g
   const int64_t at = (int64_t)row * a.ldo + h * D + c;
   if (!ACID_IN_BOUNDS(kSiteMha, at, (int64_t)a.s.nq * a.ldo)) return;
   io<T>::st(static_cast<T*>(a.out) + at, l == 0.f ? 0.f : sum / l);
-  if (c == 0) a.lse[(int64_t)h * a.s.nq + row] = l == 0.f ? -INFINITY : Base<T>::lse(m, l);
+  if (c == 0 && ACID_IN_BOUNDS(kSiteMha, h * (int64_t)a.s.nq + row, (int64_t)a.s.heads * a.s.nq))
+    a.lse[(int64_t)h * a.s.nq + row] = l == 0.f ? -INFINITY : Base<T>::lse(m, l);
 }
 
 // Query heads of a key head that a CTA takes.
@@ -304,6 +298,7 @@ acid_status launch(const MhaArgs& x, cudaStream_t s) {
   a.splits = few_splits(a.s);
   a.chunks = (a.s.group + R - 1) / R;
   a.part = static_cast<float*>(x.part);
+  a.part_floats = (int64_t)(x.part_bytes / sizeof(float));
   launch_pdl(mha_few_kernel<T, D, R>, dim3(a.splits, a.s.kv_heads * a.chunks, a.s.nq), 32 * kWarps, 0, s, a);
   ACID_CHECK_LAUNCH();
   if (a.splits > 1) {

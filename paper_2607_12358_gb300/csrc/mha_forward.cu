@@ -32,6 +32,7 @@ struct FwdArgs {
   int units;
   float* part_o;   // [split units][256][D]: unnormalised output
   float* part_ml;  // [split units][256][2]: reference max and sum
+  int64_t part_rows;  // rows of parts that the scratch has room for
 };
 
 constexpr int kBarBytes = 768;  // barriers, units
@@ -80,8 +81,12 @@ template <class C>
 __device__ __forceinline__ void write_empty(const FwdArgs& a, const FwdUnit& x, int lane) {
   const int rows = min(x.rows, kBQ);
   for (int r = lane; r < rows; r += 32) {
-    if (x.part >= 0) *reinterpret_cast<float2*>(a.part_ml + ((int64_t)x.part * kBQ + r) * 2) = make_float2(-INFINITY, 0.f);
-    else a.lse[(int64_t)x.head * a.s.nq + x.q0 + r] = -INFINITY;
+    if (x.part >= 0) {
+      const int64_t at = (int64_t)x.part * kBQ + r;
+      if (ACID_IN_BOUNDS(kSiteMha, at, a.part_rows)) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(-INFINITY, 0.f);
+    } else if (ACID_IN_BOUNDS(kSiteMha, x.head * (int64_t)a.s.nq + x.q0 + r, (int64_t)a.s.heads * a.s.nq)) {
+      a.lse[(int64_t)x.head * a.s.nq + x.q0 + r] = -INFINITY;
+    }
   }
   if (x.part >= 0) return;
   for (int i = lane; i < rows * (C::D / 8); i += 32) {
@@ -347,13 +352,14 @@ __global__ void __launch_bounds__(kAttnThreads, C::CTAS_PER_SM)
       const bool mine = row < q_end;
       if (__any_sync(0xffffffffu, part >= 0)) {
         const int64_t slot = (int64_t)part * kBQ + r;
-        if (mine) *reinterpret_cast<float2*>(a.part_ml + slot * 2) = make_float2(m_run, l_run);
+        const bool keep = mine && ACID_IN_BOUNDS(kSiteMha, slot, a.part_rows);
+        if (keep) *reinterpret_cast<float2*>(a.part_ml + slot * 2) = make_float2(m_run, l_run);
 #pragma unroll 1
         for (int c = 0; c < C::D; c += 32) {
           uint32_t o[32];
           tmem_ld32(o_addr + c, o);
           tmem_wait_ld();
-          if (!mine) continue;
+          if (!keep) continue;
           float* pp = a.part_o + slot * C::D + c;
 #pragma unroll
           for (int i = 0; i < 32; i += 4)
@@ -362,7 +368,7 @@ __global__ void __launch_bounds__(kAttnThreads, C::CTAS_PER_SM)
         continue;
       }
       const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
-      if (mine)
+      if (mine && ACID_IN_BOUNDS(kSiteMha, head * (int64_t)a.s.nq + row, (int64_t)a.s.heads * a.s.nq))
         a.lse[(int64_t)head * a.s.nq + row] =
             l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * 0.6931471805599453f;
       // The warp's 32 x 32 box leaves through shared memory and one TMA store where its
@@ -426,6 +432,7 @@ __global__ void __launch_bounds__(256) mha_merge_kernel(const __grid_constant__ 
   if (!mha_slot<kBQ, false>(a.s, slot, seq, index, tile) || tile * kBQ + rr >= seq.nq) return;
   const int64_t row = seq.q0 + tile * kBQ + rr;
   const float* ml = a.part_ml + ((int64_t)it * a.splits * kBQ + rr) * 2;
+  if (!ACID_IN_BOUNDS(kSiteMha, ((int64_t)it * a.splits + a.splits - 1) * kBQ + rr, a.part_rows)) return;
   float M = -INFINITY;
   for (int sp = 0; sp < a.splits; ++sp) M = fmaxf(M, ml[(int64_t)sp * kBQ * 2]);
   float acc[D / 32] = {}, L = 0.f;
@@ -443,7 +450,8 @@ __global__ void __launch_bounds__(256) mha_merge_kernel(const __grid_constant__ 
   if (!ACID_IN_BOUNDS(kSiteMha, at + D - 1, (int64_t)a.s.nq * a.ldo)) return;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) a.out[at + i * 32 + lane] = __float2bfloat16_rn(acc[i] * inv);
-  if (lane == 0) a.lse[(int64_t)head * a.s.nq + row] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+  if (lane == 0 && ACID_IN_BOUNDS(kSiteMha, head * (int64_t)a.s.nq + row, (int64_t)a.s.heads * a.s.nq))
+    a.lse[(int64_t)head * a.s.nq + row] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
 }
 
 // How a call's items go to CTAs (of `sms` SMs): whole ones, and how many shares each of
@@ -509,6 +517,7 @@ acid_status launch(const MhaArgs& x, cudaStream_t s) {
   a.units = p.full + (p.items - p.full) * p.splits;
   a.part_o = static_cast<float*>(x.part);
   a.part_ml = a.part_o + (size_t)(p.items - p.full) * p.splits * kBQ * D;
+  a.part_rows = (int64_t)(x.part_bytes / ((D + 2) * sizeof(float)));
   launch_pdl(mha_forward_kernel<C>, std::min(a.units, num_sms() * C::CTAS_PER_SM), kAttnThreads, kSmem<C>, s, tq, tk, tv,
              to, a);
   ACID_CHECK_LAUNCH();
