@@ -347,7 +347,9 @@ acid_status acid_mha_backward_workspace_size(const acid_mha* mha, size_t* bytes)
  * Matrices are 16-byte aligned, row strides multiples of 8; out overlaps nothing.
  * bf16 runs on tcgen05 (scores and sums in fp32; probabilities enter the second
  * product rounded to bf16, off by up to 2^-8 of themselves), fp32 on the FP32 pipes;
- * calls of at most four query rows for each sequence keep fp32 probabilities in both.
+ * calls of one query row for each sequence (two where key heads are shared), and of up to
+ * four against few keys (nq <= 4 sequences and nq heads head_dim nk / sequences <= 2^25),
+ * keep fp32 probabilities in both.
  *   workspace  device, 16-byte aligned.
  * The same call gives the same bits. */
 acid_status acid_mha_forward(const acid_mha* mha, const void* q, int64_t ldq, const void* k, int64_t ldk,

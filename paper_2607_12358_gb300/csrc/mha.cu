@@ -180,7 +180,7 @@ size_t stat_bytes(const acid_mha& m) { return (size_t)mha_stat_offset(m.heads, s
 size_t forward_bytes(const acid_mha& m) {
   const MhaArgs a = common_args(m);
   if (m.nq == 0) return 0;
-  if (mha_few(a.shape)) return mha_few_bytes(a);
+  if (mha_few(a)) return mha_few_bytes(a);
   return m.dtype == ACID_BF16 ? mha_forward_tc_bytes(a) : 0;
 }
 size_t backward_bytes(const acid_mha& m) {
@@ -242,7 +242,7 @@ extern "C" acid_status acid_mha_forward(const acid_mha* mha, const void* q, int6
   a.lse = lse;
   a.part = ws;
   a.part_bytes = ws_bytes;
-  if (mha_few(a.shape)) return mha_forward_few(a, (cudaStream_t)stream);
+  if (mha_few(a)) return mha_forward_few(a, (cudaStream_t)stream);
   return m.dtype == ACID_BF16 ? mha_forward_tc(a, (cudaStream_t)stream) : mha_forward_f32(a, (cudaStream_t)stream);
 }
 

@@ -193,7 +193,7 @@ struct MhaArgs {
 };
 
 // mha_few.cu: a few query rows.  Whether a call is one, and its bytes of scratch.
-bool mha_few(const MhaShape& s);
+bool mha_few(const MhaArgs& a);
 size_t mha_few_bytes(const MhaArgs& a);
 acid_status mha_forward_few(const MhaArgs& a, cudaStream_t s);
 // mha_forward.cu: bf16 on tcgen05.  Bytes of scratch (part) that the call needs.

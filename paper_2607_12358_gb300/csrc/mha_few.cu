@@ -1,6 +1,7 @@
 // Attention of a few query rows over many keys (acid_mha_forward): single tokens, or one
-// for each of many sequences.  The work is reading the keys and values once; the products
-// are too few to fill a tile of the tensor cores.
+// for each of many sequences, whose products are too few to fill a tile of the tensor
+// cores.  A query row's keys and values are read for it alone, once for up to four of the
+// query heads that share a key head.
 #include <math.h>
 
 #include <algorithm>
@@ -68,8 +69,10 @@ struct Running {
 
 // CTA (split, key head and chunk of its query heads, query row).  LANES lanes have a key
 // row, 8 columns each; a lane has the next BATCH key and value rows on their way, as they
-// are stored, while it works on the ones before.  HBM bound: 32760 keys, 12 heads of 128
-// 35 us with the join, 84% of the copy bandwidth (on the tiles of the tensor cores 50).
+// are stored, while it works on the ones before.  One query head to a key head is HBM
+// bound: 32760 keys, 12 heads of 128 35 us with the join, 84% of the copy bandwidth.  With
+// more heads or rows to a key the products set the pace, 8 columns a lane and three or four
+// shuffles a key (mha_few's table).
 template <typename T, int D, int R>
 __global__ void __launch_bounds__(32 * kWarps, 2) mha_few_kernel(const __grid_constant__ FewArgs a) {
   constexpr int LANES = D == 32 ? 4 : D == 64 ? 8 : 16, KEYS = 32 / LANES;  // keys a warp has at a time
@@ -109,9 +112,8 @@ __global__ void __launch_bounds__(32 * kWarps, 2) mha_few_kernel(const __grid_co
       const int j = j0 + b * KEYS;
       kr[b].zero();
       vr[b].zero();
-      const int64_t row = seq.k0 + (int64_t)j, at = hk * D + col + 7;
-      if (on && j < end && ACID_IN_BOUNDS(kSiteMha, row * a.ldk + at, (int64_t)a.s.nk * a.ldk) &&
-          ACID_IN_BOUNDS(kSiteMha, row * a.ldv + at, (int64_t)a.s.nk * a.ldv)) {
+      if (on && j < end && ACID_IN_BOUNDS(kSiteMha, (int64_t)(seq.k0 + j) * a.ldk + hk * D + col + 7, a.s.nk * a.ldk) &&
+          ACID_IN_BOUNDS(kSiteMha, (int64_t)(seq.k0 + j) * a.ldv + hk * D + col + 7, a.s.nk * a.ldv)) {
         kr[b].load(kp + (int64_t)j * a.ldk);
         vr[b].load(vp + (int64_t)j * a.ldv);
       }
@@ -318,9 +320,35 @@ acid_status by_heads(const MhaArgs& x, cudaStream_t s) {
 
 }  // namespace
 
-// At most four rows for each sequence: a tile of the tensor cores would be all but empty.
-bool mha_few(const MhaShape& s) {
-  return s.nk > 0 && s.nq <= 4 * (int64_t)s.seqs && s.nq <= 65535 && s.heads <= 4096;
+// Whether a call goes to this kernel.  Its time grows with the rows and heads, where a tile
+// of the tensor cores (256 rows; fp32: 16) takes the same for one as for all of its rows.
+// us here / on tiles, cold caches, replayed from a graph, which adds about 8 to both:
+//                                         1 row    2 rows     4 rows a sequence
+//   12 x 128, 512 keys                    11 / 17  11 / 18    13 / 18
+//   12 x 128, 4726 keys                   18 / 26  20 / 26    24 / 26
+//   24 x 128, 4726 keys                   24 / 30  28 / 30    36 / 30
+//   12 x 128, 32760 keys                  50 / 59  61 / 58    85 / 59
+//   24 on 8 x 128, 32760 keys             48 / 75  75 / 75   161 / 75
+//   16 on 1 x 128, 32760 keys             28 / 56  40 / 55    67 / 55
+//   30 x 64, 32760 keys                   61 / 70  72 / 70   120 / 71
+//   8 sequences, 12 x 128, 512 keys       18 / 20  18 / 20    26 / 19
+//   64 sequences, 12 x 128, 64 keys       20 / 38  26 / 38    40 / 38
+//   64 sequences, 24 on 8 x 128, 4096    274 / 505 511 / 511 971 / 519
+//   fp32, 4 x 64, 256 keys                13 / 16  13 / 16    12 / 16
+//   fp32, 12 x 128, 2048 keys             18 / 120 18 / 120   22 / 120
+//   fp32, 16 sequences, 4 x 64, 512 keys  18 / 26             18 / 26
+// One row a sequence is always faster here, two where query heads share the loads.  Else up to
+// four in bf16 as long as all rows' products with the keys are few.  Lengths are on the device,
+// so the rule goes by their averages: what it keeps from here is also a batch of 63 sequences of
+// one row and one of 190 rows against 32760 keys (3094 / 392).  fp32 products take as long on
+// tiles as here, and few rows leave most SMs without a tile.
+bool mha_few(const MhaArgs& a) {
+  const MhaShape& s = a.shape;
+  if (s.nk == 0 || s.nq > 65535 || s.heads > 4096) return false;
+  const int64_t seqs = s.seqs;
+  if (s.nq <= (s.group > 1 ? 2 : 1) * seqs) return true;
+  const int64_t products = (int64_t)s.nq * s.heads * a.head_dim * (s.nk / seqs);
+  return s.nq <= 4 * seqs && (a.dtype == ACID_FP32 || products <= 1 << 25);
 }
 
 size_t mha_few_bytes(const MhaArgs& x) {

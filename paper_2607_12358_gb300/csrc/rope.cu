@@ -166,8 +166,8 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
       to[k] = row * a.ldo + c;
       // (in place the columns and rows that are not turned are left alone)
       if (!a.copy_first && !(turned && row >= a.first)) rows[k] = -1;
-      const int end = HALVES && turned ? a.pairs + 7 : 7;
-      if (!ACID_IN_BOUNDS(kSiteRope, from[k] + end, a.rows * a.ldx) || !ACID_IN_BOUNDS(kSiteRope, to[k] + end, a.rows * a.ldo))
+      if (!ACID_IN_BOUNDS(kSiteRope, from[k] + (HALVES && turned ? a.pairs : 0) + 7, a.rows * a.ldx) ||
+          !ACID_IN_BOUNDS(kSiteRope, to[k] + (HALVES && turned ? a.pairs : 0) + 7, a.rows * a.ldo))
         rows[k] = -1;
       if (rows[k] >= 0) p[k].load(static_cast<const T*>(a.x) + from[k], a.pairs, turned);
     }
