@@ -271,7 +271,8 @@ acid_status acid_layernorm_mod(int32_t x_dtype, const void* x, int32_t y_dtype, 
  * each other; with R columns turned in all, pair p is columns (2p, 2p + 1), or
  * (p, p + R/2) with `halves`; columns from R on pass through.  (x1, x2) becomes
  * (x1 cos - x2 sin, x1 sin + x2 cos), formed in fp32 and rounded once; the angle is
- * right to 2^-22 of a turn at any position below 2^24.  acid_dit_block_forward
+ * right to 2^-22 of a turn at any fp32 position below 2^24 (theta below 1: below 2^24
+ * theta, since pairs then turn by up to 1 / theta radians a place).  acid_dit_block_forward
  * rotates inside its QKV projection; these calls serve callers composing their own
  * blocks, other position schemes, and gradients. */
 typedef struct {
@@ -287,7 +288,7 @@ typedef struct {
   int64_t ld_pos;
   int32_t grid[4];           /* places along each axis: row first_rows + n is place n (row-major, the last axis
                                 fastest) of the grid, which repeats (a batch of clips) */
-  float origin[4];           /* added to the grid's positions (a later chunk of a clip) */
+  float origin[4];           /* added to the grid's positions, in fp32 (a later chunk of a clip) */
 } acid_rope;
 
 /* out = the rotation of x, both device [rows, heads * head_dim] with row strides
@@ -310,7 +311,8 @@ acid_status acid_rope_backward(const acid_rope* rope, const void* dout, int64_t 
  * around the caches need beside acid_attention_forward.  Query head h reads key
  * head h / (heads / kv_heads).
  * Sequences: rows [first, end) of the queries attend to rows [first, end) of the
- * keys.  Bounds lie in order and do not overlap (gaps are padding); one sequence
+ * keys.  Bounds lie in order, an empty sequence's too: none begins before the end of
+ * the one before it (gaps are padding).  One sequence
  * without bounds has all rows.  Rows of no sequence are neither used (they may hold
  * anything) nor written.  A bound outside the operand is cut to it.
  * Frames: frame_rows > 0 makes frames of so many rows of each sequence.  Query row i

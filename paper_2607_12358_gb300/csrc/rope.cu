@@ -37,8 +37,9 @@ struct Rope {
 
 // Angle of pair p at a position, as a fraction of half a turn.  pos hi is split
 // into the product and its rounding error (one FMA each), so the whole turns drop
-// out exactly and the angle is right to 2^-23 of a turn at any position up to 2^24;
-// in fp32 radians the rounding of the angle itself is 2^-24 of it: 0.01 rad at 2e5.
+// out exactly and the angle is right to 2^-23 of a turn at any position up to 2^24 (of
+// pairs that turn by up to a radian a place; by f radians: up to 2^24 / f, from where on
+// the rounding error is itself whole turns and more); in fp32 radians the rounding of the angle itself is 2^-24 of it: 0.01 rad at 2e5.
 __device__ __forceinline__ float half_turns(float pos, float hi, float lo) {
   const float t = pos * hi, e = fmaf(pos, hi, -t);
   return 2.0f * ((t - rintf(t)) + fmaf(pos, lo, e));
