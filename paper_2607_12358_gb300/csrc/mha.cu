@@ -29,8 +29,9 @@ struct StatArgs {
 
 // -lse and -sum(dout out) of a slot's rows for one head (mha_stat_offset).  A row is
 // `lanes` lanes of 8 columns.  It reads out and dout once: 202 MB (32760 rows, 12 x 128) in
-// 37.6 us, 79% of the copy bandwidth, issue 60%.  (8190 rows, 24 x 128: 23.9 us, eight rows
-// ahead 30.5, two 23.8, heads side by side 23.6, six CTAs an SM, which spill, 28.7.)
+// 37.6 us, 79% of the copy bandwidth, issue 60%; 39 in a call, 44 with L2 full of lines that
+// have to be written back first.  (8190 rows, 24 x 128, L2 full of such lines: 23.9 us, eight
+// rows ahead 30.5, two 23.8, heads side by side 23.6, six CTAs an SM, which spill, 28.7.)
 template <typename T>
 __global__ void __launch_bounds__(kThreads) mha_stats_kernel(const StatArgs a, int lanes) {
   pdl_wait();
